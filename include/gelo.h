@@ -257,6 +257,94 @@ gelo_status gelo_qkv_forward_static(gelo_ctx* ctx, gelo_kind kind, gelo_dtype dt
                                     int d, int p, const void* H, const void* W, float shield_scale,
                                     gelo_norm_stat stat, uint64_t batch_id, void* Z, void* U, void* Y, void* stream);
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * What the trusted side does itself between two obfuscated projections: the hidden states H of the next batch from the
+ * residual stream, queries and keys rotated by their positions and kept in a paged cache, and the attention that
+ * reads the cache.  All calls are asynchronous on `stream`; device arrays are read when the kernels run.
+ *
+ * gelo_kv_cache: K and V are arrays of n_pages pages; row r of head h of page g starts at element
+ * g page_stride + h head_stride + r row_stride of either (the same strides for both, multiples of 8, head_dim
+ * contiguous values at each).  page_rows is a power of two from 16 on.  k and v are 16-byte aligned DEVICE pointers.
+ * gelo_seq_batch: sequence s brings the rows [row_start[s], row_start[s + 1]) of the batch and has kv_len[s] rows in the
+ * cache; row p of it lies in page page_table[s table_ld + p / page_rows], row p % page_rows.  row_start
+ * (n_seqs + 1 ascending values from 0 to n_rows) may be NULL if every sequence brings one row (n_rows = n_seqs,
+ * max_rows = 1).  All three are DEVICE arrays of 32-bit integers.  max_rows and max_kv_len bound the rows a sequence brings
+ * and its kv_len, on the HOST: launches and workspaces are sized by them, so a captured launch serves all batches within its
+ * bounds.  Entries of page_table behind the last used page are not read.
+ * The structures are read during the call only. */
+typedef struct gelo_kv_cache {
+    void* k;
+    void* v;
+    int n_pages, n_kv_heads, page_rows, head_dim;
+    int64_t page_stride, head_stride, row_stride;
+} gelo_kv_cache;
+
+typedef struct gelo_seq_batch {
+    int n_seqs, n_rows, max_rows, max_kv_len;
+    const int32_t* row_start;
+    const int32_t* kv_len;
+    const int32_t* page_table;
+    int64_t table_ld;
+} gelo_seq_batch;
+
+/* Which components of a head turn together: i and i + rot_dim / 2, or 2 i and 2 i + 1. */
+typedef enum { GELO_ROPE_HALF = 0, GELO_ROPE_PAIRS = 1 } gelo_rope_layout;
+
+#define GELO_NORM_MAX_D 65536  /* widest row gelo_rms_norm takes */
+
+/* Root-mean-square norm of the rows of h = X + R (R may be NULL: h = X):
+ *   R_out = h,   y = h / sqrt(mean_j h_j^2 + eps) * gamma,   H = y,   codes = e4m3(y * 448 / max_j |y_j|), scales = max_j |y_j| / 448.
+ * X, R, R_out, H: n x d of type `dtype` (ldx, ldr, ldro, ldh); gamma: d values of it.  R_out may be NULL or R itself; H (or codes and
+ * scales) may be NULL, not both.  H may be X or R.  Everything is computed in float from the unrounded h and rounded once.  codes: n x d bytes
+ * (ldq, a multiple of 8), the row quantisation of gelo_project_fp8, scales: n floats (1 for a row of zeros): together the operand of
+ * gelo_project_fp8_codes, which wants ldq to be a multiple of 16.  A NaN or infinity in a row makes the row's y NaN or zero as the formula does; a NaN among them gives the
+ * code 0x7F and the scale NaN.  d <= GELO_NORM_MAX_D, eps >= 0. */
+gelo_status gelo_rms_norm(gelo_ctx* ctx, gelo_dtype dtype, int n, int d, const void* X, int64_t ldx, const void* R, int64_t ldr,
+                          const void* gamma, float eps, void* R_out, int64_t ldro, void* H, int64_t ldh,
+                          uint8_t* codes, int64_t ldq, float* scales, void* stream);
+
+/* gelo_project_fp8 whose left operand is 8-bit codes with row scales already (as gelo_rms_norm writes them): n x d bytes,
+ * ldq a multiple of 16 bytes, n floats.  d a multiple of 128. */
+gelo_status gelo_project_fp8_codes(gelo_ctx* ctx, int n, int d, int p, const uint8_t* codes, int64_t ldq, const float* scales,
+                                   const void* Wq, void* Y, int64_t ldy, void* stream);
+
+/* Fills the table of gelo_rope_append: table[(p - first_pos) rot_dim + 2 i] = cos(p w_i), the next float sin(p w_i), for
+ * positions p = first_pos ... first_pos + n_pos - 1 and i < rot_dim / 2, from angles in double.  w_i = base^(-2 i / rot_dim),
+ * stretched for contexts longer than the trained one by `factor` (1: not at all): with lambda_i = 2 pi / w_i and
+ * t_i = (trained / lambda_i - low) / (high - low) cut to [0, 1], w_i becomes w_i (t_i + (1 - t_i) / factor) - waves that turn more than `high` times
+ * over the trained length stay, those of less than `low` turns are stretched in full.  trained = 0: all are stretched in full
+ * (linear interpolation of positions; low and high are ignored).  rot_dim a multiple of 16, table 16-byte aligned. */
+gelo_status gelo_rope_table(gelo_ctx* ctx, int rot_dim, int first_pos, int n_pos, double base, double factor, double trained,
+                            double low, double high, float* table, void* stream);
+
+/* Rotates the queries and keys of the batch's rows by their positions and appends keys and values to the cache.  QKV: n_rows x
+ * (n_q_heads + 2 n_kv_heads) head_dim of type `dtype` (ld), the fused Q | K | V that gelo_unmix writes as Z.  Row j of sequence s, which
+ * brings n of them, has position p = kv_len[s] - n + j (kv_len counts the new rows).  The first rot_dim components
+ * of every query and key head turn by the angles of `table` (row p, as gelo_rope_table writes it; positions from 0, n_table of them, at
+ * least max_kv_len); the rest and the values are copied.  Q: n_rows x n_q_heads head_dim (ldq) takes the queries; it may be QKV itself
+ * (ldq = ld: in place).  n_q_heads = 0 (Q NULL): keys and values only, as for an encoder's states.  rot_dim = 0 (table NULL): nothing
+ * turns.  A row of negative position gives zero queries and is not appended; one at or beyond max_kv_len gives NaN queries and is not
+ * appended; one whose page number lies outside the cache is not appended.  rot_dim a multiple of 16 up to head_dim, head_dim a multiple of 8. */
+gelo_status gelo_rope_append(gelo_ctx* ctx, gelo_dtype dtype, int n_q_heads, const void* QKV, int64_t ld, const gelo_kv_cache* cache,
+                             const gelo_seq_batch* batch, gelo_rope_layout layout, int rot_dim, const float* table, int n_table,
+                             void* Q, int64_t ldq, void* stream);
+
+/* Attention over the cache: O[row, h] = sum_p softmax_p(scale Q[row, h] . K[p, h']) V[p, h'], h' = h n_kv_heads / n_q_heads
+ * (n_q_heads a multiple of n_kv_heads).  causal != 0: row j of the n that sequence s brings sees the rows p <= kv_len[s] - n + j of
+ * the cache (its own last; kv_len counts the new rows, which are in the cache already); causal = 0: all p < kv_len[s] (cross
+ * attention to states of another length).  A row that sees nothing gives zeros.  Q, O: n_rows x n_q_heads head_dim of type
+ * `dtype` (ldq, ldo), O not in Q's memory; head_dim 64, 96, 128 or 256.  Rows outside [row_start[0], row_start[n_seqs]) are left as
+ * they are.  kv_len beyond max_kv_len is cut to it; a page number outside the cache is not followed: the
+ * results of its sequence are then NaN or partly so.  Statistics, products and sums are float; GELO_BF16 rounds the weights exp(s - max) to bfloat16 for the product with V, their sum does
+ * not.  What lies in cache rows that no query of the batch sees does not reach the result, NaN and infinity included.
+ * Where the rows and heads are too few to fill the chip the cache's length is cut over workgroups and their parts are joined through float
+ * workspace of the context (gelo_reserve_attention sizes it ahead; else the first call that needs more allocates): calls on one context must not
+ * overlap in time on different streams. */
+gelo_status gelo_attention(gelo_ctx* ctx, gelo_dtype dtype, int n_q_heads, const void* Q, int64_t ldq, const gelo_kv_cache* cache,
+                           const gelo_seq_batch* batch, float scale, int causal, void* O, int64_t ldo, void* stream);
+/* Allocates that workspace (as much as any batch of heads of this width needs): gelo_attention then allocates nothing. */
+gelo_status gelo_reserve_attention(gelo_ctx* ctx, int head_dim);
+
 /* Test hook: copies the secrets of a mixing object to caller DEVICE buffers (any may be NULL):
  * A and A_inv as float n x n (dense), S as float k_shield x d (dense; valid after gelo_mix).
  * attempt / kappa are HOST pointers: the accepted attempt number and the library's estimate of

@@ -14,6 +14,7 @@ import torch
 GELO_F32, GELO_BF16 = 0, 1
 GELO_ORTHOGONAL, GELO_GAUSSIAN, GELO_CONDITIONED, GELO_STRUCTURED, GELO_BLOCK_ORTHOGONAL, GELO_REFLECTOR_PRODUCT = 0, 1, 2, 3, 4, 5
 GELO_NORM_MEDIAN, GELO_NORM_MEAN = 0, 1
+GELO_ROPE_HALF, GELO_ROPE_PAIRS = 0, 1
 GELO_OK = 0
 STATUS_NAMES = ["GELO_OK", "GELO_EINVAL", "GELO_ESHAPE", "GELO_EDTYPE", "GELO_EALIGN", "GELO_ENOMEM",
                 "GELO_ECOND", "GELO_ESINGULAR", "GELO_EREUSE", "GELO_ESTATE", "GELO_EHIP"]
@@ -22,8 +23,20 @@ GELO_BATCH_WINDOW = 4096
 GELO_STATIC_MAX_N = 128
 GELO_MAX_BATCH_DRAW = 48
 GELO_STATIC_SCRATCH_BYTES = 16 << 20
+GELO_NORM_MAX_D = 65536
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libgelo.so")
+
+
+class _KvCacheStruct(ctypes.Structure):
+    _fields_ = [("k", c_void_p), ("v", c_void_p), ("n_pages", c_int), ("n_kv_heads", c_int), ("page_rows", c_int), ("head_dim", c_int),
+                ("page_stride", c_int64), ("head_stride", c_int64), ("row_stride", c_int64)]
+
+
+class _SeqBatchStruct(ctypes.Structure):
+    _fields_ = [("n_seqs", c_int), ("n_rows", c_int), ("max_rows", c_int), ("max_kv_len", c_int),
+                ("row_start", c_void_p), ("kv_len", c_void_p), ("page_table", c_void_p), ("table_ld", c_int64)]
+
 
 # name -> (restype, argtypes); mirrors include/gelo.h one to one
 SIGNATURES = {
@@ -53,6 +66,15 @@ SIGNATURES = {
     "gelo_project_fp8": (c_int, [c_void_p, c_int, c_int, c_int, c_void_p, c_int64, c_void_p, c_void_p, c_int64, c_void_p]),
     "gelo_debug_quantize_rows_fp8": (c_int, [c_void_p, c_int, c_int, c_void_p, c_int64, c_void_p, c_void_p, c_void_p]),
     "gelo_measure_matrix_rate": (c_int, [c_void_p, c_int, c_int, c_int, POINTER(c_double), POINTER(c_double), c_void_p]),
+    "gelo_rms_norm": (c_int, [c_void_p, c_int, c_int, c_int, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_float, c_void_p, c_int64,
+                              c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p]),
+    "gelo_project_fp8_codes": (c_int, [c_void_p, c_int, c_int, c_int, c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_int64, c_void_p]),
+    "gelo_rope_table": (c_int, [c_void_p, c_int, c_int, c_int, c_double, c_double, c_double, c_double, c_double, c_void_p, c_void_p]),
+    "gelo_rope_append": (c_int, [c_void_p, c_int, c_int, c_void_p, c_int64, POINTER(_KvCacheStruct), POINTER(_SeqBatchStruct), c_int, c_int,
+                                 c_void_p, c_int, c_void_p, c_int64, c_void_p]),
+    "gelo_attention": (c_int, [c_void_p, c_int, c_int, c_void_p, c_int64, POINTER(_KvCacheStruct), POINTER(_SeqBatchStruct), c_float, c_int,
+                               c_void_p, c_int64, c_void_p]),
+    "gelo_reserve_attention": (c_int, [c_void_p, c_int]),
     "gelo_debug_philox_words": (c_int, [c_void_p, c_uint32, c_uint32, c_uint64, c_uint32, c_uint32, c_void_p, c_void_p]),
     "gelo_mixing_export_table": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p]),
     "gelo_qkv_forward": (c_int, [c_void_p, c_int, c_int, c_int, c_int, c_int, c_int, c_void_p, c_void_p, c_float,
@@ -301,6 +323,150 @@ def gelo_project_fp8(ctx, U: torch.Tensor, Wq: torch.Tensor, p: int, Y: torch.Te
         raise GeloError(2, "Wq is not the prepared form of a d x p weight")
     _check(ctx, load_library().gelo_project_fp8(ctx, n, d, p, up, ldu, c_void_p(Wq.data_ptr()), yp, ldy, _stream(stream)))
     return Y
+
+
+def gelo_project_fp8_codes(ctx, codes: torch.Tensor, scales: torch.Tensor, Wq: torch.Tensor, p: int, Y: torch.Tensor, stream=None) -> torch.Tensor:
+    """The 8-bit projection of rows that are codes with scales already (gelo_rms_norm writes them)."""
+    cp, ldq = _matrix(codes, "codes")
+    yp, ldy = _matrix(Y, "Y")
+    n, d = codes.shape
+    if codes.dtype != torch.uint8 or Y.dtype != torch.bfloat16 or tuple(Y.shape) != (n, p):
+        raise ValueError("codes must be uint8, Y bf16 and n x p")
+    _vector(scales, "scales", torch.float32, n)
+    if Wq.dtype != torch.uint8 or Wq.numel() != gelo_fp8_weight_bytes(d, p):
+        raise GeloError(2, "Wq is not the prepared form of a d x p weight")
+    _check(ctx, load_library().gelo_project_fp8_codes(ctx, n, d, p, cp, ldq, scales.data_ptr(), Wq.data_ptr(), yp, ldy, _stream(stream)))
+    return Y
+
+
+class KvCache:
+    """A paged cache: K and V of shape (pages, key heads, rows of a page, width of a head) in any order of memory (permuted views) as
+    long as a head's row is contiguous and both have the same strides.  Describes the tensors and keeps them alive."""
+
+    def __init__(self, K: torch.Tensor, V: torch.Tensor):
+        if K.dim() != 4 or K.shape != V.shape or K.dtype != V.dtype:
+            raise ValueError("K and V must be of one type and shape: pages, key heads, rows of a page, width of a head")
+        if not K.is_cuda or not V.is_cuda or K.device != V.device:
+            raise ValueError("K and V must live on one GPU")
+        # (the stride of a dimension of one entry says nothing)
+        strides, other = ([x.stride(i) if x.shape[i] > 1 else K.shape[3] for i in range(3)] for x in (K, V))
+        if strides != other or (K.shape[3] > 1 and (K.stride(3) != 1 or V.stride(3) != 1)):
+            raise ValueError("K and V must have the same strides, the last of them 1")
+        self.K, self.V, self.dtype = K, V, _dtype_code(K)
+        n_pages, n_kv_heads, page_rows, head_dim = K.shape
+        self.n_kv_heads, self.head_dim = n_kv_heads, head_dim
+        self.struct = _KvCacheStruct(K.data_ptr(), V.data_ptr(), n_pages, n_kv_heads, page_rows, head_dim, *strides)
+
+
+class SeqBatch:
+    """Which rows of a batch and which pages of a cache belong to which sequence (see gelo_seq_batch in include/gelo.h): kv_len
+    (n_seqs), page_table (n_seqs x pages) and row_start (n_seqs + 1, or None: one row each) are int32 tensors on the GPU, read when the
+    kernels run."""
+
+    def __init__(self, kv_len: torch.Tensor, page_table: torch.Tensor, max_kv_len: int, row_start: torch.Tensor | None = None, max_rows: int = 1):
+        n_seqs = kv_len.shape[0] if kv_len.dim() == 1 else 0
+        _vector(kv_len, "kv_len", torch.int32, n_seqs)
+        if row_start is not None:
+            _vector(row_start, "row_start", torch.int32, n_seqs + 1)
+        if page_table.dtype != torch.int32 or page_table.dim() != 2 or page_table.shape[0] != n_seqs:
+            raise ValueError("page_table must be an int32 tensor with a row per sequence")
+        tp, table_ld = _matrix(page_table, "page_table")
+        if n_seqs == 1 or table_ld < page_table.shape[1]:
+            table_ld = page_table.shape[1]
+        self.kv_len, self.page_table, self.row_start = kv_len, page_table, row_start
+        self.n_seqs, self.pages = n_seqs, page_table.shape[1]
+        self.struct = _SeqBatchStruct(n_seqs, n_seqs, max_rows, max_kv_len, None if row_start is None else row_start.data_ptr(), kv_len.data_ptr(), tp, table_ld)
+
+
+def _vector(t: torch.Tensor, name: str, dtype, count: int):
+    if not t.is_cuda or t.dtype != dtype or t.dim() != 1 or t.shape[0] != count or (count > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name} must be a contiguous GPU vector of {count} {dtype}")
+
+
+def _rows(batch: SeqBatch, rows: int, cache: KvCache):
+    """The batch's description for matrices of `rows` rows."""
+    s = batch.struct
+    if batch.row_start is None and rows != batch.n_seqs:
+        raise GeloError(2, f"{rows} rows, but every one of {batch.n_seqs} sequences brings one")
+    if batch.pages * cache.struct.page_rows < s.max_kv_len:
+        raise GeloError(2, f"max_kv_len={s.max_kv_len} rows do not fit {batch.pages} pages of {cache.struct.page_rows}")
+    s.n_rows = rows
+    return byref(s)
+
+
+def gelo_rms_norm(ctx, X: torch.Tensor, gamma: torch.Tensor, eps: float, H: torch.Tensor | None = None, residual: torch.Tensor | None = None,
+                  residual_out: torch.Tensor | None = None, codes: torch.Tensor | None = None, scales: torch.Tensor | None = None, stream=None):
+    """h = X + residual into residual_out, h / rms(h) * gamma into H and, as 8-bit codes with row scales, into codes and scales."""
+    n, d = X.shape
+    code = _dtype_code(X)
+    args = []
+    for name, t in (("X", X), ("residual", residual), ("residual_out", residual_out), ("H", H)):
+        if t is None:
+            args += (None, 0)
+            continue
+        if t.dtype != X.dtype or tuple(t.shape) != (n, d):
+            raise ValueError(f"{name} must be of X's dtype and shape")
+        args += _matrix(t, name)
+    _vector(gamma, "gamma", X.dtype, d)
+    cp, ldq = None, 0
+    if codes is not None or scales is not None:
+        if codes is None or scales is None or codes.dtype != torch.uint8 or tuple(codes.shape) != (n, d):
+            raise ValueError("codes must be uint8 of X's shape and come with scales")
+        cp, ldq = _matrix(codes, "codes")
+        _vector(scales, "scales", torch.float32, n)
+    xp, ldx, rp, ldr, op, ldo, hp, ldh = args
+    _check(ctx, load_library().gelo_rms_norm(ctx, code, n, d, xp, ldx, rp, ldr, gamma.data_ptr(), eps, op, ldo, hp, ldh, cp, ldq,
+                                             None if scales is None else scales.data_ptr(), _stream(stream)))
+
+
+def gelo_rope_table(ctx, rot_dim: int, n_pos: int, base: float = 10000.0, factor: float = 1.0, trained: float = 0.0, low: float = 1.0,
+                    high: float = 4.0, first_pos: int = 0, stream=None) -> torch.Tensor:
+    """(n_pos x rot_dim / 2 x 2) float32 cosines and sines for gelo_rope_append."""
+    table = torch.empty((n_pos, rot_dim // 2, 2), dtype=torch.float32, device="cuda")
+    _check(ctx, load_library().gelo_rope_table(ctx, rot_dim, first_pos, n_pos, base, factor, trained, low, high, table.data_ptr(), _stream(stream)))
+    return table
+
+
+def gelo_rope_append(ctx, QKV: torch.Tensor, n_q_heads: int, cache: KvCache, batch: SeqBatch, Q: torch.Tensor | None = None,
+                     table: torch.Tensor | None = None, rot_dim: int = 0, layout: int = GELO_ROPE_HALF, stream=None):
+    """Rotates the queries and keys of QKV's rows by their positions; queries into Q, keys and values into the cache."""
+    zp, ld = _matrix(QKV, "QKV")
+    rows, width = QKV.shape
+    if _dtype_code(QKV) != cache.dtype:
+        raise GeloError(3, "QKV and the cache differ in type")
+    if width != (n_q_heads + 2 * cache.n_kv_heads) * cache.head_dim:
+        raise GeloError(2, f"a row of {width} values is not {n_q_heads} + 2 x {cache.n_kv_heads} heads of {cache.head_dim}")
+    qp, ldq = None, 0
+    if Q is not None:
+        if Q.dtype != QKV.dtype or Q.dim() != 2 or tuple(Q.shape) != (rows, n_q_heads * cache.head_dim):
+            raise ValueError("Q must be of QKV's dtype, a row of all query heads for each of its rows")
+        qp, ldq = _matrix(Q, "Q")
+    tp, n_table = None, 0
+    if table is not None:
+        if table.dtype != torch.float32 or not table.is_cuda or not table.is_contiguous() or table.numel() != table.shape[0] * rot_dim:
+            raise ValueError("table must be a contiguous float32 GPU tensor of positions x rot_dim")
+        tp, n_table = table.data_ptr(), table.shape[0]
+    _check(ctx, load_library().gelo_rope_append(ctx, cache.dtype, n_q_heads, zp, ld, byref(cache.struct), _rows(batch, rows, cache), layout, rot_dim,
+                                                tp, n_table, qp, ldq, _stream(stream)))
+
+
+def gelo_attention(ctx, Q: torch.Tensor, O: torch.Tensor, n_q_heads: int, cache: KvCache, batch: SeqBatch, scale: float, causal: bool = True,
+                   stream=None) -> torch.Tensor:
+    """softmax(scale Q K^T) V over the rows of the cache that each row of Q sees, into O."""
+    qp, ldq = _matrix(Q, "Q")
+    op, ldo = _matrix(O, "O")
+    rows, width = Q.shape
+    if _dtype_code(Q) != cache.dtype or O.dtype != Q.dtype:
+        raise GeloError(3, "Q, O and the cache differ in type")
+    if width != n_q_heads * cache.head_dim or O.shape != Q.shape:
+        raise GeloError(2, f"Q and O must have {n_q_heads} heads of {cache.head_dim} values in a row")
+    _check(ctx, load_library().gelo_attention(ctx, cache.dtype, n_q_heads, qp, ldq, byref(cache.struct), _rows(batch, rows, cache), scale,
+                                              1 if causal else 0, op, ldo, _stream(stream)))
+    return O
+
+
+def gelo_reserve_attention(ctx, head_dim: int) -> None:
+    _check(ctx, load_library().gelo_reserve_attention(ctx, head_dim))
 
 
 def gelo_debug_quantize_rows_fp8(ctx, U: torch.Tensor, stream=None):

@@ -100,6 +100,7 @@ struct gelo_ctx {
     size_t factor_ws_refused;          // the smallest size of it for several matrices that the device did not have
     void* chain_ws;  size_t chain_ws_bytes;
     void* quant_ws;  size_t quant_ws_bytes;    // FP8 projection: codes and row scales of the current U
+    void* attention_ws; size_t attention_ws_bytes; // parts of a cut cache
     void* project_ws; size_t project_ws_bytes; // bf16 projection of at most 128 rows: float partial sums of the K slices
     float* host_scalars;         // pinned: kappa read-back, one slot per lane
     int* host_flag;
@@ -379,7 +380,7 @@ static hipError_t kernels_init(int device) {
     static std::atomic<bool> done[kStaticMaxDevices];       // (two threads at once both do it: the calls may be repeated)
     if (device < kStaticMaxDevices && done[device].load(std::memory_order_acquire)) return hipSuccess;
     hipError_t (*const inits[])() = {gemm_bf16_init, gemm_f32_init, inverse_init, structured_init, small_init, gemm_fp8_init,
-                                     factor_init, block_reflect_init, block_factor_init, sampler_init};
+                                     factor_init, block_reflect_init, block_factor_init, sampler_init, attention_init};
     for (auto init : inits) {
         const hipError_t e = init();
         if (e != hipSuccess) return e;
@@ -411,6 +412,7 @@ gelo_status gelo_create(gelo_ctx** out, int device, uint64_t seed, int allow_bat
     ctx->factor_ws_refused = SIZE_MAX;
     ctx->quant_ws = nullptr; ctx->quant_ws_bytes = 0;
     ctx->project_ws = nullptr; ctx->project_ws_bytes = 0;
+    ctx->attention_ws = nullptr; ctx->attention_ws_bytes = 0;
     ctx->host_scalars = nullptr; ctx->host_flag = nullptr;
     ctx->lanes_ready = false; ctx->join_pending = false; ctx->cand = nullptr; ctx->cand_bytes = 0;
     for (int i = 0; i < kLanes; ++i) ctx->lane_graph_ok[i] = false;
@@ -445,6 +447,7 @@ gelo_status gelo_destroy(gelo_ctx* ctx) {
     if (ctx->chain_ws) (void)hipFree(ctx->chain_ws);
     if (ctx->quant_ws) (void)hipFree(ctx->quant_ws);
     if (ctx->project_ws) (void)hipFree(ctx->project_ws);
+    if (ctx->attention_ws) (void)hipFree(ctx->attention_ws);
     if (ctx->host_scalars) (void)hipHostFree(ctx->host_scalars);
     delete ctx;
     return GELO_OK;
@@ -1316,6 +1319,14 @@ static gelo_status check_fp8_shape(gelo_ctx* ctx, int d, int p) {
     return GELO_OK;
 }
 
+static gelo_status check_codes(gelo_ctx* ctx, const uint8_t* codes, int64_t ldq, const float* scales, int d, int multiple) {
+    if (!codes || !scales) return fail(ctx, GELO_EINVAL, "codes and scales must not be NULL");
+    if (!aligned16(codes) || (reinterpret_cast<uintptr_t>(scales) & 3u)) return fail(ctx, GELO_EALIGN, "codes must be 16-byte aligned, scales 4-byte");
+    if (ldq < d) return fail(ctx, GELO_EINVAL, "leading dimension of codes (%lld) is below its width (%d)", (long long)ldq, d);
+    if (ldq % multiple != 0) return fail(ctx, GELO_EALIGN, "leading dimension of codes (%lld) is not a multiple of %d", (long long)ldq, multiple);
+    return GELO_OK;
+}
+
 gelo_status gelo_prepare_weight_fp8(gelo_ctx* ctx, int d, int p, const void* W, int64_t ldw, void* Wq, void* stream) {
     if (!ctx) return GELO_EINVAL;
     gelo_status st = check_fp8_shape(ctx, d, p);
@@ -1349,6 +1360,22 @@ gelo_status gelo_project_fp8(gelo_ctx* ctx, int n, int d, int p, const void* U, 
     const float* wscale = (const float*)(wcodes + up256((size_t)p * d));
     GELO_HIP(ctx, quantize_rows_e4m3(U, ldu, n, d, ucodes, d, uscale, s));
     GELO_HIP(ctx, gemm_fp8(ucodes, d, uscale, wcodes, d, wscale, Y, ldy, n, p, d, s));
+    return GELO_OK;
+}
+
+gelo_status gelo_project_fp8_codes(gelo_ctx* ctx, int n, int d, int p, const uint8_t* codes, int64_t ldq, const float* scales,
+                                   const void* Wq, void* Y, int64_t ldy, void* stream) {
+    if (!ctx) return GELO_EINVAL;
+    if (n < 1) return fail(ctx, GELO_EINVAL, "n=%d", n);
+    gelo_status st = check_fp8_shape(ctx, d, p);
+    if (st == GELO_OK) st = check_codes(ctx, codes, ldq, scales, d, 16);
+    if (st == GELO_OK) st = check_matrix(ctx, "Y", Y, ldy, p);
+    if (st != GELO_OK) return st;
+    if (!Wq || !aligned16(Wq)) return fail(ctx, Wq ? GELO_EALIGN : GELO_EINVAL, "Wq must be a 16-byte aligned device buffer");
+    GELO_HIP(ctx, hipSetDevice(ctx->device));
+    const uint8_t* wcodes = (const uint8_t*)Wq;
+    const float* wscale = (const float*)(wcodes + up256((size_t)p * d));
+    GELO_HIP(ctx, gemm_fp8(codes, ldq, scales, wcodes, d, wscale, Y, ldy, n, p, d, (hipStream_t)stream));
     return GELO_OK;
 }
 
@@ -1389,6 +1416,143 @@ gelo_status gelo_measure_matrix_rate(gelo_ctx* ctx, int fp8, int iters, int laun
     *seconds = (double)ms * 1e-3 / launches;
     *flop = f;
     return GELO_OK;
+}
+
+// ------------------------------------------------------------------ between two projections --
+static constexpr int kMostRows = 1 << 22;      // a workgroup of up to 1024 threads each: HIP counts a launch's threads in 32 bits
+
+gelo_status gelo_rms_norm(gelo_ctx* ctx, gelo_dtype dtype, int n, int d, const void* X, int64_t ldx, const void* R, int64_t ldr,
+                          const void* gamma, float eps, void* R_out, int64_t ldro, void* H, int64_t ldh,
+                          uint8_t* codes, int64_t ldq, float* scales, void* stream) {
+    if (!ctx) return GELO_EINVAL;
+    if (dtype != GELO_F32 && dtype != GELO_BF16) return fail(ctx, GELO_EINVAL, "unknown dtype %d", (int)dtype);
+    if (n < 1 || d < 1) return fail(ctx, GELO_EINVAL, "n=%d d=%d", n, d);
+    if (d % 8 != 0) return fail(ctx, GELO_EALIGN, "d=%d is not a multiple of 8", d);
+    if (n > kMostRows) return fail(ctx, GELO_ESHAPE, "n=%d exceeds %d rows", n, kMostRows);
+    if (d > GELO_NORM_MAX_D) return fail(ctx, GELO_ESHAPE, "d=%d exceeds GELO_NORM_MAX_D = %d", d, GELO_NORM_MAX_D);
+    if (!(eps >= 0.f) || std::isinf(eps)) return fail(ctx, GELO_EINVAL, "eps=%g must be finite and not negative", (double)eps);
+    if (!gamma || !aligned16(gamma)) return fail(ctx, gamma ? GELO_EALIGN : GELO_EINVAL, "gamma must be a 16-byte aligned device vector");
+    if (!H && !codes && !scales) return fail(ctx, GELO_EINVAL, "H and codes are both NULL: nothing to write");
+    gelo_status st = check_matrix(ctx, "X", X, ldx, d);
+    if (st == GELO_OK && R) st = check_matrix(ctx, "R", R, ldr, d);
+    if (st == GELO_OK && R_out) st = check_matrix(ctx, "R_out", R_out, ldro, d);
+    if (st == GELO_OK && H) st = check_matrix(ctx, "H", H, ldh, d);
+    if (st == GELO_OK && (codes || scales)) st = check_codes(ctx, codes, ldq, scales, d, 8);
+    if (st != GELO_OK) return st;
+    GELO_HIP(ctx, hipSetDevice(ctx->device));
+    RmsNorm o;
+    o.X = X; o.ldx = ldx; o.R = R; o.ldr = ldr; o.gamma = gamma; o.R_out = R_out; o.ldro = ldro; o.H = H; o.ldh = ldh;
+    o.codes = codes; o.ldq = ldq; o.scales = scales; o.eps = eps; o.n = n; o.d = d;
+    GELO_HIP(ctx, rms_norm(o, dtype == GELO_BF16, (hipStream_t)stream));
+    return GELO_OK;
+}
+
+gelo_status gelo_rope_table(gelo_ctx* ctx, int rot_dim, int first_pos, int n_pos, double base, double factor, double trained,
+                            double low, double high, float* table, void* stream) {
+    if (!ctx) return GELO_EINVAL;
+    if (rot_dim < 16 || rot_dim % 16 != 0) return fail(ctx, GELO_EINVAL, "rot_dim=%d must be a positive multiple of 16", rot_dim);
+    if (first_pos < 0 || n_pos < 1 || first_pos > INT32_MAX - n_pos) return fail(ctx, GELO_EINVAL, "first_pos=%d n_pos=%d", first_pos, n_pos);
+    if (!(base > 0.0) || std::isinf(base) || !(factor > 0.0) || std::isinf(factor)) return fail(ctx, GELO_EINVAL, "base=%g and factor=%g must be positive", base, factor);
+    if (!(trained >= 0.0) || std::isinf(trained) || (trained > 0.0 && !(low < high && std::isfinite(low) && std::isfinite(high))))
+        return fail(ctx, GELO_EINVAL, "trained=%g low=%g high=%g: low < high is wanted", trained, low, high);
+    if (!table || !aligned16(table)) return fail(ctx, table ? GELO_EALIGN : GELO_EINVAL, "table must be a 16-byte aligned device buffer");
+    if ((int64_t)n_pos * (rot_dim / 2) > INT32_MAX) return fail(ctx, GELO_ESHAPE, "a table of %d positions is too large", n_pos);
+    GELO_HIP(ctx, hipSetDevice(ctx->device));
+    const RopeTable o = {rot_dim, first_pos, n_pos, base, factor, trained, low, high, table};
+    GELO_HIP(ctx, rope_table(o, (hipStream_t)stream));
+    return GELO_OK;
+}
+
+static gelo_status check_cache(gelo_ctx* ctx, const gelo_kv_cache* c, KvCache* out) {
+    if (!c || !c->k || !c->v) return fail(ctx, GELO_EINVAL, "cache, its keys and its values must not be NULL");
+    if (c->n_pages < 1 || c->n_kv_heads < 1 || c->head_dim < 1 || c->page_rows < 1)
+        return fail(ctx, GELO_EINVAL, "cache: n_pages=%d n_kv_heads=%d page_rows=%d head_dim=%d", c->n_pages, c->n_kv_heads, c->page_rows, c->head_dim);
+    if (c->page_rows < 16 || (c->page_rows & (c->page_rows - 1))) return fail(ctx, GELO_ESHAPE, "page_rows=%d is not a power of two from 16 on", c->page_rows);
+    if (!aligned16(c->k) || !aligned16(c->v)) return fail(ctx, GELO_EALIGN, "keys and values must be 16-byte aligned");
+    if (c->head_dim % 8 != 0 || c->page_stride % 8 != 0 || c->head_stride % 8 != 0 || c->row_stride % 8 != 0)
+        return fail(ctx, GELO_EALIGN, "cache: head_dim and strides must be multiples of 8");
+    if (c->row_stride < c->head_dim || (c->n_kv_heads > 1 && c->head_stride < c->head_dim) || (c->n_pages > 1 && c->page_stride < c->head_dim))
+        return fail(ctx, GELO_EINVAL, "a stride of the cache is below head_dim=%d", c->head_dim);
+    int shift = 0;
+    while ((1 << shift) < c->page_rows) ++shift;
+    *out = KvCache{c->k, c->v, c->n_pages, c->n_kv_heads, shift, c->head_dim, c->page_stride, c->head_stride, c->row_stride};
+    return GELO_OK;
+}
+
+static gelo_status check_batch(gelo_ctx* ctx, const gelo_seq_batch* b, int page_rows, SeqBatch* out) {
+    if (!b || !b->kv_len || !b->page_table) return fail(ctx, GELO_EINVAL, "batch, kv_len and page_table must not be NULL");
+    if (b->n_seqs < 1 || b->n_rows < 1 || b->max_rows < 1 || b->max_kv_len < 1)
+        return fail(ctx, GELO_EINVAL, "batch: n_seqs=%d n_rows=%d max_rows=%d max_kv_len=%d", b->n_seqs, b->n_rows, b->max_rows, b->max_kv_len);
+    if (!b->row_start && (b->n_rows != b->n_seqs || b->max_rows != 1)) return fail(ctx, GELO_EINVAL, "without row_start every sequence brings one row");
+    if ((reinterpret_cast<uintptr_t>(b->kv_len) | reinterpret_cast<uintptr_t>(b->page_table) | reinterpret_cast<uintptr_t>(b->row_start)) & 3u)
+        return fail(ctx, GELO_EALIGN, "kv_len, page_table and row_start must be 4-byte aligned");
+    const int64_t pages = ((int64_t)b->max_kv_len + page_rows - 1) / page_rows;
+    if (b->table_ld < pages) return fail(ctx, GELO_ESHAPE, "table_ld=%lld: %d rows take %lld pages", (long long)b->table_ld, b->max_kv_len, (long long)pages);
+    if (b->n_rows > kMostRows) return fail(ctx, GELO_ESHAPE, "n_rows=%d exceeds %d", b->n_rows, kMostRows);
+    if (b->max_kv_len > INT32_MAX - 65536 || b->max_rows > INT32_MAX - 65536) return fail(ctx, GELO_ESHAPE, "max_kv_len=%d max_rows=%d", b->max_kv_len, b->max_rows);
+    *out = SeqBatch{b->n_seqs, b->n_rows, b->max_rows, b->max_kv_len, b->row_start, b->kv_len, b->page_table, b->table_ld};
+    return GELO_OK;
+}
+
+gelo_status gelo_rope_append(gelo_ctx* ctx, gelo_dtype dtype, int n_q_heads, const void* QKV, int64_t ld, const gelo_kv_cache* cache,
+                             const gelo_seq_batch* batch, gelo_rope_layout layout, int rot_dim, const float* table, int n_table,
+                             void* Q, int64_t ldq, void* stream) {
+    if (!ctx) return GELO_EINVAL;
+    if (dtype != GELO_F32 && dtype != GELO_BF16) return fail(ctx, GELO_EINVAL, "unknown dtype %d", (int)dtype);
+    if (layout != GELO_ROPE_HALF && layout != GELO_ROPE_PAIRS) return fail(ctx, GELO_EINVAL, "unknown layout %d", (int)layout);
+    RopeAppend o;
+    gelo_status st = check_cache(ctx, cache, &o.cache);
+    if (st == GELO_OK) st = check_batch(ctx, batch, cache->page_rows, &o.batch);
+    if (st != GELO_OK) return st;
+    if (n_q_heads < 0 || (n_q_heads > 0) != (Q != nullptr)) return fail(ctx, GELO_EINVAL, "n_q_heads=%d: Q is given if there are any", n_q_heads);
+    const int64_t width = ((int64_t)n_q_heads + 2 * (int64_t)cache->n_kv_heads) * cache->head_dim;
+    if (width > (1 << 24)) return fail(ctx, GELO_ESHAPE, "a row of %lld values is too wide", (long long)width);
+    st = check_matrix(ctx, "QKV", QKV, ld, (int)width);
+    if (st == GELO_OK && Q) st = check_matrix(ctx, "Q", Q, ldq, n_q_heads * cache->head_dim);
+    if (st != GELO_OK) return st;
+    if (rot_dim < 0 || rot_dim % 16 != 0 || rot_dim > cache->head_dim) return fail(ctx, GELO_EINVAL, "rot_dim=%d must be a multiple of 16 up to head_dim=%d", rot_dim, cache->head_dim);
+    if (rot_dim > 0) {
+        if (!table || !aligned16(table)) return fail(ctx, table ? GELO_EALIGN : GELO_EINVAL, "table must be a 16-byte aligned device buffer");
+        if (n_table < batch->max_kv_len) return fail(ctx, GELO_ESHAPE, "a table of %d positions is too short for max_kv_len=%d", n_table, batch->max_kv_len);
+    }
+    GELO_HIP(ctx, hipSetDevice(ctx->device));
+    o.QKV = QKV; o.ld = ld; o.Q = Q; o.ldq = ldq; o.n_q_heads = n_q_heads; o.rot = rot_dim; o.pairs = layout == GELO_ROPE_PAIRS; o.table = table;
+    GELO_HIP(ctx, rope_append(o, dtype == GELO_BF16, (hipStream_t)stream));
+    return GELO_OK;
+}
+
+gelo_status gelo_attention(gelo_ctx* ctx, gelo_dtype dtype, int n_q_heads, const void* Q, int64_t ldq, const gelo_kv_cache* cache,
+                           const gelo_seq_batch* batch, float scale, int causal, void* O, int64_t ldo, void* stream) {
+    if (!ctx) return GELO_EINVAL;
+    if (dtype != GELO_F32 && dtype != GELO_BF16) return fail(ctx, GELO_EINVAL, "unknown dtype %d", (int)dtype);
+    Attention o;
+    gelo_status st = check_cache(ctx, cache, &o.cache);
+    if (st == GELO_OK) st = check_batch(ctx, batch, cache->page_rows, &o.batch);
+    if (st != GELO_OK) return st;
+    const int d = cache->head_dim;
+    if (d != 64 && d != 96 && d != 128 && d != 256) return fail(ctx, GELO_ESHAPE, "head_dim=%d is none of 64, 96, 128, 256", d);
+    if (n_q_heads < 1 || n_q_heads % cache->n_kv_heads != 0) return fail(ctx, GELO_EINVAL, "n_q_heads=%d is not a multiple of n_kv_heads=%d", n_q_heads, cache->n_kv_heads);
+    if ((int64_t)n_q_heads * d > (1 << 24)) return fail(ctx, GELO_ESHAPE, "n_q_heads=%d heads of %d are too many", n_q_heads, d);
+    if (!std::isfinite(scale)) return fail(ctx, GELO_EINVAL, "scale=%g", (double)scale);
+    st = check_matrix(ctx, "Q", Q, ldq, n_q_heads * d);
+    if (st == GELO_OK) st = check_matrix(ctx, "O", O, ldo, n_q_heads * d);
+    if (st != GELO_OK) return st;
+    o.Q = Q; o.ldq = ldq; o.O = O; o.ldo = ldo; o.n_q_heads = n_q_heads; o.scale = scale; o.causal = causal != 0;
+    if (!attention_fits(o, dtype == GELO_BF16)) return fail(ctx, GELO_ESHAPE, "%d sequences of up to %d rows and %d heads are too many for one launch", batch->n_seqs, batch->max_rows, n_q_heads);
+    GELO_HIP(ctx, hipSetDevice(ctx->device));
+    const size_t need = attention_workspace_bytes(o, dtype == GELO_BF16);
+    if (need > 0) st = grow(ctx, &ctx->attention_ws, &ctx->attention_ws_bytes, need);
+    if (st != GELO_OK) return st;
+    o.workspace = (float*)ctx->attention_ws;
+    GELO_HIP(ctx, attention(o, dtype == GELO_BF16, (hipStream_t)stream));
+    return GELO_OK;
+}
+
+gelo_status gelo_reserve_attention(gelo_ctx* ctx, int head_dim) {
+    if (!ctx) return GELO_EINVAL;
+    if (head_dim != 64 && head_dim != 96 && head_dim != 128 && head_dim != 256) return fail(ctx, GELO_ESHAPE, "head_dim=%d is none of 64, 96, 128, 256", head_dim);
+    GELO_HIP(ctx, hipSetDevice(ctx->device));
+    return grow(ctx, &ctx->attention_ws, &ctx->attention_ws_bytes, attention_workspace_bound(head_dim));
 }
 
 }  // extern "C"

@@ -367,4 +367,59 @@ hipError_t zero_ints(int* p, int count, hipStream_t stream);
 // zero rows/cols [n, n_pad) of M
 hipError_t pad_matrix(float* M, int64_t ld, int n, int n_pad, hipStream_t stream);
 
+// ------------------------------------------- between two projections: norm, cache, attention --
+// norm.hip: see gelo_rms_norm; d a multiple of 8, at most 65536; all matrices 16-byte aligned with leading dimensions that are multiples of 8
+struct RmsNorm {
+    const void* X; int64_t ldx;
+    const void* R; int64_t ldr;        // may be null
+    const void* gamma;
+    void* R_out; int64_t ldro;         // may be null
+    void* H; int64_t ldh;              // may be null
+    uint8_t* codes; int64_t ldq; float* scales;      // may be null (both)
+    float eps;
+    int n, d;
+};
+hipError_t rms_norm(const RmsNorm& o, int is_bf16, hipStream_t stream);
+// gelo_kv_cache and gelo_seq_batch; page_rows = 1 << page_shift
+struct KvCache {
+    void* k; void* v;
+    int n_pages, n_kv_heads, page_shift, head_dim;
+    int64_t page_stride, head_stride, row_stride;
+};
+struct SeqBatch {
+    int n_seqs, n_rows, max_rows, max_kv_len;
+    const int32_t* row_start;          // may be null: one row per sequence
+    const int32_t* kv_len;
+    const int32_t* page_table; int64_t table_ld;
+};
+// rope.hip
+struct RopeTable { int rot, first, count; double base, factor, trained, low, high; float* out; };
+hipError_t rope_table(const RopeTable& o, hipStream_t stream);
+struct RopeAppend {
+    const void* QKV; int64_t ld;
+    void* Q; int64_t ldq;
+    int n_q_heads, rot, pairs;
+    const float* table;
+    KvCache cache;
+    SeqBatch batch;
+};
+hipError_t rope_append(const RopeAppend& o, int is_bf16, hipStream_t stream);
+// attention.hip
+struct Attention {
+    const void* Q; int64_t ldq;
+    void* O; int64_t ldo;
+    int n_q_heads;
+    float scale;
+    bool causal;
+    KvCache cache;
+    SeqBatch batch;
+    float* workspace;                  // at least attention_workspace_bytes
+};
+// float workspace for the parts of a cache that is cut over workgroups: what this call needs, and the most any call of this head width needs
+bool attention_fits(const Attention& o, int is_bf16);       // as one launch
+size_t attention_workspace_bytes(const Attention& o, int is_bf16);
+size_t attention_workspace_bound(int head_dim);
+hipError_t attention(const Attention& o, int is_bf16, hipStream_t stream);
+hipError_t attention_init();
+
 }  // namespace gelo

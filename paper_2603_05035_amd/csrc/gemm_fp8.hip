@@ -13,6 +13,7 @@
 // arithmetic on the float bit pattern so that every code is defined by this file alone; the scaled value
 // never exceeds 448 * (1 + 2^-23), which rounds to 448.
 #include "gelo_internal.h"
+#include "e4m3.h"
 
 namespace gelo {
 namespace {
@@ -24,25 +25,6 @@ typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ float bf16_bits(uint32_t h) { return __uint_as_float(h << 16); }
-
-// float -> E4M3 code (1 sign, 4 exponent bits with bias 7, 3 fraction bits; largest finite value 448 = 0x7E),
-// round to nearest even, saturating, subnormals spaced 2^-9
-__device__ __forceinline__ uint32_t e4m3_code(float t) {
-    const uint32_t bits = __float_as_uint(t);
-    const uint32_t sign = (bits >> 24) & 0x80u;
-    const float a = fabsf(t);
-    uint32_t code;
-    if (a < 0.015625f) {                                     // below 2^-6: multiples of 2^-9; 8 of them is the first normal
-        code = (uint32_t)rintf(a * 512.0f);
-    } else {
-        uint32_t m = __float_as_uint(a);
-        m += 0x7FFFFu + ((m >> 20) & 1u);                    // round the 23-bit fraction to 3 bits, ties to even
-        const uint32_t e = (m >> 23) - 120u;                 // rebias: 127 -> 7
-        code = (e << 3) | ((m >> 20) & 7u);
-        code = code > 0x7Eu ? 0x7Eu : code;                  // saturate at 448 (0x7F would be NaN)
-    }
-    return sign | code;
-}
 
 __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
