@@ -1473,6 +1473,7 @@ static gelo_status check_cache(gelo_ctx* ctx, const gelo_kv_cache* c, KvCache* o
         return fail(ctx, GELO_EALIGN, "cache: head_dim and strides must be multiples of 8");
     if (c->row_stride < c->head_dim || (c->n_kv_heads > 1 && c->head_stride < c->head_dim) || (c->n_pages > 1 && c->page_stride < c->head_dim))
         return fail(ctx, GELO_EINVAL, "a stride of the cache is below head_dim=%d", c->head_dim);
+    if (c->row_stride > (1 << 24)) return fail(ctx, GELO_ESHAPE, "cache: rows %lld values apart are too far from each other", (long long)c->row_stride);
     int shift = 0;
     while ((1 << shift) < c->page_rows) ++shift;
     *out = KvCache{c->k, c->v, c->n_pages, c->n_kv_heads, shift, c->head_dim, c->page_stride, c->head_stride, c->row_stride};

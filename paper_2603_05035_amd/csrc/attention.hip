@@ -25,7 +25,9 @@ struct AttnArgs {
     float* part_o;               // [chunk][row][head][D], where the cache is cut
     float* part_ml;              // [chunk][row][head][2]: maximum (of log2) and sum
     int n_q_heads, group;        // query heads to a key head
-    float scale2;                // scale * log2 e
+    float scale2;                // |scale| log2 e
+    float scale2s;               // scale log2 e
+    uint32_t flip;               // sign bits of Q's words where scale is negative
     int causal;
     int chunk, n_chunks, col_tiles;
     KvCache kv;
@@ -232,12 +234,110 @@ template <> __device__ __forceinline__ void store4<uint16_t>(uint16_t* p, f32x4_
 
 constexpr int kFewWaves = 4;
 
+// One wave walks the keys `key`, key + stride, ... up to `last` of a tile of 16 columns, KEYS at a time: the running maximum (of log2), the sum of
+// weights over the lane's own keys and the weighted sum of the values.  limit: last key this lane's column sees, least: the least of the tile.
+template <class T, int D>
+__device__ __forceinline__ void walk_keys(const AttnArgs& a, int seq, int kvh, int key, int stride, int last, int least, int limit, int g, int c,
+                                          Few<T, D>& f, f32x4_t (&acc)[Few<T, D>::VD], float& m, float& l, bool& bad_page) {
+    typedef Few<T, D> F;
+    constexpr int VD = F::VD, SLOTS = 4 * F::TILES;
+    const int shift = a.kv.page_shift, in_page = (1 << shift) - 1;
+    const int32_t* table = a.b.page_table + seq * a.b.table_ld;
+    const T* k_head = (const T*)a.kv.k + kvh * a.kv.head_stride;
+    const T* v_head = (const T*)a.kv.v + kvh * a.kv.head_stride;
+    // keys beyond the end are read as the last key, whose address is good, and get no weight
+    auto tile_start = [&](int key) { return min(key, last & ~15); };
+    auto page_of = [&](int key) { return table[tile_start(key) >> shift]; };
+    auto page_base = [&](int key, int page) {
+        const bool good = page >= 0 && page < a.kv.n_pages;
+        bad_page |= !good;
+        return (good ? page : 0) * a.kv.page_stride + (tile_start(key) & in_page) * a.kv.row_stride;
+    };
+    auto load_k = [&](int key, const int (&page)[F::TILES]) {
+#pragma unroll
+        for (int t = 0; t < F::TILES; ++t) {
+            const int at = key + 16 * t, r = min(at + c, last) - tile_start(at);
+            f.load_k(t, k_head + page_base(at, page[t]) + r * a.kv.row_stride, g);
+        }
+    };
+    auto load_v = [&](int key, const int (&page)[F::TILES]) {
+#pragma unroll
+        for (int t = 0; t < F::TILES; ++t) {
+            const int at = key + 16 * t;
+            const T* base = v_head + page_base(at, page[t]);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int r = min(at + 4 * g + u, last) - tile_start(at);
+                f.load_v(t, u, base + r * a.kv.row_stride, c);
+            }
+        }
+    };
+    if (key > last) return;
+    int page[F::TILES];
+#pragma unroll
+    for (int t = 0; t < F::TILES; ++t) page[t] = page_of(key + 16 * t);
+    load_k(key, page);
+    load_v(key, page);
+    for (; key <= last; key += stride) {
+        const int next = key + stride;
+        if (next <= last) {
+#pragma unroll
+            for (int t = 0; t < F::TILES; ++t) page[t] = page_of(next + 16 * t);
+        }
+        float s[SLOTS];
+#pragma unroll
+        for (int t = 0; t < F::TILES; ++t) {
+            const f32x4_t x = f.scores(t);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[4 * t + r] = x[r] * a.scale2s;
+        }
+        if (next <= last) load_k(next, page);
+        // hidden: keys beyond what the column sees (uniform test first: most steps have none)
+        const bool partly = key + F::KEYS - 1 > min(least, last);
+        uint32_t seen = ~0u;
+        if (partly) {
+            const int upto = min(limit, last);
+            seen = 0;
+#pragma unroll
+            for (int t = 0; t < F::TILES; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const bool sees = key + 16 * t + 4 * g + r <= upto;
+                    s[4 * t + r] = sees ? s[4 * t + r] : -__builtin_inff();
+                    seen |= (uint32_t)sees << (4 * t + r);
+                }
+        }
+        float top = s[0];
+#pragma unroll
+        for (int r = 1; r < SLOTS; ++r) top = fmaxf(top, s[r]);
+        const float m_new = fmaxf(m, across_groups_max(top));
+        const float m_safe = m_new == -__builtin_inff() ? 0.f : m_new;        // nothing seen yet: all weights are 0
+        const float alpha = __builtin_amdgcn_exp2f(m - m_safe);
+        m = m_new;
+        l *= alpha;
+#pragma unroll
+        for (int r = 0; r < SLOTS; ++r) {
+            s[r] = __builtin_amdgcn_exp2f(s[r] - m_safe);
+            l += s[r];
+        }
+        if (__ballot(alpha != 1.f)) {
+#pragma unroll
+            for (int j = 0; j < VD; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[j][r] *= alpha;
+        }
+        if (partly && __ballot(f.odd_values())) f.accumulate_odd(acc, s, seen);
+        else f.accumulate(acc, s);
+        if (next <= last) load_v(next, page);
+    }
+}
+
 // A workgroup: one tile of 16 columns of one sequence and key head, one chunk of the cache.
 template <class T, int D>
 __global__ __launch_bounds__(64 * kFewWaves)
 void attention_few_kernel(AttnArgs a) {
     typedef Few<T, D> F;
-    constexpr int VD = F::VD, SLOTS = 4 * F::TILES;
+    constexpr int VD = F::VD;
     __shared__ float joined_o[kFewWaves][16][D + 4];
     __shared__ float joined_ml[kFewWaves][16][2];
     const int chunk = blockIdx.x % a.n_chunks;
@@ -270,99 +370,7 @@ void attention_few_kernel(AttnArgs a) {
     float m = -__builtin_inff(), l = 0.f;
     bool bad_page = false;
 
-    const int last = end - 1, shift = a.kv.page_shift, in_page = (1 << shift) - 1;
-    const int32_t* table = a.b.page_table + seq * a.b.table_ld;
-    const T* k_head = (const T*)a.kv.k + kvh * a.kv.head_stride;
-    const T* v_head = (const T*)a.kv.v + kvh * a.kv.head_stride;
-    // keys beyond the end are read as the last key, whose address is good, and get no weight
-    auto tile_start = [&](int key) { return min(key, last & ~15); };
-    auto page_of = [&](int key) { return table[tile_start(key) >> shift]; };
-    auto page_base = [&](int key, int page) {
-        const bool good = page >= 0 && page < a.kv.n_pages;
-        bad_page |= !good;
-        return (good ? page : 0) * a.kv.page_stride + (tile_start(key) & in_page) * a.kv.row_stride;
-    };
-    auto load_k = [&](int key, const int (&page)[F::TILES]) {
-#pragma unroll
-        for (int t = 0; t < F::TILES; ++t) {
-            const int at = key + 16 * t, r = min(at + c, last) - tile_start(at);
-            f.load_k(t, k_head + page_base(at, page[t]) + r * a.kv.row_stride, g);
-        }
-    };
-    auto load_v = [&](int key, const int (&page)[F::TILES]) {
-#pragma unroll
-        for (int t = 0; t < F::TILES; ++t) {
-            const int at = key + 16 * t;
-            const T* base = v_head + page_base(at, page[t]);
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int r = min(at + 4 * g + u, last) - tile_start(at);
-                f.load_v(t, u, base + r * a.kv.row_stride, c);
-            }
-        }
-    };
-
-    constexpr int STRIDE = F::KEYS * kFewWaves;
-    int key = begin + wave * F::KEYS;
-    if (key < end) {
-        int page[F::TILES];
-#pragma unroll
-        for (int t = 0; t < F::TILES; ++t) page[t] = page_of(key + 16 * t);
-        load_k(key, page);
-        load_v(key, page);
-        for (; key < end; key += STRIDE) {
-            const int next = key + STRIDE;
-            if (next < end) {
-#pragma unroll
-                for (int t = 0; t < F::TILES; ++t) page[t] = page_of(next + 16 * t);
-            }
-            float s[SLOTS];
-#pragma unroll
-            for (int t = 0; t < F::TILES; ++t) {
-                const f32x4_t x = f.scores(t);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) s[4 * t + r] = x[r] * a.scale2;
-            }
-            if (next < end) load_k(next, page);
-            // hidden: keys beyond what the column sees (uniform test first: most steps have none)
-            const bool partly = key + F::KEYS - 1 > min(least, last);
-            uint32_t seen = ~0u;
-            if (partly) {
-                const int upto = min(limit, last);
-                seen = 0;
-#pragma unroll
-                for (int t = 0; t < F::TILES; ++t)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const bool sees = key + 16 * t + 4 * g + r <= upto;
-                        s[4 * t + r] = sees ? s[4 * t + r] : -__builtin_inff();
-                        seen |= (uint32_t)sees << (4 * t + r);
-                    }
-            }
-            float top = s[0];
-#pragma unroll
-            for (int r = 1; r < SLOTS; ++r) top = fmaxf(top, s[r]);
-            const float m_new = fmaxf(m, across_groups_max(top));
-            const float m_safe = m_new == -__builtin_inff() ? 0.f : m_new;        // nothing seen yet: all weights are 0
-            const float alpha = __builtin_amdgcn_exp2f(m - m_safe);
-            m = m_new;
-            l *= alpha;
-#pragma unroll
-            for (int r = 0; r < SLOTS; ++r) {
-                s[r] = __builtin_amdgcn_exp2f(s[r] - m_safe);
-                l += s[r];
-            }
-            if (__ballot(alpha != 1.f)) {
-#pragma unroll
-                for (int j = 0; j < VD; ++j)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) acc[j][r] *= alpha;
-            }
-            if (partly && __ballot(f.odd_values())) f.accumulate_odd(acc, s, seen);
-            else f.accumulate(acc, s);
-            if (next < end) load_v(next, page);
-        }
-    }
+    walk_keys<T, D>(a, seq, kvh, begin + wave * F::KEYS, F::KEYS * kFewWaves, end - 1, least, limit, g, c, f, acc, m, l, bad_page);
     l = across_groups_sum(l);
     if (bad_page) l = __builtin_nanf("");
 
@@ -405,6 +413,298 @@ void attention_few_kernel(AttnArgs a) {
             *reinterpret_cast<f32x4_t*>(a.part_o + item * D + x) = o;
             if (x == 0) { a.part_ml[2 * item] = top; a.part_ml[2 * item + 1] = total; }
         }
+    }
+}
+
+// attention_prompt_kernel: many columns to a key head, bfloat16.  Bound by the matrix instructions and, beside them, by the exponentials.  A
+// workgroup takes kPromptWaves x 32 CB columns and walks the keys KT at a time; K and V of a step come into LDS once for all its waves, by
+// direct-to-LDS fetches a step ahead.  v_mfma_f32_32x32x16_bf16: lane (h, c) = (lane / 32, lane % 32); S^T of 32 keys leaves in register r of
+// the lane column c and key 8 (r / 4) + 4 h + r % 4, so registers 8 t ... 8 t + 7 are keys 16 t + {4 h + 0..3, 8 + 4 h + 0..3}: the B operand of step t
+// of O^T, if A = V^T takes its keys in that order - two transposing reads of four rows each.
+constexpr int kPromptWaves = 4;
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x8_t __attribute__((ext_vector_type(8)));
+
+// lds_addr must be wave-uniform (it travels in M0); lane l's 16 bytes land at lds_addr + 16 l
+__device__ __forceinline__ void fetch16(uint32_t offset, const void* base, uint32_t lds_addr) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" :: "v"(offset), "s"(base), "s"(lds_addr) : "memory", "m0");
+}
+
+template <int D> constexpr int prompt_keys() { return D == 256 ? 32 : 64; }
+template <int D> constexpr int prompt_lds() { return 2 * 2 * prompt_keys<D>() * D * 2; }
+
+// Where the 16-byte chunk c of row r lies in its row.  K: 16 lanes read the same chunk of 16 rows in a row; V: half a wave reads four chunks of
+// four rows.  Either has to meet all 64 banks: 16 chunks of 16 bytes are a round of them.
+template <int D> __device__ __forceinline__ int k_pos(int r, int c) {
+    if constexpr (D == 64) return c ^ ((r >> 1) & 7);
+    else if constexpr (D == 96) return (c + ((r >> 2) & 3)) % 12;
+    else return c ^ (r & 15);
+}
+template <int D> __device__ __forceinline__ int k_chunk(int r, int p) {
+    if constexpr (D == 96) return (p + 12 - ((r >> 2) & 3)) % 12;
+    else return k_pos<D>(r, p);
+}
+template <int D> __device__ __forceinline__ int v_pos(int r, int c) {          // its own inverse
+    if constexpr (D == 64) return c ^ ((r & 2) << 1);
+    else if constexpr (D == 96) return c;
+    else return c ^ ((r & 3) << 2);
+}
+
+template <int D, int CB>
+__global__ __launch_bounds__(64 * kPromptWaves, CB == 1 && D < 256 ? 2 : 1)
+void attention_prompt_kernel(AttnArgs a) {
+    constexpr int KT = prompt_keys<D>(), KB = KT / 32, KS = D / 16, DT = D / 32, PITCH = 2 * D, STAGE = 2 * KT * PITCH;
+    constexpr int ROWS = KT / kPromptWaves;                  // rows a wave fetches: 16 or 8
+    constexpr int NF = ROWS * PITCH / 1024;                  // fetches of 1 KB for them
+    extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+    int set, item;
+    if (!deal_to_dies(blockIdx.x, a.col_tiles * a.n_chunks, a.b.n_seqs * a.kv.n_kv_heads, &set, &item)) return;
+    const int kvh = set % a.kv.n_kv_heads, seq = set / a.kv.n_kv_heads;
+    const int chunk = item % a.n_chunks, tile = a.col_tiles - 1 - item / a.n_chunks;      // the columns that see most first
+    const NewRows rows = rows_of_sequence(a.b, seq);
+    const int columns = rows.count * a.group, first_col = tile * (32 * CB * kPromptWaves);
+    if (first_col >= columns) return;
+    const int kv_len = a.b.kv_len[seq], kv_end = min(kv_len, a.b.max_kv_len);
+    const int lane = threadIdx.x & 63, h = lane >> 5, c = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+
+    auto limit_of = [&](int col) { return min(a.causal ? kv_len - rows.count + col / a.group : kv_len - 1, kv_end - 1); };
+    const int wg_most = limit_of(min(first_col + 32 * CB * kPromptWaves, columns) - 1);
+    const int begin = chunk * a.chunk, end = min(begin + a.chunk, wg_most + 1);
+    if (begin >= end && a.n_chunks > 1) return;
+
+    // this wave's columns
+    const int wave_col = first_col + wave * 32 * CB;
+    const bool awake = wave_col < columns;
+    const int most = awake ? limit_of(min(wave_col + 32 * CB, columns) - 1) : -1, least = awake ? limit_of(wave_col) : -1;
+    int limit[CB], row[CB], head[CB];
+    bf16x8_t q[CB][KS];
+    f32x16_t acc[CB][DT];
+    float m[CB], l[CB];
+#pragma unroll
+    for (int b = 0; b < CB; ++b) {
+        const int col = min(wave_col + 32 * b + c, columns - 1), i = col / a.group;      // dead columns repeat the last one
+        limit[b] = limit_of(col);
+        row[b] = rows.first + i;
+        head[b] = kvh * a.group + col - i * a.group;
+        const uint16_t* p = (const uint16_t*)a.Q + row[b] * a.ldq + (int64_t)head[b] * D + 8 * h;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            u32x4_t w = *reinterpret_cast<const u32x4_t*>(p + 16 * s);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] ^= a.flip;
+            q[b][s] = __builtin_bit_cast(bf16x8_t, w);
+        }
+    }
+
+    // fetches: this wave's rows of a step, 1 KB at a time; the keys of 16 rows share a page
+    const uint32_t lds_base = __builtin_amdgcn_readfirstlane((uint32_t)(size_t)lds);
+    uint32_t k_off[NF], v_off[NF];
+#pragma unroll
+    for (int i = 0; i < NF; ++i) {
+        const int at = i * 1024 + lane * 16, r = at / PITCH, p = (at - r * PITCH) / 16, rr = wave * ROWS + r;
+        k_off[i] = (uint32_t)(r * (int)a.kv.row_stride + 8 * k_chunk<D>(rr, p)) * 2;
+        v_off[i] = (uint32_t)(r * (int)a.kv.row_stride + 8 * v_pos<D>(rr, p)) * 2;
+    }
+    const int last = end - 1, shift = a.kv.page_shift, in_page = (1 << shift) - 1;
+    const int32_t* table = a.b.page_table + seq * a.b.table_ld;
+    const uint16_t* k_head = (const uint16_t*)a.kv.k + kvh * a.kv.head_stride;
+    const uint16_t* v_head = (const uint16_t*)a.kv.v + kvh * a.kv.head_stride;
+    bool bad_page = false;
+    // rows beyond the last key are fetched as that key's (they are masked, but 0 times what lies there might be NaN)
+    auto group_of = [&](int key) { return min(key + wave * ROWS, last & ~(ROWS - 1)); };
+    auto page_of = [&](int key) { return table[group_of(key) >> shift]; };
+    auto fetch = [&](int key, int page, int stage) {
+        const bool good = page >= 0 && page < a.kv.n_pages;
+        bad_page |= !good;
+        const int64_t at = (good ? page : 0) * a.kv.page_stride + (group_of(key) & in_page) * a.kv.row_stride;
+        const uint16_t* kp = k_head + at;
+        const uint16_t* vp = v_head + at;
+        const uint32_t to = lds_base + stage * STAGE + wave * ROWS * PITCH;
+        const int over = group_of(key) + ROWS - 1 - last;    // rows that are not there
+        if (over <= 0) {
+#pragma unroll
+            for (int i = 0; i < NF; ++i) fetch16(k_off[i], kp, to + i * 1024);
+#pragma unroll
+            for (int i = 0; i < NF; ++i) fetch16(v_off[i], vp, to + KT * PITCH + i * 1024);
+        } else {
+#pragma unroll
+            for (int i = 0; i < NF; ++i) {
+                const int r = (i * 1024 + lane * 16) / PITCH, back = max(r - (ROWS - 1 - over), 0);
+                const uint32_t by = (uint32_t)(back * (int)a.kv.row_stride) * 2;
+                fetch16(k_off[i] - by, kp, to + i * 1024);
+                fetch16(v_off[i] - by, vp, to + KT * PITCH + i * 1024);
+            }
+        }
+    };
+
+    const int s16 = lane & 15, nh = (lane >> 4) & 1;
+    const int steps = end > begin ? (end - begin + KT - 1) / KT : 0;
+    // 0 times a value that is not finite is NaN also in columns that do not see its key.  Such values are rare, and they show in the result: a
+    // workgroup that finds any there walks its keys once more with zeros in their place and adds them to the columns that see them.
+    __shared__ int any_odd, any_bad, first_odd[2][D];
+    if (threadIdx.x == 0) any_odd = any_bad = 0;
+    for (int x = threadIdx.x; x < 2 * D; x += 64 * kPromptWaves) (&first_odd[0][0])[x] = 0x7FFFFFFF;
+    for (int pass = 0;; ++pass) {
+#pragma unroll
+        for (int b = 0; b < CB; ++b) {
+            m[b] = -__builtin_inff();
+            l[b] = 0.f;
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[b][t][r] = 0.f;
+        }
+        int page = 0;
+        if (steps > 0) {
+            fetch(begin, page_of(begin), 0);
+            if (steps > 1) page = page_of(begin + KT);
+        }
+        for (int step = 0; step < steps; ++step) {
+            const int key = begin + step * KT;
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            if (step + 1 < steps) {
+                fetch(key + KT, page, (step + 1) & 1);
+                if (step + 2 < steps) page = page_of(key + 2 * KT);
+            }
+            if (pass == 1) {
+                // the values that are not finite go, and per component the first key that had one is kept
+                for (int at = threadIdx.x * 16; at < KT * PITCH; at += 64 * kPromptWaves * 16) {
+                    const int r = at / PITCH, x = 8 * v_pos<D>(r, (at - r * PITCH) / 16);
+                    s16x8_t* where = reinterpret_cast<s16x8_t*>(lds + (step & 1) * STAGE + KT * PITCH + at);
+                    s16x8_t v = *where;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        if ((v[e] & 0x7F80) != 0x7F80) continue;
+                        const bool nan = v[e] & 0x7F;
+                        if (nan || v[e] > 0) atomicMin(&first_odd[0][x + e], key + r);
+                        if (nan || v[e] < 0) atomicMin(&first_odd[1][x + e], key + r);
+                        v[e] = 0;
+                    }
+                    *where = v;
+                }
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                __builtin_amdgcn_s_barrier();
+            }
+            if (key > most) continue;                            // nothing here for this wave's columns
+            const uint32_t k_at = lds_base + (step & 1) * STAGE, v_at = k_at + KT * PITCH;
+            typedef const bf16x8_t __attribute__((address_space(3))) * k_ptr_t;
+            typedef s16x4_t __attribute__((address_space(3))) * v_ptr_t;
+            f32x16_t s[CB][KB];
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) {
+#pragma unroll
+                for (int b = 0; b < CB; ++b)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[b][kb][r] = 0.f;
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    const int r = 32 * kb + c;
+                    const bf16x8_t kf = *(k_ptr_t)(size_t)(k_at + r * PITCH + 16 * k_pos<D>(r, 2 * ks + h));
+#pragma unroll
+                    for (int b = 0; b < CB; ++b) s[b][kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[b][ks], s[b][kb], 0, 0, 0);
+                }
+            }
+            const bool partly = key + KT - 1 > least;
+            bf16x8_t p[CB][2 * KB];
+#pragma unroll
+            for (int b = 0; b < CB; ++b) {
+                if (partly) {
+                    const int upto = limit[b] - key;
+#pragma unroll
+                    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            s[b][kb][r] = 32 * kb + 8 * (r >> 2) + 4 * h + (r & 3) <= upto ? s[b][kb][r] : -__builtin_inff();
+                }
+                float top = s[b][0][0];
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][kb][r]);
+                top = fmaxf(top, __shfl_xor(top, 32, 64));
+                const float m_new = fmaxf(m[b], top);
+                const float base = m_new == -__builtin_inff() ? 0.f : m_new * a.scale2;
+                const float alpha = __builtin_amdgcn_exp2f(m[b] * a.scale2 - base);
+                if (__ballot(m_new != m[b])) {
+                    l[b] *= alpha;
+#pragma unroll
+                    for (int t = 0; t < DT; ++t)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) acc[b][t][r] *= alpha;
+                }
+                m[b] = m_new;
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const float w = __builtin_amdgcn_exp2f(s[b][kb][r] * a.scale2 - base);
+                        l[b] += w;
+                        p[b][2 * kb + (r >> 3)][r & 7] = (__bf16)w;
+                    }
+            }
+            // V^T of component block t and the 16 keys of ks
+            auto v_frag = [&](int t, int ks) {
+                s16x8_t f;
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int r = 16 * ks + 8 * half + 4 * h + (s16 >> 2);
+                    const uint32_t at = v_at + r * PITCH + 16 * v_pos<D>(r, 4 * t + 2 * nh + ((s16 >> 1) & 1)) + 8 * (s16 & 1);
+                    const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v_ptr_t)(size_t)at);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) f[4 * half + e] = x[e];
+                }
+                return f;
+            };
+#pragma unroll
+            for (int ks = 0; ks < 2 * KB; ++ks)
+#pragma unroll
+                for (int t = 0; t < DT; ++t) {
+                    const s16x8_t f = v_frag(t, ks);
+#pragma unroll
+                    for (int b = 0; b < CB; ++b) acc[b][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, f), p[b][ks], acc[b][t], 0, 0, 0);
+                }
+        }
+        if (pass == 1) break;
+        bool odd = false;
+#pragma unroll
+        for (int b = 0; b < CB; ++b)
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) odd |= (__float_as_uint(acc[b][t][r]) & 0x7F800000u) == 0x7F800000u;
+        __syncthreads();
+        if (odd) any_odd = 1;
+        if (bad_page) any_bad = 1;                           // a page that is not there: any wave may have met it
+        __syncthreads();
+        if (!any_odd) break;
+    }
+    if (!awake) return;
+    const bool whole = a.n_chunks == 1;
+#pragma unroll
+    for (int b = 0; b < CB; ++b) {
+        if (wave_col + 32 * b + c >= columns) continue;
+        float total = l[b] + __shfl_xor(l[b], 32, 64);
+        if (any_bad) total = __builtin_nanf("");
+        const float inv = total == 0.f ? 0.f : 1.f / total;
+        const int64_t part = ((int64_t)chunk * a.b.n_rows + row[b]) * a.n_q_heads + head[b];
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int x = 32 * t + 8 * e + 4 * h;
+                f32x4_t o;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    o[u] = total == 0.f ? 0.f : whole ? acc[b][t][4 * e + u] * inv : acc[b][t][4 * e + u];
+                    if (any_odd) o[u] += (first_odd[0][x + u] <= limit[b] ? __builtin_inff() : 0.f) - (first_odd[1][x + u] <= limit[b] ? __builtin_inff() : 0.f);
+                }
+                if (whole) store4((uint16_t*)a.O + row[b] * a.ldo + (int64_t)head[b] * D + x, o);
+                else *reinterpret_cast<f32x4_t*>(a.part_o + part * D + x) = o;
+            }
+        if (!whole && h == 0) { a.part_ml[2 * part] = total == 0.f ? -__builtin_inff() : m[b] * a.scale2; a.part_ml[2 * part + 1] = total; }
     }
 }
 
@@ -458,25 +758,27 @@ void attention_join_kernel(AttnArgs a) {
     store4((T*)a.O + row * a.ldo + (item - (int64_t)row * a.n_q_heads) * D + x, o);
 }
 
-// How the cache is cut: chunks of `chunk` keys, n_chunks of them to the longest sequence.
-struct Plan { int col_tiles, chunk, n_chunks; int64_t workgroups; };
-constexpr int kFewTarget = 1024;         // workgroups that fill the chip
+// Which kernel, and how the cache is cut: chunks of `chunk` keys, n_chunks of them to the longest sequence.
+struct Plan { bool prompt; int col_tiles, chunk, n_chunks; int64_t workgroups; };
 constexpr int64_t kMostWorkgroups = 1 << 23;     // of a launch: 2^31 threads and no more fit HIP's 32-bit counts
-constexpr int kFewLeast = 256;           // keys to a chunk, at least
+constexpr int kFewTarget = 1024, kFewLeast = 256;        // workgroups that fill the chip, keys to a chunk at least
+constexpr int kPromptTarget = 512, kPromptLeast = 256;
+constexpr int kPromptBlocks = 1;                 // blocks of 32 columns to a wave
 
-Plan plan_few(const Attention& o) {
+Plan plan_of(const Attention& o, int is_bf16) {
     Plan p;
-    const int group = o.n_q_heads / o.cache.n_kv_heads;
-    p.col_tiles = (int)(((int64_t)o.batch.max_rows * group + 15) / 16);
-    const int64_t tiles = (int64_t)o.batch.n_seqs * o.cache.n_kv_heads * p.col_tiles;
-    int64_t cuts = kFewTarget / tiles;
-    const int64_t most = (o.batch.max_kv_len + kFewLeast - 1) / kFewLeast;
+    const int64_t columns = (int64_t)o.batch.max_rows * (o.n_q_heads / o.cache.n_kv_heads);
+    p.prompt = is_bf16 && columns > 16;
+    const int wide = p.prompt ? 32 * kPromptBlocks * kPromptWaves : 16, target = p.prompt ? kPromptTarget : kFewTarget, least = p.prompt ? kPromptLeast : kFewLeast;
+    p.col_tiles = (int)((columns + wide - 1) / wide);
+    const int64_t sets = (int64_t)o.batch.n_seqs * o.cache.n_kv_heads, tiles = sets * p.col_tiles;
+    const int64_t most = (o.batch.max_kv_len + least - 1) / least;
+    int64_t cuts = target / tiles;
     cuts = cuts < 1 ? 1 : cuts < most ? cuts : most;
-    if (cuts < 1) cuts = 1;
     p.chunk = (int)round_up((o.batch.max_kv_len + cuts - 1) / cuts, 128);
-    p.n_chunks = p.chunk > 0 ? (o.batch.max_kv_len + p.chunk - 1) / p.chunk : 1;
-    if (p.n_chunks < 1) p.n_chunks = 1;
+    p.n_chunks = (o.batch.max_kv_len + p.chunk - 1) / p.chunk;
     p.workgroups = tiles * p.n_chunks;
+    if (p.prompt && p.workgroups <= kMostWorkgroups) p.workgroups = 8 * (int64_t)dies_slots(p.col_tiles * p.n_chunks, (int)sets);
     return p;
 }
 
@@ -486,17 +788,24 @@ size_t part_bytes(const Attention& o, const Plan& p) {
 
 template <class T, int D>
 hipError_t launch(const Attention& o, hipStream_t stream) {
-    const Plan p = plan_few(o);
+    const Plan p = plan_of(o, sizeof(T) == 2);
     AttnArgs a;
     a.Q = o.Q; a.ldq = o.ldq; a.O = o.O; a.ldo = o.ldo;
     a.n_q_heads = o.n_q_heads; a.group = o.n_q_heads / o.cache.n_kv_heads;
-    a.scale2 = o.scale * kLog2E; a.causal = o.causal;
+    a.scale2s = o.scale * kLog2E;
+    a.scale2 = o.scale == 0.f ? 1e-30f : fabsf(a.scale2s);      // (-inf, a hidden score, times 0 would be NaN)
+    a.flip = o.scale < 0.f ? 0x80008000u : 0u;
+    a.causal = o.causal;
     a.chunk = p.chunk; a.n_chunks = p.n_chunks; a.col_tiles = p.col_tiles;
     a.kv = o.cache; a.b = o.batch;
     const int64_t items = (int64_t)o.batch.n_rows * o.n_q_heads;
     a.part_o = o.workspace;
     a.part_ml = p.n_chunks == 1 ? nullptr : o.workspace + (int64_t)p.n_chunks * items * D;
-    hipLaunchKernelGGL((attention_few_kernel<T, D>), dim3((unsigned)p.workgroups), dim3(64 * kFewWaves), 0, stream, a);
+    if constexpr (sizeof(T) == 2) {
+        if (p.prompt)
+            hipLaunchKernelGGL((attention_prompt_kernel<D, kPromptBlocks>), dim3((unsigned)p.workgroups), dim3(64 * kPromptWaves), (size_t)prompt_lds<D>(), stream, a);
+    }
+    if (!p.prompt) hipLaunchKernelGGL((attention_few_kernel<T, D>), dim3((unsigned)p.workgroups), dim3(64 * kFewWaves), 0, stream, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.n_chunks == 1) return e;
     hipLaunchKernelGGL((attention_join_kernel<T, D>), dim3((unsigned)((items * (D / 4) + 255) / 256)), dim3(256), 0, stream, a);
@@ -516,17 +825,30 @@ hipError_t of_width(const Attention& o, hipStream_t stream) {
 
 }  // namespace
 
-bool attention_fits(const Attention& o, int) {
-    return plan_few(o).workgroups <= kMostWorkgroups && ((int64_t)o.batch.n_rows * o.n_q_heads * (o.cache.head_dim / 4) + 255) / 256 <= kMostWorkgroups;
+bool attention_fits(const Attention& o, int is_bf16) {
+    return plan_of(o, is_bf16).workgroups <= kMostWorkgroups && ((int64_t)o.batch.n_rows * o.n_q_heads * (o.cache.head_dim / 4) + 255) / 256 <= kMostWorkgroups;
 }
-size_t attention_workspace_bytes(const Attention& o, int) { return part_bytes(o, plan_few(o)); }
-// a plan with more than one chunk has at most kFewTarget workgroups of 16 columns
-size_t attention_workspace_bound(int head_dim) { return (size_t)kFewTarget * 16 * (head_dim + 2) * sizeof(float); }
+size_t attention_workspace_bytes(const Attention& o, int is_bf16) { return part_bytes(o, plan_of(o, is_bf16)); }
+// a plan of more than one chunk has at most its target of workgroups, and every row's head is a column of one of them
+size_t attention_workspace_bound(int head_dim) {
+    const size_t columns = kPromptTarget * 32 * kPromptBlocks * kPromptWaves;
+    static_assert(kFewTarget * 16 <= kPromptTarget * 32 * kPromptBlocks * kPromptWaves, "");
+    return columns * (head_dim + 2) * sizeof(float);
+}
 
 hipError_t attention(const Attention& o, int is_bf16, hipStream_t stream) {
     return is_bf16 ? of_width<uint16_t>(o, stream) : of_width<float>(o, stream);
 }
 
-hipError_t attention_init() { return hipSuccess; }
+hipError_t attention_init() {
+    const void* kernels[] = {(const void*)&attention_prompt_kernel<64, kPromptBlocks>, (const void*)&attention_prompt_kernel<96, kPromptBlocks>,
+                             (const void*)&attention_prompt_kernel<128, kPromptBlocks>, (const void*)&attention_prompt_kernel<256, kPromptBlocks>};
+    const int bytes[] = {prompt_lds<64>(), prompt_lds<96>(), prompt_lds<128>(), prompt_lds<256>()};
+    for (int i = 0; i < 4; ++i) {
+        const hipError_t e = hipFuncSetAttribute(kernels[i], hipFuncAttributeMaxDynamicSharedMemorySize, bytes[i]);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
 
 }  // namespace gelo

@@ -516,7 +516,7 @@ def test_refusals_of_append_and_attention(ctx):
         for bad in ({"k": None}, {"v": None}, {"n_pages": 0}, {"n_kv_heads": 0}, {"page_rows": 0}, {"row_stride": 56}, {"head_stride": 0}, {"page_stride": 8},
                     {"n_seqs": 0}, {"n_rows": 0}, {"max_rows": 0}, {"max_kv_len": 0}, {"kv_len": None}, {"page_table": None}, {"n_rows": 3}, {"max_rows": 2}, {"dtype": 3}):
             assert call(**bad) == "GELO_EINVAL", bad
-        for bad in ({"page_rows": 8}, {"page_rows": 48}, {"table_ld": 1}, {"max_kv_len": 33}, {"row_start": i, "n_rows": (1 << 22) + 1}):
+        for bad in ({"page_rows": 8}, {"page_rows": 48}, {"table_ld": 1}, {"max_kv_len": 33}, {"row_stride": (1 << 24) + 8}, {"row_start": i, "n_rows": (1 << 22) + 1}):
             assert call(**bad) == "GELO_ESHAPE", bad
         for bad in ({"k": x + 8}, {"row_stride": 68}, {"head_stride": 1028}, {"kv_len": i + 2}, {"page_table": i + 1}):
             assert call(**bad) == "GELO_EALIGN", bad
