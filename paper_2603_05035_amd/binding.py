@@ -116,7 +116,10 @@ def _check(ctx, status: int):
 
 def _stream(stream) -> c_void_p:
     if stream is None:
-        stream = torch.cuda.current_stream()
+        # the current stream's handle alone: torch.cuda.current_stream() makes an object around it, 2.7 us of a call's 9
+        if not torch.cuda.is_initialized():
+            torch.cuda.init()
+        return c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
     return c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
 
@@ -132,9 +135,10 @@ def _matrix(t: torch.Tensor, name: str):
     """(pointer, leading dimension) of a 2-D row-major device tensor."""
     if not t.is_cuda:
         raise ValueError(f"{name} must live on the GPU")
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or (shape[1] > 1 and stride[1] != 1):
         raise ValueError(f"{name} must be a row-major 2-D tensor")
-    return c_void_p(t.data_ptr()), int(t.stride(0)) if t.shape[0] > 1 else int(max(t.stride(0), t.shape[1]))
+    return c_void_p(t.data_ptr()), stride[0] if shape[0] > 1 else max(stride[0], shape[1])
 
 
 def gelo_create(device: int = 0, seed: int = 0, allow_batch_reuse: bool = False) -> c_void_p:
@@ -379,7 +383,7 @@ class SeqBatch:
 
 
 def _vector(t: torch.Tensor, name: str, dtype, count: int):
-    if not t.is_cuda or t.dtype != dtype or t.dim() != 1 or t.shape[0] != count or (count > 1 and t.stride(0) != 1):
+    if not t.is_cuda or t.dtype != dtype or t.shape != (count,) or (count > 1 and t.stride(0) != 1):
         raise ValueError(f"{name} must be a contiguous GPU vector of {count} {dtype}")
 
 
@@ -397,26 +401,27 @@ def _rows(batch: SeqBatch, rows: int, cache: KvCache):
 def gelo_rms_norm(ctx, X: torch.Tensor, gamma: torch.Tensor, eps: float, H: torch.Tensor | None = None, residual: torch.Tensor | None = None,
                   residual_out: torch.Tensor | None = None, codes: torch.Tensor | None = None, scales: torch.Tensor | None = None, stream=None):
     """h = X + residual into residual_out, h / rms(h) * gamma into H and, as 8-bit codes with row scales, into codes and scales."""
-    n, d = X.shape
-    code = _dtype_code(X)
-    args = []
-    for name, t in (("X", X), ("residual", residual), ("residual_out", residual_out), ("H", H)):
+    shape, dtype = X.shape, X.dtype
+    n, d = shape
+    args = [*_matrix(X, "X")]
+    for name, t in (("residual", residual), ("residual_out", residual_out), ("H", H)):
         if t is None:
             args += (None, 0)
-            continue
-        if t.dtype != X.dtype or tuple(t.shape) != (n, d):
+        elif t.dtype != dtype or t.shape != shape:
             raise ValueError(f"{name} must be of X's dtype and shape")
-        args += _matrix(t, name)
-    _vector(gamma, "gamma", X.dtype, d)
-    cp, ldq = None, 0
+        else:
+            args += _matrix(t, name)
+    _vector(gamma, "gamma", dtype, d)
+    xp, ldx, rp, ldr, op, ldo, hp, ldh = args
+    cp, ldq, sp = None, 0, None
     if codes is not None or scales is not None:
-        if codes is None or scales is None or codes.dtype != torch.uint8 or tuple(codes.shape) != (n, d):
+        if codes is None or scales is None or codes.dtype != torch.uint8 or codes.shape != shape:
             raise ValueError("codes must be uint8 of X's shape and come with scales")
         cp, ldq = _matrix(codes, "codes")
         _vector(scales, "scales", torch.float32, n)
-    xp, ldx, rp, ldr, op, ldo, hp, ldh = args
-    _check(ctx, load_library().gelo_rms_norm(ctx, code, n, d, xp, ldx, rp, ldr, gamma.data_ptr(), eps, op, ldo, hp, ldh, cp, ldq,
-                                             None if scales is None else scales.data_ptr(), _stream(stream)))
+        sp = scales.data_ptr()
+    _check(ctx, load_library().gelo_rms_norm(ctx, _dtype_code(X), n, d, xp, ldx, rp, ldr, gamma.data_ptr(), eps, op, ldo, hp, ldh, cp, ldq, sp,
+                                             _stream(stream)))
 
 
 def gelo_rope_table(ctx, rot_dim: int, n_pos: int, base: float = 10000.0, factor: float = 1.0, trained: float = 0.0, low: float = 1.0,
@@ -438,7 +443,7 @@ def gelo_rope_append(ctx, QKV: torch.Tensor, n_q_heads: int, cache: KvCache, bat
         raise GeloError(2, f"a row of {width} values is not {n_q_heads} + 2 x {cache.n_kv_heads} heads of {cache.head_dim}")
     qp, ldq = None, 0
     if Q is not None:
-        if Q.dtype != QKV.dtype or Q.dim() != 2 or tuple(Q.shape) != (rows, n_q_heads * cache.head_dim):
+        if Q.dtype != QKV.dtype or Q.shape != (rows, n_q_heads * cache.head_dim):
             raise ValueError("Q must be of QKV's dtype, a row of all query heads for each of its rows")
         qp, ldq = _matrix(Q, "Q")
     tp, n_table = None, 0

@@ -296,7 +296,8 @@ __device__ __forceinline__ void walk_keys(const AttnArgs& a, int seq, int kvh, i
         const bool partly = key + F::KEYS - 1 > min(least, last);
         uint32_t seen = ~0u;
         if (partly) {
-            const int upto = min(limit, last);
+            int upto = min(limit, last);
+            asm volatile("" : "+v"(upto));                   // a branch: as selects it would cost every step
             seen = 0;
 #pragma unroll
             for (int t = 0; t < F::TILES; ++t)
@@ -481,7 +482,8 @@ void attention_prompt_kernel(AttnArgs a) {
     int limit[CB], row[CB], head[CB];
     bf16x8_t q[CB][KS];
     f32x16_t acc[CB][DT];
-    float m[CB], l[CB];
+    float m[CB], base[CB], l[CB];                            // maximum the weights are relative to, the same times scale2, sum
+    const float slack = 8.f / a.scale2;
 #pragma unroll
     for (int b = 0; b < CB; ++b) {
         const int col = min(wave_col + 32 * b + c, columns - 1), i = col / a.group;      // dead columns repeat the last one
@@ -540,6 +542,20 @@ void attention_prompt_kernel(AttnArgs a) {
     };
 
     const int s16 = lane & 15, nh = (lane >> 4) & 1;
+    typedef const bf16x8_t __attribute__((address_space(3))) * k_ptr_t;
+    typedef s16x4_t __attribute__((address_space(3))) * v_ptr_t;
+    // reads of a step: 32 rows of K from row c on, four rows of V and eight below them; a row's chunks lie alike every 16 rows
+    uint32_t k_at[KS], v_at[DT];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) k_at[ks] = lds_base + c * PITCH + 16 * k_pos<D>(c, 2 * ks + h);
+#pragma unroll
+    for (int t = 0; t < DT; ++t) {
+        const int r = 4 * h + (s16 >> 2);
+        v_at[t] = lds_base + (KT + r) * PITCH + 16 * v_pos<D>(r, 4 * t + 2 * nh + ((s16 >> 1) & 1)) + 8 * (s16 & 1);
+    }
+    f32x16_t zero;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) zero[r] = 0.f;
     const int steps = end > begin ? (end - begin + KT - 1) / KT : 0;
     // 0 times a value that is not finite is NaN also in columns that do not see its key.  Such values are rare, and they show in the result: a
     // workgroup that finds any there walks its keys once more with zeros in their place and adds them to the columns that see them.
@@ -550,7 +566,7 @@ void attention_prompt_kernel(AttnArgs a) {
 #pragma unroll
         for (int b = 0; b < CB; ++b) {
             m[b] = -__builtin_inff();
-            l[b] = 0.f;
+            base[b] = l[b] = 0.f;
 #pragma unroll
             for (int t = 0; t < DT; ++t)
 #pragma unroll
@@ -561,19 +577,21 @@ void attention_prompt_kernel(AttnArgs a) {
             fetch(begin, page_of(begin), 0);
             if (steps > 1) page = page_of(begin + KT);
         }
-        for (int step = 0; step < steps; ++step) {
+        // (stages as constants: then no address of the reads changes from step to step)
+        auto one_step = [&](auto stage, int step) {
+            constexpr int AT = decltype(stage)::value;
             const int key = begin + step * KT;
             asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();
             if (step + 1 < steps) {
-                fetch(key + KT, page, (step + 1) & 1);
+                fetch(key + KT, page, AT ^ 1);
                 if (step + 2 < steps) page = page_of(key + 2 * KT);
             }
             if (pass == 1) {
                 // the values that are not finite go, and per component the first key that had one is kept
                 for (int at = threadIdx.x * 16; at < KT * PITCH; at += 64 * kPromptWaves * 16) {
                     const int r = at / PITCH, x = 8 * v_pos<D>(r, (at - r * PITCH) / 16);
-                    s16x8_t* where = reinterpret_cast<s16x8_t*>(lds + (step & 1) * STAGE + KT * PITCH + at);
+                    s16x8_t* where = reinterpret_cast<s16x8_t*>(lds + AT * STAGE + KT * PITCH + at);
                     s16x8_t v = *where;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
@@ -588,84 +606,81 @@ void attention_prompt_kernel(AttnArgs a) {
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                 __builtin_amdgcn_s_barrier();
             }
-            if (key > most) continue;                            // nothing here for this wave's columns
-            const uint32_t k_at = lds_base + (step & 1) * STAGE, v_at = k_at + KT * PITCH;
-            typedef const bf16x8_t __attribute__((address_space(3))) * k_ptr_t;
-            typedef s16x4_t __attribute__((address_space(3))) * v_ptr_t;
+            if (key > most) return;                          // nothing here for this wave's columns
             f32x16_t s[CB][KB];
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb) {
-#pragma unroll
-                for (int b = 0; b < CB; ++b)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) s[b][kb][r] = 0.f;
+            for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) {
-                    const int r = 32 * kb + c;
-                    const bf16x8_t kf = *(k_ptr_t)(size_t)(k_at + r * PITCH + 16 * k_pos<D>(r, 2 * ks + h));
+                    const bf16x8_t kf = *(k_ptr_t)(size_t)(k_at[ks] + (AT * STAGE + 32 * kb * PITCH));
 #pragma unroll
-                    for (int b = 0; b < CB; ++b) s[b][kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[b][ks], s[b][kb], 0, 0, 0);
+                    for (int b = 0; b < CB; ++b) s[b][kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[b][ks], ks == 0 ? zero : s[b][kb], 0, 0, 0);
                 }
-            }
             const bool partly = key + KT - 1 > least;
             bf16x8_t p[CB][2 * KB];
 #pragma unroll
             for (int b = 0; b < CB; ++b) {
                 if (partly) {
-                    const int upto = limit[b] - key;
+                    int upto = limit[b] - key;
+                    asm volatile("" : "+v"(upto));           // a branch: as selects it would cost every step
 #pragma unroll
                     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
                         for (int r = 0; r < 16; ++r)
                             s[b][kb][r] = 32 * kb + 8 * (r >> 2) + 4 * h + (r & 3) <= upto ? s[b][kb][r] : -__builtin_inff();
                 }
-                float top = s[b][0][0];
+                float part[4];
 #pragma unroll
-                for (int kb = 0; kb < KB; ++kb)
+                for (int u = 0; u < 4; ++u) {
+                    part[u] = s[b][0][u];
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][kb][r]);
+                    for (int r = 4 + u; r < 16 * KB; r += 4) part[u] = fmaxf(part[u], s[b][r >> 4][r & 15]);
+                }
+                float top = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
                 top = fmaxf(top, __shfl_xor(top, 32, 64));
-                const float m_new = fmaxf(m[b], top);
-                const float base = m_new == -__builtin_inff() ? 0.f : m_new * a.scale2;
-                const float alpha = __builtin_amdgcn_exp2f(m[b] * a.scale2 - base);
-                if (__ballot(m_new != m[b])) {
+                // any base that leaves the weights in range gives the same quotient: it moves only where a column's maximum has grown by 2^8
+                if (__ballot(top > m[b] + slack)) {
+                    const float m_new = fmaxf(m[b], top);
+                    const float base_new = m_new == -__builtin_inff() ? 0.f : m_new * a.scale2;       // nothing seen yet: all weights are 0
+                    const float alpha = m[b] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(base[b] - base_new);
+                    m[b] = m_new;
+                    base[b] = base_new;
                     l[b] *= alpha;
 #pragma unroll
                     for (int t = 0; t < DT; ++t)
 #pragma unroll
                         for (int r = 0; r < 16; ++r) acc[b][t][r] *= alpha;
                 }
-                m[b] = m_new;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) part[u] = 0.f;
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
-                        const float w = __builtin_amdgcn_exp2f(s[b][kb][r] * a.scale2 - base);
-                        l[b] += w;
+                        const float w = __builtin_amdgcn_exp2f(s[b][kb][r] * a.scale2 - base[b]);
+                        part[r & 3] += w;
                         p[b][2 * kb + (r >> 3)][r & 7] = (__bf16)w;
                     }
+                l[b] += (part[0] + part[1]) + (part[2] + part[3]);
             }
-            // V^T of component block t and the 16 keys of ks
-            auto v_frag = [&](int t, int ks) {
-                s16x8_t f;
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const int r = 16 * ks + 8 * half + 4 * h + (s16 >> 2);
-                    const uint32_t at = v_at + r * PITCH + 16 * v_pos<D>(r, 4 * t + 2 * nh + ((s16 >> 1) & 1)) + 8 * (s16 & 1);
-                    const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v_ptr_t)(size_t)at);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) f[4 * half + e] = x[e];
-                }
-                return f;
-            };
 #pragma unroll
             for (int ks = 0; ks < 2 * KB; ++ks)
 #pragma unroll
                 for (int t = 0; t < DT; ++t) {
-                    const s16x8_t f = v_frag(t, ks);
+                    s16x8_t f;                               // V^T of component block t and the 16 keys of ks
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v_ptr_t)(size_t)(v_at[t] + (AT * STAGE + (16 * ks + 8 * half) * PITCH)));
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) f[4 * half + e] = x[e];
+                    }
 #pragma unroll
                     for (int b = 0; b < CB; ++b) acc[b][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, f), p[b][ks], acc[b][t], 0, 0, 0);
                 }
+        };
+        for (int step = 0; step < steps; step += 2) {
+            one_step(std::integral_constant<int, 0>{}, step);
+            if (step + 1 < steps) one_step(std::integral_constant<int, 1>{}, step + 1);
         }
         if (pass == 1) break;
         bool odd = false;
@@ -704,7 +719,7 @@ void attention_prompt_kernel(AttnArgs a) {
                 if (whole) store4((uint16_t*)a.O + row[b] * a.ldo + (int64_t)head[b] * D + x, o);
                 else *reinterpret_cast<f32x4_t*>(a.part_o + part * D + x) = o;
             }
-        if (!whole && h == 0) { a.part_ml[2 * part] = total == 0.f ? -__builtin_inff() : m[b] * a.scale2; a.part_ml[2 * part + 1] = total; }
+        if (!whole && h == 0) { a.part_ml[2 * part] = total == 0.f ? -__builtin_inff() : base[b]; a.part_ml[2 * part + 1] = total; }
     }
 }
 
