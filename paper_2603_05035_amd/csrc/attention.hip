@@ -418,10 +418,12 @@ void attention_few_kernel(AttnArgs a) {
 }
 
 // attention_prompt_kernel: many columns to a key head, bfloat16.  Bound by the matrix instructions and, beside them, by the exponentials.  A
-// workgroup takes kPromptWaves x 32 CB columns and walks the keys KT at a time; K and V of a step come into LDS once for all its waves, by
+// workgroup takes kPromptWaves x 32 columns and walks the keys kPromptKeys at a time; K and V come into LDS once for all its waves, by
 // direct-to-LDS fetches a step ahead.  v_mfma_f32_32x32x16_bf16: lane (h, c) = (lane / 32, lane % 32); S^T of 32 keys leaves in register r of
 // the lane column c and key 8 (r / 4) + 4 h + r % 4, so registers 8 t ... 8 t + 7 are keys 16 t + {4 h + 0..3, 8 + 4 h + 0..3}: the B operand of step t
 // of O^T, if A = V^T takes its keys in that order - two transposing reads of four rows each.
+// A wave works on three groups of 32 keys at once, whose instructions depend on nothing of each other: the scores of the next group and the
+// weighted sum of the last one (matrix pipe) beside the weights of the present one (vector pipe).
 constexpr int kPromptWaves = 4;
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
@@ -432,8 +434,8 @@ __device__ __forceinline__ void fetch16(uint32_t offset, const void* base, uint3
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" :: "v"(offset), "s"(base), "s"(lds_addr) : "memory", "m0");
 }
 
-template <int D> constexpr int prompt_keys() { return D == 256 ? 32 : 64; }
-template <int D> constexpr int prompt_lds() { return 2 * 2 * prompt_keys<D>() * D * 2; }
+constexpr int kPromptKeys = 64;
+template <int D> constexpr int prompt_lds() { return 2 * 2 * kPromptKeys * D * 2; }        // two steps of K, then two of V
 
 // Where the 16-byte chunk c of row r lies in its row.  K: 16 lanes read the same chunk of 16 rows in a row; V: half a wave reads four chunks of
 // four rows.  Either has to meet all 64 banks: 16 chunks of 16 bytes are a round of them.
@@ -452,11 +454,11 @@ template <int D> __device__ __forceinline__ int v_pos(int r, int c) {          /
     else return c ^ ((r & 3) << 2);
 }
 
-template <int D, int CB>
-__global__ __launch_bounds__(64 * kPromptWaves, CB == 1 && D < 256 ? 2 : 1)
+template <int D>
+__global__ __launch_bounds__(64 * kPromptWaves, D < 256 ? 2 : 1)
 void attention_prompt_kernel(AttnArgs a) {
-    constexpr int KT = prompt_keys<D>(), KB = KT / 32, KS = D / 16, DT = D / 32, PITCH = 2 * D, STAGE = 2 * KT * PITCH;
-    constexpr int ROWS = KT / kPromptWaves;                  // rows a wave fetches: 16 or 8
+    constexpr int KT = kPromptKeys, KS = D / 16, DT = D / 32, PITCH = 2 * D, SLOT = KT * PITCH, WIDE = 32 * kPromptWaves;
+    constexpr int ROWS = KT / kPromptWaves;                  // rows a wave fetches
     constexpr int NF = ROWS * PITCH / 1024;                  // fetches of 1 KB for them
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
     int set, item;
@@ -464,141 +466,234 @@ void attention_prompt_kernel(AttnArgs a) {
     const int kvh = set % a.kv.n_kv_heads, seq = set / a.kv.n_kv_heads;
     const int chunk = item % a.n_chunks, tile = a.col_tiles - 1 - item / a.n_chunks;      // the columns that see most first
     const NewRows rows = rows_of_sequence(a.b, seq);
-    const int columns = rows.count * a.group, first_col = tile * (32 * CB * kPromptWaves);
+    const int columns = rows.count * a.group, first_col = tile * WIDE;
     if (first_col >= columns) return;
     const int kv_len = a.b.kv_len[seq], kv_end = min(kv_len, a.b.max_kv_len);
     const int lane = threadIdx.x & 63, h = lane >> 5, c = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
     auto limit_of = [&](int col) { return min(a.causal ? kv_len - rows.count + col / a.group : kv_len - 1, kv_end - 1); };
-    const int wg_most = limit_of(min(first_col + 32 * CB * kPromptWaves, columns) - 1);
+    const int wg_most = limit_of(min(first_col + WIDE, columns) - 1);
     const int begin = chunk * a.chunk, end = min(begin + a.chunk, wg_most + 1);
     if (begin >= end && a.n_chunks > 1) return;
+    const int last = end - 1, steps = end > begin ? (end - begin + KT - 1) / KT : 0;
 
-    // this wave's columns
-    const int wave_col = first_col + wave * 32 * CB;
-    const bool awake = wave_col < columns;
-    const int most = awake ? limit_of(min(wave_col + 32 * CB, columns) - 1) : -1, least = awake ? limit_of(wave_col) : -1;
-    int limit[CB], row[CB], head[CB];
-    bf16x8_t q[CB][KS];
-    f32x16_t acc[CB][DT];
-    float m[CB], base[CB], l[CB];                            // maximum the weights are relative to, the same times scale2, sum
-    const float slack = 8.f / a.scale2;
+    // fetches: this wave's 16 rows of a step, 1 KB at a time; the keys of 16 rows share a page
+    const uint32_t lds_base = __builtin_amdgcn_readfirstlane((uint32_t)(size_t)lds);
+    const uint32_t my_rows = lds_base + wave * ROWS * PITCH;
+    uint32_t k_off[NF], v_off[NF];
+    const int shift = a.kv.page_shift, in_page = (1 << shift) - 1;
+    const int32_t* table = a.b.page_table + seq * a.b.table_ld;
+    const uint16_t* k_head = (const uint16_t*)a.kv.k + kvh * a.kv.head_stride;
+    const uint16_t* v_head = (const uint16_t*)a.kv.v + kvh * a.kv.head_stride;
+    bool bad_page = false;
+    auto group_of = [&](int step) { return min(begin + step * KT + wave * ROWS, last & ~(ROWS - 1)); };
+    // (a vector load: beside a scalar one every wait for LDS would be a wait for it as well)
+    auto load_page = [&](int step) { return table[(group_of(min(step, steps - 1)) + (lane >> 6)) >> shift]; };
+    auto rows_at = [&](int step, int page) {                 // values from the start of a head to these rows
+        const bool good = page >= 0 && page < a.kv.n_pages;
+        bad_page |= !good;
+        return (good ? page : 0) * a.kv.page_stride + (group_of(step) & in_page) * a.kv.row_stride;
+    };
+    // rows beyond the last key are fetched as that key's (they are masked, but 0 times what lies there might be NaN): in the last step
+    auto trim = [&](uint32_t (&off)[NF], int step) {
+        const int there = last - group_of(step);             // last row of the 16 that is there
+        if (step < steps - 1 || there >= ROWS - 1) return;
 #pragma unroll
-    for (int b = 0; b < CB; ++b) {
-        const int col = min(wave_col + 32 * b + c, columns - 1), i = col / a.group;      // dead columns repeat the last one
-        limit[b] = limit_of(col);
-        row[b] = rows.first + i;
-        head[b] = kvh * a.group + col - i * a.group;
-        const uint16_t* p = (const uint16_t*)a.Q + row[b] * a.ldq + (int64_t)head[b] * D + 8 * h;
+        for (int i = 0; i < NF; ++i) off[i] -= (uint32_t)(max((i * 1024 + lane * 16) / PITCH - there, 0) * (int)a.kv.row_stride) * 2;
+    };
+
+    // this wave's columns, one to a lane (and to the lane 32 further on)
+    const int wave_col = first_col + wave * 32;
+    const bool awake = wave_col < columns;
+    const int most = awake ? min(limit_of(min(wave_col + 32, columns) - 1), last) : -1, least = awake ? limit_of(wave_col) : -1;
+    const int my_steps = most >= begin ? (most - begin) / KT + 1 : 0;
+    const int col = min(wave_col + c, columns - 1);          // dead columns repeat the last one
+    const int limit = limit_of(col), row = rows.first + col / a.group, head = kvh * a.group + col % a.group;
+    bf16x8_t q[KS];
+    {
+        const uint16_t* p = (const uint16_t*)a.Q + row * a.ldq + (int64_t)head * D + 8 * h;
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             u32x4_t w = *reinterpret_cast<const u32x4_t*>(p + 16 * s);
 #pragma unroll
             for (int e = 0; e < 4; ++e) w[e] ^= a.flip;
-            q[b][s] = __builtin_bit_cast(bf16x8_t, w);
+            q[s] = __builtin_bit_cast(bf16x8_t, w);
         }
     }
+    f32x16_t acc[DT], s[2], zero;
+    bf16x8_t p[2][2];                                        // weights of two groups of 32 keys
+    float m, base, l;                                        // the maximum that weights are relative to, times scale2 as a whole number, their sum
+    const float slack = 8.f / a.scale2;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) zero[r] = 0.f;
 
-    // fetches: this wave's rows of a step, 1 KB at a time; the keys of 16 rows share a page
-    const uint32_t lds_base = __builtin_amdgcn_readfirstlane((uint32_t)(size_t)lds);
-    uint32_t k_off[NF], v_off[NF];
-#pragma unroll
-    for (int i = 0; i < NF; ++i) {
-        const int at = i * 1024 + lane * 16, r = at / PITCH, p = (at - r * PITCH) / 16, rr = wave * ROWS + r;
-        k_off[i] = (uint32_t)(r * (int)a.kv.row_stride + 8 * k_chunk<D>(rr, p)) * 2;
-        v_off[i] = (uint32_t)(r * (int)a.kv.row_stride + 8 * v_pos<D>(rr, p)) * 2;
-    }
-    const int last = end - 1, shift = a.kv.page_shift, in_page = (1 << shift) - 1;
-    const int32_t* table = a.b.page_table + seq * a.b.table_ld;
-    const uint16_t* k_head = (const uint16_t*)a.kv.k + kvh * a.kv.head_stride;
-    const uint16_t* v_head = (const uint16_t*)a.kv.v + kvh * a.kv.head_stride;
-    bool bad_page = false;
-    // rows beyond the last key are fetched as that key's (they are masked, but 0 times what lies there might be NaN)
-    auto group_of = [&](int key) { return min(key + wave * ROWS, last & ~(ROWS - 1)); };
-    auto page_of = [&](int key) { return table[group_of(key) >> shift]; };
-    auto fetch = [&](int key, int page, int stage) {
-        const bool good = page >= 0 && page < a.kv.n_pages;
-        bad_page |= !good;
-        const int64_t at = (good ? page : 0) * a.kv.page_stride + (group_of(key) & in_page) * a.kv.row_stride;
-        const uint16_t* kp = k_head + at;
-        const uint16_t* vp = v_head + at;
-        const uint32_t to = lds_base + stage * STAGE + wave * ROWS * PITCH;
-        const int over = group_of(key) + ROWS - 1 - last;    // rows that are not there
-        if (over <= 0) {
-#pragma unroll
-            for (int i = 0; i < NF; ++i) fetch16(k_off[i], kp, to + i * 1024);
-#pragma unroll
-            for (int i = 0; i < NF; ++i) fetch16(v_off[i], vp, to + KT * PITCH + i * 1024);
-        } else {
-#pragma unroll
-            for (int i = 0; i < NF; ++i) {
-                const int r = (i * 1024 + lane * 16) / PITCH, back = max(r - (ROWS - 1 - over), 0);
-                const uint32_t by = (uint32_t)(back * (int)a.kv.row_stride) * 2;
-                fetch16(k_off[i] - by, kp, to + i * 1024);
-                fetch16(v_off[i] - by, vp, to + KT * PITCH + i * 1024);
-            }
-        }
-    };
-
-    const int s16 = lane & 15, nh = (lane >> 4) & 1;
+    // reads of a step: 32 rows of K from row c on, four rows of V and eight below them; a row's chunks lie alike every 16 rows
+    typedef uint8_t __attribute__((address_space(3))) * lds_ptr_t;
     typedef const bf16x8_t __attribute__((address_space(3))) * k_ptr_t;
     typedef s16x4_t __attribute__((address_space(3))) * v_ptr_t;
-    // reads of a step: 32 rows of K from row c on, four rows of V and eight below them; a row's chunks lie alike every 16 rows
-    uint32_t k_at[KS], v_at[DT];
+    const int s16 = lane & 15, nh = (lane >> 4) & 1;
+    lds_ptr_t k_at[KS], v_at[DT];
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) k_at[ks] = lds_base + c * PITCH + 16 * k_pos<D>(c, 2 * ks + h);
+    for (int ks = 0; ks < KS; ++ks) k_at[ks] = (lds_ptr_t)lds + (c * PITCH + 16 * k_pos<D>(c, 2 * ks + h));
 #pragma unroll
     for (int t = 0; t < DT; ++t) {
         const int r = 4 * h + (s16 >> 2);
-        v_at[t] = lds_base + (KT + r) * PITCH + 16 * v_pos<D>(r, 4 * t + 2 * nh + ((s16 >> 1) & 1)) + 8 * (s16 & 1);
+        v_at[t] = (lds_ptr_t)lds + (3 * SLOT + r * PITCH + 16 * v_pos<D>(r, 4 * t + 2 * nh + ((s16 >> 1) & 1)) + 8 * (s16 & 1));
     }
-    f32x16_t zero;
+    // The matrix instructions of a group, in this order: KS for the scores of 32 keys, whose rows begin `kfrom` bytes into the slots of K, then
+    // KS for the weighted values of 32 others, `vfrom` bytes into those of V.  Each has one fragment to read, AHEAD instructions before.
+    constexpr int N = 2 * KS, AHEAD = 3;
+    auto read_k = [&](int ks, int kfrom) { return *(k_ptr_t)(k_at[ks] + (kfrom)); };
+    auto read_v = [&](int j, int vfrom) {                    // V^T of component block j % DT and 16 keys
+        s16x8_t f;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) zero[r] = 0.f;
-    const int steps = end > begin ? (end - begin + KT - 1) / KT : 0;
+        for (int half = 0; half < 2; ++half) {
+            const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v_ptr_t)(v_at[j % DT] + (vfrom + (16 * (j / DT) + 8 * half) * PITCH)));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f[4 * half + e] = x[e];
+        }
+        return __builtin_bit_cast(bf16x8_t, f);
+    };
+    // Both go from slot to slot in the middle of a step: K then reads the next step's, V this one's.
+    auto turn_addresses = [&](int by) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) k_at[ks] += by;
+#pragma unroll
+        for (int t = 0; t < DT; ++t) v_at[t] -= by;
+    };
+    // The largest of 16 scores, in four pieces.
+    float top2[2], top = 0.f;
+    auto top_piece = [&](auto ic, const f32x16_t& x) {
+        constexpr int i = decltype(ic)::value;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            if constexpr (i == 0) top2[u] = fmaxf(fmaxf(x[8 * u], x[8 * u + 1]), x[8 * u + 2]);
+            else if constexpr (i < 3) top2[u] = fmaxf(fmaxf(top2[u], x[8 * u + 2 * i + 1]), x[8 * u + 2 * i + 2]);
+        }
+        if constexpr (i == 3) top = fmaxf(fmaxf(top2[0], x[7]), fmaxf(top2[1], x[15]));
+    };
+    // Weights of the 32 keys from `key` on, whose scores are s[G] and whose largest score is top; beside them the scores of the next group, their
+    // largest one, and the weighted values of the one before.  The order is kept as it stands here (sched_barrier): a matrix instruction, and
+    // while it runs a read, a share of the weights and extra(slot).
+    auto group = [&](auto g, auto kfrom, auto vfrom, int key, auto&& extra) {
+        constexpr int G = decltype(g)::value, KFROM = decltype(kfrom)::value, VFROM = decltype(vfrom)::value;
+        bf16x8_t frag[AHEAD + 1];
+        static_for<AHEAD>([&](auto ic) { frag[decltype(ic)::value] = read_k(decltype(ic)::value, KFROM); });
+        if (key + 31 > min(least, last)) {
+            int upto = min(limit, last) - key;
+            asm volatile("" : "+v"(upto));                   // a branch: as selects it would cost every step
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[G][r] = 8 * (r >> 2) + 4 * h + (r & 3) <= upto ? s[G][r] : -__builtin_inff();
+            static_for<4>([&](auto ic) { top_piece(ic, s[G]); });
+        }
+        // any base that leaves the weights in range gives the same quotient: it moves only where a column's maximum has grown by 2^8, and by
+        // whole powers of two, which scale everything there is without a rounding
+        if (__ballot(top > m + slack)) {
+            const float m_new = fmaxf(m, fmaxf(top, __shfl_xor(top, 32, 64)));
+            const float base_new = m_new == -__builtin_inff() ? 0.f : rintf(m_new * a.scale2);       // nothing seen yet: all weights are 0
+            const float alpha = m == -__builtin_inff() ? 0.f : ldexpf(1.f, (int)fmaxf(base - base_new, -200.f));
+            m = m_new;
+            base = base_new;
+            l *= alpha;
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[t][r] *= alpha;
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) p[G ^ 1][ks][e] = (__bf16)((float)p[G ^ 1][ks][e] * alpha);
+        }
+        float part[2] = {0.f, 0.f};
+        __builtin_amdgcn_sched_barrier(0);
+        static_for<N>([&](auto ic) {
+            constexpr int i = decltype(ic)::value, ahead = i + AHEAD;
+            if constexpr (ahead < KS) frag[ahead % (AHEAD + 1)] = read_k(ahead, KFROM);
+            else if constexpr (ahead < N) frag[ahead % (AHEAD + 1)] = read_v(ahead - KS, VFROM);
+            if constexpr (i < KS) s[G ^ 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[i % (AHEAD + 1)], q[i], i == 0 ? zero : s[G ^ 1], 0, 0, 0);
+            else acc[(i - KS) % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[i % (AHEAD + 1)], p[G ^ 1][(i - KS) / DT], acc[(i - KS) % DT], 0, 0, 0);
+            static_for<(i + 1) * 16 / N - i * 16 / N>([&](auto rc) {
+                constexpr int r = i * 16 / N + decltype(rc)::value;
+                const float w = __builtin_amdgcn_exp2f(s[G][r] * a.scale2 - base);
+                part[r & 1] += w;
+                asm volatile("" : "+v"(part[r & 1]));        // here: extra() may hold branches, behind which it would sink to its use
+                s[G][r] = w;
+                if constexpr (r % 2 == 1) { p[G][r >> 3][(r & 7) - 1] = (__bf16)s[G][r - 1]; p[G][r >> 3][r & 7] = (__bf16)w; }
+            });
+            // (the scores are there two instructions after the last of them)
+            constexpr int j = i - KS - 2, SPAN = KS - 2;
+            if constexpr (j >= 0) static_for<(j + 1) * 4 / SPAN - j * 4 / SPAN>([&](auto x) { top_piece(std::integral_constant<int, j * 4 / SPAN + decltype(x)::value>{}, s[G ^ 1]); });
+            extra(ic);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        l += part[0] + part[1];
+        asm volatile("" :: "v"(p[G][0]), "v"(p[G][1]), "v"(s[G ^ 1]), "v"(l), "v"(top));      // here, and not where they are used next
+    };
+    constexpr std::integral_constant<int, 0> c0{};
+    constexpr std::integral_constant<int, 1> c1{};
+    constexpr std::integral_constant<int, 0> first{};                // where the two groups of a step begin in a slot
+    constexpr std::integral_constant<int, 32 * PITCH> second{};
+
     // 0 times a value that is not finite is NaN also in columns that do not see its key.  Such values are rare, and they show in the result: a
     // workgroup that finds any there walks its keys once more with zeros in their place and adds them to the columns that see them.
     __shared__ int any_odd, any_bad, first_odd[2][D];
     if (threadIdx.x == 0) any_odd = any_bad = 0;
     for (int x = threadIdx.x; x < 2 * D; x += 64 * kPromptWaves) (&first_odd[0][0])[x] = 0x7FFFFFFF;
     for (int pass = 0;; ++pass) {
+        m = -__builtin_inff();
+        base = l = 0.f;
 #pragma unroll
-        for (int b = 0; b < CB; ++b) {
-            m[b] = -__builtin_inff();
-            base[b] = l[b] = 0.f;
+        for (int t = 0; t < DT; ++t) acc[t] = zero;
 #pragma unroll
-            for (int t = 0; t < DT; ++t)
+        for (int e = 0; e < 8; ++e) p[1][0][e] = p[1][1][e] = (__bf16)0.f;
+        // nothing comes before the first group: no weights, and zeros in the place of its values
+        for (int x = threadIdx.x * 16; x < 32 * PITCH; x += 64 * kPromptWaves * 16) *reinterpret_cast<u32x4_t*>(lds + 3 * SLOT + 32 * PITCH + x) = u32x4_t{0, 0, 0, 0};
+        int page = 0;                                        // in a lane's register: of the step three further on
+        int64_t k_rows = 0, v_rows = 0;                      // where the rows of the next fetches begin
 #pragma unroll
-                for (int r = 0; r < 16; ++r) acc[b][t][r] = 0.f;
+        for (int i = 0; i < NF; ++i) {
+            const int at = i * 1024 + lane * 16, r = at / PITCH, x = (at - r * PITCH) / 16, rr = wave * ROWS + r;
+            k_off[i] = (uint32_t)(r * (int)a.kv.row_stride + 8 * k_chunk<D>(rr, x)) * 2;
+            v_off[i] = (uint32_t)(r * (int)a.kv.row_stride + 8 * v_pos<D>(rr, x)) * 2;
         }
-        int page = 0;
         if (steps > 0) {
-            fetch(begin, page_of(begin), 0);
-            if (steps > 1) page = page_of(begin + KT);
+            const int page0 = load_page(0), page1 = load_page(1);
+            page = load_page(2);
+            v_rows = rows_at(0, __builtin_amdgcn_readfirstlane(page0));
+            trim(k_off, 0);
+#pragma unroll
+            for (int i = 0; i < NF; ++i) fetch16(k_off[i], k_head + v_rows, my_rows + i * 1024);
+            if (steps > 1) {
+                k_rows = rows_at(1, __builtin_amdgcn_readfirstlane(page1));
+                trim(k_off, 1);
+#pragma unroll
+                for (int i = 0; i < NF; ++i) fetch16(k_off[i], k_head + k_rows, my_rows + SLOT + i * 1024);
+            }
+            trim(v_off, 0);
+#pragma unroll
+            for (int i = 0; i < NF; ++i) fetch16(v_off[i], v_head + v_rows, my_rows + 2 * SLOT + i * 1024);
+            if (steps > 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(2 * NF) : "memory");
+            else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(NF) : "memory");
+            __builtin_amdgcn_s_barrier();
         }
-        // (stages as constants: then no address of the reads changes from step to step)
-        auto one_step = [&](auto stage, int step) {
-            constexpr int AT = decltype(stage)::value;
-            const int key = begin + step * KT;
+        int step = 0;
+        // between the two groups of a step: its V and the next step's K are there
+        auto turn = [&] {
             asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();
-            if (step + 1 < steps) {
-                fetch(key + KT, page, AT ^ 1);
-                if (step + 2 < steps) page = page_of(key + 2 * KT);
-            }
             if (pass == 1) {
                 // the values that are not finite go, and per component the first key that had one is kept
-                for (int at = threadIdx.x * 16; at < KT * PITCH; at += 64 * kPromptWaves * 16) {
-                    const int r = at / PITCH, x = 8 * v_pos<D>(r, (at - r * PITCH) / 16);
-                    s16x8_t* where = reinterpret_cast<s16x8_t*>(lds + AT * STAGE + KT * PITCH + at);
+                for (int x = threadIdx.x * 16; x < SLOT; x += 64 * kPromptWaves * 16) {
+                    const int r = x / PITCH, d = 8 * v_pos<D>(r, (x - r * PITCH) / 16);
+                    s16x8_t* where = reinterpret_cast<s16x8_t*>(lds + (2 + (step & 1)) * SLOT + x);
                     s16x8_t v = *where;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         if ((v[e] & 0x7F80) != 0x7F80) continue;
                         const bool nan = v[e] & 0x7F;
-                        if (nan || v[e] > 0) atomicMin(&first_odd[0][x + e], key + r);
-                        if (nan || v[e] < 0) atomicMin(&first_odd[1][x + e], key + r);
+                        if (nan || v[e] > 0) atomicMin(&first_odd[0][d + e], begin + step * KT + r);
+                        if (nan || v[e] < 0) atomicMin(&first_odd[1][d + e], begin + step * KT + r);
                         v[e] = 0;
                     }
                     *where = v;
@@ -606,121 +701,79 @@ void attention_prompt_kernel(AttnArgs a) {
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                 __builtin_amdgcn_s_barrier();
             }
-            if (key > most) return;                          // nothing here for this wave's columns
-            f32x16_t s[CB][KB];
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    const bf16x8_t kf = *(k_ptr_t)(size_t)(k_at[ks] + (AT * STAGE + 32 * kb * PITCH));
-#pragma unroll
-                    for (int b = 0; b < CB; ++b) s[b][kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[b][ks], ks == 0 ? zero : s[b][kb], 0, 0, 0);
-                }
-            const bool partly = key + KT - 1 > least;
-            bf16x8_t p[CB][2 * KB];
-#pragma unroll
-            for (int b = 0; b < CB; ++b) {
-                if (partly) {
-                    int upto = limit[b] - key;
-                    asm volatile("" : "+v"(upto));           // a branch: as selects it would cost every step
-#pragma unroll
-                    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            s[b][kb][r] = 32 * kb + 8 * (r >> 2) + 4 * h + (r & 3) <= upto ? s[b][kb][r] : -__builtin_inff();
-                }
-                float part[4];
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    part[u] = s[b][0][u];
-#pragma unroll
-                    for (int r = 4 + u; r < 16 * KB; r += 4) part[u] = fmaxf(part[u], s[b][r >> 4][r & 15]);
-                }
-                float top = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
-                top = fmaxf(top, __shfl_xor(top, 32, 64));
-                // any base that leaves the weights in range gives the same quotient: it moves only where a column's maximum has grown by 2^8
-                if (__ballot(top > m[b] + slack)) {
-                    const float m_new = fmaxf(m[b], top);
-                    const float base_new = m_new == -__builtin_inff() ? 0.f : m_new * a.scale2;       // nothing seen yet: all weights are 0
-                    const float alpha = m[b] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(base[b] - base_new);
-                    m[b] = m_new;
-                    base[b] = base_new;
-                    l[b] *= alpha;
-#pragma unroll
-                    for (int t = 0; t < DT; ++t)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) acc[b][t][r] *= alpha;
-                }
-#pragma unroll
-                for (int u = 0; u < 4; ++u) part[u] = 0.f;
-#pragma unroll
-                for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const float w = __builtin_amdgcn_exp2f(s[b][kb][r] * a.scale2 - base[b]);
-                        part[r & 3] += w;
-                        p[b][2 * kb + (r >> 3)][r & 7] = (__bf16)w;
-                    }
-                l[b] += (part[0] + part[1]) + (part[2] + part[3]);
-            }
-#pragma unroll
-            for (int ks = 0; ks < 2 * KB; ++ks)
-#pragma unroll
-                for (int t = 0; t < DT; ++t) {
-                    s16x8_t f;                               // V^T of component block t and the 16 keys of ks
-#pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v_ptr_t)(size_t)(v_at[t] + (AT * STAGE + (16 * ks + 8 * half) * PITCH)));
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) f[4 * half + e] = x[e];
-                    }
-#pragma unroll
-                    for (int b = 0; b < CB; ++b) acc[b][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, f), p[b][ks], acc[b][t], 0, 0, 0);
-                }
         };
-        for (int step = 0; step < steps; step += 2) {
-            one_step(std::integral_constant<int, 0>{}, step);
-            if (step + 1 < steps) one_step(std::integral_constant<int, 1>{}, step + 1);
+        // what follows it: V of the next step and K of the one after are sent for, in 1 + 2 NF pieces
+        auto send = [&](auto ic) {
+            constexpr int i = decltype(ic)::value;
+            const int at = step & 1;
+            if constexpr (i == 0) {
+                if (step + 1 < steps) {
+                    v_rows = k_rows;
+                    trim(v_off, step + 1);
+                    if (step + 2 < steps) {
+                        k_rows = rows_at(step + 2, __builtin_amdgcn_readfirstlane(page));
+                        trim(k_off, step + 2);
+                    }
+                    page = load_page(step + 3);
+                }
+            } else if constexpr (i <= NF) {
+                if (step + 1 < steps) fetch16(v_off[i - 1], v_head + v_rows, my_rows + (3 - at) * SLOT + (i - 1) * 1024);
+            } else if constexpr (i <= 2 * NF) {
+                if (step + 2 < steps) fetch16(k_off[i - 1 - NF], k_head + k_rows, my_rows + at * SLOT + (i - 1 - NF) * 1024);
+            }
+        };
+        // Behind the last step there is nothing to score: what its second group multiplies beside its weights is not used.
+        if (my_steps > 0) {
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_k(ks, 0), q[ks], ks == 0 ? zero : s[0], 0, 0, 0);
+            static_for<4>([&](auto ic) { top_piece(ic, s[0]); });
+            do {
+                group(c0, second, second, begin + step * KT, [](auto) {});
+                turn();
+                turn_addresses(step & 1 ? -SLOT : SLOT);
+                group(c1, first, first, begin + step * KT + 32, send);
+            } while (++step < my_steps);
+#pragma unroll
+            for (int j = 0; j < KS; ++j) acc[j % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_v(j, 32 * PITCH), p[1][j / DT], acc[j % DT], 0, 0, 0);
+            if (pass == 0 && (my_steps & 1)) turn_addresses(-SLOT);      // as they were
+        }
+        for (; step < steps; ++step) {                       // for the other waves
+            turn();
+            static_for<1 + 2 * NF>([&](auto ic) { send(ic); });
         }
         if (pass == 1) break;
         bool odd = false;
 #pragma unroll
-        for (int b = 0; b < CB; ++b)
+        for (int t = 0; t < DT; ++t)
 #pragma unroll
-            for (int t = 0; t < DT; ++t)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) odd |= (__float_as_uint(acc[b][t][r]) & 0x7F800000u) == 0x7F800000u;
+            for (int r = 0; r < 16; ++r) odd |= (__float_as_uint(acc[t][r]) & 0x7F800000u) == 0x7F800000u;
         __syncthreads();
         if (odd) any_odd = 1;
         if (bad_page) any_bad = 1;                           // a page that is not there: any wave may have met it
         __syncthreads();
         if (!any_odd) break;
     }
-    if (!awake) return;
+    if (wave_col + c >= columns) return;
     const bool whole = a.n_chunks == 1;
+    float total = l + __shfl_xor(l, 32, 64);
+    if (any_bad) total = __builtin_nanf("");
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+    const int64_t part = ((int64_t)chunk * a.b.n_rows + row) * a.n_q_heads + head;
 #pragma unroll
-    for (int b = 0; b < CB; ++b) {
-        if (wave_col + 32 * b + c >= columns) continue;
-        float total = l[b] + __shfl_xor(l[b], 32, 64);
-        if (any_bad) total = __builtin_nanf("");
-        const float inv = total == 0.f ? 0.f : 1.f / total;
-        const int64_t part = ((int64_t)chunk * a.b.n_rows + row[b]) * a.n_q_heads + head[b];
+    for (int t = 0; t < DT; ++t)
 #pragma unroll
-        for (int t = 0; t < DT; ++t)
+        for (int e = 0; e < 4; ++e) {
+            const int x = 32 * t + 8 * e + 4 * h;
+            f32x4_t o;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int x = 32 * t + 8 * e + 4 * h;
-                f32x4_t o;
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    o[u] = total == 0.f ? 0.f : whole ? acc[b][t][4 * e + u] * inv : acc[b][t][4 * e + u];
-                    if (any_odd) o[u] += (first_odd[0][x + u] <= limit[b] ? __builtin_inff() : 0.f) - (first_odd[1][x + u] <= limit[b] ? __builtin_inff() : 0.f);
-                }
-                if (whole) store4((uint16_t*)a.O + row[b] * a.ldo + (int64_t)head[b] * D + x, o);
-                else *reinterpret_cast<f32x4_t*>(a.part_o + part * D + x) = o;
+            for (int u = 0; u < 4; ++u) {
+                o[u] = total == 0.f ? 0.f : whole ? acc[t][4 * e + u] * inv : acc[t][4 * e + u];
+                if (any_odd) o[u] += (first_odd[0][x + u] <= limit ? __builtin_inff() : 0.f) - (first_odd[1][x + u] <= limit ? __builtin_inff() : 0.f);
             }
-        if (!whole && h == 0) { a.part_ml[2 * part] = total == 0.f ? -__builtin_inff() : base[b]; a.part_ml[2 * part + 1] = total; }
-    }
+            if (whole) store4((uint16_t*)a.O + row * a.ldo + (int64_t)head * D + x, o);
+            else *reinterpret_cast<f32x4_t*>(a.part_o + part * D + x) = o;
+        }
+    if (!whole && h == 0) { a.part_ml[2 * part] = total == 0.f ? -__builtin_inff() : base; a.part_ml[2 * part + 1] = total; }
 }
 
 // Joins the chunks' parts of a row's head: O = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.
@@ -778,13 +831,12 @@ struct Plan { bool prompt; int col_tiles, chunk, n_chunks; int64_t workgroups; }
 constexpr int64_t kMostWorkgroups = 1 << 23;     // of a launch: 2^31 threads and no more fit HIP's 32-bit counts
 constexpr int kFewTarget = 1024, kFewLeast = 256;        // workgroups that fill the chip, keys to a chunk at least
 constexpr int kPromptTarget = 512, kPromptLeast = 256;
-constexpr int kPromptBlocks = 1;                 // blocks of 32 columns to a wave
 
 Plan plan_of(const Attention& o, int is_bf16) {
     Plan p;
     const int64_t columns = (int64_t)o.batch.max_rows * (o.n_q_heads / o.cache.n_kv_heads);
     p.prompt = is_bf16 && columns > 16;
-    const int wide = p.prompt ? 32 * kPromptBlocks * kPromptWaves : 16, target = p.prompt ? kPromptTarget : kFewTarget, least = p.prompt ? kPromptLeast : kFewLeast;
+    const int wide = p.prompt ? 32 * kPromptWaves : 16, target = p.prompt ? kPromptTarget : kFewTarget, least = p.prompt ? kPromptLeast : kFewLeast;
     p.col_tiles = (int)((columns + wide - 1) / wide);
     const int64_t sets = (int64_t)o.batch.n_seqs * o.cache.n_kv_heads, tiles = sets * p.col_tiles;
     const int64_t most = (o.batch.max_kv_len + least - 1) / least;
@@ -818,7 +870,7 @@ hipError_t launch(const Attention& o, hipStream_t stream) {
     a.part_ml = p.n_chunks == 1 ? nullptr : o.workspace + (int64_t)p.n_chunks * items * D;
     if constexpr (sizeof(T) == 2) {
         if (p.prompt)
-            hipLaunchKernelGGL((attention_prompt_kernel<D, kPromptBlocks>), dim3((unsigned)p.workgroups), dim3(64 * kPromptWaves), (size_t)prompt_lds<D>(), stream, a);
+            hipLaunchKernelGGL((attention_prompt_kernel<D>), dim3((unsigned)p.workgroups), dim3(64 * kPromptWaves), (size_t)prompt_lds<D>(), stream, a);
     }
     if (!p.prompt) hipLaunchKernelGGL((attention_few_kernel<T, D>), dim3((unsigned)p.workgroups), dim3(64 * kFewWaves), 0, stream, a);
     hipError_t e = hipGetLastError();
@@ -846,8 +898,8 @@ bool attention_fits(const Attention& o, int is_bf16) {
 size_t attention_workspace_bytes(const Attention& o, int is_bf16) { return part_bytes(o, plan_of(o, is_bf16)); }
 // a plan of more than one chunk has at most its target of workgroups, and every row's head is a column of one of them
 size_t attention_workspace_bound(int head_dim) {
-    const size_t columns = kPromptTarget * 32 * kPromptBlocks * kPromptWaves;
-    static_assert(kFewTarget * 16 <= kPromptTarget * 32 * kPromptBlocks * kPromptWaves, "");
+    const size_t columns = kPromptTarget * 32 * kPromptWaves;
+    static_assert(kFewTarget * 16 <= kPromptTarget * 32 * kPromptWaves, "");
     return columns * (head_dim + 2) * sizeof(float);
 }
 
@@ -856,8 +908,8 @@ hipError_t attention(const Attention& o, int is_bf16, hipStream_t stream) {
 }
 
 hipError_t attention_init() {
-    const void* kernels[] = {(const void*)&attention_prompt_kernel<64, kPromptBlocks>, (const void*)&attention_prompt_kernel<96, kPromptBlocks>,
-                             (const void*)&attention_prompt_kernel<128, kPromptBlocks>, (const void*)&attention_prompt_kernel<256, kPromptBlocks>};
+    const void* kernels[] = {(const void*)&attention_prompt_kernel<64>, (const void*)&attention_prompt_kernel<96>,
+                             (const void*)&attention_prompt_kernel<128>, (const void*)&attention_prompt_kernel<256>};
     const int bytes[] = {prompt_lds<64>(), prompt_lds<96>(), prompt_lds<128>(), prompt_lds<256>()};
     for (int i = 0; i < 4; ++i) {
         const hipError_t e = hipFuncSetAttribute(kernels[i], hipFuncAttributeMaxDynamicSharedMemorySize, bytes[i]);
