@@ -776,54 +776,100 @@ void attention_prompt_kernel(AttnArgs a) {
     if (!whole && h == 0) { a.part_ml[2 * part] = total == 0.f ? -__builtin_inff() : base; a.part_ml[2 * part + 1] = total; }
 }
 
-// Joins the chunks' parts of a row's head: O = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.
-template <class T, int D>
+// Joins the chunks' parts of a row's head: O = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  D / 4 threads (padded to a power of two) take
+// a part each P-th chunk's, four components a thread; the P sums are joined in LDS in their order.  With one thread after another through all
+// chunks (P = 1) 37 chunks of 96 heads took 31 us: a chain of trips to memory.
+template <class T, int D, int P>
 __global__ __launch_bounds__(256)
 void attention_join_kernel(AttnArgs a) {
-    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t items = (int64_t)a.b.n_rows * a.n_q_heads;
-    int64_t item = e / (D / 4);
-    const int x = 4 * (int)(e - item * (D / 4));
-    const bool there = item < items;
-    if (!there) item = items - 1;
-    const int row = (int)(item / a.n_q_heads);
-    int seq = row, i = 0, count = 1;
-    if (a.b.row_start) {
-        // the rows of a wave differ by a few at most, yet each thread looks for its own
-        int lo = 0, hi = a.b.n_seqs;
-        while (lo < hi) {
-            const int mid = (lo + hi) >> 1;
-            if (a.b.row_start[mid + 1] <= row) lo = mid + 1; else hi = mid;
+    constexpr int TH = D == 96 ? 32 : D / 4, ITEMS = 256 / (TH * P);
+    __shared__ float ml[P > 1 ? 256 / TH : 1][2];
+    __shared__ f32x4_t parts[P > 1 ? 256 : 1];
+    const int x = 4 * (threadIdx.x % TH), sub = threadIdx.x / TH, turn = sub % P;
+    const int64_t items = (int64_t)a.b.n_rows * a.n_q_heads, item = (int64_t)blockIdx.x * ITEMS + sub / P;
+    bool there = item < items && x < D;
+    const int row = there ? (int)(item / a.n_q_heads) : 0;
+    int used = 0;
+    if (there) {
+        int seq = row, i = 0, count = 1;
+        if (a.b.row_start) {
+            int lo = 0, hi = a.b.n_seqs;                     // the number of sequences that end at or before the row
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (a.b.row_start[mid + 1] <= row) lo = mid + 1; else hi = mid;
+            }
+            seq = lo;
+            there = seq < a.b.n_seqs;
+            if (there) {
+                const NewRows rows = rows_of_sequence(a.b, seq);
+                i = row - rows.first;
+                count = rows.count;
+                there = i >= 0 && i < count;
+            }
         }
-        seq = lo;
-        if (seq >= a.b.n_seqs) return;
-        const NewRows rows = rows_of_sequence(a.b, seq);
-        i = row - rows.first;
-        count = rows.count;
-        if (i < 0 || i >= count) return;
+        if (there) {
+            const int kv_len = a.b.kv_len[seq], kv_end = min(kv_len, a.b.max_kv_len);
+            const int limit = min(a.causal ? kv_len - count + i : kv_len - 1, kv_end - 1);
+            used = limit < 0 ? 0 : limit / a.chunk + 1;
+        }
+    }
+    float top = -__builtin_inff(), total = 0.f;
+    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+    constexpr int DEEP = 4;                                  // chunks whose parts are sent for together
+    for (int s0 = turn; s0 < used; s0 += DEEP * P) {
+        float2 part[DEEP];
+        f32x4_t y[DEEP];
+#pragma unroll
+        for (int k = 0; k < DEEP; ++k) {
+            const int64_t at = min(s0 + k * P, used - 1) * items + item;
+            part[k] = *reinterpret_cast<const float2*>(a.part_ml + 2 * at);
+            y[k] = *reinterpret_cast<const f32x4_t*>(a.part_o + at * D + x);
+        }
+#pragma unroll
+        for (int k = 0; k < DEEP; ++k) {
+            if (s0 + k * P >= used || part[k].y == 0.f) continue;            // nothing seen: 0 times what it holds need not be 0
+            const float m = fmaxf(top, part[k].x), safe = m == -__builtin_inff() ? 0.f : m;
+            const float was = __builtin_amdgcn_exp2f(top - safe), is = __builtin_amdgcn_exp2f(part[k].x - safe);
+            total = total * was + is * part[k].y;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) o[u] = o[u] * was + is * y[k][u];
+            top = m;
+        }
+    }
+    if constexpr (P > 1) {
+        parts[threadIdx.x] = o;
+        if (x == 0) { ml[sub][0] = top; ml[sub][1] = total; }
+        __syncthreads();
+        if (turn != 0) return;
+        float m = top;
+#pragma unroll
+        for (int s = 1; s < P; ++s) m = fmaxf(m, ml[sub + s][0]);
+        const float safe = m == -__builtin_inff() ? 0.f : m;
+        total = 0.f;
+        o = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < P; ++s) {
+            if (ml[sub + s][1] == 0.f) continue;
+            const float k = __builtin_amdgcn_exp2f(ml[sub + s][0] - safe);
+            total += k * ml[sub + s][1];
+            const f32x4_t y = parts[threadIdx.x + s * TH];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) o[u] += k * y[u];
+        }
     }
     if (!there) return;
-    const int kv_len = a.b.kv_len[seq], kv_end = min(kv_len, a.b.max_kv_len);
-    const int limit = min(a.causal ? kv_len - count + i : kv_len - 1, kv_end - 1);
-    const int used = limit < 0 ? 0 : limit / a.chunk + 1;
-    float top = -__builtin_inff(), total = 0.f;
-    for (int s = 0; s < used; ++s) top = fmaxf(top, a.part_ml[2 * (s * items + item)]);
-    const float safe = top == -__builtin_inff() ? 0.f : top;
-    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < used; ++s) {
-        const int64_t at = s * items + item;
-        const float ls = a.part_ml[2 * at + 1];
-        if (ls == 0.f) continue;
-        const float k = __builtin_amdgcn_exp2f(a.part_ml[2 * at] - safe);
-        total += k * ls;
-        const f32x4_t y = *reinterpret_cast<const f32x4_t*>(a.part_o + at * D + x);
-#pragma unroll
-        for (int u = 0; u < 4; ++u) o[u] += k * y[u];
-    }
     const float inv = total == 0.f ? 0.f : 1.f / total;
 #pragma unroll
     for (int u = 0; u < 4; ++u) o[u] = total == 0.f ? 0.f : o[u] * inv;
     store4((T*)a.O + row * a.ldo + (item - (int64_t)row * a.n_q_heads) * D + x, o);
+}
+
+template <class T, int D, int P>
+hipError_t join(const AttnArgs& a, hipStream_t stream) {
+    constexpr int ITEMS = 256 / ((D == 96 ? 32 : D / 4) * P);
+    const int64_t items = (int64_t)a.b.n_rows * a.n_q_heads;
+    hipLaunchKernelGGL((attention_join_kernel<T, D, P>), dim3((unsigned)((items + ITEMS - 1) / ITEMS)), dim3(256), 0, stream, a);
+    return hipGetLastError();
 }
 
 // Which kernel, and how the cache is cut: chunks of `chunk` keys, n_chunks of them to the longest sequence.
@@ -875,8 +921,8 @@ hipError_t launch(const Attention& o, hipStream_t stream) {
     if (!p.prompt) hipLaunchKernelGGL((attention_few_kernel<T, D>), dim3((unsigned)p.workgroups), dim3(64 * kFewWaves), 0, stream, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.n_chunks == 1) return e;
-    hipLaunchKernelGGL((attention_join_kernel<T, D>), dim3((unsigned)((items * (D / 4) + 255) / 256)), dim3(256), 0, stream, a);
-    return hipGetLastError();
+    if (p.n_chunks <= 4) return join<T, D, 1>(a, stream);
+    return p.n_chunks <= 16 ? join<T, D, 4>(a, stream) : join<T, D, D == 256 ? 4 : 8>(a, stream);
 }
 
 template <class T>
@@ -893,7 +939,7 @@ hipError_t of_width(const Attention& o, hipStream_t stream) {
 }  // namespace
 
 bool attention_fits(const Attention& o, int is_bf16) {
-    return plan_of(o, is_bf16).workgroups <= kMostWorkgroups && ((int64_t)o.batch.n_rows * o.n_q_heads * (o.cache.head_dim / 4) + 255) / 256 <= kMostWorkgroups;
+    return plan_of(o, is_bf16).workgroups <= kMostWorkgroups && (int64_t)o.batch.n_rows * o.n_q_heads <= kMostWorkgroups;
 }
 size_t attention_workspace_bytes(const Attention& o, int is_bf16) { return part_bytes(o, plan_of(o, is_bf16)); }
 // a plan of more than one chunk has at most its target of workgroups, and every row's head is a column of one of them
