@@ -29,7 +29,7 @@ struct AttnArgs {
     float scale2s;               // scale log2 e
     uint32_t flip;               // sign bits of Q's words where scale is negative
     int causal;
-    int chunk, n_chunks, col_tiles;
+    int chunk, n_chunks, col_tiles, paired;
     KvCache kv;
     SeqBatch b;
 };
@@ -454,17 +454,13 @@ template <int D> __device__ __forceinline__ int v_pos(int r, int c) {          /
     else return c ^ ((r & 3) << 2);
 }
 
+// One tile of columns of a sequence and key head, one chunk of the cache.
 template <int D>
-__global__ __launch_bounds__(64 * kPromptWaves, D < 256 ? 2 : 1)
-void attention_prompt_kernel(AttnArgs a) {
+__device__ __forceinline__ void prompt_tile(const AttnArgs& a, int seq, int kvh, int chunk, int tile) {
     constexpr int KT = kPromptKeys, KS = D / 16, DT = D / 32, PITCH = 2 * D, SLOT = KT * PITCH, WIDE = 32 * kPromptWaves;
     constexpr int ROWS = KT / kPromptWaves;                  // rows a wave fetches
     constexpr int NF = ROWS * PITCH / 1024;                  // fetches of 1 KB for them
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
-    int set, item;
-    if (!deal_to_dies(blockIdx.x, a.col_tiles * a.n_chunks, a.b.n_seqs * a.kv.n_kv_heads, &set, &item)) return;
-    const int kvh = set % a.kv.n_kv_heads, seq = set / a.kv.n_kv_heads;
-    const int chunk = item % a.n_chunks, tile = a.col_tiles - 1 - item / a.n_chunks;      // the columns that see most first
     const NewRows rows = rows_of_sequence(a.b, seq);
     const int columns = rows.count * a.group, first_col = tile * WIDE;
     if (first_col >= columns) return;
@@ -509,10 +505,12 @@ void attention_prompt_kernel(AttnArgs a) {
     const int most = awake ? min(limit_of(min(wave_col + 32, columns) - 1), last) : -1, least = awake ? limit_of(wave_col) : -1;
     const int my_steps = most >= begin ? (most - begin) / KT + 1 : 0;
     const int col = min(wave_col + c, columns - 1);          // dead columns repeat the last one
-    const int limit = limit_of(col), row = rows.first + col / a.group, head = kvh * a.group + col % a.group;
+    const int limit = limit_of(col);
+    auto row_of = [&](int x) { return rows.first + x / a.group; };
+    auto head_of = [&](int x) { return kvh * a.group + x % a.group; };
     bf16x8_t q[KS];
     {
-        const uint16_t* p = (const uint16_t*)a.Q + row * a.ldq + (int64_t)head * D + 8 * h;
+        const uint16_t* p = (const uint16_t*)a.Q + row_of(col) * a.ldq + (int64_t)head_of(col) * D + 8 * h;
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             u32x4_t w = *reinterpret_cast<const u32x4_t*>(p + 16 * s);
@@ -754,6 +752,9 @@ void attention_prompt_kernel(AttnArgs a) {
         if (!any_odd) break;
     }
     if (wave_col + c >= columns) return;
+    int my_col = wave_col + c;
+    asm volatile("" : "+v"(my_col));                         // (row and head are worked out again: kept, they take registers the loop needs)
+    const int row = row_of(my_col), head = head_of(my_col);
     const bool whole = a.n_chunks == 1;
     float total = l + __shfl_xor(l, 32, 64);
     if (any_bad) total = __builtin_nanf("");
@@ -774,6 +775,22 @@ void attention_prompt_kernel(AttnArgs a) {
             else *reinterpret_cast<f32x4_t*>(a.part_o + part * D + x) = o;
         }
     if (!whole && h == 0) { a.part_ml[2 * part] = total == 0.f ? -__builtin_inff() : base; a.part_ml[2 * part + 1] = total; }
+}
+
+template <int D>
+__global__ __launch_bounds__(64 * kPromptWaves, D < 256 ? 2 : 1)
+void attention_prompt_kernel(AttnArgs a) {
+    int set, item;
+    const int dealt = a.paired ? (a.col_tiles + 1) / 2 : a.col_tiles;
+    if (!deal_to_dies(blockIdx.x, dealt * a.n_chunks, a.b.n_seqs * a.kv.n_kv_heads, &set, &item)) return;
+    const int kvh = set % a.kv.n_kv_heads, seq = set / a.kv.n_kv_heads;
+    const int chunk = item % a.n_chunks;
+    int tile = a.col_tiles - 1 - item / a.n_chunks;          // the columns that see most first
+    for (;; tile = a.col_tiles - 1 - tile) {
+        prompt_tile<D>(a, seq, kvh, chunk, tile);
+        if (!a.paired || 2 * tile < a.col_tiles) break;      // the middle one of an odd number has no partner
+        __syncthreads();
+    }
 }
 
 // Joins the chunks' parts of a row's head: O = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  D / 4 threads (padded to a power of two) take
@@ -873,26 +890,81 @@ hipError_t join(const AttnArgs& a, hipStream_t stream) {
 }
 
 // Which kernel, and how the cache is cut: chunks of `chunk` keys, n_chunks of them to the longest sequence.
-struct Plan { bool prompt; int col_tiles, chunk, n_chunks; int64_t workgroups; };
+struct Plan { bool prompt, paired; int col_tiles, chunk, n_chunks; int64_t workgroups; };
 constexpr int64_t kMostWorkgroups = 1 << 23;     // of a launch: 2^31 threads and no more fit HIP's 32-bit counts
-constexpr int kFewTarget = 1024, kFewLeast = 256;        // workgroups that fill the chip, keys to a chunk at least
-constexpr int kPromptTarget = 512, kPromptLeast = 256;
+constexpr int kCus = 256;
+constexpr int kFewTarget = 512, kFewLeast = 256;         // workgroups that fill the chip (two to a CU), keys to a chunk at least
+constexpr int kPromptTarget = 512, kPromptLeast = 128;
+
+// The cache cut `cuts` times, rounded to whole steps of both kernels.
+void cut(Plan* p, int max_kv_len, int64_t cuts) {
+    p->chunk = (int)round_up((max_kv_len + cuts - 1) / cuts, 128);
+    p->n_chunks = (max_kv_len + p->chunk - 1) / p->chunk;
+}
+// The join: a launch behind another one, and the parts written and read.
+double join_us(const Attention& o, const Plan& p) {
+    return p.n_chunks == 1 ? 0.0 : 5.0 + 8.0 * p.n_chunks * o.batch.n_rows * o.n_q_heads * o.cache.head_dim / 4e6;
+}
+
+Plan plan_few(const Attention& o, int64_t columns, double* us) {
+    Plan p;
+    p.prompt = p.paired = false;
+    p.col_tiles = (int)((columns + 15) / 16);
+    const int64_t tiles = (int64_t)o.batch.n_seqs * o.cache.n_kv_heads * p.col_tiles;
+    const int64_t most = (o.batch.max_kv_len + kFewLeast - 1) / kFewLeast;
+    int64_t cuts = kFewTarget / tiles;
+    cut(&p, o.batch.max_kv_len, cuts < 1 ? 1 : cuts < most ? cuts : most);
+    p.workgroups = tiles * p.n_chunks;
+    // every tile of 16 columns reads the cache's rows again, from L2 as a rule; a wave's step is a trip to memory
+    const double rounds = (double)((p.workgroups + kFewTarget - 1) / kFewTarget);
+    const double reads = 4.0 * tiles * o.batch.max_kv_len * o.cache.head_dim / 9e6, trips = rounds * (p.chunk / 128) * 1.5;
+    *us = 4.0 * rounds + (reads > trips ? reads : trips) + join_us(o, p);
+    return p;
+}
+
+// Cuts fill the chip but cost the join, and two workgroups on a CU share its matrix pipes: of the counts that fit, the one that this reckoning
+// likes best.  A workgroup takes 5 us until its first weights, then per step of 64 keys 1.3 us alone on its CU (a fetch's way) and 1.1 us
+// times the width over 128 of the CU's pipes.  With two workgroups on every CU wherever the columns allowed it (at 256 keys to a chunk) 8 x 128
+// rows against 512 keys of 32 heads of 128 took 37 us where one cut less takes 22, against 1024 52 and 40, 2 x 300 rows of 8 heads of 256
+// against 3000 77 and 56; 512 rows behind 7680, 32/8 heads, take 86 us cut in four and 95 in two.
+Plan plan_prompt(const Attention& o, int64_t columns, double* us) {
+    Plan best;
+    best.prompt = true;
+    best.col_tiles = (int)((columns + 32 * kPromptWaves - 1) / (32 * kPromptWaves));
+    const int64_t sets = (int64_t)o.batch.n_seqs * o.cache.n_kv_heads, tiles = sets * best.col_tiles;
+    const int d = o.cache.head_dim, per_cu = d == 256 ? 1 : 2;
+    const double bytes = 4.0 * sets * o.batch.max_kv_len * d;
+    *us = 1e30;
+    int64_t most = kPromptTarget / tiles;
+    const int64_t whole = (o.batch.max_kv_len + kPromptLeast - 1) / kPromptLeast;
+    most = most < 1 ? 1 : most < whole ? most : whole;
+    for (int64_t cuts = 1; cuts <= most; ++cuts) {
+        Plan p = best;
+        cut(&p, o.batch.max_kv_len, cuts);
+        p.workgroups = tiles * p.n_chunks;
+        const int64_t slots = kCus * per_cu, rounds = (p.workgroups + slots - 1) / slots;
+        const int64_t together = rounds > 1 || p.workgroups > kCus ? per_cu : 1;
+        const double pipes = 1.1 * d / 128 * together, step = pipes > 1.3 ? pipes : 1.3;
+        double main = (double)rounds * (5.0 + p.chunk / 64 * step);
+        if (main < 5.0 + bytes / 5.5e6) main = 5.0 + bytes / 5.5e6;
+        const double all = main + join_us(o, p);
+        if (all < *us) { *us = all; best.chunk = p.chunk; best.n_chunks = p.n_chunks; best.workgroups = p.workgroups; }
+    }
+    // Causal rows: the last tile of columns walks the most keys, the first one the fewest.  Where the tiles are more than the chip holds at
+    // once but no more than twice that, a workgroup takes a long and a short one: all end together.
+    const int64_t pairs = sets * ((best.col_tiles + 1) / 2);
+    best.paired = o.causal && best.n_chunks == 1 && best.col_tiles > 1 && best.workgroups > kCus * per_cu && pairs <= kCus * per_cu;
+    if (best.workgroups <= kMostWorkgroups) best.workgroups = 8 * (int64_t)dies_slots((best.paired ? (best.col_tiles + 1) / 2 : best.col_tiles) * best.n_chunks, (int)sets);
+    return best;
+}
 
 Plan plan_of(const Attention& o, int is_bf16) {
-    Plan p;
     const int64_t columns = (int64_t)o.batch.max_rows * (o.n_q_heads / o.cache.n_kv_heads);
-    p.prompt = is_bf16 && columns > 16;
-    const int wide = p.prompt ? 32 * kPromptWaves : 16, target = p.prompt ? kPromptTarget : kFewTarget, least = p.prompt ? kPromptLeast : kFewLeast;
-    p.col_tiles = (int)((columns + wide - 1) / wide);
-    const int64_t sets = (int64_t)o.batch.n_seqs * o.cache.n_kv_heads, tiles = sets * p.col_tiles;
-    const int64_t most = (o.batch.max_kv_len + least - 1) / least;
-    int64_t cuts = target / tiles;
-    cuts = cuts < 1 ? 1 : cuts < most ? cuts : most;
-    p.chunk = (int)round_up((o.batch.max_kv_len + cuts - 1) / cuts, 128);
-    p.n_chunks = (o.batch.max_kv_len + p.chunk - 1) / p.chunk;
-    p.workgroups = tiles * p.n_chunks;
-    if (p.prompt && p.workgroups <= kMostWorkgroups) p.workgroups = 8 * (int64_t)dies_slots(p.col_tiles * p.n_chunks, (int)sets);
-    return p;
+    double few_us, prompt_us;
+    const Plan few = plan_few(o, columns, &few_us);
+    if (!is_bf16 || columns <= 16) return few;
+    const Plan prompt = plan_prompt(o, columns, &prompt_us);
+    return few_us < prompt_us ? few : prompt;
 }
 
 size_t part_bytes(const Attention& o, const Plan& p) {
@@ -909,7 +981,7 @@ hipError_t launch(const Attention& o, hipStream_t stream) {
     a.scale2 = o.scale == 0.f ? 1e-30f : fabsf(a.scale2s);      // (-inf, a hidden score, times 0 would be NaN)
     a.flip = o.scale < 0.f ? 0x80008000u : 0u;
     a.causal = o.causal;
-    a.chunk = p.chunk; a.n_chunks = p.n_chunks; a.col_tiles = p.col_tiles;
+    a.chunk = p.chunk; a.n_chunks = p.n_chunks; a.col_tiles = p.col_tiles; a.paired = p.paired;
     a.kv = o.cache; a.b = o.batch;
     const int64_t items = (int64_t)o.batch.n_rows * o.n_q_heads;
     a.part_o = o.workspace;
