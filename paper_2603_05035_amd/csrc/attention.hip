@@ -1010,6 +1010,16 @@ hipError_t of_width(const Attention& o, hipStream_t stream) {
 
 }  // namespace
 
+// Which way a call of these sizes goes: 0 few columns, 1 many, 2 many with causal tiles in pairs; plus 4 where the cache is cut.
+int attention_way(int is_bf16, int causal, int n_q_heads, int n_kv_heads, int head_dim, int n_seqs, int n_rows, int max_rows, int max_kv_len) {
+    Attention o = {};
+    o.causal = causal != 0; o.n_q_heads = n_q_heads;
+    o.cache.n_kv_heads = n_kv_heads; o.cache.head_dim = head_dim;
+    o.batch.n_seqs = n_seqs; o.batch.n_rows = n_rows; o.batch.max_rows = max_rows; o.batch.max_kv_len = max_kv_len;
+    const Plan p = plan_of(o, is_bf16);
+    return (p.prompt ? p.paired ? 2 : 1 : 0) + (p.n_chunks > 1 ? 4 : 0);
+}
+
 bool attention_fits(const Attention& o, int is_bf16) {
     return plan_of(o, is_bf16).workgroups <= kMostWorkgroups && (int64_t)o.batch.n_rows * o.n_q_heads <= kMostWorkgroups;
 }

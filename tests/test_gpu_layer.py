@@ -318,6 +318,47 @@ def test_attention_of_prompts(ctx, dtype, new, kv, hq, hkv, d, page, order, caus
     run_attention(ctx, dtype, new, kv, hq, hkv, d, page, order, causal)
 
 
+LARGE = [  # dtype, new rows, kv, q heads, kv heads, d, page, order, causal
+    (BF16, [512, 377, 512, 1, 130, 512, 256, 400], [512, 377, 600, 1, 130, 512, 256, 400], 32, 32, 128, 16, "head", True),      # tiles of columns in pairs
+    (BF16, [384, 200, 384, 384, 129, 384, 300, 384], [384, 200, 384, 500, 129, 384, 300, 384], 32, 32, 128, 64, "row", True),   # ... of an odd number
+    (BF16, [384, 130, 384, 70], [384, 130, 390, 70], 32, 32, 256, 32, "head", True),
+    (BF16, [390, 128] * 4, [390, 300] * 4, 32, 32, 64, 16, "row", True),
+    (BF16, [200], [5000], 8, 8, 64, 64, "head", True),                  # many columns and a cut cache
+    (BF16, [65, 200], [3000, 4111], 12, 4, 96, 16, "row", False),
+    (BF16, [90], [7000], 16, 4, 128, 32, "head", True),
+    (BF16, [300, 20], [2500, 90], 8, 4, 256, 16, "head", True),
+    (BF16, [1500], [2777], 14, 2, 128, 128, "row", True),
+    (BF16, [1, 1], [30011, 9], 16, 2, 128, 64, "head", True),           # few columns and many cuts
+    (F32, [1], [20000], 8, 2, 96, 16, "row", True),
+    (F32, [700, 33], [1300, 33], 8, 2, 128, 64, "head", True),
+    (BF16, [1, 1, 1], [4100, 3000, 1], 48, 2, 64, 32, "head", True),    # more than 16 heads to a key head
+]
+
+
+@pytest.mark.parametrize("dtype,new,kv,hq,hkv,d,page,order,causal", LARGE)
+def test_attention_at_the_sizes_where_launches_differ(ctx, dtype, new, kv, hq, hkv, d, page, order, causal):
+    """The reference in float64 on the GPU, for every sequence and two of the heads; the same bound as above."""
+    batch, table, row_start, n_pages = make_batch(new, kv, page, 3, one_row=max(new) == 1)
+    rows = int(row_start[-1])
+    K, V = make_cache(n_pages, hkv, page, d, dtype, order, seed=5)
+    Q, O = rand((rows, hq * d), 8, dtype), torch.full((rows, hq * d), 7.0, dtype=dtype, device="cuda")
+    g.gelo_attention(ctx, Q, O, hq, g.KvCache(K, V), batch, 1 / math.sqrt(d), causal=causal)
+    assert torch.isfinite(O.float()).all()
+    for s in range(len(kv)):
+        used = torch.from_numpy(table[s, :(kv[s] + page - 1) // page]).long().cuda()
+        at = slice(int(row_start[s]), int(row_start[s + 1]))
+        for h in {0, (7 * s + 5) % hq}:
+            kh = h * hkv // hq
+            k, v = (x[used, kh].reshape(-1, d)[:kv[s]].double() for x in (K, V))
+            q = Q[at, h * d:(h + 1) * d].double()
+            score = q @ k.T / math.sqrt(d)
+            if causal:
+                score.masked_fill_(torch.arange(kv[s], device="cuda")[None] > torch.arange(new[s], device="cuda")[:, None] + (kv[s] - new[s]), -math.inf)
+            w = torch.softmax(score, -1)
+            ref, absolute = host(w @ v), host(w @ v.abs())
+            within(O[at, h * d:(h + 1) * d], ref, attention_bound(ref, absolute, host(q), host(k), 1 / math.sqrt(d), kv[s], d, dtype), (s, h))
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("scale", [0.0, -0.2, 3.0])
 def test_attention_scales(ctx, dtype, scale):
@@ -350,6 +391,114 @@ def test_values_that_are_not_finite_reach_only_rows_that_see_them(ctx, dtype, d,
     K[at // page, 0, at % page, 0] = float("nan")
     g.gelo_attention(ctx, Q, O, 1, g.KvCache(K, clean), batch, 1 / math.sqrt(d))
     assert torch.equal(O[:at], want[:at]) and torch.isnan(O[at:]).all()
+
+
+def way(ctx, Q, new, kv, hq, hkv, d, causal):
+    """Which way such a bfloat16 call goes (1: the kernel for many columns to a key head, the cache whole)."""
+    return ctypes.CDLL(g.LIB_PATH)["_ZN4gelo13attention_wayEiiiiiiiii"](1, int(causal), hq, hkv, d, len(kv), Q.shape[0], max(new), max(kv))
+
+
+EDGES = [(1, 1), (5, 1), (16, 16), (17, 17), (31, 40), (32, 32), (33, 63), (63, 64), (64, 65), (65, 64), (127, 128), (128, 127), (129, 200), (2, 0), (0, 9),
+         (140, 15), (64, 191), (96, 192), (130, 193), (20, 257), (257, 300), (48, 48), (200, 112), (70, 129)]
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("d,hq,hkv,page,order", [(64, 32, 16, 16, "head"), (96, 16, 16, 32, "row"), (128, 32, 16, 16, "row"), (256, 16, 16, 64, "head")])
+def test_many_columns_at_the_edges_of_tiles(ctx, d, hq, hkv, page, order, causal):
+    """New rows and lengths at, before and behind the ends of tiles, steps and groups, none, and more rows than keys; rows of the cache that
+    belong to nobody hold NaN.  All rows of three heads."""
+    new, kv = [x[0] for x in EDGES], [x[1] for x in EDGES]
+    batch, table, row_start, n_pages = make_batch(new, kv, page, 3)
+    K, V = make_cache(n_pages, hkv, page, d, BF16, order, seed=5)
+    hidden = torch.ones((n_pages, page), dtype=torch.bool)
+    for s, n in enumerate(kv):
+        for p in range(n):
+            hidden[table[s, p // page], p % page] = False
+    K.masked_fill_(hidden.cuda()[:, None, :, None], float("nan"))
+    V.masked_fill_(hidden.cuda()[:, None, :, None], float("nan"))
+    Q = rand((int(row_start[-1]), hq * d), 8, BF16)
+    O = torch.full_like(Q, 7.0)
+    assert way(ctx, Q, new, kv, hq, hkv, d, causal) == 1
+    g.gelo_attention(ctx, Q, O, hq, g.KvCache(K, V), batch, 1 / math.sqrt(d), causal=causal)
+    for h in (0, hq // 2 + 1, hq - 1):
+        kh = h * hkv // hq
+        ref, absolute = lo.attention(host(Q[:, h * d:(h + 1) * d]), host(K[:, kh:kh + 1]), host(V[:, kh:kh + 1]), 1, row_start, kv, table, 1 / math.sqrt(d), causal)
+        within(O[:, h * d:(h + 1) * d], ref, attention_bound(ref, absolute, host(Q), host(K), 1 / math.sqrt(d), max(kv), d, BF16), h)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.2, 3.0])
+def test_many_columns_at_other_scales(ctx, scale):
+    new, kv, hq, d, page = [150] * 16, [150 + 9 * i for i in range(16)], 16, 128, 16
+    batch, table, row_start, n_pages = make_batch(new, kv, page, 3)
+    K, V = make_cache(n_pages, hq, page, d, BF16, "head", seed=5)
+    Q = rand((int(row_start[-1]), hq * d), 8, BF16)
+    O = torch.full_like(Q, 7.0)
+    assert way(ctx, Q, new, kv, hq, hq, d, True) == 1
+    g.gelo_attention(ctx, Q, O, hq, g.KvCache(K, V), batch, scale)
+    for h in (0, hq - 1):
+        ref, absolute = lo.attention(host(Q[:, h * d:(h + 1) * d]), host(K[:, h:h + 1]), host(V[:, h:h + 1]), 1, row_start, kv, table, scale, True)
+        within(O[:, h * d:(h + 1) * d], ref, attention_bound(ref, absolute, host(Q), host(K), scale, max(kv), d, BF16), h)
+
+
+@pytest.mark.parametrize("rows,want", [(150, 1), (512, 2)])
+@pytest.mark.parametrize("d", [64, 96, 128, 256])
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+def test_many_columns_and_values_that_are_not_finite(ctx, d, value, rows, want):
+    """One component of one value in every sequence and head: only rows from its own on, and only that component; everything else keeps its
+    bits.  A key that is NaN: the rows before it do not see it.  A page number outside the cache: its sequence alone."""
+    n_seqs, hq = (8 if d == 256 else 16), 16               # (at this width a workgroup has a CU to itself: half as many fit)
+    rows = 384 if want == 2 and d == 256 else rows
+    page, at = 16, 75
+    each = (rows + page - 1) // page
+    K, V = make_cache(n_seqs * each, hq, page, d, BF16, "head", seed=3)
+    table = torch.arange(n_seqs * each, dtype=torch.int32, device="cuda").view(n_seqs, each)
+    pages = table[:, at // page].long()
+    K[pages, :, at % page] = 0
+    odd = V.clone()
+    odd[pages, :, at % page, 5] = value
+    V[pages, :, at % page, 5] = 0
+    row_start = (torch.arange(n_seqs + 1, device="cuda") * rows).int()
+    batch = g.SeqBatch(torch.full((n_seqs,), rows, dtype=torch.int32).cuda(), table, rows, row_start=row_start, max_rows=rows)
+    Q = rand((n_seqs * rows, hq * d), 9, BF16)
+    assert way(ctx, Q, [rows] * n_seqs, [rows] * n_seqs, hq, hq, d, True) == want
+    O, clean = torch.empty_like(Q), torch.empty_like(Q)
+    g.gelo_attention(ctx, Q, clean, hq, g.KvCache(K, V), batch, 1 / math.sqrt(d))
+    g.gelo_attention(ctx, Q, O, hq, g.KvCache(K, odd), batch, 1 / math.sqrt(d))
+    o, w = (x.view(n_seqs, rows, hq, d) for x in (O, clean))
+    other = torch.arange(d, device="cuda") != 5
+    assert torch.isfinite(w.float()).all()
+    assert torch.equal(o[..., other], w[..., other]) and torch.equal(o[:, :at], w[:, :at])
+    assert torch.isnan(o[:, at:, :, 5]).all() if math.isnan(value) else torch.all(o[:, at:, :, 5] == value)
+    K[pages, :, at % page, 0] = float("nan")
+    g.gelo_attention(ctx, Q, O, hq, g.KvCache(K, V), batch, 1 / math.sqrt(d))
+    assert torch.equal(o[:, :at], w[:, :at]) and torch.isnan(o[:, at:]).all()
+    K[pages, :, at % page, 0] = 0
+    table[3, 2] = n_seqs * each
+    table[7, 0] = -3
+    g.gelo_attention(ctx, Q, O, hq, g.KvCache(K, V), batch, 1 / math.sqrt(d))
+    assert torch.isnan(o[7]).all() and torch.isnan(o[3, -1]).all()
+    rest = [s for s in range(n_seqs) if s not in (3, 7)]
+    assert torch.equal(o[rest], w[rest])
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_cut_cache_and_values_that_are_not_finite(ctx, d):
+    """Many columns, the keys in chunks whose parts are joined: the value lies in one chunk."""
+    rows, kv, hq, page, at = 200, 5000, 8, 64, 4900
+    K, V = make_cache(79, hq, page, d, BF16, "row", seed=3)
+    table = torch.arange(79, dtype=torch.int32, device="cuda")[None]
+    batch = g.SeqBatch(torch.tensor([kv], dtype=torch.int32).cuda(), table, kv, row_start=torch.tensor([0, rows], dtype=torch.int32).cuda(), max_rows=rows)
+    Q = rand((rows, hq * d), 9, BF16)
+    assert way(ctx, Q, [rows], [kv], hq, hq, d, True) == 5
+    K[at // page, :, at % page] = 0
+    V[at // page, :, at % page, 5] = 0
+    O, clean = torch.empty_like(Q), torch.empty_like(Q)
+    g.gelo_attention(ctx, Q, clean, hq, g.KvCache(K, V), batch, 1 / math.sqrt(d))
+    V[at // page, :, at % page, 5] = float("inf")
+    g.gelo_attention(ctx, Q, O, hq, g.KvCache(K, V), batch, 1 / math.sqrt(d))
+    o, w = (x.view(rows, hq, d) for x in (O, clean))
+    first, other = at - (kv - rows), torch.arange(d, device="cuda") != 5
+    assert torch.equal(o[..., other], w[..., other]) and torch.equal(o[:first], w[:first]) and torch.all(o[first:, :, 5] == float("inf"))
 
 
 def test_page_numbers_outside_the_cache_are_not_followed(ctx):
