@@ -70,9 +70,9 @@ SIGNATURES = {
                               c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p]),
     "gelo_project_fp8_codes": (c_int, [c_void_p, c_int, c_int, c_int, c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_int64, c_void_p]),
     "gelo_rope_table": (c_int, [c_void_p, c_int, c_int, c_int, c_double, c_double, c_double, c_double, c_double, c_void_p, c_void_p]),
-    "gelo_rope_append": (c_int, [c_void_p, c_int, c_int, c_void_p, c_int64, POINTER(_KvCacheStruct), POINTER(_SeqBatchStruct), c_int, c_int,
+    "gelo_rope_append": (c_int, [c_void_p, c_int, c_int, c_void_p, c_int64, c_void_p, c_void_p, c_int, c_int,
                                  c_void_p, c_int, c_void_p, c_int64, c_void_p]),
-    "gelo_attention": (c_int, [c_void_p, c_int, c_int, c_void_p, c_int64, POINTER(_KvCacheStruct), POINTER(_SeqBatchStruct), c_float, c_int,
+    "gelo_attention": (c_int, [c_void_p, c_int, c_int, c_void_p, c_int64, c_void_p, c_void_p, c_float, c_int,
                                c_void_p, c_int64, c_void_p]),
     "gelo_reserve_attention": (c_int, [c_void_p, c_int]),
     "gelo_debug_philox_words": (c_int, [c_void_p, c_uint32, c_uint32, c_uint64, c_uint32, c_uint32, c_void_p, c_void_p]),
@@ -114,12 +114,15 @@ def _check(ctx, status: int):
         raise GeloError(status, (msg or b"").decode())
 
 
-def _stream(stream) -> c_void_p:
+_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+
+
+def _stream(stream):
     if stream is None:
         # the current stream's handle alone: torch.cuda.current_stream() makes an object around it, 2.7 us of a call's 9
         if not torch.cuda.is_initialized():
             torch.cuda.init()
-        return c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
+        return _raw_stream(_current_device())
     return c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
 
@@ -138,7 +141,7 @@ def _matrix(t: torch.Tensor, name: str):
     shape, stride = t.shape, t.stride()
     if len(shape) != 2 or (shape[1] > 1 and stride[1] != 1):
         raise ValueError(f"{name} must be a row-major 2-D tensor")
-    return c_void_p(t.data_ptr()), stride[0] if shape[0] > 1 else max(stride[0], shape[1])
+    return t.data_ptr(), stride[0] if shape[0] > 1 else max(stride[0], shape[1])
 
 
 def gelo_create(device: int = 0, seed: int = 0, allow_batch_reuse: bool = False) -> c_void_p:
@@ -356,10 +359,11 @@ class KvCache:
         strides, other = ([x.stride(i) if x.shape[i] > 1 else K.shape[3] for i in range(3)] for x in (K, V))
         if strides != other or (K.shape[3] > 1 and (K.stride(3) != 1 or V.stride(3) != 1)):
             raise ValueError("K and V must have the same strides, the last of them 1")
-        self.K, self.V, self.dtype = K, V, _dtype_code(K)
+        self.K, self.V, self.torch_dtype, self.dtype = K, V, K.dtype, _dtype_code(K)
         n_pages, n_kv_heads, page_rows, head_dim = K.shape
-        self.n_kv_heads, self.head_dim = n_kv_heads, head_dim
+        self.n_kv_heads, self.page_rows, self.head_dim = n_kv_heads, page_rows, head_dim
         self.struct = _KvCacheStruct(K.data_ptr(), V.data_ptr(), n_pages, n_kv_heads, page_rows, head_dim, *strides)
+        self.address = ctypes.addressof(self.struct)
 
 
 class SeqBatch:
@@ -378,8 +382,9 @@ class SeqBatch:
         if n_seqs == 1 or table_ld < page_table.shape[1]:
             table_ld = page_table.shape[1]
         self.kv_len, self.page_table, self.row_start = kv_len, page_table, row_start
-        self.n_seqs, self.pages = n_seqs, page_table.shape[1]
+        self.n_seqs, self.n_rows, self.pages, self.max_kv_len = n_seqs, n_seqs, page_table.shape[1], max_kv_len
         self.struct = _SeqBatchStruct(n_seqs, n_seqs, max_rows, max_kv_len, None if row_start is None else row_start.data_ptr(), kv_len.data_ptr(), tp, table_ld)
+        self.address = ctypes.addressof(self.struct)
 
 
 def _vector(t: torch.Tensor, name: str, dtype, count: int):
@@ -387,15 +392,14 @@ def _vector(t: torch.Tensor, name: str, dtype, count: int):
         raise ValueError(f"{name} must be a contiguous GPU vector of {count} {dtype}")
 
 
-def _rows(batch: SeqBatch, rows: int, cache: KvCache):
-    """The batch's description for matrices of `rows` rows."""
-    s = batch.struct
-    if batch.row_start is None and rows != batch.n_seqs:
-        raise GeloError(2, f"{rows} rows, but every one of {batch.n_seqs} sequences brings one")
-    if batch.pages * cache.struct.page_rows < s.max_kv_len:
-        raise GeloError(2, f"max_kv_len={s.max_kv_len} rows do not fit {batch.pages} pages of {cache.struct.page_rows}")
-    s.n_rows = rows
-    return byref(s)
+def _check_rows(batch: SeqBatch, rows: int, cache: KvCache) -> None:
+    """Makes the batch's description one for matrices of `rows` rows."""
+    if batch.pages * cache.page_rows < batch.max_kv_len:
+        raise GeloError(2, f"max_kv_len={batch.max_kv_len} rows do not fit {batch.pages} pages of {cache.page_rows}")
+    if rows != batch.n_rows:
+        if batch.row_start is None:
+            raise GeloError(2, f"{rows} rows, but every one of {batch.n_seqs} sequences brings one")
+        batch.n_rows = batch.struct.n_rows = rows
 
 
 def gelo_rms_norm(ctx, X: torch.Tensor, gamma: torch.Tensor, eps: float, H: torch.Tensor | None = None, residual: torch.Tensor | None = None,
@@ -403,16 +407,22 @@ def gelo_rms_norm(ctx, X: torch.Tensor, gamma: torch.Tensor, eps: float, H: torc
     """h = X + residual into residual_out, h / rms(h) * gamma into H and, as 8-bit codes with row scales, into codes and scales."""
     shape, dtype = X.shape, X.dtype
     n, d = shape
-    args = [*_matrix(X, "X")]
-    for name, t in (("residual", residual), ("residual_out", residual_out), ("H", H)):
-        if t is None:
-            args += (None, 0)
-        elif t.dtype != dtype or t.shape != shape:
-            raise ValueError(f"{name} must be of X's dtype and shape")
-        else:
-            args += _matrix(t, name)
+    xp, ldx = _matrix(X, "X")
+    rp = op = hp = None
+    ldr = ldo = ldh = 0
+    if residual is not None:
+        if residual.dtype != dtype or residual.shape != shape:
+            raise ValueError("residual must be of X's dtype and shape")
+        rp, ldr = _matrix(residual, "residual")
+    if residual_out is not None:
+        if residual_out.dtype != dtype or residual_out.shape != shape:
+            raise ValueError("residual_out must be of X's dtype and shape")
+        op, ldo = _matrix(residual_out, "residual_out")
+    if H is not None:
+        if H.dtype != dtype or H.shape != shape:
+            raise ValueError("H must be of X's dtype and shape")
+        hp, ldh = _matrix(H, "H")
     _vector(gamma, "gamma", dtype, d)
-    xp, ldx, rp, ldr, op, ldo, hp, ldh = args
     cp, ldq, sp = None, 0, None
     if codes is not None or scales is not None:
         if codes is None or scales is None or codes.dtype != torch.uint8 or codes.shape != shape:
@@ -420,8 +430,9 @@ def gelo_rms_norm(ctx, X: torch.Tensor, gamma: torch.Tensor, eps: float, H: torc
         cp, ldq = _matrix(codes, "codes")
         _vector(scales, "scales", torch.float32, n)
         sp = scales.data_ptr()
-    _check(ctx, load_library().gelo_rms_norm(ctx, _dtype_code(X), n, d, xp, ldx, rp, ldr, gamma.data_ptr(), eps, op, ldo, hp, ldh, cp, ldq, sp,
-                                             _stream(stream)))
+    status = load_library().gelo_rms_norm(ctx, _dtype_code(X), n, d, xp, ldx, rp, ldr, gamma.data_ptr(), eps, op, ldo, hp, ldh, cp, ldq, sp, _stream(stream))
+    if status != GELO_OK:
+        _check(ctx, status)
 
 
 def gelo_rope_table(ctx, rot_dim: int, n_pos: int, base: float = 10000.0, factor: float = 1.0, trained: float = 0.0, low: float = 1.0,
@@ -437,22 +448,26 @@ def gelo_rope_append(ctx, QKV: torch.Tensor, n_q_heads: int, cache: KvCache, bat
     """Rotates the queries and keys of QKV's rows by their positions; queries into Q, keys and values into the cache."""
     zp, ld = _matrix(QKV, "QKV")
     rows, width = QKV.shape
-    if _dtype_code(QKV) != cache.dtype:
+    if QKV.dtype != cache.torch_dtype:
         raise GeloError(3, "QKV and the cache differ in type")
     if width != (n_q_heads + 2 * cache.n_kv_heads) * cache.head_dim:
         raise GeloError(2, f"a row of {width} values is not {n_q_heads} + 2 x {cache.n_kv_heads} heads of {cache.head_dim}")
     qp, ldq = None, 0
     if Q is not None:
-        if Q.dtype != QKV.dtype or Q.shape != (rows, n_q_heads * cache.head_dim):
+        if Q.dtype != cache.torch_dtype or Q.shape != (rows, n_q_heads * cache.head_dim):
             raise ValueError("Q must be of QKV's dtype, a row of all query heads for each of its rows")
         qp, ldq = _matrix(Q, "Q")
     tp, n_table = None, 0
     if table is not None:
-        if table.dtype != torch.float32 or not table.is_cuda or not table.is_contiguous() or table.numel() != table.shape[0] * rot_dim:
+        n_table = table.shape[0]
+        if table.dtype != torch.float32 or not table.is_cuda or not table.is_contiguous() or table.numel() != n_table * rot_dim:
             raise ValueError("table must be a contiguous float32 GPU tensor of positions x rot_dim")
-        tp, n_table = table.data_ptr(), table.shape[0]
-    _check(ctx, load_library().gelo_rope_append(ctx, cache.dtype, n_q_heads, zp, ld, byref(cache.struct), _rows(batch, rows, cache), layout, rot_dim,
-                                                tp, n_table, qp, ldq, _stream(stream)))
+        tp = table.data_ptr()
+    _check_rows(batch, rows, cache)
+    status = load_library().gelo_rope_append(ctx, cache.dtype, n_q_heads, zp, ld, cache.address, batch.address, layout, rot_dim, tp, n_table, qp, ldq,
+                                             _stream(stream))
+    if status != GELO_OK:
+        _check(ctx, status)
 
 
 def gelo_attention(ctx, Q: torch.Tensor, O: torch.Tensor, n_q_heads: int, cache: KvCache, batch: SeqBatch, scale: float, causal: bool = True,
@@ -460,13 +475,15 @@ def gelo_attention(ctx, Q: torch.Tensor, O: torch.Tensor, n_q_heads: int, cache:
     """softmax(scale Q K^T) V over the rows of the cache that each row of Q sees, into O."""
     qp, ldq = _matrix(Q, "Q")
     op, ldo = _matrix(O, "O")
-    rows, width = Q.shape
-    if _dtype_code(Q) != cache.dtype or O.dtype != Q.dtype:
+    shape = Q.shape
+    if Q.dtype != cache.torch_dtype or O.dtype != cache.torch_dtype:
         raise GeloError(3, "Q, O and the cache differ in type")
-    if width != n_q_heads * cache.head_dim or O.shape != Q.shape:
+    if shape[1] != n_q_heads * cache.head_dim or O.shape != shape:
         raise GeloError(2, f"Q and O must have {n_q_heads} heads of {cache.head_dim} values in a row")
-    _check(ctx, load_library().gelo_attention(ctx, cache.dtype, n_q_heads, qp, ldq, byref(cache.struct), _rows(batch, rows, cache), scale,
-                                              1 if causal else 0, op, ldo, _stream(stream)))
+    _check_rows(batch, shape[0], cache)
+    status = load_library().gelo_attention(ctx, cache.dtype, n_q_heads, qp, ldq, cache.address, batch.address, scale, causal, op, ldo, _stream(stream))
+    if status != GELO_OK:
+        _check(ctx, status)
     return O
 
 
