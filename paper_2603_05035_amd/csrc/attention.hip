@@ -15,7 +15,10 @@ namespace gelo {
 namespace {
 
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x3_t __attribute__((ext_vector_type(3), aligned(4)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 constexpr float kLog2E = 1.4426950408889634f;
 
@@ -43,15 +46,22 @@ __device__ __forceinline__ float across_groups_sum(float v) {
     return v + __shfl_xor(v, 32, 64);
 }
 
-template <class T, int D> struct Few;
+// PAST: cache rows are read past the caches (nobody reads them again soon)
+template <class V, bool PAST>
+__device__ __forceinline__ V read_row(const void* p) {
+    if constexpr (PAST) return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
+    else return *reinterpret_cast<const V*>(p);
+}
+
+template <class T, int D, bool PAST> struct Few;
 
 // bfloat16, 32 keys a step.  Lane (g, c) = (lane / 16, lane % 16).
 //   S^T, tile t of 16 keys: A = K, row c = key 16 t + c, contraction values 32 s + 8 g ...: 16 bytes of that key; B = Q^T alike.
 //   The lane then holds S of column c and keys 16 t + 4 g + r.  O^T: the B operand wants 8 keys of column c: those very ones, slot i =
 //   4 t + r.  So A = V^T must have in slot i of group g the key 16 (i / 4) + 4 g + i % 4, for row c: a lane loads VD = D / 16 consecutive values
 //   of these 8 keys (16 lanes: one whole row) and transposes its 8 x VD block in registers; instruction j computes components VD m + j.
-template <int D>
-struct Few<uint16_t, D> {
+template <int D, bool PAST>
+struct Few<uint16_t, D, PAST> {
     static constexpr int KEYS = 32, TILES = 2, KS = D / 32, VD = D / 16, VW = VD / 2;      // VW: 32-bit words of VD values
     typedef bf16x8_t KFrag;
     bf16x8_t q[KS];
@@ -63,7 +73,7 @@ struct Few<uint16_t, D> {
     }
     __device__ __forceinline__ void load_k(int t, const uint16_t* row, int g) {
 #pragma unroll
-        for (int s = 0; s < KS; ++s) k[t][s] = *reinterpret_cast<const bf16x8_t*>(row + 32 * s + 8 * g);
+        for (int s = 0; s < KS; ++s) k[t][s] = read_row<bf16x8_t, PAST>(row + 32 * s + 8 * g);
     }
     // r: slot of the tile's group of four
     __device__ __forceinline__ void load_v(int t, int r, const uint16_t* row, int c) {
@@ -71,16 +81,16 @@ struct Few<uint16_t, D> {
         if constexpr (VW % 4 == 0) {
 #pragma unroll
             for (int w = 0; w < VW; w += 4) {
-                const u32x4_t x = *reinterpret_cast<const u32x4_t*>(p + w);
+                const u32x4_t x = read_row<u32x4_t, PAST>(p + w);
 #pragma unroll
                 for (int u = 0; u < 4; ++u) v[4 * t + r][w + u] = x[u];
             }
         } else if constexpr (VW == 2) {
-            const uint2 x = *reinterpret_cast<const uint2*>(p);
-            v[4 * t + r][0] = x.x; v[4 * t + r][1] = x.y;
+            const u32x2_t x = read_row<u32x2_t, PAST>(p);
+            v[4 * t + r][0] = x[0]; v[4 * t + r][1] = x[1];
         } else {
-            const uint3 x = *reinterpret_cast<const uint3*>(p);                     // 12 bytes, 4-byte aligned
-            v[4 * t + r][0] = x.x; v[4 * t + r][1] = x.y; v[4 * t + r][2] = x.z;
+            const u32x3_t x = read_row<u32x3_t, PAST>(p);
+            v[4 * t + r][0] = x[0]; v[4 * t + r][1] = x[1]; v[4 * t + r][2] = x[2];
         }
     }
     __device__ __forceinline__ f32x4_t scores(int t) const {
@@ -155,8 +165,8 @@ struct Few<uint16_t, D> {
 
 // float, 16 keys a step: v_mfma_f32_16x16x4_f32, one contraction value per lane.  Instruction (s, e) of S^T takes component 16 s + 4 g + e,
 // instruction (r, j) of O^T the key 4 g + r, whose weight is register r of the scores.
-template <int D>
-struct Few<float, D> {
+template <int D, bool PAST>
+struct Few<float, D, PAST> {
     static constexpr int KEYS = 16, TILES = 1, KS = D / 16, VD = D / 16;
     f32x4_t q[KS], k[1][KS];
     float v[4][VD];
@@ -166,22 +176,22 @@ struct Few<float, D> {
     }
     __device__ __forceinline__ void load_k(int, const float* row, int g) {
 #pragma unroll
-        for (int s = 0; s < KS; ++s) k[0][s] = *reinterpret_cast<const f32x4_t*>(row + 16 * s + 4 * g);
+        for (int s = 0; s < KS; ++s) k[0][s] = read_row<f32x4_t, PAST>(row + 16 * s + 4 * g);
     }
     __device__ __forceinline__ void load_v(int, int r, const float* row, int c) {
         const float* p = row + VD * c;
         if constexpr (VD % 4 == 0) {
 #pragma unroll
             for (int w = 0; w < VD; w += 4) {
-                const f32x4_t x = *reinterpret_cast<const f32x4_t*>(p + w);
+                const f32x4_t x = read_row<f32x4_t, PAST>(p + w);
 #pragma unroll
                 for (int u = 0; u < 4; ++u) v[r][w + u] = x[u];
             }
         } else {
 #pragma unroll
             for (int w = 0; w < VD; w += 2) {
-                const float2 x = *reinterpret_cast<const float2*>(p + w);
-                v[r][w] = x.x; v[r][w + 1] = x.y;
+                const f32x2_t x = read_row<f32x2_t, PAST>(p + w);
+                v[r][w] = x[0]; v[r][w + 1] = x[1];
             }
         }
     }
@@ -236,10 +246,10 @@ constexpr int kFewWaves = 4;
 
 // One wave walks the keys `key`, key + stride, ... up to `last` of a tile of 16 columns, KEYS at a time: the running maximum (of log2), the sum of
 // weights over the lane's own keys and the weighted sum of the values.  limit: last key this lane's column sees, least: the least of the tile.
-template <class T, int D>
+template <class T, int D, bool PAST>
 __device__ __forceinline__ void walk_keys(const AttnArgs& a, int seq, int kvh, int key, int stride, int last, int least, int limit, int g, int c,
-                                          Few<T, D>& f, f32x4_t (&acc)[Few<T, D>::VD], float& m, float& l, bool& bad_page) {
-    typedef Few<T, D> F;
+                                          Few<T, D, PAST>& f, f32x4_t (&acc)[Few<T, D, PAST>::VD], float& m, float& l, bool& bad_page) {
+    typedef Few<T, D, PAST> F;
     constexpr int VD = F::VD, SLOTS = 4 * F::TILES;
     const int shift = a.kv.page_shift, in_page = (1 << shift) - 1;
     const int32_t* table = a.b.page_table + seq * a.b.table_ld;
@@ -334,10 +344,10 @@ __device__ __forceinline__ void walk_keys(const AttnArgs& a, int seq, int kvh, i
 }
 
 // A workgroup: one tile of 16 columns of one sequence and key head, one chunk of the cache.
-template <class T, int D>
+template <class T, int D, bool PAST>
 __global__ __launch_bounds__(64 * kFewWaves)
 void attention_few_kernel(AttnArgs a) {
-    typedef Few<T, D> F;
+    typedef Few<T, D, PAST> F;
     constexpr int VD = F::VD;
     __shared__ float joined_o[kFewWaves][16][D + 4];
     __shared__ float joined_ml[kFewWaves][16][2];
@@ -371,7 +381,7 @@ void attention_few_kernel(AttnArgs a) {
     float m = -__builtin_inff(), l = 0.f;
     bool bad_page = false;
 
-    walk_keys<T, D>(a, seq, kvh, begin + wave * F::KEYS, F::KEYS * kFewWaves, end - 1, least, limit, g, c, f, acc, m, l, bad_page);
+    walk_keys<T, D, PAST>(a, seq, kvh, begin + wave * F::KEYS, F::KEYS * kFewWaves, end - 1, least, limit, g, c, f, acc, m, l, bad_page);
     l = across_groups_sum(l);
     if (bad_page) l = __builtin_nanf("");
 
@@ -890,7 +900,7 @@ hipError_t join(const AttnArgs& a, hipStream_t stream) {
 }
 
 // Which kernel, and how the cache is cut: chunks of `chunk` keys, n_chunks of them to the longest sequence.
-struct Plan { bool prompt, paired; int col_tiles, chunk, n_chunks; int64_t workgroups; };
+struct Plan { bool prompt, paired, past; int col_tiles, chunk, n_chunks; int64_t workgroups; };
 constexpr int64_t kMostWorkgroups = 1 << 23;     // of a launch: 2^31 threads and no more fit HIP's 32-bit counts
 constexpr int kCus = 256;
 constexpr int kFewTarget = 512, kFewLeast = 256;         // workgroups that fill the chip (two to a CU), keys to a chunk at least
@@ -906,15 +916,19 @@ double join_us(const Attention& o, const Plan& p) {
     return p.n_chunks == 1 ? 0.0 : 5.0 + 8.0 * p.n_chunks * o.batch.n_rows * o.n_q_heads * o.cache.head_dim / 4e6;
 }
 
-Plan plan_few(const Attention& o, int64_t columns, double* us) {
+Plan plan_few(const Attention& o, int64_t columns, int bytes, double* us) {
     Plan p;
-    p.prompt = p.paired = false;
+    p.prompt = p.paired = p.past = false;
     p.col_tiles = (int)((columns + 15) / 16);
     const int64_t tiles = (int64_t)o.batch.n_seqs * o.cache.n_kv_heads * p.col_tiles;
     const int64_t most = (o.batch.max_kv_len + kFewLeast - 1) / kFewLeast;
     int64_t cuts = kFewTarget / tiles;
     cut(&p, o.batch.max_kv_len, cuts < 1 ? 1 : cuts < most ? cuts : most);
     p.workgroups = tiles * p.n_chunks;
+    // A large cache that is read once passes the caches by: it would not stay there anyway.  64 x 4096 keys of 32 heads of 128, bf16 (4.3 GB), 711
+    // and 621 us (6.9 TB/s), 64 x 512 (0.54 GB) 92 and 84, 16 x 8192 of 2 heads (134 MB) 29.8 and 27.9; 67 MB, which the last-level cache
+    // holds, 16.8 and 17.7.
+    p.past = p.col_tiles == 1 && 2.0 * bytes * tiles * o.batch.max_kv_len * o.cache.head_dim > 100e6;
     // every tile of 16 columns reads the cache's rows again, from L2 as a rule; a wave's step is a trip to memory
     const double rounds = (double)((p.workgroups + kFewTarget - 1) / kFewTarget);
     const double reads = 4.0 * tiles * o.batch.max_kv_len * o.cache.head_dim / 9e6, trips = rounds * (p.chunk / 128) * 1.5;
@@ -930,6 +944,7 @@ Plan plan_few(const Attention& o, int64_t columns, double* us) {
 Plan plan_prompt(const Attention& o, int64_t columns, double* us) {
     Plan best;
     best.prompt = true;
+    best.past = false;
     best.col_tiles = (int)((columns + 32 * kPromptWaves - 1) / (32 * kPromptWaves));
     const int64_t sets = (int64_t)o.batch.n_seqs * o.cache.n_kv_heads, tiles = sets * best.col_tiles;
     const int d = o.cache.head_dim, per_cu = d == 256 ? 1 : 2;
@@ -961,7 +976,7 @@ Plan plan_prompt(const Attention& o, int64_t columns, double* us) {
 Plan plan_of(const Attention& o, int is_bf16) {
     const int64_t columns = (int64_t)o.batch.max_rows * (o.n_q_heads / o.cache.n_kv_heads);
     double few_us, prompt_us;
-    const Plan few = plan_few(o, columns, &few_us);
+    const Plan few = plan_few(o, columns, is_bf16 ? 2 : 4, &few_us);
     if (!is_bf16 || columns <= 16) return few;
     const Plan prompt = plan_prompt(o, columns, &prompt_us);
     return few_us < prompt_us ? few : prompt;
@@ -990,7 +1005,8 @@ hipError_t launch(const Attention& o, hipStream_t stream) {
         if (p.prompt)
             hipLaunchKernelGGL((attention_prompt_kernel<D>), dim3((unsigned)p.workgroups), dim3(64 * kPromptWaves), (size_t)prompt_lds<D>(), stream, a);
     }
-    if (!p.prompt) hipLaunchKernelGGL((attention_few_kernel<T, D>), dim3((unsigned)p.workgroups), dim3(64 * kFewWaves), 0, stream, a);
+    if (!p.prompt && p.past) hipLaunchKernelGGL((attention_few_kernel<T, D, true>), dim3((unsigned)p.workgroups), dim3(64 * kFewWaves), 0, stream, a);
+    else if (!p.prompt) hipLaunchKernelGGL((attention_few_kernel<T, D, false>), dim3((unsigned)p.workgroups), dim3(64 * kFewWaves), 0, stream, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.n_chunks == 1) return e;
     if (p.n_chunks <= 4) return join<T, D, 1>(a, stream);

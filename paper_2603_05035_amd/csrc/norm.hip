@@ -24,17 +24,25 @@ __device__ __forceinline__ void load8(const T* p, float (&v)[8]) {
     }
 }
 
-template <class T>
+// PAST: past the caches, see norm_of_type (not a flag at run time: the compiler makes one plain store of the two)
+template <bool PAST, class T>
 __device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
     if constexpr (sizeof(T) == 2) {
         typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
         bf16x8_t o;
 #pragma unroll
         for (int i = 0; i < 8; ++i) o[i] = (__bf16)v[i];
-        *reinterpret_cast<bf16x8_t*>(p) = o;
+        if constexpr (PAST) __builtin_nontemporal_store(o, reinterpret_cast<bf16x8_t*>(p));
+        else *reinterpret_cast<bf16x8_t*>(p) = o;
     } else {
-        *reinterpret_cast<f32x4_t*>(p) = f32x4_t{v[0], v[1], v[2], v[3]};
-        *reinterpret_cast<f32x4_t*>(p + 4) = f32x4_t{v[4], v[5], v[6], v[7]};
+        const f32x4_t lo = {v[0], v[1], v[2], v[3]}, hi = {v[4], v[5], v[6], v[7]};
+        if constexpr (PAST) {
+            __builtin_nontemporal_store(lo, reinterpret_cast<f32x4_t*>(p));
+            __builtin_nontemporal_store(hi, reinterpret_cast<f32x4_t*>(p + 4));
+        } else {
+            *reinterpret_cast<f32x4_t*>(p) = lo;
+            *reinterpret_cast<f32x4_t*>(p + 4) = hi;
+        }
     }
 }
 
@@ -73,7 +81,7 @@ struct NormArgs {
 };
 
 // TPR threads to a row, up to VPT vectors of 8 values in each; WG threads in all.
-template <class T, int TPR, int VPT, int WG>
+template <class T, int TPR, int VPT, int WG, bool PAST>
 __global__ __launch_bounds__(WG)
 void rms_norm_kernel(NormArgs<T> a) {
     __shared__ float part[2][WG / 64];
@@ -117,7 +125,7 @@ void rms_norm_kernel(NormArgs<T> a) {
     for (int i = 0; i < VPT; ++i) {
         const int v = t + i * TPR;
         if (v >= vecs) continue;
-        if (a.R_out && live) store8(a.R_out + row * a.ldro + 8 * v, h[i]);
+        if (a.R_out && live) store8<PAST>(a.R_out + row * a.ldro + 8 * v, h[i]);
         float g[8];
         load8(a.gamma + 8 * v, g);
 #pragma unroll
@@ -125,7 +133,7 @@ void rms_norm_kernel(NormArgs<T> a) {
             h[i][e] = h[i][e] * inv * g[e];
             top = max_or_nan(top, fabsf(h[i][e]));
         }
-        if (a.H && live) store8(a.H + row * a.ldh + 8 * v, h[i]);
+        if (a.H && live) store8<PAST>(a.H + row * a.ldh + 8 * v, h[i]);
     }
     if (!a.codes) return;
     top = over_row<TPR, true>(top, part[1]);
@@ -147,9 +155,11 @@ void rms_norm_kernel(NormArgs<T> a) {
 }
 
 template <class T, int TPR, int VPT, int WG = (TPR > 256 ? TPR : 256)>
-hipError_t launch(const NormArgs<T>& a, hipStream_t stream) {
+hipError_t launch(const NormArgs<T>& a, bool past, hipStream_t stream) {
     const int rows = WG / TPR;
-    hipLaunchKernelGGL((rms_norm_kernel<T, TPR, VPT, WG>), dim3((a.n + rows - 1) / rows), dim3(WG), 0, stream, a);
+    const dim3 grid((a.n + rows - 1) / rows);
+    if (past) hipLaunchKernelGGL((rms_norm_kernel<T, TPR, VPT, WG, true>), grid, dim3(WG), 0, stream, a);
+    else hipLaunchKernelGGL((rms_norm_kernel<T, TPR, VPT, WG, false>), grid, dim3(WG), 0, stream, a);
     return hipGetLastError();
 }
 
@@ -159,13 +169,19 @@ hipError_t norm_of_type(const RmsNorm& o, hipStream_t stream) {
     a.X = (const T*)o.X; a.ldx = o.ldx; a.R = (const T*)o.R; a.ldr = o.ldr; a.gamma = (const T*)o.gamma;
     a.R_out = (T*)o.R_out; a.ldro = o.ldro; a.H = (T*)o.H; a.ldh = o.ldh;
     a.codes = o.codes; a.ldq = o.ldq; a.scales = o.scales; a.eps = o.eps; a.n = o.n; a.d = o.d;
+    // Results that are more than the L2s hold push each other and the inputs out of them on their way: past the caches 4096 x 4096 bf16 with
+    // residual take 20.1 us (6.7 TB/s) instead of 26.7, and with a kernel behind that reads H 39 instead of 42.  2048 rows (34 MB) take 11 us either
+    // way, and the reader finds less there: 18.8 against 17.5.
+    const bool past = ((o.H ? 1.0 : 0.0) + (o.R_out ? 1.0 : 0.0)) * o.n * o.d * sizeof(T) > 40e6;
     const int vecs = o.d / 8;
-    if (vecs <= 64) return launch<T, 64, 1>(a, stream);
-    if (vecs <= 256) return launch<T, 256, 1>(a, stream);
-    if (vecs <= 512) return launch<T, 256, 2>(a, stream);
-    if (vecs <= 1024) return launch<T, 256, 4>(a, stream);
-    if (vecs <= 2048) return launch<T, 1024, 2>(a, stream);
-    return launch<T, 1024, 8>(a, stream);
+    if (vecs <= 64) return launch<T, 64, 1>(a, past, stream);
+    if (vecs <= 256) return launch<T, 256, 1>(a, past, stream);
+    // (4096 x 4096: 512 threads to a row 20.1 and 26.7 us, 256 21.4 and 28.7; with codes, 2048 rows, 15.0 and 14.6)
+    if (vecs <= 512 && !o.codes) return launch<T, 512, 1>(a, past, stream);
+    if (vecs <= 512) return launch<T, 256, 2>(a, past, stream);
+    if (vecs <= 1024) return launch<T, 256, 4>(a, past, stream);
+    if (vecs <= 2048) return launch<T, 1024, 2>(a, past, stream);
+    return launch<T, 1024, 8>(a, past, stream);
 }
 
 }  // namespace
