@@ -125,7 +125,7 @@ void rms_norm_kernel(NormArgs<T> a) {
     for (int i = 0; i < VPT; ++i) {
         const int v = t + i * TPR;
         if (v >= vecs) continue;
-        if (a.R_out && live) store8<PAST>(a.R_out + row * a.ldro + 8 * v, h[i]);
+        if (a.R_out && live) store8<true>(a.R_out + row * a.ldro + 8 * v, h[i]);
         float g[8];
         load8(a.gamma + 8 * v, g);
 #pragma unroll
@@ -169,9 +169,10 @@ hipError_t norm_of_type(const RmsNorm& o, hipStream_t stream) {
     a.X = (const T*)o.X; a.ldx = o.ldx; a.R = (const T*)o.R; a.ldr = o.ldr; a.gamma = (const T*)o.gamma;
     a.R_out = (T*)o.R_out; a.ldro = o.ldro; a.H = (T*)o.H; a.ldh = o.ldh;
     a.codes = o.codes; a.ldq = o.ldq; a.scales = o.scales; a.eps = o.eps; a.n = o.n; a.d = o.d;
-    // Results that are more than the L2s hold push each other and the inputs out of them on their way: past the caches 4096 x 4096 bf16 with
-    // residual take 20.1 us (6.7 TB/s) instead of 26.7, and with a kernel behind that reads H 39 instead of 42.  2048 rows (34 MB) take 11 us either
-    // way, and the reader finds less there: 18.8 against 17.5.
+    // The residual is read again a layer later, so it always passes the caches by: with codes 2048 x 4096 bf16 take 13.6 us instead of 15.0, 4096
+    // rows 22.3 (5.3 TB/s) instead of 29.2, the 8-bit product behind them 62.7 and 85.0 together instead of 63.4 and 89.8.  H, which the next kernel
+    // reads, goes the same way where both are more than the L2s hold and push the inputs out of them: 4096 x 4096 20.2 us (6.6 TB/s)
+    // instead of 26.7, with a kernel behind that reads H 39 instead of 42; at 2048 rows that reader takes 18.8 and 17.1.
     const bool past = ((o.H ? 1.0 : 0.0) + (o.R_out ? 1.0 : 0.0)) * o.n * o.d * sizeof(T) > 40e6;
     const int vecs = o.d / 8;
     if (vecs <= 64) return launch<T, 64, 1>(a, past, stream);

@@ -693,3 +693,17 @@ def test_refusals_of_append_and_attention(ctx):
     assert status_of(g.gelo_attention, ctx, Q, torch.empty_like(Q), 3, cache, batch, 1.0) == "GELO_ESHAPE"
     three = torch.zeros((3, 128), dtype=BF16, device="cuda")
     assert status_of(g.gelo_attention, ctx, three, torch.empty_like(three), 2, cache, batch, 1.0) == "GELO_ESHAPE"
+
+
+@pytest.mark.parametrize("dtype,bound", [(BF16, 6e-2), (F32, 3e-4)])
+def test_the_layer_example(dtype, bound):
+    """Prompts and single tokens through norm, obfuscated projections, cache and attention.  Each of the two projections may be off by its
+    contract (2e-2 bf16, 1e-4 float), the first one's error passes attention as it is; norm, rotation and attention round once more each."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "serve_layer.py")
+    spec = importlib.util.spec_from_file_location("serve_layer", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    error, _, _ = example.serve(seqs=3, prompt=150, steps=4, dtype=dtype, d=512, q_heads=8, kv_heads=2)
+    assert error < bound
