@@ -32,7 +32,7 @@ struct AttnArgs {
     float scale2s;               // scale log2 e
     uint32_t flip;               // sign bits of Q's words where scale is negative
     int causal;
-    int chunk, n_chunks, col_tiles, paired;
+    int chunk, n_chunks, col_tiles, paired, by_head;
     KvCache kv;
     SeqBatch b;
 };
@@ -343,7 +343,8 @@ __device__ __forceinline__ void walk_keys(const AttnArgs& a, int seq, int kvh, i
     }
 }
 
-// A workgroup: one tile of 16 columns of one sequence and key head, one chunk of the cache.
+// A workgroup: one tile of 16 columns of one sequence and key head, one chunk of the cache, whose keys its waves share out; or (by_head) one
+// sequence and four neighbouring key heads, one to a wave.
 template <class T, int D, bool PAST>
 __global__ __launch_bounds__(64 * kFewWaves)
 void attention_few_kernel(AttnArgs a) {
@@ -351,17 +352,16 @@ void attention_few_kernel(AttnArgs a) {
     constexpr int VD = F::VD;
     __shared__ float joined_o[kFewWaves][16][D + 4];
     __shared__ float joined_ml[kFewWaves][16][2];
-    const int chunk = blockIdx.x % a.n_chunks;
-    int rest = blockIdx.x / a.n_chunks;
-    const int tile = rest % a.col_tiles; rest /= a.col_tiles;
-    const int kvh = rest % a.kv.n_kv_heads, seq = rest / a.kv.n_kv_heads;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tile = a.n_chunks == 1 ? blockIdx.x : blockIdx.x / a.n_chunks, chunk = blockIdx.x - tile * a.n_chunks;
+    const int heads = a.by_head ? kFewWaves : 1;             // key heads of a workgroup
+    const int first_kvh = blockIdx.y * heads, kvh = first_kvh + (a.by_head ? wave : 0), seq = blockIdx.z;
     const NewRows rows = rows_of_sequence(a.b, seq);
     const int columns = rows.count * a.group;
     if (tile * 16 >= columns) return;
     const int kv_len = a.b.kv_len[seq], kv_end = min(kv_len, a.b.max_kv_len);
 
     const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = tile * 16 + c;
     const bool live = col < columns;
     const int my = live ? col : columns - 1;                 // dead columns repeat the last one
@@ -381,7 +381,8 @@ void attention_few_kernel(AttnArgs a) {
     float m = -__builtin_inff(), l = 0.f;
     bool bad_page = false;
 
-    walk_keys<T, D, PAST>(a, seq, kvh, begin + wave * F::KEYS, F::KEYS * kFewWaves, end - 1, least, limit, g, c, f, acc, m, l, bad_page);
+    walk_keys<T, D, PAST>(a, seq, kvh, a.by_head ? begin : begin + wave * F::KEYS, a.by_head ? F::KEYS : F::KEYS * kFewWaves, end - 1, least, limit, g, c, f, acc, m,
+                          l, bad_page);
     l = across_groups_sum(l);
     if (bad_page) l = __builtin_nanf("");
 
@@ -392,19 +393,18 @@ void attention_few_kernel(AttnArgs a) {
         for (int j = 0; j < VD; ++j) joined_o[wave][c][VD * (4 * g + r) + j] = acc[j][r];
     if (g == 0) { joined_ml[wave][c][0] = m; joined_ml[wave][c][1] = l; }
     __syncthreads();
-    const int first_head = kvh * a.group;
-    for (int e = threadIdx.x; e < 16 * (D / 4); e += 64 * kFewWaves) {
-        const int cc = e / (D / 4), x = 4 * (e - cc * (D / 4));
+    for (int e = threadIdx.x; e < heads * 16 * (D / 4); e += 64 * kFewWaves) {
+        const int k16 = e / (D / 4), cc = k16 & 15, hd = k16 >> 4, x = 4 * (e - k16 * (D / 4));
+        const int first_head = (first_kvh + hd) * a.group;
+        const int from = a.by_head ? hd : 0, to = a.by_head ? hd + 1 : kFewWaves;             // the waves that have parts of this column
         const int cl = tile * 16 + cc;
         if (cl >= columns) continue;
-        float top = joined_ml[0][cc][0];
-#pragma unroll
-        for (int w = 1; w < kFewWaves; ++w) top = fmaxf(top, joined_ml[w][cc][0]);
+        float top = joined_ml[from][cc][0];
+        for (int w = from + 1; w < to; ++w) top = fmaxf(top, joined_ml[w][cc][0]);
         const float safe = top == -__builtin_inff() ? 0.f : top;
         float total = 0.f;
         f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int w = 0; w < kFewWaves; ++w) {
+        for (int w = from; w < to; ++w) {
             if (joined_ml[w][cc][1] == 0.f) continue;        // nothing seen: 0 times what it holds need not be 0
             const float k = __builtin_amdgcn_exp2f(joined_ml[w][cc][0] - safe);
             total += k * joined_ml[w][cc][1];
@@ -900,7 +900,7 @@ hipError_t join(const AttnArgs& a, hipStream_t stream) {
 }
 
 // Which kernel, and how the cache is cut: chunks of `chunk` keys, n_chunks of them to the longest sequence.
-struct Plan { bool prompt, paired, past; int col_tiles, chunk, n_chunks; int64_t workgroups; };
+struct Plan { bool prompt, paired, past, by_head; int col_tiles, chunk, n_chunks; int64_t workgroups; };
 constexpr int64_t kMostWorkgroups = 1 << 23;     // of a launch: 2^31 threads and no more fit HIP's 32-bit counts
 constexpr int kCus = 256;
 constexpr int kFewTarget = 512, kFewLeast = 256;         // workgroups that fill the chip (two to a CU), keys to a chunk at least
@@ -918,7 +918,7 @@ double join_us(const Attention& o, const Plan& p) {
 
 Plan plan_few(const Attention& o, int64_t columns, int bytes, double* us) {
     Plan p;
-    p.prompt = p.paired = p.past = false;
+    p.prompt = p.paired = p.past = p.by_head = false;
     p.col_tiles = (int)((columns + 15) / 16);
     const int64_t tiles = (int64_t)o.batch.n_seqs * o.cache.n_kv_heads * p.col_tiles;
     const int64_t most = (o.batch.max_kv_len + kFewLeast - 1) / kFewLeast;
@@ -929,6 +929,10 @@ Plan plan_few(const Attention& o, int64_t columns, int bytes, double* us) {
     // and 621 us (6.9 TB/s), 64 x 512 (0.54 GB) 92 and 84, 16 x 8192 of 2 heads (134 MB) 29.8 and 27.9; 67 MB, which the last-level cache
     // holds, 16.8 and 17.7.
     p.past = p.col_tiles == 1 && 2.0 * bytes * tiles * o.batch.max_kv_len * o.cache.head_dim > 100e6;
+    // Where the rows of all heads lie side by side, four heads' are one piece of memory: 64 x 4096 keys of 32 heads of 128, bf16, 714 us with
+    // the keys of a head shared out over the waves and 653 with a head to each, 64 x 512 94 and 89; with a head's rows side by side 621 and 622.
+    p.by_head = p.n_chunks == 1 && p.col_tiles == 1 && o.cache.n_kv_heads % kFewWaves == 0 && o.cache.head_stride == o.cache.head_dim && tiles / kFewWaves >= kFewTarget;
+    if (p.by_head) p.workgroups = tiles / kFewWaves;
     // every tile of 16 columns reads the cache's rows again, from L2 as a rule; a wave's step is a trip to memory
     const double rounds = (double)((p.workgroups + kFewTarget - 1) / kFewTarget);
     const double reads = 4.0 * tiles * o.batch.max_kv_len * o.cache.head_dim / 9e6, trips = rounds * (p.chunk / 128) * 1.5;
@@ -944,7 +948,7 @@ Plan plan_few(const Attention& o, int64_t columns, int bytes, double* us) {
 Plan plan_prompt(const Attention& o, int64_t columns, double* us) {
     Plan best;
     best.prompt = true;
-    best.past = false;
+    best.past = best.by_head = false;
     best.col_tiles = (int)((columns + 32 * kPromptWaves - 1) / (32 * kPromptWaves));
     const int64_t sets = (int64_t)o.batch.n_seqs * o.cache.n_kv_heads, tiles = sets * best.col_tiles;
     const int d = o.cache.head_dim, per_cu = d == 256 ? 1 : 2;
@@ -996,7 +1000,7 @@ hipError_t launch(const Attention& o, hipStream_t stream) {
     a.scale2 = o.scale == 0.f ? 1e-30f : fabsf(a.scale2s);      // (-inf, a hidden score, times 0 would be NaN)
     a.flip = o.scale < 0.f ? 0x80008000u : 0u;
     a.causal = o.causal;
-    a.chunk = p.chunk; a.n_chunks = p.n_chunks; a.col_tiles = p.col_tiles; a.paired = p.paired;
+    a.chunk = p.chunk; a.n_chunks = p.n_chunks; a.col_tiles = p.col_tiles; a.paired = p.paired; a.by_head = p.by_head;
     a.kv = o.cache; a.b = o.batch;
     const int64_t items = (int64_t)o.batch.n_rows * o.n_q_heads;
     a.part_o = o.workspace;
@@ -1005,8 +1009,9 @@ hipError_t launch(const Attention& o, hipStream_t stream) {
         if (p.prompt)
             hipLaunchKernelGGL((attention_prompt_kernel<D>), dim3((unsigned)p.workgroups), dim3(64 * kPromptWaves), (size_t)prompt_lds<D>(), stream, a);
     }
-    if (!p.prompt && p.past) hipLaunchKernelGGL((attention_few_kernel<T, D, true>), dim3((unsigned)p.workgroups), dim3(64 * kFewWaves), 0, stream, a);
-    else if (!p.prompt) hipLaunchKernelGGL((attention_few_kernel<T, D, false>), dim3((unsigned)p.workgroups), dim3(64 * kFewWaves), 0, stream, a);
+    const dim3 few((unsigned)(p.col_tiles * p.n_chunks), (unsigned)(o.cache.n_kv_heads / (p.by_head ? kFewWaves : 1)), (unsigned)o.batch.n_seqs);
+    if (!p.prompt && p.past) hipLaunchKernelGGL((attention_few_kernel<T, D, true>), few, dim3(64 * kFewWaves), 0, stream, a);
+    else if (!p.prompt) hipLaunchKernelGGL((attention_few_kernel<T, D, false>), few, dim3(64 * kFewWaves), 0, stream, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.n_chunks == 1) return e;
     if (p.n_chunks <= 4) return join<T, D, 1>(a, stream);
@@ -1037,6 +1042,7 @@ int attention_way(int is_bf16, int causal, int n_q_heads, int n_kv_heads, int he
 }
 
 bool attention_fits(const Attention& o, int is_bf16) {
+    if (o.batch.n_seqs > 65535 || o.cache.n_kv_heads > 65535) return false;          // dimensions of a launch
     return plan_of(o, is_bf16).workgroups <= kMostWorkgroups && (int64_t)o.batch.n_rows * o.n_q_heads <= kMostWorkgroups;
 }
 size_t attention_workspace_bytes(const Attention& o, int is_bf16) { return part_bytes(o, plan_of(o, is_bf16)); }

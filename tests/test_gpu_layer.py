@@ -291,6 +291,15 @@ def test_attention_of_single_tokens(ctx, dtype, kv, hq, hkv, d, page, order):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("order", ["row", "head"])
+def test_single_tokens_of_many_sequences(ctx, dtype, order):
+    """So many sequences and heads that a wave has a head of its own where the heads' rows lie side by side; lengths at the edges of tiles."""
+    kv = [0, 1, 15, 16, 17, 31, 32, 33, 100, 127, 128, 129] * 11
+    run_attention(ctx, dtype, [1] * len(kv), kv, 16, 16, 64, 16, order, True, one_row=True, seed=2)
+    run_attention(ctx, dtype, [1] * len(kv), kv, 48, 16, 96, 32, order, True, one_row=True, seed=2)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 def test_attention_where_the_bound_is_far_above_the_lengths(ctx, dtype):
     """A captured launch is sized for the longest context: chunks that no sequence reaches."""
     run_attention(ctx, dtype, [1] * 3, [3, 700, 0], 4, 2, 128, 16, "head", True, one_row=True, max_kv=9000)
