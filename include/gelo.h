@@ -332,7 +332,7 @@ gelo_status gelo_rope_append(gelo_ctx* ctx, gelo_dtype dtype, int n_q_heads, con
 /* Attention over the cache: O[row, h] = sum_p softmax_p(scale Q[row, h] . K[p, h']) V[p, h'], h' = h n_kv_heads / n_q_heads
  * (n_q_heads a multiple of n_kv_heads).  causal != 0: row j of the n that sequence s brings sees the rows p <= kv_len[s] - n + j of
  * the cache (its own last; kv_len counts the new rows, which are in the cache already); causal = 0: all p < kv_len[s] (cross
- * attention to states of another length).  A row that sees nothing gives zeros.  Q, O: n_rows x n_q_heads head_dim of type
+ * attention to states of another length).  A row that sees nothing gives zeros (one that sees only scores of -infinity: NaN).  Q, O: n_rows x n_q_heads head_dim of type
  * `dtype` (ldq, ldo), O not in Q's memory; head_dim 64, 96, 128 or 256.  Rows outside [row_start[0], row_start[n_seqs]) are left as
  * they are.  kv_len beyond max_kv_len is cut to it; a page number outside the cache is not followed: the
  * results of its sequence are then NaN or partly so.  Statistics, products and sums are float; GELO_BF16 rounds the weights exp(s - max) to bfloat16 for the product with V, their sum does

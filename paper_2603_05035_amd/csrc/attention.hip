@@ -235,6 +235,10 @@ struct Few<float, D, PAST> {
     }
 };
 
+// What a row's sums are divided by, as a factor.  No weight at all: a row that sees nothing is to give zeros; one that sees only scores of
+// -infinity has no softmax.
+__device__ __forceinline__ float inverse_of(float total, bool sees) { return total == 0.f ? sees ? __builtin_nanf("") : 0.f : 1.f / total; }
+
 template <class T> __device__ __forceinline__ void store4(T* p, f32x4_t v);
 template <> __device__ __forceinline__ void store4<float>(float* p, f32x4_t v) { *reinterpret_cast<f32x4_t*>(p) = v; }
 template <> __device__ __forceinline__ void store4<uint16_t>(uint16_t* p, f32x4_t v) {
@@ -367,7 +371,8 @@ void attention_few_kernel(AttnArgs a) {
     const int my = live ? col : columns - 1;                 // dead columns repeat the last one
     const int i = my / a.group, head = kvh * a.group + my - i * a.group;
     const int row = rows.first + i;
-    const int limit = min(a.causal ? kv_len - rows.count + i : kv_len - 1, kv_end - 1);      // last key this column sees
+    auto limit_of = [&](int i) { return min(a.causal ? kv_len - rows.count + i : kv_len - 1, kv_end - 1); };
+    const int limit = limit_of(i);                           // last key this column sees
     // the last column sees most, the first one least
     const int most = __builtin_amdgcn_readlane(limit, 15), least = __builtin_amdgcn_readfirstlane(limit);
     const int begin = chunk * a.chunk, end = min(begin + a.chunk, most + 1);
@@ -415,9 +420,9 @@ void attention_few_kernel(AttnArgs a) {
         const int ri = cl / a.group, h = first_head + cl - ri * a.group;
         const int64_t rr = rows.first + ri;
         if (a.n_chunks == 1) {
-            const float inv = total == 0.f ? 0.f : 1.f / total;
+            const float inv = inverse_of(total, limit_of(ri) >= 0);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) o[u] = total == 0.f ? 0.f : o[u] * inv;
+            for (int u = 0; u < 4; ++u) o[u] *= inv;         // (nothing was added to o where there was no weight)
             store4((T*)a.O + rr * a.ldo + (int64_t)h * D + x, o);
         } else {
             const int64_t item = ((int64_t)chunk * a.b.n_rows + rr) * a.n_q_heads + h;
@@ -768,7 +773,7 @@ __device__ __forceinline__ void prompt_tile(const AttnArgs& a, int seq, int kvh,
     const bool whole = a.n_chunks == 1;
     float total = l + __shfl_xor(l, 32, 64);
     if (any_bad) total = __builtin_nanf("");
-    const float inv = total == 0.f ? 0.f : 1.f / total;
+    const float by = whole ? inverse_of(total, limit >= 0) : 1.f;       // (without weights acc is 0: what was not finite is out of it by now)
     const int64_t part = ((int64_t)chunk * a.b.n_rows + row) * a.n_q_heads + head;
 #pragma unroll
     for (int t = 0; t < DT; ++t)
@@ -778,7 +783,7 @@ __device__ __forceinline__ void prompt_tile(const AttnArgs& a, int seq, int kvh,
             f32x4_t o;
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                o[u] = total == 0.f ? 0.f : whole ? acc[t][4 * e + u] * inv : acc[t][4 * e + u];
+                o[u] = acc[t][4 * e + u] * by;
                 if (any_odd) o[u] += (first_odd[0][x + u] <= limit ? __builtin_inff() : 0.f) - (first_odd[1][x + u] <= limit ? __builtin_inff() : 0.f);
             }
             if (whole) store4((uint16_t*)a.O + row * a.ldo + (int64_t)head * D + x, o);
@@ -885,9 +890,9 @@ void attention_join_kernel(AttnArgs a) {
         }
     }
     if (!there) return;
-    const float inv = total == 0.f ? 0.f : 1.f / total;
+    const float inv = inverse_of(total, used > 0);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) o[u] = total == 0.f ? 0.f : o[u] * inv;
+    for (int u = 0; u < 4; ++u) o[u] *= inv;                 // (nothing was added to o where there was no weight)
     store4((T*)a.O + row * a.ldo + (item - (int64_t)row * a.n_q_heads) * D + x, o);
 }
 

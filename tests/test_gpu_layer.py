@@ -510,6 +510,34 @@ def test_a_cut_cache_and_values_that_are_not_finite(ctx, d):
     assert torch.equal(o[..., other], w[..., other]) and torch.equal(o[:first], w[:first]) and torch.all(o[first:, :, 5] == float("inf"))
 
 
+# the ways are the numbers of `way`; float goes through the one kernel it has
+NO_SOFTMAX = [(F32, [1, 1], [300, 0], 4, 64, None), (F32, [40, 7], [40, 1500], 2, 128, None), (BF16, [1, 1], [200, 0], 4, 96, 0),
+              (BF16, [1, 1], [9000, 0], 4, 128, 4), (BF16, [150] * 14 + [3], [150] * 14 + [0], 16, 128, 1),
+              (BF16, [150] * 16 + [3], [150] * 16 + [0], 16, 96, 2), (BF16, [200, 4], [4096, 0], 4, 64, 5)]
+
+
+@pytest.mark.parametrize("dtype,new,kv,hq,d,want", NO_SOFTMAX)
+def test_a_row_that_sees_only_scores_of_minus_infinity_has_no_softmax(ctx, dtype, new, kv, hq, d, want):
+    """exp(-inf - max) / sum is 0 / 0 there: NaN, unlike the zeros of a row that sees no key.  The other rows and heads do not notice."""
+    page = 16
+    batch, table, row_start, n_pages = make_batch(new, kv, page, 3)
+    K, V = make_cache(n_pages, hq, page, d, dtype, "head", seed=5)
+    K[..., 0] = K[..., 0].abs() + 0.125
+    rows = int(row_start[-1])
+    Q = rand((rows, hq * d), 8, dtype)
+    row, head = min(rows - 1, 33) if new[0] > 1 else 0, hq - 1
+    Q[row, head * d] = -math.inf
+    O = torch.full_like(Q, 7.0)
+    if want is not None:
+        assert way(ctx, Q, new, kv, hq, hq, d, True) == want
+    g.gelo_attention(ctx, Q, O, hq, g.KvCache(K, V), batch, 1 / math.sqrt(d))
+    there = torch.isnan(O).view(rows, hq, d)
+    assert there[row, head].all() and there.sum() == d
+    for s, n in enumerate(kv):
+        if n == 0:
+            assert torch.all(O[int(row_start[s]):int(row_start[s + 1])] == 0)
+
+
 def test_page_numbers_outside_the_cache_are_not_followed(ctx):
     K, V = make_cache(4, 2, 16, 64, BF16, "head", seed=3)
     table = torch.tensor([[0, 1 << 29], [2, 3], [-5, 1]], dtype=torch.int32, device="cuda")
