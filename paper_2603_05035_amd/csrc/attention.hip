@@ -55,18 +55,21 @@ __device__ __forceinline__ V read_row(const void* p) {
 
 template <class T, int D, bool PAST> struct Few;
 
-// bfloat16, 32 keys a step.  Lane (g, c) = (lane / 16, lane % 16).
+// bfloat16, 32 keys a step, of heads of 256 half of that (what follows is for 32): with 32 the registers leave one wave to a SIMD, and few keys
+// take long: 14 sequences of 21 rows and 60 keys, 32 heads, 36.4 us with 32 and 22.7 with 16, one row of 256 sequences of 64 keys, 8 heads, 47.6
+// and 31.3, of 16 sequences of 2048 keys 54.2 and 51.5.  Lane (g, c) = (lane / 16, lane % 16).
 //   S^T, tile t of 16 keys: A = K, row c = key 16 t + c, contraction values 32 s + 8 g ...: 16 bytes of that key; B = Q^T alike.
 //   The lane then holds S of column c and keys 16 t + 4 g + r.  O^T: the B operand wants 8 keys of column c: those very ones, slot i =
 //   4 t + r.  So A = V^T must have in slot i of group g the key 16 (i / 4) + 4 g + i % 4, for row c: a lane loads VD = D / 16 consecutive values
 //   of these 8 keys (16 lanes: one whole row) and transposes its 8 x VD block in registers; instruction j computes components VD m + j.
 template <int D, bool PAST>
 struct Few<uint16_t, D, PAST> {
-    static constexpr int KEYS = 32, TILES = 2, KS = D / 32, VD = D / 16, VW = VD / 2;      // VW: 32-bit words of VD values
-    typedef bf16x8_t KFrag;
+    static constexpr int TILES = D < 256 ? 2 : 1, KEYS = 16 * TILES, SLOTS = 4 * TILES;
+    static constexpr int KS = D / 32, VD = D / 16, VW = VD / 2;        // VW: 32-bit words of VD values
+    typedef uint32_t frag_t __attribute__((ext_vector_type(2 * TILES)));       // SLOTS weights or values
     bf16x8_t q[KS];
     bf16x8_t k[TILES][KS];
-    uint32_t v[8][VW];
+    uint32_t v[SLOTS][VW];
     __device__ __forceinline__ void load_q(const uint16_t* p, int g) {
 #pragma unroll
         for (int s = 0; s < KS; ++s) q[s] = *reinterpret_cast<const bf16x8_t*>(p + 32 * s + 8 * g);
@@ -99,47 +102,53 @@ struct Few<uint16_t, D, PAST> {
         for (int i = 0; i < KS; ++i) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[t][i], q[i], s, 0, 0, 0);
         return s;
     }
-    // operand of O^T for component j of the lane's VD: half j % 2 of word j / 2 of the 8 slots
-    __device__ __forceinline__ u32x4_t v_frag(int j) const {
-        u32x4_t f;
+    // operand of O^T for component j of the lane's VD: half j % 2 of word j / 2 of the slots
+    __device__ __forceinline__ frag_t v_frag(int j) const {
+        frag_t f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 2 * TILES; ++i)
             f[i] = __builtin_amdgcn_perm(v[2 * i + 1][j >> 1], v[2 * i][j >> 1], (j & 1) ? 0x07060302u : 0x05040100u);
         return f;
     }
-    static __device__ __forceinline__ bf16x8_t weights(const float (&p)[8]) {
-        bf16x8_t o;
+    static __device__ __forceinline__ frag_t weights(const float (&p)[SLOTS]) {
+        typedef __bf16 pack_t __attribute__((ext_vector_type(SLOTS)));
+        pack_t o;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = (__bf16)p[i];
-        return o;
+        for (int i = 0; i < SLOTS; ++i) o[i] = (__bf16)p[i];
+        return __builtin_bit_cast(frag_t, o);
     }
-    __device__ __forceinline__ void accumulate(f32x4_t (&acc)[VD], const float (&p)[8]) const {
-        const bf16x8_t w = weights(p);
+    static __device__ __forceinline__ f32x4_t product(frag_t values, frag_t weights, f32x4_t sum) {
+        typedef short s16x4_t __attribute__((ext_vector_type(4)));
+        if constexpr (TILES == 2) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, values), __builtin_bit_cast(bf16x8_t, weights), sum, 0, 0, 0);
+        else return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4_t, values), __builtin_bit_cast(s16x4_t, weights), sum, 0, 0, 0);
+    }
+    __device__ __forceinline__ void accumulate(f32x4_t (&acc)[VD], const float (&p)[SLOTS]) const {
+        const frag_t w = weights(p);
 #pragma unroll
-        for (int j = 0; j < VD; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, v_frag(j)), w, acc[j], 0, 0, 0);
+        for (int j = 0; j < VD; ++j) acc[j] = product(v_frag(j), w, acc[j]);
     }
     __device__ __forceinline__ bool odd_values() const {       // a NaN or an infinity among the values
         bool odd = false;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < SLOTS; ++i)
 #pragma unroll
             for (int w = 0; w < VW; ++w) odd |= (v[i][w] & 0x7F80u) == 0x7F80u || (v[i][w] & 0x7F800000u) == 0x7F800000u;
         return odd;
     }
     // as accumulate, where some keys are hidden from some columns (seen: bit per slot) and some values are not finite: 0 times those would be
     // NaN in columns that do not see them.  The finite part is summed as ever; how many +inf (-inf, NaN: both) a column sees is counted by two more products.
-    __device__ __forceinline__ void accumulate_odd(f32x4_t (&acc)[VD], const float (&p)[8], uint32_t seen) const {
-        const bf16x8_t w = weights(p);
-        float one[8];
+    __device__ __forceinline__ void accumulate_odd(f32x4_t (&acc)[VD], const float (&p)[SLOTS], uint32_t seen) const {
+        const frag_t w = weights(p);
+        float one[SLOTS];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) one[i] = (seen >> i) & 1 ? 1.f : 0.f;
-        const bf16x8_t sees = weights(one);
+        for (int i = 0; i < SLOTS; ++i) one[i] = (seen >> i) & 1 ? 1.f : 0.f;
+        const frag_t sees = weights(one);
         for (int j = 0; j < VD; ++j) {
-            u32x4_t f = {0, 0, 0, 0}, fin = f, up = {0, 0, 0, 0}, down = {0, 0, 0, 0};
+            frag_t f = frag_t(0u), fin = f, up = f, down = f;
 #pragma unroll
             for (int jj = 0; jj < VD; ++jj) if (jj == j) f = v_frag(jj);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 2 * TILES; ++i)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const uint32_t x = (f[i] >> (16 * h)) & 0xFFFFu;
@@ -152,9 +161,8 @@ struct Few<uint16_t, D, PAST> {
             f32x4_t sum = zero;
 #pragma unroll
             for (int jj = 0; jj < VD; ++jj) if (jj == j) sum = acc[jj];
-            sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, fin), w, sum, 0, 0, 0);
-            const f32x4_t ups = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, up), sees, zero, 0, 0, 0);
-            const f32x4_t downs = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, down), sees, zero, 0, 0, 0);
+            sum = product(fin, w, sum);
+            const f32x4_t ups = product(up, sees, zero), downs = product(down, sees, zero);
 #pragma unroll
             for (int r = 0; r < 4; ++r) sum[r] += (ups[r] > 0.f ? __builtin_inff() : 0.f) - (downs[r] > 0.f ? __builtin_inff() : 0.f);
 #pragma unroll
@@ -350,7 +358,7 @@ __device__ __forceinline__ void walk_keys(const AttnArgs& a, int seq, int kvh, i
 // A workgroup: one tile of 16 columns of one sequence and key head, one chunk of the cache, whose keys its waves share out; or (by_head) one
 // sequence and four neighbouring key heads, one to a wave.
 template <class T, int D, bool PAST>
-__global__ __launch_bounds__(64 * kFewWaves)
+__global__ __launch_bounds__(64 * kFewWaves, sizeof(T) == 2 || D < 256 ? 2 : 1)
 void attention_few_kernel(AttnArgs a) {
     typedef Few<T, D, PAST> F;
     constexpr int VD = F::VD;
