@@ -477,16 +477,23 @@ template <int D> __device__ __forceinline__ int v_pos(int r, int c) {          /
     else return c ^ ((r & 3) << 2);
 }
 
-// One tile of columns of a sequence and key head, one chunk of the cache.
-template <int D>
-__device__ __forceinline__ void prompt_tile(const AttnArgs& a, int seq, int kvh, int chunk, int tile) {
+// 0 times a value that is not finite is NaN also in columns that do not see its key.  Such values are rare, and they show in the result: a
+// workgroup that finds any there walks its keys once more (ODD) with zeros in their place and adds them to the columns that see them.
+template <int D> struct PromptNotes {
+    int odd, bad;                                            // results that are not finite, page numbers outside the cache
+    int first[2][D];                                         // per component the first key whose value is +infinity (-infinity), NaN: both
+};
+
+// One tile of columns of a sequence and key head, one chunk of the cache.  True: to be done again with ODD.
+template <int D, bool ODD>
+__device__ __forceinline__ bool prompt_tile(const AttnArgs& a, int seq, int kvh, int chunk, int tile, PromptNotes<D>& notes) {
     constexpr int KT = kPromptKeys, KS = D / 16, DT = D / 32, PITCH = 2 * D, SLOT = KT * PITCH, WIDE = 32 * kPromptWaves;
     constexpr int ROWS = KT / kPromptWaves;                  // rows a wave fetches
     constexpr int NF = ROWS * PITCH / 1024;                  // fetches of 1 KB for them
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
     const NewRows rows = rows_of_sequence(a.b, seq);
     const int columns = rows.count * a.group, first_col = tile * WIDE;
-    if (first_col >= columns) return;
+    if (first_col >= columns) return false;
     const int kv_len = a.b.kv_len[seq], kv_end = min(kv_len, a.b.max_kv_len);
     const int lane = threadIdx.x & 63, h = lane >> 5, c = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -494,7 +501,7 @@ __device__ __forceinline__ void prompt_tile(const AttnArgs& a, int seq, int kvh,
     auto limit_of = [&](int col) { return min(a.causal ? kv_len - rows.count + col / a.group : kv_len - 1, kv_end - 1); };
     const int wg_most = limit_of(min(first_col + WIDE, columns) - 1);
     const int begin = chunk * a.chunk, end = min(begin + a.chunk, wg_most + 1);
-    if (begin >= end && a.n_chunks > 1) return;
+    if (begin >= end && a.n_chunks > 1) return false;
     const int last = end - 1, steps = end > begin ? (end - begin + KT - 1) / KT : 0;
 
     // fetches: this wave's 16 rows of a step, 1 KB at a time; the keys of 16 rows share a page
@@ -656,131 +663,129 @@ __device__ __forceinline__ void prompt_tile(const AttnArgs& a, int seq, int kvh,
     constexpr std::integral_constant<int, 0> first{};                // where the two groups of a step begin in a slot
     constexpr std::integral_constant<int, 32 * PITCH> second{};
 
-    // 0 times a value that is not finite is NaN also in columns that do not see its key.  Such values are rare, and they show in the result: a
-    // workgroup that finds any there walks its keys once more with zeros in their place and adds them to the columns that see them.
-    __shared__ int any_odd, any_bad, first_odd[2][D];
-    if (threadIdx.x == 0) any_odd = any_bad = 0;
-    for (int x = threadIdx.x; x < 2 * D; x += 64 * kPromptWaves) (&first_odd[0][0])[x] = 0x7FFFFFFF;
-    for (int pass = 0;; ++pass) {
-        m = -__builtin_inff();
-        base = l = 0.f;
+    if constexpr (ODD) {
+        for (int x = threadIdx.x; x < 2 * D; x += 64 * kPromptWaves) (&notes.first[0][0])[x] = 0x7FFFFFFF;
+    } else if (threadIdx.x == 0) {
+        notes.odd = notes.bad = 0;
+    }
+    m = -__builtin_inff();
+    base = l = 0.f;
 #pragma unroll
-        for (int t = 0; t < DT; ++t) acc[t] = zero;
+    for (int t = 0; t < DT; ++t) acc[t] = zero;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) p[1][0][e] = p[1][1][e] = (__bf16)0.f;
-        // nothing comes before the first group: no weights, and zeros in the place of its values
-        for (int x = threadIdx.x * 16; x < 32 * PITCH; x += 64 * kPromptWaves * 16) *reinterpret_cast<u32x4_t*>(lds + 3 * SLOT + 32 * PITCH + x) = u32x4_t{0, 0, 0, 0};
-        int page = 0;                                        // in a lane's register: of the step three further on
-        int64_t k_rows = 0, v_rows = 0;                      // where the rows of the next fetches begin
+    for (int e = 0; e < 8; ++e) p[1][0][e] = p[1][1][e] = (__bf16)0.f;
+    // nothing comes before the first group: no weights, and zeros in the place of its values
+    for (int x = threadIdx.x * 16; x < 32 * PITCH; x += 64 * kPromptWaves * 16) *reinterpret_cast<u32x4_t*>(lds + 3 * SLOT + 32 * PITCH + x) = u32x4_t{0, 0, 0, 0};
+    int page = 0;                                        // in a lane's register: of the step three further on
+    int64_t k_rows = 0, v_rows = 0;                      // where the rows of the next fetches begin
 #pragma unroll
-        for (int i = 0; i < NF; ++i) {
-            const int at = i * 1024 + lane * 16, r = at / PITCH, x = (at - r * PITCH) / 16, rr = wave * ROWS + r;
-            k_off[i] = (uint32_t)(r * (int)a.kv.row_stride + 8 * k_chunk<D>(rr, x)) * 2;
-            v_off[i] = (uint32_t)(r * (int)a.kv.row_stride + 8 * v_pos<D>(rr, x)) * 2;
+    for (int i = 0; i < NF; ++i) {
+        const int at = i * 1024 + lane * 16, r = at / PITCH, x = (at - r * PITCH) / 16, rr = wave * ROWS + r;
+        k_off[i] = (uint32_t)(r * (int)a.kv.row_stride + 8 * k_chunk<D>(rr, x)) * 2;
+        v_off[i] = (uint32_t)(r * (int)a.kv.row_stride + 8 * v_pos<D>(rr, x)) * 2;
+    }
+    if (steps > 0) {
+        const int page0 = load_page(0), page1 = load_page(1);
+        page = load_page(2);
+        v_rows = rows_at(0, __builtin_amdgcn_readfirstlane(page0));
+        trim(k_off, 0);
+#pragma unroll
+        for (int i = 0; i < NF; ++i) fetch16(k_off[i], k_head + v_rows, my_rows + i * 1024);
+        if (steps > 1) {
+            k_rows = rows_at(1, __builtin_amdgcn_readfirstlane(page1));
+            trim(k_off, 1);
+#pragma unroll
+            for (int i = 0; i < NF; ++i) fetch16(k_off[i], k_head + k_rows, my_rows + SLOT + i * 1024);
         }
-        if (steps > 0) {
-            const int page0 = load_page(0), page1 = load_page(1);
-            page = load_page(2);
-            v_rows = rows_at(0, __builtin_amdgcn_readfirstlane(page0));
-            trim(k_off, 0);
+        trim(v_off, 0);
 #pragma unroll
-            for (int i = 0; i < NF; ++i) fetch16(k_off[i], k_head + v_rows, my_rows + i * 1024);
-            if (steps > 1) {
-                k_rows = rows_at(1, __builtin_amdgcn_readfirstlane(page1));
-                trim(k_off, 1);
+        for (int i = 0; i < NF; ++i) fetch16(v_off[i], v_head + v_rows, my_rows + 2 * SLOT + i * 1024);
+        if (steps > 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(2 * NF) : "memory");
+        else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(NF) : "memory");
+        __builtin_amdgcn_s_barrier();
+    }
+    int step = 0;
+    // between the two groups of a step: its V and the next step's K are there
+    auto turn = [&] {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        if constexpr (ODD) {
+            // the values that are not finite go, and per component the first key that had one is kept
+            for (int x = threadIdx.x * 16; x < SLOT; x += 64 * kPromptWaves * 16) {
+                const int r = x / PITCH, d = 8 * v_pos<D>(r, (x - r * PITCH) / 16);
+                s16x8_t* where = reinterpret_cast<s16x8_t*>(lds + (2 + (step & 1)) * SLOT + x);
+                s16x8_t v = *where;
 #pragma unroll
-                for (int i = 0; i < NF; ++i) fetch16(k_off[i], k_head + k_rows, my_rows + SLOT + i * 1024);
+                for (int e = 0; e < 8; ++e) {
+                    if ((v[e] & 0x7F80) != 0x7F80) continue;
+                    const bool nan = v[e] & 0x7F;
+                    if (nan || v[e] > 0) atomicMin(&notes.first[0][d + e], begin + step * KT + r);
+                    if (nan || v[e] < 0) atomicMin(&notes.first[1][d + e], begin + step * KT + r);
+                    v[e] = 0;
+                }
+                *where = v;
             }
-            trim(v_off, 0);
-#pragma unroll
-            for (int i = 0; i < NF; ++i) fetch16(v_off[i], v_head + v_rows, my_rows + 2 * SLOT + i * 1024);
-            if (steps > 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(2 * NF) : "memory");
-            else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(NF) : "memory");
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();
         }
-        int step = 0;
-        // between the two groups of a step: its V and the next step's K are there
-        auto turn = [&] {
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-            __builtin_amdgcn_s_barrier();
-            if (pass == 1) {
-                // the values that are not finite go, and per component the first key that had one is kept
-                for (int x = threadIdx.x * 16; x < SLOT; x += 64 * kPromptWaves * 16) {
-                    const int r = x / PITCH, d = 8 * v_pos<D>(r, (x - r * PITCH) / 16);
-                    s16x8_t* where = reinterpret_cast<s16x8_t*>(lds + (2 + (step & 1)) * SLOT + x);
-                    s16x8_t v = *where;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        if ((v[e] & 0x7F80) != 0x7F80) continue;
-                        const bool nan = v[e] & 0x7F;
-                        if (nan || v[e] > 0) atomicMin(&first_odd[0][d + e], begin + step * KT + r);
-                        if (nan || v[e] < 0) atomicMin(&first_odd[1][d + e], begin + step * KT + r);
-                        v[e] = 0;
-                    }
-                    *where = v;
+    };
+    // what follows it: V of the next step and K of the one after are sent for, in 1 + 2 NF pieces
+    auto send = [&](auto ic) {
+        constexpr int i = decltype(ic)::value;
+        const int at = step & 1;
+        if constexpr (i == 0) {
+            if (step + 1 < steps) {
+                v_rows = k_rows;
+                trim(v_off, step + 1);
+                if (step + 2 < steps) {
+                    k_rows = rows_at(step + 2, __builtin_amdgcn_readfirstlane(page));
+                    trim(k_off, step + 2);
                 }
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                __builtin_amdgcn_s_barrier();
+                page = load_page(step + 3);
             }
-        };
-        // what follows it: V of the next step and K of the one after are sent for, in 1 + 2 NF pieces
-        auto send = [&](auto ic) {
-            constexpr int i = decltype(ic)::value;
-            const int at = step & 1;
-            if constexpr (i == 0) {
-                if (step + 1 < steps) {
-                    v_rows = k_rows;
-                    trim(v_off, step + 1);
-                    if (step + 2 < steps) {
-                        k_rows = rows_at(step + 2, __builtin_amdgcn_readfirstlane(page));
-                        trim(k_off, step + 2);
-                    }
-                    page = load_page(step + 3);
-                }
-            } else if constexpr (i <= NF) {
-                if (step + 1 < steps) fetch16(v_off[i - 1], v_head + v_rows, my_rows + (3 - at) * SLOT + (i - 1) * 1024);
-            } else if constexpr (i <= 2 * NF) {
-                if (step + 2 < steps) fetch16(k_off[i - 1 - NF], k_head + k_rows, my_rows + at * SLOT + (i - 1 - NF) * 1024);
-            }
-        };
-        // Behind the last step there is nothing to score: what its second group multiplies beside its weights is not used.
-        if (my_steps > 0) {
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_k(ks, 0), q[ks], ks == 0 ? zero : s[0], 0, 0, 0);
-            static_for<4>([&](auto ic) { top_piece(ic, s[0]); });
-            do {
-                group(c0, second, second, begin + step * KT, [](auto) {});
-                turn();
-                turn_addresses(step & 1 ? -SLOT : SLOT);
-                group(c1, first, first, begin + step * KT + 32, send);
-            } while (++step < my_steps);
-#pragma unroll
-            for (int j = 0; j < KS; ++j) acc[j % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_v(j, 32 * PITCH), p[1][j / DT], acc[j % DT], 0, 0, 0);
-            if (pass == 0 && (my_steps & 1)) turn_addresses(-SLOT);      // as they were
+        } else if constexpr (i <= NF) {
+            if (step + 1 < steps) fetch16(v_off[i - 1], v_head + v_rows, my_rows + (3 - at) * SLOT + (i - 1) * 1024);
+        } else if constexpr (i <= 2 * NF) {
+            if (step + 2 < steps) fetch16(k_off[i - 1 - NF], k_head + k_rows, my_rows + at * SLOT + (i - 1 - NF) * 1024);
         }
-        for (; step < steps; ++step) {                       // for the other waves
+    };
+    // Behind the last step there is nothing to score: what its second group multiplies beside its weights is not used.
+    if (my_steps > 0) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_k(ks, 0), q[ks], ks == 0 ? zero : s[0], 0, 0, 0);
+        static_for<4>([&](auto ic) { top_piece(ic, s[0]); });
+        do {
+            group(c0, second, second, begin + step * KT, [](auto) {});
             turn();
-            static_for<1 + 2 * NF>([&](auto ic) { send(ic); });
-        }
-        if (pass == 1) break;
+            turn_addresses(step & 1 ? -SLOT : SLOT);
+            group(c1, first, first, begin + step * KT + 32, send);
+        } while (++step < my_steps);
+#pragma unroll
+        for (int j = 0; j < KS; ++j) acc[j % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_v(j, 32 * PITCH), p[1][j / DT], acc[j % DT], 0, 0, 0);
+    }
+    for (; step < steps; ++step) {                       // for the other waves
+        turn();
+        static_for<1 + 2 * NF>([&](auto ic) { send(ic); });
+    }
+    if constexpr (!ODD) {
         bool odd = false;
 #pragma unroll
         for (int t = 0; t < DT; ++t)
 #pragma unroll
             for (int r = 0; r < 16; ++r) odd |= (__float_as_uint(acc[t][r]) & 0x7F800000u) == 0x7F800000u;
         __syncthreads();
-        if (odd) any_odd = 1;
-        if (bad_page) any_bad = 1;                           // a page that is not there: any wave may have met it
+        if (odd) notes.odd = 1;
+        if (bad_page) notes.bad = 1;                         // any wave may have met it
         __syncthreads();
-        if (!any_odd) break;
+        if (notes.odd) return true;
     }
-    if (wave_col + c >= columns) return;
+    if (wave_col + c >= columns) return false;
     int my_col = wave_col + c;
     asm volatile("" : "+v"(my_col));                         // (row and head are worked out again: kept, they take registers the loop needs)
     const int row = row_of(my_col), head = head_of(my_col);
     const bool whole = a.n_chunks == 1;
     float total = l + __shfl_xor(l, 32, 64);
-    if (any_bad) total = __builtin_nanf("");
+    if (notes.bad) total = __builtin_nanf("");
     const float by = whole ? inverse_of(total, limit >= 0) : 1.f;       // (without weights acc is 0: what was not finite is out of it by now)
     const int64_t part = ((int64_t)chunk * a.b.n_rows + row) * a.n_q_heads + head;
 #pragma unroll
@@ -792,17 +797,19 @@ __device__ __forceinline__ void prompt_tile(const AttnArgs& a, int seq, int kvh,
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 o[u] = acc[t][4 * e + u] * by;
-                if (any_odd) o[u] += (first_odd[0][x + u] <= limit ? __builtin_inff() : 0.f) - (first_odd[1][x + u] <= limit ? __builtin_inff() : 0.f);
+                if (ODD) o[u] += (notes.first[0][x + u] <= limit ? __builtin_inff() : 0.f) - (notes.first[1][x + u] <= limit ? __builtin_inff() : 0.f);
             }
             if (whole) store4((uint16_t*)a.O + row * a.ldo + (int64_t)head * D + x, o);
             else *reinterpret_cast<f32x4_t*>(a.part_o + part * D + x) = o;
         }
     if (!whole && h == 0) { a.part_ml[2 * part] = total == 0.f ? -__builtin_inff() : base; a.part_ml[2 * part + 1] = total; }
+    return false;
 }
 
 template <int D>
 __global__ __launch_bounds__(64 * kPromptWaves, D < 256 ? 2 : 1)
 void attention_prompt_kernel(AttnArgs a) {
+    __shared__ PromptNotes<D> notes;
     int set, item;
     const int dealt = a.paired ? (a.col_tiles + 1) / 2 : a.col_tiles;
     if (!deal_to_dies(blockIdx.x, dealt * a.n_chunks, a.b.n_seqs * a.kv.n_kv_heads, &set, &item)) return;
@@ -810,7 +817,7 @@ void attention_prompt_kernel(AttnArgs a) {
     const int chunk = item % a.n_chunks;
     int tile = a.col_tiles - 1 - item / a.n_chunks;          // the columns that see most first
     for (;; tile = a.col_tiles - 1 - tile) {
-        prompt_tile<D>(a, seq, kvh, chunk, tile);
+        if (prompt_tile<D, false>(a, seq, kvh, chunk, tile, notes)) prompt_tile<D, true>(a, seq, kvh, chunk, tile, notes);
         if (!a.paired || 2 * tile < a.col_tiles) break;      // the middle one of an odd number has no partner
         __syncthreads();
     }
