@@ -491,12 +491,14 @@ __device__ __forceinline__ bool prompt_tile(const AttnArgs& a, int seq, int kvh,
     constexpr int ROWS = KT / kPromptWaves;                  // rows a wave fetches
     constexpr int NF = ROWS * PITCH / 1024;                  // fetches of 1 KB for them
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+    int thread = threadIdx.x;
+    asm volatile("" : "+v"(thread));                         // another tile's or pass's addresses are worked out again: kept, they take registers
     const NewRows rows = rows_of_sequence(a.b, seq);
     const int columns = rows.count * a.group, first_col = tile * WIDE;
     if (first_col >= columns) return false;
     const int kv_len = a.b.kv_len[seq], kv_end = min(kv_len, a.b.max_kv_len);
-    const int lane = threadIdx.x & 63, h = lane >> 5, c = lane & 31;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = thread & 63, h = lane >> 5, c = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(thread >> 6);
 
     auto limit_of = [&](int col) { return min(a.causal ? kv_len - rows.count + col / a.group : kv_len - 1, kv_end - 1); };
     const int wg_most = limit_of(min(first_col + WIDE, columns) - 1);
@@ -664,8 +666,8 @@ __device__ __forceinline__ bool prompt_tile(const AttnArgs& a, int seq, int kvh,
     constexpr std::integral_constant<int, 32 * PITCH> second{};
 
     if constexpr (ODD) {
-        for (int x = threadIdx.x; x < 2 * D; x += 64 * kPromptWaves) (&notes.first[0][0])[x] = 0x7FFFFFFF;
-    } else if (threadIdx.x == 0) {
+        for (int x = thread; x < 2 * D; x += 64 * kPromptWaves) (&notes.first[0][0])[x] = 0x7FFFFFFF;
+    } else if (thread == 0) {
         notes.odd = notes.bad = 0;
     }
     m = -__builtin_inff();
@@ -675,7 +677,7 @@ __device__ __forceinline__ bool prompt_tile(const AttnArgs& a, int seq, int kvh,
 #pragma unroll
     for (int e = 0; e < 8; ++e) p[1][0][e] = p[1][1][e] = (__bf16)0.f;
     // nothing comes before the first group: no weights, and zeros in the place of its values
-    for (int x = threadIdx.x * 16; x < 32 * PITCH; x += 64 * kPromptWaves * 16) *reinterpret_cast<u32x4_t*>(lds + 3 * SLOT + 32 * PITCH + x) = u32x4_t{0, 0, 0, 0};
+    for (int x = thread * 16; x < 32 * PITCH; x += 64 * kPromptWaves * 16) *reinterpret_cast<u32x4_t*>(lds + 3 * SLOT + 32 * PITCH + x) = u32x4_t{0, 0, 0, 0};
     int page = 0;                                        // in a lane's register: of the step three further on
     int64_t k_rows = 0, v_rows = 0;                      // where the rows of the next fetches begin
 #pragma unroll
@@ -711,7 +713,7 @@ __device__ __forceinline__ bool prompt_tile(const AttnArgs& a, int seq, int kvh,
         __builtin_amdgcn_s_barrier();
         if constexpr (ODD) {
             // the values that are not finite go, and per component the first key that had one is kept
-            for (int x = threadIdx.x * 16; x < SLOT; x += 64 * kPromptWaves * 16) {
+            for (int x = thread * 16; x < SLOT; x += 64 * kPromptWaves * 16) {
                 const int r = x / PITCH, d = 8 * v_pos<D>(r, (x - r * PITCH) / 16);
                 s16x8_t* where = reinterpret_cast<s16x8_t*>(lds + (2 + (step & 1)) * SLOT + x);
                 s16x8_t v = *where;
