@@ -6,8 +6,10 @@
 // one column, so maximum, sum and the rescaling stay in the lane, and the weights are at once the operand of O^T = V^T P^T: the matrix
 // instruction sums over keys in any order, as long as both operands agree on it.
 //
-// Scores, weights, maximum, sum and weighted sum are float.  Where the values are bfloat16 the weights, at most 1 (2^8.5 in the kernel for prompts), are rounded to it for the
-// second product (its other operand has no more bits); the sum they are divided by is that of the unrounded ones.
+// Scores, weights, maximum, sum and weighted sum are float.  Where the values are bfloat16 the weights, at most 1 (2^8.5 in the kernel for prompts),
+// are rounded to it for the second product, whose other operand has no more bits, and their sum is that of the rounded ones: a row that sees one key
+// is then that key's value, and rounding moves the others by no more than the values' distance from their mean (15 sequences of 1 to 3 keys, 48/2
+// heads of 64: 0.0019 of the result's norm off with the sum of the unrounded ones).
 //
 // attention_few_kernel: single tokens and a few rows, and all of float.  Bound by the cache's bytes: every one is read once by one wave, and a
 // CU has about 130 KB of them on their way.  K and V go from memory to registers with nothing between, as the matrix instructions want them (15
@@ -52,6 +54,12 @@ __device__ __forceinline__ float across_groups_max(float v) {
 __device__ __forceinline__ float across_groups_sum(float v) {
     v += __shfl_xor(v, 16, 64);
     return v + __shfl_xor(v, 32, 64);
+}
+
+// sum + the two bfloat16 of a word: their products with 1
+__device__ __forceinline__ float add_pair(uint32_t pair, float sum) {
+    typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, pair), bf16x2_t{(__bf16)1.f, (__bf16)1.f}, sum, false);
 }
 
 // PAST: cache rows are read past the caches (nobody reads them again soon)
@@ -130,8 +138,12 @@ struct Few<uint16_t, D, PAST> {
         if constexpr (TILES == 2) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, values), __builtin_bit_cast(bf16x8_t, weights), sum, 0, 0, 0);
         else return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4_t, values), __builtin_bit_cast(s16x4_t, weights), sum, 0, 0, 0);
     }
-    __device__ __forceinline__ void accumulate(f32x4_t (&acc)[VD], const float (&p)[SLOTS]) const {
-        const frag_t w = weights(p);
+    static __device__ __forceinline__ float sum_of(frag_t w, float sum) {
+#pragma unroll
+        for (int i = 0; i < 2 * TILES; ++i) sum = add_pair(w[i], sum);
+        return sum;
+    }
+    __device__ __forceinline__ void accumulate(f32x4_t (&acc)[VD], frag_t w) const {
 #pragma unroll
         for (int j = 0; j < VD; ++j) acc[j] = product(v_frag(j), w, acc[j]);
     }
@@ -145,8 +157,7 @@ struct Few<uint16_t, D, PAST> {
     }
     // as accumulate, where some keys are hidden from some columns (seen: bit per slot) and some values are not finite: 0 times those would be
     // NaN in columns that do not see them.  The finite part is summed as ever; how many +inf (-inf, NaN: both) a column sees is counted by two more products.
-    __device__ __forceinline__ void accumulate_odd(f32x4_t (&acc)[VD], const float (&p)[SLOTS], uint32_t seen) const {
-        const frag_t w = weights(p);
+    __device__ __forceinline__ void accumulate_odd(f32x4_t (&acc)[VD], frag_t w, uint32_t seen) const {
         float one[SLOTS];
 #pragma unroll
         for (int i = 0; i < SLOTS; ++i) one[i] = (seen >> i) & 1 ? 1.f : 0.f;
@@ -219,7 +230,14 @@ struct Few<float, D, PAST> {
             for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k[0][i][e], q[i][e], s, 0, 0, 0);
         return s;
     }
-    __device__ __forceinline__ void accumulate(f32x4_t (&acc)[VD], const float (&p)[4]) const {
+    typedef f32x4_t frag_t;
+    static __device__ __forceinline__ frag_t weights(const float (&p)[4]) { return f32x4_t{p[0], p[1], p[2], p[3]}; }
+    static __device__ __forceinline__ float sum_of(frag_t w, float sum) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sum += w[r];
+        return sum;
+    }
+    __device__ __forceinline__ void accumulate(f32x4_t (&acc)[VD], frag_t p) const {
 #pragma unroll
         for (int j = 0; j < VD; ++j)
 #pragma unroll
@@ -233,7 +251,7 @@ struct Few<float, D, PAST> {
             for (int j = 0; j < VD; ++j) odd |= (__float_as_uint(v[r][j]) & 0x7F800000u) == 0x7F800000u;
         return odd;
     }
-    __device__ __forceinline__ void accumulate_odd(f32x4_t (&acc)[VD], const float (&p)[4], uint32_t seen) const {
+    __device__ __forceinline__ void accumulate_odd(f32x4_t (&acc)[VD], frag_t p, uint32_t seen) const {
 #pragma unroll
         for (int j = 0; j < VD; ++j) {
             f32x4_t ups = {0.f, 0.f, 0.f, 0.f}, downs = ups;
@@ -345,20 +363,18 @@ __device__ __forceinline__ void walk_keys(const AttnArgs& a, int seq, int kvh, i
         const float m_safe = m_new == -__builtin_inff() ? 0.f : m_new;        // nothing seen yet: all weights are 0
         const float alpha = __builtin_amdgcn_exp2f(m - m_safe);
         m = m_new;
-        l *= alpha;
 #pragma unroll
-        for (int r = 0; r < SLOTS; ++r) {
-            s[r] = __builtin_amdgcn_exp2f(s[r] - m_safe);
-            l += s[r];
-        }
+        for (int r = 0; r < SLOTS; ++r) s[r] = __builtin_amdgcn_exp2f(s[r] - m_safe);
+        const typename F::frag_t w = F::weights(s);
+        l = F::sum_of(w, l * alpha);
         if (__ballot(alpha != 1.f)) {
 #pragma unroll
             for (int j = 0; j < VD; ++j)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) acc[j][r] *= alpha;
         }
-        if (partly && __ballot(f.odd_values())) f.accumulate_odd(acc, s, seen);
-        else f.accumulate(acc, s);
+        if (partly && __ballot(f.odd_values())) f.accumulate_odd(acc, w, seen);
+        else f.accumulate(acc, w);
         if (next <= last) load_v(next, page);
     }
 }
@@ -657,10 +673,17 @@ __device__ __forceinline__ bool prompt_tile(const AttnArgs& a, int seq, int kvh,
             static_for<(i + 1) * 16 / N - i * 16 / N>([&](auto rc) {
                 constexpr int r = i * 16 / N + decltype(rc)::value;
                 const float w = __builtin_amdgcn_exp2f(s[G][r] * a.scale2 - base);
-                part[r & 1] += w;
-                asm volatile("" : "+v"(part[r & 1]));        // here: extra() may hold branches, behind which it would sink to its use
                 s[G][r] = w;
-                if constexpr (r % 2 == 1) { p[G][r >> 3][(r & 7) - 1] = (__bf16)s[G][r - 1]; p[G][r >> 3][r & 7] = (__bf16)w; }
+                if constexpr (r % 2 == 0) {
+                    asm volatile("" : "+v"(s[G][r]));        // here: extra() may hold branches, behind which it would sink to its use
+                } else {
+                    typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+                    const bf16x2_t pair = {(__bf16)s[G][r - 1], (__bf16)w};
+                    p[G][r >> 3][(r & 7) - 1] = pair[0];
+                    p[G][r >> 3][r & 7] = pair[1];
+                    part[(r >> 1) & 1] = add_pair(__builtin_bit_cast(uint32_t, pair), part[(r >> 1) & 1]);
+                    asm volatile("" : "+v"(part[(r >> 1) & 1]));
+                }
             });
             // (the scores are there two instructions after the last of them)
             constexpr int j = i - KS - 2, SPAN = KS - 2;

@@ -240,13 +240,13 @@ def test_rows_that_have_no_place(ctx):
 def attention_bound(ref, absolute, Q, K, scale, kv, d, dtype):
     """A score is a sum of d products, scaled: (d + 6) U32 of |q| |k| scale, which the exponential makes a relative error of its weight; the sums
     over the keys err by a U32 per key and rescaling; all of it twice (weights and their sum) on sum w |v|.  bfloat16: every
-    weight rounded (U16 of sum w |v|), the result rounded once."""
+    weight rounded, in their sum too, which is U16 of sum w |v - O|, at most that of sum w |v| + |O|; the result rounded once."""
     q = np.linalg.norm(Q.reshape(-1, d), axis=1).max()
     k = np.linalg.norm(np.nan_to_num(K, nan=0.0, posinf=0.0, neginf=0.0).reshape(-1, d), axis=1).max()
     e = U32 * ((d + 6) * abs(scale) * q * k + kv + 64)
     bound = 2 * e * absolute
     if dtype == BF16:
-        bound = bound + 1.01 * U16 * (absolute + np.abs(ref))
+        bound = bound + 1.01 * U16 * (absolute + 2 * np.abs(ref))
     return bound + 1e-30
 
 
@@ -536,6 +536,22 @@ def test_a_row_that_sees_only_scores_of_minus_infinity_has_no_softmax(ctx, dtype
     for s, n in enumerate(kv):
         if n == 0:
             assert torch.all(O[int(row_start[s]):int(row_start[s + 1])] == 0)
+
+
+@pytest.mark.parametrize("d", [64, 96, 128, 256])
+@pytest.mark.parametrize("new,hq,hkv,want", [([1] * 5, 4, 2, 0), ([150] * 16, 16, 16, 1)])
+def test_a_row_that_sees_one_key_is_its_value(ctx, new, hq, hkv, want, d):
+    """Weight times value over weight, for every weight: the value's own bits, since the same rounded weight stands above and below."""
+    new = new[:8] if d == 256 else new                     # (at this width half as many workgroups fit, and more go in pairs)
+    batch, table, row_start, n_pages = make_batch(new, [1] * len(new), 16, 3)
+    K, V = make_cache(n_pages, hkv, 16, d, BF16, "head", seed=5)
+    Q = rand((int(row_start[-1]), hq * d), 8, BF16)
+    O = torch.full_like(Q, 7.0)
+    assert way(ctx, Q, new, [1] * len(new), hq, hkv, d, False) == want
+    g.gelo_attention(ctx, Q, O, hq, g.KvCache(K, V), batch, 1 / math.sqrt(d), causal=False)
+    heads = torch.arange(hq, device="cuda") * hkv // hq
+    for s in range(len(new)):
+        assert torch.equal(O[int(row_start[s]):int(row_start[s + 1])].view(-1, hq, d), V[int(table[s, 0]), heads, 0].expand(new[s], hq, d))
 
 
 def test_page_numbers_outside_the_cache_are_not_followed(ctx):
