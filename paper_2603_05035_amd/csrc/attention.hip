@@ -16,8 +16,7 @@
 // of 16 columns are idle where a key head has one query: the matrix pipes have that to spare); four waves of a workgroup walk different keys and join at
 // the end.  A single token of each of 64 sequences, 32 heads of 128, bfloat16: 3500 to 4095 rows 624 us (6.3 TB/s of those there are), 400 to 639 rows 92
 // (6.0), 3 sequences of 20000 to 32767 rows of 8 heads 64 and 4.3 for the join (5.8 without it).  Three sequences of up to 200 rows 7.7: trips to memory
-// one after another - lengths, page numbers, keys.  Float rows of prompts, 1 x 3000 behind 1000, 32/8 heads of 128: 1430 us = 86 of the 154 TFLOP/s
-// that a library's float product reaches.
+// one after another - lengths, page numbers, keys.
 #include "gelo_internal.h"
 #include "paged.h"
 
@@ -462,6 +461,148 @@ void attention_few_kernel(AttnArgs a) {
             if (x == 0) { a.part_ml[2 * item] = top; a.part_ml[2 * item + 1] = total; }
         }
     }
+}
+
+// attention_float_kernel: many columns to a key head, float.  Bound by the matrix instructions and the softmax between them.  A wave has a tile of 16 columns,
+// four of them share the keys and values that a workgroup brings into LDS, kFloatKeys at a time, a step ahead: through registers, since the rows' pitch
+// is 16 bytes more than they are long (16 lanes read the same piece of 16 rows).  8 x 512 rows, 32 heads of 128: 291 us, 478 with a workgroup to every 16
+// columns; 1 x 3000 behind 1000, 32/8 heads: 1133 us = 109 TFLOP/s, of the 154 that a library's product reaches, and 1434.  16 keys at a time 295 and 1163.
+constexpr int kFloatWaves = 4, kFloatKeys = 32;
+template <int D> constexpr int float_lds() { return 2 * 2 * kFloatKeys * (D + 4) * 4; }        // two steps of K and V
+
+template <int D>
+__global__ __launch_bounds__(64 * kFloatWaves, 2)
+void attention_float_kernel(AttnArgs a) {
+    typedef Few<float, D, false> F;
+    constexpr int VD = F::VD, KT = kFloatKeys, TILES = KT / 16, PITCH = D + 4, THREADS = 64 * kFloatWaves, VECS = KT * (D / 4) / THREADS;
+    static_assert(KT * (D / 4) % THREADS == 0, "");
+    extern __shared__ __attribute__((aligned(16))) float tiles[];
+    int set, item;
+    if (!deal_to_dies(blockIdx.x, a.col_tiles * a.n_chunks, a.b.n_seqs * a.kv.n_kv_heads, &set, &item)) return;
+    const int kvh = set % a.kv.n_kv_heads, seq = set / a.kv.n_kv_heads, chunk = item % a.n_chunks;
+    const int tile = a.col_tiles - 1 - item / a.n_chunks;    // the columns that see most first
+    const NewRows rows = rows_of_sequence(a.b, seq);
+    const int columns = rows.count * a.group, first_col = tile * 16 * kFloatWaves;
+    if (first_col >= columns) return;
+    const int kv_len = a.b.kv_len[seq], kv_end = min(kv_len, a.b.max_kv_len);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+    auto limit_of = [&](int col) { return min(a.causal ? kv_len - rows.count + col / a.group : kv_len - 1, kv_end - 1); };
+    const int begin = chunk * a.chunk, end = min(begin + a.chunk, limit_of(min(first_col + 16 * kFloatWaves, columns) - 1) + 1);
+    if (begin >= end && a.n_chunks > 1) return;              // the join does not look at it
+    const int last = end - 1, steps = end > begin ? (end - begin + KT - 1) / KT : 0;
+
+    const int wave_col = first_col + 16 * wave;
+    const bool awake = wave_col < columns;
+    const int col = min(wave_col + c, columns - 1), i = col / a.group, head = kvh * a.group + col - i * a.group;     // dead columns repeat the last one
+    const int64_t row = rows.first + i;
+    const int limit = limit_of(col);
+    const int most = awake ? min(__builtin_amdgcn_readlane(limit, 15), last) : -1, least = __builtin_amdgcn_readfirstlane(limit);
+    F f;
+    f.load_q((const float*)a.Q + row * a.ldq + (int64_t)head * D, g);
+    f32x4_t acc[VD];
+#pragma unroll
+    for (int j = 0; j < VD; ++j) acc[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    float m = -__builtin_inff(), l = 0.f;
+    bool bad_page = false;
+
+    // this thread's pieces of a step: rows beyond the last key are read as that one
+    const int shift = a.kv.page_shift, in_page = (1 << shift) - 1;
+    const int32_t* table = a.b.page_table + seq * a.b.table_ld;
+    f32x4_t stage[2][VECS];
+    auto send = [&](int step) {
+#pragma unroll
+        for (int u = 0; u < VECS; ++u) {
+            const int e = threadIdx.x + u * THREADS, r = e / (D / 4), x = 4 * (e - r * (D / 4));
+            const int key = min(begin + step * KT + r, last);
+            const int page = table[key >> shift];
+            const bool good = page >= 0 && page < a.kv.n_pages;
+            bad_page |= !good;
+            const int64_t at = (good ? page : 0) * a.kv.page_stride + kvh * a.kv.head_stride + (key & in_page) * a.kv.row_stride + x;
+            stage[0][u] = *reinterpret_cast<const f32x4_t*>((const float*)a.kv.k + at);
+            stage[1][u] = *reinterpret_cast<const f32x4_t*>((const float*)a.kv.v + at);
+        }
+    };
+    auto put = [&](int step) {
+        float* to = tiles + (step & 1) * 2 * KT * PITCH;
+#pragma unroll
+        for (int u = 0; u < VECS; ++u) {
+            const int e = threadIdx.x + u * THREADS, r = e / (D / 4), x = 4 * (e - r * (D / 4));
+            *reinterpret_cast<f32x4_t*>(to + r * PITCH + x) = stage[0][u];
+            *reinterpret_cast<f32x4_t*>(to + KT * PITCH + r * PITCH + x) = stage[1][u];
+        }
+    };
+    if (steps > 0) { send(0); put(0); }
+    __syncthreads();
+    for (int step = 0; step < steps; ++step) {
+        if (step + 1 < steps) send(step + 1);
+        const float* from = tiles + (step & 1) * 2 * KT * PITCH;
+        const int key = begin + step * KT;
+        if (key <= most) {
+            float s[4 * TILES];
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+                f.load_k(0, from + (16 * t + c) * PITCH, g);
+                const f32x4_t x = f.scores(0);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[4 * t + r] = x[r] * a.scale2s;
+            }
+            const bool partly = key + KT - 1 > min(least, last);
+            uint32_t seen = ~0u;
+            if (partly) {
+                int upto = min(limit, last);
+                asm volatile("" : "+v"(upto));               // a branch: as selects it would cost every step
+                seen = 0;
+#pragma unroll
+                for (int t = 0; t < TILES; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const bool sees = key + 16 * t + 4 * g + r <= upto;
+                        s[4 * t + r] = sees ? s[4 * t + r] : -__builtin_inff();
+                        seen |= (uint32_t)sees << (4 * t + r);
+                    }
+            }
+            float top = s[0];
+#pragma unroll
+            for (int r = 1; r < 4 * TILES; ++r) top = fmaxf(top, s[r]);
+            const float m_new = fmaxf(m, across_groups_max(top)), m_safe = m_new == -__builtin_inff() ? 0.f : m_new;
+            const float alpha = __builtin_amdgcn_exp2f(m - m_safe);
+            m = m_new;
+            l *= alpha;
+            if (__ballot(alpha != 1.f)) {
+#pragma unroll
+                for (int j = 0; j < VD; ++j)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[j][r] *= alpha;
+            }
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+#pragma unroll
+                for (int u = 0; u < 4; ++u) f.load_v(0, u, from + (KT + 16 * t + 4 * g + u) * PITCH, c);
+                f32x4_t w;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) w[r] = __builtin_amdgcn_exp2f(s[4 * t + r] - m_safe);
+                l = F::sum_of(w, l);
+                if (partly && __ballot(f.odd_values())) f.accumulate_odd(acc, w, seen >> (4 * t));
+                else f.accumulate(acc, w);
+            }
+        }
+        if (step + 1 < steps) put(step + 1);                 // into the half that nobody has read since the last barrier
+        __syncthreads();
+    }
+    const bool any_bad = __syncthreads_or(bad_page);
+    float total = across_groups_sum(l);
+    if (any_bad) total = __builtin_nanf("");
+    if (wave_col + c >= columns) return;
+    const bool whole = a.n_chunks == 1;
+    const float by = whole ? inverse_of(total, limit >= 0) : 1.f;
+    const int64_t part = ((int64_t)chunk * a.b.n_rows + row) * a.n_q_heads + head;
+    float* out = whole ? (float*)a.O + row * a.ldo + (int64_t)head * D : a.part_o + part * D;
+    // acc[j][r]: component VD (4 g + r) + j
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int j = 0; j < VD; j += 2) *reinterpret_cast<f32x2_t*>(out + VD * (4 * g + r) + j) = f32x2_t{acc[j][r] * by, acc[j + 1][r] * by};
+    if (!whole && g == 0) { a.part_ml[2 * part] = m; a.part_ml[2 * part + 1] = total; }
 }
 
 // attention_prompt_kernel: many columns to a key head, bfloat16.  Bound by the matrix instructions and, beside them, by the exponentials.  A
@@ -957,7 +1098,7 @@ hipError_t join(const AttnArgs& a, hipStream_t stream) {
 }
 
 // Which kernel, and how the cache is cut: chunks of `chunk` keys, n_chunks of them to the longest sequence.
-struct Plan { bool prompt, paired, past, by_head; int col_tiles, chunk, n_chunks; int64_t workgroups; };
+struct Plan { bool prompt, shared, paired, past, by_head; int col_tiles, chunk, n_chunks; int64_t workgroups; };
 constexpr int64_t kMostWorkgroups = 1 << 23;     // of a launch: 2^31 threads and no more fit HIP's 32-bit counts
 constexpr int kCus = 256;
 constexpr int kFewTarget = 512, kFewLeast = 256;         // workgroups that fill the chip (two to a CU), keys to a chunk at least
@@ -975,7 +1116,7 @@ double join_us(const Attention& o, const Plan& p) {
 
 Plan plan_few(const Attention& o, int64_t columns, int bytes, double* us) {
     Plan p;
-    p.prompt = p.paired = p.past = p.by_head = false;
+    p.prompt = p.shared = p.paired = p.past = p.by_head = false;
     p.col_tiles = (int)((columns + 15) / 16);
     const int64_t tiles = (int64_t)o.batch.n_seqs * o.cache.n_kv_heads * p.col_tiles;
     const int64_t most = (o.batch.max_kv_len + kFewLeast - 1) / kFewLeast;
@@ -1005,7 +1146,7 @@ Plan plan_few(const Attention& o, int64_t columns, int bytes, double* us) {
 Plan plan_prompt(const Attention& o, int64_t columns, double* us) {
     Plan best;
     best.prompt = true;
-    best.past = best.by_head = false;
+    best.shared = best.past = best.by_head = false;
     best.col_tiles = (int)((columns + 32 * kPromptWaves - 1) / (32 * kPromptWaves));
     const int64_t sets = (int64_t)o.batch.n_seqs * o.cache.n_kv_heads, tiles = sets * best.col_tiles;
     const int d = o.cache.head_dim, per_cu = d == 256 ? 1 : 2;
@@ -1034,11 +1175,35 @@ Plan plan_prompt(const Attention& o, int64_t columns, double* us) {
     return best;
 }
 
+// Float: tiles of 64 columns pay where they fill the chip, or where they are long ones (every row sees half of the keys at least) and it takes a cut or two.
+// 16 columns to a workgroup and 64, us: heads of 128, 8 x 512 rows 478 and 291 (2048 tiles), 64 x 48 on 200 61 and 50 (512), 16 x 24 on 500, 32/8 heads, 72
+// and 55 (256), 4 x 200 on 1000, all seen, 109 and 93 (256), 2 x 512 on 2000 99 and 93 (128); 1 x 2000 148 and 162 (256), 32 x 64 on 300 56 and 61
+// (256), 1 x 32 on 4096 20 and 33; of 96, 16 x 33 on 1000, 28/4 heads, 92 and 76 (256), 4 x 378 24 and 43 (192).  Of 64, where four of the small ones fit a CU, 8 x
+// 200 37 and 41, of 256, where one of either does, 8 x 300 on 600 386 and 440: never.
+bool float_shares(const Attention& o, int64_t columns) {
+    const int64_t tiles = (int64_t)o.batch.n_seqs * o.cache.n_kv_heads * ((columns + 16 * kFloatWaves - 1) / (16 * kFloatWaves));
+    const bool lengthy = !o.causal || o.batch.max_kv_len >= 2 * (int64_t)o.batch.max_rows;
+    return (o.cache.head_dim == 96 || o.cache.head_dim == 128) && ((columns >= 48 && tiles >= 512) || (columns >= 96 && tiles >= 128 && lengthy));
+}
+Plan plan_float(const Attention& o, int64_t columns) {
+    Plan p;
+    p.shared = true;
+    p.prompt = p.paired = p.past = p.by_head = false;
+    p.col_tiles = (int)((columns + 16 * kFloatWaves - 1) / (16 * kFloatWaves));
+    const int64_t sets = (int64_t)o.batch.n_seqs * o.cache.n_kv_heads, tiles = sets * p.col_tiles;
+    const int64_t most = (o.batch.max_kv_len + kFewLeast - 1) / kFewLeast, cuts = kFewTarget / tiles;
+    cut(&p, o.batch.max_kv_len, cuts < 1 ? 1 : cuts < most ? cuts : most);
+    p.workgroups = tiles * p.n_chunks;
+    if (p.workgroups <= kMostWorkgroups) p.workgroups = 8 * (int64_t)dies_slots(p.col_tiles * p.n_chunks, (int)sets);
+    return p;
+}
+
 Plan plan_of(const Attention& o, int is_bf16) {
     const int64_t columns = (int64_t)o.batch.max_rows * (o.n_q_heads / o.cache.n_kv_heads);
     double few_us, prompt_us;
     const Plan few = plan_few(o, columns, is_bf16 ? 2 : 4, &few_us);
-    if (!is_bf16 || columns <= 16) return few;
+    if (!is_bf16) return float_shares(o, columns) ? plan_float(o, columns) : few;
+    if (columns <= 16) return few;
     const Plan prompt = plan_prompt(o, columns, &prompt_us);
     return few_us < prompt_us ? few : prompt;
 }
@@ -1066,9 +1231,13 @@ hipError_t launch(const Attention& o, hipStream_t stream) {
         if (p.prompt)
             hipLaunchKernelGGL((attention_prompt_kernel<D>), dim3((unsigned)p.workgroups), dim3(64 * kPromptWaves), (size_t)prompt_lds<D>(), stream, a);
     }
+    if constexpr (sizeof(T) == 4 && (D == 96 || D == 128)) {
+        if (p.shared) hipLaunchKernelGGL((attention_float_kernel<D>), dim3((unsigned)p.workgroups), dim3(64 * kFloatWaves), (size_t)float_lds<D>(), stream, a);
+    }
+    const bool direct = !p.prompt && !p.shared;
     const dim3 few((unsigned)(p.col_tiles * p.n_chunks), (unsigned)(o.cache.n_kv_heads / (p.by_head ? kFewWaves : 1)), (unsigned)o.batch.n_seqs);
-    if (!p.prompt && p.past) hipLaunchKernelGGL((attention_few_kernel<T, D, true>), few, dim3(64 * kFewWaves), 0, stream, a);
-    else if (!p.prompt) hipLaunchKernelGGL((attention_few_kernel<T, D, false>), few, dim3(64 * kFewWaves), 0, stream, a);
+    if (direct && p.past) hipLaunchKernelGGL((attention_few_kernel<T, D, true>), few, dim3(64 * kFewWaves), 0, stream, a);
+    else if (direct) hipLaunchKernelGGL((attention_few_kernel<T, D, false>), few, dim3(64 * kFewWaves), 0, stream, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.n_chunks == 1) return e;
     if (p.n_chunks <= 4) return join<T, D, 1>(a, stream);
@@ -1098,6 +1267,16 @@ int attention_way(int is_bf16, int causal, int n_q_heads, int n_kv_heads, int he
     return (p.prompt ? p.paired ? 2 : 1 : 0) + (p.n_chunks > 1 ? 4 : 0);
 }
 
+// Whether a float call goes by tiles of 64 columns: 1, with a cut cache 5.
+int attention_float_way(int causal, int n_q_heads, int n_kv_heads, int head_dim, int n_seqs, int n_rows, int max_rows, int max_kv_len) {
+    Attention o = {};
+    o.causal = causal != 0; o.n_q_heads = n_q_heads;
+    o.cache.n_kv_heads = n_kv_heads; o.cache.head_dim = head_dim;
+    o.batch.n_seqs = n_seqs; o.batch.n_rows = n_rows; o.batch.max_rows = max_rows; o.batch.max_kv_len = max_kv_len;
+    const Plan p = plan_of(o, 0);
+    return (p.shared ? 1 : 0) + (p.n_chunks > 1 ? 4 : 0);
+}
+
 bool attention_fits(const Attention& o, int is_bf16) {
     if (o.batch.n_seqs > 65535 || o.cache.n_kv_heads > 65535) return false;          // dimensions of a launch
     return plan_of(o, is_bf16).workgroups <= kMostWorkgroups && (int64_t)o.batch.n_rows * o.n_q_heads <= kMostWorkgroups;
@@ -1116,9 +1295,10 @@ hipError_t attention(const Attention& o, int is_bf16, hipStream_t stream) {
 
 hipError_t attention_init() {
     const void* kernels[] = {(const void*)&attention_prompt_kernel<64>, (const void*)&attention_prompt_kernel<96>,
-                             (const void*)&attention_prompt_kernel<128>, (const void*)&attention_prompt_kernel<256>};
-    const int bytes[] = {prompt_lds<64>(), prompt_lds<96>(), prompt_lds<128>(), prompt_lds<256>()};
-    for (int i = 0; i < 4; ++i) {
+                             (const void*)&attention_prompt_kernel<128>, (const void*)&attention_prompt_kernel<256>,
+                             (const void*)&attention_float_kernel<96>, (const void*)&attention_float_kernel<128>};
+    const int bytes[] = {prompt_lds<64>(), prompt_lds<96>(), prompt_lds<128>(), prompt_lds<256>(), float_lds<96>(), float_lds<128>()};
+    for (int i = 0; i < 6; ++i) {
         const hipError_t e = hipFuncSetAttribute(kernels[i], hipFuncAttributeMaxDynamicSharedMemorySize, bytes[i]);
         if (e != hipSuccess) return e;
     }

@@ -417,6 +417,7 @@ struct Attention {
 };
 // float workspace for the parts of a cache that is cut over workgroups: what this call needs, and the most any call of this head width needs
 int attention_way(int is_bf16, int causal, int n_q_heads, int n_kv_heads, int head_dim, int n_seqs, int n_rows, int max_rows, int max_kv_len);
+int attention_float_way(int causal, int n_q_heads, int n_kv_heads, int head_dim, int n_seqs, int n_rows, int max_rows, int max_kv_len);
 bool attention_fits(const Attention& o, int is_bf16);       // as one launch
 size_t attention_workspace_bytes(const Attention& o, int is_bf16);
 size_t attention_workspace_bound(int head_dim);

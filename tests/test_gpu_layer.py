@@ -554,6 +554,81 @@ def test_a_row_that_sees_one_key_is_its_value(ctx, new, hq, hkv, want, d):
         assert torch.equal(O[int(row_start[s]):int(row_start[s + 1])].view(-1, hq, d), V[int(table[s, 0]), heads, 0].expand(new[s], hq, d))
 
 
+def float_way(new, kv, hq, hkv, d, causal):
+    """1: float by tiles of 64 columns, 5: with a cut cache."""
+    return ctypes.CDLL(g.LIB_PATH)["_ZN4gelo19attention_float_wayEiiiiiiii"](int(causal), hq, hkv, d, len(kv), sum(new), max(new), max(kv))
+
+
+FLOAT_TILES = [  # new, kv, q heads, kv heads, d, page, order, causal, scale, way
+    ([x[0] for x in EDGES], [x[1] for x in EDGES], 16, 16, 96, 16, "row", True, None, 1),
+    ([x[0] for x in EDGES], [x[1] for x in EDGES], 32, 16, 128, 32, "head", False, None, 1),
+    ([200, 1, 64, 65], [1000, 1, 513, 0], 16, 16, 128, 64, "head", False, None, 5),
+    ([65, 17], [700, 300], 64, 8, 96, 16, "row", True, None, 5),
+    ([60] * 34, [60 + i for i in range(34)], 16, 16, 128, 16, "head", True, -0.2, 1),
+    ([60] * 34, [60 + i for i in range(34)], 16, 16, 96, 16, "head", True, 0.0, 1),
+]
+
+
+@pytest.mark.parametrize("new,kv,hq,hkv,d,page,order,causal,scale,want", FLOAT_TILES)
+def test_float_by_tiles_of_64_columns(ctx, new, kv, hq, hkv, d, page, order, causal, scale, want):
+    """Edges of tiles and steps, cut caches, rows of the cache that belong to nobody hold NaN; all rows of three heads."""
+    batch, table, row_start, n_pages = make_batch(new, kv, page, 3)
+    K, V = make_cache(n_pages, hkv, page, d, F32, order, seed=5)
+    hidden = torch.ones((n_pages, page), dtype=torch.bool)
+    for s, n in enumerate(kv):
+        for p in range(n):
+            hidden[table[s, p // page], p % page] = False
+    K.masked_fill_(hidden.cuda()[:, None, :, None], float("nan"))
+    V.masked_fill_(hidden.cuda()[:, None, :, None], float("nan"))
+    Q = rand((int(row_start[-1]), hq * d), 8, F32)
+    O = torch.full_like(Q, 7.0)
+    scale = 1 / math.sqrt(d) if scale is None else scale
+    assert float_way(new, kv, hq, hkv, d, causal) == want
+    g.gelo_attention(ctx, Q, O, hq, g.KvCache(K, V), batch, scale, causal=causal)
+    for h in (0, hq // 2 + 1, hq - 1):
+        kh = h * hkv // hq
+        ref, absolute = lo.attention(host(Q[:, h * d:(h + 1) * d]), host(K[:, kh:kh + 1]), host(V[:, kh:kh + 1]), 1, row_start, kv, table, scale, causal)
+        within(O[:, h * d:(h + 1) * d], ref, attention_bound(ref, absolute, host(Q), host(K), scale, max(kv), d, F32), h)
+
+
+@pytest.mark.parametrize("d", [96, 128])
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+def test_float_by_tiles_of_64_columns_and_values_that_are_not_finite(ctx, d, value):
+    """One component of one value in every sequence and head, a key that is NaN, a page number outside the cache: as for bfloat16."""
+    n_seqs, hq, rows, page, at = 16, 16, 150, 16, 75
+    each = (rows + page - 1) // page
+    K, V = make_cache(n_seqs * each, hq, page, d, F32, "head", seed=3)
+    table = torch.arange(n_seqs * each, dtype=torch.int32, device="cuda").view(n_seqs, each)
+    pages = table[:, at // page].long()
+    K[pages, :, at % page] = 0
+    odd = V.clone()
+    odd[pages, :, at % page, 5] = value
+    V[pages, :, at % page, 5] = 0
+    row_start = (torch.arange(n_seqs + 1, device="cuda") * rows).int()
+    kv_len = torch.full((n_seqs,), rows, dtype=torch.int32).cuda()
+    batch = g.SeqBatch(kv_len, table, rows, row_start=row_start, max_rows=rows)
+    assert float_way([rows] * n_seqs, [rows] * n_seqs, hq, hq, d, True) == 1
+    Q = rand((n_seqs * rows, hq * d), 9, F32)
+    want, O = torch.empty_like(Q), torch.empty_like(Q)
+    g.gelo_attention(ctx, Q, want, hq, g.KvCache(K, V), batch, 1 / math.sqrt(d))
+    g.gelo_attention(ctx, Q, O, hq, g.KvCache(K, odd), batch, 1 / math.sqrt(d))
+    o, w = (x.view(n_seqs, rows, hq, d) for x in (O, want))
+    assert torch.isfinite(w).all()
+    other = torch.arange(d, device="cuda") != 5
+    assert torch.equal(o[..., other], w[..., other]) and torch.equal(o[:, :at], w[:, :at])
+    seen = o[:, at:, :, 5]
+    assert torch.isnan(seen).all() if math.isnan(value) else torch.all(seen == value)
+    K[pages, :, at % page, 0] = float("nan")
+    g.gelo_attention(ctx, Q, O, hq, g.KvCache(K, V), batch, 1 / math.sqrt(d))
+    assert torch.equal(o[:, :at], w[:, :at]) and torch.isnan(o[:, at:]).all()
+    K[pages, :, at % page, 0] = 0
+    bad = table.clone()
+    bad[3, 1] = n_seqs * each
+    g.gelo_attention(ctx, Q, O, hq, g.KvCache(K, V), g.SeqBatch(kv_len, bad, rows, row_start=row_start, max_rows=rows), 1 / math.sqrt(d))
+    good = torch.arange(n_seqs, device="cuda") != 3
+    assert torch.equal(o[good], w[good]) and torch.isnan(o[3, 64:]).all()
+
+
 def test_page_numbers_outside_the_cache_are_not_followed(ctx):
     K, V = make_cache(4, 2, 16, 64, BF16, "head", seed=3)
     table = torch.tensor([[0, 1 << 29], [2, 3], [-5, 1]], dtype=torch.int32, device="cuda")
