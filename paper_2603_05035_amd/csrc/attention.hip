@@ -11,7 +11,7 @@
 // is then that key's value, and rounding moves the others by no more than the values' distance from their mean (15 sequences of 1 to 3 keys, 48/2
 // heads of 64: 0.0019 of the result's norm off with the sum of the unrounded ones).
 //
-// attention_few_kernel: single tokens and a few rows, and all of float.  Bound by the cache's bytes: every one is read once by one wave, and a
+// attention_few_kernel: single tokens and a few rows, and float where its prompts do not fill the chip.  Bound by the cache's bytes: every one is read once by one wave, and a
 // CU has about 130 KB of them on their way.  K and V go from memory to registers with nothing between, as the matrix instructions want them (15
 // of 16 columns are idle where a key head has one query: the matrix pipes have that to spare); four waves of a workgroup walk different keys and join at
 // the end.  A single token of each of 64 sequences, 32 heads of 128, bfloat16: 3500 to 4095 rows 624 us (6.3 TB/s of those there are), 400 to 639 rows 92
