@@ -378,9 +378,7 @@ class SeqBatch:
             _vector(row_start, "row_start", torch.int32, n_seqs + 1)
         if page_table.dtype != torch.int32 or page_table.dim() != 2 or page_table.shape[0] != n_seqs:
             raise ValueError("page_table must be an int32 tensor with a row per sequence")
-        tp, table_ld = _matrix(page_table, "page_table")
-        if n_seqs == 1 or table_ld < page_table.shape[1]:
-            table_ld = page_table.shape[1]
+        tp, table_ld = _matrix(page_table, "page_table")     # (rows closer than max_kv_len takes, an expanded table's too, are refused by the library)
         self.kv_len, self.page_table, self.row_start = kv_len, page_table, row_start
         self.n_seqs, self.n_rows, self.pages, self.max_kv_len = n_seqs, n_seqs, page_table.shape[1], max_kv_len
         self.struct = _SeqBatchStruct(n_seqs, n_seqs, max_rows, max_kv_len, None if row_start is None else row_start.data_ptr(), kv_len.data_ptr(), tp, table_ld)
