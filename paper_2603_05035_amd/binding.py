@@ -320,14 +320,20 @@ def gelo_prepare_weight_fp8(ctx, W: torch.Tensor, stream=None) -> torch.Tensor:
     return Wq
 
 
+def _prepared(Wq: torch.Tensor, d: int, p: int):
+    if Wq.dtype != torch.uint8 or Wq.numel() != gelo_fp8_weight_bytes(d, p):
+        raise GeloError(2, "Wq is not the prepared form of a d x p weight")
+    if not Wq.is_cuda or not Wq.is_contiguous():
+        raise ValueError("Wq must be a contiguous GPU tensor")
+
+
 def gelo_project_fp8(ctx, U: torch.Tensor, Wq: torch.Tensor, p: int, Y: torch.Tensor, stream=None) -> torch.Tensor:
     up, ldu = _matrix(U, "U")
     yp, ldy = _matrix(Y, "Y")
     n, d = U.shape
     if U.dtype != torch.bfloat16 or Y.dtype != torch.bfloat16 or tuple(Y.shape) != (n, p):
         raise ValueError("U and Y must be bf16, Y n x p")
-    if Wq.dtype != torch.uint8 or Wq.numel() != gelo_fp8_weight_bytes(d, p):
-        raise GeloError(2, "Wq is not the prepared form of a d x p weight")
+    _prepared(Wq, d, p)
     _check(ctx, load_library().gelo_project_fp8(ctx, n, d, p, up, ldu, c_void_p(Wq.data_ptr()), yp, ldy, _stream(stream)))
     return Y
 
@@ -340,8 +346,7 @@ def gelo_project_fp8_codes(ctx, codes: torch.Tensor, scales: torch.Tensor, Wq: t
     if codes.dtype != torch.uint8 or Y.dtype != torch.bfloat16 or tuple(Y.shape) != (n, p):
         raise ValueError("codes must be uint8, Y bf16 and n x p")
     _vector(scales, "scales", torch.float32, n)
-    if Wq.dtype != torch.uint8 or Wq.numel() != gelo_fp8_weight_bytes(d, p):
-        raise GeloError(2, "Wq is not the prepared form of a d x p weight")
+    _prepared(Wq, d, p)
     _check(ctx, load_library().gelo_project_fp8_codes(ctx, n, d, p, cp, ldq, scales.data_ptr(), Wq.data_ptr(), yp, ldy, _stream(stream)))
     return Y
 
