@@ -394,7 +394,7 @@ void attention_few_kernel(AttnArgs a) {
     const NewRows rows = rows_of_sequence(a.b, seq);
     const int columns = rows.count * a.group;
     if (tile * 16 >= columns) return;
-    const int kv_len = a.b.kv_len[seq], kv_end = min(kv_len, a.b.max_kv_len);
+    const int kv_len = length_of_sequence(a.b, seq), kv_end = min(kv_len, a.b.max_kv_len);
 
     const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
     const int col = tile * 16 + c;
@@ -484,7 +484,7 @@ void attention_float_kernel(AttnArgs a) {
     const NewRows rows = rows_of_sequence(a.b, seq);
     const int columns = rows.count * a.group, first_col = tile * 16 * kFloatWaves;
     if (first_col >= columns) return;
-    const int kv_len = a.b.kv_len[seq], kv_end = min(kv_len, a.b.max_kv_len);
+    const int kv_len = length_of_sequence(a.b, seq), kv_end = min(kv_len, a.b.max_kv_len);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
     auto limit_of = [&](int col) { return min(a.causal ? kv_len - rows.count + col / a.group : kv_len - 1, kv_end - 1); };
     const int begin = chunk * a.chunk, end = min(begin + a.chunk, limit_of(min(first_col + 16 * kFloatWaves, columns) - 1) + 1);
@@ -664,7 +664,7 @@ __device__ __forceinline__ bool prompt_tile(const AttnArgs& a, int seq, int kvh,
     const NewRows rows = rows_of_sequence(a.b, seq);
     const int columns = rows.count * a.group, first_col = tile * WIDE;
     if (first_col >= columns) return false;
-    const int kv_len = a.b.kv_len[seq], kv_end = min(kv_len, a.b.max_kv_len);
+    const int kv_len = length_of_sequence(a.b, seq), kv_end = min(kv_len, a.b.max_kv_len);
     const int lane = thread & 63, h = lane >> 5, c = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(thread >> 6);
 
@@ -1033,7 +1033,7 @@ void attention_join_kernel(AttnArgs a) {
             }
         }
         if (there) {
-            const int kv_len = a.b.kv_len[seq], kv_end = min(kv_len, a.b.max_kv_len);
+            const int kv_len = length_of_sequence(a.b, seq), kv_end = min(kv_len, a.b.max_kv_len);
             const int limit = min(a.causal ? kv_len - count + i : kv_len - 1, kv_end - 1);
             used = limit < 0 ? 0 : limit / a.chunk + 1;
         }

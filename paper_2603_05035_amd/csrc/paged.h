@@ -23,8 +23,11 @@ __device__ __forceinline__ int sequence_of_row(const int32_t* __restrict__ row_s
 struct NewRows { int first, count; };
 __device__ __forceinline__ NewRows rows_of_sequence(const SeqBatch& b, int s) {
     if (!b.row_start) return NewRows{s, 1};
-    const int first = max(b.row_start[s], 0), end = min(b.row_start[s + 1], b.n_rows);
+    const int first = max(b.row_start[s], 0), end = max(min(b.row_start[s + 1], b.n_rows), 0);        // (a difference of two such fits in 32 bits)
     return NewRows{first, min(max(end - first, 0), b.max_rows)};
 }
+
+// kv_len of a sequence.  Below zero means as little as zero does, but positions reckoned from it could leave 32 bits and come out beyond the cache.
+__device__ __forceinline__ int length_of_sequence(const SeqBatch& b, int s) { return max(b.kv_len[s], 0); }
 
 }  // namespace gelo

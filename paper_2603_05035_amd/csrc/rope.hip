@@ -77,7 +77,7 @@ void rope_append_kernel(RopeAppend o) {
         j = row - b.row_start[seq];
         count = b.row_start[seq + 1] - b.row_start[seq];
     }
-    const int pos = b.kv_len[seq] - count + j;
+    const int pos = length_of_sequence(b, seq) - count + j;
     const bool beyond = pos >= b.max_kv_len, placed = pos >= 0 && !beyond;
     const int page = placed ? b.page_table[seq * b.table_ld + (pos >> kv.page_shift)] : -1;
     const bool kept = page >= 0 && page < kv.n_pages;

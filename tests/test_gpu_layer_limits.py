@@ -1,0 +1,65 @@
+"""The operators between two projections at the limits of what their arguments may hold, through the C ABI."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import test_gpu_layer as base
+from oracle import layer_oracle as lo
+from paper_2603_05035_amd import binding as g
+from test_gpu_layer import BF16, F32, attention_bound, float_way, host, make_batch, make_cache, rand, way, within
+
+pytestmark = pytest.mark.gpu
+
+INT_MIN, INT_MAX = -2 ** 31, 2 ** 31 - 1
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = g.gelo_create(0, 1)
+    yield c
+    g.gelo_destroy(c)
+
+
+def int32(*values):
+    return torch.tensor(values, dtype=torch.int32).cuda()
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,d,many", [(BF16, 2, 2, 64, 0), (BF16, 128, 1, 128, 1), (F32, 2, 2, 96, 0), (F32, 64, 1, 128, 1)])
+def test_lengths_and_row_starts_at_the_ends_of_32_bits(ctx, dtype, hq, hkv, d, many):
+    """A length below zero is one of zero.  Row starts that do not ascend bring no rows."""
+    page, n_seqs, rows = 16, 16, 8
+    K, V = make_cache(2 * n_seqs, hkv, page, d, dtype, "head", seed=3)
+    table = torch.arange(2 * n_seqs, dtype=torch.int32, device="cuda").view(n_seqs, 2)
+    kv = int32(INT_MIN, 20, INT_MIN + 1, 32, -1, 9, INT_MIN + rows, 1, *[12] * 8)
+    zero = kv.clamp(min=0)
+    for causal in (True, False):
+        Q = rand((n_seqs * rows, hq * d), 9, dtype)
+        news, lens = [rows] * n_seqs, [32] * n_seqs
+        assert (way(ctx, Q, news, lens, hq, hkv, d, causal) if dtype == BF16 else float_way(news, lens, hq, hkv, d, causal)) == many
+        starts = torch.arange(n_seqs + 1, dtype=torch.int32, device="cuda") * rows
+        O, want = torch.full_like(Q, 7.0), torch.full_like(Q, 7.0)
+        for lens, out in ((kv, O), (zero, want)):
+            g.gelo_attention(ctx, Q, out, hq, g.KvCache(K, V), g.SeqBatch(lens, table, 32, row_start=starts, max_rows=rows), d ** -0.5, causal=causal)
+        assert torch.equal(O, want) and torch.all(O.view(n_seqs, -1)[[0, 2, 4, 6]] == 0) and torch.isfinite(O.float()).all()
+        # sequence 2 begins at the largest number and ends at the smallest
+        starts = int32(0, 2, INT_MAX, INT_MIN, *[0] * (n_seqs - 3))
+        plain = int32(0, 2, 2 + rows, *[2 + rows] * (n_seqs - 2))
+        lens = torch.full_like(kv, 30)
+        O, want = torch.full_like(Q, 7.0), torch.full_like(Q, 7.0)
+        for at, out in ((starts, O), (plain, want)):
+            g.gelo_attention(ctx, Q, out, hq, g.KvCache(K, V), g.SeqBatch(lens, table, 32, row_start=at, max_rows=rows), d ** -0.5, causal=causal)
+        assert torch.equal(O, want) and torch.all(O[2 + rows:] == 7) and torch.all(O[:2 + rows] != 7)
+
+
+def test_appended_rows_of_lengths_at_the_ends_of_32_bits(ctx):
+    """Negative positions: zero queries, nothing appended; positions at the bound and beyond: NaN."""
+    K, V = make_cache(8, 1, 16, 64, BF16, "head", fill=3.0)
+    table = torch.arange(8, dtype=torch.int32, device="cuda").view(4, 2)
+    batch = g.SeqBatch(int32(INT_MIN, INT_MAX, INT_MIN + 1, -1), table, 32, row_start=int32(0, 2, 4, 6, 8), max_rows=2)
+    QKV, Q = rand((8, 192), 3, BF16), torch.full((8, 64), 7.0, dtype=BF16, device="cuda")
+    g.gelo_rope_append(ctx, QKV, 1, g.KvCache(K, V), batch, Q=Q)
+    assert torch.all(Q[[0, 1, 4, 5, 6, 7]] == 0) and torch.isnan(Q[2:4]).all()
+    assert torch.all(K == 3) and torch.all(V == 3)
