@@ -383,6 +383,8 @@ class SeqBatch:
             _vector(row_start, "row_start", torch.int32, n_seqs + 1)
         if page_table.dtype != torch.int32 or page_table.dim() != 2 or page_table.shape[0] != n_seqs:
             raise ValueError("page_table must be an int32 tensor with a row per sequence")
+        if not -2 ** 31 <= max_rows < 2 ** 31:
+            raise ValueError(f"max_rows={max_rows} does not fit 32 bits")
         tp, table_ld = _matrix(page_table, "page_table")     # (rows closer than max_kv_len takes, an expanded table's too, are refused by the library)
         self.kv_len, self.page_table, self.row_start = kv_len, page_table, row_start
         self.n_seqs, self.n_rows, self.pages, self.max_kv_len = n_seqs, n_seqs, page_table.shape[1], max_kv_len

@@ -1491,7 +1491,7 @@ static gelo_status check_batch(gelo_ctx* ctx, const gelo_seq_batch* b, int page_
     if (b->table_ld < pages) return fail(ctx, GELO_ESHAPE, "table_ld=%lld: %d rows take %lld pages", (long long)b->table_ld, b->max_kv_len, (long long)pages);
     if (b->n_rows > kMostRows) return fail(ctx, GELO_ESHAPE, "n_rows=%d exceeds %d", b->n_rows, kMostRows);
     if (b->max_kv_len > INT32_MAX - 65536 || b->max_rows > INT32_MAX - 65536) return fail(ctx, GELO_ESHAPE, "max_kv_len=%d max_rows=%d", b->max_kv_len, b->max_rows);
-    *out = SeqBatch{b->n_seqs, b->n_rows, b->max_rows, b->max_kv_len, b->row_start, b->kv_len, b->page_table, b->table_ld};
+    *out = SeqBatch{b->n_seqs, b->n_rows, rows_bound(b->max_rows, b->n_rows), b->max_kv_len, b->row_start, b->kv_len, b->page_table, b->table_ld};
     return GELO_OK;
 }
 

@@ -1098,7 +1098,7 @@ hipError_t join(const AttnArgs& a, hipStream_t stream) {
 }
 
 // Which kernel, and how the cache is cut: chunks of `chunk` keys, n_chunks of them to the longest sequence.
-struct Plan { bool prompt, shared, paired, past, by_head; int col_tiles, chunk, n_chunks; int64_t workgroups; };
+struct Plan { bool prompt, shared, paired, past, by_head; int chunk, n_chunks; int64_t col_tiles, workgroups; };
 constexpr int64_t kMostWorkgroups = 1 << 23;     // of a launch: 2^31 threads and no more fit HIP's 32-bit counts
 constexpr int kCus = 256;
 constexpr int kFewTarget = 512, kFewLeast = 256;         // workgroups that fill the chip (two to a CU), keys to a chunk at least
@@ -1117,7 +1117,7 @@ double join_us(const Attention& o, const Plan& p) {
 Plan plan_few(const Attention& o, int64_t columns, int bytes, double* us) {
     Plan p;
     p.prompt = p.shared = p.paired = p.past = p.by_head = false;
-    p.col_tiles = (int)((columns + 15) / 16);
+    p.col_tiles = (columns + 15) / 16;
     const int64_t tiles = (int64_t)o.batch.n_seqs * o.cache.n_kv_heads * p.col_tiles;
     const int64_t most = (o.batch.max_kv_len + kFewLeast - 1) / kFewLeast;
     int64_t cuts = kFewTarget / tiles;
@@ -1147,7 +1147,7 @@ Plan plan_prompt(const Attention& o, int64_t columns, double* us) {
     Plan best;
     best.prompt = true;
     best.shared = best.past = best.by_head = false;
-    best.col_tiles = (int)((columns + 32 * kPromptWaves - 1) / (32 * kPromptWaves));
+    best.col_tiles = (columns + 32 * kPromptWaves - 1) / (32 * kPromptWaves);
     const int64_t sets = (int64_t)o.batch.n_seqs * o.cache.n_kv_heads, tiles = sets * best.col_tiles;
     const int d = o.cache.head_dim, per_cu = d == 256 ? 1 : 2;
     const double bytes = 4.0 * sets * o.batch.max_kv_len * d;
@@ -1171,7 +1171,7 @@ Plan plan_prompt(const Attention& o, int64_t columns, double* us) {
     // once but no more than twice that, a workgroup takes a long and a short one: all end together.
     const int64_t pairs = sets * ((best.col_tiles + 1) / 2);
     best.paired = o.causal && best.n_chunks == 1 && best.col_tiles > 1 && best.workgroups > kCus * per_cu && pairs <= kCus * per_cu;
-    if (best.workgroups <= kMostWorkgroups) best.workgroups = 8 * (int64_t)dies_slots((best.paired ? (best.col_tiles + 1) / 2 : best.col_tiles) * best.n_chunks, (int)sets);
+    if (best.workgroups <= kMostWorkgroups) best.workgroups = 8 * (int64_t)dies_slots((int)((best.paired ? (best.col_tiles + 1) / 2 : best.col_tiles) * best.n_chunks), (int)sets);
     return best;
 }
 
@@ -1189,12 +1189,12 @@ Plan plan_float(const Attention& o, int64_t columns) {
     Plan p;
     p.shared = true;
     p.prompt = p.paired = p.past = p.by_head = false;
-    p.col_tiles = (int)((columns + 16 * kFloatWaves - 1) / (16 * kFloatWaves));
+    p.col_tiles = (columns + 16 * kFloatWaves - 1) / (16 * kFloatWaves);
     const int64_t sets = (int64_t)o.batch.n_seqs * o.cache.n_kv_heads, tiles = sets * p.col_tiles;
     const int64_t most = (o.batch.max_kv_len + kFewLeast - 1) / kFewLeast, cuts = kFewTarget / tiles;
     cut(&p, o.batch.max_kv_len, cuts < 1 ? 1 : cuts < most ? cuts : most);
     p.workgroups = tiles * p.n_chunks;
-    if (p.workgroups <= kMostWorkgroups) p.workgroups = 8 * (int64_t)dies_slots(p.col_tiles * p.n_chunks, (int)sets);
+    if (p.workgroups <= kMostWorkgroups) p.workgroups = 8 * (int64_t)dies_slots((int)(p.col_tiles * p.n_chunks), (int)sets);
     return p;
 }
 
@@ -1222,7 +1222,7 @@ hipError_t launch(const Attention& o, hipStream_t stream) {
     a.scale2 = o.scale == 0.f ? 1e-30f : fabsf(a.scale2s);      // (-inf, a hidden score, times 0 would be NaN)
     a.flip = o.scale < 0.f ? 0x80008000u : 0u;
     a.causal = o.causal;
-    a.chunk = p.chunk; a.n_chunks = p.n_chunks; a.col_tiles = p.col_tiles; a.paired = p.paired; a.by_head = p.by_head;
+    a.chunk = p.chunk; a.n_chunks = p.n_chunks; a.col_tiles = (int)p.col_tiles; a.paired = p.paired; a.by_head = p.by_head;
     a.kv = o.cache; a.b = o.batch;
     const int64_t items = (int64_t)o.batch.n_rows * o.n_q_heads;
     a.part_o = o.workspace;
@@ -1257,30 +1257,39 @@ hipError_t of_width(const Attention& o, hipStream_t stream) {
 
 }  // namespace
 
-// Which way a call of these sizes goes: 0 few columns, 1 many, 2 many with causal tiles in pairs; plus 4 where the cache is cut.
-int attention_way(int is_bf16, int causal, int n_q_heads, int n_kv_heads, int head_dim, int n_seqs, int n_rows, int max_rows, int max_kv_len) {
+bool attention_fits(const Attention& o, int is_bf16) {
+    if (o.batch.n_seqs > 65535 || o.cache.n_kv_heads > 65535) return false;          // dimensions of a launch
+    // (before the plan: a column is a row's head, so what this lets through has few enough of them for the plan's counts)
+    if ((int64_t)o.batch.n_rows * o.n_q_heads > kMostWorkgroups) return false;
+    return plan_of(o, is_bf16).workgroups <= kMostWorkgroups;
+}
+
+namespace {
+Attention described(int causal, int n_q_heads, int n_kv_heads, int head_dim, int n_seqs, int n_rows, int max_rows, int max_kv_len) {
     Attention o = {};
     o.causal = causal != 0; o.n_q_heads = n_q_heads;
     o.cache.n_kv_heads = n_kv_heads; o.cache.head_dim = head_dim;
-    o.batch.n_seqs = n_seqs; o.batch.n_rows = n_rows; o.batch.max_rows = max_rows; o.batch.max_kv_len = max_kv_len;
+    o.batch.n_seqs = n_seqs; o.batch.n_rows = n_rows; o.batch.max_rows = rows_bound(max_rows, n_rows); o.batch.max_kv_len = max_kv_len;
+    return o;
+}
+}  // namespace
+
+// Which way a call of these sizes goes: 0 few columns, 1 many, 2 many with causal tiles in pairs; plus 4 where the cache is cut; -1: too large.
+int attention_way(int is_bf16, int causal, int n_q_heads, int n_kv_heads, int head_dim, int n_seqs, int n_rows, int max_rows, int max_kv_len) {
+    const Attention o = described(causal, n_q_heads, n_kv_heads, head_dim, n_seqs, n_rows, max_rows, max_kv_len);
+    if (!attention_fits(o, is_bf16)) return -1;
     const Plan p = plan_of(o, is_bf16);
     return (p.prompt ? p.paired ? 2 : 1 : 0) + (p.n_chunks > 1 ? 4 : 0);
 }
 
-// Whether a float call goes by tiles of 64 columns: 1, with a cut cache 5.
+// Whether a float call goes by tiles of 64 columns: 1, with a cut cache 5; -1: too large.
 int attention_float_way(int causal, int n_q_heads, int n_kv_heads, int head_dim, int n_seqs, int n_rows, int max_rows, int max_kv_len) {
-    Attention o = {};
-    o.causal = causal != 0; o.n_q_heads = n_q_heads;
-    o.cache.n_kv_heads = n_kv_heads; o.cache.head_dim = head_dim;
-    o.batch.n_seqs = n_seqs; o.batch.n_rows = n_rows; o.batch.max_rows = max_rows; o.batch.max_kv_len = max_kv_len;
+    const Attention o = described(causal, n_q_heads, n_kv_heads, head_dim, n_seqs, n_rows, max_rows, max_kv_len);
+    if (!attention_fits(o, 0)) return -1;
     const Plan p = plan_of(o, 0);
     return (p.shared ? 1 : 0) + (p.n_chunks > 1 ? 4 : 0);
 }
 
-bool attention_fits(const Attention& o, int is_bf16) {
-    if (o.batch.n_seqs > 65535 || o.cache.n_kv_heads > 65535) return false;          // dimensions of a launch
-    return plan_of(o, is_bf16).workgroups <= kMostWorkgroups && (int64_t)o.batch.n_rows * o.n_q_heads <= kMostWorkgroups;
-}
 size_t attention_workspace_bytes(const Attention& o, int is_bf16) { return part_bytes(o, plan_of(o, is_bf16)); }
 // a plan of more than one chunk has at most its target of workgroups, and every row's head is a column of one of them
 size_t attention_workspace_bound(int head_dim) {

@@ -392,6 +392,8 @@ struct SeqBatch {
     const int32_t* kv_len;
     const int32_t* page_table; int64_t table_ld;
 };
+// max_rows is a bound, however far above them: no sequence brings more rows than there are
+inline int rows_bound(int max_rows, int n_rows) { return max_rows < n_rows ? max_rows : n_rows; }
 // rope.hip
 struct RopeTable { int rot, first, count; double base, factor, trained, low, high; float* out; };
 hipError_t rope_table(const RopeTable& o, hipStream_t stream);

@@ -63,3 +63,16 @@ def test_appended_rows_of_lengths_at_the_ends_of_32_bits(ctx):
     g.gelo_rope_append(ctx, QKV, 1, g.KvCache(K, V), batch, Q=Q)
     assert torch.all(Q[[0, 1, 4, 5, 6, 7]] == 0) and torch.isnan(Q[2:4]).all()
     assert torch.all(K == 3) and torch.all(V == 3)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("hq,max_rows", [(64, 2 ** 30), (64, 2 ** 30 + 16), (32, 2147418111)])
+def test_a_bound_of_rows_far_above_them(ctx, dtype, hq, max_rows):
+    d, page, rows = 128, 16, 100
+    K, V = make_cache(8, 1, page, d, dtype, "head", seed=3)
+    table, starts = torch.arange(8, dtype=torch.int32, device="cuda")[None], int32(0, rows)
+    Q = rand((rows, hq * d), 9, dtype)
+    O, want = torch.full_like(Q, 7.0), torch.full_like(Q, 7.0)
+    for most, out in ((max_rows, O), (rows, want)):
+        g.gelo_attention(ctx, Q, out, hq, g.KvCache(K, V), g.SeqBatch(int32(128), table, 128, row_start=starts, max_rows=most), d ** -0.5)
+    assert torch.equal(O, want) and torch.all(O != 7)

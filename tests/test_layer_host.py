@@ -1,5 +1,8 @@
 """The host's side of the operators between two projections: what the binding makes of tensors, and what the library reckons from
 sizes.  Nothing here launches a kernel or needs a GPU."""
+import subprocess
+import sys
+
 import pytest
 import torch
 
@@ -45,3 +48,27 @@ def test_a_prepared_weight_that_the_kernels_cannot_read_is_refused(wrong):
         g.gelo_project_fp8_codes(None, codes, scales, Wq, p, Y, stream=0)
     with pytest.raises(ValueError):
         g.gelo_project_fp8(None, U, Wq, p, Y, stream=0)
+
+
+def reckoned(hook, *args):
+    """What a hook of the library returns, asked in a process of its own (a division by zero ends one)."""
+    code = f"import ctypes; print(ctypes.CDLL({g.LIB_PATH!r})[{hook!r}](*{args!r}))"
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=60)
+    assert r.returncode == 0, (hook, args, r.returncode)
+    return int(r.stdout)
+
+
+WAY, FLOAT_WAY = "_ZN4gelo13attention_wayEiiiiiiiii", "_ZN4gelo19attention_float_wayEiiiiiiii"
+
+
+@pytest.mark.parametrize("heads,max_rows", [(64, 2 ** 30), (64, 2 ** 30 + 16), (64, 2 ** 30 - 1), (32, 2147418111), (1, 2147418111)])
+def test_a_bound_of_rows_far_above_them_plans_as_the_rows_do(heads, max_rows):
+    """Rows times heads to a key head pass 32 bits there."""
+    for rows in (16, 100, 4096):
+        for causal in (0, 1):
+            for bf16 in (0, 1):
+                assert reckoned(WAY, bf16, causal, heads, 1, 128, 1, rows, max_rows, 4096) == reckoned(WAY, bf16, causal, heads, 1, 128, 1, rows, rows, 4096) >= 0
+            assert reckoned(FLOAT_WAY, causal, heads, 1, 128, 1, rows, max_rows, 4096) == reckoned(FLOAT_WAY, causal, heads, 1, 128, 1, rows, rows, 4096) >= 0
+    assert reckoned(WAY, 1, 1, heads, 1, 128, 1, 2 ** 23 + 1, max_rows, 4096) == -1         # rows' heads beyond one launch
+    with pytest.raises(ValueError):
+        g.SeqBatch(on_gpu(ints(1)), on_gpu(ints(1, 6)), 32, row_start=on_gpu(ints(2)), max_rows=2 ** 32 + 1)
