@@ -34,8 +34,8 @@ constexpr float kLog2E = 1.4426950408889634f;
 struct AttnArgs {
     const void* Q; int64_t ldq;
     void* O; int64_t ldo;
-    float* part_o;               // [chunk][row][head][D], where the cache is cut
-    float* part_ml;              // [chunk][row][head][2]: maximum (of log2) and sum
+    float* part_o;               // [chunk][sequence, its row][head][D], where the cache is cut: max_rows places to a sequence
+    float* part_ml;              // [chunk][sequence, its row][head][2]: maximum (of log2) and sum
     int n_q_heads, group;        // query heads to a key head
     float scale2;                // |scale| log2 e
     float scale2s;               // scale log2 e
@@ -53,6 +53,11 @@ __device__ __forceinline__ float across_groups_max(float v) {
 __device__ __forceinline__ float across_groups_sum(float v) {
     v += __shfl_xor(v, 16, 64);
     return v + __shfl_xor(v, 32, 64);
+}
+
+// the place of the part that chunk `chunk` makes of head `head` of a sequence's row i
+__device__ __forceinline__ int64_t part_of(const AttnArgs& a, int chunk, int seq, int i, int head) {
+    return (((int64_t)chunk * a.b.n_seqs + seq) * a.b.max_rows + i) * a.n_q_heads + head;
 }
 
 // sum + the two bfloat16 of a word: their products with 1
@@ -456,7 +461,7 @@ void attention_few_kernel(AttnArgs a) {
             for (int u = 0; u < 4; ++u) o[u] *= inv;         // (nothing was added to o where there was no weight)
             store4((T*)a.O + rr * a.ldo + (int64_t)h * D + x, o);
         } else {
-            const int64_t item = ((int64_t)chunk * a.b.n_rows + rr) * a.n_q_heads + h;
+            const int64_t item = part_of(a, chunk, seq, ri, h);
             *reinterpret_cast<f32x4_t*>(a.part_o + item * D + x) = o;
             if (x == 0) { a.part_ml[2 * item] = top; a.part_ml[2 * item + 1] = total; }
         }
@@ -595,7 +600,7 @@ void attention_float_kernel(AttnArgs a) {
     if (wave_col + c >= columns) return;
     const bool whole = a.n_chunks == 1;
     const float by = whole ? inverse_of(total, limit >= 0) : 1.f;
-    const int64_t part = ((int64_t)chunk * a.b.n_rows + row) * a.n_q_heads + head;
+    const int64_t part = part_of(a, chunk, seq, i, head);
     float* out = whole ? (float*)a.O + row * a.ldo + (int64_t)head * D : a.part_o + part * D;
     // acc[j][r]: component VD (4 g + r) + j
 #pragma unroll
@@ -964,7 +969,7 @@ __device__ __forceinline__ bool prompt_tile(const AttnArgs& a, int seq, int kvh,
     float total = l + __shfl_xor(l, 32, 64);
     if (notes.bad) total = __builtin_nanf("");
     const float by = whole ? inverse_of(total, limit >= 0) : 1.f;       // (without weights acc is 0: what was not finite is out of it by now)
-    const int64_t part = ((int64_t)chunk * a.b.n_rows + row) * a.n_q_heads + head;
+    const int64_t part = part_of(a, chunk, seq, my_col / a.group, head);
 #pragma unroll
     for (int t = 0; t < DT; ++t)
 #pragma unroll
@@ -1015,6 +1020,7 @@ void attention_join_kernel(AttnArgs a) {
     bool there = item < items && x < D;
     const int row = there ? (int)(item / a.n_q_heads) : 0;
     int used = 0;
+    int64_t part0 = 0;                                       // the first chunk's part
     if (there) {
         int seq = row, i = 0, count = 1;
         if (a.b.row_start) {
@@ -1036,17 +1042,19 @@ void attention_join_kernel(AttnArgs a) {
             const int kv_len = length_of_sequence(a.b, seq), kv_end = min(kv_len, a.b.max_kv_len);
             const int limit = min(a.causal ? kv_len - count + i : kv_len - 1, kv_end - 1);
             used = limit < 0 ? 0 : limit / a.chunk + 1;
+            part0 = part_of(a, 0, seq, i, (int)(item - (int64_t)row * a.n_q_heads));
         }
     }
     float top = -__builtin_inff(), total = 0.f;
     f32x4_t o = {0.f, 0.f, 0.f, 0.f};
     constexpr int DEEP = 4;                                  // chunks whose parts are sent for together
+    const int64_t apart = (int64_t)a.b.n_seqs * a.b.max_rows * a.n_q_heads;      // parts of a chunk
     for (int s0 = turn; s0 < used; s0 += DEEP * P) {
         float2 part[DEEP];
         f32x4_t y[DEEP];
 #pragma unroll
         for (int k = 0; k < DEEP; ++k) {
-            const int64_t at = min(s0 + k * P, used - 1) * items + item;
+            const int64_t at = min(s0 + k * P, used - 1) * apart + part0;
             part[k] = *reinterpret_cast<const float2*>(a.part_ml + 2 * at);
             y[k] = *reinterpret_cast<const f32x4_t*>(a.part_o + at * D + x);
         }
@@ -1111,7 +1119,8 @@ void cut(Plan* p, int max_kv_len, int64_t cuts) {
 }
 // The join: a launch behind another one, and the parts written and read.
 double join_us(const Attention& o, const Plan& p) {
-    return p.n_chunks == 1 ? 0.0 : 5.0 + 8.0 * p.n_chunks * o.batch.n_rows * o.n_q_heads * o.cache.head_dim / 4e6;
+    const double rows = (double)o.batch.n_seqs * o.batch.max_rows;
+    return p.n_chunks == 1 ? 0.0 : 5.0 + 8.0 * p.n_chunks * (rows < o.batch.n_rows ? rows : o.batch.n_rows) * o.n_q_heads * o.cache.head_dim / 4e6;
 }
 
 Plan plan_few(const Attention& o, int64_t columns, int bytes, double* us) {
@@ -1208,8 +1217,8 @@ Plan plan_of(const Attention& o, int is_bf16) {
     return few_us < prompt_us ? few : prompt;
 }
 
-size_t part_bytes(const Attention& o, const Plan& p) {
-    return p.n_chunks == 1 ? 0 : (size_t)p.n_chunks * o.batch.n_rows * o.n_q_heads * (o.cache.head_dim + 2) * sizeof(float);
+int64_t parts(const Attention& o, const Plan& p) {
+    return p.n_chunks == 1 ? 0 : (int64_t)p.n_chunks * o.batch.n_seqs * o.batch.max_rows * o.n_q_heads;
 }
 
 template <class T, int D>
@@ -1224,9 +1233,8 @@ hipError_t launch(const Attention& o, hipStream_t stream) {
     a.causal = o.causal;
     a.chunk = p.chunk; a.n_chunks = p.n_chunks; a.col_tiles = (int)p.col_tiles; a.paired = p.paired; a.by_head = p.by_head;
     a.kv = o.cache; a.b = o.batch;
-    const int64_t items = (int64_t)o.batch.n_rows * o.n_q_heads;
     a.part_o = o.workspace;
-    a.part_ml = p.n_chunks == 1 ? nullptr : o.workspace + (int64_t)p.n_chunks * items * D;
+    a.part_ml = p.n_chunks == 1 ? nullptr : o.workspace + parts(o, p) * D;
     if constexpr (sizeof(T) == 2) {
         if (p.prompt)
             hipLaunchKernelGGL((attention_prompt_kernel<D>), dim3((unsigned)p.workgroups), dim3(64 * kPromptWaves), (size_t)prompt_lds<D>(), stream, a);
@@ -1290,12 +1298,19 @@ int attention_float_way(int causal, int n_q_heads, int n_kv_heads, int head_dim,
     return (p.shared ? 1 : 0) + (p.n_chunks > 1 ? 4 : 0);
 }
 
-size_t attention_workspace_bytes(const Attention& o, int is_bf16) { return part_bytes(o, plan_of(o, is_bf16)); }
-// a plan of more than one chunk has at most its target of workgroups, and every row's head is a column of one of them
+size_t attention_workspace_bytes(const Attention& o, int is_bf16) { return parts(o, plan_of(o, is_bf16)) * (o.cache.head_dim + 2) * sizeof(float); }
+// A plan of more than one chunk has at most its target of workgroups, and every part is a column of one of them: parts have places by sequence and row
+// of it, so rows that belong to no sequence have none.
 size_t attention_workspace_bound(int head_dim) {
     const size_t columns = kPromptTarget * 32 * kPromptWaves;
     static_assert(kFewTarget * 16 <= kPromptTarget * 32 * kPromptWaves, "");
     return columns * (head_dim + 2) * sizeof(float);
+}
+
+// attention_workspace_bytes of these sizes
+size_t attention_parts(int is_bf16, int causal, int n_q_heads, int n_kv_heads, int head_dim, int n_seqs, int n_rows, int max_rows, int max_kv_len) {
+    const Attention o = described(causal, n_q_heads, n_kv_heads, head_dim, n_seqs, n_rows, max_rows, max_kv_len);
+    return attention_fits(o, is_bf16) ? attention_workspace_bytes(o, is_bf16) : 0;
 }
 
 hipError_t attention(const Attention& o, int is_bf16, hipStream_t stream) {

@@ -422,6 +422,7 @@ int attention_way(int is_bf16, int causal, int n_q_heads, int n_kv_heads, int he
 int attention_float_way(int causal, int n_q_heads, int n_kv_heads, int head_dim, int n_seqs, int n_rows, int max_rows, int max_kv_len);
 bool attention_fits(const Attention& o, int is_bf16);       // as one launch
 size_t attention_workspace_bytes(const Attention& o, int is_bf16);
+size_t attention_parts(int is_bf16, int causal, int n_q_heads, int n_kv_heads, int head_dim, int n_seqs, int n_rows, int max_rows, int max_kv_len);
 size_t attention_workspace_bound(int head_dim);
 hipError_t attention(const Attention& o, int is_bf16, hipStream_t stream);
 hipError_t attention_init();

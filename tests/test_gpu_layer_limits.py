@@ -76,3 +76,30 @@ def test_a_bound_of_rows_far_above_them(ctx, dtype, hq, max_rows):
     for most, out in ((max_rows, O), (rows, want)):
         g.gelo_attention(ctx, Q, out, hq, g.KvCache(K, V), g.SeqBatch(int32(128), table, 128, row_start=starts, max_rows=most), d ** -0.5)
     assert torch.equal(O, want) and torch.all(O != 7)
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,d,new,kv,many", [(BF16, 8, 2, 64, [1, 3], [9000, 500], 0), (BF16, 8, 8, 128, [200, 30], [5000, 900], 1),
+                                                        (F32, 64, 8, 96, [65, 17], [700, 300], 1), (F32, 4, 2, 128, [1, 2], [3000, 4], 0)])
+def test_a_cut_cache_and_rows_of_no_sequence(ctx, dtype, hq, hkv, d, new, kv, many):
+    """Rows in front of and behind those of the sequences, far more than they bring: the parts of a cut cache have no places for them, and the
+    memory that was reserved is not grown."""
+    front, behind, page = 300, 2000, 16
+    own = g.gelo_create(0, 1)
+    try:
+        g.gelo_reserve_attention(own, d)
+        batch, table, row_start, n_pages = make_batch(new, kv, page, 3)
+        K, V = make_cache(n_pages, hkv, page, d, dtype, "head", seed=5)
+        Q = rand((front + sum(new) + behind, hq * d), 8, dtype)
+        O, want = torch.full_like(Q, 7.0), torch.full_like(Q, 7.0)
+        inner = slice(front, front + sum(new))
+        assert (way(own, Q[inner], new, kv, hq, hkv, d, True) if dtype == BF16 else float_way(new, kv, hq, hkv, d, True)) == many + 4
+        padded = g.SeqBatch(batch.kv_len, batch.page_table, max(kv), row_start=torch.from_numpy(row_start).cuda() + front, max_rows=max(new))
+        g.gelo_attention(own, Q[inner], want[inner], hq, g.KvCache(K, V), batch, d ** -0.5)
+        torch.cuda.synchronize()
+        free = torch.cuda.mem_get_info()[0]
+        g.gelo_attention(own, Q, O, hq, g.KvCache(K, V), padded, d ** -0.5)
+        torch.cuda.synchronize()
+        assert torch.cuda.mem_get_info()[0] == free
+        assert torch.equal(O, want) and torch.all(O[:front] == 7) and torch.all(O[inner.stop:] == 7) and torch.all(O[inner] != 7)
+    finally:
+        g.gelo_destroy(own)

@@ -1,5 +1,7 @@
 """The host's side of the operators between two projections: what the binding makes of tensors, and what the library reckons from
 sizes.  Nothing here launches a kernel or needs a GPU."""
+import ctypes
+import random
 import subprocess
 import sys
 
@@ -72,3 +74,21 @@ def test_a_bound_of_rows_far_above_them_plans_as_the_rows_do(heads, max_rows):
     assert reckoned(WAY, 1, 1, heads, 1, 128, 1, 2 ** 23 + 1, max_rows, 4096) == -1         # rows' heads beyond one launch
     with pytest.raises(ValueError):
         g.SeqBatch(on_gpu(ints(1)), on_gpu(ints(1, 6)), 32, row_start=on_gpu(ints(2)), max_rows=2 ** 32 + 1)
+
+
+def test_the_workspace_that_is_reserved_is_enough_for_any_batch():
+    """gelo_reserve_attention promises that no call allocates after it: rows of one sequence or many, cut caches, and more rows than the sequences
+    may bring (a batch padded for a captured launch)."""
+    lib = ctypes.CDLL(g.LIB_PATH)
+    need, most = lib["_ZN4gelo15attention_partsEiiiiiiiii"], lib["_ZN4gelo25attention_workspace_boundEi"]
+    need.restype = most.restype = ctypes.c_size_t
+    assert need(1, 1, 32, 8, 128, 1, 4096, 1, 32768) == need(1, 1, 32, 8, 128, 1, 1, 1, 32768) > 0
+    rng, cut = random.Random(1), 0
+    for _ in range(20000):
+        hkv, d = rng.choice([1, 2, 5, 8, 32]), rng.choice([64, 96, 128, 256])
+        hq, seqs, rows = hkv * rng.choice([1, 2, 4, 7, 16]), int(2 ** rng.uniform(0, 8)), int(2 ** rng.uniform(0, 13))
+        n_rows = min(rng.choice([seqs, seqs * rows, max(rows, seqs), int(2 ** rng.uniform(0, 15))]), 2 ** 23 // hq)
+        size = need(rng.randint(0, 1), rng.randint(0, 1), hq, hkv, d, seqs, n_rows, rows, int(2 ** rng.uniform(4, 20)))
+        assert size <= most(d), (hq, hkv, d, seqs, n_rows, rows)
+        cut += size > 0
+    assert cut > 1000
