@@ -298,7 +298,7 @@ typedef enum { GELO_ROPE_HALF = 0, GELO_ROPE_PAIRS = 1 } gelo_rope_layout;
  * scales) may be NULL, not both.  H may be X or R.  Everything is computed in float from the unrounded h and rounded once.  codes: n x d bytes
  * (ldq, a multiple of 8), the row quantisation of gelo_project_fp8, scales: n floats (1 for a row of zeros): together the operand of
  * gelo_project_fp8_codes, which wants ldq to be a multiple of 16.  A NaN or infinity in a row makes the row's y NaN or zero as the formula does; a NaN among them gives the
- * code 0x7F and the scale NaN.  d <= GELO_NORM_MAX_D, eps >= 0. */
+ * code 0x7F and the scale NaN.  d <= GELO_NORM_MAX_D, eps >= 0, n up to 2^22 (d > 8192: 2^21). */
 gelo_status gelo_rms_norm(gelo_ctx* ctx, gelo_dtype dtype, int n, int d, const void* X, int64_t ldx, const void* R, int64_t ldr,
                           const void* gamma, float eps, void* R_out, int64_t ldro, void* H, int64_t ldh,
                           uint8_t* codes, int64_t ldq, float* scales, void* stream);

@@ -1419,7 +1419,8 @@ gelo_status gelo_measure_matrix_rate(gelo_ctx* ctx, int fp8, int iters, int laun
 }
 
 // ------------------------------------------------------------------ between two projections --
-static constexpr int kMostRows = 1 << 22;      // a workgroup of up to 1024 threads each: HIP counts a launch's threads in 32 bits
+static constexpr int kMostRows = 1 << 22;      // of a batch: the append has a workgroup of 256 threads to each
+static_assert((int64_t)kMostRows * 256 <= kMostThreads, "");
 
 gelo_status gelo_rms_norm(gelo_ctx* ctx, gelo_dtype dtype, int n, int d, const void* X, int64_t ldx, const void* R, int64_t ldr,
                           const void* gamma, float eps, void* R_out, int64_t ldro, void* H, int64_t ldh,
@@ -1428,7 +1429,7 @@ gelo_status gelo_rms_norm(gelo_ctx* ctx, gelo_dtype dtype, int n, int d, const v
     if (dtype != GELO_F32 && dtype != GELO_BF16) return fail(ctx, GELO_EINVAL, "unknown dtype %d", (int)dtype);
     if (n < 1 || d < 1) return fail(ctx, GELO_EINVAL, "n=%d d=%d", n, d);
     if (d % 8 != 0) return fail(ctx, GELO_EALIGN, "d=%d is not a multiple of 8", d);
-    if (n > kMostRows) return fail(ctx, GELO_ESHAPE, "n=%d exceeds %d rows", n, kMostRows);
+    if (n > rms_norm_most_rows(d)) return fail(ctx, GELO_ESHAPE, "n=%d exceeds %d rows of %d", n, rms_norm_most_rows(d), d);
     if (d > GELO_NORM_MAX_D) return fail(ctx, GELO_ESHAPE, "d=%d exceeds GELO_NORM_MAX_D = %d", d, GELO_NORM_MAX_D);
     if (!(eps >= 0.f) || std::isinf(eps)) return fail(ctx, GELO_EINVAL, "eps=%g must be finite and not negative", (double)eps);
     if (!gamma || !aligned16(gamma)) return fail(ctx, gamma ? GELO_EALIGN : GELO_EINVAL, "gamma must be a 16-byte aligned device vector");

@@ -1107,7 +1107,8 @@ hipError_t join(const AttnArgs& a, hipStream_t stream) {
 
 // Which kernel, and how the cache is cut: chunks of `chunk` keys, n_chunks of them to the longest sequence.
 struct Plan { bool prompt, shared, paired, past, by_head; int chunk, n_chunks; int64_t col_tiles, workgroups; };
-constexpr int64_t kMostWorkgroups = 1 << 23;     // of a launch: 2^31 threads and no more fit HIP's 32-bit counts
+constexpr int64_t kMostWorkgroups = kMostThreads / 256;      // all kernels here have workgroups of 256
+static_assert(64 * kFewWaves <= 256 && 64 * kFloatWaves <= 256 && 64 * kPromptWaves <= 256, "");
 constexpr int kCus = 256;
 constexpr int kFewTarget = 512, kFewLeast = 256;         // workgroups that fill the chip (two to a CU), keys to a chunk at least
 constexpr int kPromptTarget = 512, kPromptLeast = 128;

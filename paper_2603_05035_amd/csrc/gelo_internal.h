@@ -368,6 +368,7 @@ hipError_t zero_ints(int* p, int count, hipStream_t stream);
 hipError_t pad_matrix(float* M, int64_t ld, int n, int n_pad, hipStream_t stream);
 
 // ------------------------------------------- between two projections: norm, cache, attention --
+constexpr int64_t kMostThreads = (int64_t)1 << 31;          // of a launch: HIP counts them in 32 bits
 // norm.hip: see gelo_rms_norm; d a multiple of 8, at most 65536; all matrices 16-byte aligned with leading dimensions that are multiples of 8
 struct RmsNorm {
     const void* X; int64_t ldx;
@@ -380,6 +381,7 @@ struct RmsNorm {
     int n, d;
 };
 hipError_t rms_norm(const RmsNorm& o, int is_bf16, hipStream_t stream);
+int rms_norm_most_rows(int d);
 // gelo_kv_cache and gelo_seq_batch; page_rows = 1 << page_shift
 struct KvCache {
     void* k; void* v;

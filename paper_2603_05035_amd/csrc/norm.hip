@@ -189,6 +189,9 @@ hipError_t norm_of_type(const RmsNorm& o, hipStream_t stream) {
 
 }  // namespace
 
+// Rows of one launch: a row of more than 8192 values has a workgroup of 1024 threads, the others at most 512 threads.
+int rms_norm_most_rows(int d) { return (int)(kMostThreads / (d > 8192 ? 1024 : 512)); }
+
 hipError_t rms_norm(const RmsNorm& o, int is_bf16, hipStream_t stream) {
     return is_bf16 ? norm_of_type<uint16_t>(o, stream) : norm_of_type<float>(o, stream);
 }

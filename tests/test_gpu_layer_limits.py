@@ -65,6 +65,17 @@ def test_appended_rows_of_lengths_at_the_ends_of_32_bits(ctx):
     assert torch.all(K == 3) and torch.all(V == 3)
 
 
+def test_more_rows_than_a_launch_of_the_norm_holds_are_refused(ctx):
+    """Refused by their number, before anything is read: no such rows are there."""
+    lib, x = g.load_library(), torch.full((64,), 5.0, device="cuda")
+    p = ctypes.c_void_p(x.data_ptr())
+    for n, d in ((2 ** 21 + 1, 8200), (2 ** 22, 65536), (2 ** 22 + 1, 8192)):
+        status = lib.gelo_rms_norm(ctx, 0, n, d, p, d, None, 0, p, 1e-5, None, 0, p, d, None, 0, None, None)
+        assert g.STATUS_NAMES[status] == "GELO_ESHAPE" and b"exceeds" in lib.gelo_last_error(ctx)
+    torch.cuda.synchronize()
+    assert torch.all(x == 5)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("hq,max_rows", [(64, 2 ** 30), (64, 2 ** 30 + 16), (32, 2147418111)])
 def test_a_bound_of_rows_far_above_them(ctx, dtype, hq, max_rows):

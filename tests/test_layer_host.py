@@ -76,6 +76,16 @@ def test_a_bound_of_rows_far_above_them_plans_as_the_rows_do(heads, max_rows):
         g.SeqBatch(on_gpu(ints(1)), on_gpu(ints(1, 6)), 32, row_start=on_gpu(ints(2)), max_rows=2 ** 32 + 1)
 
 
+def test_a_norm_of_the_most_rows_is_a_launch_of_at_most_2_to_the_31_threads():
+    """Threads to a row as the launches of norm.hip have them, for d up to the second number of each pair."""
+    most = ctypes.CDLL(g.LIB_PATH)["_ZN4gelo18rms_norm_most_rowsEi"]
+    first = 8
+    for threads, last in ((64, 512), (256, 2048), (512, 4096), (256, 8192), (1024, 65536)):
+        for d in (first, last):
+            assert 2 ** 20 < most(d) and most(d) * threads <= 2 ** 31, d
+        first = last + 8
+
+
 def test_the_workspace_that_is_reserved_is_enough_for_any_batch():
     """gelo_reserve_attention promises that no call allocates after it: rows of one sequence or many, cut caches, and more rows than the sequences
     may bring (a batch padded for a captured launch)."""
