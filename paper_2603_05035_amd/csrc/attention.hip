@@ -652,10 +652,19 @@ template <int D> __device__ __forceinline__ int v_pos(int r, int c) {          /
 
 // 0 times a value that is not finite is NaN also in columns that do not see its key.  Such values are rare, and they show in the result: a
 // workgroup that finds any there walks its keys once more (ODD) with zeros in their place and adds them to the columns that see them.
+// So it does where a base ended far out.  An exponent is s scale2 - base in one rounding, and the base is the rounding of one such product: from 2^32 on
+// they can stand 2^8 apart, and the largest weight of a column leaves float's range.  ODD rounds the product of such columns first.  (A base that was far
+// below zero and came back has left infinities or nothing: either is found or does not matter.)
 template <int D> struct PromptNotes {
-    int odd, bad;                                            // results that are not finite, page numbers outside the cache
+    int odd, bad;                                            // results that are not finite or a base far out, page numbers outside the cache
     int first[2][D];                                         // per component the first key whose value is +infinity (-infinity), NaN: both
 };
+
+constexpr float kFarBase = 0x1p28f;                         // products of this size are rounded by 16 at most
+__device__ __forceinline__ float rounded_exponent(float score, float scale2, float base) {
+#pragma clang fp contract(off)
+    return score * scale2 - base;
+}
 
 // One tile of columns of a sequence and key head, one chunk of the cache.  True: to be done again with ODD.
 template <int D, bool ODD>
@@ -808,6 +817,15 @@ __device__ __forceinline__ bool prompt_tile(const AttnArgs& a, int seq, int kvh,
 #pragma unroll
                 for (int e = 0; e < 8; ++e) p[G ^ 1][ks][e] = (__bf16)((float)p[G ^ 1][ks][e] * alpha);
         }
+        float from = base;
+        if constexpr (ODD) {
+            const bool far = fabsf(base) >= kFarBase;
+            if (__ballot(far)) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[G][r] = far ? rounded_exponent(s[G][r], a.scale2, base) / a.scale2 : s[G][r];
+                from = far ? 0.f : base;
+            }
+        }
         float part[2] = {0.f, 0.f};
         __builtin_amdgcn_sched_barrier(0);
         static_for<N>([&](auto ic) {
@@ -818,7 +836,7 @@ __device__ __forceinline__ bool prompt_tile(const AttnArgs& a, int seq, int kvh,
             else acc[(i - KS) % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[i % (AHEAD + 1)], p[G ^ 1][(i - KS) / DT], acc[(i - KS) % DT], 0, 0, 0);
             static_for<(i + 1) * 16 / N - i * 16 / N>([&](auto rc) {
                 constexpr int r = i * 16 / N + decltype(rc)::value;
-                const float w = __builtin_amdgcn_exp2f(s[G][r] * a.scale2 - base);
+                const float w = __builtin_amdgcn_exp2f(s[G][r] * a.scale2 - from);
                 s[G][r] = w;
                 if constexpr (r % 2 == 0) {
                     asm volatile("" : "+v"(s[G][r]));        // here: extra() may hold branches, behind which it would sink to its use
@@ -950,7 +968,7 @@ __device__ __forceinline__ bool prompt_tile(const AttnArgs& a, int seq, int kvh,
         static_for<1 + 2 * NF>([&](auto ic) { send(ic); });
     }
     if constexpr (!ODD) {
-        bool odd = false;
+        bool odd = fabsf(base) >= kFarBase;
 #pragma unroll
         for (int t = 0; t < DT; ++t)
 #pragma unroll

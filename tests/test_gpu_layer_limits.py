@@ -9,7 +9,7 @@ import torch
 import test_gpu_layer as base
 from oracle import layer_oracle as lo
 from paper_2603_05035_amd import binding as g
-from test_gpu_layer import BF16, F32, attention_bound, float_way, host, make_batch, make_cache, rand, way, within
+from test_gpu_layer import BF16, F32, U16, U32, attention_bound, float_way, host, make_batch, make_cache, rand, way, within
 
 pytestmark = pytest.mark.gpu
 
@@ -114,3 +114,45 @@ def test_a_cut_cache_and_rows_of_no_sequence(ctx, dtype, hq, hkv, d, new, kv, ma
         assert torch.equal(O, want) and torch.all(O[:front] == 7) and torch.all(O[inner.stop:] == 7) and torch.all(O[inner] != 7)
     finally:
         g.gelo_destroy(own)
+
+
+LARGE_SCORES = [  # dtype, new, kv, q heads, kv heads, d, way (of float calls as float_way has it)
+    (BF16, [1, 1], [200, 37], 4, 2, 64, 0), (BF16, [1, 2], [9000, 700], 4, 2, 128, 4),
+    (BF16, [150] * 16, [150 + 9 * i for i in range(16)], 16, 16, 128, 1), (BF16, [150] * 16, [150 + 9 * i for i in range(16)], 16, 16, 96, 1),
+    (BF16, [512, 377] * 4, [512, 400] * 4, 32, 32, 128, 2), (BF16, [200, 9], [5000, 4100], 8, 8, 64, 5), (BF16, [300], [2500], 8, 4, 256, 5),
+    (F32, [1, 1], [200, 37], 4, 2, 64, 0), (F32, [1, 2], [3000, 700], 4, 2, 256, 4),
+    (F32, [60] * 34, [60 + i for i in range(34)], 16, 16, 128, 1), (F32, [200, 65], [1000, 513], 16, 16, 96, 5),
+]
+
+
+@pytest.mark.parametrize("sign", [1, -1, 0])
+@pytest.mark.parametrize("power", [20, 30, 32, 33, 40, 90])
+@pytest.mark.parametrize("dtype,new,kv,hq,hkv,d,want", LARGE_SCORES)
+def test_scores_that_are_large_and_finite(ctx, dtype, new, kv, hq, hkv, d, want, power, sign):
+    """One component makes the scores: numbers of 8 bits, of about 2^power after the scale, exact in every type.  Different ones are at least
+    2^(power - 12) apart, so a row's weights are 1 where its largest score is and 0 elsewhere: the mean of those keys' values, with a rounding of the sum
+    (weights of 1 and their sum are exact) and one of the result.  sign 0: of either sign and nought, so that rows begin far below and come back."""
+    page = 32
+    batch, table, row_start, n_pages = make_batch(new, kv, page, 3)
+    K, V = make_cache(n_pages, hkv, page, d, dtype, "head", seed=5)
+    gen = torch.Generator().manual_seed(power)
+    bits, shift = (torch.randint(0, n, K.shape[:3], generator=gen) for n in (128, 4))
+    K.zero_()
+    signs = torch.randint(-3, 2, bits.shape, generator=gen).clamp(min=-1) if sign == 0 else torch.full_like(bits, sign)
+    K[..., 0] = (signs * (128 + bits) * 2.0 ** (shift - 10)).to(dtype).cuda()         # 2^-3 to 2
+    Q = torch.zeros((int(row_start[-1]), hq * d), dtype=dtype, device="cuda")
+    Q[:, ::d] = 2.0 ** power
+    O = torch.full_like(Q, 7.0)
+    assert (way(ctx, Q, new, kv, hq, hkv, d, True) if dtype == BF16 else float_way(new, kv, hq, hkv, d, True)) == want
+    g.gelo_attention(ctx, Q, O, hq, g.KvCache(K, V), batch, 0.9)
+    u = U16 if dtype == BF16 else U32
+    for s in range(len(kv)):
+        used = torch.from_numpy(table[s, :(kv[s] + page - 1) // page]).long().cuda()
+        for h in {0, (7 * s + 5) % hq, hq - 1}:
+            k, v = (x[used, h * hkv // hq].reshape(-1, d)[:kv[s]].double() for x in (K, V))
+            hidden = torch.arange(kv[s], device="cuda")[None] > torch.arange(new[s], device="cuda")[:, None] + (kv[s] - new[s])
+            score = k[:, 0][None].expand(new[s], -1).masked_fill(hidden, -math.inf)
+            w = (score == score.amax(1, keepdim=True)).double()
+            w /= w.sum(1, keepdim=True)
+            got = O[int(row_start[s]):int(row_start[s + 1]), h * d:(h + 1) * d]
+            within(got, host(w @ v), host(64 * U32 * (w @ v.abs()) + 1.01 * u * (w @ v).abs()), (s, h))
