@@ -294,8 +294,8 @@ typedef enum { GELO_ROPE_HALF = 0, GELO_ROPE_PAIRS = 1 } gelo_rope_layout;
 
 /* Root-mean-square norm of the rows of h = X + R (R may be NULL: h = X):
  *   R_out = h,   y = h / sqrt(mean_j h_j^2 + eps) * gamma,   H = y,   codes = e4m3(y * 448 / max_j |y_j|), scales = max_j |y_j| / 448.
- * X, R, R_out, H: n x d of type `dtype` (ldx, ldr, ldro, ldh); gamma: d values of it.  R_out may be NULL or R itself; H (or codes and
- * scales) may be NULL, not both.  H may be X or R.  Everything is computed in float from the unrounded h and rounded once.  codes: n x d bytes
+ * X, R, R_out, H: n x d of type `dtype` (ldx, ldr, ldro, ldh); gamma: d values of it.  R_out may be NULL; H (or codes and
+ * scales) may be NULL, not both.  H and R_out may be X or R; but for that no output shares memory with another matrix of the call.  Everything is computed in float from the unrounded h and rounded once.  codes: n x d bytes
  * (ldq, a multiple of 8), the row quantisation of gelo_project_fp8, scales: n floats (1 for a row of zeros): together the operand of
  * gelo_project_fp8_codes, which wants ldq to be a multiple of 16.  A NaN or infinity in a row makes the row's y NaN or zero as the formula does; a NaN among them gives the
  * code 0x7F and the scale NaN.  d <= GELO_NORM_MAX_D, eps >= 0, n up to 2^22 (d > 8192: 2^21). */
@@ -322,7 +322,7 @@ gelo_status gelo_rope_table(gelo_ctx* ctx, int rot_dim, int first_pos, int n_pos
  * brings n of them, has position p = kv_len[s] - n + j (kv_len counts the new rows).  The first rot_dim components
  * of every query and key head turn by the angles of `table` (row p, as gelo_rope_table writes it; positions from 0, n_table of them, at
  * least max_kv_len); the rest and the values are copied.  Q: n_rows x n_q_heads head_dim (ldq) takes the queries; it may be QKV itself
- * (ldq = ld: in place).  n_q_heads = 0 (Q NULL): keys and values only, as for an encoder's states.  rot_dim = 0 (table NULL): nothing
+ * (ldq = ld: in place), but not share its memory otherwise.  n_q_heads = 0 (Q NULL): keys and values only, as for an encoder's states.  rot_dim = 0 (table NULL): nothing
  * turns.  A row of negative position gives zero queries and is not appended; one at or beyond max_kv_len gives NaN queries and is not
  * appended; one whose page number lies outside the cache is not appended.  rot_dim a multiple of 16 up to head_dim, head_dim a multiple of 8. */
 gelo_status gelo_rope_append(gelo_ctx* ctx, gelo_dtype dtype, int n_q_heads, const void* QKV, int64_t ld, const gelo_kv_cache* cache,
@@ -333,7 +333,7 @@ gelo_status gelo_rope_append(gelo_ctx* ctx, gelo_dtype dtype, int n_q_heads, con
  * (n_q_heads a multiple of n_kv_heads).  causal != 0: row j of the n that sequence s brings sees the rows p <= kv_len[s] - n + j of
  * the cache (its own last; kv_len counts the new rows, which are in the cache already); causal = 0: all p < kv_len[s] (cross
  * attention to states of another length).  A row that sees nothing gives zeros (one that sees only scores of -infinity: NaN).  Q, O: n_rows x n_q_heads head_dim of type
- * `dtype` (ldq, ldo), O not in Q's memory; head_dim 64, 96, 128 or 256.  Rows outside [row_start[0], row_start[n_seqs]) are left as
+ * `dtype` (ldq, ldo), no bytes in common; head_dim 64, 96, 128 or 256.  Rows outside [row_start[0], row_start[n_seqs]) are left as
  * they are.  kv_len beyond max_kv_len is cut to it, below zero is zero; a page number outside the cache is not followed: the
  * results of its sequence are then NaN or partly so.  Statistics, products and sums are float; GELO_BF16 rounds the weights exp(s - max) to bfloat16, for
  * the product with V and for their sum alike.  What lies in cache rows that no query of the batch sees does not reach the result, NaN and infinity included.

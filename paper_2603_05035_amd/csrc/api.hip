@@ -1422,6 +1422,25 @@ gelo_status gelo_measure_matrix_rate(gelo_ctx* ctx, int fp8, int iters, int laun
 static constexpr int kMostRows = 1 << 22;      // of a batch: the append has a workgroup of 256 threads to each
 static_assert((int64_t)kMostRows * 256 <= kMostThreads, "");
 
+namespace {
+
+// n rows of `width` bytes, `ld` bytes apart
+struct Extent {
+    uintptr_t at; int64_t ld, width;
+    Extent(const void* p, int64_t ld_, int64_t width_, int64_t each) : at(reinterpret_cast<uintptr_t>(p)), ld(ld_ * each), width(width_ * each) {}
+};
+bool same_place(const Extent& a, const Extent& b, int64_t n) { return a.at == b.at && (n == 1 || a.ld == b.ld); }
+// Whether two matrices of n rows have bytes in common; where their rows are differently far apart, whether one begins before the other ends.
+bool share(const Extent& a, const Extent& b, int64_t n) {
+    if (!a.at || !b.at || a.at + (n - 1) * a.ld + a.width <= b.at || b.at + (n - 1) * b.ld + b.width <= a.at) return false;
+    if (n == 1 || a.ld != b.ld) return true;
+    int64_t off = (int64_t)(b.at - a.at) % a.ld;             // where b's rows begin in those of a
+    if (off < 0) off += a.ld;
+    return off < a.width || off + b.width > a.ld;
+}
+
+}  // namespace
+
 gelo_status gelo_rms_norm(gelo_ctx* ctx, gelo_dtype dtype, int n, int d, const void* X, int64_t ldx, const void* R, int64_t ldr,
                           const void* gamma, float eps, void* R_out, int64_t ldro, void* H, int64_t ldh,
                           uint8_t* codes, int64_t ldq, float* scales, void* stream) {
@@ -1440,6 +1459,11 @@ gelo_status gelo_rms_norm(gelo_ctx* ctx, gelo_dtype dtype, int n, int d, const v
     if (st == GELO_OK && H) st = check_matrix(ctx, "H", H, ldh, d);
     if (st == GELO_OK && (codes || scales)) st = check_codes(ctx, codes, ldq, scales, d, 8);
     if (st != GELO_OK) return st;
+    const int64_t each = dtype == GELO_BF16 ? 2 : 4;
+    const Extent in[] = {{X, ldx, d, each}, {R, ldr, d, each}}, h(H, ldh, d, each), out(R_out, ldro, d, each), q(codes, ldq, d, 1);
+    bool clash = share(h, out, n) || share(q, h, n) || share(q, out, n);
+    for (const Extent& e : in) clash |= share(q, e, n) || (share(h, e, n) && !same_place(h, e, n)) || (share(out, e, n) && !same_place(out, e, n));
+    if (clash) return fail(ctx, GELO_EINVAL, "H, R_out and codes must not share memory with each other, nor with X or R unless H or R_out is that matrix");
     GELO_HIP(ctx, hipSetDevice(ctx->device));
     RmsNorm o;
     o.X = X; o.ldx = ldx; o.R = R; o.ldr = ldr; o.gamma = gamma; o.R_out = R_out; o.ldro = ldro; o.H = H; o.ldh = ldh;
@@ -1517,6 +1541,9 @@ gelo_status gelo_rope_append(gelo_ctx* ctx, gelo_dtype dtype, int n_q_heads, con
         if (!table || !aligned16(table)) return fail(ctx, table ? GELO_EALIGN : GELO_EINVAL, "table must be a 16-byte aligned device buffer");
         if (n_table < batch->max_kv_len) return fail(ctx, GELO_ESHAPE, "a table of %d positions is too short for max_kv_len=%d", n_table, batch->max_kv_len);
     }
+    const int64_t each = dtype == GELO_BF16 ? 2 : 4, rows = batch->n_rows;
+    const Extent in(QKV, ld, width, each), out(Q, ldq, (int64_t)n_q_heads * cache->head_dim, each);
+    if (share(out, in, rows) && !same_place(out, in, rows)) return fail(ctx, GELO_EINVAL, "Q must not share memory with QKV unless it is that matrix");
     GELO_HIP(ctx, hipSetDevice(ctx->device));
     o.QKV = QKV; o.ld = ld; o.Q = Q; o.ldq = ldq; o.n_q_heads = n_q_heads; o.rot = rot_dim; o.pairs = layout == GELO_ROPE_PAIRS; o.table = table;
     GELO_HIP(ctx, rope_append(o, dtype == GELO_BF16, (hipStream_t)stream));
@@ -1540,6 +1567,8 @@ gelo_status gelo_attention(gelo_ctx* ctx, gelo_dtype dtype, int n_q_heads, const
     if (st == GELO_OK) st = check_matrix(ctx, "O", O, ldo, n_q_heads * d);
     if (st != GELO_OK) return st;
     o.Q = Q; o.ldq = ldq; o.O = O; o.ldo = ldo; o.n_q_heads = n_q_heads; o.scale = scale; o.causal = causal != 0;
+    const int64_t each = dtype == GELO_BF16 ? 2 : 4;
+    if (share(Extent(Q, ldq, (int64_t)n_q_heads * d, each), Extent(O, ldo, (int64_t)n_q_heads * d, each), batch->n_rows)) return fail(ctx, GELO_EINVAL, "O must not share memory with Q");
     if (!attention_fits(o, dtype == GELO_BF16)) return fail(ctx, GELO_ESHAPE, "%d sequences of up to %d rows and %d heads are too many for one launch", batch->n_seqs, batch->max_rows, n_q_heads);
     GELO_HIP(ctx, hipSetDevice(ctx->device));
     const size_t need = attention_workspace_bytes(o, dtype == GELO_BF16);

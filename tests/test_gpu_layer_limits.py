@@ -156,3 +156,71 @@ def test_scores_that_are_large_and_finite(ctx, dtype, new, kv, hq, hkv, d, want,
             w /= w.sum(1, keepdim=True)
             got = O[int(row_start[s]):int(row_start[s + 1]), h * d:(h + 1) * d]
             within(got, host(w @ v), host(64 * U32 * (w @ v.abs()) + 1.01 * u * (w @ v).abs()), (s, h))
+
+
+def refused(fn, *a, **kw):
+    with pytest.raises(g.GeloError) as e:
+        fn(*a, **kw)
+    return g.STATUS_NAMES[e.value.status] == "GELO_EINVAL"
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n", [1, 37])
+def test_outputs_of_the_norm_that_share_memory(ctx, n, dtype):
+    d = 264
+    gamma, wide = rand((d,), 3, dtype), rand((n + 1, 4 * d), 4, dtype)
+    X, R, H, out = (wide[:n, i * d:(i + 1) * d] for i in range(4))
+    x, r = X.clone(), R.clone()
+    want_h, want_r = torch.empty_like(x), torch.empty_like(x)
+    g.gelo_rms_norm(ctx, x, gamma, 1e-6, H=want_h, residual=r, residual_out=want_r)
+    # side by side in one buffer
+    g.gelo_rms_norm(ctx, X, gamma, 1e-6, H=H, residual=R, residual_out=out)
+    assert torch.equal(H, want_h) and torch.equal(out, want_r) and torch.equal(X, x) and torch.equal(R, r)
+    before = wide.clone()
+    shifted = wide.view(-1)[8:8 + n * 4 * d].view(n, 4 * d)[:, :d]                 # X, 8 values on
+    bytes_of = wide.view(torch.uint8)[:n, :d]
+    scales = torch.empty(n, device="cuda")
+    assert refused(g.gelo_rms_norm, ctx, X, gamma, 1e-6, H=H, residual_out=H)
+    assert refused(g.gelo_rms_norm, ctx, X, gamma, 1e-6, H=X, residual=R, residual_out=X)
+    assert refused(g.gelo_rms_norm, ctx, X, gamma, 1e-6, H=shifted)
+    assert refused(g.gelo_rms_norm, ctx, x, gamma, 1e-6, H=H, residual=X, residual_out=shifted)
+    assert refused(g.gelo_rms_norm, ctx, X, gamma, 1e-6, codes=bytes_of, scales=scales)
+    assert refused(g.gelo_rms_norm, ctx, x, gamma, 1e-6, H=X, codes=bytes_of, scales=scales)
+    assert refused(g.gelo_rms_norm, ctx, x, gamma, 1e-6, H=H, residual_out=X, codes=bytes_of, scales=scales)
+    if n > 1:                                                # of one width, but rows differently far apart
+        assert refused(g.gelo_rms_norm, ctx, X, gamma, 1e-6, H=wide.view(-1)[:n * d].view(n, d))
+    torch.cuda.synchronize()
+    assert torch.equal(wide, before)
+    g.gelo_rms_norm(ctx, X, gamma, 1e-6, H=X, residual=R, residual_out=R)          # either in the place of an input
+    assert torch.equal(X, want_h) and torch.equal(R, want_r)
+    X.copy_(x), R.copy_(r)
+    g.gelo_rms_norm(ctx, X, gamma, 1e-6, H=R, residual=R, residual_out=X)
+    assert torch.equal(R, want_h) and torch.equal(X, want_r)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n", [1, 5])
+def test_queries_and_results_that_share_memory(ctx, n, dtype):
+    d, page = 64, 16
+    K, V = make_cache(4, 1, page, d, dtype, "head", seed=3)
+    cache = g.KvCache(K, V)
+    batch = g.SeqBatch(int32(40), torch.arange(4, dtype=torch.int32, device="cuda")[None], 64, row_start=int32(0, n), max_rows=n)
+    wide = rand((n + 1, 4 * d), 4, dtype)
+    Q, O = wide[:n, :d], wide[:n, 2 * d:3 * d]
+    want = torch.empty_like(Q)
+    g.gelo_attention(ctx, Q.clone(), want, 1, cache, batch, 0.125)
+    g.gelo_attention(ctx, Q, O, 1, cache, batch, 0.125)                            # side by side
+    assert torch.equal(O, want)
+    before = wide.clone()
+    shifted = wide.view(-1)[8:8 + n * 4 * d].view(n, 4 * d)[:, :d]
+    assert refused(g.gelo_attention, ctx, Q, Q, 1, cache, batch, 0.125) and refused(g.gelo_attention, ctx, Q, shifted, 1, cache, batch, 0.125)
+    assert refused(g.gelo_attention, ctx, shifted, Q, 1, cache, batch, 0.125)
+    QKV = wide[:n, :3 * d]
+    keys = K.clone()
+    assert refused(g.gelo_rope_append, ctx, QKV, 1, cache, batch, Q=wide[:n, d:2 * d]) and refused(g.gelo_rope_append, ctx, QKV, 1, cache, batch, Q=shifted)
+    torch.cuda.synchronize()
+    assert torch.equal(wide, before) and torch.equal(K, keys)
+    g.gelo_rope_append(ctx, QKV, 1, cache, batch, Q=wide[:n, 3 * d:])              # behind the rows that it reads
+    assert torch.equal(wide[:n, 3 * d:], before[:n, :d])
+    g.gelo_rope_append(ctx, QKV, 1, cache, batch, Q=Q)
+    assert torch.equal(wide[:n, :3 * d], before[:n, :3 * d])
