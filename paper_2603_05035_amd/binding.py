@@ -387,9 +387,9 @@ class SeqBatch:
             raise ValueError(f"max_rows={max_rows} does not fit 32 bits")
         tp, table_ld = _matrix(page_table, "page_table")     # (rows closer than max_kv_len takes, an expanded table's too, are refused by the library)
         self.kv_len, self.page_table, self.row_start = kv_len, page_table, row_start
-        self.n_seqs, self.n_rows, self.pages, self.max_kv_len = n_seqs, n_seqs, page_table.shape[1], max_kv_len
+        self.n_seqs, self.pages, self.max_kv_len = n_seqs, page_table.shape[1], max_kv_len
         self.struct = _SeqBatchStruct(n_seqs, n_seqs, max_rows, max_kv_len, None if row_start is None else row_start.data_ptr(), kv_len.data_ptr(), tp, table_ld)
-        self.address = ctypes.addressof(self.struct)
+        self.described = n_seqs, self.struct, ctypes.addressof(self.struct)
 
 
 def _vector(t: torch.Tensor, name: str, dtype, count: int):
@@ -397,14 +397,19 @@ def _vector(t: torch.Tensor, name: str, dtype, count: int):
         raise ValueError(f"{name} must be a contiguous GPU vector of {count} {dtype}")
 
 
-def _check_rows(batch: SeqBatch, rows: int, cache: KvCache) -> None:
-    """Makes the batch's description one for matrices of `rows` rows."""
+def _described(batch: SeqBatch, rows: int, cache: KvCache):
+    """(rows, structure, its address) of the batch for matrices of `rows` rows; to be held while the address is in use.  Another number of rows
+    gets another structure: threads may share a batch."""
     if batch.pages * cache.page_rows < batch.max_kv_len:
         raise GeloError(2, f"max_kv_len={batch.max_kv_len} rows do not fit {batch.pages} pages of {cache.page_rows}")
-    if rows != batch.n_rows:
+    described = batch.described
+    if rows != described[0]:
         if batch.row_start is None:
             raise GeloError(2, f"{rows} rows, but every one of {batch.n_seqs} sequences brings one")
-        batch.n_rows = batch.struct.n_rows = rows
+        struct = _SeqBatchStruct.from_buffer_copy(batch.struct)
+        struct.n_rows = rows
+        batch.described = described = rows, struct, ctypes.addressof(struct)
+    return described
 
 
 def gelo_rms_norm(ctx, X: torch.Tensor, gamma: torch.Tensor, eps: float, H: torch.Tensor | None = None, residual: torch.Tensor | None = None,
@@ -468,8 +473,8 @@ def gelo_rope_append(ctx, QKV: torch.Tensor, n_q_heads: int, cache: KvCache, bat
         if table.dtype != torch.float32 or not table.is_cuda or not table.is_contiguous() or table.numel() != n_table * rot_dim:
             raise ValueError("table must be a contiguous float32 GPU tensor of positions x rot_dim")
         tp = table.data_ptr()
-    _check_rows(batch, rows, cache)
-    status = load_library().gelo_rope_append(ctx, cache.dtype, n_q_heads, zp, ld, cache.address, batch.address, layout, rot_dim, tp, n_table, qp, ldq,
+    described = _described(batch, rows, cache)
+    status = load_library().gelo_rope_append(ctx, cache.dtype, n_q_heads, zp, ld, cache.address, described[2], layout, rot_dim, tp, n_table, qp, ldq,
                                              _stream(stream))
     if status != GELO_OK:
         _check(ctx, status)
@@ -485,8 +490,8 @@ def gelo_attention(ctx, Q: torch.Tensor, O: torch.Tensor, n_q_heads: int, cache:
         raise GeloError(3, "Q, O and the cache differ in type")
     if shape[1] != n_q_heads * cache.head_dim or O.shape != shape:
         raise GeloError(2, f"Q and O must have {n_q_heads} heads of {cache.head_dim} values in a row")
-    _check_rows(batch, shape[0], cache)
-    status = load_library().gelo_attention(ctx, cache.dtype, n_q_heads, qp, ldq, cache.address, batch.address, scale, causal, op, ldo, _stream(stream))
+    described = _described(batch, shape[0], cache)
+    status = load_library().gelo_attention(ctx, cache.dtype, n_q_heads, qp, ldq, cache.address, described[2], scale, causal, op, ldo, _stream(stream))
     if status != GELO_OK:
         _check(ctx, status)
     return O

@@ -102,3 +102,28 @@ def test_the_workspace_that_is_reserved_is_enough_for_any_batch():
         assert size <= most(d), (hq, hkv, d, seqs, n_rows, rows)
         cut += size > 0
     assert cut > 1000
+
+
+def test_calls_of_other_rows_do_not_change_a_description_in_use(monkeypatch):
+    """Threads that share a batch: a call of 7 rows comes in while one of 5 rows is in the library."""
+    K, V = (on_gpu(torch.zeros((2, 1, 16, 64), dtype=torch.bfloat16)) for _ in range(2))
+    batch = g.SeqBatch(on_gpu(ints(1)), on_gpu(ints(1, 2)), 32, row_start=on_gpu(ints(2)), max_rows=7)
+    cache, seen = g.KvCache(K, V), []
+
+    def attention(rows):
+        Q, O = (on_gpu(torch.zeros((rows, 64), dtype=torch.bfloat16)) for _ in range(2))
+        g.gelo_attention(None, Q, O, 1, cache, batch, 1.0, stream=0)
+
+    class Library:
+        @staticmethod
+        def gelo_attention(*args):
+            described = g._SeqBatchStruct.from_address(args[6])
+            seen.append(described.n_rows)
+            if len(seen) == 1:
+                attention(7)
+            seen.append(described.n_rows)
+            return g.GELO_OK
+
+    monkeypatch.setattr(g, "load_library", Library)
+    attention(5)
+    assert seen == [5, 7, 7, 5]
