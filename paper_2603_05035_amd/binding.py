@@ -114,10 +114,13 @@ def _check(ctx, status: int):
         raise GeloError(status, (msg or b"").decode())
 
 
-_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+# not torch's public names: a build may lack them
+_raw_stream, _current_device = (getattr(torch._C, name, None) for name in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
 
 
 def _stream(stream):
+    if stream is None and (_raw_stream is None or _current_device is None):
+        stream = torch.cuda.current_stream()
     if stream is None:
         # the current stream's handle alone: torch.cuda.current_stream() makes an object around it, 2.7 us of a call's 9
         if not torch.cuda.is_initialized():

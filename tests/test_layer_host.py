@@ -1,6 +1,7 @@
 """The host's side of the operators between two projections: what the binding makes of tensors, and what the library reckons from
 sizes.  Nothing here launches a kernel or needs a GPU."""
 import ctypes
+import os
 import random
 import subprocess
 import sys
@@ -102,6 +103,23 @@ def test_the_workspace_that_is_reserved_is_enough_for_any_batch():
         assert size <= most(d), (hq, hkv, d, seqs, n_rows, rows)
         cut += size > 0
     assert cut > 1000
+
+
+@pytest.mark.parametrize("missing", ["_cuda_getCurrentRawStream", "_cuda_getDevice"])
+def test_a_torch_without_its_private_names(missing):
+    """The binding imports, and the current stream comes from torch's public call."""
+    code = f"""
+import torch
+if hasattr(torch._C, {missing!r}):
+    delattr(torch._C, {missing!r})
+from paper_2603_05035_amd import binding
+class Stream:
+    cuda_stream = 77
+torch.cuda.current_stream = Stream
+assert binding._stream(None).value == 77 and binding._stream(Stream()).value == 77 and binding._stream(5).value == 5
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=120, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert r.returncode == 0, r.stderr[-2000:]
 
 
 def test_calls_of_other_rows_do_not_change_a_description_in_use(monkeypatch):
