@@ -296,7 +296,7 @@ typedef enum { GELO_ROPE_HALF = 0, GELO_ROPE_PAIRS = 1 } gelo_rope_layout;
  *   R_out = h,   y = h / sqrt(mean_j h_j^2 + eps) * gamma,   H = y,   codes = e4m3(y * 448 / max_j |y_j|), scales = max_j |y_j| / 448.
  * X, R, R_out, H: n x d of type `dtype` (ldx, ldr, ldro, ldh); gamma: d values of it.  R_out may be NULL; H (or codes and
  * scales) may be NULL, not both.  H and R_out may be X or R; but for that no output shares memory with another matrix of the call.  Everything is computed in float from the unrounded h and rounded once.  codes: n x d bytes
- * (ldq, a multiple of 8), the row quantisation of gelo_project_fp8, scales: n floats (1 for a row of zeros): together the operand of
+ * (ldq, a multiple of 8), the row quantisation of gelo_project_fp8, scales: n floats (1 for a row of zeros, 2^-126 where the largest |y| is below 1.3e-36): together the operand of
  * gelo_project_fp8_codes, which wants ldq to be a multiple of 16.  A NaN or infinity in a row makes the row's y NaN or zero as the formula does; a NaN among them gives the
  * code 0x7F and the scale NaN.  d <= GELO_NORM_MAX_D, eps >= 0, n up to 2^22 (d > 8192: 2^21). */
 gelo_status gelo_rms_norm(gelo_ctx* ctx, gelo_dtype dtype, int n, int d, const void* X, int64_t ldx, const void* R, int64_t ldr,

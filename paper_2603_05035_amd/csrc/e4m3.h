@@ -24,4 +24,13 @@ __device__ __forceinline__ uint32_t e4m3_code(float t) {
     return sign | code;
 }
 
+// How values of up to `top` are scaled to codes: times 448 / top, and back by top / 448 (1 where there are only zeros).  From 1.3e-36 down the
+// first would be infinite; numbers of that size are scaled by 2^126, to at most 112.
+struct E4m3Scale { float back, times; };
+__device__ __forceinline__ E4m3Scale e4m3_scale(float top) {
+    if (top == 0.f) return {1.f, 1.f};
+    const float times = 448.0f / top;
+    return times == __builtin_inff() ? E4m3Scale{0x1p-126f, 0x1p126f} : E4m3Scale{top / 448.0f, times};
+}
+
 }  // namespace gelo

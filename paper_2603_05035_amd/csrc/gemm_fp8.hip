@@ -49,8 +49,8 @@ void quantize_rows_kernel(const uint16_t* X, int64_t ld, int cols, uint8_t* code
     if ((tid & 63) == 0) part[tid >> 6] = amax;
     __syncthreads();
     amax = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
-    const float inv = amax > 0.f ? 448.0f / amax : 1.0f;
-    if (tid == 0) scale[row] = amax > 0.f ? amax / 448.0f : 1.0f;
+    const float inv = e4m3_scale(amax).times;
+    if (tid == 0) scale[row] = e4m3_scale(amax).back;
     for (int c = tid * 8; c < cols; c += 256 * 8) {
         const u32x4_t v = *reinterpret_cast<const u32x4_t*>(xr + c);
         uint32_t lo = 0, hi = 0;
@@ -80,8 +80,8 @@ void quantize_weight_kernel(const uint16_t* W, int64_t ldw, int d, int p, uint8_
     part[g][c] = amax;
     __syncthreads();
     amax = fmaxf(fmaxf(part[0][c], part[1][c]), fmaxf(part[2][c], part[3][c]));
-    const float inv = amax > 0.f ? 448.0f / amax : 1.0f;
-    if (g == 0 && live) scale[col] = amax > 0.f ? amax / 448.0f : 1.0f;
+    const float inv = e4m3_scale(amax).times;
+    if (g == 0 && live) scale[col] = e4m3_scale(amax).back;
     for (int r0 = g * 16; r0 < d; r0 += 64) {                // d is a multiple of 128
         u32x4_t out;
 #pragma unroll

@@ -139,9 +139,9 @@ void rms_norm_kernel(NormArgs<T> a) {
     }
     if (!a.codes) return;
     top = over_row<TPR, true>(top, part[1]);
-    const float scale = top == 0.f ? 1.f : top / 448.0f, times = top == 0.f ? 1.f : 448.0f / top;
+    const E4m3Scale scale = e4m3_scale(top);
     if (!live) return;
-    if (t == 0) a.scales[row] = scale;
+    if (t == 0) a.scales[row] = scale.back;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
         const int v = t + i * TPR;
@@ -149,7 +149,7 @@ void rms_norm_kernel(NormArgs<T> a) {
         uint32_t w[2] = {0, 0};
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float q = h[i][e] * times;
+            const float q = h[i][e] * scale.times;
             w[e >> 2] |= (q != q ? 0x7Fu : e4m3_code(q)) << (8 * (e & 3));
         }
         *reinterpret_cast<u32x2_t*>(a.codes + row * a.ldq + 8 * v) = u32x2_t{w[0], w[1]};

@@ -224,3 +224,45 @@ def test_queries_and_results_that_share_memory(ctx, n, dtype):
     assert torch.equal(wide[:n, 3 * d:], before[:n, :d])
     g.gelo_rope_append(ctx, QKV, 1, cache, batch, Q=Q)
     assert torch.equal(wide[:n, :3 * d], before[:n, :3 * d])
+
+
+def grid_of(codes, scales, want):
+    """Codes times scales against numbers, as in the norm's test: half a step of the E4M3 grid, and 1e-6 of the grid's unit for numbers that float
+    holds as multiples of 2^-149."""
+    t = want / host(scales)[:, None]
+    within(codes.view(torch.float8_e4m3fn), t, np.maximum(2.0 ** -4 * np.abs(t), 2.0 ** -10) + 256 * U32 * np.abs(t) + 1e-6)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [512, 4096])
+def test_codes_of_rows_whose_largest_value_is_next_to_nothing(ctx, dtype, d):
+    """448 over it is beyond float from 1.3e-36 down.  Every third value is nought and stays it."""
+    size = torch.tensor([1e-37, 1e-38, 2e-39, 1e-39, 1e-40, 1e-41, 1.0], dtype=torch.float64)[:, None]
+    x = (size * torch.randn((7, d), generator=torch.Generator().manual_seed(d), dtype=torch.float64)).to(dtype).cuda()
+    x[:, ::3] = 0
+    gamma = torch.ones(d, dtype=dtype, device="cuda")
+    codes, scales = torch.empty((7, d), dtype=torch.uint8, device="cuda"), torch.empty(7, device="cuda")
+    g.gelo_rms_norm(ctx, x, gamma, 1e-5, codes=codes, scales=scales)
+    want = lo.rms_norm(host(x), host(gamma), 1e-5)[1]
+    assert torch.all(codes[:, ::3] & 0x7F == 0) and torch.all(scales > 0)
+    grid_of(codes, scales, want)
+    if dtype == BF16:
+        codes, scales = g.gelo_debug_quantize_rows_fp8(ctx, x)
+        assert torch.all(codes[:, ::3] & 0x7F == 0) and torch.all(scales > 0)
+        grid_of(codes, scales, host(x))
+
+
+def test_codes_of_weights_whose_largest_value_is_next_to_nothing(ctx):
+    """A column of the weight alike: its products are what they are with the column 2^100 times as large, over 2^100."""
+    d, p = 128, 16
+    U, W = rand((8, d), 3, BF16), rand((d, p), 4, BF16)
+    W[::3] = 0
+    Y, small = (torch.empty((8, p), dtype=BF16, device="cuda") for _ in range(2))
+    W[:, 5] *= 2.0 ** -124
+    g.gelo_project_fp8(ctx, U, g.gelo_prepare_weight_fp8(ctx, W), p, small)
+    W[:, 5] *= 2.0 ** 100
+    g.gelo_project_fp8(ctx, U, g.gelo_prepare_weight_fp8(ctx, W), p, Y)
+    rest = [c for c in range(p) if c != 5]
+    assert torch.equal(Y[:, rest], small[:, rest])
+    got, want = host(small[:, 5]), host(U) @ host(W[:, 5]) * 2.0 ** -100
+    assert np.linalg.norm(got - want) < 2 * 2.0 ** -4 * np.linalg.norm(want)
