@@ -6,10 +6,10 @@
 // one column, so maximum, sum and the rescaling stay in the lane, and the weights are at once the operand of O^T = V^T P^T: the matrix
 // instruction sums over keys in any order, as long as both operands agree on it.
 //
-// Scores, weights, maximum, sum and weighted sum are float.  Where the values are bfloat16 the weights, at most 1 (2^8.5 in the kernel for prompts),
-// are rounded to it for the second product, whose other operand has no more bits, and their sum is that of the rounded ones: a row that sees one key
-// is then that key's value, and rounding moves the others by no more than the values' distance from their mean (15 sequences of 1 to 3 keys, 48/2
-// heads of 64: 0.0019 of the result's norm off with the sum of the unrounded ones).
+// Scores, weights, maximum, sum and weighted sum are float.  Where the values are bfloat16 the second product takes bfloat16 weights.  With few columns
+// the matrix pipes have time to spare and a weight is two of them, 16 bits: results are as near as their own rounding.  In the kernel for prompts, which the
+// matrix pipes bound, weights (at most 2^8.5) are rounded to one, and their sum is that of the rounded ones: a row that sees one key is then that
+// key's value, and rounding moves the others by no more than the values' distance from their mean.
 //
 // attention_few_kernel: single tokens and a few rows, and float where its prompts do not fill the chip.  Bound by the cache's bytes: every one is read once by one wave, and a
 // CU has about 130 KB of them on their way.  K and V go from memory to registers with nothing between, as the matrix instructions want them (15
@@ -87,12 +87,22 @@ struct Few<uint16_t, D, PAST> {
     static constexpr int TILES = D < 256 ? 2 : 1, KEYS = 16 * TILES, SLOTS = 4 * TILES;
     static constexpr int KS = D / 32, VD = D / 16, VW = VD / 2;        // VW: 32-bit words of VD values
     typedef uint32_t frag_t __attribute__((ext_vector_type(2 * TILES)));       // SLOTS weights or values
-    bf16x8_t q[KS];
+    // Of heads of 256 the last pieces of Q lie in LDS: with all of them in registers some would be kept in memory, and a wait for those is one for
+    // the keys and values on their way.
+    static constexpr int APART = D < 256 ? 0 : 2;
+    bf16x8_t q[KS - APART];
+    bf16x8_t* q_apart;                                       // this lane's: 64 lanes to a piece
     bf16x8_t k[TILES][KS];
     uint32_t v[SLOTS][VW];
-    __device__ __forceinline__ void load_q(const uint16_t* p, int g) {
+    // lds: the wave's own, 1 KB to a piece
+    __device__ __forceinline__ void load_q(const uint16_t* p, int g, float* lds) {
+        q_apart = reinterpret_cast<bf16x8_t*>(lds) + (threadIdx.x & 63);
 #pragma unroll
-        for (int s = 0; s < KS; ++s) q[s] = *reinterpret_cast<const bf16x8_t*>(p + 32 * s + 8 * g);
+        for (int s = 0; s < KS; ++s) {
+            const bf16x8_t x = *reinterpret_cast<const bf16x8_t*>(p + 32 * s + 8 * g);
+            if (s < KS - APART) q[s] = x;
+            else q_apart[64 * (s - (KS - APART))] = x;
+        }
     }
     __device__ __forceinline__ void load_k(int t, const uint16_t* row, int g) {
 #pragma unroll
@@ -119,7 +129,12 @@ struct Few<uint16_t, D, PAST> {
     __device__ __forceinline__ f32x4_t scores(int t) const {
         f32x4_t s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < KS; ++i) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[t][i], q[i], s, 0, 0, 0);
+        for (int i = 0; i < KS - APART; ++i) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[t][i], q[i], s, 0, 0, 0);
+        if constexpr (APART > 0) {
+            asm volatile("" ::: "memory");                   // read here, not kept
+#pragma unroll
+            for (int i = KS - APART; i < KS; ++i) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[t][i], q_apart[64 * (i - (KS - APART))], s, 0, 0, 0);
+        }
         return s;
     }
     // operand of O^T for component j of the lane's VD: half j % 2 of word j / 2 of the slots
@@ -130,26 +145,33 @@ struct Few<uint16_t, D, PAST> {
             f[i] = __builtin_amdgcn_perm(v[2 * i + 1][j >> 1], v[2 * i][j >> 1], (j & 1) ? 0x07060302u : 0x05040100u);
         return f;
     }
-    static __device__ __forceinline__ frag_t weights(const float (&p)[SLOTS]) {
+    // A weight is the sum of two bfloat16: its upper half as it stands and what is left of it.  Neither is nought or negative where the weight is
+    // not nought: an infinite value times both is that infinity.
+    struct weights_t { frag_t high, low; };
+    static __device__ __forceinline__ weights_t weights(const float (&p)[SLOTS]) {
         typedef __bf16 pack_t __attribute__((ext_vector_type(SLOTS)));
-        pack_t o;
+        frag_t high;
+        pack_t low;
 #pragma unroll
-        for (int i = 0; i < SLOTS; ++i) o[i] = (__bf16)p[i];
-        return __builtin_bit_cast(frag_t, o);
+        for (int i = 0; i < 2 * TILES; ++i) high[i] = __builtin_amdgcn_perm(__float_as_uint(p[2 * i + 1]), __float_as_uint(p[2 * i]), 0x07060302u);
+#pragma unroll
+        for (int i = 0; i < SLOTS; ++i) {
+            const float up = __uint_as_float(__float_as_uint(p[i]) & 0xFFFF0000u);
+            low[i] = (__bf16)fmaxf(p[i] - up, fminf(up, 0x1p-120f));
+        }
+        return {high, __builtin_bit_cast(frag_t, low)};
     }
     static __device__ __forceinline__ f32x4_t product(frag_t values, frag_t weights, f32x4_t sum) {
         typedef short s16x4_t __attribute__((ext_vector_type(4)));
         if constexpr (TILES == 2) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, values), __builtin_bit_cast(bf16x8_t, weights), sum, 0, 0, 0);
         else return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4_t, values), __builtin_bit_cast(s16x4_t, weights), sum, 0, 0, 0);
     }
-    static __device__ __forceinline__ float sum_of(frag_t w, float sum) {
+    __device__ __forceinline__ void accumulate(f32x4_t (&acc)[VD], weights_t w) const {
 #pragma unroll
-        for (int i = 0; i < 2 * TILES; ++i) sum = add_pair(w[i], sum);
-        return sum;
-    }
-    __device__ __forceinline__ void accumulate(f32x4_t (&acc)[VD], frag_t w) const {
-#pragma unroll
-        for (int j = 0; j < VD; ++j) acc[j] = product(v_frag(j), w, acc[j]);
+        for (int j = 0; j < VD; ++j) {
+            const frag_t f = v_frag(j);
+            acc[j] = product(f, w.low, product(f, w.high, acc[j]));
+        }
     }
     __device__ __forceinline__ bool odd_values() const {       // a NaN or an infinity among the values
         bool odd = false;
@@ -161,11 +183,11 @@ struct Few<uint16_t, D, PAST> {
     }
     // as accumulate, where some keys are hidden from some columns (seen: bit per slot) and some values are not finite: 0 times those would be
     // NaN in columns that do not see them.  The finite part is summed as ever; how many +inf (-inf, NaN: both) a column sees is counted by two more products.
-    __device__ __forceinline__ void accumulate_odd(f32x4_t (&acc)[VD], frag_t w, uint32_t seen) const {
+    __device__ __forceinline__ void accumulate_odd(f32x4_t (&acc)[VD], weights_t w, uint32_t seen) const {
         float one[SLOTS];
 #pragma unroll
         for (int i = 0; i < SLOTS; ++i) one[i] = (seen >> i) & 1 ? 1.f : 0.f;
-        const frag_t sees = weights(one);
+        const frag_t sees = weights(one).high;
         for (int j = 0; j < VD; ++j) {
             frag_t f = frag_t(0u), fin = f, up = f, down = f;
 #pragma unroll
@@ -184,12 +206,13 @@ struct Few<uint16_t, D, PAST> {
             f32x4_t sum = zero;
 #pragma unroll
             for (int jj = 0; jj < VD; ++jj) if (jj == j) sum = acc[jj];
-            sum = product(fin, w, sum);
+            sum = product(fin, w.low, product(fin, w.high, sum));
             const f32x4_t ups = product(up, sees, zero), downs = product(down, sees, zero);
 #pragma unroll
             for (int r = 0; r < 4; ++r) sum[r] += (ups[r] > 0.f ? __builtin_inff() : 0.f) - (downs[r] > 0.f ? __builtin_inff() : 0.f);
 #pragma unroll
             for (int jj = 0; jj < VD; ++jj) if (jj == j) acc[jj] = sum;
+            __builtin_amdgcn_sched_barrier(0);               // one component after another: together their masks take registers that the loop needs
         }
     }
 };
@@ -201,7 +224,7 @@ struct Few<float, D, PAST> {
     static constexpr int KEYS = 16, TILES = 1, KS = D / 16, VD = D / 16;
     f32x4_t q[KS], k[1][KS];
     float v[4][VD];
-    __device__ __forceinline__ void load_q(const float* p, int g) {
+    __device__ __forceinline__ void load_q(const float* p, int g, float*) {
 #pragma unroll
         for (int s = 0; s < KS; ++s) q[s] = *reinterpret_cast<const f32x4_t*>(p + 16 * s + 4 * g);
     }
@@ -235,12 +258,8 @@ struct Few<float, D, PAST> {
         return s;
     }
     typedef f32x4_t frag_t;
-    static __device__ __forceinline__ frag_t weights(const float (&p)[4]) { return f32x4_t{p[0], p[1], p[2], p[3]}; }
-    static __device__ __forceinline__ float sum_of(frag_t w, float sum) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) sum += w[r];
-        return sum;
-    }
+    typedef frag_t weights_t;
+    static __device__ __forceinline__ weights_t weights(const float (&p)[4]) { return f32x4_t{p[0], p[1], p[2], p[3]}; }
     __device__ __forceinline__ void accumulate(f32x4_t (&acc)[VD], frag_t p) const {
 #pragma unroll
         for (int j = 0; j < VD; ++j)
@@ -369,8 +388,10 @@ __device__ __forceinline__ void walk_keys(const AttnArgs& a, int seq, int kvh, i
         m = m_new;
 #pragma unroll
         for (int r = 0; r < SLOTS; ++r) s[r] = __builtin_amdgcn_exp2f(s[r] - m_safe);
-        const typename F::frag_t w = F::weights(s);
-        l = F::sum_of(w, l * alpha);
+        const typename F::weights_t w = F::weights(s);
+        l *= alpha;
+#pragma unroll
+        for (int r = 0; r < SLOTS; ++r) l += s[r];
         if (__ballot(alpha != 1.f)) {
 #pragma unroll
             for (int j = 0; j < VD; ++j)
@@ -390,7 +411,7 @@ __global__ __launch_bounds__(64 * kFewWaves, sizeof(T) == 2 || D < 256 ? 2 : 1)
 void attention_few_kernel(AttnArgs a) {
     typedef Few<T, D, PAST> F;
     constexpr int VD = F::VD;
-    __shared__ float joined_o[kFewWaves][16][D + 4];
+    __shared__ __attribute__((aligned(16))) float joined_o[kFewWaves][16][D + 4];
     __shared__ float joined_ml[kFewWaves][16][2];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int tile = a.n_chunks == 1 ? blockIdx.x : blockIdx.x / a.n_chunks, chunk = blockIdx.x - tile * a.n_chunks;
@@ -415,7 +436,7 @@ void attention_few_kernel(AttnArgs a) {
     if (begin >= end && a.n_chunks > 1) return;              // the join does not look at it
 
     F f;
-    f.load_q((const T*)a.Q + row * a.ldq + (int64_t)head * D, g);
+    f.load_q((const T*)a.Q + row * a.ldq + (int64_t)head * D, g, &joined_o[wave][0][0]);
     f32x4_t acc[VD];
 #pragma unroll
     for (int j = 0; j < VD; ++j) acc[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -503,7 +524,7 @@ void attention_float_kernel(AttnArgs a) {
     const int limit = limit_of(col);
     const int most = awake ? min(__builtin_amdgcn_readlane(limit, 15), last) : -1, least = __builtin_amdgcn_readfirstlane(limit);
     F f;
-    f.load_q((const float*)a.Q + row * a.ldq + (int64_t)head * D, g);
+    f.load_q((const float*)a.Q + row * a.ldq + (int64_t)head * D, g, nullptr);
     f32x4_t acc[VD];
 #pragma unroll
     for (int j = 0; j < VD; ++j) acc[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -586,7 +607,8 @@ void attention_float_kernel(AttnArgs a) {
                 f32x4_t w;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) w[r] = __builtin_amdgcn_exp2f(s[4 * t + r] - m_safe);
-                l = F::sum_of(w, l);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) l += w[r];
                 if (partly && __ballot(f.odd_values())) f.accumulate_odd(acc, w, seen >> (4 * t));
                 else f.accumulate(acc, w);
             }

@@ -266,3 +266,26 @@ def test_codes_of_weights_whose_largest_value_is_next_to_nothing(ctx):
     assert torch.equal(Y[:, rest], small[:, rest])
     got, want = host(small[:, 5]), host(U) @ host(W[:, 5]) * 2.0 ** -100
     assert np.linalg.norm(got - want) < 2 * 2.0 ** -4 * np.linalg.norm(want)
+
+
+WHOLE_WEIGHTS = [  # new, kv, q heads, kv heads, d, way
+    ([1] * 5, [200, 3, 77, 130, 256], 4, 2, 64, 0), ([1] * 3, [2100, 900, 17], 8, 8, 96, 4), ([1] * 2, [513, 1030], 48, 2, 128, 4),
+    ([1] * 3, [77, 250, 129], 16, 2, 256, 0), ([3, 20, 11], [70, 200, 256], 3, 3, 128, 0), ([2], [1500], 8, 1, 256, 4),
+]
+
+
+@pytest.mark.parametrize("new,kv,hq,hkv,d,want", WHOLE_WEIGHTS)
+def test_few_columns_keep_their_weights(ctx, new, kv, hq, hkv, d, want):
+    """bfloat16 with few columns: a weight is the sum of two bfloat16, off by half a unit of the second, at most 2^-7 of the first: 2^-16 of the
+    weight.  With it the float bounds of the other tests and one rounding of the result, for which nothing is allowed but U16 of itself: values that
+    cancel in the sum must not be moved by what rounding the weights to 8 bits would move them."""
+    page = 16
+    batch, table, row_start, n_pages = make_batch(new, kv, page, 3)
+    K, V = make_cache(n_pages, hkv, page, d, BF16, "head", seed=5)
+    Q = rand((int(row_start[-1]), hq * d), 8, BF16)
+    O = torch.full_like(Q, 7.0)
+    assert way(ctx, Q, new, kv, hq, hkv, d, True) == want
+    g.gelo_attention(ctx, Q, O, hq, g.KvCache(K, V), batch, d ** -0.5)
+    ref, absolute = lo.attention(host(Q), host(K), host(V), hq, row_start, kv, table, d ** -0.5, True)
+    bound = attention_bound(ref, absolute, host(Q), host(K), d ** -0.5, max(kv), d, F32) + 2.0 ** -16 * absolute + 1.01 * U16 * np.abs(ref)
+    within(O, ref, bound)
