@@ -289,3 +289,74 @@ def test_few_columns_keep_their_weights(ctx, new, kv, hq, hkv, d, want):
     ref, absolute = lo.attention(host(Q), host(K), host(V), hq, row_start, kv, table, d ** -0.5, True)
     bound = attention_bound(ref, absolute, host(Q), host(K), d ** -0.5, max(kv), d, F32) + 2.0 ** -16 * absolute + 1.01 * U16 * np.abs(ref)
     within(O, ref, bound)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,d", [(1, 2056), (3, 4096), (65, 4088), (65, 4096), (7, 3000)])
+def test_norm_without_codes(ctx, n, d, dtype):
+    """The widths at which a row has more threads where no codes are asked for.  Bounds as in test_norm."""
+    x, r, gamma = rand((n, d), d, dtype, 3.0), rand((n, d), d + 1, dtype), rand((d,), d + 2, dtype)
+    u = U16 if dtype == BF16 else 0.0
+    for residual in (None, r):
+        for keep in (False, True):
+            H, H_all = base.padded(n, d, d + 8, dtype)
+            R, R_all = base.padded(n, d, d + 16, dtype)
+            g.gelo_rms_norm(ctx, x, gamma, 1e-5, H=H, residual=residual, residual_out=R if keep else None)
+            h, y = lo.rms_norm(host(x), host(gamma), 1e-5, None if residual is None else host(residual))
+            within(H, y, (64 * U32 + u) * np.abs(y) * 1.01 + 1e-38, "H")
+            assert torch.all(H_all[:, d:] == 7) and torch.all(R_all[:, d if keep else 0:] == 7)
+            if keep:
+                within(R, h, (U32 + u) * np.abs(h) * 1.01, "residual")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [512, 2048, 4096, 8192, 16384, 65536])
+def test_norms_whose_results_are_stored_past_the_caches(ctx, d, dtype):
+    """More than 40 MB of results, for every number of threads to a row; in float64 on the GPU, bounds as in test_norm."""
+    size = 2 if dtype == BF16 else 4
+    n = 21_000_000 // (d * size) + 3
+    gen = torch.Generator(device="cuda").manual_seed(d)
+    x, r = ((3 * torch.randn((n, d), generator=gen, device="cuda")).to(dtype) for _ in range(2))
+    gamma = torch.randn(d, generator=gen, device="cuda").to(dtype)
+    H, R = (torch.full((n, d + 8), 7.0, dtype=dtype, device="cuda") for _ in range(2))
+    assert 2 * n * d * size > 40e6
+    g.gelo_rms_norm(ctx, x, gamma, 1e-5, H=H[:, :d], residual=r, residual_out=R[:, :d])
+    h = x.double() + r.double()
+    y = h / (h.pow(2).mean(-1, keepdim=True) + 1e-5).sqrt() * gamma.double()
+    u = U16 if dtype == BF16 else 0.0
+    assert torch.all((R[:, :d].double() - h).abs() <= (U32 + u) * 1.01 * h.abs())
+    assert torch.all((H[:, :d].double() - y).abs() <= (64 * U32 + u) * 1.01 * y.abs() + 1e-38)
+    assert torch.all(H[:, d:] == 7) and torch.all(R[:, d:] == 7)
+
+
+LARGE_CACHES = [  # dtype, sequences, kv (fewest, most), q heads, kv heads, d, page
+    (BF16, 64, (350, 512), 16, 8, 128, 16), (BF16, 64, (100, 128), 32, 32, 128, 64), (BF16, 64, (40, 64), 64, 32, 256, 16), (BF16, 32, (300, 512), 16, 8, 256, 32),
+    (BF16, 64, (200, 256), 32, 32, 64, 32), (F32, 64, (40, 64), 32, 32, 128, 16), (F32, 64, (30, 64), 32, 32, 256, 16), (BF16, 3, (20000, 32767), 32, 8, 128, 64),
+]
+
+
+@pytest.mark.parametrize("order", ["head", "row"])
+@pytest.mark.parametrize("dtype,n_seqs,lengths,hq,hkv,d,page", LARGE_CACHES)
+def test_single_tokens_against_caches_that_are_read_past_the_caches(ctx, dtype, n_seqs, lengths, hq, hkv, d, page, order):
+    """More than 100 MB of keys and values; where the heads of a row lie side by side and are 2048 and more in all, a wave has a head.  The
+    reference in float64 on the GPU, for every sequence and three of the heads."""
+    rng = np.random.default_rng(d)
+    kv = [lengths[1]] + [int(x) for x in rng.integers(lengths[0], lengths[1] + 1, n_seqs - 1)]
+    batch, table, row_start, n_pages = make_batch([1] * n_seqs, kv, page, 3, one_row=True)
+    gen = torch.Generator(device="cuda").manual_seed(d)
+    shape = (n_pages, hkv, page, d) if order == "head" else (n_pages, page, hkv, d)
+    K, V = (torch.randn(shape, generator=gen, device="cuda", dtype=torch.float32).to(dtype) for _ in range(2))
+    if order == "row":
+        K, V = K.permute(0, 2, 1, 3), V.permute(0, 2, 1, 3)
+    assert 2 * K.element_size() * n_seqs * hkv * max(kv) * d > 100e6
+    Q, O = rand((n_seqs, hq * d), 8, dtype), torch.full((n_seqs, hq * d), 7.0, dtype=dtype, device="cuda")
+    g.gelo_attention(ctx, Q, O, hq, g.KvCache(K, V), batch, d ** -0.5)
+    assert torch.isfinite(O.float()).all()
+    for s in range(n_seqs):
+        used = torch.from_numpy(table[s, :(kv[s] + page - 1) // page]).long().cuda()
+        for h in {0, (7 * s + 5) % hq, hq - 1}:
+            k, v = (x[used, h * hkv // hq].reshape(-1, d)[:kv[s]].double() for x in (K, V))
+            q = Q[s:s + 1, h * d:(h + 1) * d].double()
+            w = torch.softmax(q @ k.T * d ** -0.5, -1)
+            ref, absolute = host(w @ v), host(w @ v.abs())
+            within(O[s:s + 1, h * d:(h + 1) * d], ref, attention_bound(ref, absolute, host(q), host(k), d ** -0.5, kv[s], d, dtype), (s, h))
