@@ -360,3 +360,11 @@ def test_single_tokens_against_caches_that_are_read_past_the_caches(ctx, dtype, 
             w = torch.softmax(q @ k.T * d ** -0.5, -1)
             ref, absolute = host(w @ v), host(w @ v.abs())
             within(O[s:s + 1, h * d:(h + 1) * d], ref, attention_bound(ref, absolute, host(q), host(k), d ** -0.5, kv[s], d, dtype), (s, h))
+
+
+@pytest.mark.parametrize("new,kv,hq,d,want", [([60] * 34 + [3], [60] * 34 + [0], 16, 128, 1), ([60] * 34 + [3], [60] * 34 + [0], 16, 96, 1),
+                                              ([200, 65, 4], [1000, 513, 0], 16, 96, 5), ([200, 65, 4], [1000, 513, 0], 16, 128, 5)])
+def test_float_by_tiles_of_64_columns_and_a_row_without_a_softmax(ctx, new, kv, hq, d, want):
+    """Float has two kernels: the one for tiles of 64 columns, the cache whole and cut."""
+    assert float_way(new, kv, hq, hq, d, True) == want
+    base.test_a_row_that_sees_only_scores_of_minus_infinity_has_no_softmax(ctx, F32, new, kv, hq, d, None)

@@ -145,3 +145,14 @@ def test_calls_of_other_rows_do_not_change_a_description_in_use(monkeypatch):
     monkeypatch.setattr(g, "load_library", Library)
     attention(5)
     assert seen == [5, 7, 7, 5]
+
+
+def test_which_way_float_attention_goes():
+    """attention_way tells the kernels of bfloat16 apart (float is 0 or cut there, whichever kernel takes it); which one takes float is
+    attention_float_way's to say: 1 by tiles of 64 columns, 0 by 16, plus 4 where the cache is cut.  Measured, us, 16 columns and 64: 8 x 512 rows of 32 heads
+    of 128 478 and 291, 2 x 512 on 2000 of 8 heads 99 and 93, 1 x 2000 of 8 heads 148 and 162."""
+    for want, args in ((1, (1, 32, 32, 128, 8, 4096, 512, 512)), (5, (1, 8, 8, 128, 2, 1024, 512, 2000)), (0, (1, 8, 8, 128, 1, 2000, 2000, 2000)),
+                       (0, (1, 32, 32, 64, 8, 4096, 512, 512)), (0, (1, 32, 32, 256, 8, 4096, 512, 512)), (4, (1, 32, 8, 128, 3, 3, 1, 32768)),
+                       (0, (1, 32, 32, 128, 64, 64, 1, 4096))):
+        assert reckoned(FLOAT_WAY, *args) == want, args
+        assert reckoned(WAY, 0, *args) == want & 4, args
