@@ -43,22 +43,23 @@ def build(verbose: bool = False) -> str:
 def build_sanitized(verbose: bool = False) -> str:
     """Host-side sanitizer target: api.hip's HOST code (argument checks, context and mixing-object life cycle)
     compiled with AddressSanitizer + UndefinedBehaviorSanitizer, linked with the other, uninstrumented objects of
-    `build()` into libgelo_hostsan.so, plus the driver tests/host_sanitize/lifecycle.cpp -> lifecycle_hostsan (both beside libgelo.so).
+    `build()` into libgelo_hostsan.so, plus the drivers of tests/host_sanitize/, lifecycle.cpp -> lifecycle_hostsan and layer.cpp ->
+    layer_hostsan (all beside libgelo.so).
     The GPU code is not instrumented.  Call build() first."""
     obj_dir = os.path.join(HERE, "_build")
     root = os.path.dirname(HERE)
     san = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined", "-Xarch_host", "-fno-omit-frame-pointer", "-g"]
     api_obj = os.path.join(obj_dir, "api_hostsan.o")
     lib = os.path.join(HERE, "libgelo_hostsan.so")           # beside libgelo.so, where the host-side tests look for it
-    exe = os.path.join(HERE, "lifecycle_hostsan")
+    exes = [os.path.join(HERE, f"{name}_hostsan") for name in ("lifecycle", "layer")]
     cmds = [
         [HIPCC, *FLAGS, *san, "-c", os.path.join(CSRC, "api.hip"), "-o", api_obj],
         [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-fsanitize=address", "-fsanitize=undefined", "-fno-gpu-sanitize", api_obj,
          *[os.path.join(obj_dir, src.replace(".hip", ".o")) for src in SOURCES if src != "api.hip"], "-o", lib],
-        [HIPCC, "-x", "c++", "-std=c++17", "-O1", "-g", "-fsanitize=address", "-fsanitize=undefined", "-fno-gpu-sanitize", "-fno-omit-frame-pointer",
-         "-I", os.path.join(root, "include"), "-I", "/opt/rocm/include", "-D__HIP_PLATFORM_AMD__",
-         os.path.join(root, "tests", "host_sanitize", "lifecycle.cpp"), "-L", HERE, "-lgelo_hostsan", "-L", "/opt/rocm/lib", "-lamdhip64",
-         "-Wl,-rpath,$ORIGIN", "-Wl,-rpath,/opt/rocm/lib", "-o", exe],
+        *[[HIPCC, "-x", "c++", "-std=c++17", "-O1", "-g", "-fsanitize=address", "-fsanitize=undefined", "-fno-gpu-sanitize", "-fno-omit-frame-pointer",
+           "-I", os.path.join(root, "include"), "-I", "/opt/rocm/include", "-D__HIP_PLATFORM_AMD__",
+           os.path.join(root, "tests", "host_sanitize", os.path.basename(exe).replace("_hostsan", ".cpp")), "-L", HERE, "-lgelo_hostsan",
+           "-L", "/opt/rocm/lib", "-lamdhip64", "-Wl,-rpath,$ORIGIN", "-Wl,-rpath,/opt/rocm/lib", "-o", exe] for exe in exes],
     ]
     for cmd in cmds:
         proc = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
@@ -67,7 +68,7 @@ def build_sanitized(verbose: bool = False) -> str:
             sys.stderr.write(out + "\n")
         if proc.returncode != 0:
             raise RuntimeError("hipcc failed (host sanitizer target)")
-    return exe
+    return exes[0]
 
 
 if __name__ == "__main__":
