@@ -265,6 +265,7 @@ gelo_status gelo_qkv_forward_static(gelo_ctx* ctx, gelo_kind kind, gelo_dtype dt
  * gelo_kv_cache: K and V are arrays of n_pages pages; row r of head h of page g starts at element
  * g page_stride + h head_stride + r row_stride of either (the same strides for both, multiples of 8, row_stride at
  * most 2^24, head_dim contiguous values at each).  page_rows is a power of two from 16 on.  k and v are 16-byte aligned DEVICE pointers.
+ * (gelo_rope_append fills caches of any head_dim that is a multiple of 8, gelo_attention reads those of 64, 96, 128 and 256.)
  * gelo_seq_batch: sequence s brings the rows [row_start[s], row_start[s + 1]) of the batch and has kv_len[s] rows in the
  * cache; row p of it lies in page page_table[s table_ld + p / page_rows], row p % page_rows.  row_start
  * (n_seqs + 1 ascending values from 0 to n_rows) may be NULL if every sequence brings one row (n_rows = n_seqs,

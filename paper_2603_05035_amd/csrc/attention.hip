@@ -14,9 +14,10 @@
 // attention_few_kernel: single tokens and a few rows, and float where its prompts do not fill the chip.  Bound by the cache's bytes: every one is read once by one wave, and a
 // CU has about 130 KB of them on their way.  K and V go from memory to registers with nothing between, as the matrix instructions want them (15
 // of 16 columns are idle where a key head has one query: the matrix pipes have that to spare); four waves of a workgroup walk different keys and join at
-// the end.  A single token of each of 64 sequences, 32 heads of 128, bfloat16: 3500 to 4095 rows 624 us (6.3 TB/s of those there are), 400 to 639 rows 92
-// (6.0), 3 sequences of 20000 to 32767 rows of 8 heads 64 and 4.3 for the join (5.8 without it).  Three sequences of up to 200 rows 7.7: trips to memory
-// one after another - lengths, page numbers, keys.
+// the end.  A single token of each of 64 sequences, 32 heads of 128, bfloat16: 3500 to 4095 rows 626 us (6.3 TB/s of those there are), 400 to 639 rows 93
+// (5.9; 92 with weights of 8 bits), 3 sequences of 20000 to 32767 rows of 8 heads 64 and 4.3 for the join (5.8 without it).  In float 1297 (6.1), 200 (5.5) and
+// 145 (5.2); of heads of 256, whose 416 registers leave one wave to a SIMD and half the bytes on their way, 64 x 2048 keys of 8 heads 465 (4.6).  Three
+// sequences of up to 200 rows 7.7: trips to memory one after another - lengths, page numbers, keys.
 #include "gelo_internal.h"
 #include "paged.h"
 
@@ -641,7 +642,7 @@ void attention_float_kernel(AttnArgs a) {
 // weighted sum of the last one (matrix pipe) beside the weights of the present one (vector pipe).
 // 6000 rows behind 2000, 32/8 heads of 128: 472 us on one chip, 477 to 490 on others = 1.00 to 1.04 PFLOP/s, at 1.83 GHz under the power limit; a library's product
 // of 8192^3 reaches 1.24.  Of 507 us (an earlier step) the fetches were 73, maximum and masks 114, the reads of LDS 159, each taken out alone.
-// 8 prompts of 301 to 512 rows, 32 heads of 128: 40 to 43 us = 0.26 PFLOP/s of what causal rows see: 12 us for one row of keys, and tiles that end early.
+// 8 prompts of 301 to 512 rows, 32 heads of 128: 38 to 43 us = 0.26 PFLOP/s of what causal rows see: 12 us for one row of keys, and tiles that end early.
 constexpr int kPromptWaves = 4;
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
@@ -1228,8 +1229,9 @@ Plan plan_prompt(const Attention& o, int64_t columns, double* us) {
 // Float: tiles of 64 columns pay where they fill the chip, or where they are long ones (every row sees half of the keys at least) and it takes a cut or two.
 // 16 columns to a workgroup and 64, us: heads of 128, 8 x 512 rows 478 and 291 (2048 tiles), 64 x 48 on 200 61 and 50 (512), 16 x 24 on 500, 32/8 heads, 72
 // and 55 (256), 4 x 200 on 1000, all seen, 109 and 93 (256), 2 x 512 on 2000 99 and 93 (128); 1 x 2000 148 and 162 (256), 32 x 64 on 300 56 and 61
-// (256), 1 x 32 on 4096 20 and 33; of 96, 16 x 33 on 1000, 28/4 heads, 92 and 76 (256), 4 x 378 24 and 43 (192).  Of 64, where four of the small ones fit a CU, 8 x
-// 200 37 and 41, of 256, where one of either does, 8 x 300 on 600 386 and 440: never.
+// (256), 1 x 32 on 4096 20 and 33; of 96, 16 x 33 on 1000, 28/4 heads, 92 and 76 (256), 4 x 378 24 and 43 (192).  Heads of 64, where four of the small ones fit a
+// CU, and of 256, where one of either does, stay with 16 columns: of 64 one size was timed, 8 x 200 37 and 41, of 256 8 x 300 on 600 386 and 440 but 4 x 378
+// on 600 446 and 365, and no count that tells such calls apart.
 bool float_shares(const Attention& o, int64_t columns) {
     const int64_t tiles = (int64_t)o.batch.n_seqs * o.cache.n_kv_heads * ((columns + 16 * kFloatWaves - 1) / (16 * kFloatWaves));
     const bool lengthy = !o.causal || o.batch.max_kv_len >= 2 * (int64_t)o.batch.max_rows;

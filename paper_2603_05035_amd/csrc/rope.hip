@@ -2,7 +2,8 @@
 // queries go to a matrix, keys and values to the row's place in the cache.  Bytes bound: every value is read once and written once.
 // A pair (a, b) of components i becomes (a cos - b sin, b cos + a sin), in float, rounded once; angles are worked out in double when the table is
 // filled, since a float of position times frequency would be off by 0.004 at position 65536.  8 prompts of 301 to 512 rows, 32/8 heads of 128,
-// bfloat16: 14.1 to 15.9 us = 4.9 to 5.5 TB/s, a large copy's rate; one row of each of 64 sequences 4.8, called from Python 6.4.
+// bfloat16: 14.1 to 15.9 us = 4.9 to 5.5 TB/s, float 32.9 (4.7; an elementwise kernel over 1 GiB reads and writes at 6.2); one row of each of 64 sequences
+// 4.8, called from Python 6.3, float 7.8.
 // Stores past the caches: 8 x 512 rows of 32/32 heads 37.8 us instead of 42.8, but with the attention behind them 88.5 instead of 83.8.
 #include "gelo_internal.h"
 #include "paged.h"
