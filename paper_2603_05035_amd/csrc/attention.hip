@@ -1157,7 +1157,7 @@ constexpr int kPromptTarget = 512, kPromptLeast = 128;
 // The cache cut `cuts` times, rounded to whole steps of both kernels.
 void cut(Plan* p, int max_kv_len, int64_t cuts) {
     p->chunk = (int)round_up((max_kv_len + cuts - 1) / cuts, 128);
-    p->n_chunks = (max_kv_len + p->chunk - 1) / p->chunk;
+    p->n_chunks = (int)(((int64_t)max_kv_len + p->chunk - 1) / p->chunk);
 }
 // The join: a launch behind another one, and the parts written and read.
 double join_us(const Attention& o, const Plan& p) {

@@ -368,3 +368,22 @@ def test_float_by_tiles_of_64_columns_and_a_row_without_a_softmax(ctx, new, kv, 
     """Float has two kernels: the one for tiles of 64 columns, the cache whole and cut."""
     assert float_way(new, kv, hq, hq, d, True) == want
     base.test_a_row_that_sees_only_scores_of_minus_infinity_has_no_softmax(ctx, F32, new, kv, hq, d, None)
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 64), (BF16, 128), (F32, 96)])
+@pytest.mark.parametrize("n_seqs,rows", [(1, 1), (2, 40), (40, 20)])
+def test_a_bound_of_lengths_near_2_to_the_31(ctx, dtype, d, n_seqs, rows):
+    """A captured launch may be sized for any length; pages of 65536 rows keep the table short."""
+    hq, page, most = 16, 65536, 2 ** 31 - 65537
+    K, V = make_cache(2, hq, page, d, dtype, "row", seed=3)
+    table = torch.zeros((n_seqs, 32768), dtype=torch.int32, device="cuda")
+    table[:, 0] = 1
+    kv = torch.arange(200, 200 + n_seqs, dtype=torch.int32, device="cuda")
+    starts = torch.arange(n_seqs + 1, dtype=torch.int32, device="cuda") * rows
+    Q = rand((n_seqs * rows, hq * d), 9, dtype)
+    O = torch.full_like(Q, 7.0)
+    g.gelo_attention(ctx, Q, O, hq, g.KvCache(K, V), g.SeqBatch(kv, table, most, row_start=starts, max_rows=rows), d ** -0.5)
+    for h in (0, hq - 1):
+        at = slice(h * d, (h + 1) * d)
+        ref, absolute = lo.attention(host(Q[:, at]), host(K[:, h:h + 1, :256]), host(V[:, h:h + 1, :256]), 1, starts.tolist(), kv.tolist(), table.cpu().numpy(), d ** -0.5, True)
+        within(O[:, at], ref, attention_bound(ref, absolute, host(Q), host(K[:, :, :256]), d ** -0.5, 256, d, dtype), h)

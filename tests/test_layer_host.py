@@ -156,3 +156,14 @@ def test_which_way_float_attention_goes():
                        (0, (1, 32, 32, 128, 64, 64, 1, 4096))):
         assert reckoned(FLOAT_WAY, *args) == want, args
         assert reckoned(WAY, 0, *args) == want & 4, args
+
+
+@pytest.mark.parametrize("max_kv_len", [2 ** 30 + 1, 2 ** 31 - 65537])
+@pytest.mark.parametrize("n_seqs,heads", [(64, 32), (1, 1), (1, 8), (3, 50)])
+def test_a_bound_of_lengths_near_2_to_the_31_is_cut_as_others_are(max_kv_len, n_seqs, heads):
+    """A bound and the chunk together pass 32 bits.  The parts that a call needs are those of its chunks: none for a whole cache, and no fewer with a longer bound."""
+    def parts(most):
+        return reckoned("_ZN4gelo15attention_partsEiiiiiiiii", 1, 1, heads, heads, 64, n_seqs, n_seqs, 1, most)
+    few = parts(2 ** 29)
+    assert parts(max_kv_len) == few and (few > 0) == (n_seqs * heads <= 256)
+    assert reckoned(WAY, 1, 1, heads, heads, 64, n_seqs, n_seqs, 1, max_kv_len) == (4 if few else 0)
