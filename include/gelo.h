@@ -337,7 +337,7 @@ gelo_status gelo_rope_append(gelo_ctx* ctx, gelo_dtype dtype, int n_q_heads, con
  * `dtype` (ldq, ldo), no bytes in common; head_dim 64, 96, 128 or 256.  Rows outside [row_start[0], row_start[n_seqs]) are left as
  * they are.  kv_len beyond max_kv_len is cut to it, below zero is zero; a page number outside the cache is not followed: the
  * results of its sequence are then NaN or partly so.  Statistics, products and sums are float; GELO_BF16 holds the weights exp(s - max) in 16
- * bits for the product with V, or, where rows times the query heads of a key head are many (more than 16), rounds them to bfloat16, in their sum too.  What lies in
+ * bits for the product with V; a call where max_rows times the query heads of a key head is more than 16 may round them to bfloat16, in their sum too.  What lies in
  * cache rows that no query of the batch sees does not reach the result, NaN and infinity included.
  * Where the rows and heads are too few to fill the chip the cache's length is cut over workgroups and their parts are joined through float
  * workspace of the context (gelo_reserve_attention sizes it ahead; else the first call that needs more allocates): calls on one context must not
