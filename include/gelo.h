@@ -347,6 +347,74 @@ gelo_status gelo_attention(gelo_ctx* ctx, gelo_dtype dtype, int n_q_heads, const
 /* Allocates that workspace (as much as any batch of heads of this width needs): gelo_attention then allocates nothing. */
 gelo_status gelo_reserve_attention(gelo_ctx* ctx, int head_dim);
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * A paged cache of 4 bits: a block of 32 values of a head's row is held as codes - a sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 -
+ * times 2^e, e the least whole number from -110 to 125 with max |value| <= 7 2^e, each to nearest, ties to the even code: no value is off by more than
+ * 2^e, a seventh of the block's largest at least and two sevenths at most.  A block with a NaN or an infinity is NaN as a whole.  17/32 of a byte to
+ * a value: 2.1 GB of keys and values of bfloat16 are 0.57 GB.
+ *
+ * gelo_kv_cache_fp4: K and V are arrays of n_pages pages; head h of page g is a piece of gelo_fp4_page_bytes(page_rows, head_dim) bytes from byte
+ * g page_stride + h head_stride of either (strides in bytes, multiples of 16).  page_rows is a power of two from 16 on, head_dim a multiple of 32, their
+ * product at most 2^28.  k and v are 16-byte aligned DEVICE pointers.  A piece is the codes of its rows, then their scale bytes (e + 127; 255: NaN), as
+ * gelo_rope_append_fp4 writes them: two codes to a byte, the value of even number in the lower half; of keys row by row, of values four rows at a time: of each
+ * of the four rows the first head_dim / 32 bytes of its codes, then of each the next, 16 times; and of each the first block's scale, then of each the next block's. */
+typedef struct gelo_kv_cache_fp4 {
+    uint8_t* k;
+    uint8_t* v;
+    int n_pages, n_kv_heads, page_rows, head_dim;
+    int64_t page_stride, head_stride;
+} gelo_kv_cache_fp4;
+
+/* bytes = 17 page_rows head_dim / 32 */
+gelo_status gelo_fp4_page_bytes(int page_rows, int head_dim, size_t* bytes);
+
+/* gelo_rope_append into such a cache; everything said there holds.  Queries come out as there, to the bit; a key's codes are those of its rotation worked out
+ * in double, a value's those of the value.  Entries of rows of the cache that the batch does not bring are left as they are. */
+gelo_status gelo_rope_append_fp4(gelo_ctx* ctx, gelo_dtype dtype, int n_q_heads, const void* QKV, int64_t ld, const gelo_kv_cache_fp4* cache,
+                                 const gelo_seq_batch* batch, gelo_rope_layout layout, int rot_dim, const float* table, int n_table,
+                                 void* Q, int64_t ldq, void* stream);
+
+/* The values that the batch's rows are held as: row j of sequence s, which brings n of them, is the cache's row kv_len[s] - n + j, so a batch that brings all
+ * kv_len[s] rows reads whole sequences.  K, V: n_rows x n_kv_heads head_dim of type `dtype` (ldk, ldv), no bytes in common; either may be NULL.  Exact in
+ * both types.  A row of negative position gives zeros; one at or beyond max_kv_len and one whose page number lies outside the cache give NaN. */
+gelo_status gelo_cache_rows_fp4(gelo_ctx* ctx, gelo_dtype dtype, const gelo_kv_cache_fp4* cache, const gelo_seq_batch* batch,
+                                void* K, int64_t ldk, void* V, int64_t ldv, void* stream);
+
+/* gelo_attention over such a cache; everything said there holds, for keys and values as they are held.  They are multiplied exactly; GELO_F32 has queries
+ * and weights in full.  Weights are relative to a maximum that may lag up to 2^8 behind: sums of values beyond 2^100 can overflow. */
+gelo_status gelo_attention_fp4(gelo_ctx* ctx, gelo_dtype dtype, int n_q_heads, const void* Q, int64_t ldq, const gelo_kv_cache_fp4* cache,
+                               const gelo_seq_batch* batch, float scale, int causal, void* O, int64_t ldo, void* stream);
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * Low-rank adapters of many requests beside one projection, on the trusted side: the shared weight is public, what a request adds to it is not.
+ *
+ * gelo_adapters: n_adapters of them.  The p columns are n_parts parts (the queries, keys and values of a fused projection) that end at columns
+ * part_end[0] < part_end[1] < ... = p, multiples of 16 but for the last.  Adapter w has an A of n_parts rank rows of d values, row r at a + w a_stride + r lda
+ * (rows k rank ... belong to part k), a B of p rows of rank values, row j at b + w b_stride + j ldb, both of the call's type, and a factor scale[w]
+ * (scale NULL: 1).  rank is a multiple of 8 up to GELO_ADAPT_MAX_RANK: a smaller one is filled up with zeros.  a, b (16-byte aligned), scale: DEVICE pointers; strides
+ * in values, multiples of 8, lda and ldb at most 2^24.  The structure is read during the call only. */
+#define GELO_ADAPT_MAX_RANK 128
+#define GELO_ADAPT_MAX_PARTS 4
+typedef struct gelo_adapters {
+    const void* a;
+    const void* b;
+    const float* scale;
+    int n_adapters, rank, n_parts;
+    int part_end[GELO_ADAPT_MAX_PARTS];
+    int64_t a_stride, lda, b_stride, ldb;
+} gelo_adapters;
+
+/* Z[i, j] = base[i, j] + scale[w] sum_r (sum_k H[i, k] A_w[r, k]) B_w[j, r], r over the rank rows of j's part, w = which[i] (DEVICE, n 32-bit
+ * integers).  A row whose number is no adapter's (-1, say) gets base[i].  H: n x d (ldh), base, Z: n x p (ldb, ldz) of type `dtype`; Z may be base itself, and
+ * shares no memory with H or with base otherwise.  Sums are float, one rounding at the end; GELO_BF16 holds the inner sum in 16 bits for the second product.  A
+ * NaN or infinity in H, base or an adapter reaches only the rows it belongs to.  Rows in any order; those of one adapter side by side take least.
+ * The inner sums go through float workspace of the context (gelo_reserve_adapt sizes it ahead; else the first call that needs more allocates, and what it replaces stays
+ * until the context ends): calls on one context must not overlap in time on different streams. */
+gelo_status gelo_adapt(gelo_ctx* ctx, gelo_dtype dtype, int n, int d, int p, const void* H, int64_t ldh, const gelo_adapters* adapters, const int32_t* which,
+                       const void* base, int64_t ldb, void* Z, int64_t ldz, void* stream);
+/* Allocates that workspace for a call of these sizes: gelo_adapt then allocates nothing. */
+gelo_status gelo_reserve_adapt(gelo_ctx* ctx, gelo_dtype dtype, int n, int d, int rank, int n_parts);
+
 /* Test hook: copies the secrets of a mixing object to caller DEVICE buffers (any may be NULL):
  * A and A_inv as float n x n (dense), S as float k_shield x d (dense; valid after gelo_mix).
  * attempt / kappa are HOST pointers: the accepted attempt number and the library's estimate of

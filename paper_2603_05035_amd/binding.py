@@ -24,6 +24,7 @@ GELO_STATIC_MAX_N = 128
 GELO_MAX_BATCH_DRAW = 48
 GELO_STATIC_SCRATCH_BYTES = 16 << 20
 GELO_NORM_MAX_D = 65536
+GELO_ADAPT_MAX_RANK, GELO_ADAPT_MAX_PARTS = 128, 4
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libgelo.so")
 
@@ -36,6 +37,16 @@ class _KvCacheStruct(ctypes.Structure):
 class _SeqBatchStruct(ctypes.Structure):
     _fields_ = [("n_seqs", c_int), ("n_rows", c_int), ("max_rows", c_int), ("max_kv_len", c_int),
                 ("row_start", c_void_p), ("kv_len", c_void_p), ("page_table", c_void_p), ("table_ld", c_int64)]
+
+
+class _KvCacheFp4Struct(ctypes.Structure):
+    _fields_ = [("k", c_void_p), ("v", c_void_p), ("n_pages", c_int), ("n_kv_heads", c_int), ("page_rows", c_int), ("head_dim", c_int),
+                ("page_stride", c_int64), ("head_stride", c_int64)]
+
+
+class _AdaptersStruct(ctypes.Structure):
+    _fields_ = [("a", c_void_p), ("b", c_void_p), ("scale", c_void_p), ("n_adapters", c_int), ("rank", c_int), ("n_parts", c_int),
+                ("part_end", c_int * GELO_ADAPT_MAX_PARTS), ("a_stride", c_int64), ("lda", c_int64), ("b_stride", c_int64), ("ldb", c_int64)]
 
 
 # name -> (restype, argtypes); mirrors include/gelo.h one to one
@@ -75,6 +86,14 @@ SIGNATURES = {
     "gelo_attention": (c_int, [c_void_p, c_int, c_int, c_void_p, c_int64, c_void_p, c_void_p, c_float, c_int,
                                c_void_p, c_int64, c_void_p]),
     "gelo_reserve_attention": (c_int, [c_void_p, c_int]),
+    "gelo_fp4_page_bytes": (c_int, [c_int, c_int, POINTER(ctypes.c_size_t)]),
+    "gelo_rope_append_fp4": (c_int, [c_void_p, c_int, c_int, c_void_p, c_int64, c_void_p, c_void_p, c_int, c_int,
+                                     c_void_p, c_int, c_void_p, c_int64, c_void_p]),
+    "gelo_cache_rows_fp4": (c_int, [c_void_p, c_int, c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_void_p]),
+    "gelo_attention_fp4": (c_int, [c_void_p, c_int, c_int, c_void_p, c_int64, c_void_p, c_void_p, c_float, c_int,
+                                   c_void_p, c_int64, c_void_p]),
+    "gelo_adapt": (c_int, [c_void_p, c_int, c_int, c_int, c_int, c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_void_p]),
+    "gelo_reserve_adapt": (c_int, [c_void_p, c_int, c_int, c_int, c_int, c_int]),
     "gelo_debug_philox_words": (c_int, [c_void_p, c_uint32, c_uint32, c_uint64, c_uint32, c_uint32, c_void_p, c_void_p]),
     "gelo_mixing_export_table": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p]),
     "gelo_qkv_forward": (c_int, [c_void_p, c_int, c_int, c_int, c_int, c_int, c_int, c_void_p, c_void_p, c_float,
@@ -374,6 +393,62 @@ class KvCache:
         self.address = ctypes.addressof(self.struct)
 
 
+def gelo_fp4_page_bytes(page_rows: int, head_dim: int) -> int:
+    """Bytes of a head's piece of a page of a cache of 4 bits."""
+    v = ctypes.c_size_t()
+    st = load_library().gelo_fp4_page_bytes(page_rows, head_dim, byref(v))
+    if st != GELO_OK:
+        raise GeloError(st, f"page_rows={page_rows} must be a power of two from 16 on, head_dim={head_dim} a multiple of 32")
+    return v.value
+
+
+class KvCacheFp4:
+    """A paged cache of 4 bits (see gelo_kv_cache_fp4 in include/gelo.h): K and V are uint8 of shape (pages, key heads, gelo_fp4_page_bytes(page_rows,
+    head_dim)), the last dimension contiguous, both with the same strides.  Describes the tensors and keeps them alive."""
+
+    def __init__(self, K: torch.Tensor, V: torch.Tensor, page_rows: int, head_dim: int):
+        piece = gelo_fp4_page_bytes(page_rows, head_dim)
+        if K.dtype != torch.uint8 or V.dtype != torch.uint8 or K.dim() != 3 or K.shape != V.shape or K.shape[2] != piece:
+            raise ValueError(f"K and V must be uint8 of one shape: pages, key heads, {piece} bytes")
+        if not K.is_cuda or not V.is_cuda or K.device != V.device:
+            raise ValueError("K and V must live on one GPU")
+        # (the stride of a dimension of one entry says nothing)
+        strides, other = ([x.stride(i) if x.shape[i] > 1 else (piece + 15) // 16 * 16 for i in range(2)] for x in (K, V))
+        if strides != other or K.stride(2) != 1 or V.stride(2) != 1:
+            raise ValueError("K and V must have the same strides, the last of them 1")
+        self.K, self.V = K, V
+        self.n_kv_heads, self.page_rows, self.head_dim = K.shape[1], page_rows, head_dim
+        self.struct = _KvCacheFp4Struct(K.data_ptr(), V.data_ptr(), K.shape[0], K.shape[1], page_rows, head_dim, *strides)
+        self.address = ctypes.addressof(self.struct)
+
+
+class Adapters:
+    """Low-rank adapters beside one projection (see gelo_adapters in include/gelo.h): A (adapters, parts x rank, width of H), B (adapters, columns of Z, rank),
+    rows contiguous; scale: a float32 factor to each, or None; part_ends: the columns where the parts of a fused projection end (None: one part).  Describes the
+    tensors and keeps them alive."""
+
+    def __init__(self, A: torch.Tensor, B: torch.Tensor, scale: torch.Tensor | None = None, part_ends=None):
+        part_ends = [B.shape[1]] if part_ends is None else [int(x) for x in part_ends]
+        if A.dim() != 3 or B.dim() != 3 or A.dtype != B.dtype or A.shape[0] != B.shape[0] or A.shape[1] != len(part_ends) * B.shape[2]:
+            raise ValueError("A must be adapters x (parts x rank) x width and B adapters x columns x rank, of one type")
+        if not 1 <= len(part_ends) <= GELO_ADAPT_MAX_PARTS or part_ends[-1] != B.shape[1]:
+            raise ValueError(f"part_ends={part_ends}: up to {GELO_ADAPT_MAX_PARTS} parts, the last of which ends at column {B.shape[1]}")
+        if not A.is_cuda or not B.is_cuda or A.device != B.device:
+            raise ValueError("A and B must live on one GPU")
+        if any(t.shape[2] > 1 and t.stride(2) != 1 for t in (A, B)):
+            raise ValueError("rows of A and B must be contiguous")
+        if scale is not None:
+            _vector(scale, "scale", torch.float32, A.shape[0])
+        count, _, self.d = A.shape
+        _, self.p, rank = B.shape
+        self.A, self.B, self.scale, self.torch_dtype, self.dtype = A, B, scale, A.dtype, _dtype_code(A)
+        # (the stride of a dimension of one entry says nothing)
+        steps = [t.stride(i) if t.shape[i] > 1 else t.shape[2] for t in (A, B) for i in range(2)]
+        self.struct = _AdaptersStruct(A.data_ptr(), B.data_ptr(), None if scale is None else scale.data_ptr(), count, rank, len(part_ends),
+                                      (c_int * GELO_ADAPT_MAX_PARTS)(*part_ends), *steps)
+        self.address = ctypes.addressof(self.struct)
+
+
 class SeqBatch:
     """Which rows of a batch and which pages of a cache belong to which sequence (see gelo_seq_batch in include/gelo.h): kv_len
     (n_seqs), page_table (n_seqs x pages) and row_start (n_seqs + 1, or None: one row each) are int32 tensors on the GPU, read when the
@@ -456,18 +531,14 @@ def gelo_rope_table(ctx, rot_dim: int, n_pos: int, base: float = 10000.0, factor
     return table
 
 
-def gelo_rope_append(ctx, QKV: torch.Tensor, n_q_heads: int, cache: KvCache, batch: SeqBatch, Q: torch.Tensor | None = None,
-                     table: torch.Tensor | None = None, rot_dim: int = 0, layout: int = GELO_ROPE_HALF, stream=None):
-    """Rotates the queries and keys of QKV's rows by their positions; queries into Q, keys and values into the cache."""
+def _append(call, ctx, QKV, n_q_heads, cache, code, batch, Q, table, rot_dim, layout, stream):
     zp, ld = _matrix(QKV, "QKV")
     rows, width = QKV.shape
-    if QKV.dtype != cache.torch_dtype:
-        raise GeloError(3, "QKV and the cache differ in type")
     if width != (n_q_heads + 2 * cache.n_kv_heads) * cache.head_dim:
         raise GeloError(2, f"a row of {width} values is not {n_q_heads} + 2 x {cache.n_kv_heads} heads of {cache.head_dim}")
     qp, ldq = None, 0
     if Q is not None:
-        if Q.dtype != cache.torch_dtype or Q.shape != (rows, n_q_heads * cache.head_dim):
+        if Q.dtype != QKV.dtype or Q.shape != (rows, n_q_heads * cache.head_dim):
             raise ValueError("Q must be of QKV's dtype, a row of all query heads for each of its rows")
         qp, ldq = _matrix(Q, "Q")
     tp, n_table = None, 0
@@ -477,31 +548,98 @@ def gelo_rope_append(ctx, QKV: torch.Tensor, n_q_heads: int, cache: KvCache, bat
             raise ValueError("table must be a contiguous float32 GPU tensor of positions x rot_dim")
         tp = table.data_ptr()
     described = _described(batch, rows, cache)
-    status = load_library().gelo_rope_append(ctx, cache.dtype, n_q_heads, zp, ld, cache.address, described[2], layout, rot_dim, tp, n_table, qp, ldq,
-                                             _stream(stream))
+    status = call(ctx, code, n_q_heads, zp, ld, cache.address, described[2], layout, rot_dim, tp, n_table, qp, ldq, _stream(stream))
     if status != GELO_OK:
         _check(ctx, status)
 
 
-def gelo_attention(ctx, Q: torch.Tensor, O: torch.Tensor, n_q_heads: int, cache: KvCache, batch: SeqBatch, scale: float, causal: bool = True,
-                   stream=None) -> torch.Tensor:
-    """softmax(scale Q K^T) V over the rows of the cache that each row of Q sees, into O."""
+def gelo_rope_append(ctx, QKV: torch.Tensor, n_q_heads: int, cache: KvCache, batch: SeqBatch, Q: torch.Tensor | None = None,
+                     table: torch.Tensor | None = None, rot_dim: int = 0, layout: int = GELO_ROPE_HALF, stream=None):
+    """Rotates the queries and keys of QKV's rows by their positions; queries into Q, keys and values into the cache."""
+    if QKV.dtype != cache.torch_dtype:
+        raise GeloError(3, "QKV and the cache differ in type")
+    _append(load_library().gelo_rope_append, ctx, QKV, n_q_heads, cache, cache.dtype, batch, Q, table, rot_dim, layout, stream)
+
+
+def gelo_rope_append_fp4(ctx, QKV: torch.Tensor, n_q_heads: int, cache: KvCacheFp4, batch: SeqBatch, Q: torch.Tensor | None = None,
+                         table: torch.Tensor | None = None, rot_dim: int = 0, layout: int = GELO_ROPE_HALF, stream=None):
+    """gelo_rope_append into a cache of 4 bits."""
+    _append(load_library().gelo_rope_append_fp4, ctx, QKV, n_q_heads, cache, _dtype_code(QKV), batch, Q, table, rot_dim, layout, stream)
+
+
+def gelo_cache_rows_fp4(ctx, cache: KvCacheFp4, batch: SeqBatch, K: torch.Tensor | None = None, V: torch.Tensor | None = None, stream=None):
+    """The values that the batch's rows are held as, a row of all key heads to each, into K and V (either may be None)."""
+    some = K if K is not None else V
+    if some is None:
+        raise ValueError("K and V are both None: nothing to write")
+    at = []
+    for name, t in (("K", K), ("V", V)):
+        if t is None:
+            at += [None, 0]
+            continue
+        if t.dtype != some.dtype or t.dim() != 2 or t.shape != (some.shape[0], cache.n_kv_heads * cache.head_dim):
+            raise ValueError(f"{name} must have a row of {cache.n_kv_heads} heads of {cache.head_dim} for each row of the batch, of the other's type")
+        at += _matrix(t, name)
+    described = _described(batch, some.shape[0], cache)
+    _check(ctx, load_library().gelo_cache_rows_fp4(ctx, _dtype_code(some), cache.address, described[2], *at, _stream(stream)))
+
+
+def _attend(call, ctx, Q, O, n_q_heads, cache, code, batch, scale, causal, stream):
     qp, ldq = _matrix(Q, "Q")
     op, ldo = _matrix(O, "O")
     shape = Q.shape
-    if Q.dtype != cache.torch_dtype or O.dtype != cache.torch_dtype:
-        raise GeloError(3, "Q, O and the cache differ in type")
     if shape[1] != n_q_heads * cache.head_dim or O.shape != shape:
         raise GeloError(2, f"Q and O must have {n_q_heads} heads of {cache.head_dim} values in a row")
     described = _described(batch, shape[0], cache)
-    status = load_library().gelo_attention(ctx, cache.dtype, n_q_heads, qp, ldq, cache.address, described[2], scale, causal, op, ldo, _stream(stream))
+    status = call(ctx, code, n_q_heads, qp, ldq, cache.address, described[2], scale, causal, op, ldo, _stream(stream))
     if status != GELO_OK:
         _check(ctx, status)
     return O
 
 
+def gelo_attention(ctx, Q: torch.Tensor, O: torch.Tensor, n_q_heads: int, cache: KvCache, batch: SeqBatch, scale: float, causal: bool = True,
+                   stream=None) -> torch.Tensor:
+    """softmax(scale Q K^T) V over the rows of the cache that each row of Q sees, into O."""
+    if Q.dtype != cache.torch_dtype or O.dtype != cache.torch_dtype:
+        raise GeloError(3, "Q, O and the cache differ in type")
+    return _attend(load_library().gelo_attention, ctx, Q, O, n_q_heads, cache, cache.dtype, batch, scale, causal, stream)
+
+
+def gelo_attention_fp4(ctx, Q: torch.Tensor, O: torch.Tensor, n_q_heads: int, cache: KvCacheFp4, batch: SeqBatch, scale: float, causal: bool = True,
+                       stream=None) -> torch.Tensor:
+    """gelo_attention over a cache of 4 bits."""
+    if O.dtype != Q.dtype:
+        raise GeloError(3, "Q and O differ in type")
+    return _attend(load_library().gelo_attention_fp4, ctx, Q, O, n_q_heads, cache, _dtype_code(Q), batch, scale, causal, stream)
+
+
 def gelo_reserve_attention(ctx, head_dim: int) -> None:
     _check(ctx, load_library().gelo_reserve_attention(ctx, head_dim))
+
+
+def gelo_adapt(ctx, H: torch.Tensor, adapters: Adapters, which: torch.Tensor, Z: torch.Tensor, base: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Z = base + what the adapter of each row adds (base None: Z's own values).  which: int32, the adapter of every row; a number that is none's: base alone."""
+    if base is None:
+        base = Z
+    shape, out = H.shape, Z.shape
+    hp, ldh = _matrix(H, "H")
+    bp, ldb = _matrix(base, "base")
+    zp, ldz = _matrix(Z, "Z")
+    dtype = adapters.torch_dtype
+    if H.dtype != dtype or Z.dtype != dtype or base.dtype != dtype:
+        raise GeloError(3, "H, base, Z and the adapters differ in type")
+    if shape[1] != adapters.d or out != (shape[0], adapters.p) or base.shape != out:
+        raise GeloError(2, f"H must have rows of {adapters.d} values, base and Z as many of {adapters.p}")
+    _vector(which, "which", torch.int32, shape[0])
+    status = load_library().gelo_adapt(ctx, adapters.dtype, shape[0], adapters.d, adapters.p, hp, ldh, adapters.address, which.data_ptr(), bp, ldb, zp, ldz,
+                                       _stream(stream))
+    if status != GELO_OK:
+        _check(ctx, status)
+    return Z
+
+
+def gelo_reserve_adapt(ctx, dtype: int, n: int, d: int, rank: int, n_parts: int = 1) -> None:
+    _check(ctx, load_library().gelo_reserve_adapt(ctx, dtype, n, d, rank, n_parts))
 
 
 def gelo_debug_quantize_rows_fp8(ctx, U: torch.Tensor, stream=None):

@@ -101,6 +101,8 @@ struct gelo_ctx {
     void* chain_ws;  size_t chain_ws_bytes;
     void* quant_ws;  size_t quant_ws_bytes;    // FP8 projection: codes and row scales of the current U
     void* attention_ws; size_t attention_ws_bytes; // parts of a cut cache
+    void* adapt_ws; size_t adapt_ws_bytes;         // the first products of adapters
+    std::vector<void*> adapt_outgrown;             // smaller ones that captured calls may still name
     void* project_ws; size_t project_ws_bytes; // bf16 projection of at most 128 rows: float partial sums of the K slices
     float* host_scalars;         // pinned: kappa read-back, one slot per lane
     int* host_flag;
@@ -380,7 +382,7 @@ static hipError_t kernels_init(int device) {
     static std::atomic<bool> done[kStaticMaxDevices];       // (two threads at once both do it: the calls may be repeated)
     if (device < kStaticMaxDevices && done[device].load(std::memory_order_acquire)) return hipSuccess;
     hipError_t (*const inits[])() = {gemm_bf16_init, gemm_f32_init, inverse_init, structured_init, small_init, gemm_fp8_init,
-                                     factor_init, block_reflect_init, block_factor_init, sampler_init, attention_init};
+                                     factor_init, block_reflect_init, block_factor_init, sampler_init, attention_init, attention_fp4_init};
     for (auto init : inits) {
         const hipError_t e = init();
         if (e != hipSuccess) return e;
@@ -413,6 +415,7 @@ gelo_status gelo_create(gelo_ctx** out, int device, uint64_t seed, int allow_bat
     ctx->quant_ws = nullptr; ctx->quant_ws_bytes = 0;
     ctx->project_ws = nullptr; ctx->project_ws_bytes = 0;
     ctx->attention_ws = nullptr; ctx->attention_ws_bytes = 0;
+    ctx->adapt_ws = nullptr; ctx->adapt_ws_bytes = 0;
     ctx->host_scalars = nullptr; ctx->host_flag = nullptr;
     ctx->lanes_ready = false; ctx->join_pending = false; ctx->cand = nullptr; ctx->cand_bytes = 0;
     for (int i = 0; i < kLanes; ++i) ctx->lane_graph_ok[i] = false;
@@ -448,6 +451,8 @@ gelo_status gelo_destroy(gelo_ctx* ctx) {
     if (ctx->quant_ws) (void)hipFree(ctx->quant_ws);
     if (ctx->project_ws) (void)hipFree(ctx->project_ws);
     if (ctx->attention_ws) (void)hipFree(ctx->attention_ws);
+    if (ctx->adapt_ws) (void)hipFree(ctx->adapt_ws);
+    for (void* p : ctx->adapt_outgrown) (void)hipFree(p);
     if (ctx->host_scalars) (void)hipHostFree(ctx->host_scalars);
     delete ctx;
     return GELO_OK;
@@ -1520,6 +1525,47 @@ static gelo_status check_batch(gelo_ctx* ctx, const gelo_seq_batch* b, int page_
     return GELO_OK;
 }
 
+static gelo_status check_cache_fp4(gelo_ctx* ctx, const gelo_kv_cache_fp4* c, KvCache* out) {
+    if (!c || !c->k || !c->v) return fail(ctx, GELO_EINVAL, "cache, its keys and its values must not be NULL");
+    if (c->n_pages < 1 || c->n_kv_heads < 1 || c->head_dim < 1 || c->page_rows < 1)
+        return fail(ctx, GELO_EINVAL, "cache: n_pages=%d n_kv_heads=%d page_rows=%d head_dim=%d", c->n_pages, c->n_kv_heads, c->page_rows, c->head_dim);
+    size_t piece = 0;
+    if (gelo_fp4_page_bytes(c->page_rows, c->head_dim, &piece) != GELO_OK)
+        return fail(ctx, GELO_ESHAPE, "page_rows=%d must be a power of two from 16 on, head_dim=%d a multiple of 32, their product at most 2^28", c->page_rows, c->head_dim);
+    if (!aligned16(c->k) || !aligned16(c->v)) return fail(ctx, GELO_EALIGN, "keys and values must be 16-byte aligned");
+    if (c->page_stride % 16 != 0 || c->head_stride % 16 != 0) return fail(ctx, GELO_EALIGN, "cache: strides must be multiples of 16 bytes");
+    if ((c->n_kv_heads > 1 && c->head_stride < (int64_t)piece) || (c->n_pages > 1 && c->page_stride < (int64_t)piece))
+        return fail(ctx, GELO_EINVAL, "a stride of the cache is below the %zu bytes of a head's piece of a page", piece);
+    int shift = 0;
+    while ((1 << shift) < c->page_rows) ++shift;
+    *out = KvCache{c->k, c->v, c->n_pages, c->n_kv_heads, shift, c->head_dim, c->page_stride, c->head_stride, 0};
+    return GELO_OK;
+}
+
+// What gelo_rope_append and gelo_rope_append_fp4 check behind their caches, and what they leave to their kernels.
+static gelo_status check_append(gelo_ctx* ctx, gelo_dtype dtype, int n_q_heads, const void* QKV, int64_t ld, const gelo_seq_batch* batch, gelo_rope_layout layout,
+                                int rot_dim, const float* table, int n_table, void* Q, int64_t ldq, RopeAppend* o) {
+    const int head_dim = o->cache.head_dim, n_kv_heads = o->cache.n_kv_heads;
+    gelo_status st = check_batch(ctx, batch, 1 << o->cache.page_shift, &o->batch);
+    if (st != GELO_OK) return st;
+    if (n_q_heads < 0 || (n_q_heads > 0) != (Q != nullptr)) return fail(ctx, GELO_EINVAL, "n_q_heads=%d: Q is given if there are any", n_q_heads);
+    const int64_t width = ((int64_t)n_q_heads + 2 * (int64_t)n_kv_heads) * head_dim;
+    if (width > (1 << 24)) return fail(ctx, GELO_ESHAPE, "a row of %lld values is too wide", (long long)width);
+    st = check_matrix(ctx, "QKV", QKV, ld, (int)width);
+    if (st == GELO_OK && Q) st = check_matrix(ctx, "Q", Q, ldq, n_q_heads * head_dim);
+    if (st != GELO_OK) return st;
+    if (rot_dim < 0 || rot_dim % 16 != 0 || rot_dim > head_dim) return fail(ctx, GELO_EINVAL, "rot_dim=%d must be a multiple of 16 up to head_dim=%d", rot_dim, head_dim);
+    if (rot_dim > 0) {
+        if (!table || !aligned16(table)) return fail(ctx, table ? GELO_EALIGN : GELO_EINVAL, "table must be a 16-byte aligned device buffer");
+        if (n_table < batch->max_kv_len) return fail(ctx, GELO_ESHAPE, "a table of %d positions is too short for max_kv_len=%d", n_table, batch->max_kv_len);
+    }
+    const int64_t each = dtype == GELO_BF16 ? 2 : 4, rows = batch->n_rows;
+    const Extent in(QKV, ld, width, each), out(Q, ldq, (int64_t)n_q_heads * head_dim, each);
+    if (share(out, in, rows) && !same_place(out, in, rows)) return fail(ctx, GELO_EINVAL, "Q must not share memory with QKV unless it is that matrix");
+    o->QKV = QKV; o->ld = ld; o->Q = Q; o->ldq = ldq; o->n_q_heads = n_q_heads; o->rot = rot_dim; o->pairs = layout == GELO_ROPE_PAIRS; o->table = table;
+    return GELO_OK;
+}
+
 gelo_status gelo_rope_append(gelo_ctx* ctx, gelo_dtype dtype, int n_q_heads, const void* QKV, int64_t ld, const gelo_kv_cache* cache,
                              const gelo_seq_batch* batch, gelo_rope_layout layout, int rot_dim, const float* table, int n_table,
                              void* Q, int64_t ldq, void* stream) {
@@ -1528,26 +1574,77 @@ gelo_status gelo_rope_append(gelo_ctx* ctx, gelo_dtype dtype, int n_q_heads, con
     if (layout != GELO_ROPE_HALF && layout != GELO_ROPE_PAIRS) return fail(ctx, GELO_EINVAL, "unknown layout %d", (int)layout);
     RopeAppend o;
     gelo_status st = check_cache(ctx, cache, &o.cache);
-    if (st == GELO_OK) st = check_batch(ctx, batch, cache->page_rows, &o.batch);
+    if (st == GELO_OK) st = check_append(ctx, dtype, n_q_heads, QKV, ld, batch, layout, rot_dim, table, n_table, Q, ldq, &o);
     if (st != GELO_OK) return st;
-    if (n_q_heads < 0 || (n_q_heads > 0) != (Q != nullptr)) return fail(ctx, GELO_EINVAL, "n_q_heads=%d: Q is given if there are any", n_q_heads);
-    const int64_t width = ((int64_t)n_q_heads + 2 * (int64_t)cache->n_kv_heads) * cache->head_dim;
-    if (width > (1 << 24)) return fail(ctx, GELO_ESHAPE, "a row of %lld values is too wide", (long long)width);
-    st = check_matrix(ctx, "QKV", QKV, ld, (int)width);
-    if (st == GELO_OK && Q) st = check_matrix(ctx, "Q", Q, ldq, n_q_heads * cache->head_dim);
-    if (st != GELO_OK) return st;
-    if (rot_dim < 0 || rot_dim % 16 != 0 || rot_dim > cache->head_dim) return fail(ctx, GELO_EINVAL, "rot_dim=%d must be a multiple of 16 up to head_dim=%d", rot_dim, cache->head_dim);
-    if (rot_dim > 0) {
-        if (!table || !aligned16(table)) return fail(ctx, table ? GELO_EALIGN : GELO_EINVAL, "table must be a 16-byte aligned device buffer");
-        if (n_table < batch->max_kv_len) return fail(ctx, GELO_ESHAPE, "a table of %d positions is too short for max_kv_len=%d", n_table, batch->max_kv_len);
-    }
-    const int64_t each = dtype == GELO_BF16 ? 2 : 4, rows = batch->n_rows;
-    const Extent in(QKV, ld, width, each), out(Q, ldq, (int64_t)n_q_heads * cache->head_dim, each);
-    if (share(out, in, rows) && !same_place(out, in, rows)) return fail(ctx, GELO_EINVAL, "Q must not share memory with QKV unless it is that matrix");
     GELO_HIP(ctx, hipSetDevice(ctx->device));
-    o.QKV = QKV; o.ld = ld; o.Q = Q; o.ldq = ldq; o.n_q_heads = n_q_heads; o.rot = rot_dim; o.pairs = layout == GELO_ROPE_PAIRS; o.table = table;
     GELO_HIP(ctx, rope_append(o, dtype == GELO_BF16, (hipStream_t)stream));
     return GELO_OK;
+}
+
+gelo_status gelo_fp4_page_bytes(int page_rows, int head_dim, size_t* bytes) {
+    if (!bytes || page_rows < 1 || head_dim < 1) return GELO_EINVAL;
+    if (page_rows < 16 || (page_rows & (page_rows - 1)) || head_dim % 32 != 0 || (int64_t)page_rows * head_dim > (1 << 28)) return GELO_ESHAPE;
+    *bytes = (size_t)page_rows * (head_dim / 32) * 17;
+    return GELO_OK;
+}
+
+gelo_status gelo_rope_append_fp4(gelo_ctx* ctx, gelo_dtype dtype, int n_q_heads, const void* QKV, int64_t ld, const gelo_kv_cache_fp4* cache,
+                                 const gelo_seq_batch* batch, gelo_rope_layout layout, int rot_dim, const float* table, int n_table,
+                                 void* Q, int64_t ldq, void* stream) {
+    if (!ctx) return GELO_EINVAL;
+    if (dtype != GELO_F32 && dtype != GELO_BF16) return fail(ctx, GELO_EINVAL, "unknown dtype %d", (int)dtype);
+    if (layout != GELO_ROPE_HALF && layout != GELO_ROPE_PAIRS) return fail(ctx, GELO_EINVAL, "unknown layout %d", (int)layout);
+    RopeAppend o;
+    gelo_status st = check_cache_fp4(ctx, cache, &o.cache);
+    if (st == GELO_OK) st = check_append(ctx, dtype, n_q_heads, QKV, ld, batch, layout, rot_dim, table, n_table, Q, ldq, &o);
+    if (st != GELO_OK) return st;
+    GELO_HIP(ctx, hipSetDevice(ctx->device));
+    GELO_HIP(ctx, rope_append_fp4(o, dtype == GELO_BF16, (hipStream_t)stream));
+    return GELO_OK;
+}
+
+gelo_status gelo_cache_rows_fp4(gelo_ctx* ctx, gelo_dtype dtype, const gelo_kv_cache_fp4* cache, const gelo_seq_batch* batch,
+                                void* K, int64_t ldk, void* V, int64_t ldv, void* stream) {
+    if (!ctx) return GELO_EINVAL;
+    if (dtype != GELO_F32 && dtype != GELO_BF16) return fail(ctx, GELO_EINVAL, "unknown dtype %d", (int)dtype);
+    CacheRows o;
+    gelo_status st = check_cache_fp4(ctx, cache, &o.cache);
+    if (st == GELO_OK) st = check_batch(ctx, batch, cache->page_rows, &o.batch);
+    if (st != GELO_OK) return st;
+    const int64_t width = (int64_t)cache->n_kv_heads * cache->head_dim, each = dtype == GELO_BF16 ? 2 : 4;
+    if (width > (1 << 23)) return fail(ctx, GELO_ESHAPE, "a row of %lld values is too wide", (long long)width);
+    if (!K && !V) return fail(ctx, GELO_EINVAL, "K and V are both NULL: nothing to write");
+    if (K) st = check_matrix(ctx, "K", K, ldk, (int)width);
+    if (st == GELO_OK && V) st = check_matrix(ctx, "V", V, ldv, (int)width);
+    if (st != GELO_OK) return st;
+    if (share(Extent(K, ldk, width, each), Extent(V, ldv, width, each), batch->n_rows)) return fail(ctx, GELO_EINVAL, "K must not share memory with V");
+    GELO_HIP(ctx, hipSetDevice(ctx->device));
+    o.K = K; o.ldk = ldk; o.V = V; o.ldv = ldv;
+    GELO_HIP(ctx, cache_rows_fp4(o, dtype == GELO_BF16, (hipStream_t)stream));
+    return GELO_OK;
+}
+
+// What gelo_attention and gelo_attention_fp4 check behind their caches, and what they leave to their kernels.
+static gelo_status check_attention(gelo_ctx* ctx, gelo_dtype dtype, int n_q_heads, const void* Q, int64_t ldq, const gelo_seq_batch* batch, float scale, int causal,
+                                   void* O, int64_t ldo, Attention* o) {
+    const int d = o->cache.head_dim, n_kv_heads = o->cache.n_kv_heads;
+    gelo_status st = check_batch(ctx, batch, 1 << o->cache.page_shift, &o->batch);
+    if (st != GELO_OK) return st;
+    if (d != 64 && d != 96 && d != 128 && d != 256) return fail(ctx, GELO_ESHAPE, "head_dim=%d is none of 64, 96, 128, 256", d);
+    if (n_q_heads < 1 || n_q_heads % n_kv_heads != 0) return fail(ctx, GELO_EINVAL, "n_q_heads=%d is not a multiple of n_kv_heads=%d", n_q_heads, n_kv_heads);
+    if ((int64_t)n_q_heads * d > (1 << 24)) return fail(ctx, GELO_ESHAPE, "n_q_heads=%d heads of %d are too many", n_q_heads, d);
+    if (!std::isfinite(scale)) return fail(ctx, GELO_EINVAL, "scale=%g", (double)scale);
+    st = check_matrix(ctx, "Q", Q, ldq, n_q_heads * d);
+    if (st == GELO_OK) st = check_matrix(ctx, "O", O, ldo, n_q_heads * d);
+    if (st != GELO_OK) return st;
+    o->Q = Q; o->ldq = ldq; o->O = O; o->ldo = ldo; o->n_q_heads = n_q_heads; o->scale = scale; o->causal = causal != 0;
+    const int64_t each = dtype == GELO_BF16 ? 2 : 4;
+    if (share(Extent(Q, ldq, (int64_t)n_q_heads * d, each), Extent(O, ldo, (int64_t)n_q_heads * d, each), batch->n_rows)) return fail(ctx, GELO_EINVAL, "O must not share memory with Q");
+    return GELO_OK;
+}
+
+static gelo_status too_many_for_a_launch(gelo_ctx* ctx, const gelo_seq_batch* batch, int n_q_heads) {
+    return fail(ctx, GELO_ESHAPE, "%d sequences of up to %d rows and %d heads are too many for one launch", batch->n_seqs, batch->max_rows, n_q_heads);
 }
 
 gelo_status gelo_attention(gelo_ctx* ctx, gelo_dtype dtype, int n_q_heads, const void* Q, int64_t ldq, const gelo_kv_cache* cache,
@@ -1556,20 +1653,9 @@ gelo_status gelo_attention(gelo_ctx* ctx, gelo_dtype dtype, int n_q_heads, const
     if (dtype != GELO_F32 && dtype != GELO_BF16) return fail(ctx, GELO_EINVAL, "unknown dtype %d", (int)dtype);
     Attention o;
     gelo_status st = check_cache(ctx, cache, &o.cache);
-    if (st == GELO_OK) st = check_batch(ctx, batch, cache->page_rows, &o.batch);
+    if (st == GELO_OK) st = check_attention(ctx, dtype, n_q_heads, Q, ldq, batch, scale, causal, O, ldo, &o);
     if (st != GELO_OK) return st;
-    const int d = cache->head_dim;
-    if (d != 64 && d != 96 && d != 128 && d != 256) return fail(ctx, GELO_ESHAPE, "head_dim=%d is none of 64, 96, 128, 256", d);
-    if (n_q_heads < 1 || n_q_heads % cache->n_kv_heads != 0) return fail(ctx, GELO_EINVAL, "n_q_heads=%d is not a multiple of n_kv_heads=%d", n_q_heads, cache->n_kv_heads);
-    if ((int64_t)n_q_heads * d > (1 << 24)) return fail(ctx, GELO_ESHAPE, "n_q_heads=%d heads of %d are too many", n_q_heads, d);
-    if (!std::isfinite(scale)) return fail(ctx, GELO_EINVAL, "scale=%g", (double)scale);
-    st = check_matrix(ctx, "Q", Q, ldq, n_q_heads * d);
-    if (st == GELO_OK) st = check_matrix(ctx, "O", O, ldo, n_q_heads * d);
-    if (st != GELO_OK) return st;
-    o.Q = Q; o.ldq = ldq; o.O = O; o.ldo = ldo; o.n_q_heads = n_q_heads; o.scale = scale; o.causal = causal != 0;
-    const int64_t each = dtype == GELO_BF16 ? 2 : 4;
-    if (share(Extent(Q, ldq, (int64_t)n_q_heads * d, each), Extent(O, ldo, (int64_t)n_q_heads * d, each), batch->n_rows)) return fail(ctx, GELO_EINVAL, "O must not share memory with Q");
-    if (!attention_fits(o, dtype == GELO_BF16)) return fail(ctx, GELO_ESHAPE, "%d sequences of up to %d rows and %d heads are too many for one launch", batch->n_seqs, batch->max_rows, n_q_heads);
+    if (!attention_fits(o, dtype == GELO_BF16)) return too_many_for_a_launch(ctx, batch, n_q_heads);
     GELO_HIP(ctx, hipSetDevice(ctx->device));
     const size_t need = attention_workspace_bytes(o, dtype == GELO_BF16);
     if (need > 0) st = grow(ctx, &ctx->attention_ws, &ctx->attention_ws_bytes, need);
@@ -1579,11 +1665,107 @@ gelo_status gelo_attention(gelo_ctx* ctx, gelo_dtype dtype, int n_q_heads, const
     return GELO_OK;
 }
 
+gelo_status gelo_attention_fp4(gelo_ctx* ctx, gelo_dtype dtype, int n_q_heads, const void* Q, int64_t ldq, const gelo_kv_cache_fp4* cache,
+                               const gelo_seq_batch* batch, float scale, int causal, void* O, int64_t ldo, void* stream) {
+    if (!ctx) return GELO_EINVAL;
+    if (dtype != GELO_F32 && dtype != GELO_BF16) return fail(ctx, GELO_EINVAL, "unknown dtype %d", (int)dtype);
+    Attention o;
+    gelo_status st = check_cache_fp4(ctx, cache, &o.cache);
+    if (st == GELO_OK) st = check_attention(ctx, dtype, n_q_heads, Q, ldq, batch, scale, causal, O, ldo, &o);
+    if (st != GELO_OK) return st;
+    if (!attention_fp4_fits(o, dtype == GELO_BF16)) return too_many_for_a_launch(ctx, batch, n_q_heads);
+    GELO_HIP(ctx, hipSetDevice(ctx->device));
+    const size_t need = attention_fp4_workspace_bytes(o, dtype == GELO_BF16);
+    if (need > 0) st = grow(ctx, &ctx->attention_ws, &ctx->attention_ws_bytes, need);
+    if (st != GELO_OK) return st;
+    o.workspace = (float*)ctx->attention_ws;
+    GELO_HIP(ctx, attention_fp4(o, dtype == GELO_BF16, (hipStream_t)stream));
+    return GELO_OK;
+}
+
 gelo_status gelo_reserve_attention(gelo_ctx* ctx, int head_dim) {
     if (!ctx) return GELO_EINVAL;
     if (head_dim != 64 && head_dim != 96 && head_dim != 128 && head_dim != 256) return fail(ctx, GELO_ESHAPE, "head_dim=%d is none of 64, 96, 128, 256", head_dim);
     GELO_HIP(ctx, hipSetDevice(ctx->device));
     return grow(ctx, &ctx->attention_ws, &ctx->attention_ws_bytes, attention_workspace_bound(head_dim));
+}
+
+// The first products' workspace.  What is outgrown stays until the context ends: a captured call has its address.
+static gelo_status grow_adapt(gelo_ctx* ctx, size_t need) {
+    if (ctx->adapt_ws_bytes >= need) return GELO_OK;
+    if (need < 2 * ctx->adapt_ws_bytes) need = 2 * ctx->adapt_ws_bytes;
+    void* old = ctx->adapt_ws;
+    size_t have = 0;
+    if (old) ctx->adapt_outgrown.push_back(old);
+    ctx->adapt_ws = nullptr;
+    const gelo_status st = grow(ctx, &ctx->adapt_ws, &have, need);
+    if (st != GELO_OK) {
+        if (old) ctx->adapt_outgrown.pop_back();
+        ctx->adapt_ws = old;
+        return st;
+    }
+    ctx->adapt_ws_bytes = have;
+    return GELO_OK;
+}
+
+static gelo_status check_adapters(gelo_ctx* ctx, const gelo_adapters* a, int d, int p) {
+    if (!a || !a->a || !a->b) return fail(ctx, GELO_EINVAL, "adapters and their matrices must not be NULL");
+    if (a->n_adapters < 1 || a->n_parts < 1 || a->rank < 1) return fail(ctx, GELO_EINVAL, "adapters: n_adapters=%d n_parts=%d rank=%d", a->n_adapters, a->n_parts, a->rank);
+    if (a->rank % 8 != 0 || a->rank > GELO_ADAPT_MAX_RANK) return fail(ctx, GELO_ESHAPE, "rank=%d must be a multiple of 8 up to %d", a->rank, GELO_ADAPT_MAX_RANK);
+    if (a->n_parts > GELO_ADAPT_MAX_PARTS) return fail(ctx, GELO_ESHAPE, "n_parts=%d exceeds %d", a->n_parts, GELO_ADAPT_MAX_PARTS);
+    for (int k = 0; k < a->n_parts; ++k) {
+        const int begin = k ? a->part_end[k - 1] : 0, end = a->part_end[k];
+        if (end <= begin || (k == a->n_parts - 1 ? end != p : end % 16 != 0))
+            return fail(ctx, GELO_EINVAL, "part_end[%d]=%d: parts end at ascending multiples of 16, the last at p=%d", k, end, p);
+    }
+    gelo_status st = check_matrix(ctx, "A", a->a, a->lda, d);
+    if (st == GELO_OK) st = check_matrix(ctx, "B", a->b, a->ldb, a->rank);
+    if (st != GELO_OK) return st;
+    if (a->a_stride % 8 != 0 || a->b_stride % 8 != 0) return fail(ctx, GELO_EALIGN, "strides of adapters must be multiples of 8");
+    if (a->a_stride < 0 || a->b_stride < 0 || a->lda > (1 << 24) || a->ldb > (1 << 24)) return fail(ctx, GELO_ESHAPE, "adapters: a stride is negative or a row's exceeds 2^24");
+    if (reinterpret_cast<uintptr_t>(a->scale) & 3u) return fail(ctx, GELO_EALIGN, "scale must be 4-byte aligned");
+    return GELO_OK;
+}
+
+gelo_status gelo_adapt(gelo_ctx* ctx, gelo_dtype dtype, int n, int d, int p, const void* H, int64_t ldh, const gelo_adapters* adapters, const int32_t* which,
+                       const void* base, int64_t ldb, void* Z, int64_t ldz, void* stream) {
+    if (!ctx) return GELO_EINVAL;
+    if (dtype != GELO_F32 && dtype != GELO_BF16) return fail(ctx, GELO_EINVAL, "unknown dtype %d", (int)dtype);
+    if (n < 1 || d < 1 || p < 1) return fail(ctx, GELO_EINVAL, "n=%d d=%d p=%d", n, d, p);
+    if (d % 8 != 0 || p % 8 != 0) return fail(ctx, GELO_EALIGN, "d=%d and p=%d must be multiples of 8", d, p);
+    if (d > (1 << 24) || p > (1 << 24)) return fail(ctx, GELO_ESHAPE, "d=%d p=%d", d, p);
+    gelo_status st = check_matrix(ctx, "H", H, ldh, d);
+    if (st == GELO_OK) st = check_matrix(ctx, "base", base, ldb, p);
+    if (st == GELO_OK) st = check_matrix(ctx, "Z", Z, ldz, p);
+    if (st == GELO_OK) st = check_adapters(ctx, adapters, d, p);
+    if (st != GELO_OK) return st;
+    if (!which || (reinterpret_cast<uintptr_t>(which) & 3u)) return fail(ctx, which ? GELO_EALIGN : GELO_EINVAL, "which must be a device array of 32-bit integers");
+    const int64_t each = dtype == GELO_BF16 ? 2 : 4;
+    const Extent h(H, ldh, d, each), from(base, ldb, p, each), to(Z, ldz, p, each);
+    if (share(to, h, n) || (share(to, from, n) && !same_place(to, from, n)))
+        return fail(ctx, GELO_EINVAL, "Z must not share memory with H, nor with base unless it is that matrix");
+    Adapt o;
+    o.H = H; o.ldh = ldh; o.base = base; o.ldb = ldb; o.Z = Z; o.ldz = ldz; o.which = which; o.n = n; o.d = d; o.p = p;
+    o.A = adapters->a; o.a_stride = adapters->a_stride; o.lda = adapters->lda; o.B = adapters->b; o.b_stride = adapters->b_stride; o.ldbw = adapters->ldb;
+    o.scale = adapters->scale; o.rank = adapters->rank; o.n_parts = adapters->n_parts; o.n_adapters = adapters->n_adapters;
+    for (int k = 0; k < kMostParts; ++k) o.part_end[k] = k < o.n_parts ? adapters->part_end[k] : p;
+    if (!adapt_fits(o)) return fail(ctx, GELO_ESHAPE, "%d rows of %d columns are too many for one launch", n, p);
+    GELO_HIP(ctx, hipSetDevice(ctx->device));
+    st = grow_adapt(ctx, adapt_workspace_bytes(dtype == GELO_BF16, n, d, o.rank, o.n_parts));
+    if (st != GELO_OK) return st;
+    o.workspace = (float*)ctx->adapt_ws;
+    GELO_HIP(ctx, adapt(o, dtype == GELO_BF16, (hipStream_t)stream));
+    return GELO_OK;
+}
+
+gelo_status gelo_reserve_adapt(gelo_ctx* ctx, gelo_dtype dtype, int n, int d, int rank, int n_parts) {
+    if (!ctx) return GELO_EINVAL;
+    if (dtype != GELO_F32 && dtype != GELO_BF16) return fail(ctx, GELO_EINVAL, "unknown dtype %d", (int)dtype);
+    if (n < 1 || d < 8 || d % 8 != 0 || d > (1 << 24)) return fail(ctx, GELO_EINVAL, "n=%d d=%d", n, d);
+    if (rank < 8 || rank % 8 != 0 || rank > GELO_ADAPT_MAX_RANK || n_parts < 1 || n_parts > GELO_ADAPT_MAX_PARTS)
+        return fail(ctx, GELO_ESHAPE, "rank=%d n_parts=%d", rank, n_parts);
+    GELO_HIP(ctx, hipSetDevice(ctx->device));
+    return grow_adapt(ctx, adapt_workspace_bytes(dtype == GELO_BF16, n, d, rank, n_parts));
 }
 
 }  // extern "C"

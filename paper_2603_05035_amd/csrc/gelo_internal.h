@@ -408,6 +408,15 @@ struct RopeAppend {
     SeqBatch batch;
 };
 hipError_t rope_append(const RopeAppend& o, int is_bf16, hipStream_t stream);
+// The same with a cache of 4 bits (fp4.h): there and in the two below, cache's strides of pages and heads are bytes, row_stride is not used.
+hipError_t rope_append_fp4(const RopeAppend& o, int is_bf16, hipStream_t stream);
+struct CacheRows {
+    KvCache cache;
+    SeqBatch batch;
+    void* K; int64_t ldk;              // may be null
+    void* V; int64_t ldv;              // may be null
+};
+hipError_t cache_rows_fp4(const CacheRows& o, int is_bf16, hipStream_t stream);
 // attention.hip
 struct Attention {
     const void* Q; int64_t ldq;
@@ -428,5 +437,28 @@ size_t attention_parts(int is_bf16, int causal, int n_q_heads, int n_kv_heads, i
 size_t attention_workspace_bound(int head_dim);
 hipError_t attention(const Attention& o, int is_bf16, hipStream_t stream);
 hipError_t attention_init();
+// attention_fp4.hip
+bool attention_fp4_fits(const Attention& o, int is_bf16);
+size_t attention_fp4_workspace_bytes(const Attention& o, int is_bf16);
+hipError_t attention_fp4(const Attention& o, int is_bf16, hipStream_t stream);
+hipError_t attention_fp4_init();
+
+// adapt.hip: see gelo_adapt.  Parts of the columns end at part_end[0 ... n_parts - 1], multiples of 16 but for the last; ranks are multiples of 8.
+constexpr int kMostParts = 4;
+struct Adapt {
+    const void* H; int64_t ldh;
+    const void* base; int64_t ldb;
+    void* Z; int64_t ldz;
+    const void* A; int64_t a_stride, lda;        // adapter w, row k: A + w a_stride + k lda
+    const void* B; int64_t b_stride, ldbw;       // adapter w, column j: B + w b_stride + j ldbw
+    const float* scale;                          // may be null
+    const int32_t* which;                        // the adapter of every row
+    int n, d, p, rank, n_parts, n_adapters;
+    int part_end[kMostParts];
+    float* workspace;                            // at least adapt_workspace_bytes
+};
+bool adapt_fits(const Adapt& o);                 // as one launch each
+size_t adapt_workspace_bytes(int is_bf16, int n, int d, int rank, int n_parts);
+hipError_t adapt(const Adapt& o, int is_bf16, hipStream_t stream);
 
 }  // namespace gelo

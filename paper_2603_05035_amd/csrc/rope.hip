@@ -5,7 +5,7 @@
 // bfloat16: 14.1 to 15.9 us = 4.9 to 5.5 TB/s, float 32.9 (4.7; an elementwise kernel over 1 GiB reads and writes at 6.2); one row of each of 64 sequences
 // 4.8, called from Python 6.3, float 7.8.
 // Stores past the caches: 8 x 512 rows of 32/32 heads 37.8 us instead of 42.8, but with the attention behind them 88.5 instead of 83.8.
-#include "gelo_internal.h"
+#include "fp4.h"
 #include "paged.h"
 
 namespace gelo {
@@ -62,6 +62,39 @@ template <> struct Eight<float> {
     __device__ __forceinline__ void set(const float (&v)[8]) { a = f32x4_t{v[0], v[1], v[2], v[3]}; b = f32x4_t{v[4], v[5], v[6], v[7]}; }
 };
 
+// The items x and, rot / 2 components further on, y turn; without `two` the neighbours in x.  angles: cosine and sine of the first pair.
+template <class T>
+__device__ __forceinline__ void turn_item(Eight<T>& x, Eight<T>& y, bool two, const float* angles) {
+    float v[8], cs[16];
+    x.get(v);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        if (!two && t >= 2) break;
+        const f32x4_t c = *reinterpret_cast<const f32x4_t*>(angles + 4 * t);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) cs[4 * t + u] = c[u];
+    }
+    if (two) {
+        float w[8], p[8], q[8];
+        y.get(w);
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+            p[t] = v[t] * cs[2 * t] - w[t] * cs[2 * t + 1];
+            q[t] = w[t] * cs[2 * t] + v[t] * cs[2 * t + 1];
+        }
+        x.set(p);
+        y.set(q);
+    } else {
+        float p[8];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            p[2 * t] = v[2 * t] * cs[2 * t] - v[2 * t + 1] * cs[2 * t + 1];
+            p[2 * t + 1] = v[2 * t + 1] * cs[2 * t] + v[2 * t] * cs[2 * t + 1];
+        }
+        x.set(p);
+    }
+}
+
 // A workgroup takes a row of QKV.  Its work is cut into items of 8 values, or of 8 + 8 where components rot / 2 apart turn together: a
 // head that turns has `per_turned` items, rot / 16 such pairs and then the components behind rot; a value head has d / 8.
 template <class T>
@@ -101,37 +134,7 @@ void rope_append_kernel(RopeAppend o) {
         x.load(in + (int64_t)from * d + col);
         const bool two = turns && !o.pairs;
         if (two) y.load(in + (int64_t)from * d + col + o.rot / 2);
-        if (turns) {
-            float v[8], cs[16];
-            x.get(v);
-            const int at_angle = two ? 2 * col : col;          // float of the table's row
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                if (!two && t >= 2) break;
-                const f32x4_t c = *reinterpret_cast<const f32x4_t*>(angles + at_angle + 4 * t);
-#pragma unroll
-                for (int u = 0; u < 4; ++u) cs[4 * t + u] = c[u];
-            }
-            if (two) {
-                float w[8], p[8], q[8];
-                y.get(w);
-#pragma unroll
-                for (int t = 0; t < 8; ++t) {
-                    p[t] = v[t] * cs[2 * t] - w[t] * cs[2 * t + 1];
-                    q[t] = w[t] * cs[2 * t] + v[t] * cs[2 * t + 1];
-                }
-                x.set(p);
-                y.set(q);
-            } else {
-                float p[8];
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    p[2 * t] = v[2 * t] * cs[2 * t] - v[2 * t + 1] * cs[2 * t + 1];
-                    p[2 * t + 1] = v[2 * t + 1] * cs[2 * t] + v[2 * t] * cs[2 * t + 1];
-                }
-                x.set(p);
-            }
-        }
+        if (turns) turn_item(x, y, two, angles + (two ? 2 * col : col));
         T* out;
         if (!is_value && head < hq) {
             out = (T*)o.Q + (int64_t)row * o.ldq + (int64_t)head * d + col;
@@ -152,6 +155,191 @@ void rope_append_kernel(RopeAppend o) {
     }
 }
 
+// Where a row of the batch lies in a cache of 4 bits, and whether it does.
+struct Fp4Row {
+    int pos, page, in_page;
+    bool beyond, placed, kept;
+};
+__device__ __forceinline__ bool find_row(const SeqBatch& b, const KvCache& kv, int row, Fp4Row* at) {
+    int seq = row, count = 1, j = 0;
+    if (b.row_start) {
+        if (row < b.row_start[0]) return false;
+        seq = sequence_of_row(b.row_start, b.n_seqs, row);
+        if (seq >= b.n_seqs) return false;                   // a row of no sequence is left alone
+        j = row - b.row_start[seq];
+        count = b.row_start[seq + 1] - b.row_start[seq];
+    }
+    at->pos = length_of_sequence(b, seq) - count + j;
+    at->beyond = at->pos >= b.max_kv_len;
+    at->placed = at->pos >= 0 && !at->beyond;
+    at->page = at->placed ? b.page_table[seq * b.table_ld + (at->pos >> kv.page_shift)] : -1;
+    at->kept = at->page >= 0 && at->page < kv.n_pages;
+    at->in_page = at->pos & ((1 << kv.page_shift) - 1);
+    return true;
+}
+// Bytes from the start of a head's piece: of four bytes of codes, 8 values, from byte `byte` of the row on where they lie side by side, and of a block's scale.
+__device__ __forceinline__ int key_codes_at(int d, int in_page, int byte) { return in_page * (d / 2) + byte; }
+__device__ __forceinline__ int value_codes_at(int d, int in_page, int byte) {
+    const int unit = d / 32, piece = byte / unit;
+    return (in_page >> 2) * 2 * d + (4 * piece + (in_page & 3)) * unit + byte - piece * unit;
+}
+__device__ __forceinline__ int scale_at(int d, int page_shift, int in_page, int block, bool is_value) {
+    const int first = fp4_scales_at(d, page_shift), per = d / 32;
+    return is_value ? first + (in_page >> 2) * 4 * per + 4 * block + (in_page & 3) : first + in_page * per + block;
+}
+
+// A workgroup takes a row of QKV.  Keys and values go by items of 8 components, four lanes to a block: each of them loads the components that its own turn
+// with, too, so that any rot / 2 will do.  A turned key is worked out in double, where the two products are exact and their sum as good as, and its code is
+// that value's: in float one in some millions would fall on the other side of the middle between two codes.  Queries turn as in rope_append_kernel, to the bit.
+template <class T>
+__global__ __launch_bounds__(256)
+void rope_append_fp4_kernel(RopeAppend o) {
+    const SeqBatch& b = o.batch;
+    const KvCache& kv = o.cache;
+    const int row = blockIdx.x;
+    Fp4Row at;
+    if (!find_row(b, kv, row, &at)) return;
+    const float* angles = o.table + (int64_t)(at.placed ? at.pos : 0) * o.rot;
+    const int d = kv.head_dim, hq = o.n_q_heads, hkv = kv.n_kv_heads, per_head = d / 8;
+    const T* in = (const T*)o.QKV + (int64_t)row * o.ld;
+    const int kept = at.kept ? 2 * hkv * per_head : 0;       // items of keys and values: a multiple of 4
+    for (int e = threadIdx.x; e < kept; e += 256) {
+        const int head2 = e / per_head, i = e - head2 * per_head, col = 8 * i;
+        const bool is_value = head2 >= hkv;
+        const int head = is_value ? head2 - hkv : head2;
+        const T* from = in + (int64_t)(hq + head2) * d;
+        Eight<T> x;
+        x.load(from + col);
+        float v[8];
+        x.get(v);
+        bool finite = true;
+#pragma unroll
+        for (int t = 0; t < 8; ++t) finite &= fabsf(v[t]) < __builtin_inff();
+        if (!is_value && col < o.rot) {
+            const int half = o.rot / 2;
+            const bool upper = !o.pairs && col >= half;
+            float w[8], cs[16];
+            if (!o.pairs) {
+                Eight<T> y;
+                y.load(from + (upper ? col - half : col + half));
+                y.get(w);
+            }
+            const float* c = angles + (o.pairs ? col : 2 * (upper ? col - half : col));
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                if (o.pairs && t >= 2) break;
+                const f32x4_t z = *reinterpret_cast<const f32x4_t*>(c + 4 * t);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) cs[4 * t + u] = z[u];
+            }
+            double p[8];
+            if (o.pairs) {
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const double c0 = cs[2 * t], s0 = cs[2 * t + 1], a0 = v[2 * t], b0 = v[2 * t + 1];
+                    p[2 * t] = a0 * c0 - b0 * s0;
+                    p[2 * t + 1] = b0 * c0 + a0 * s0;
+                }
+            } else {
+#pragma unroll
+                for (int t = 0; t < 8; ++t) {
+                    const double c0 = cs[2 * t], s0 = upper ? cs[2 * t + 1] : -cs[2 * t + 1];
+                    p[t] = v[t] * c0 + w[t] * s0;
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < 8; ++t) {
+                finite &= fabs(p[t]) < (double)__builtin_inff();
+                v[t] = odd_float(p[t]);
+            }
+        }
+        float top = 0.f;
+#pragma unroll
+        for (int t = 0; t < 8; ++t) top = fmaxf(top, fabsf(v[t]));
+        top = finite ? top : __builtin_nanf("");
+        // the block's: of four lanes; a NaN stays (fmaxf would drop it)
+#pragma unroll
+        for (int by = 1; by < 4; by *= 2) {
+            const float other = __shfl_xor(top, by, 64);
+            top = top != top || other != other ? __builtin_nanf("") : fmaxf(top, other);
+        }
+        const uint32_t byte = top != top ? 255u : fp4_scale_byte(top);
+        const uint32_t codes = top != top ? 0u : fp4_codes(v, fp4_scale(byte));
+        uint8_t* piece = (uint8_t*)(is_value ? kv.v : kv.k) + at.page * kv.page_stride + head * kv.head_stride;
+        if (!is_value || d % 128 == 0) {
+            *reinterpret_cast<uint32_t*>(piece + (is_value ? value_codes_at(d, at.in_page, 4 * i) : key_codes_at(d, at.in_page, 4 * i))) = codes;
+        } else if (d % 64 == 0) {
+#pragma unroll
+            for (int t = 0; t < 4; t += 2) *reinterpret_cast<uint16_t*>(piece + value_codes_at(d, at.in_page, 4 * i + t)) = (uint16_t)(codes >> (8 * t));
+        } else {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) piece[value_codes_at(d, at.in_page, 4 * i + t)] = (uint8_t)(codes >> (8 * t));
+        }
+        if ((i & 3) == 0) piece[scale_at(d, kv.page_shift, at.in_page, i / 4, is_value)] = (uint8_t)byte;
+    }
+    const int turning = o.pairs ? o.rot / 8 : o.rot / 16, per_turned = turning + (d - o.rot) / 8;
+    for (int e = threadIdx.x; e < hq * per_turned; e += 256) {
+        const int head = e / per_turned, i = e - head * per_turned;
+        const bool turns = i < turning, two = turns && !o.pairs;
+        const int col = turns || o.pairs ? 8 * i : o.rot + 8 * (i - turning);
+        Eight<T> x, y;
+        x.load(in + (int64_t)head * d + col);
+        if (two) y.load(in + (int64_t)head * d + col + o.rot / 2);
+        if (turns) turn_item(x, y, two, angles + (two ? 2 * col : col));
+        if (!at.placed) {
+            float v[8];
+#pragma unroll
+            for (int t = 0; t < 8; ++t) v[t] = at.beyond ? __builtin_nanf("") : 0.f;
+            x.set(v);
+            y = x;
+        }
+        T* out = (T*)o.Q + (int64_t)row * o.ldq + (int64_t)head * d + col;
+        x.store(out);
+        if (two) y.store(out + o.rot / 2);
+    }
+}
+
+// Rows of a cache of 4 bits as values: 8 to an item.
+template <class T>
+__global__ __launch_bounds__(256)
+void cache_rows_fp4_kernel(CacheRows o) {
+    const KvCache& kv = o.cache;
+    const int row = blockIdx.x;
+    Fp4Row at;
+    if (!find_row(o.batch, kv, row, &at)) return;
+    const int d = kv.head_dim, hkv = kv.n_kv_heads, per_head = d / 8;
+    for (int e = threadIdx.x; e < 2 * hkv * per_head; e += 256) {
+        const int head2 = e / per_head, i = e - head2 * per_head;
+        const bool is_value = head2 >= hkv;
+        const int head = is_value ? head2 - hkv : head2;
+        T* out = (T*)(is_value ? o.V : o.K);
+        if (!out) continue;
+        float v[8];
+#pragma unroll
+        for (int t = 0; t < 8; ++t) v[t] = at.pos < 0 ? 0.f : __builtin_nanf("");
+        if (at.kept) {
+            const uint8_t* piece = (const uint8_t*)(is_value ? kv.v : kv.k) + at.page * kv.page_stride + head * kv.head_stride;
+            uint32_t codes = 0;
+            if (!is_value || d % 128 == 0) {
+                codes = *reinterpret_cast<const uint32_t*>(piece + (is_value ? value_codes_at(d, at.in_page, 4 * i) : key_codes_at(d, at.in_page, 4 * i)));
+            } else {
+#pragma unroll
+                for (int t = 0; t < 4; ++t) codes |= (uint32_t)piece[value_codes_at(d, at.in_page, 4 * i + t)] << (8 * t);
+            }
+            const float scale = fp4_scale(piece[scale_at(d, kv.page_shift, at.in_page, i / 4, is_value)]);
+            static_for<4>([&](auto ic) {
+                constexpr int t = decltype(ic)::value;
+                const uint32_t pair = fp4_pair<t>(codes, scale);
+                v[2 * t] = __uint_as_float(pair << 16);
+                v[2 * t + 1] = __uint_as_float(pair & 0xFFFF0000u);
+            });
+        }
+        Eight<T> x;
+        x.set(v);
+        x.store(out + (int64_t)row * (is_value ? o.ldv : o.ldk) + head * d + 8 * i);
+    }
+}
+
 }  // namespace
 
 hipError_t rope_table(const RopeTable& o, hipStream_t stream) {
@@ -163,6 +351,18 @@ hipError_t rope_table(const RopeTable& o, hipStream_t stream) {
 hipError_t rope_append(const RopeAppend& o, int is_bf16, hipStream_t stream) {
     if (is_bf16) hipLaunchKernelGGL(rope_append_kernel<uint16_t>, dim3(o.batch.n_rows), dim3(256), 0, stream, o);
     else hipLaunchKernelGGL(rope_append_kernel<float>, dim3(o.batch.n_rows), dim3(256), 0, stream, o);
+    return hipGetLastError();
+}
+
+hipError_t rope_append_fp4(const RopeAppend& o, int is_bf16, hipStream_t stream) {
+    if (is_bf16) hipLaunchKernelGGL(rope_append_fp4_kernel<uint16_t>, dim3(o.batch.n_rows), dim3(256), 0, stream, o);
+    else hipLaunchKernelGGL(rope_append_fp4_kernel<float>, dim3(o.batch.n_rows), dim3(256), 0, stream, o);
+    return hipGetLastError();
+}
+
+hipError_t cache_rows_fp4(const CacheRows& o, int is_bf16, hipStream_t stream) {
+    if (is_bf16) hipLaunchKernelGGL(cache_rows_fp4_kernel<uint16_t>, dim3(o.batch.n_rows), dim3(256), 0, stream, o);
+    else hipLaunchKernelGGL(cache_rows_fp4_kernel<float>, dim3(o.batch.n_rows), dim3(256), 0, stream, o);
     return hipGetLastError();
 }
 

@@ -1,0 +1,134 @@
+"""The host's side of the cache of 4 bits and of adapters: what the binding makes of tensors and refuses, and what the library reckons from sizes.  Nothing
+here launches a kernel or needs a GPU."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2603_05035_amd import binding as g
+
+
+class OnGpu(torch.Tensor):
+    """A host tensor that says it lives on the GPU: for code that looks at shapes and strides only."""
+
+    @property
+    def is_cuda(self):
+        return True
+
+
+def on_gpu(t):
+    return t.as_subclass(OnGpu)
+
+
+def zeros(*shape, dtype=torch.bfloat16):
+    return on_gpu(torch.zeros(shape, dtype=dtype))
+
+
+def test_bytes_of_a_piece():
+    lib = g.load_library()
+    for page, d in ((16, 32), (16, 64), (64, 96), (128, 128), (16, 256), (1 << 20, 256)):
+        assert g.gelo_fp4_page_bytes(page, d) == page * d * 17 // 32
+    v = ctypes.c_size_t(5)
+    for page, d, want in ((0, 64, "GELO_EINVAL"), (16, 0, "GELO_EINVAL"), (8, 64, "GELO_ESHAPE"), (48, 64, "GELO_ESHAPE"), (16, 48, "GELO_ESHAPE"),
+                          (1 << 24, 32, "GELO_ESHAPE")):
+        assert g.STATUS_NAMES[lib.gelo_fp4_page_bytes(page, d, ctypes.byref(v))] == want, (page, d)
+    assert v.value == 5 and g.STATUS_NAMES[lib.gelo_fp4_page_bytes(16, 64, None)] == "GELO_EINVAL"
+    with pytest.raises(g.GeloError):
+        g.gelo_fp4_page_bytes(24, 64)
+
+
+def test_a_cache_s_strides_are_those_of_its_tensors():
+    piece = g.gelo_fp4_page_bytes(16, 64)
+    s = g.KvCacheFp4(zeros(5, 3, piece, dtype=torch.uint8), zeros(5, 3, piece, dtype=torch.uint8), 16, 64).struct
+    assert (s.n_pages, s.n_kv_heads, s.page_rows, s.head_dim, s.page_stride, s.head_stride) == (5, 3, 16, 64, 3 * piece, piece)
+    both = zeros(5, 2, 3, piece + 16, dtype=torch.uint8)
+    s = g.KvCacheFp4(both[:, 0, :, :piece], both[:, 1, :, :piece], 16, 64).struct
+    assert (s.page_stride, s.head_stride) == (6 * (piece + 16), piece + 16)
+    heads_first = zeros(3, 5, piece, dtype=torch.uint8).permute(1, 0, 2)
+    s = g.KvCacheFp4(heads_first, heads_first, 16, 64).struct
+    assert (s.page_stride, s.head_stride) == (piece, 5 * piece)
+    one = zeros(1, 1, piece, dtype=torch.uint8)
+    assert g.KvCacheFp4(one, one, 16, 64).struct.head_stride % 16 == 0
+
+
+def test_caches_that_are_refused():
+    piece = g.gelo_fp4_page_bytes(16, 64)
+    good = zeros(5, 3, piece, dtype=torch.uint8)
+    for K, V in ((good, zeros(5, 3, piece)), (good, zeros(4, 3, piece, dtype=torch.uint8)), (good[..., :-1], good[..., :-1]), (torch.zeros_like(good).as_subclass(torch.Tensor), good),
+                 (good, zeros(3, 5, piece, dtype=torch.uint8).permute(1, 0, 2)), (zeros(5, 3, 2 * piece, dtype=torch.uint8)[..., ::2],) * 2):
+        with pytest.raises(ValueError):
+            g.KvCacheFp4(K, V, 16, 64)
+    with pytest.raises(g.GeloError):
+        g.KvCacheFp4(good, good, 16, 48)
+
+
+def test_adapters_are_described_by_their_tensors():
+    A, B = zeros(7, 24, 64), zeros(7, 80, 8)
+    s = g.Adapters(A, B, part_ends=[16, 48, 80]).struct
+    assert (s.n_adapters, s.rank, s.n_parts, list(s.part_end)[:3]) == (7, 8, 3, [16, 48, 80])
+    assert (s.a_stride, s.lda, s.b_stride, s.ldb, s.scale) == (24 * 64, 64, 640, 8, None)
+    wide = zeros(7, 2, 40, 72)
+    s = g.Adapters(wide[:, 0, :16, :64], zeros(7, 32, 24)[..., :16], scale=zeros(7, dtype=torch.float32)).struct
+    assert (s.rank, s.n_parts, s.part_end[0], s.a_stride, s.lda, s.b_stride, s.ldb) == (16, 1, 32, 2 * 40 * 72, 72, 32 * 24, 24)
+    s = g.Adapters(A.expand(7, 24, 64)[:1].expand(3, 24, 64), zeros(3, 80, 8), part_ends=(16, 48, 80)).struct
+    assert s.a_stride == 0                                   # the same A for all
+
+
+def test_adapters_that_are_refused():
+    A, B = zeros(7, 24, 64), zeros(7, 80, 8)
+    for bad in (dict(A=zeros(6, 24, 64)), dict(A=zeros(7, 16, 64)), dict(A=zeros(7, 24, 64, dtype=torch.float32)), dict(part_ends=[16, 48, 72]), dict(part_ends=[]),
+                dict(A=zeros(7, 40, 64), part_ends=[16, 32, 48, 64, 80]), dict(A=torch.zeros((7, 24, 64), dtype=torch.bfloat16)),
+                dict(A=zeros(7, 24, 128)[..., ::2]), dict(B=zeros(7, 8, 80).transpose(1, 2)), dict(scale=zeros(7)), dict(scale=zeros(6, dtype=torch.float32)),
+                dict(scale=zeros(14, dtype=torch.float32)[::2]), dict(A=zeros(24, 64))):
+        with pytest.raises(ValueError):
+            g.Adapters(**{"A": A, "B": B, "part_ends": [16, 48, 80], **bad})
+    with pytest.raises(TypeError):
+        g.Adapters(zeros(7, 24, 64, dtype=torch.float16), zeros(7, 80, 8, dtype=torch.float16), part_ends=[16, 48, 80])
+
+
+def test_calls_of_adapters_that_the_binding_refuses():
+    """Before anything reaches the library (whose context is none here)."""
+    ad = g.Adapters(zeros(7, 24, 64), zeros(7, 80, 8), part_ends=[16, 48, 80])
+    H, Z, which = zeros(5, 64), zeros(5, 80), zeros(5, dtype=torch.int32)
+    good = dict(H=H, which=which, Z=Z, base=None)
+    for bad, kind in ((dict(H=zeros(5, 72)), g.GeloError), (dict(Z=zeros(4, 80)), g.GeloError), (dict(base=zeros(5, 88)), g.GeloError),
+                      (dict(H=zeros(5, 64, dtype=torch.float32)), g.GeloError), (dict(base=zeros(5, 80, dtype=torch.float32)), g.GeloError),
+                      (dict(which=zeros(4, dtype=torch.int32)), ValueError), (dict(which=zeros(5, dtype=torch.int64)), ValueError),
+                      (dict(which=torch.zeros(5, dtype=torch.int32)), ValueError), (dict(H=torch.zeros((5, 64), dtype=torch.bfloat16)), ValueError),
+                      (dict(Z=zeros(80, 5).t()), ValueError)):
+        with pytest.raises(kind):
+            g.gelo_adapt(None, adapters=ad, stream=0, **{**good, **bad})
+    with pytest.raises(g.GeloError):                         # no context
+        g.gelo_adapt(None, adapters=ad, stream=0, **good)
+
+
+def test_calls_on_a_cache_of_4_bits_that_the_binding_refuses():
+    piece = g.gelo_fp4_page_bytes(16, 64)
+    pool = zeros(8, 2, piece, dtype=torch.uint8)
+    cache = g.KvCacheFp4(pool, pool.clone(), 16, 64)
+    batch = g.SeqBatch(zeros(3, dtype=torch.int32), zeros(3, 2, dtype=torch.int32), 32)
+    Q, QKV = zeros(3, 256), zeros(3, 512)
+    for call, kind in ((lambda: g.gelo_attention_fp4(None, Q, zeros(3, 256, dtype=torch.float32), 4, cache, batch, 1.0, stream=0), g.GeloError),
+                       (lambda: g.gelo_attention_fp4(None, Q, zeros(3, 128), 4, cache, batch, 1.0, stream=0), g.GeloError),
+                       (lambda: g.gelo_attention_fp4(None, Q, zeros(3, 256), 2, cache, batch, 1.0, stream=0), g.GeloError),
+                       (lambda: g.gelo_attention_fp4(None, zeros(4, 256), zeros(4, 256), 4, cache, batch, 1.0, stream=0), g.GeloError),
+                       (lambda: g.gelo_attention_fp4(None, Q, zeros(3, 256), 4, cache, g.SeqBatch(batch.kv_len, batch.page_table, 33), 1.0, stream=0), g.GeloError),
+                       (lambda: g.gelo_rope_append_fp4(None, zeros(3, 520), 4, cache, batch, Q=Q, stream=0), g.GeloError),
+                       (lambda: g.gelo_rope_append_fp4(None, QKV, 4, cache, batch, Q=zeros(3, 256, dtype=torch.float32), stream=0), ValueError),
+                       (lambda: g.gelo_rope_append_fp4(None, QKV, 4, cache, batch, Q=Q, table=zeros(32, 32, 2), rot_dim=64, stream=0), ValueError),
+                       (lambda: g.gelo_rope_append_fp4(None, torch.zeros((3, 512), dtype=torch.bfloat16), 4, cache, batch, Q=Q, stream=0), ValueError),
+                       (lambda: g.gelo_cache_rows_fp4(None, cache, batch, stream=0), ValueError),
+                       (lambda: g.gelo_cache_rows_fp4(None, cache, batch, zeros(3, 64), stream=0), ValueError),
+                       (lambda: g.gelo_cache_rows_fp4(None, cache, batch, zeros(3, 128), zeros(3, 128, dtype=torch.float32), stream=0), ValueError),
+                       (lambda: g.gelo_cache_rows_fp4(None, cache, batch, zeros(4, 128), stream=0), g.GeloError)):
+        with pytest.raises(kind):
+            call()
+
+
+def test_every_call_wants_a_context():
+    lib, P = g.load_library(), ctypes.c_void_p
+    assert lib.gelo_rope_append_fp4(None, 1, 4, P(16), 512, None, None, 0, 0, None, 0, P(16), 256, None) == 1
+    assert lib.gelo_cache_rows_fp4(None, 1, None, None, P(16), 128, None, 0, None) == 1
+    assert lib.gelo_attention_fp4(None, 1, 4, P(16), 256, None, None, 1.0, 1, P(16), 256, None) == 1
+    assert lib.gelo_adapt(None, 1, 4, 64, 64, P(16), 64, None, P(16), P(16), 64, P(16), 64, None) == 1
+    assert lib.gelo_reserve_adapt(None, 1, 4, 64, 8, 1) == 1
