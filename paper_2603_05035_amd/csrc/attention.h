@@ -47,6 +47,25 @@ __device__ __forceinline__ V read_row(const void* p) {
     else return *reinterpret_cast<const V*>(p);
 }
 
+// words side by side: 2, 3, 4 or 8
+template <int W, bool PAST>
+__device__ __forceinline__ void read_words(const uint8_t* p, uint32_t (&w)[W]) {
+    if constexpr (W == 2) {
+        const u32x2_t x = read_row<u32x2_t, PAST>(p);
+        w[0] = x[0]; w[1] = x[1];
+    } else if constexpr (W == 3) {
+        const u32x3_t x = read_row<u32x3_t, PAST>(p);
+        w[0] = x[0]; w[1] = x[1]; w[2] = x[2];
+    } else {
+#pragma unroll
+        for (int i = 0; i < W; i += 4) {
+            const u32x4_t x = read_row<u32x4_t, PAST>(p + 4 * i);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) w[i + u] = x[u];
+        }
+    }
+}
+
 // the place of the part that chunk `chunk` makes of head `head` of a sequence's row i
 __device__ __forceinline__ int64_t part_of(const AttnArgs& a, int chunk, int seq, int i, int head) {
     return (((int64_t)chunk * a.b.n_seqs + seq) * a.b.max_rows + i) * a.n_q_heads + head;
@@ -168,6 +187,24 @@ template <class T, int D>
 hipError_t join_parts(const AttnArgs& a, hipStream_t stream) {
     if (a.n_chunks <= 4) return join<T, D, 1>(a, stream);
     return a.n_chunks <= 16 ? join<T, D, 4>(a, stream) : join<T, D, D == 256 ? 4 : 8>(a, stream);
+}
+
+// Which kernel, and how the cache is cut: chunks of `chunk` keys, n_chunks of them to the longest sequence.
+struct Plan { bool prompt, shared, paired, past, by_head; int chunk, n_chunks; int64_t col_tiles, workgroups; };
+constexpr int64_t kMostWorkgroups = kMostThreads / 256;      // all kernels here have workgroups of 256
+constexpr int kCus = 256;
+constexpr int kFewTarget = 512, kFewLeast = 256;         // workgroups that fill the chip (two to a CU), keys to a chunk at least
+constexpr int kPromptTarget = 512, kPromptLeast = 128;
+
+// The cache cut `cuts` times, rounded to whole steps of both kernels.
+void cut(Plan* p, int max_kv_len, int64_t cuts) {
+    p->chunk = (int)round_up((max_kv_len + cuts - 1) / cuts, 128);
+    p->n_chunks = (int)(((int64_t)max_kv_len + p->chunk - 1) / p->chunk);
+}
+// The join: a launch behind another one, and the parts written and read.
+double join_us(const Attention& o, const Plan& p) {
+    const double rows = (double)o.batch.n_seqs * o.batch.max_rows;
+    return p.n_chunks == 1 ? 0.0 : 5.0 + 8.0 * p.n_chunks * (rows < o.batch.n_rows ? rows : o.batch.n_rows) * o.n_q_heads * o.cache.head_dim / 4e6;
 }
 
 }  // namespace

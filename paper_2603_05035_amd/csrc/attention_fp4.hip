@@ -10,33 +10,13 @@
 // column; the weights are at once the operand of O^T = V^T P^T.  Lane (g, c) = (lane / 16, lane % 16).  S^T, 16 keys: the lane's operand is a quarter of key c,
 // components (D / 4) g ..., step s of the product takes 8 of them, and of column c's query alike.  It then holds the scores of keys 4 g + r.  O^T: the
 // operand's slot 4 t + r of the lane is key 16 t + 4 g + r; the lane has components (D / 16) c + j of it, instruction j takes one of each.
-#include "attention.h"
-#include "fp4.h"
+#include "attention_prompt.h"
 
 namespace gelo {
 namespace {
 
 typedef uint16_t u16_t;
 constexpr int kFewWaves = 4;
-
-// D / 32 words side by side
-template <int W, bool PAST>
-__device__ __forceinline__ void read_words(const uint8_t* p, uint32_t (&w)[W]) {
-    if constexpr (W == 2) {
-        const u32x2_t x = read_row<u32x2_t, PAST>(p);
-        w[0] = x[0]; w[1] = x[1];
-    } else if constexpr (W == 3) {
-        const u32x3_t x = read_row<u32x3_t, PAST>(p);
-        w[0] = x[0]; w[1] = x[1]; w[2] = x[2];
-    } else {
-#pragma unroll
-        for (int i = 0; i < W; i += 4) {
-            const u32x4_t x = read_row<u32x4_t, PAST>(p + 4 * i);
-#pragma unroll
-            for (int u = 0; u < 4; ++u) w[i + u] = x[u];
-        }
-    }
-}
 
 // 32 keys a half of a step
 template <class T, int D, bool PAST>
@@ -375,24 +355,32 @@ void attention_few_fp4_kernel(AttnArgs a) {
     }
 }
 
-// How the cache is cut: chunks of `chunk` keys, n_chunks of them to the longest sequence.
-struct Plan { bool past; int chunk, n_chunks; int64_t col_tiles, workgroups; };
-constexpr int64_t kMostWorkgroups = kMostThreads / 256;
-constexpr int kFewTarget = 512, kFewLeast = 256;         // workgroups that fill the chip (two to a CU), keys to a chunk at least
+static_assert(64 * kFewWaves <= 256 && 64 * kPromptWaves <= 256, "workgroups as kMostWorkgroups has them");
 
-Plan plan_of(const Attention& o, int) {
+Plan plan_few(const Attention& o, int64_t columns, double* us) {
     Plan p;
-    const int64_t columns = (int64_t)o.batch.max_rows * (o.n_q_heads / o.cache.n_kv_heads);
+    p.prompt = p.shared = p.paired = p.past = p.by_head = false;
     p.col_tiles = (columns + 15) / 16;
     const int64_t tiles = (int64_t)o.batch.n_seqs * o.cache.n_kv_heads * p.col_tiles;
     const int64_t most = (o.batch.max_kv_len + kFewLeast - 1) / kFewLeast;
-    int64_t cuts = kFewTarget / tiles;
-    cuts = cuts < 1 ? 1 : cuts < most ? cuts : most;
-    p.chunk = (int)round_up((o.batch.max_kv_len + cuts - 1) / cuts, 256);
-    p.n_chunks = (int)(((int64_t)o.batch.max_kv_len + p.chunk - 1) / p.chunk);
+    const int64_t cuts = kFewTarget / tiles;
+    cut(&p, o.batch.max_kv_len, cuts < 1 ? 1 : cuts < most ? cuts : most);
     p.workgroups = tiles * p.n_chunks;
     p.past = p.col_tiles == 1 && 17.0 / 16 * tiles * o.batch.max_kv_len * o.cache.head_dim > 100e6;
+    // a wave's step of 64 keys takes its SIMD 1.3 us at a width of 128, and a trip to memory 1.5
+    const double rounds = (double)((p.workgroups + kFewTarget - 1) / kFewTarget), steps = (p.chunk + 255) / 256;
+    const double work = p.workgroups * steps * 4 / 1024 * 1.3 * o.cache.head_dim / 128, trips = rounds * steps * 1.5;
+    *us = 4.0 * rounds + (work > trips ? work : trips) + join_us(o, p);
     return p;
+}
+
+Plan plan_of(const Attention& o, int is_bf16) {
+    const int64_t columns = (int64_t)o.batch.max_rows * (o.n_q_heads / o.cache.n_kv_heads);
+    double few_us, prompt_us;
+    const Plan few = plan_few(o, columns, &few_us);
+    if (!is_bf16 || columns <= 16) return few;
+    const Plan prompt = plan_prompt(o, columns, &prompt_us);
+    return few_us < prompt_us ? few : prompt;
 }
 
 int64_t parts(const Attention& o, const Plan& p) {
@@ -409,12 +397,17 @@ hipError_t launch(const Attention& o, hipStream_t stream) {
     a.scale2 = o.scale == 0.f ? 1e-30f : fabsf(a.scale2s);      // (-inf, a hidden score, times 0 would be NaN)
     a.flip = o.scale < 0.f ? 0x80008000u : 0u;
     a.causal = o.causal;
-    a.chunk = p.chunk; a.n_chunks = p.n_chunks; a.col_tiles = (int)p.col_tiles; a.paired = 0; a.by_head = 0;
+    a.chunk = p.chunk; a.n_chunks = p.n_chunks; a.col_tiles = (int)p.col_tiles; a.paired = p.paired; a.by_head = 0;
     a.kv = o.cache; a.b = o.batch;
     a.part_o = o.workspace;
     a.part_ml = p.n_chunks == 1 ? nullptr : o.workspace + parts(o, p) * D;
+    if constexpr (sizeof(T) == 2) {
+        if (p.prompt)
+            hipLaunchKernelGGL((attention_prompt_kernel<D, true>), dim3((unsigned)p.workgroups), dim3(64 * kPromptWaves), (size_t)prompt_lds<D>(), stream, a);
+    }
     const dim3 few((unsigned)(p.col_tiles * p.n_chunks), (unsigned)o.cache.n_kv_heads, (unsigned)o.batch.n_seqs);
-    if (p.past) hipLaunchKernelGGL((attention_few_fp4_kernel<T, D, true>), few, dim3(64 * kFewWaves), 0, stream, a);
+    if (p.prompt) {}
+    else if (p.past) hipLaunchKernelGGL((attention_few_fp4_kernel<T, D, true>), few, dim3(64 * kFewWaves), 0, stream, a);
     else hipLaunchKernelGGL((attention_few_fp4_kernel<T, D, false>), few, dim3(64 * kFewWaves), 0, stream, a);
     const hipError_t e = hipGetLastError();
     return e != hipSuccess || p.n_chunks == 1 ? e : join_parts<T, D>(a, stream);
@@ -441,8 +434,28 @@ bool attention_fp4_fits(const Attention& o, int is_bf16) {
 
 size_t attention_fp4_workspace_bytes(const Attention& o, int is_bf16) { return parts(o, plan_of(o, is_bf16)) * (o.cache.head_dim + 2) * sizeof(float); }
 
+// Which way a call of these sizes goes, as attention_way says it.
+int attention_fp4_way(int is_bf16, int causal, int n_q_heads, int n_kv_heads, int head_dim, int n_seqs, int n_rows, int max_rows, int max_kv_len) {
+    Attention o = {};
+    o.causal = causal != 0; o.n_q_heads = n_q_heads;
+    o.cache.n_kv_heads = n_kv_heads; o.cache.head_dim = head_dim;
+    o.batch.n_seqs = n_seqs; o.batch.n_rows = n_rows; o.batch.max_rows = rows_bound(max_rows, n_rows); o.batch.max_kv_len = max_kv_len;
+    if (!attention_fp4_fits(o, is_bf16)) return -1;
+    const Plan p = plan_of(o, is_bf16);
+    return (p.prompt ? p.paired ? 2 : 1 : 0) + (p.n_chunks > 1 ? 4 : 0);
+}
+
 hipError_t attention_fp4(const Attention& o, int is_bf16, hipStream_t stream) { return is_bf16 ? of_width<uint16_t>(o, stream) : of_width<float>(o, stream); }
 
-hipError_t attention_fp4_init() { return hipSuccess; }
+hipError_t attention_fp4_init() {
+    const void* kernels[] = {(const void*)&attention_prompt_kernel<64, true>, (const void*)&attention_prompt_kernel<96, true>,
+                             (const void*)&attention_prompt_kernel<128, true>, (const void*)&attention_prompt_kernel<256, true>};
+    const int bytes[] = {prompt_lds<64>(), prompt_lds<96>(), prompt_lds<128>(), prompt_lds<256>()};
+    for (int i = 0; i < 4; ++i) {
+        const hipError_t e = hipFuncSetAttribute(kernels[i], hipFuncAttributeMaxDynamicSharedMemorySize, bytes[i]);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
 
 }  // namespace gelo
