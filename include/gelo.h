@@ -407,13 +407,13 @@ typedef struct gelo_adapters {
 /* Z[i, j] = base[i, j] + scale[w] sum_r (sum_k H[i, k] A_w[r, k]) B_w[j, r], r over the rank rows of j's part, w = which[i] (DEVICE, n 32-bit
  * integers).  A row whose number is no adapter's (-1, say) gets base[i].  H: n x d (ldh), base, Z: n x p (ldb, ldz) of type `dtype`; Z may be base itself, and
  * shares no memory with H or with base otherwise.  Sums are float, one rounding at the end; GELO_BF16 holds the inner sum in 16 bits for the second product.  A
- * NaN or infinity in H, base or an adapter reaches only the rows it belongs to.  Rows in any order; those of one adapter side by side take least.
+ * NaN or infinity in H, base or an adapter reaches only the rows it belongs to.  Rows in any order.
  * The inner sums go through float workspace of the context (gelo_reserve_adapt sizes it ahead; else the first call that needs more allocates, and what it replaces stays
  * until the context ends): calls on one context must not overlap in time on different streams. */
 gelo_status gelo_adapt(gelo_ctx* ctx, gelo_dtype dtype, int n, int d, int p, const void* H, int64_t ldh, const gelo_adapters* adapters, const int32_t* which,
                        const void* base, int64_t ldb, void* Z, int64_t ldz, void* stream);
-/* Allocates that workspace for a call of these sizes: gelo_adapt then allocates nothing. */
-gelo_status gelo_reserve_adapt(gelo_ctx* ctx, gelo_dtype dtype, int n, int d, int rank, int n_parts);
+/* Allocates that workspace for calls of up to so many rows, ranks, parts and adapters: gelo_adapt then allocates nothing. */
+gelo_status gelo_reserve_adapt(gelo_ctx* ctx, int n, int rank, int n_parts, int n_adapters);
 
 /* Test hook: copies the secrets of a mixing object to caller DEVICE buffers (any may be NULL):
  * A and A_inv as float n x n (dense), S as float k_shield x d (dense; valid after gelo_mix).

@@ -93,7 +93,7 @@ SIGNATURES = {
     "gelo_attention_fp4": (c_int, [c_void_p, c_int, c_int, c_void_p, c_int64, c_void_p, c_void_p, c_float, c_int,
                                    c_void_p, c_int64, c_void_p]),
     "gelo_adapt": (c_int, [c_void_p, c_int, c_int, c_int, c_int, c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_void_p]),
-    "gelo_reserve_adapt": (c_int, [c_void_p, c_int, c_int, c_int, c_int, c_int]),
+    "gelo_reserve_adapt": (c_int, [c_void_p, c_int, c_int, c_int, c_int]),
     "gelo_debug_philox_words": (c_int, [c_void_p, c_uint32, c_uint32, c_uint64, c_uint32, c_uint32, c_void_p, c_void_p]),
     "gelo_mixing_export_table": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p]),
     "gelo_qkv_forward": (c_int, [c_void_p, c_int, c_int, c_int, c_int, c_int, c_int, c_void_p, c_void_p, c_float,
@@ -638,8 +638,8 @@ def gelo_adapt(ctx, H: torch.Tensor, adapters: Adapters, which: torch.Tensor, Z:
     return Z
 
 
-def gelo_reserve_adapt(ctx, dtype: int, n: int, d: int, rank: int, n_parts: int = 1) -> None:
-    _check(ctx, load_library().gelo_reserve_adapt(ctx, dtype, n, d, rank, n_parts))
+def gelo_reserve_adapt(ctx, n: int, rank: int, n_parts: int, n_adapters: int) -> None:
+    _check(ctx, load_library().gelo_reserve_adapt(ctx, n, rank, n_parts, n_adapters))
 
 
 def gelo_debug_quantize_rows_fp8(ctx, U: torch.Tensor, stream=None):

@@ -1,8 +1,11 @@
 // Low-rank adapters of many requests beside one projection: Z[i] = base[i] + scale_w (H[i] A_w^T) B_w^T, w = which[i] the adapter of row i.  Parts of the
 // columns (the queries, keys and values of a fused projection) have an A each: rows k rank ... (k + 1) rank - 1 of A_w belong to part k.
 //
-// Two launches: T = H A_w^T for all parts, in float, cut over d where rows are few; then base + scale T B_w^T.  Bound by the bytes of H, base, Z and the
-// adapters.  Rows go 16 to a tile, one of a tile's adapters after another: rows of other adapters count as zeros there, and their results are dropped.
+// T = H A_w^T for all parts, in float, d cut over workgroups whose sums lie side by side; then base + scale T B_w^T.  Bound by the bytes of H, base, Z and the
+// adapters.
+//   few rows   two launches.  A tile is 16 rows as they come; a tile's adapters go side by side, rows of others count as zeros and their results are dropped.
+//   many rows  three: the first puts the rows of an adapter together, 64 to a group (rows that are so already stay in runs); then a tile is a group.
+// A row's sums do not go by the rows around it: each is a column of a matrix instruction.
 //
 // bfloat16 takes v_mfma_f32_16x16x32_bf16, and the float T of the second product as two bfloat16, 16 bits of it: with one, its rounding would show where what the
 // adapter adds is as large as base.  float takes v_mfma_f32_16x16x4_f32.
@@ -40,9 +43,21 @@ template <class T> __device__ __forceinline__ typename Lane<T>::piece_t none() {
 struct AdaptArgs {
     Adapt o;
     int all;                             // rank n_parts: values of a row of T
-    int slots, splits, steps;            // workgroups that share a tile's adapters; parts of d, `steps` steps of 4 PER values each
-    int first_group[kMostParts + 1];     // groups of 64 columns before a part
+    int splits, steps;                   // parts of d, `steps` steps of 4 PER values each
+    int wide;                            // columns of a workgroup of the second product: a multiple of 64
+    int first_block[kMostParts + 1];     // blocks of so many columns before a part
+    float* t;                            // [split][row][all]
+    // many rows
+    int* order;                          // rows, those of one adapter side by side
+    int4* groups;                        // of each group: its adapter (-1: none), where it begins in `order`, its rows; null: rows as they come
+    int* n_groups;
 };
+
+__device__ __forceinline__ int part_of_block(const AdaptArgs& a, int block) {
+    int part = 0;
+    while (block >= a.first_block[part + 1]) ++part;
+    return part;
+}
 
 // The adapters of a tile of 16 rows, one after the other: `left` has a bit for every row still to come.
 struct Tile {
@@ -63,16 +78,16 @@ struct Tile {
     }
 };
 
-// T[split][row][rank of all parts].  A workgroup: the adapters of one tile from `slot` on, 64 rows of A, one part of d, whose steps its waves share out.
+// Few rows, the first product.  A workgroup: one of the adapters of a tile, 64 rows of A, one part of d, whose steps its waves share out.
 template <class T>
 __global__ __launch_bounds__(64 * kWaves)
-void adapt_down_kernel(AdaptArgs a) {
+void adapt_few_down_kernel(AdaptArgs a) {
     typedef Lane<T> L;
     typedef typename L::piece_t piece_t;
     constexpr int STEP = 4 * L::PER, RT = 4, AHEAD = 4;
     const Adapt& o = a.o;
     __shared__ f32x4_t sums[kWaves][RT][64];
-    const int tile = blockIdx.x / a.slots, slot = blockIdx.x - tile * a.slots, split = blockIdx.y, first_rank = blockIdx.z * 16 * RT;
+    const int tile = blockIdx.x >> 4, slot = blockIdx.x & 15, split = blockIdx.y, first_rank = blockIdx.z * 16 * RT;
     const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int tiles = min((a.all - first_rank + 15) / 16, RT);
     Tile rows(o, tile);
@@ -81,7 +96,7 @@ void adapt_down_kernel(AdaptArgs a) {
     const T* h = (const T*)o.H + row * o.ldh;
     for (int k = 0; rows.left; ++k) {
         const int w = rows.next();
-        if (k % a.slots != slot) continue;
+        if (k != slot) continue;
         const bool live = rows.live;
         const T* A = (const T*)o.A + w * o.a_stride;
         f32x4_t sum[RT];
@@ -116,18 +131,19 @@ void adapt_down_kernel(AdaptArgs a) {
 #pragma unroll
             for (int i = 1; i < kWaves; ++i) all += sums[i][wave][lane];
             const int r = first_rank + 16 * wave + 4 * g;
-            if (r < a.all) *reinterpret_cast<f32x4_t*>(o.workspace + ((int64_t)split * o.n + row) * a.all + r) = all;
+            if (r < a.all) *reinterpret_cast<f32x4_t*>(a.t + ((int64_t)split * o.n + row) * a.all + r) = all;
         }
-        __syncthreads();
+        return;
     }
 }
 
-// 4 PER / 4 = PER rank values of a lane, summed over the parts of d and scaled, as the operand's pieces
+// A row's PER values of T from `t` on, summed over the parts of d and scaled
 template <class T>
 __device__ __forceinline__ void read_t(const AdaptArgs& a, const float* t, float scale, float (&v)[Lane<T>::PER]) {
     constexpr int PER = Lane<T>::PER;
 #pragma unroll
     for (int e = 0; e < PER; ++e) v[e] = 0.f;
+#pragma unroll 4
     for (int s = 0; s < a.splits; ++s) {
 #pragma unroll
         for (int e = 0; e < PER; e += 4) {
@@ -139,7 +155,7 @@ __device__ __forceinline__ void read_t(const AdaptArgs& a, const float* t, float
 #pragma unroll
     for (int e = 0; e < PER; ++e) v[e] *= scale;
 }
-// of bfloat16 the upper part, or what it leaves
+// as an operand: of bfloat16 the upper part, or (rest) what it leaves
 __device__ __forceinline__ bf16x8_t piece_of(const float (&v)[8], bool rest) {
     bf16x8_t f;
 #pragma unroll
@@ -152,16 +168,20 @@ __device__ __forceinline__ bf16x8_t piece_of(const float (&v)[8], bool rest) {
 }
 __device__ __forceinline__ f32x4_t piece_of(const float (&v)[4], bool) { return f32x4_t{v[0], v[1], v[2], v[3]}; }
 
-template <class T> struct Sixteen;                           // 16 columns of a row
+// The second product is B T^T, 64 columns of Z at a time: instruction t takes for its rows m the columns column_of(t, m) from a block's first on, so that a lane
+// (g, c) ends with 8 columns of row c side by side from 8 g on and 8 from 32 + 8 g on.
+__device__ __forceinline__ int column_of(int t, int m) { return 32 * (t >> 1) + 8 * (m >> 2) + 4 * (t & 1) + (m & 3); }
+
+template <class T> struct Sixteen;                           // those columns of a row; one: the first 8 are there, two: the others are
 template <> struct Sixteen<uint16_t> {
     u32x4_t w[2];
-    __device__ __forceinline__ void load(const uint16_t* p, bool second) {
-        w[0] = *reinterpret_cast<const u32x4_t*>(p);
-        w[1] = second ? *reinterpret_cast<const u32x4_t*>(p + 8) : u32x4_t{0, 0, 0, 0};
+    __device__ __forceinline__ void load(const uint16_t* p, bool one, bool two) {
+        if (one) w[0] = *reinterpret_cast<const u32x4_t*>(p);
+        if (two) w[1] = *reinterpret_cast<const u32x4_t*>(p + 32);
     }
-    __device__ __forceinline__ void store(uint16_t* p, bool second) const {
-        *reinterpret_cast<u32x4_t*>(p) = w[0];
-        if (second) *reinterpret_cast<u32x4_t*>(p + 8) = w[1];
+    __device__ __forceinline__ void store(uint16_t* p, bool one, bool two) const {
+        if (one) *reinterpret_cast<u32x4_t*>(p) = w[0];
+        if (two) *reinterpret_cast<u32x4_t*>(p + 32) = w[1];
     }
     __device__ __forceinline__ void add(const f32x4_t (&x)[4]) {
         typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
@@ -175,13 +195,13 @@ template <> struct Sixteen<uint16_t> {
 };
 template <> struct Sixteen<float> {
     f32x4_t w[4];
-    __device__ __forceinline__ void load(const float* p, bool second) {
+    __device__ __forceinline__ void load(const float* p, bool one, bool two) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = i < 2 || second ? *reinterpret_cast<const f32x4_t*>(p + 4 * i) : f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < 4; ++i) if (i < 2 ? one : two) w[i] = *reinterpret_cast<const f32x4_t*>(p + 32 * (i >> 1) + 4 * (i & 1));
     }
-    __device__ __forceinline__ void store(float* p, bool second) const {
+    __device__ __forceinline__ void store(float* p, bool one, bool two) const {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) if (i < 2 || second) *reinterpret_cast<f32x4_t*>(p + 4 * i) = w[i];
+        for (int i = 0; i < 4; ++i) if (i < 2 ? one : two) *reinterpret_cast<f32x4_t*>(p + 32 * (i >> 1) + 4 * (i & 1)) = w[i];
     }
     __device__ __forceinline__ void add(const f32x4_t (&x)[4]) {
 #pragma unroll
@@ -189,79 +209,428 @@ template <> struct Sixteen<float> {
     }
 };
 
-// A workgroup: a tile of 16 rows, 64 columns of one part; its waves share the tile's adapters out.  The second product is B T^T: instruction t takes the columns
-// 16 (m / 4) + 4 t + m % 4 for its rows m, so that a lane ends with 16 columns of one row side by side.
+// Rank values go by pieces of PER; of bfloat16 every one comes twice, its upper parts and the rests.  Ranks of up to 16 put both into one instruction.
+template <class T> __device__ __forceinline__ int steps_of_rank(int rank) {
+    const int pieces = rank / Lane<T>::PER;
+    if (sizeof(T) == 4) return (pieces + 3) / 4;
+    return pieces <= 2 ? 1 : 2 * ((pieces + 3) / 4);
+}
+// Which piece lane g has in step s, and whether it is of the rests; `there`: it has one.
+struct Rank { int piece; bool rest, there; };
+template <class T> __device__ __forceinline__ Rank rank_of(int rank, int s, int g) {
+    const int pieces = rank / Lane<T>::PER, half = (pieces + 3) / 4;
+    if (sizeof(T) == 4) return Rank{4 * s + g, false, 4 * s + g < pieces};
+    if (pieces <= 2) return Rank{g >= pieces ? g - pieces : g, g >= pieces, g < 2 * pieces};
+    const int q = 4 * (s >= half ? s - half : s) + g;
+    return Rank{q, s >= half, q < pieces};
+}
+
+// Few rows, the second product.  A workgroup: a tile of 16 rows, 64 columns of one part; its waves share the tile's adapters out.
 template <class T>
 __global__ __launch_bounds__(64 * kWaves)
-void adapt_up_kernel(AdaptArgs a) {
+void adapt_few_up_kernel(AdaptArgs a) {
     typedef Lane<T> L;
     typedef typename L::piece_t piece_t;
-    constexpr int PER = L::PER, TWICE = sizeof(T) == 2 ? 2 : 1;          // pieces of a rank value: its two halves
+    constexpr int PER = L::PER, TOGETHER = 4;                // adapters whose loads are sent for together
     const Adapt& o = a.o;
     const int tile = blockIdx.y, lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    int part = 0;
-    while ((int)blockIdx.x >= a.first_group[part + 1]) ++part;
-    const int first = (part > 0 ? o.part_end[part - 1] : 0) + 64 * (blockIdx.x - a.first_group[part]), end = o.part_end[part];
-    Tile rows(o, tile);
-    const int row = min(tile * 16 + c, o.n - 1), col = first + 16 * g;
-    const bool in = col < end, second = col + 8 < end, in_place = o.base == o.Z;
+    const int part = part_of_block(a, blockIdx.x);
+    const int first = (part > 0 ? o.part_end[part - 1] : 0) + 64 * (blockIdx.x - a.first_block[part]), end = o.part_end[part];
+    const int row = min(tile * 16 + c, o.n - 1), col = first + 8 * g;
+    const bool one = col < end, two = col + 32 < end, in_place = o.base == o.Z;
     const T* base = (const T*)o.base + row * o.ldb + col;
     T* out = (T*)o.Z + row * o.ldz + col;
-    if (wave == 0 && rows.id < 0 && tile * 16 + c < o.n && in && !in_place) {          // rows without an adapter
-        Sixteen<T> x;
-        x.load(base, second);
-        x.store(out, second);
-    }
-    const int pieces = o.rank / PER, steps = (TWICE * pieces + 3) / 4;
-    for (int k = 0; rows.left; ++k) {
-        const int w = rows.next();
-        if (k % kWaves != wave) continue;
-        const bool live = rows.live;
-        const T* B = (const T*)o.B + w * o.b_stride;
-        const float scale = o.scale ? o.scale[w] : 1.f;
-        Sixteen<T> x;
-        if (live && in) x.load(base, second);
-        f32x4_t sum[4];
+    Sixteen<T> x;
+    x.load(base, one, two);
+    Tile rows(o, tile);
+    const int steps = steps_of_rank<T>(o.rank);
+    const float scale = rows.id >= 0 && o.scale ? o.scale[rows.id] : 1.f;
+    // rows that this wave finishes: those without an adapter too
+    bool mine = wave == 0 && rows.id < 0 && !in_place;
+    f32x4_t sum[4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) sum[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        for (int s = 0; s < steps; ++s) {
-            const int q = 4 * s + g, at = (q >= pieces ? q - pieces : q) * PER;
-            const bool there = q < TWICE * pieces;
-            piece_t y[4], z = none<T>();
+    for (int t = 0; t < 4; ++t) sum[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < steps; ++s) {
+        const Rank r = rank_of<T>(o.rank, s, g);
+        piece_t z = none<T>();
+        Tile of = rows;
+        bool first_batch = true;
+        for (int k = 0; of.left;) {
+            int w[TOGETHER], n = 0;
+            bool live[TOGETHER];
+            piece_t y[TOGETHER][4];
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const int j = first + 16 * (c >> 2) + 4 * t + (c & 3);
-                y[t] = none<T>();
-                if (there && j < end) y[t] = *reinterpret_cast<const piece_t*>(B + j * o.ldbw + at);
+            for (int u = 0; u < TOGETHER; ++u) {
+                // the next adapter of this wave
+                w[u] = -1;
+                live[u] = false;
+                while (of.left) {
+                    const int next = of.next();
+                    if (k++ % kWaves == wave) { w[u] = next; live[u] = of.live; ++n; break; }
+                }
+                const T* B = (const T*)o.B + w[u] * o.b_stride + r.piece * PER;
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const int j = first + column_of(t, c);
+                    y[u][t] = none<T>();
+                    if (w[u] >= 0 && r.there && j < end) y[u][t] = *reinterpret_cast<const piece_t*>(B + j * o.ldbw);
+                }
             }
-            if (there && live) {
-                float v[PER];
-                read_t<T>(a, o.workspace + (int64_t)row * a.all + part * o.rank + at, scale, v);
-                z = piece_of(v, q >= pieces);
+            if (first_batch) {                               // (behind the adapters' loads: the two trips go together)
+                first_batch = false;
+                if (r.there && rows.id >= 0) {
+                    float v[PER];
+                    read_t<T>(a, a.t + (int64_t)row * a.all + part * o.rank + r.piece * PER, scale, v);
+                    z = piece_of(v, r.rest);
+                }
             }
 #pragma unroll
-            for (int t = 0; t < 4; ++t) sum[t] = L::multiply(y[t], z, sum[t]);
+            for (int u = 0; u < TOGETHER; ++u) {
+                if (u >= n) break;
+                mine |= live[u];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const f32x4_t with = L::multiply(y[u][t], z, sum[t]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[t][e] = live[u] ? with[e] : sum[t][e];
+                }
+            }
         }
-        if (live && in) {
-            x.add(sum);
-            x.store(out, second);
+    }
+    if (!mine || tile * 16 + c >= o.n) return;
+    if (rows.id >= 0) x.add(sum);
+    x.store(out, one, two);
+}
+
+// Many rows: which go together.  One workgroup counts the rows of every adapter (and of none), deals out places and groups, and puts the rows into their
+// places; where among its adapter's a row comes goes by the order of atomic additions, and nothing goes by that.
+constexpr int kOrderThreads = 1024, kMostBins = 12288, kGroup = 64;
+__global__ __launch_bounds__(kOrderThreads)
+void adapt_order_kernel(AdaptArgs a) {
+    const Adapt& o = a.o;
+    __shared__ int bins[kMostBins];
+    __shared__ int2 sums[kOrderThreads / 64];
+    const int n_bins = o.n_adapters + 1, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    auto bin_of = [&](int w) { return w >= 0 && w < o.n_adapters ? w : o.n_adapters; };
+    for (int i = threadIdx.x; i < n_bins; i += kOrderThreads) bins[i] = 0;
+    __syncthreads();
+    // Adds the rows of a wave to their bins and returns where each comes.  Rows of one adapter side by side are one addition: as many from one address are one after
+    // the other (4096 rows of 8 adapters: 10.8 us with an addition each).
+    auto add = [&](int bin, bool there) {
+        int at = 0;
+        uint64_t left = __ballot(there);
+        for (int turn = 0; turn < 4 && left; ++turn) {
+            const int leader = __builtin_ctzll(left), same = __shfl(bin, leader, 64);
+            const uint64_t those = __ballot(bin == same) & left;
+            int first = 0;
+            if (lane == leader) first = atomicAdd(&bins[same], __popcll(those));
+            first = __shfl(first, leader, 64);
+            if ((those >> lane) & 1) at = first + __popcll(those & ((1ull << lane) - 1));
+            left &= ~those;
+        }
+        if ((left >> lane) & 1) at = atomicAdd(&bins[bin], 1);
+        return at;
+    };
+    const int rounds = (o.n + kOrderThreads - 1) / kOrderThreads;
+    auto row_of = [&](int i) { return i * kOrderThreads + (int)threadIdx.x; };
+    auto read = [&](int i) { return row_of(i) < o.n ? bin_of(o.which[row_of(i)]) : 0; };
+    constexpr int KEPT = 8;                                  // rounds whose numbers stay in registers
+    int kept[KEPT];
+#pragma unroll
+    for (int i = 0; i < KEPT; ++i) kept[i] = read(i);
+#pragma unroll
+    for (int i = 0; i < KEPT; ++i) add(kept[i], row_of(i) < o.n);
+    for (int i = KEPT; i < rounds; ++i) add(read(i), row_of(i) < o.n);
+    __syncthreads();
+    // rows and groups before each thread's bins
+    const int each = (n_bins + kOrderThreads - 1) / kOrderThreads, first = threadIdx.x * each, last = min(first + each, n_bins);
+    int2 mine = {0, 0};
+    for (int i = first; i < last; ++i) { mine.x += bins[i]; mine.y += (bins[i] + kGroup - 1) / kGroup; }
+    int2 upto = mine;
+    for (int by = 1; by < 64; by *= 2) {
+        const int x = __shfl_up(upto.x, by, 64), y = __shfl_up(upto.y, by, 64);
+        if (lane >= by) { upto.x += x; upto.y += y; }
+    }
+    if (lane == 63) sums[wave] = upto;
+    __syncthreads();
+    int2 before = {upto.x - mine.x, upto.y - mine.y};
+    int groups = 0;
+    for (int i = 0; i < kOrderThreads / 64; ++i) {
+        if (i < wave) { before.x += sums[i].x; before.y += sums[i].y; }
+        groups += sums[i].y;
+    }
+    if (threadIdx.x == 0) *a.n_groups = groups;
+    for (int j = 0; j < each; ++j) {
+        const int i = first + j, count = i < last ? bins[i] : 0, w = i < o.n_adapters ? i : -1, in_bin = (count + kGroup - 1) / kGroup;
+        if (i < last) bins[i] = before.x;
+        auto put = [&](int k, int w, int2 before, int count) { a.groups[before.y + k] = int4{w, before.x + kGroup * k, min(count - kGroup * k, kGroup), 0}; };
+        constexpr int FEW = 4;
+        for (int k = 0; k < min(in_bin, FEW); ++k) put(k, w, before, count);
+        // the other groups of a large bin: its wave
+        for (uint64_t large = __ballot(in_bin > FEW); large; large &= large - 1) {
+            const int from = __builtin_ctzll(large), all = __shfl(in_bin, from, 64), c = __shfl(count, from, 64), its = __shfl(w, from, 64);
+            const int2 at = {__shfl(before.x, from, 64), __shfl(before.y, from, 64)};
+            for (int k = FEW + lane; k < all; k += 64) put(k, its, at, c);
+        }
+        before.x += count;
+        before.y += in_bin;
+    }
+    __syncthreads();
+    auto put = [&](int i, int bin) {
+        const int at = add(bin, row_of(i) < o.n);
+        if (row_of(i) < o.n) a.order[at] = row_of(i);
+    };
+#pragma unroll
+    for (int i = 0; i < KEPT; ++i) put(i, kept[i]);
+    for (int i = KEPT; i < rounds; ++i) put(i, read(i));
+}
+
+// The rows of a workgroup's group, or, where none were made, 64 rows as they come: lane l of a wave has row l and its adapter.
+struct Group {
+    int count, id, row_of_lane;
+    uint64_t left;                       // rows of adapters still to come
+    __device__ __forceinline__ bool find(const AdaptArgs& a) {
+        const int lane = threadIdx.x & 63;
+        if (a.groups) {
+            if ((int)blockIdx.x >= *a.n_groups) return false;
+            const int4 group = a.groups[blockIdx.x];
+            count = group.z;
+            row_of_lane = a.order[group.y + min(lane, count - 1)];
+            id = lane < count ? group.x : -1;
+        } else {
+            count = min(a.o.n - (int)blockIdx.x * kGroup, kGroup);
+            row_of_lane = blockIdx.x * kGroup + min(lane, count - 1);
+            id = lane < count ? a.o.which[row_of_lane] : -1;
+            if (id >= a.o.n_adapters) id = -1;
+        }
+        left = __ballot(id >= 0);
+        return true;
+    }
+    __device__ __forceinline__ int next(uint64_t* those) {
+        const int w = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
+        *those = __ballot(id == w);
+        left &= ~*those;
+        return w;
+    }
+};
+
+// Many rows, the first product.  A workgroup: one group, 64 rows of A, one part of d, whose steps its waves share out.
+template <class T>
+__global__ __launch_bounds__(64 * kWaves, 2)
+void adapt_many_down_kernel(AdaptArgs a) {
+    typedef Lane<T> L;
+    typedef typename L::piece_t piece_t;
+    constexpr int STEP = 4 * L::PER, RT = 4, HT = kGroup / 16, AHEAD = 4;
+    const Adapt& o = a.o;
+    __shared__ f32x4_t sums[kWaves][RT][64];
+    Group group;
+    if (!group.find(a)) return;
+    const int split = blockIdx.y, first_rank = blockIdx.z * 16 * RT;
+    const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int rank_tiles = min((a.all - first_rank + 15) / 16, RT);
+    const int begin = split * a.steps, end = min(begin + a.steps, (o.d + STEP - 1) / STEP);
+    int row[HT];
+    const T* h[HT];
+#pragma unroll
+    for (int i = 0; i < HT; ++i) {
+        row[i] = __shfl(group.row_of_lane, 16 * i + c, 64);
+        h[i] = (const T*)o.H + row[i] * o.ldh;
+    }
+    while (group.left) {
+        uint64_t those;
+        const int w = group.next(&those);
+        const T* A = (const T*)o.A + w * o.a_stride;
+        bool live[HT], any[HT];
+#pragma unroll
+        for (int i = 0; i < HT; ++i) { live[i] = (those >> (16 * i + c)) & 1; any[i] = (those >> (16 * i)) & 0xFFFF; }
+        f32x4_t sum[HT][RT];
+#pragma unroll
+        for (int i = 0; i < HT; ++i)
+#pragma unroll
+            for (int t = 0; t < RT; ++t) sum[i][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int s0 = begin + wave; s0 < end; s0 += kWaves * AHEAD) {
+            piece_t x[AHEAD][HT], y[AHEAD][RT];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const int s = s0 + u * kWaves, col = s * STEP + g * L::PER;
+                const bool there = s < end && col < o.d;
+#pragma unroll
+                for (int i = 0; i < HT; ++i) {
+                    x[u][i] = none<T>();
+                    if (there && live[i]) x[u][i] = *reinterpret_cast<const piece_t*>(h[i] + col);
+                }
+#pragma unroll
+                for (int t = 0; t < RT; ++t) {
+                    const int r = first_rank + 16 * t + c;
+                    y[u][t] = none<T>();
+                    if (there && r < a.all) y[u][t] = *reinterpret_cast<const piece_t*>(A + r * o.lda + col);
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+                if (t >= rank_tiles) break;
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+                    for (int i = 0; i < HT; ++i) sum[i][t] = L::multiply(y[u][t], x[u][i], sum[i][t]);
+            }
+        }
+        // one tile of rows after the other through LDS; wave t adds up tile t of ranks: rank 16 t + 4 g + r of row c
+#pragma unroll
+        for (int i = 0; i < HT; ++i) {
+            if (!any[i]) continue;
+            __syncthreads();
+#pragma unroll
+            for (int t = 0; t < RT; ++t) sums[wave][t][lane] = sum[i][t];
+            __syncthreads();
+            if (wave < rank_tiles && live[i]) {
+                f32x4_t all = sums[0][wave][lane];
+#pragma unroll
+                for (int k = 1; k < kWaves; ++k) all += sums[k][wave][lane];
+                const int r = first_rank + 16 * wave + 4 * g;
+                if (r < a.all) *reinterpret_cast<f32x4_t*>(a.t + ((int64_t)split * o.n + row[i]) * a.all + r) = all;
+            }
+        }
+    }
+}
+
+// Many rows, the second product.  A workgroup: one group, `wide` columns of one part, 64 at a time to a wave.  The operands that T makes lie in LDS.
+template <class T>
+__global__ __launch_bounds__(64 * kWaves, 2)
+void adapt_many_up_kernel(AdaptArgs a) {
+    typedef Lane<T> L;
+    typedef typename L::piece_t piece_t;
+    constexpr int PER = L::PER, HT = kGroup / 16, MOST = 8;  // steps of a rank of 128
+    const Adapt& o = a.o;
+    __shared__ piece_t z[MOST][HT][64];
+    Group group;
+    if (!group.find(a)) return;
+    const bool in_place = o.base == o.Z;
+    const uint64_t with = group.left;                        // rows that have an adapter
+    if (!with && in_place) return;
+    const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int part = part_of_block(a, blockIdx.y);
+    const int first = (part > 0 ? o.part_end[part - 1] : 0) + a.wide * (blockIdx.y - a.first_block[part]), end = min(first + a.wide, o.part_end[part]);
+    const int steps = steps_of_rank<T>(o.rank), tiles = (group.count + 15) / 16;
+    const T* base[HT];
+    T* out[HT];
+#pragma unroll
+    for (int i = 0; i < HT; ++i) {
+        const int64_t row = __shfl(group.row_of_lane, 16 * i + c, 64);
+        base[i] = (const T*)o.base + row * o.ldb;
+        out[i] = (T*)o.Z + row * o.ldz;
+    }
+    Sixteen<T> x[HT];
+    auto read = [&](int at) {
+        const int col = at + 8 * g;
+#pragma unroll
+        for (int i = 0; i < HT; ++i)
+            if (i < tiles) x[i].load(base[i] + col, col < end, col + 32 < end);
+    };
+    read(first + 64 * wave);
+    // a thread: one row's PER rank values
+    const int pieces = o.rank / PER;
+    for (int e = threadIdx.x; e < kGroup * MOST * 4; e += 64 * kWaves) {
+        const int i = e & (kGroup - 1), q = e / kGroup;      // (a row of its own to each lane of a wave, whose q is one)
+        if (q >= 4 * steps) break;
+        const bool there = q < pieces && ((with >> i) & 1);
+        float v[PER];
+#pragma unroll
+        for (int k = 0; k < PER; ++k) v[k] = 0.f;
+        const int row = __shfl(group.row_of_lane, i, 64), w = __shfl(group.id, i, 64);
+        if (there) read_t<T>(a, a.t + (int64_t)row * a.all + part * o.rank + q * PER, o.scale ? o.scale[w] : 1.f, v);
+        const int half = (pieces + 3) / 4, to = (i & 15);
+        if constexpr (sizeof(T) == 4) {
+            z[q >> 2][i >> 4][16 * (q & 3) + to] = piece_of(v, false);
+        } else if (pieces <= 2) {
+            // upper parts, rests, nothing
+            if (q < pieces) {
+                z[0][i >> 4][16 * q + to] = piece_of(v, false);
+                z[0][i >> 4][16 * (pieces + q) + to] = piece_of(v, true);
+            } else if (q >= 2 * pieces) {
+                z[0][i >> 4][16 * q + to] = none<T>();
+            }
+        } else if (q < 4 * half) {
+            z[q >> 2][i >> 4][16 * (q & 3) + to] = piece_of(v, false);
+            z[half + (q >> 2)][i >> 4][16 * (q & 3) + to] = piece_of(v, true);
+        }
+    }
+    __syncthreads();
+    for (int at = first + 64 * wave; at < end; at += 64 * kWaves) {
+        const int col = at + 8 * g;
+        f32x4_t sum[HT][4];
+#pragma unroll
+        for (int i = 0; i < HT; ++i)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) sum[i][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        Group of = group;
+        while (of.left) {
+            uint64_t those;
+            const int w = of.next(&those);
+            const T* B = (const T*)o.B + w * o.b_stride;
+            const bool alone = those == with;                // no rows of other adapters: they would have to be kept
+            for (int s = 0; s < steps; ++s) {
+                const Rank r = rank_of<T>(o.rank, s, g);
+                piece_t y[4];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const int j = at + column_of(t, c);
+                    y[t] = none<T>();
+                    if (r.there && j < end) y[t] = *reinterpret_cast<const piece_t*>(B + j * o.ldbw + r.piece * PER);
+                }
+#pragma unroll
+                for (int i = 0; i < HT; ++i) {
+                    const piece_t zi = z[s][i][lane];
+                    const bool live = alone || ((those >> (16 * i + c)) & 1);
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        const f32x4_t more = L::multiply(y[t], zi, sum[i][t]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sum[i][t][e] = live ? more[e] : sum[i][t][e];
+                    }
+                }
+            }
+        }
+        Sixteen<T> was[HT];
+#pragma unroll
+        for (int i = 0; i < HT; ++i) was[i] = x[i];
+        read(at + 64 * kWaves);
+#pragma unroll
+        for (int i = 0; i < HT; ++i) {
+            const int k = 16 * i + c;
+            const bool has = (with >> k) & 1;
+            if (k >= group.count || (!has && in_place)) continue;
+            if (has) was[i].add(sum[i]);
+            was[i].store(out[i] + col, col < end, col + 32 < end);
         }
     }
 }
 
 int steps_of(int is_bf16, int d) { return (d + (is_bf16 ? 31 : 15)) / (is_bf16 ? 32 : 16); }
 
-// Workgroups for the first product: 512 fill the chip.  A tile of few rows has an adapter to each of them as a rule: they go side by side.
-void plan(int is_bf16, int n, int d, int rank, int n_parts, int* slots, int* splits, int* steps) {
-    const int tiles = (n + 15) / 16, all = steps_of(is_bf16, d), groups = (rank * n_parts + 63) / 64;
-    *slots = tiles <= 16 ? 16 : 1;
-    const int64_t items = (int64_t)(*slots == 1 ? tiles : n) * groups;
+constexpr int kFewRows = 256;
+constexpr int kFewAdapters = 8;
+struct Plan { bool many, ordered; int splits, steps, wide; int64_t most_groups, t_bytes, bytes; };
+Plan plan_of(int is_bf16, int n, int d, int p, int rank, int n_parts, int n_adapters) {
+    Plan r;
+    r.many = n > kFewRows && n_adapters < kMostBins;
+    r.ordered = r.many && n_adapters > kFewAdapters;
+    const int all = steps_of(is_bf16, d), rank_groups = (rank * n_parts + 63) / 64;
+    const int64_t alone = n_adapters < n ? n_adapters + 1 : n;          // groups that are not full
+    r.most_groups = r.ordered ? n / kGroup + alone : r.many ? (n + kGroup - 1) / kGroup : 0;
+    // 512 workgroups for the first product fill the chip; few rows have an adapter each as a rule
+    const int64_t items = (r.many ? (n + kGroup - 1) / kGroup : n) * (int64_t)rank_groups;
     int64_t cuts = items >= 512 ? 1 : 512 / items;
     const int most = (all + 15) / 16;                        // four steps to a wave
-    if (cuts > most) cuts = most;
-    if (cuts > 16) cuts = 16;
-    *steps = (int)((all + cuts - 1) / cuts);
-    *splits = (all + *steps - 1) / *steps;
+    cuts = cuts < most ? cuts : most;
+    cuts = cuts < (r.many ? 8 : 16) ? cuts : (r.many ? 8 : 16);
+    r.steps = (int)((all + cuts - 1) / cuts);
+    r.splits = (all + r.steps - 1) / r.steps;
+    r.wide = 64;
+    if (r.many) for (r.wide = 1024; r.wide > 256 && (n + kGroup - 1) / kGroup * (int64_t)((p + r.wide - 1) / r.wide) < 512;) r.wide /= 2;
+    r.t_bytes = round_up((int64_t)r.splits * n * rank * n_parts * sizeof(float), 256);
+    r.bytes = r.t_bytes + (r.ordered ? round_up(4 * (int64_t)n, 256) + 16 * r.most_groups + 256 : 0);
+    return r;
 }
 
 template <class T>
@@ -269,27 +638,48 @@ hipError_t launch(const Adapt& o, hipStream_t stream) {
     AdaptArgs a;
     a.o = o;
     a.all = o.rank * o.n_parts;
-    plan(sizeof(T) == 2, o.n, o.d, o.rank, o.n_parts, &a.slots, &a.splits, &a.steps);
-    a.first_group[0] = 0;
+    const Plan p = plan_of(sizeof(T) == 2, o.n, o.d, o.p, o.rank, o.n_parts, o.n_adapters);
+    a.splits = p.splits; a.steps = p.steps; a.wide = p.wide;
+    a.first_block[0] = 0;
     for (int k = 0; k < kMostParts; ++k)
-        a.first_group[k + 1] = a.first_group[k] + (k < o.n_parts ? (o.part_end[k] - (k ? o.part_end[k - 1] : 0) + 63) / 64 : 0);
+        a.first_block[k + 1] = a.first_block[k] + (k < o.n_parts ? (o.part_end[k] - (k ? o.part_end[k - 1] : 0) + a.wide - 1) / a.wide : 0);
+    const int blocks = a.first_block[o.n_parts], rank_groups = (a.all + 63) / 64;
+    uint8_t* ws = (uint8_t*)o.workspace;
+    a.t = (float*)ws;
+    a.n_groups = (int*)(ws + p.t_bytes);
+    a.groups = p.ordered ? (int4*)(ws + p.t_bytes + 256) : nullptr;
+    a.order = (int*)(ws + p.t_bytes + 256 + 16 * p.most_groups);
+    if (p.many) {
+        if (p.ordered) hipLaunchKernelGGL(adapt_order_kernel, dim3(1), dim3(kOrderThreads), 0, stream, a);
+        hipLaunchKernelGGL(adapt_many_down_kernel<T>, dim3((unsigned)p.most_groups, a.splits, rank_groups), dim3(64 * kWaves), 0, stream, a);
+        hipLaunchKernelGGL(adapt_many_up_kernel<T>, dim3((unsigned)p.most_groups, blocks), dim3(64 * kWaves), 0, stream, a);
+        return hipGetLastError();
+    }
     const int tiles = (o.n + 15) / 16;
-    hipLaunchKernelGGL(adapt_down_kernel<T>, dim3(tiles * a.slots, a.splits, (a.all + 63) / 64), dim3(64 * kWaves), 0, stream, a);
-    hipLaunchKernelGGL(adapt_up_kernel<T>, dim3(a.first_group[o.n_parts], tiles), dim3(64 * kWaves), 0, stream, a);
+    hipLaunchKernelGGL(adapt_few_down_kernel<T>, dim3(tiles * 16, a.splits, rank_groups), dim3(64 * kWaves), 0, stream, a);
+    hipLaunchKernelGGL(adapt_few_up_kernel<T>, dim3(blocks, tiles), dim3(64 * kWaves), 0, stream, a);
     return hipGetLastError();
 }
 
 }  // namespace
 
-bool adapt_fits(const Adapt& o) {
-    const int64_t tiles = (o.n + 15) / 16, groups = o.p / 64 + o.n_parts;
-    return tiles <= 65535 && tiles * groups <= kMostThreads / 256;
+bool adapt_fits(const Adapt& o, int is_bf16) {
+    const Plan p = plan_of(is_bf16, o.n, o.d, o.p, o.rank, o.n_parts, o.n_adapters);
+    const int64_t groups = p.many ? p.most_groups : (o.n + 15) / 16 * 16, blocks = o.p / p.wide + o.n_parts, most = kMostThreads / (64 * kWaves);
+    return (p.many || (o.n + 15) / 16 <= 65535) && blocks <= 65535 && groups * blocks <= most && groups * p.splits * ((o.rank * o.n_parts + 63) / 64) <= most;
 }
 
-size_t adapt_workspace_bytes(int is_bf16, int n, int d, int rank, int n_parts) {
-    int slots, splits, steps;
-    plan(is_bf16, n, d, rank, n_parts, &slots, &splits, &steps);
-    return (size_t)splits * n * rank * n_parts * sizeof(float);
+size_t adapt_workspace_bytes(const Adapt& o, int is_bf16) { return (size_t)plan_of(is_bf16, o.n, o.d, o.p, o.rank, o.n_parts, o.n_adapters).bytes; }
+// What any call of up to so many rows, ranks and adapters needs: the parts of d are at most 512 over the workgroups of one part, of 1 row or 64.
+size_t adapt_workspace_bound(int n, int rank, int n_parts, int n_adapters) {
+    const int64_t most = 8 * (int64_t)n < 512 * kGroup ? 8 * (int64_t)n : 512 * kGroup, rows = n <= kFewRows ? 512 : n > most ? n : most;
+    const int64_t alone = n_adapters < n ? n_adapters + 1 : n;
+    return (size_t)(round_up(rows * rank * n_parts * (int64_t)sizeof(float), 256) + round_up(4 * (int64_t)n, 256) + 16 * (n / kGroup + alone) + 256);
+}
+
+// adapt_workspace_bytes of these sizes
+size_t adapt_needs(int is_bf16, int n, int d, int p, int rank, int n_parts, int n_adapters) {
+    return (size_t)plan_of(is_bf16, n, d, p, rank, n_parts, n_adapters).bytes;
 }
 
 hipError_t adapt(const Adapt& o, int is_bf16, hipStream_t stream) { return is_bf16 ? launch<uint16_t>(o, stream) : launch<float>(o, stream); }

@@ -1749,23 +1749,22 @@ gelo_status gelo_adapt(gelo_ctx* ctx, gelo_dtype dtype, int n, int d, int p, con
     o.A = adapters->a; o.a_stride = adapters->a_stride; o.lda = adapters->lda; o.B = adapters->b; o.b_stride = adapters->b_stride; o.ldbw = adapters->ldb;
     o.scale = adapters->scale; o.rank = adapters->rank; o.n_parts = adapters->n_parts; o.n_adapters = adapters->n_adapters;
     for (int k = 0; k < kMostParts; ++k) o.part_end[k] = k < o.n_parts ? adapters->part_end[k] : p;
-    if (!adapt_fits(o)) return fail(ctx, GELO_ESHAPE, "%d rows of %d columns are too many for one launch", n, p);
+    if (!adapt_fits(o, dtype == GELO_BF16)) return fail(ctx, GELO_ESHAPE, "%d rows of %d columns are too many for one launch", n, p);
     GELO_HIP(ctx, hipSetDevice(ctx->device));
-    st = grow_adapt(ctx, adapt_workspace_bytes(dtype == GELO_BF16, n, d, o.rank, o.n_parts));
+    st = grow_adapt(ctx, adapt_workspace_bytes(o, dtype == GELO_BF16));
     if (st != GELO_OK) return st;
     o.workspace = (float*)ctx->adapt_ws;
     GELO_HIP(ctx, adapt(o, dtype == GELO_BF16, (hipStream_t)stream));
     return GELO_OK;
 }
 
-gelo_status gelo_reserve_adapt(gelo_ctx* ctx, gelo_dtype dtype, int n, int d, int rank, int n_parts) {
+gelo_status gelo_reserve_adapt(gelo_ctx* ctx, int n, int rank, int n_parts, int n_adapters) {
     if (!ctx) return GELO_EINVAL;
-    if (dtype != GELO_F32 && dtype != GELO_BF16) return fail(ctx, GELO_EINVAL, "unknown dtype %d", (int)dtype);
-    if (n < 1 || d < 8 || d % 8 != 0 || d > (1 << 24)) return fail(ctx, GELO_EINVAL, "n=%d d=%d", n, d);
+    if (n < 1 || n_adapters < 1) return fail(ctx, GELO_EINVAL, "n=%d n_adapters=%d", n, n_adapters);
     if (rank < 8 || rank % 8 != 0 || rank > GELO_ADAPT_MAX_RANK || n_parts < 1 || n_parts > GELO_ADAPT_MAX_PARTS)
         return fail(ctx, GELO_ESHAPE, "rank=%d n_parts=%d", rank, n_parts);
     GELO_HIP(ctx, hipSetDevice(ctx->device));
-    return grow_adapt(ctx, adapt_workspace_bytes(dtype == GELO_BF16, n, d, rank, n_parts));
+    return grow_adapt(ctx, adapt_workspace_bound(n, rank, n_parts, n_adapters));
 }
 
 }  // extern "C"

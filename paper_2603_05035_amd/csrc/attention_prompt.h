@@ -143,7 +143,9 @@ __device__ __forceinline__ bool prompt_tile(const AttnArgs& a, int seq, int kvh,
     // chunk j of the lane's keys into slot `slot`
     auto put_k4 = [&](auto jc, int slot, const uint32_t (&codes)[W], uint32_t scale) {
         constexpr int j = decltype(jc)::value;
-        const int r = lane >> 2, quarter = lane & 3, turn = D == 96 ? (32 * (24 * quarter / 32 + 1) - 24 * quarter) / 8 : W / 2;
+        int my = lane;
+        asm volatile("" : "+v"(my));                         // (addresses are worked out again: kept, they take registers the loop needs)
+        const int r = my >> 2, quarter = my & 3, turn = D == 96 ? (32 * (24 * quarter / 32 + 1) - 24 * quarter) / 8 : W / 2;
         const float by = fp4_scale(((D == 96 || D == 256) && j >= turn ? scale >> 8 : scale) & 0xFFu);
         const u32x4_t x = {fp4_pair<0>(codes[j], by), fp4_pair<1>(codes[j], by), fp4_pair<2>(codes[j], by), fp4_pair<3>(codes[j], by)};
         *reinterpret_cast<u32x4_t*>(lds + slot * SLOT + (wave * ROWS + r) * PITCH + 16 * k_pos<D>(r, quarter * W + j)) = x;
@@ -158,7 +160,9 @@ __device__ __forceinline__ bool prompt_tile(const AttnArgs& a, int seq, int kvh,
     };
     auto put_v4 = [&](auto rc, int slot) {
         constexpr int r = decltype(rc)::value;
-        const int row = 4 * (lane >> 4) + r, col = lane & 15, turn = (32 * (D / 16 * col / 32 + 1) - D / 16 * col) / 2;
+        int my = lane;
+        asm volatile("" : "+v"(my));
+        const int row = 4 * (my >> 4) + r, col = my & 15, turn = (32 * (D / 16 * col / 32 + 1) - D / 16 * col) / 2;
         float by[D == 96 ? 2 : 1];
 #pragma unroll
         for (int b = 0; b < (D == 96 ? 2 : 1); ++b) by[b] = fp4_scale((v_scale[b] >> (8 * r)) & 0xFFu);

@@ -458,8 +458,10 @@ struct Adapt {
     int part_end[kMostParts];
     float* workspace;                            // at least adapt_workspace_bytes
 };
-bool adapt_fits(const Adapt& o);                 // as one launch each
-size_t adapt_workspace_bytes(int is_bf16, int n, int d, int rank, int n_parts);
+bool adapt_fits(const Adapt& o, int is_bf16);    // as one launch each
+size_t adapt_workspace_bytes(const Adapt& o, int is_bf16);
+size_t adapt_workspace_bound(int n, int rank, int n_parts, int n_adapters);
+size_t adapt_needs(int is_bf16, int n, int d, int p, int rank, int n_parts, int n_adapters);
 hipError_t adapt(const Adapt& o, int is_bf16, hipStream_t stream);
 
 }  // namespace gelo

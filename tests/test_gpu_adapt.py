@@ -215,7 +215,7 @@ def test_workspace_that_is_outgrown_serves_captured_calls(ctx):
         adapters = g.Adapters(A, B, scale=scale, part_ends=ends)
         which = torch.tensor([i % 4 for i in range(20)], dtype=torch.int32).cuda()
         Z, Y = torch.empty_like(base), torch.empty_like(base)
-        g.gelo_reserve_adapt(c, g.GELO_BF16, 20, 264, 16, 2)
+        g.gelo_reserve_adapt(c, 20, 16, 2, 4)
         graph = torch.cuda.CUDAGraph()
         torch.cuda.synchronize()
         with torch.cuda.graph(graph):
@@ -281,8 +281,8 @@ def test_refusals(ctx):
         assert call(**bad) == "GELO_EALIGN", bad
     st = lib.gelo_adapt(ctx, 0, 4, 64, 80, P(x), 64, None, P(i), P(x + 8192), 80, P(x + 16384), 80, P(None))
     assert g.STATUS_NAMES[st] == "GELO_EINVAL"
-    for bad, want in (((2, 4, 64, 8, 1), "GELO_EINVAL"), ((1, 0, 64, 8, 1), "GELO_EINVAL"), ((1, 4, 60, 8, 1), "GELO_EINVAL"), ((1, 4, 64, 12, 1), "GELO_ESHAPE"),
-                      ((1, 4, 64, 8, 5), "GELO_ESHAPE")):
+    for bad, want in (((0, 8, 1, 1), "GELO_EINVAL"), ((4, 8, 1, 0), "GELO_EINVAL"), ((4, 12, 1, 1), "GELO_ESHAPE"), ((4, 8, 5, 1), "GELO_ESHAPE"),
+                      ((4, 136, 1, 1), "GELO_ESHAPE")):
         with pytest.raises(g.GeloError) as e:
             g.gelo_reserve_adapt(ctx, *bad)
         assert g.STATUS_NAMES[e.value.status] == want, bad

@@ -594,7 +594,7 @@ def serve_state(ctx, kv, seed):
 def test_other_streams_and_captured_graphs(ctx):
     """The calls on a stream of their own, and captured once and replayed for other inputs in the same buffers, against plain calls."""
     g.gelo_reserve_attention(ctx, 64)
-    g.gelo_reserve_adapt(ctx, g.GELO_BF16, 4, 256, 8, 3)
+    g.gelo_reserve_adapt(ctx, 4, 8, 3, 3)
     a = serve_state(ctx, [2500, 40, 7, 0], 20)
     pool = a["cache"].K.clone(), a["cache"].V.clone()
     side = torch.cuda.Stream()

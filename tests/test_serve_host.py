@@ -1,6 +1,7 @@
 """The host's side of the cache of 4 bits and of adapters: what the binding makes of tensors and refuses, and what the library reckons from sizes.  Nothing
 here launches a kernel or needs a GPU."""
 import ctypes
+import random
 
 import pytest
 import torch
@@ -131,4 +132,20 @@ def test_every_call_wants_a_context():
     assert lib.gelo_cache_rows_fp4(None, 1, None, None, P(16), 128, None, 0, None) == 1
     assert lib.gelo_attention_fp4(None, 1, 4, P(16), 256, None, None, 1.0, 1, P(16), 256, None) == 1
     assert lib.gelo_adapt(None, 1, 4, 64, 64, P(16), 64, None, P(16), P(16), 64, P(16), 64, None) == 1
-    assert lib.gelo_reserve_adapt(None, 1, 4, 64, 8, 1) == 1
+    assert lib.gelo_reserve_adapt(None, 4, 8, 1, 1) == 1
+
+
+def test_reserved_workspace_of_adapters_serves_every_smaller_call():
+    lib = ctypes.CDLL(g.LIB_PATH)
+    needs, bound = lib["_ZN4gelo11adapt_needsEiiiiiii"], lib["_ZN4gelo21adapt_workspace_boundEiiii"]
+    needs.restype = bound.restype = ctypes.c_size_t
+    rng = random.Random(1)
+    for _ in range(20000):
+        n = int(2 ** rng.uniform(0, 15))
+        rank, parts, count = 8 * rng.randint(1, 16), rng.randint(1, 4), int(2 ** rng.uniform(0, 15))
+        reserved = bound(n, rank, parts, count)
+        for _ in range(4):
+            less = rng.choice([n, rng.randint(1, n), min(n, 256), min(n, 257)])
+            d, p = 8 * rng.randint(1, 2000), 8 * rng.randint(2, 3000)
+            got = needs(rng.randint(0, 1), less, d, p, rng.choice([8, rank]), rng.randint(1, parts), rng.choice([count, rng.randint(1, count)]))
+            assert 0 < got <= reserved, (n, rank, parts, count, less, d, p)
