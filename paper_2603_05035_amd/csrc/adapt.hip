@@ -102,12 +102,12 @@ void adapt_few_down_kernel(AdaptArgs a) {
         f32x4_t sum[RT];
 #pragma unroll
         for (int t = 0; t < RT; ++t) sum[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        for (int s0 = begin + wave; s0 < end; s0 += kWaves * AHEAD) {
+        for (int s0 = begin + wave * AHEAD; s0 < end; s0 += kWaves * AHEAD) {
             piece_t x[AHEAD], y[AHEAD][RT];
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
-                const int col = (s0 + u * kWaves) * STEP + g * L::PER;
-                const bool there = s0 + u * kWaves < end && col < o.d;
+                const int col = (s0 + u) * STEP + g * L::PER;
+                const bool there = s0 + u < end && col < o.d;
                 x[u] = none<T>();
                 if (there && live) x[u] = *reinterpret_cast<const piece_t*>(h + col);
 #pragma unroll
@@ -168,46 +168,22 @@ __device__ __forceinline__ bf16x8_t piece_of(const float (&v)[8], bool rest) {
 }
 __device__ __forceinline__ f32x4_t piece_of(const float (&v)[4], bool) { return f32x4_t{v[0], v[1], v[2], v[3]}; }
 
-// The second product is B T^T, 64 columns of Z at a time: instruction t takes for its rows m the columns column_of(t, m) from a block's first on, so that a lane
-// (g, c) ends with 8 columns of row c side by side from 8 g on and 8 from 32 + 8 g on.
-__device__ __forceinline__ int column_of(int t, int m) { return 32 * (t >> 1) + 8 * (m >> 2) + 4 * (t & 1) + (m & 3); }
-
-template <class T> struct Sixteen;                           // those columns of a row; one: the first 8 are there, two: the others are
-template <> struct Sixteen<uint16_t> {
-    u32x4_t w[2];
-    __device__ __forceinline__ void load(const uint16_t* p, bool one, bool two) {
-        if (one) w[0] = *reinterpret_cast<const u32x4_t*>(p);
-        if (two) w[1] = *reinterpret_cast<const u32x4_t*>(p + 32);
-    }
-    __device__ __forceinline__ void store(uint16_t* p, bool one, bool two) const {
-        if (one) *reinterpret_cast<u32x4_t*>(p) = w[0];
-        if (two) *reinterpret_cast<u32x4_t*>(p + 32) = w[1];
-    }
-    __device__ __forceinline__ void add(const f32x4_t (&x)[4]) {
-        typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+// 16 bytes of Z: base's and what lies at `more`, rounded once
+__device__ __forceinline__ void add_to(u32x4_t& x, const float* more, uint16_t) {
+    typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+    const f32x4_t a = *reinterpret_cast<const f32x4_t*>(more), b = *reinterpret_cast<const f32x4_t*>(more + 4);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t was = w[i >> 2][i & 3];
-            const bf16x2_t pair = {(__bf16)(__uint_as_float(was << 16) + x[i >> 1][2 * (i & 1)]), (__bf16)(__uint_as_float(was & 0xFFFF0000u) + x[i >> 1][2 * (i & 1) + 1])};
-            w[i >> 2][i & 3] = __builtin_bit_cast(uint32_t, pair);
-        }
+    for (int i = 0; i < 4; ++i) {
+        const float m0 = i < 2 ? a[2 * i] : b[2 * i - 4], m1 = i < 2 ? a[2 * i + 1] : b[2 * i - 3];
+        const bf16x2_t pair = {(__bf16)(__uint_as_float(x[i] << 16) + m0), (__bf16)(__uint_as_float(x[i] & 0xFFFF0000u) + m1)};
+        x[i] = __builtin_bit_cast(uint32_t, pair);
     }
-};
-template <> struct Sixteen<float> {
-    f32x4_t w[4];
-    __device__ __forceinline__ void load(const float* p, bool one, bool two) {
+}
+__device__ __forceinline__ void add_to(u32x4_t& x, const float* more, float) {
+    const f32x4_t a = *reinterpret_cast<const f32x4_t*>(more);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) if (i < 2 ? one : two) w[i] = *reinterpret_cast<const f32x4_t*>(p + 32 * (i >> 1) + 4 * (i & 1));
-    }
-    __device__ __forceinline__ void store(float* p, bool one, bool two) const {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) if (i < 2 ? one : two) *reinterpret_cast<f32x4_t*>(p + 32 * (i >> 1) + 4 * (i & 1)) = w[i];
-    }
-    __device__ __forceinline__ void add(const f32x4_t (&x)[4]) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] += x[i];
-    }
-};
+    for (int i = 0; i < 4; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) + a[i]);
+}
 
 // Rank values go by pieces of PER; of bfloat16 every one comes twice, its upper parts and the rests.  Ranks of up to 16 put both into one instruction.
 template <class T> __device__ __forceinline__ int steps_of_rank(int rank) {
@@ -225,81 +201,67 @@ template <class T> __device__ __forceinline__ Rank rank_of(int rank, int s, int 
     return Rank{q, s >= half, q < pieces};
 }
 
-// Few rows, the second product.  A workgroup: a tile of 16 rows, 64 columns of one part; its waves share the tile's adapters out.
+// Few rows, the second product, as sums of products: a row has its adapter to itself as a rule, and a matrix instruction would multiply 15 rows of zeros.  A
+// workgroup: one row, kFewCols columns of one part, two side by side to a thread.  64 rows with 48 adapters, 12288 columns, rank 16: see launch().
+constexpr int kFewCols = 512;
 template <class T>
-__global__ __launch_bounds__(64 * kWaves)
+__global__ __launch_bounds__(256)
 void adapt_few_up_kernel(AdaptArgs a) {
-    typedef Lane<T> L;
-    typedef typename L::piece_t piece_t;
-    constexpr int PER = L::PER, TOGETHER = 4;                // adapters whose loads are sent for together
     const Adapt& o = a.o;
-    const int tile = blockIdx.y, lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int part = part_of_block(a, blockIdx.x);
-    const int first = (part > 0 ? o.part_end[part - 1] : 0) + 64 * (blockIdx.x - a.first_block[part]), end = o.part_end[part];
-    const int row = min(tile * 16 + c, o.n - 1), col = first + 8 * g;
-    const bool one = col < end, two = col + 32 < end, in_place = o.base == o.Z;
-    const T* base = (const T*)o.base + row * o.ldb + col;
-    T* out = (T*)o.Z + row * o.ldz + col;
-    Sixteen<T> x;
-    x.load(base, one, two);
-    Tile rows(o, tile);
-    const int steps = steps_of_rank<T>(o.rank);
-    const float scale = rows.id >= 0 && o.scale ? o.scale[rows.id] : 1.f;
-    // rows that this wave finishes: those without an adapter too
-    bool mine = wave == 0 && rows.id < 0 && !in_place;
-    f32x4_t sum[4];
+    __shared__ __attribute__((aligned(16))) float t[128];    // the row's T
+    const int blocks = a.first_block[o.n_parts], row = blockIdx.x / blocks, block = blockIdx.x - row * blocks;
+    const int id = o.which[row], part = part_of_block(a, block);
+    const int first = (part > 0 ? o.part_end[part - 1] : 0) + kFewCols * (block - a.first_block[part]), col = first + 2 * threadIdx.x;
+    const bool in = col < o.part_end[part], has = id >= 0 && id < o.n_adapters;
+    if (!has && o.base == o.Z) return;
+    typedef T pair_t __attribute__((ext_vector_type(2)));
+    pair_t x = {};
+    if (in) x = *reinterpret_cast<const pair_t*>((const T*)o.base + row * o.ldb + col);
+    if (has) {
+        constexpr int PER = 16 / sizeof(T), TOGETHER = 16 / PER;             // rank values of a load, loads sent for together
+        const T* B = (const T*)o.B + id * o.b_stride + col * o.ldbw;
+        u32x4_t y[2][TOGETHER];
+        auto read = [&](int r) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t) sum[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < steps; ++s) {
-        const Rank r = rank_of<T>(o.rank, s, g);
-        piece_t z = none<T>();
-        Tile of = rows;
-        bool first_batch = true;
-        for (int k = 0; of.left;) {
-            int w[TOGETHER], n = 0;
-            bool live[TOGETHER];
-            piece_t y[TOGETHER][4];
+            for (int k = 0; k < 2; ++k)
 #pragma unroll
-            for (int u = 0; u < TOGETHER; ++u) {
-                // the next adapter of this wave
-                w[u] = -1;
-                live[u] = false;
-                while (of.left) {
-                    const int next = of.next();
-                    if (k++ % kWaves == wave) { w[u] = next; live[u] = of.live; ++n; break; }
-                }
-                const T* B = (const T*)o.B + w[u] * o.b_stride + r.piece * PER;
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const int j = first + column_of(t, c);
-                    y[u][t] = none<T>();
-                    if (w[u] >= 0 && r.there && j < end) y[u][t] = *reinterpret_cast<const piece_t*>(B + j * o.ldbw);
-                }
-            }
-            if (first_batch) {                               // (behind the adapters' loads: the two trips go together)
-                first_batch = false;
-                if (r.there && rows.id >= 0) {
-                    float v[PER];
-                    read_t<T>(a, a.t + (int64_t)row * a.all + part * o.rank + r.piece * PER, scale, v);
-                    z = piece_of(v, r.rest);
-                }
-            }
+                for (int u = 0; u < TOGETHER; ++u)
+                    if (in && r + u * PER < o.rank) y[k][u] = *reinterpret_cast<const u32x4_t*>(B + k * o.ldbw + r + u * PER);
+        };
+        read(0);
+        if ((int)threadIdx.x < o.rank) {
+            float sum = 0.f;
+            const float* from = a.t + (int64_t)row * a.all + part * o.rank + threadIdx.x;
+#pragma unroll 8
+            for (int s = 0; s < a.splits; ++s) sum += from[(int64_t)s * o.n * a.all];
+            t[threadIdx.x] = sum;
+        }
+        const float scale = o.scale ? o.scale[id] : 1.f;
+        __syncthreads();
+        float sum[2] = {0.f, 0.f};
+        for (int r = 0; r < o.rank; r += 16) {
 #pragma unroll
             for (int u = 0; u < TOGETHER; ++u) {
-                if (u >= n) break;
-                mine |= live[u];
+                if (r + u * PER >= o.rank) break;
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const f32x4_t with = L::multiply(y[u][t], z, sum[t]);
+                for (int e = 0; e < PER; ++e) {
+                    const float with = t[r + u * PER + e];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sum[t][e] = live[u] ? with[e] : sum[t][e];
+                    for (int k = 0; k < 2; ++k) {
+                        const float b = sizeof(T) == 4 ? __uint_as_float(y[k][u][e & 3]) : __uint_as_float(e & 1 ? y[k][u][e >> 1] & 0xFFFF0000u : y[k][u][e >> 1] << 16);
+                        sum[k] += with * b;
+                    }
                 }
             }
+            read(r + 16);
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if constexpr (sizeof(T) == 4) x[k] += scale * sum[k];
+            else x[k] = __builtin_bit_cast(uint16_t, (__bf16)(__uint_as_float((uint32_t)x[k] << 16) + scale * sum[k]));
         }
     }
-    if (!mine || tile * 16 + c >= o.n) return;
-    if (rows.id >= 0) x.add(sum);
-    x.store(out, one, two);
+    if (in) *reinterpret_cast<pair_t*>((T*)o.Z + row * o.ldz + col) = x;
 }
 
 // Many rows: which go together.  One workgroup counts the rows of every adapter (and of none), deals out places and groups, and puts the rows into their
@@ -385,22 +347,26 @@ void adapt_order_kernel(AdaptArgs a) {
     for (int i = KEPT; i < rounds; ++i) put(i, read(i));
 }
 
-// The rows of a workgroup's group, or, where none were made, 64 rows as they come: lane l of a wave has row l and its adapter.
-struct Group {
-    int count, id, row_of_lane;
+// Rows `first` ... of a group, or, where none were made, of 64 rows as they come, up to SIZE of them: lane l of a wave has row l (the last one's again behind the last),
+// its adapter, and whether there is one.
+template <int SIZE>
+struct Some {
+    int count, id, row;
     uint64_t left;                       // rows of adapters still to come
-    __device__ __forceinline__ bool find(const AdaptArgs& a) {
+    __device__ __forceinline__ bool find(const AdaptArgs& a, int at, int first) {
         const int lane = threadIdx.x & 63;
         if (a.groups) {
-            if ((int)blockIdx.x >= *a.n_groups) return false;
-            const int4 group = a.groups[blockIdx.x];
-            count = group.z;
-            row_of_lane = a.order[group.y + min(lane, count - 1)];
+            if (at >= *a.n_groups) return false;
+            const int4 group = a.groups[at];
+            count = min(group.z - first, SIZE);
+            if (count <= 0) return false;
+            row = a.order[group.y + first + min(lane, count - 1)];
             id = lane < count ? group.x : -1;
         } else {
-            count = min(a.o.n - (int)blockIdx.x * kGroup, kGroup);
-            row_of_lane = blockIdx.x * kGroup + min(lane, count - 1);
-            id = lane < count ? a.o.which[row_of_lane] : -1;
+            count = min(a.o.n - at * kGroup - first, SIZE);
+            if (count <= 0) return false;
+            row = at * kGroup + first + min(lane, count - 1);
+            id = lane < count ? a.o.which[row] : -1;
             if (id >= a.o.n_adapters) id = -1;
         }
         left = __ballot(id >= 0);
@@ -414,132 +380,135 @@ struct Group {
     }
 };
 
-// Many rows, the first product.  A workgroup: one group, 64 rows of A, one part of d, whose steps its waves share out.
+// Many rows, the first product.  A workgroup: one group, 64 rows of A, one part of d, whose steps its waves share out.  Columns of rows of other adapters come
+// out as they may and are not kept, so the rows are sent for before their adapters are known.  Neighbouring groups go to one die: its L2 then has their A.
+// (16 rows and all of d to a workgroup: every 16 rows read A for themselves, 4096 rows 26 us instead of 13.  Half as many waves: twice the parts of d, which the second
+// product reads once for each of its workgroups, 60 instead of 57.5 for both.)
+constexpr int kDownWaves = 8;
 template <class T>
-__global__ __launch_bounds__(64 * kWaves, 2)
+__global__ __launch_bounds__(64 * kDownWaves, 2)
 void adapt_many_down_kernel(AdaptArgs a) {
     typedef Lane<T> L;
     typedef typename L::piece_t piece_t;
     constexpr int STEP = 4 * L::PER, RT = 4, HT = kGroup / 16, AHEAD = 4;
     const Adapt& o = a.o;
-    __shared__ f32x4_t sums[kWaves][RT][64];
-    Group group;
-    if (!group.find(a)) return;
+    __shared__ f32x4_t sums[kDownWaves][RT][64];
+    const int groups = a.groups ? *a.n_groups : (o.n + kGroup - 1) / kGroup, to_die = (groups + 7) / 8;
+    if ((int)blockIdx.x >> 3 >= to_die) return;
+    Some<kGroup> rows;
+    if (!rows.find(a, (blockIdx.x & 7) * to_die + (blockIdx.x >> 3), 0)) return;
     const int split = blockIdx.y, first_rank = blockIdx.z * 16 * RT;
     const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int rank_tiles = min((a.all - first_rank + 15) / 16, RT);
     const int begin = split * a.steps, end = min(begin + a.steps, (o.d + STEP - 1) / STEP);
-    int row[HT];
     const T* h[HT];
 #pragma unroll
-    for (int i = 0; i < HT; ++i) {
-        row[i] = __shfl(group.row_of_lane, 16 * i + c, 64);
-        h[i] = (const T*)o.H + row[i] * o.ldh;
-    }
-    while (group.left) {
-        uint64_t those;
-        const int w = group.next(&those);
-        const T* A = (const T*)o.A + w * o.a_stride;
-        bool live[HT], any[HT];
+    for (int i = 0; i < HT; ++i) h[i] = (const T*)o.H + __shfl(rows.row, 16 * i + c, 64) * o.ldh;
+    piece_t x[AHEAD][HT];
+    auto read_h = [&](int s0) {
 #pragma unroll
-        for (int i = 0; i < HT; ++i) { live[i] = (those >> (16 * i + c)) & 1; any[i] = (those >> (16 * i)) & 0xFFFF; }
+        for (int u = 0; u < AHEAD; ++u) {
+            const int col = (s0 + u) * STEP + g * L::PER;
+#pragma unroll
+            for (int i = 0; i < HT; ++i) {
+                x[u][i] = none<T>();
+                if (s0 + u < end && col < o.d) x[u][i] = *reinterpret_cast<const piece_t*>(h[i] + col);
+            }
+        }
+    };
+    const int first = begin + wave * AHEAD;
+    read_h(first);
+    bool there = true;
+    while (rows.left) {
+        uint64_t those;
+        const int w = rows.next(&those);
+        const T* A = (const T*)o.A + w * o.a_stride;
         f32x4_t sum[HT][RT];
 #pragma unroll
         for (int i = 0; i < HT; ++i)
 #pragma unroll
             for (int t = 0; t < RT; ++t) sum[i][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        for (int s0 = begin + wave; s0 < end; s0 += kWaves * AHEAD) {
-            piece_t x[AHEAD][HT], y[AHEAD][RT];
-#pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                const int s = s0 + u * kWaves, col = s * STEP + g * L::PER;
-                const bool there = s < end && col < o.d;
-#pragma unroll
-                for (int i = 0; i < HT; ++i) {
-                    x[u][i] = none<T>();
-                    if (there && live[i]) x[u][i] = *reinterpret_cast<const piece_t*>(h[i] + col);
-                }
-#pragma unroll
-                for (int t = 0; t < RT; ++t) {
-                    const int r = first_rank + 16 * t + c;
-                    y[u][t] = none<T>();
-                    if (there && r < a.all) y[u][t] = *reinterpret_cast<const piece_t*>(A + r * o.lda + col);
-                }
-            }
+        for (int s0 = first; s0 < end; s0 += kDownWaves * AHEAD) {
+            if (!there) read_h(s0);
+            there = false;
 #pragma unroll
             for (int t = 0; t < RT; ++t) {
                 if (t >= rank_tiles) break;
+                const int r = first_rank + 16 * t + c;
+                piece_t y[AHEAD];
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) {
+                    const int col = (s0 + u) * STEP + g * L::PER;
+                    y[u] = none<T>();
+                    if (s0 + u < end && col < o.d && r < a.all) y[u] = *reinterpret_cast<const piece_t*>(A + r * o.lda + col);
+                }
 #pragma unroll
                 for (int u = 0; u < AHEAD; ++u)
 #pragma unroll
-                    for (int i = 0; i < HT; ++i) sum[i][t] = L::multiply(y[u][t], x[u][i], sum[i][t]);
+                    for (int i = 0; i < HT; ++i) sum[i][t] = L::multiply(y[u], x[u][i], sum[i][t]);
             }
         }
         // one tile of rows after the other through LDS; wave t adds up tile t of ranks: rank 16 t + 4 g + r of row c
 #pragma unroll
         for (int i = 0; i < HT; ++i) {
-            if (!any[i]) continue;
+            if (!((those >> (16 * i)) & 0xFFFF)) continue;
             __syncthreads();
 #pragma unroll
             for (int t = 0; t < RT; ++t) sums[wave][t][lane] = sum[i][t];
             __syncthreads();
-            if (wave < rank_tiles && live[i]) {
-                f32x4_t all = sums[0][wave][lane];
+            const int r = first_rank + 16 * wave + 4 * g, row = __shfl(rows.row, 16 * i + c, 64);
+            if (wave >= rank_tiles || r >= a.all || !((those >> (16 * i + c)) & 1)) continue;
+            f32x4_t all = sums[0][wave][lane];
 #pragma unroll
-                for (int k = 1; k < kWaves; ++k) all += sums[k][wave][lane];
-                const int r = first_rank + 16 * wave + 4 * g;
-                if (r < a.all) *reinterpret_cast<f32x4_t*>(a.t + ((int64_t)split * o.n + row[i]) * a.all + r) = all;
-            }
+            for (int k = 1; k < kDownWaves; ++k) all += sums[k][wave][lane];
+            *reinterpret_cast<f32x4_t*>(a.t + ((int64_t)split * o.n + row) * a.all + r) = all;
         }
     }
 }
 
-// Many rows, the second product.  A workgroup: one group, `wide` columns of one part, 64 at a time to a wave.  The operands that T makes lie in LDS.
-template <class T>
-__global__ __launch_bounds__(64 * kWaves, 2)
+// Many rows, the second product.  A workgroup: half a group, 256 columns of one part, 64 to a wave.  What the matrix instructions leave goes through LDS, so that base is read
+// and Z written a row's 256 columns at a time (4096 x 12288 values in and out: 36 us; as the instructions leave them, 16 rows at a time, 41 to 45).  The workgroups of a
+// row's columns come one after the other, for memory's sake too (42 where those of a column do).  HALF: steps of a rank's upper parts at most.
+constexpr int kUpRows = 32, kUpCols = 256;
+template <class T, int HALF>
+__global__ __launch_bounds__(64 * kWaves, HALF <= 2 ? 4 : 2)
 void adapt_many_up_kernel(AdaptArgs a) {
     typedef Lane<T> L;
     typedef typename L::piece_t piece_t;
-    constexpr int PER = L::PER, HT = kGroup / 16, MOST = 8;  // steps of a rank of 128
+    constexpr int PER = L::PER, HT = kUpRows / 16, TWICE = sizeof(T) == 2 ? 2 : 1, THREADS = 64 * kWaves;
+    constexpr int VEC = 16 / sizeof(T), TO_ROW = kUpCols / VEC, VECS = kUpRows * TO_ROW / THREADS;         // 16 bytes of a row to a thread
     const Adapt& o = a.o;
-    __shared__ piece_t z[MOST][HT][64];
-    Group group;
-    if (!group.find(a)) return;
+    __shared__ piece_t z[TWICE * HALF][HT][64];
+    __shared__ __attribute__((aligned(16))) float sums[kUpRows][kUpCols + 4];
+    const int blocks = a.first_block[o.n_parts], of_rows = blockIdx.x / blocks, block = blockIdx.x - of_rows * blocks;
+    Some<kUpRows> rows;
+    if (!rows.find(a, of_rows / (kGroup / kUpRows), kUpRows * (of_rows % (kGroup / kUpRows)))) return;
     const bool in_place = o.base == o.Z;
-    const uint64_t with = group.left;                        // rows that have an adapter
-    if (!with && in_place) return;
+    const uint64_t with = rows.left;                         // rows that have an adapter
     const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int part = part_of_block(a, blockIdx.y);
-    const int first = (part > 0 ? o.part_end[part - 1] : 0) + a.wide * (blockIdx.y - a.first_block[part]), end = min(first + a.wide, o.part_end[part]);
-    const int steps = steps_of_rank<T>(o.rank), tiles = (group.count + 15) / 16;
-    const T* base[HT];
-    T* out[HT];
-#pragma unroll
-    for (int i = 0; i < HT; ++i) {
-        const int64_t row = __shfl(group.row_of_lane, 16 * i + c, 64);
-        base[i] = (const T*)o.base + row * o.ldb;
-        out[i] = (T*)o.Z + row * o.ldz;
-    }
-    Sixteen<T> x[HT];
+    const int part = part_of_block(a, block);
+    const int first = (part > 0 ? o.part_end[part - 1] : 0) + a.wide * (block - a.first_block[part]), end = min(first + a.wide, o.part_end[part]);
+    const int pieces = o.rank / PER, steps = steps_of_rank<T>(o.rank), half = (pieces + 3) / 4;
+    // base: 16 bytes of row i of the group, 256 columns at a time
+    u32x4_t x[VECS];
     auto read = [&](int at) {
-        const int col = at + 8 * g;
 #pragma unroll
-        for (int i = 0; i < HT; ++i)
-            if (i < tiles) x[i].load(base[i] + col, col < end, col + 32 < end);
+        for (int k = 0; k < VECS; ++k) {
+            const int e = threadIdx.x + k * THREADS, i = e / TO_ROW, col = at + VEC * (e - i * TO_ROW);
+            const int64_t row = __shfl(rows.row, i, 64);
+            if (col < end && i < rows.count) x[k] = *reinterpret_cast<const u32x4_t*>((const T*)o.base + row * o.ldb + col);
+        }
     };
-    read(first + 64 * wave);
-    // a thread: one row's PER rank values
-    const int pieces = o.rank / PER;
-    for (int e = threadIdx.x; e < kGroup * MOST * 4; e += 64 * kWaves) {
-        const int i = e & (kGroup - 1), q = e / kGroup;      // (a row of its own to each lane of a wave, whose q is one)
-        if (q >= 4 * steps) break;
-        const bool there = q < pieces && ((with >> i) & 1);
+    read(first);
+    // one row's PER rank values to a thread, those of a row side by side (what a row without an adapter has there is not used)
+    const int slots = 4 * half;                              // pieces, and nothing to fill a step up with
+    for (int e = threadIdx.x; e < kUpRows * slots; e += THREADS) {
+        const int i = e / slots, q = e - i * slots, to = i & 15;
+        const int row = __shfl(rows.row, i, 64), w = __shfl(rows.id, i, 64);
         float v[PER];
 #pragma unroll
         for (int k = 0; k < PER; ++k) v[k] = 0.f;
-        const int row = __shfl(group.row_of_lane, i, 64), w = __shfl(group.id, i, 64);
-        if (there) read_t<T>(a, a.t + (int64_t)row * a.all + part * o.rank + q * PER, o.scale ? o.scale[w] : 1.f, v);
-        const int half = (pieces + 3) / 4, to = (i & 15);
+        if (q < pieces) read_t<T>(a, a.t + (int64_t)row * a.all + part * o.rank + q * PER, w >= 0 && o.scale ? o.scale[w] : 1.f, v);
         if constexpr (sizeof(T) == 4) {
             z[q >> 2][i >> 4][16 * (q & 3) + to] = piece_of(v, false);
         } else if (pieces <= 2) {
@@ -550,58 +519,79 @@ void adapt_many_up_kernel(AdaptArgs a) {
             } else if (q >= 2 * pieces) {
                 z[0][i >> 4][16 * q + to] = none<T>();
             }
-        } else if (q < 4 * half) {
+        } else {
             z[q >> 2][i >> 4][16 * (q & 3) + to] = piece_of(v, false);
             z[half + (q >> 2)][i >> 4][16 * (q & 3) + to] = piece_of(v, true);
         }
     }
-    __syncthreads();
-    for (int at = first + 64 * wave; at < end; at += 64 * kWaves) {
-        const int col = at + 8 * g;
-        f32x4_t sum[HT][4];
+    piece_t y[HALF][4];
+    auto read_b = [&](int w, int at) {
+        const T* B = (const T*)o.B + w * o.b_stride;
 #pragma unroll
-        for (int i = 0; i < HT; ++i)
+        for (int s = 0; s < HALF; ++s) {
+            if (s >= half) break;
+            const Rank r = rank_of<T>(o.rank, s, g);
 #pragma unroll
-            for (int t = 0; t < 4; ++t) sum[i][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        Group of = group;
-        while (of.left) {
-            uint64_t those;
-            const int w = of.next(&those);
-            const T* B = (const T*)o.B + w * o.b_stride;
-            const bool alone = those == with;                // no rows of other adapters: they would have to be kept
-            for (int s = 0; s < steps; ++s) {
-                const Rank r = rank_of<T>(o.rank, s, g);
-                piece_t y[4];
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const int j = at + column_of(t, c);
-                    y[t] = none<T>();
-                    if (r.there && j < end) y[t] = *reinterpret_cast<const piece_t*>(B + j * o.ldbw + r.piece * PER);
-                }
-#pragma unroll
-                for (int i = 0; i < HT; ++i) {
-                    const piece_t zi = z[s][i][lane];
-                    const bool live = alone || ((those >> (16 * i + c)) & 1);
-#pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        const f32x4_t more = L::multiply(y[t], zi, sum[i][t]);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) sum[i][t][e] = live ? more[e] : sum[i][t][e];
-                    }
-                }
+            for (int t = 0; t < 4; ++t) {
+                const int j = at + 64 * wave + 16 * t + c;
+                y[s][t] = none<T>();
+                if (r.there && j < end) y[s][t] = *reinterpret_cast<const piece_t*>(B + j * o.ldbw + r.piece * PER);
             }
         }
-        Sixteen<T> was[HT];
+    };
+    Some<kUpRows> of = rows;
+    uint64_t those = 0;
+    const int w0 = with ? of.next(&those) : 0;
+    const bool alone = those == with;                        // one adapter at most
+    if (with && alone) read_b(w0, first);
+    for (int at = first; at < end; at += kUpCols) {
+        __syncthreads();
+        if (with) {
 #pragma unroll
-        for (int i = 0; i < HT; ++i) was[i] = x[i];
-        read(at + 64 * kWaves);
+            for (int i = 0; i < HT; ++i) {
+                f32x4_t sum[4];
 #pragma unroll
-        for (int i = 0; i < HT; ++i) {
-            const int k = 16 * i + c;
-            const bool has = (with >> k) & 1;
-            if (k >= group.count || (!has && in_place)) continue;
-            if (has) was[i].add(sum[i]);
-            was[i].store(out[i] + col, col < end, col + 32 < end);
+                for (int t = 0; t < 4; ++t) sum[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+                of = rows;
+                of.left &= 0xFFFFull << (16 * i);            // this tile's rows
+                while (of.left) {
+                    const int w = of.next(&those);
+                    of.left &= 0xFFFFull << (16 * i);
+                    if (!alone) read_b(w, at);
+                    const bool live = alone || ((those >> (16 * i + c)) & 1);
+#pragma unroll
+                    for (int s = 0; s < HALF; ++s) {
+                        if (s >= half) break;
+                        for (int k = s; k < steps; k += half) {
+                            const piece_t zi = z[k][i][lane];
+#pragma unroll
+                            for (int t = 0; t < 4; ++t) {
+                                const f32x4_t more = L::multiply(y[s][t], zi, sum[t]);
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) sum[t][e] = live ? more[e] : sum[t][e];
+                            }
+                        }
+                    }
+                }
+                // columns 16 t + 4 g ... of row c
+#pragma unroll
+                for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4_t*>(&sums[16 * i + c][64 * wave + 16 * t + 4 * g]) = sum[t];
+            }
+        }
+        if (with && alone && at + kUpCols < end) read_b(w0, at + kUpCols);
+        __syncthreads();
+        u32x4_t was[VECS];
+#pragma unroll
+        for (int k = 0; k < VECS; ++k) was[k] = x[k];
+        if (at + kUpCols < end) read(at + kUpCols);
+#pragma unroll
+        for (int k = 0; k < VECS; ++k) {
+            const int e = threadIdx.x + k * THREADS, i = e / TO_ROW, col = at + VEC * (e - i * TO_ROW);
+            const int64_t row = __shfl(rows.row, i, 64);
+            const bool has = (with >> i) & 1;
+            if (col >= end || i >= rows.count || (!has && in_place)) continue;
+            if (has) add_to(was[k], &sums[i][col - at], T());
+            *reinterpret_cast<u32x4_t*>((T*)o.Z + row * o.ldz + col) = was[k];
         }
     }
 }
@@ -618,16 +608,17 @@ Plan plan_of(int is_bf16, int n, int d, int p, int rank, int n_parts, int n_adap
     const int all = steps_of(is_bf16, d), rank_groups = (rank * n_parts + 63) / 64;
     const int64_t alone = n_adapters < n ? n_adapters + 1 : n;          // groups that are not full
     r.most_groups = r.ordered ? n / kGroup + alone : r.many ? (n + kGroup - 1) / kGroup : 0;
-    // 512 workgroups for the first product fill the chip; few rows have an adapter each as a rule
-    const int64_t items = (r.many ? (n + kGroup - 1) / kGroup : n) * (int64_t)rank_groups;
-    int64_t cuts = items >= 512 ? 1 : 512 / items;
-    const int most = (all + 15) / 16;                        // four steps to a wave
+    // workgroups that fill the chip with the first product, of 8 waves or (few rows, which have an adapter each as a rule) 4; four steps to a wave at least
+    const int64_t items = (r.many ? (n + kGroup - 1) / kGroup : n) * (int64_t)rank_groups, target = r.many ? 256 : 512;
+    int64_t cuts = items >= target ? 1 : target / items;
+    const int to_each = 4 * (r.many ? kDownWaves : kWaves), most = (all + to_each - 1) / to_each;
     cuts = cuts < most ? cuts : most;
     cuts = cuts < (r.many ? 8 : 16) ? cuts : (r.many ? 8 : 16);
     r.steps = (int)((all + cuts - 1) / cuts);
     r.splits = (all + r.steps - 1) / r.steps;
-    r.wide = 64;
-    if (r.many) for (r.wide = 1024; r.wide > 256 && (n + kGroup - 1) / kGroup * (int64_t)((p + r.wide - 1) / r.wide) < 512;) r.wide /= 2;
+    // two blocks of columns to a workgroup of the second product where that leaves 1024 of them: it reads T once (4096 rows, us: 62 with one, 57.5, 61 with four)
+    r.wide = kFewCols;
+    if (r.many) for (r.wide = 2 * kUpCols; r.wide > kUpCols && (n + kUpRows - 1) / kUpRows * (int64_t)((p + r.wide - 1) / r.wide) < 1024;) r.wide /= 2;
     r.t_bytes = round_up((int64_t)r.splits * n * rank * n_parts * sizeof(float), 256);
     r.bytes = r.t_bytes + (r.ordered ? round_up(4 * (int64_t)n, 256) + 16 * r.most_groups + 256 : 0);
     return r;
@@ -651,13 +642,18 @@ hipError_t launch(const Adapt& o, hipStream_t stream) {
     a.order = (int*)(ws + p.t_bytes + 256 + 16 * p.most_groups);
     if (p.many) {
         if (p.ordered) hipLaunchKernelGGL(adapt_order_kernel, dim3(1), dim3(kOrderThreads), 0, stream, a);
-        hipLaunchKernelGGL(adapt_many_down_kernel<T>, dim3((unsigned)p.most_groups, a.splits, rank_groups), dim3(64 * kWaves), 0, stream, a);
-        hipLaunchKernelGGL(adapt_many_up_kernel<T>, dim3((unsigned)p.most_groups, blocks), dim3(64 * kWaves), 0, stream, a);
+        hipLaunchKernelGGL(adapt_many_down_kernel<T>, dim3((unsigned)round_up(p.most_groups, 8), a.splits, rank_groups), dim3(64 * kDownWaves), 0, stream, a);
+        const dim3 up((unsigned)(kGroup / kUpRows * p.most_groups * blocks));
+        const int half = (o.rank + 4 * Lane<T>::PER - 1) / (4 * Lane<T>::PER);
+        if (half <= 1) hipLaunchKernelGGL((adapt_many_up_kernel<T, 1>), up, dim3(64 * kWaves), 0, stream, a);
+        else if (half <= 2) hipLaunchKernelGGL((adapt_many_up_kernel<T, 2>), up, dim3(64 * kWaves), 0, stream, a);
+        else if (half <= 4) hipLaunchKernelGGL((adapt_many_up_kernel<T, 4>), up, dim3(64 * kWaves), 0, stream, a);
+        else hipLaunchKernelGGL((adapt_many_up_kernel<T, 8>), up, dim3(64 * kWaves), 0, stream, a);
         return hipGetLastError();
     }
     const int tiles = (o.n + 15) / 16;
     hipLaunchKernelGGL(adapt_few_down_kernel<T>, dim3(tiles * 16, a.splits, rank_groups), dim3(64 * kWaves), 0, stream, a);
-    hipLaunchKernelGGL(adapt_few_up_kernel<T>, dim3(blocks, tiles), dim3(64 * kWaves), 0, stream, a);
+    hipLaunchKernelGGL(adapt_few_up_kernel<T>, dim3((unsigned)(blocks * o.n)), dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 
@@ -665,12 +661,14 @@ hipError_t launch(const Adapt& o, hipStream_t stream) {
 
 bool adapt_fits(const Adapt& o, int is_bf16) {
     const Plan p = plan_of(is_bf16, o.n, o.d, o.p, o.rank, o.n_parts, o.n_adapters);
-    const int64_t groups = p.many ? p.most_groups : (o.n + 15) / 16 * 16, blocks = o.p / p.wide + o.n_parts, most = kMostThreads / (64 * kWaves);
-    return (p.many || (o.n + 15) / 16 <= 65535) && blocks <= 65535 && groups * blocks <= most && groups * p.splits * ((o.rank * o.n_parts + 63) / 64) <= most;
+    const int64_t blocks = o.p / p.wide + o.n_parts, most = kMostThreads / (64 * kWaves), rank_groups = (o.rank * o.n_parts + 63) / 64;
+    if (p.many) return kGroup / kUpRows * p.most_groups * blocks <= most && 2 * round_up(p.most_groups, 8) * p.splits * rank_groups <= most;
+    const int64_t tiles = (o.n + 15) / 16;
+    return o.n * blocks <= most && 16 * tiles * p.splits * rank_groups <= most;
 }
 
 size_t adapt_workspace_bytes(const Adapt& o, int is_bf16) { return (size_t)plan_of(is_bf16, o.n, o.d, o.p, o.rank, o.n_parts, o.n_adapters).bytes; }
-// What any call of up to so many rows, ranks and adapters needs: the parts of d are at most 512 over the workgroups of one part, of 1 row or 64.
+// What any call of up to so many rows, ranks and adapters needs: the parts of d are at most 512 over the workgroups of one part, of 1 row (many rows: 64).
 size_t adapt_workspace_bound(int n, int rank, int n_parts, int n_adapters) {
     const int64_t most = 8 * (int64_t)n < 512 * kGroup ? 8 * (int64_t)n : 512 * kGroup, rows = n <= kFewRows ? 512 : n > most ? n : most;
     const int64_t alone = n_adapters < n ? n_adapters + 1 : n;
