@@ -47,10 +47,10 @@ struct AdaptArgs {
     int wide;                            // columns of a workgroup of the second product: a multiple of 64
     int first_block[kMostParts + 1];     // blocks of so many columns before a part
     float* t;                            // [split][row][all]
-    // many rows
-    int* order;                          // rows, those of one adapter side by side
-    int4* groups;                        // of each group: its adapter (-1: none), where it begins in `order`, its rows; null: rows as they come
-    int* n_groups;
+    // many rows put in order; null: as they come
+    int2* groups;                        // of each group its adapter (-1: none) and how many rows it has; n_groups of them, some have none
+    int* order;                          // 64 places to each group
+    int n_groups;
 };
 
 __device__ __forceinline__ int part_of_block(const AdaptArgs& a, int block) {
@@ -264,87 +264,84 @@ void adapt_few_up_kernel(AdaptArgs a) {
     if (in) *reinterpret_cast<pair_t*>((T*)o.Z + row * o.ldz + col) = x;
 }
 
-// Many rows: which go together.  One workgroup counts the rows of every adapter (and of none), deals out places and groups, and puts the rows into their
-// places; where among its adapter's a row comes goes by the order of atomic additions, and nothing goes by that.
+// Many rows: which go together.  One workgroup counts the rows of every adapter (and of none), deals out groups, and puts the rows into their places; where
+// among its adapter's a row comes goes by the order of atomic additions, and nothing goes by that.  Groups of one adapter have numbers 8 apart: workgroups of such numbers
+// meet on one die, whose L2 then has what they share.
 constexpr int kOrderThreads = 1024, kMostBins = 12288, kGroup = 64;
 __global__ __launch_bounds__(kOrderThreads)
 void adapt_order_kernel(AdaptArgs a) {
     const Adapt& o = a.o;
     __shared__ int bins[kMostBins];
-    __shared__ int2 sums[kOrderThreads / 64];
+    __shared__ int sums[kOrderThreads / 64];
     const int n_bins = o.n_adapters + 1, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     auto bin_of = [&](int w) { return w >= 0 && w < o.n_adapters ? w : o.n_adapters; };
     for (int i = threadIdx.x; i < n_bins; i += kOrderThreads) bins[i] = 0;
     __syncthreads();
     // Adds the rows of a wave to their bins and returns where each comes.  Rows of one adapter side by side are one addition: as many from one address are one after
-    // the other (4096 rows of 8 adapters: 10.8 us with an addition each).
-    auto add = [&](int bin, bool there) {
-        int at = 0;
-        uint64_t left = __ballot(there);
-        for (int turn = 0; turn < 4 && left; ++turn) {
-            const int leader = __builtin_ctzll(left), same = __shfl(bin, leader, 64);
-            const uint64_t those = __ballot(bin == same) & left;
-            int first = 0;
-            if (lane == leader) first = atomicAdd(&bins[same], __popcll(those));
-            first = __shfl(first, leader, 64);
-            if ((those >> lane) & 1) at = first + __popcll(those & ((1ull << lane) - 1));
-            left &= ~those;
-        }
-        if ((left >> lane) & 1) at = atomicAdd(&bins[bin], 1);
-        return at;
+    // the other.
+    auto add = [&](int bin, bool there) -> int {
+        const uint64_t all = __ballot(there);
+        if (!all) return 0;
+        const int leader = __builtin_ctzll(all), same = __builtin_amdgcn_readlane(bin, leader);
+        if ((__ballot(bin == same) & all) != all) return there ? atomicAdd(&bins[bin], 1) : 0;
+        int first = 0;
+        if (lane == leader) first = atomicAdd(&bins[same], __popcll(all));
+        return __builtin_amdgcn_readlane(first, leader) + __popcll(all & ((1ull << lane) - 1));
     };
     const int rounds = (o.n + kOrderThreads - 1) / kOrderThreads;
     auto row_of = [&](int i) { return i * kOrderThreads + (int)threadIdx.x; };
     auto read = [&](int i) { return row_of(i) < o.n ? bin_of(o.which[row_of(i)]) : 0; };
-    constexpr int KEPT = 8;                                  // rounds whose numbers stay in registers
-    int kept[KEPT];
+    constexpr int KEPT = 8;                                  // rounds whose numbers and places stay in registers: the last places of their bins
+    int kept[KEPT], place[KEPT];
 #pragma unroll
     for (int i = 0; i < KEPT; ++i) kept[i] = read(i);
-#pragma unroll
-    for (int i = 0; i < KEPT; ++i) add(kept[i], row_of(i) < o.n);
     for (int i = KEPT; i < rounds; ++i) add(read(i), row_of(i) < o.n);
+    if (rounds > KEPT) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < KEPT; ++i) place[i] = i < rounds ? add(kept[i], row_of(i) < o.n) : 0;
     __syncthreads();
-    // rows and groups before each thread's bins
+    // groups before each thread's bins
     const int each = (n_bins + kOrderThreads - 1) / kOrderThreads, first = threadIdx.x * each, last = min(first + each, n_bins);
-    int2 mine = {0, 0};
-    for (int i = first; i < last; ++i) { mine.x += bins[i]; mine.y += (bins[i] + kGroup - 1) / kGroup; }
-    int2 upto = mine;
+    int mine = 0;
+    for (int i = first; i < last; ++i) mine += (bins[i] + kGroup - 1) / kGroup;
+    int upto = mine;
     for (int by = 1; by < 64; by *= 2) {
-        const int x = __shfl_up(upto.x, by, 64), y = __shfl_up(upto.y, by, 64);
-        if (lane >= by) { upto.x += x; upto.y += y; }
+        const int x = __shfl_up(upto, by, 64);
+        if (lane >= by) upto += x;
     }
     if (lane == 63) sums[wave] = upto;
     __syncthreads();
-    int2 before = {upto.x - mine.x, upto.y - mine.y};
-    int groups = 0;
+    int before = upto - mine, groups = 0;
     for (int i = 0; i < kOrderThreads / 64; ++i) {
-        if (i < wave) { before.x += sums[i].x; before.y += sums[i].y; }
-        groups += sums[i].y;
+        if (i < wave) before += sums[i];
+        groups += sums[i];
     }
-    if (threadIdx.x == 0) *a.n_groups = groups;
+    const int to_die = (groups + 7) / 8;
+    auto number = [&](int k) { return k % to_die * 8 + k / to_die; };            // of the k-th group
+    for (int i = threadIdx.x; i < a.n_groups; i += kOrderThreads)
+        if (i >> 3 >= to_die || (i & 7) * to_die + (i >> 3) >= groups) a.groups[i] = int2{-1, 0};
     for (int j = 0; j < each; ++j) {
         const int i = first + j, count = i < last ? bins[i] : 0, w = i < o.n_adapters ? i : -1, in_bin = (count + kGroup - 1) / kGroup;
-        if (i < last) bins[i] = before.x;
-        auto put = [&](int k, int w, int2 before, int count) { a.groups[before.y + k] = int4{w, before.x + kGroup * k, min(count - kGroup * k, kGroup), 0}; };
+        if (i < last) bins[i] = before * kGroup;
+        auto put = [&](int k, int w, int before, int count) { a.groups[number(before + k)] = int2{w, min(count - kGroup * k, kGroup)}; };
         constexpr int FEW = 4;
         for (int k = 0; k < min(in_bin, FEW); ++k) put(k, w, before, count);
         // the other groups of a large bin: its wave
         for (uint64_t large = __ballot(in_bin > FEW); large; large &= large - 1) {
-            const int from = __builtin_ctzll(large), all = __shfl(in_bin, from, 64), c = __shfl(count, from, 64), its = __shfl(w, from, 64);
-            const int2 at = {__shfl(before.x, from, 64), __shfl(before.y, from, 64)};
+            const int from = __builtin_ctzll(large), all = __shfl(in_bin, from, 64), c = __shfl(count, from, 64), its = __shfl(w, from, 64), at = __shfl(before, from, 64);
             for (int k = FEW + lane; k < all; k += 64) put(k, its, at, c);
         }
-        before.x += count;
-        before.y += in_bin;
+        before += in_bin;
     }
     __syncthreads();
-    auto put = [&](int i, int bin) {
-        const int at = add(bin, row_of(i) < o.n);
-        if (row_of(i) < o.n) a.order[at] = row_of(i);
+    auto put = [&](int i, int at) {
+        if (row_of(i) < o.n) a.order[number(at / kGroup) * kGroup + at % kGroup] = row_of(i);
     };
 #pragma unroll
-    for (int i = 0; i < KEPT; ++i) put(i, kept[i]);
-    for (int i = KEPT; i < rounds; ++i) put(i, read(i));
+    for (int i = 0; i < KEPT; ++i) if (i < rounds) put(i, bins[kept[i]] + place[i]);
+    if (rounds <= KEPT) return;
+    __syncthreads();
+    for (int i = KEPT; i < rounds; ++i) put(i, add(read(i), row_of(i) < o.n));
 }
 
 // Rows `first` ... of a group, or, where none were made, of 64 rows as they come, up to SIZE of them: lane l of a wave has row l (the last one's again behind the last),
@@ -356,11 +353,12 @@ struct Some {
     __device__ __forceinline__ bool find(const AdaptArgs& a, int at, int first) {
         const int lane = threadIdx.x & 63;
         if (a.groups) {
-            if (at >= *a.n_groups) return false;
-            const int4 group = a.groups[at];
-            count = min(group.z - first, SIZE);
+            const int2 group = a.groups[at];
+            row = a.order[at * kGroup + first + min(lane, SIZE - 1)];
+            count = min(group.y - first, SIZE);
             if (count <= 0) return false;
-            row = a.order[group.y + first + min(lane, count - 1)];
+            const int end = __builtin_amdgcn_readlane(row, count - 1);
+            row = lane < count ? row : end;
             id = lane < count ? group.x : -1;
         } else {
             count = min(a.o.n - at * kGroup - first, SIZE);
@@ -393,10 +391,9 @@ void adapt_many_down_kernel(AdaptArgs a) {
     constexpr int STEP = 4 * L::PER, RT = 4, HT = kGroup / 16, AHEAD = 4;
     const Adapt& o = a.o;
     __shared__ f32x4_t sums[kDownWaves][RT][64];
-    const int groups = a.groups ? *a.n_groups : (o.n + kGroup - 1) / kGroup, to_die = (groups + 7) / 8;
-    if ((int)blockIdx.x >> 3 >= to_die) return;
     Some<kGroup> rows;
-    if (!rows.find(a, (blockIdx.x & 7) * to_die + (blockIdx.x >> 3), 0)) return;
+    // (rows as they come: neighbours to one die, as the order has it)
+    if (!rows.find(a, a.groups ? blockIdx.x : (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3), 0)) return;
     const int split = blockIdx.y, first_rank = blockIdx.z * 16 * RT;
     const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int rank_tiles = min((a.all - first_rank + 15) / 16, RT);
@@ -430,7 +427,7 @@ void adapt_many_down_kernel(AdaptArgs a) {
             for (int t = 0; t < RT; ++t) sum[i][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         for (int s0 = first; s0 < end; s0 += kDownWaves * AHEAD) {
             if (!there) read_h(s0);
-            there = false;
+            there = end - first <= kDownWaves * AHEAD;       // nothing came behind them: another adapter finds them there
 #pragma unroll
             for (int t = 0; t < RT; ++t) {
                 if (t >= rank_tiles) break;
@@ -471,7 +468,7 @@ void adapt_many_down_kernel(AdaptArgs a) {
 // row's columns come one after the other, for memory's sake too (42 where those of a column do).  HALF: steps of a rank's upper parts at most.
 constexpr int kUpRows = 32, kUpCols = 256;
 template <class T, int HALF>
-__global__ __launch_bounds__(64 * kWaves, HALF <= 2 ? 4 : 2)
+__global__ __launch_bounds__(64 * kWaves, HALF == 1 && sizeof(T) == 2 ? 4 : HALF <= 2 ? 3 : 2)
 void adapt_many_up_kernel(AdaptArgs a) {
     typedef Lane<T> L;
     typedef typename L::piece_t piece_t;
@@ -598,16 +595,23 @@ void adapt_many_up_kernel(AdaptArgs a) {
 
 int steps_of(int is_bf16, int d) { return (d + (is_bf16 ? 31 : 15)) / (is_bf16 ? 32 : 16); }
 
-constexpr int kFewRows = 256;
-constexpr int kFewAdapters = 8;
+// Rows by themselves read their adapters at 7.5 TB/s, from L2 for the most part; groups take three launches and their trips, 10 us more, and read an adapter once for 64
+// rows.  4096 -> 12288 columns, rank 16, one adapter, us by rows and by groups: 64 rows 10.9 and 16.2, 96 (75 MB) 16.5 and 16.4, 128 18.2 and 16.4, 256 28.2 and 17.4; 4096 ->
+// 4096, rank 128, 64 rows (134 MB) 22.4 and 20.9; 1024 -> 1024, rank 8, 1024 rows (34 MB) 10.9 and 19.3.
+constexpr double kRowsRead = 80e6, kOrderedRead = 110e6;
+// Putting rows in order is a launch of 4 to 6 us, and what follows finds its rows a trip later.  Without it a group's adapters follow each other.  Of that kind, us in order and as
+// they come: 1024 rows of eight adapters in any order 34.5 and 50, of four 36.9 as they come, 4096 rows of eight in any order 67 and 92, in runs 67 and 57.5; so many rows are
+// prompts, whose rows lie side by side, more often than not.
+int few_adapters(int n) { return n >= 2048 ? 8 : 4; }
 struct Plan { bool many, ordered; int splits, steps, wide; int64_t most_groups, t_bytes, bytes; };
 Plan plan_of(int is_bf16, int n, int d, int p, int rank, int n_parts, int n_adapters) {
     Plan r;
-    r.many = n > kFewRows && n_adapters < kMostBins;
-    r.ordered = r.many && n_adapters > kFewAdapters;
+    const double read = (double)n * rank * ((double)n_parts * d + p) * (is_bf16 ? 2 : 4);
+    r.many = n_adapters < kMostBins && read > (n_adapters > few_adapters(n) ? kOrderedRead : kRowsRead);
+    r.ordered = r.many && n_adapters > few_adapters(n);
     const int all = steps_of(is_bf16, d), rank_groups = (rank * n_parts + 63) / 64;
     const int64_t alone = n_adapters < n ? n_adapters + 1 : n;          // groups that are not full
-    r.most_groups = r.ordered ? n / kGroup + alone : r.many ? (n + kGroup - 1) / kGroup : 0;
+    r.most_groups = round_up(r.ordered ? n / kGroup + alone : r.many ? (n + kGroup - 1) / kGroup : 0, 8);
     // workgroups that fill the chip with the first product, of 8 waves or (few rows, which have an adapter each as a rule) 4; four steps to a wave at least
     const int64_t items = (r.many ? (n + kGroup - 1) / kGroup : n) * (int64_t)rank_groups, target = r.many ? 256 : 512;
     int64_t cuts = items >= target ? 1 : target / items;
@@ -620,7 +624,7 @@ Plan plan_of(int is_bf16, int n, int d, int p, int rank, int n_parts, int n_adap
     r.wide = kFewCols;
     if (r.many) for (r.wide = 2 * kUpCols; r.wide > kUpCols && (n + kUpRows - 1) / kUpRows * (int64_t)((p + r.wide - 1) / r.wide) < 1024;) r.wide /= 2;
     r.t_bytes = round_up((int64_t)r.splits * n * rank * n_parts * sizeof(float), 256);
-    r.bytes = r.t_bytes + (r.ordered ? round_up(4 * (int64_t)n, 256) + 16 * r.most_groups + 256 : 0);
+    r.bytes = r.t_bytes + (r.ordered ? (8 + 4 * kGroup) * r.most_groups : 0);
     return r;
 }
 
@@ -637,12 +641,12 @@ hipError_t launch(const Adapt& o, hipStream_t stream) {
     const int blocks = a.first_block[o.n_parts], rank_groups = (a.all + 63) / 64;
     uint8_t* ws = (uint8_t*)o.workspace;
     a.t = (float*)ws;
-    a.n_groups = (int*)(ws + p.t_bytes);
-    a.groups = p.ordered ? (int4*)(ws + p.t_bytes + 256) : nullptr;
-    a.order = (int*)(ws + p.t_bytes + 256 + 16 * p.most_groups);
+    a.n_groups = (int)p.most_groups;
+    a.groups = p.ordered ? (int2*)(ws + p.t_bytes) : nullptr;
+    a.order = (int*)(ws + p.t_bytes + 8 * p.most_groups);
     if (p.many) {
         if (p.ordered) hipLaunchKernelGGL(adapt_order_kernel, dim3(1), dim3(kOrderThreads), 0, stream, a);
-        hipLaunchKernelGGL(adapt_many_down_kernel<T>, dim3((unsigned)round_up(p.most_groups, 8), a.splits, rank_groups), dim3(64 * kDownWaves), 0, stream, a);
+        hipLaunchKernelGGL(adapt_many_down_kernel<T>, dim3((unsigned)p.most_groups, a.splits, rank_groups), dim3(64 * kDownWaves), 0, stream, a);
         const dim3 up((unsigned)(kGroup / kUpRows * p.most_groups * blocks));
         const int half = (o.rank + 4 * Lane<T>::PER - 1) / (4 * Lane<T>::PER);
         if (half <= 1) hipLaunchKernelGGL((adapt_many_up_kernel<T, 1>), up, dim3(64 * kWaves), 0, stream, a);
@@ -662,17 +666,23 @@ hipError_t launch(const Adapt& o, hipStream_t stream) {
 bool adapt_fits(const Adapt& o, int is_bf16) {
     const Plan p = plan_of(is_bf16, o.n, o.d, o.p, o.rank, o.n_parts, o.n_adapters);
     const int64_t blocks = o.p / p.wide + o.n_parts, most = kMostThreads / (64 * kWaves), rank_groups = (o.rank * o.n_parts + 63) / 64;
-    if (p.many) return kGroup / kUpRows * p.most_groups * blocks <= most && 2 * round_up(p.most_groups, 8) * p.splits * rank_groups <= most;
+    if (p.many) return kGroup / kUpRows * p.most_groups * blocks <= most && 2 * p.most_groups * p.splits * rank_groups <= most;
     const int64_t tiles = (o.n + 15) / 16;
     return o.n * blocks <= most && 16 * tiles * p.splits * rank_groups <= most;
 }
 
 size_t adapt_workspace_bytes(const Adapt& o, int is_bf16) { return (size_t)plan_of(is_bf16, o.n, o.d, o.p, o.rank, o.n_parts, o.n_adapters).bytes; }
-// What any call of up to so many rows, ranks and adapters needs: the parts of d are at most 512 over the workgroups of one part, of 1 row (many rows: 64).
+// What any call of up to so many rows, ranks and adapters needs: the parts of d are at most 512 over the workgroups of one part, of 1 row, or 256, of 64.
 size_t adapt_workspace_bound(int n, int rank, int n_parts, int n_adapters) {
-    const int64_t most = 8 * (int64_t)n < 512 * kGroup ? 8 * (int64_t)n : 512 * kGroup, rows = n <= kFewRows ? 512 : n > most ? n : most;
-    const int64_t alone = n_adapters < n ? n_adapters + 1 : n;
-    return (size_t)(round_up(rows * rank * n_parts * (int64_t)sizeof(float), 256) + round_up(4 * (int64_t)n, 256) + 16 * (n / kGroup + alone) + 256);
+    const int64_t grouped = 8 * (int64_t)n < 256 * kGroup ? 8 * (int64_t)n : 256 * kGroup, alone = n_adapters < n ? n_adapters + 1 : n;
+    int64_t rows = grouped > 512 ? grouped : 512;
+    if (rows < n) rows = n;
+    return (size_t)(round_up(rows * rank * n_parts * (int64_t)sizeof(float), 256) + (8 + 4 * kGroup) * round_up(n / kGroup + alone, 8));
+}
+// Which way a call of these sizes goes: 0 rows by themselves, 1 groups of rows as they come, 2 groups of rows put in order.
+int adapt_way(int is_bf16, int n, int d, int p, int rank, int n_parts, int n_adapters) {
+    const Plan r = plan_of(is_bf16, n, d, p, rank, n_parts, n_adapters);
+    return r.many + r.ordered;
 }
 
 // adapt_workspace_bytes of these sizes

@@ -85,6 +85,11 @@ def check(ctx, H, base, A, B, scale, ends, which, dtype, rows=None):
     return Z
 
 
+def way(n, d, p, rank, parts, count, dtype):
+    """0: rows by themselves, 1: groups of rows as they come, 2: groups of rows put in order."""
+    return ctypes.CDLL(g.LIB_PATH)["_ZN4gelo9adapt_wayEiiiiiii"](int(dtype == BF16), n, d, p, rank, parts, count)
+
+
 CASES = [  # n, d, widths of the parts, rank, adapters
     (1, 8, (8,), 8, 1),
     (3, 72, (16, 24), 8, 2),
@@ -109,12 +114,45 @@ def test_adapters_in_any_order(ctx, n, d, parts, rank, count, gap, dtype):
     check(ctx, *make(n, d, parts, rank, count, dtype, n + d, gap), which, dtype)
 
 
+GROUPS = [  # n, d, widths of the parts, rank, adapters, way
+    (300, 1032, (1040,), 128, 1, 1),
+    (513, 1000, (560, 48, 24), 72, 2, 1),
+    (1000, 520, (272, 512), 104, 4, 1),
+    (4100, 1024, (1264,), 8, 3, 1),
+    (700, 1000, (512, 256, 248), 40, 600, 2),
+    (1025, 1544, (1024, 16), 24, 9, 2),
+    (2050, 800, (800,), 56, 30, 2),
+    (1100, 1000, (1000,), 128, 5, 2),
+    (2100, 1000, (1000,), 32, 8, 1),
+    (5000, 2048, (256, 256, 256), 16, 1200, 2),
+    (9000, 1024, (1024,), 8, 70, 2),
+]
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("n,count", [(512, 3), (1000, 8), (2050, 2), (4100, 1), (1500, 1200)])
-def test_rows_of_one_adapter_side_by_side(ctx, n, count, dtype):
-    """Prompts: runs whose ends lie inside tiles, one of them without an adapter."""
-    which = [-1 if 100 <= i < 137 else (i * count) // n for i in range(n)]
-    check(ctx, *make(n, 320, (128, 64, 64), 16, count, dtype, n, 8), which, dtype)
+@pytest.mark.parametrize("order", ["any", "runs", "one"])
+@pytest.mark.parametrize("n,d,parts,rank,count,want", GROUPS)
+def test_groups_of_rows(ctx, n, d, parts, rank, count, want, order, dtype):
+    """Rows in any order, side by side (prompts: runs whose ends lie inside tiles), and all but a few of one adapter; some without one.  A row of each tile and all that are
+    next to a change are looked at."""
+    assert way(n, d, sum(parts), rank, len(parts), count, dtype) == want
+    rng = np.random.default_rng(n)
+    which = [int(w) for w in rng.integers(-1, count + 1, n)] if order == "any" else [i * count // n for i in range(n)] if order == "runs" else [count - 1] * n
+    for i in (range(100, 137) if order != "any" else []):
+        which[i] = -1
+    if order == "one":
+        which[5] = which[n - 1] = 0
+    rows = sorted({i for i in range(0, n, 61)} | {i for i in range(1, n) if order != "any" and which[i] != which[i - 1]} | {n - 1})[:150] + [n - 1]
+    check(ctx, *make(n, d, parts, rank, count, dtype, n + d, 8), which, dtype, rows=rows)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("count,want", [(3, 1), (20, 2)])
+@pytest.mark.parametrize("n", [319, 320, 321, 335, 336, 337, 351, 352, 353, 383, 384, 385])
+def test_numbers_of_rows_at_the_edges_of_groups(ctx, n, count, want, dtype):
+    """The last group is of 63, 64, 1 ... rows."""
+    assert way(n, 1400, 800, 128, 1, count, dtype) == want
+    check(ctx, *make(n, 1400, (800,), 128, count, dtype, n, 8), [(i // 5) % (count + 1) - 1 for i in range(n)], dtype, rows=[*range(0, n, 40), *range(n - 20, n)])
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
@@ -124,20 +162,22 @@ def test_numbers_of_rows_at_the_edges_of_tiles(ctx, n, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("n", [1, 20, 600])
-def test_without_factors_and_without_any_adapter(ctx, n, dtype):
-    H, base, A, B, _, ends = make(n, 136, (48, 16), 16, 4, dtype, n)
-    check(ctx, H, base, A, B, None, ends, [i % 4 for i in range(n)], dtype)
-    Z = check(ctx, H, base, A, B, None, ends, [-(2 ** 31) if i % 2 else 2 ** 31 - 1 for i in range(n)], dtype)
+@pytest.mark.parametrize("n,d,rank,count", [(1, 136, 16, 4), (20, 136, 16, 4), (600, 1400, 104, 4), (600, 1400, 104, 9)])
+def test_without_factors_and_without_any_adapter(ctx, n, d, rank, count, dtype):
+    H, base, A, B, _, ends = make(n, d, (48, 16), rank, count, dtype, n)
+    rows = range(0, n, max(1, n // 50))
+    check(ctx, H, base, A, B, None, ends, [i % count for i in range(n)], dtype, rows)
+    Z = check(ctx, H, base, A, B, None, ends, [-(2 ** 31) if i % 2 else 2 ** 31 - 1 for i in range(n)], dtype, rows)
     assert torch.equal(Z, base)
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("n", [40, 700])
+@pytest.mark.parametrize("n,d,rank,count,want", [(40, 136, 16, 4, 0), (700, 1400, 48, 4, 1), (700, 1400, 64, 9, 2)])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
-def test_what_is_not_finite_reaches_only_its_rows(ctx, bad, n, dtype):
+def test_what_is_not_finite_reaches_only_its_rows(ctx, bad, n, d, rank, count, want, dtype):
     """In one row of H, in A and in B of one adapter, in base: everything else keeps its bits.  An infinity in B's column: that column."""
-    H, base, A, B, scale, ends = make(n, 136, (48, 32), 16, 4, dtype, 3)
+    H, base, A, B, scale, ends = make(n, d, (48, 32), rank, count, dtype, 3)
+    assert way(n, d, 80, rank, 2, count, dtype) == want
     which = [i % 5 - 1 for i in range(n)]
     ids = torch.tensor(which, dtype=torch.int32).cuda()
 
@@ -154,14 +194,14 @@ def test_what_is_not_finite_reaches_only_its_rows(ctx, bad, n, dtype):
     rest[7] = False
     assert which[7] >= 0 and which[10] == -1
     assert torch.equal(Z[rest], clean[rest]) and not torch.isfinite(Z[7].float()).any()
-    for name, m, where in (("A", A, (2, 17, 5)), ("B", B, (2, 50, 3))):
+    for name, m, where in (("A", A, (2, rank + 1, 5)), ("B", B, (2, 50, 3))):
         x = m.clone()
         x[where] = bad
         Z = run(**{name: x})
         mine = ids == 2
         assert torch.equal(Z[~mine], clean[~mine])
         cols = torch.zeros(80, dtype=torch.bool)
-        cols[48 if name == "A" else 50:80 if name == "A" else 51] = True         # row 17 of A is the second part's
+        cols[48 if name == "A" else 50:80 if name == "A" else 51] = True         # that row of A is the second part's
         assert not torch.isfinite(Z[mine][:, cols].float()).any() and torch.equal(Z[mine][:, ~cols], clean[mine][:, ~cols])
     b = base.clone()
     b[9, 11] = bad
@@ -172,12 +212,13 @@ def test_what_is_not_finite_reaches_only_its_rows(ctx, bad, n, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("n", [33, 600])
-def test_a_row_s_bits_do_not_go_by_the_rows_around_it(ctx, n, dtype):
+@pytest.mark.parametrize("n,d,rank,count,want", [(33, 264, 16, 6, 0), (600, 1400, 56, 4, 1), (600, 1400, 80, 6, 2)])
+def test_a_row_s_bits_do_not_go_by_the_rows_around_it(ctx, n, d, rank, count, want, dtype):
     """The same rows in another order, and with other adapters beside them."""
-    H, base, A, B, scale, ends = make(n, 264, (48, 32), 16, 6, dtype, 5)
+    H, base, A, B, scale, ends = make(n, d, (48, 32), rank, count, dtype, 5)
+    assert way(n, d, 80, rank, 2, count, dtype) == want
     adapters = g.Adapters(A, B, scale=scale, part_ends=ends)
-    which = torch.randint(0, 6, (n,), generator=torch.Generator().manual_seed(1)).int().cuda()
+    which = torch.randint(0, count, (n,), generator=torch.Generator().manual_seed(1)).int().cuda()
     Z, Y = torch.empty_like(base), torch.empty_like(base)
     g.gelo_adapt(ctx, H, adapters, which, Z, base=base)
     order = torch.randperm(n, generator=torch.Generator().manual_seed(2)).cuda()
@@ -193,11 +234,12 @@ def test_one_a_for_all_adapters(ctx):
     check(ctx, H, base, A[:1].expand(4, -1, -1), B, scale, ends, [i % 4 for i in range(50)], BF16)
 
 
-def test_adapters_beyond_32_bit_offsets(ctx):
+@pytest.mark.parametrize("n,ways", [(16, (0, 0)), (70, (2, 1))])
+def test_adapters_beyond_32_bit_offsets(ctx, n, ways):
     """Adapters 2^31 values and more behind the first one's."""
     count, rank, d, p = 1100, 128, 8192, 8192
+    assert (way(n, d, p, rank, 1, count, BF16), way(n, d, p, rank, 1, 1, BF16)) == ways
     A, B = (torch.zeros((count, *s), dtype=BF16, device="cuda") for s in ((rank, d), (p, rank)))
-    n = 20
     last = count - 1
     A[last], B[last] = rand((rank, d), 1, BF16, d ** -0.5), rand((p, rank), 2, BF16, 0.3)
     H, base = rand((n, d), 3, BF16), rand((n, p), 4, BF16)
@@ -220,7 +262,7 @@ def test_workspace_that_is_outgrown_serves_captured_calls(ctx):
         torch.cuda.synchronize()
         with torch.cuda.graph(graph):
             g.gelo_adapt(c, H, adapters, which, Z, base=base)
-        big = make(3000, 264, (48, 32), 16, 4, BF16, 6)
+        big = make(3000, 1400, (48, 32), 16, 4, BF16, 6)
         for turn in range(3):
             H.copy_(rand(H.shape, 30 + turn, BF16))
             graph.replay()
