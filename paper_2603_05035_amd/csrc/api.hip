@@ -1536,9 +1536,10 @@ static gelo_status check_cache_fp4(gelo_ctx* ctx, const gelo_kv_cache_fp4* c, Kv
     if (c->page_stride % 16 != 0 || c->head_stride % 16 != 0) return fail(ctx, GELO_EALIGN, "cache: strides must be multiples of 16 bytes");
     if ((c->n_kv_heads > 1 && c->head_stride < (int64_t)piece) || (c->n_pages > 1 && c->page_stride < (int64_t)piece))
         return fail(ctx, GELO_EINVAL, "a stride of the cache is below the %zu bytes of a head's piece of a page", piece);
+    if (c->n_pages > 1 && c->page_stride > INT32_MAX) return fail(ctx, GELO_ESHAPE, "cache: pages %lld bytes apart are too far from each other", (long long)c->page_stride);
     int shift = 0;
     while ((1 << shift) < c->page_rows) ++shift;
-    *out = KvCache{c->k, c->v, c->n_pages, c->n_kv_heads, shift, c->head_dim, c->page_stride, c->head_stride, 0};
+    *out = KvCache{c->k, c->v, c->n_pages, c->n_kv_heads, shift, c->head_dim, c->n_pages > 1 ? c->page_stride : 0, c->head_stride, 0};
     return GELO_OK;
 }
 

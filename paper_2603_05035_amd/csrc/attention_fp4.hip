@@ -29,8 +29,12 @@ struct Few {
     typedef bf16x8_t frag_t;
     frag_t q[APART ? 1 : QP][APART ? 1 : KS];
     const frag_t* q_apart;
-    uint32_t k[TILES][W], v[TILES][W];
-    uint32_t k_scale[TILES], v_scale[TILES][D == 96 ? 2 : 1];    // 1 or 2 bytes; 4 rows' bytes of a block, of heads of 96 two blocks'
+    // EARLY: the next step's values are sent for with its keys, before this step's arithmetic (64 x 3500-4095 keys of 32 heads of 128 188 us and 179, of heads of 256, whose
+    // registers are scarce, 32 x 2000 keys 31.6 and 37.4)
+    static constexpr bool EARLY = !FLOAT && D == 128;
+    static constexpr int VB = D == 96 ? 2 : 1;                   // blocks a lane's components lie in
+    uint32_t k[TILES][W], v[TILES][W], v_next[EARLY ? TILES : 1][W];
+    uint32_t k_scale[TILES], v_scale[TILES][VB], v_scale_next[EARLY ? TILES : 1][VB];          // 1 or 2 bytes; 4 rows' bytes of a block
 
     // to: LDS for the parts of a float query where they lie there (the waves of a workgroup write the same)
     __device__ __forceinline__ void load_q(const T* p, int g, frag_t* to) {
@@ -64,20 +68,31 @@ struct Few {
             }
         }
     }
-    // piece: a head's piece of a page; tile: 16 rows of it; scales: where its scale bytes begin
-    __device__ __forceinline__ void load_k(int t, const uint8_t* piece, int tile, int scales, int g, int c) {
-        read_words<W, PAST>(piece + tile * (8 * D) + (4 * c + g) * (D / 8), k[t]);
-        const uint8_t* s = piece + scales + tile * (D / 2) + c * (D / 32);
-        if constexpr (D == 64) k_scale[t] = s[g >> 1];
-        else if constexpr (D == 96) k_scale[t] = s[24 * g / 32] | (uint32_t)s[(24 * g + 23) / 32] << 8;
-        else if constexpr (D == 128) k_scale[t] = s[g];
-        else k_scale[t] = *reinterpret_cast<const u16_t*>(s + 2 * g);
+    // piece: a head's piece of a page; row: the tile's first in it; scales: where its scale bytes begin
+    __device__ __forceinline__ void load_k(int t, const uint8_t* piece, int row, int scales, int g, int c) {
+        read_words<W, PAST>(piece + (uint32_t)(row * (D / 2) + (4 * c + g) * (D / 8)), k[t]);
+        const uint8_t* s = piece + (uint32_t)(scales + row * (D / 32) + c * (D / 32) + (D == 64 ? g >> 1 : D == 128 ? g : D == 256 ? 2 * g : 24 * g / 32));
+        if constexpr (D == 64 || D == 128) k_scale[t] = *s;
+        else if constexpr (D == 96) k_scale[t] = s[0] | (uint32_t)s[(24 * g + 23) / 32 - 24 * g / 32] << 8;
+        else k_scale[t] = *reinterpret_cast<const u16_t*>(s);
     }
-    __device__ __forceinline__ void load_v(int t, const uint8_t* piece, int tile, int scales, int g, int c) {
-        read_words<W, PAST>(piece + tile * (8 * D) + (16 * g + c) * (D / 8), v[t]);
-        const uint8_t* s = piece + scales + tile * (D / 2) + g * (D / 8);
-        v_scale[t][0] = *reinterpret_cast<const uint32_t*>(s + 4 * (VD * c / 32));
-        if constexpr (D == 96) v_scale[t][1] = *reinterpret_cast<const uint32_t*>(s + 4 * ((VD * c + 5) / 32));
+    __device__ __forceinline__ void load_v(int t, const uint8_t* piece, int row, int scales, int g, int c) {
+        auto& codes = [&]() -> uint32_t (&)[W] { if constexpr (EARLY) return v_next[t]; else return v[t]; }();
+        auto& bytes = [&]() -> uint32_t (&)[VB] { if constexpr (EARLY) return v_scale_next[t]; else return v_scale[t]; }();
+        read_words<W, PAST>(piece + (uint32_t)(row * (D / 2) + (16 * g + c) * (D / 8)), codes);
+        const uint8_t* s = piece + (uint32_t)(scales + row * (D / 32) + g * (D / 8) + 4 * (VD * c / 32));
+        bytes[0] = *reinterpret_cast<const uint32_t*>(s);
+        if constexpr (D == 96) bytes[1] = *reinterpret_cast<const uint32_t*>(s + 4 * ((VD * c + 5) / 32 - VD * c / 32));
+    }
+    __device__ __forceinline__ void turn_values() {              // those sent for early become this step's
+        if constexpr (EARLY) {
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+#pragma unroll
+                for (int w = 0; w < W; ++w) v[t][w] = v_next[t][w];
+                v_scale[t][0] = v_scale_next[t][0];
+            }
+        }
     }
     __device__ __forceinline__ f32x4_t scores(int t, int g) const {
         f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
@@ -112,9 +127,9 @@ struct Few {
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[WP - 1][i] = (__bf16)rest[i];
         }
-        float scale[D == 96 ? 2 : 1][8];
+        float scale[VB][8];
 #pragma unroll
-        for (int b = 0; b < (D == 96 ? 2 : 1); ++b)
+        for (int b = 0; b < VB; ++b)
 #pragma unroll
             for (int i = 0; i < 8; ++i) scale[b][i] = fp4_scale((v_scale[2 * half + (i >> 2)][b] >> (8 * (i & 3))) & 0xFFu);
         const int turn = (32 * (VD * c / 32 + 1) - VD * c) / 2;           // heads of 96: the pair that begins the second block
@@ -153,7 +168,7 @@ struct Few {
         for (int i = 0; i < 8; ++i) sees[i] = (__bf16)((seen >> i) & 1 ? 1.f : 0.f);
         const int turn = (32 * (VD * c / 32 + 1) - VD * c) / 2;
 #pragma unroll
-        for (int b = 0; b < (D == 96 ? 2 : 1); ++b)
+        for (int b = 0; b < VB; ++b)
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 if ((odd[b] >> i) & 1) v_scale[2 * half + (i >> 2)][b] &= ~(0xFFu << (8 * (i & 3)));
@@ -187,34 +202,48 @@ __device__ __forceinline__ void walk_keys(const AttnArgs& a, int seq, int kvh, i
     const int32_t* table = a.b.page_table + seq * a.b.table_ld;
     const uint8_t* k_head = (const uint8_t*)a.kv.k + kvh * a.kv.head_stride;
     const uint8_t* v_head = (const uint8_t*)a.kv.v + kvh * a.kv.head_stride;
-    // tiles beyond the end are read as the last one, whose rows are there, and get no weight
+    // Tiles beyond the end are read as the last one, whose rows are there, and get no weight.  Where a tile lies is worked out once for keys and values: 64-bit
+    // products of its own for each were as long as the arithmetic beside them (64 x 3500-4095 keys of 32 heads 202 us).
+    const uint32_t page_stride = (uint32_t)a.kv.page_stride;             // (below 2^31)
+    uint64_t place[F::TILES];
+    int in_piece[F::TILES];
     auto tile_start = [&](int key) { return min(key, last & ~15); };
     auto page_of = [&](int key) { return table[tile_start(key) >> shift]; };
-    auto page_base = [&](int page) {
-        const bool good = page >= 0 && page < a.kv.n_pages;
-        bad_page |= !good;
-        return (good ? page : 0) * a.kv.page_stride;
-    };
-    auto load_k = [&](int key, const int (&page)[F::TILES]) {
+    auto find = [&](int key, const int (&page)[F::TILES]) {
 #pragma unroll
-        for (int t = 0; t < F::TILES; ++t) f.load_k(t, k_head + page_base(page[t]), (tile_start(key + 16 * t) & in_page) >> 4, scales, g, c);
+        for (int t = 0; t < F::TILES; ++t) {
+            const bool good = (uint32_t)page[t] < (uint32_t)a.kv.n_pages;
+            bad_page |= !good;
+            place[t] = (uint64_t)(good ? (uint32_t)page[t] : 0u) * page_stride;
+            in_piece[t] = tile_start(key + 16 * t) & in_page;
+        }
     };
-    auto load_v = [&](int key, const int (&page)[F::TILES]) {
+    auto load_k = [&] {
 #pragma unroll
-        for (int t = 0; t < F::TILES; ++t) f.load_v(t, v_head + page_base(page[t]), (tile_start(key + 16 * t) & in_page) >> 4, scales, g, c);
+        for (int t = 0; t < F::TILES; ++t) f.load_k(t, k_head + place[t], in_piece[t], scales, g, c);
+    };
+    auto load_v = [&] {
+#pragma unroll
+        for (int t = 0; t < F::TILES; ++t) f.load_v(t, v_head + place[t], in_piece[t], scales, g, c);
     };
     if (key > last) return;
     float base = 0.f;                                        // m, or 0 where nothing has been seen yet: all weights are 0
     int page[F::TILES];
 #pragma unroll
     for (int t = 0; t < F::TILES; ++t) page[t] = page_of(key + 16 * t);
-    load_k(key, page);
-    load_v(key, page);
+    find(key, page);
+    load_k();
+    load_v();
+    f.turn_values();
     for (; key <= last; key += stride) {
         const int next = key + stride;
         if (next <= last) {
 #pragma unroll
             for (int t = 0; t < F::TILES; ++t) page[t] = page_of(next + 16 * t);
+        }
+        if (next <= last) {
+            find(next, page);
+            if constexpr (F::EARLY) load_v();
         }
         float s[SLOTS];
 #pragma unroll
@@ -223,7 +252,7 @@ __device__ __forceinline__ void walk_keys(const AttnArgs& a, int seq, int kvh, i
 #pragma unroll
             for (int r = 0; r < 4; ++r) s[4 * t + r] = x[r] * a.scale2s;
         }
-        if (next <= last) load_k(next, page);
+        if (next <= last) load_k();
         // hidden: keys beyond what the column sees (uniform test first: most steps have none)
         const bool partly = key + F::KEYS - 1 > min(least, last);
         uint32_t seen = ~0u;
@@ -264,7 +293,8 @@ __device__ __forceinline__ void walk_keys(const AttnArgs& a, int seq, int kvh, i
             if (partly && __ballot((f.odd_slots(h, 0) | f.odd_slots(h, D == 96 ? 1 : 0)) != 0)) f.accumulate_odd(h, s + 8 * h, acc, c, seen >> (8 * h));
             else f.accumulate(h, s + 8 * h, acc, c);
         }
-        if (next <= last) load_v(next, page);
+        if constexpr (F::EARLY) f.turn_values();
+        else if (next <= last) load_v();
     }
 }
 
@@ -273,9 +303,10 @@ template <class T, int D> constexpr int few_lds() {
     return joined > parts ? joined : parts;
 }
 
-// A workgroup: one tile of 16 columns of one sequence and key head, one chunk of the cache, whose keys its waves share out.
+// A workgroup: one tile of 16 columns of one sequence and key head, one chunk of the cache, whose keys its waves share out; or (by_head) one
+// sequence and four key heads, one to a wave.
 template <class T, int D, bool PAST>
-__global__ __launch_bounds__(64 * kFewWaves, 2)
+__global__ __launch_bounds__(64 * kFewWaves, sizeof(T) == 4 && D == 128 ? 3 : 2)
 void attention_few_fp4_kernel(AttnArgs a) {
     typedef Few<T, D, PAST> F;
     constexpr int VD = F::VD;
@@ -284,7 +315,8 @@ void attention_few_fp4_kernel(AttnArgs a) {
     auto joined_o = reinterpret_cast<float (*)[16][D + 4]>(lds);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int tile = a.n_chunks == 1 ? blockIdx.x : blockIdx.x / a.n_chunks, chunk = blockIdx.x - tile * a.n_chunks;
-    const int kvh = blockIdx.y, seq = blockIdx.z;
+    const int heads = a.by_head ? kFewWaves : 1;             // key heads of a workgroup
+    const int first_kvh = blockIdx.y * heads, kvh = first_kvh + (a.by_head ? wave : 0), seq = blockIdx.z;
     const NewRows rows = rows_of_sequence(a.b, seq);
     const int columns = rows.count * a.group;
     if (tile * 16 >= columns) return;
@@ -312,7 +344,7 @@ void attention_few_fp4_kernel(AttnArgs a) {
     float m = -__builtin_inff(), l = 0.f;
     bool bad_page = false;
 
-    walk_keys<T, D, PAST>(a, seq, kvh, begin + wave * F::KEYS, F::KEYS * kFewWaves, end - 1, least, limit, g, c, f, acc, m, l, bad_page);
+    walk_keys<T, D, PAST>(a, seq, kvh, a.by_head ? begin : begin + wave * F::KEYS, a.by_head ? F::KEYS : F::KEYS * kFewWaves, end - 1, least, limit, g, c, f, acc, m, l, bad_page);
     l = across_groups_sum(l);
     if (bad_page) l = __builtin_nanf("");
     if constexpr (F::APART) __syncthreads();                 // nobody reads the query's parts any more
@@ -324,15 +356,16 @@ void attention_few_fp4_kernel(AttnArgs a) {
         for (int j = 0; j < VD; ++j) joined_o[wave][c][VD * (4 * g + r) + j] = acc[j][r];
     if (g == 0) { joined_ml[wave][c][0] = m; joined_ml[wave][c][1] = l; }
     __syncthreads();
-    for (int e = threadIdx.x; e < 16 * (D / 4); e += 64 * kFewWaves) {
-        const int cc = e / (D / 4), x = 4 * (e - cc * (D / 4)), cl = tile * 16 + cc;
+    for (int e = threadIdx.x; e < heads * 16 * (D / 4); e += 64 * kFewWaves) {
+        const int k16 = e / (D / 4), cc = k16 & 15, hd = k16 >> 4, x = 4 * (e - k16 * (D / 4)), cl = tile * 16 + cc;
+        const int from = a.by_head ? hd : 0, to = a.by_head ? hd + 1 : kFewWaves;             // the waves that have parts of this column
         if (cl >= columns) continue;
-        float top = joined_ml[0][cc][0];
-        for (int w = 1; w < kFewWaves; ++w) top = fmaxf(top, joined_ml[w][cc][0]);
+        float top = joined_ml[from][cc][0];
+        for (int w = from + 1; w < to; ++w) top = fmaxf(top, joined_ml[w][cc][0]);
         const float safe = top == -__builtin_inff() ? 0.f : top;
         float total = 0.f;
         f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-        for (int w = 0; w < kFewWaves; ++w) {
+        for (int w = from; w < to; ++w) {
             if (joined_ml[w][cc][1] == 0.f) continue;        // nothing seen: 0 times what it holds need not be 0
             const float k = __builtin_amdgcn_exp2f(joined_ml[w][cc][0] - safe);
             total += k * joined_ml[w][cc][1];
@@ -340,7 +373,7 @@ void attention_few_fp4_kernel(AttnArgs a) {
 #pragma unroll
             for (int u = 0; u < 4; ++u) o[u] += k * y[u];
         }
-        const int ri = cl / a.group, h = kvh * a.group + cl - ri * a.group;
+        const int ri = cl / a.group, h = (first_kvh + hd) * a.group + cl - ri * a.group;
         const int64_t rr = rows.first + ri;
         if (a.n_chunks == 1) {
             const float inv = inverse_of(total, limit_of(ri) >= 0);
@@ -357,7 +390,7 @@ void attention_few_fp4_kernel(AttnArgs a) {
 
 static_assert(64 * kFewWaves <= 256 && 64 * kPromptWaves <= 256, "workgroups as kMostWorkgroups has them");
 
-Plan plan_few(const Attention& o, int64_t columns, double* us) {
+Plan plan_few(const Attention& o, int64_t columns, int is_bf16, double* us) {
     Plan p;
     p.prompt = p.shared = p.paired = p.past = p.by_head = false;
     p.col_tiles = (columns + 15) / 16;
@@ -366,6 +399,8 @@ Plan plan_few(const Attention& o, int64_t columns, double* us) {
     const int64_t cuts = kFewTarget / tiles;
     cut(&p, o.batch.max_kv_len, cuts < 1 ? 1 : cuts < most ? cuts : most);
     p.workgroups = tiles * p.n_chunks;
+    p.by_head = (is_bf16 || o.cache.head_dim < 128) && p.n_chunks == 1 && p.col_tiles == 1 && o.cache.n_kv_heads % kFewWaves == 0 && tiles / kFewWaves >= kFewTarget;
+    if (p.by_head) p.workgroups = tiles / kFewWaves;
     p.past = p.col_tiles == 1 && 17.0 / 16 * tiles * o.batch.max_kv_len * o.cache.head_dim > 100e6;
     // a wave's step of 64 keys takes its SIMD 1.3 us at a width of 128, and a trip to memory 1.5
     const double rounds = (double)((p.workgroups + kFewTarget - 1) / kFewTarget), steps = (p.chunk + 255) / 256;
@@ -377,7 +412,7 @@ Plan plan_few(const Attention& o, int64_t columns, double* us) {
 Plan plan_of(const Attention& o, int is_bf16) {
     const int64_t columns = (int64_t)o.batch.max_rows * (o.n_q_heads / o.cache.n_kv_heads);
     double few_us, prompt_us;
-    const Plan few = plan_few(o, columns, &few_us);
+    const Plan few = plan_few(o, columns, is_bf16, &few_us);
     if (!is_bf16 || columns <= 16) return few;
     const Plan prompt = plan_prompt(o, columns, &prompt_us);
     return few_us < prompt_us ? few : prompt;
@@ -397,7 +432,7 @@ hipError_t launch(const Attention& o, hipStream_t stream) {
     a.scale2 = o.scale == 0.f ? 1e-30f : fabsf(a.scale2s);      // (-inf, a hidden score, times 0 would be NaN)
     a.flip = o.scale < 0.f ? 0x80008000u : 0u;
     a.causal = o.causal;
-    a.chunk = p.chunk; a.n_chunks = p.n_chunks; a.col_tiles = (int)p.col_tiles; a.paired = p.paired; a.by_head = 0;
+    a.chunk = p.chunk; a.n_chunks = p.n_chunks; a.col_tiles = (int)p.col_tiles; a.paired = p.paired; a.by_head = p.by_head;
     a.kv = o.cache; a.b = o.batch;
     a.part_o = o.workspace;
     a.part_ml = p.n_chunks == 1 ? nullptr : o.workspace + parts(o, p) * D;
@@ -405,7 +440,7 @@ hipError_t launch(const Attention& o, hipStream_t stream) {
         if (p.prompt)
             hipLaunchKernelGGL((attention_prompt_kernel<D, true>), dim3((unsigned)p.workgroups), dim3(64 * kPromptWaves), (size_t)prompt_lds<D>(), stream, a);
     }
-    const dim3 few((unsigned)(p.col_tiles * p.n_chunks), (unsigned)o.cache.n_kv_heads, (unsigned)o.batch.n_seqs);
+    const dim3 few((unsigned)(p.col_tiles * p.n_chunks), (unsigned)(o.cache.n_kv_heads / (p.by_head ? kFewWaves : 1)), (unsigned)o.batch.n_seqs);
     if (p.prompt) {}
     else if (p.past) hipLaunchKernelGGL((attention_few_fp4_kernel<T, D, true>), few, dim3(64 * kFewWaves), 0, stream, a);
     else hipLaunchKernelGGL((attention_few_fp4_kernel<T, D, false>), few, dim3(64 * kFewWaves), 0, stream, a);

@@ -688,7 +688,7 @@ def test_refusals(ctx):
         for bad in ({"k": None}, {"v": None}, {"n_pages": 0}, {"n_kv_heads": 0}, {"page_rows": 0}, {"head_dim": 0}, {"head_stride": piece - 16}, {"page_stride": 16},
                     {"n_seqs": 0}, {"n_rows": 0}, {"max_rows": 0}, {"max_kv_len": 0}, {"kv_len": None}, {"page_table": None}, {"n_rows": 3}, {"max_rows": 2}, {"dtype": 3}):
             assert call(**bad) == "GELO_EINVAL", bad
-        for bad in ({"page_rows": 8}, {"page_rows": 48}, {"head_dim": 48}, {"page_rows": 1 << 24}, {"table_ld": 1}, {"max_kv_len": 33}, {"row_start": i, "n_rows": (1 << 22) + 1}):
+        for bad in ({"page_rows": 8}, {"page_rows": 48}, {"head_dim": 48}, {"page_rows": 1 << 24}, {"page_stride": 1 << 31}, {"table_ld": 1}, {"max_kv_len": 33}, {"row_start": i, "n_rows": (1 << 22) + 1}):
             assert call(**bad) == "GELO_ESHAPE", bad
         for bad in ({"k": x + 8}, {"head_stride": piece + 8}, {"page_stride": 2 * piece + 4}, {"kv_len": i + 2}, {"page_table": i + 1}):
             assert call(**bad) == "GELO_EALIGN", bad
