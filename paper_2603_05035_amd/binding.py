@@ -531,7 +531,36 @@ def gelo_rope_table(ctx, rot_dim: int, n_pos: int, base: float = 10000.0, factor
     return table
 
 
-def _append(call, ctx, QKV, n_q_heads, cache, code, batch, Q, table, rot_dim, layout, stream):
+def gelo_rope_append(ctx, QKV: torch.Tensor, n_q_heads: int, cache: KvCache, batch: SeqBatch, Q: torch.Tensor | None = None,
+                     table: torch.Tensor | None = None, rot_dim: int = 0, layout: int = GELO_ROPE_HALF, stream=None):
+    """Rotates the queries and keys of QKV's rows by their positions; queries into Q, keys and values into the cache."""
+    zp, ld = _matrix(QKV, "QKV")
+    rows, width = QKV.shape
+    if QKV.dtype != cache.torch_dtype:
+        raise GeloError(3, "QKV and the cache differ in type")
+    if width != (n_q_heads + 2 * cache.n_kv_heads) * cache.head_dim:
+        raise GeloError(2, f"a row of {width} values is not {n_q_heads} + 2 x {cache.n_kv_heads} heads of {cache.head_dim}")
+    qp, ldq = None, 0
+    if Q is not None:
+        if Q.dtype != cache.torch_dtype or Q.shape != (rows, n_q_heads * cache.head_dim):
+            raise ValueError("Q must be of QKV's dtype, a row of all query heads for each of its rows")
+        qp, ldq = _matrix(Q, "Q")
+    tp, n_table = None, 0
+    if table is not None:
+        n_table = table.shape[0]
+        if table.dtype != torch.float32 or not table.is_cuda or not table.is_contiguous() or table.numel() != n_table * rot_dim:
+            raise ValueError("table must be a contiguous float32 GPU tensor of positions x rot_dim")
+        tp = table.data_ptr()
+    described = _described(batch, rows, cache)
+    status = load_library().gelo_rope_append(ctx, cache.dtype, n_q_heads, zp, ld, cache.address, described[2], layout, rot_dim, tp, n_table, qp, ldq,
+                                             _stream(stream))
+    if status != GELO_OK:
+        _check(ctx, status)
+
+
+def gelo_rope_append_fp4(ctx, QKV: torch.Tensor, n_q_heads: int, cache: KvCacheFp4, batch: SeqBatch, Q: torch.Tensor | None = None,
+                         table: torch.Tensor | None = None, rot_dim: int = 0, layout: int = GELO_ROPE_HALF, stream=None):
+    """gelo_rope_append into a cache of 4 bits."""
     zp, ld = _matrix(QKV, "QKV")
     rows, width = QKV.shape
     if width != (n_q_heads + 2 * cache.n_kv_heads) * cache.head_dim:
@@ -548,69 +577,66 @@ def _append(call, ctx, QKV, n_q_heads, cache, code, batch, Q, table, rot_dim, la
             raise ValueError("table must be a contiguous float32 GPU tensor of positions x rot_dim")
         tp = table.data_ptr()
     described = _described(batch, rows, cache)
-    status = call(ctx, code, n_q_heads, zp, ld, cache.address, described[2], layout, rot_dim, tp, n_table, qp, ldq, _stream(stream))
+    status = load_library().gelo_rope_append_fp4(ctx, _dtype_code(QKV), n_q_heads, zp, ld, cache.address, described[2], layout, rot_dim, tp, n_table, qp,
+                                                 ldq, _stream(stream))
     if status != GELO_OK:
         _check(ctx, status)
-
-
-def gelo_rope_append(ctx, QKV: torch.Tensor, n_q_heads: int, cache: KvCache, batch: SeqBatch, Q: torch.Tensor | None = None,
-                     table: torch.Tensor | None = None, rot_dim: int = 0, layout: int = GELO_ROPE_HALF, stream=None):
-    """Rotates the queries and keys of QKV's rows by their positions; queries into Q, keys and values into the cache."""
-    if QKV.dtype != cache.torch_dtype:
-        raise GeloError(3, "QKV and the cache differ in type")
-    _append(load_library().gelo_rope_append, ctx, QKV, n_q_heads, cache, cache.dtype, batch, Q, table, rot_dim, layout, stream)
-
-
-def gelo_rope_append_fp4(ctx, QKV: torch.Tensor, n_q_heads: int, cache: KvCacheFp4, batch: SeqBatch, Q: torch.Tensor | None = None,
-                         table: torch.Tensor | None = None, rot_dim: int = 0, layout: int = GELO_ROPE_HALF, stream=None):
-    """gelo_rope_append into a cache of 4 bits."""
-    _append(load_library().gelo_rope_append_fp4, ctx, QKV, n_q_heads, cache, _dtype_code(QKV), batch, Q, table, rot_dim, layout, stream)
 
 
 def gelo_cache_rows_fp4(ctx, cache: KvCacheFp4, batch: SeqBatch, K: torch.Tensor | None = None, V: torch.Tensor | None = None, stream=None):
     """The values that the batch's rows are held as, a row of all key heads to each, into K and V (either may be None)."""
-    some = K if K is not None else V
+    some = V if K is None else K
     if some is None:
         raise ValueError("K and V are both None: nothing to write")
-    at = []
-    for name, t in (("K", K), ("V", V)):
-        if t is None:
-            at += [None, 0]
-            continue
-        if t.dtype != some.dtype or t.dim() != 2 or t.shape != (some.shape[0], cache.n_kv_heads * cache.head_dim):
-            raise ValueError(f"{name} must have a row of {cache.n_kv_heads} heads of {cache.head_dim} for each row of the batch, of the other's type")
-        at += _matrix(t, name)
-    described = _described(batch, some.shape[0], cache)
-    _check(ctx, load_library().gelo_cache_rows_fp4(ctx, _dtype_code(some), cache.address, described[2], *at, _stream(stream)))
-
-
-def _attend(call, ctx, Q, O, n_q_heads, cache, code, batch, scale, causal, stream):
-    qp, ldq = _matrix(Q, "Q")
-    op, ldo = _matrix(O, "O")
-    shape = Q.shape
-    if shape[1] != n_q_heads * cache.head_dim or O.shape != shape:
-        raise GeloError(2, f"Q and O must have {n_q_heads} heads of {cache.head_dim} values in a row")
+    shape, dtype = some.shape, some.dtype
+    if len(shape) != 2 or shape[1] != cache.n_kv_heads * cache.head_dim:
+        raise ValueError(f"K and V must have a row of {cache.n_kv_heads} heads of {cache.head_dim} for each row of the batch")
+    kp = vp = None
+    ldk = ldv = 0
+    if K is not None:
+        kp, ldk = _matrix(K, "K")
+    if V is not None:
+        if V.dtype != dtype or V.shape != shape:
+            raise ValueError("K and V must be of one type and shape")
+        vp, ldv = _matrix(V, "V")
     described = _described(batch, shape[0], cache)
-    status = call(ctx, code, n_q_heads, qp, ldq, cache.address, described[2], scale, causal, op, ldo, _stream(stream))
+    status = load_library().gelo_cache_rows_fp4(ctx, _dtype_code(some), cache.address, described[2], kp, ldk, vp, ldv, _stream(stream))
     if status != GELO_OK:
         _check(ctx, status)
-    return O
 
 
 def gelo_attention(ctx, Q: torch.Tensor, O: torch.Tensor, n_q_heads: int, cache: KvCache, batch: SeqBatch, scale: float, causal: bool = True,
                    stream=None) -> torch.Tensor:
     """softmax(scale Q K^T) V over the rows of the cache that each row of Q sees, into O."""
+    qp, ldq = _matrix(Q, "Q")
+    op, ldo = _matrix(O, "O")
+    shape = Q.shape
     if Q.dtype != cache.torch_dtype or O.dtype != cache.torch_dtype:
         raise GeloError(3, "Q, O and the cache differ in type")
-    return _attend(load_library().gelo_attention, ctx, Q, O, n_q_heads, cache, cache.dtype, batch, scale, causal, stream)
+    if shape[1] != n_q_heads * cache.head_dim or O.shape != shape:
+        raise GeloError(2, f"Q and O must have {n_q_heads} heads of {cache.head_dim} values in a row")
+    described = _described(batch, shape[0], cache)
+    status = load_library().gelo_attention(ctx, cache.dtype, n_q_heads, qp, ldq, cache.address, described[2], scale, causal, op, ldo, _stream(stream))
+    if status != GELO_OK:
+        _check(ctx, status)
+    return O
 
 
 def gelo_attention_fp4(ctx, Q: torch.Tensor, O: torch.Tensor, n_q_heads: int, cache: KvCacheFp4, batch: SeqBatch, scale: float, causal: bool = True,
                        stream=None) -> torch.Tensor:
     """gelo_attention over a cache of 4 bits."""
+    qp, ldq = _matrix(Q, "Q")
+    op, ldo = _matrix(O, "O")
+    shape = Q.shape
     if O.dtype != Q.dtype:
         raise GeloError(3, "Q and O differ in type")
-    return _attend(load_library().gelo_attention_fp4, ctx, Q, O, n_q_heads, cache, _dtype_code(Q), batch, scale, causal, stream)
+    if shape[1] != n_q_heads * cache.head_dim or O.shape != shape:
+        raise GeloError(2, f"Q and O must have {n_q_heads} heads of {cache.head_dim} values in a row")
+    described = _described(batch, shape[0], cache)
+    status = load_library().gelo_attention_fp4(ctx, _dtype_code(Q), n_q_heads, qp, ldq, cache.address, described[2], scale, causal, op, ldo, _stream(stream))
+    if status != GELO_OK:
+        _check(ctx, status)
+    return O
 
 
 def gelo_reserve_attention(ctx, head_dim: int) -> None:

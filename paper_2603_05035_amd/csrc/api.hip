@@ -102,7 +102,7 @@ struct gelo_ctx {
     void* quant_ws;  size_t quant_ws_bytes;    // FP8 projection: codes and row scales of the current U
     void* attention_ws; size_t attention_ws_bytes; // parts of a cut cache
     void* adapt_ws; size_t adapt_ws_bytes;         // the first products of adapters
-    std::vector<void*> adapt_outgrown;             // smaller ones that captured calls may still name
+    void* adapt_outgrown[48]; int n_outgrown;      // smaller ones that captured calls may still name: each at least twice the one before
     void* project_ws; size_t project_ws_bytes; // bf16 projection of at most 128 rows: float partial sums of the K slices
     float* host_scalars;         // pinned: kappa read-back, one slot per lane
     int* host_flag;
@@ -415,7 +415,7 @@ gelo_status gelo_create(gelo_ctx** out, int device, uint64_t seed, int allow_bat
     ctx->quant_ws = nullptr; ctx->quant_ws_bytes = 0;
     ctx->project_ws = nullptr; ctx->project_ws_bytes = 0;
     ctx->attention_ws = nullptr; ctx->attention_ws_bytes = 0;
-    ctx->adapt_ws = nullptr; ctx->adapt_ws_bytes = 0;
+    ctx->adapt_ws = nullptr; ctx->adapt_ws_bytes = 0; ctx->n_outgrown = 0;
     ctx->host_scalars = nullptr; ctx->host_flag = nullptr;
     ctx->lanes_ready = false; ctx->join_pending = false; ctx->cand = nullptr; ctx->cand_bytes = 0;
     for (int i = 0; i < kLanes; ++i) ctx->lane_graph_ok[i] = false;
@@ -452,7 +452,7 @@ gelo_status gelo_destroy(gelo_ctx* ctx) {
     if (ctx->project_ws) (void)hipFree(ctx->project_ws);
     if (ctx->attention_ws) (void)hipFree(ctx->attention_ws);
     if (ctx->adapt_ws) (void)hipFree(ctx->adapt_ws);
-    for (void* p : ctx->adapt_outgrown) (void)hipFree(p);
+    for (int i = 0; i < ctx->n_outgrown; ++i) (void)hipFree(ctx->adapt_outgrown[i]);
     if (ctx->host_scalars) (void)hipHostFree(ctx->host_scalars);
     delete ctx;
     return GELO_OK;
@@ -1695,16 +1695,12 @@ gelo_status gelo_reserve_attention(gelo_ctx* ctx, int head_dim) {
 static gelo_status grow_adapt(gelo_ctx* ctx, size_t need) {
     if (ctx->adapt_ws_bytes >= need) return GELO_OK;
     if (need < 2 * ctx->adapt_ws_bytes) need = 2 * ctx->adapt_ws_bytes;
-    void* old = ctx->adapt_ws;
+    void* larger = nullptr;
     size_t have = 0;
-    if (old) ctx->adapt_outgrown.push_back(old);
-    ctx->adapt_ws = nullptr;
-    const gelo_status st = grow(ctx, &ctx->adapt_ws, &have, need);
-    if (st != GELO_OK) {
-        if (old) ctx->adapt_outgrown.pop_back();
-        ctx->adapt_ws = old;
-        return st;
-    }
+    const gelo_status st = grow(ctx, &larger, &have, need);
+    if (st != GELO_OK) return st;
+    if (ctx->adapt_ws) ctx->adapt_outgrown[ctx->n_outgrown++] = ctx->adapt_ws;         // (48 doublings of 512 bytes are more than any device has)
+    ctx->adapt_ws = larger;
     ctx->adapt_ws_bytes = have;
     return GELO_OK;
 }

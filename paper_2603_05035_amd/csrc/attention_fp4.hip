@@ -469,15 +469,27 @@ bool attention_fp4_fits(const Attention& o, int is_bf16) {
 
 size_t attention_fp4_workspace_bytes(const Attention& o, int is_bf16) { return parts(o, plan_of(o, is_bf16)) * (o.cache.head_dim + 2) * sizeof(float); }
 
-// Which way a call of these sizes goes, as attention_way says it.
-int attention_fp4_way(int is_bf16, int causal, int n_q_heads, int n_kv_heads, int head_dim, int n_seqs, int n_rows, int max_rows, int max_kv_len) {
+namespace {
+Attention described(int causal, int n_q_heads, int n_kv_heads, int head_dim, int n_seqs, int n_rows, int max_rows, int max_kv_len) {
     Attention o = {};
     o.causal = causal != 0; o.n_q_heads = n_q_heads;
     o.cache.n_kv_heads = n_kv_heads; o.cache.head_dim = head_dim;
     o.batch.n_seqs = n_seqs; o.batch.n_rows = n_rows; o.batch.max_rows = rows_bound(max_rows, n_rows); o.batch.max_kv_len = max_kv_len;
+    return o;
+}
+}  // namespace
+
+// Which way a call of these sizes goes, as attention_way says it, plus 8 where a wave has a head to itself.
+int attention_fp4_way(int is_bf16, int causal, int n_q_heads, int n_kv_heads, int head_dim, int n_seqs, int n_rows, int max_rows, int max_kv_len) {
+    const Attention o = described(causal, n_q_heads, n_kv_heads, head_dim, n_seqs, n_rows, max_rows, max_kv_len);
     if (!attention_fp4_fits(o, is_bf16)) return -1;
     const Plan p = plan_of(o, is_bf16);
-    return (p.prompt ? p.paired ? 2 : 1 : 0) + (p.n_chunks > 1 ? 4 : 0);
+    return (p.prompt ? p.paired ? 2 : 1 : 0) + (p.n_chunks > 1 ? 4 : 0) + (p.by_head ? 8 : 0);
+}
+// attention_fp4_workspace_bytes of these sizes
+size_t attention_fp4_parts(int is_bf16, int causal, int n_q_heads, int n_kv_heads, int head_dim, int n_seqs, int n_rows, int max_rows, int max_kv_len) {
+    const Attention o = described(causal, n_q_heads, n_kv_heads, head_dim, n_seqs, n_rows, max_rows, max_kv_len);
+    return attention_fp4_fits(o, is_bf16) ? attention_fp4_workspace_bytes(o, is_bf16) : 0;
 }
 
 hipError_t attention_fp4(const Attention& o, int is_bf16, hipStream_t stream) { return is_bf16 ? of_width<uint16_t>(o, stream) : of_width<float>(o, stream); }

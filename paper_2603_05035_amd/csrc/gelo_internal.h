@@ -439,6 +439,7 @@ hipError_t attention(const Attention& o, int is_bf16, hipStream_t stream);
 hipError_t attention_init();
 // attention_fp4.hip
 int attention_fp4_way(int is_bf16, int causal, int n_q_heads, int n_kv_heads, int head_dim, int n_seqs, int n_rows, int max_rows, int max_kv_len);
+size_t attention_fp4_parts(int is_bf16, int causal, int n_q_heads, int n_kv_heads, int head_dim, int n_seqs, int n_rows, int max_rows, int max_kv_len);
 bool attention_fp4_fits(const Attention& o, int is_bf16);
 size_t attention_fp4_workspace_bytes(const Attention& o, int is_bf16);
 hipError_t attention_fp4(const Attention& o, int is_bf16, hipStream_t stream);

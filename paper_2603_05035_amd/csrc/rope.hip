@@ -188,7 +188,7 @@ __device__ __forceinline__ int scale_at(int d, int page_shift, int in_page, int 
     return is_value ? first + (in_page >> 2) * 4 * per + 4 * block + (in_page & 3) : first + in_page * per + block;
 }
 
-// A workgroup takes a row of QKV.  Keys and values go by items of 8 components, four lanes to a block: each of them loads the components that its own turn
+// A workgroup takes a row of QKV, or a share of its items (grid y).  Keys and values go by items of 8 components, four lanes to a block: each of them loads the components that its own turn
 // with, too, so that any rot / 2 will do.  A turned key is worked out in double, where the two products are exact and their sum as good as, and its code is
 // that value's: in float one in some millions would fall on the other side of the middle between two codes.  Queries turn as in rope_append_kernel, to the bit.
 template <class T>
@@ -202,8 +202,30 @@ void rope_append_fp4_kernel(RopeAppend o) {
     const float* angles = o.table + (int64_t)(at.placed ? at.pos : 0) * o.rot;
     const int d = kv.head_dim, hq = o.n_q_heads, hkv = kv.n_kv_heads, per_head = d / 8;
     const T* in = (const T*)o.QKV + (int64_t)row * o.ld;
-    const int kept = at.kept ? 2 * hkv * per_head : 0;       // items of keys and values: a multiple of 4
-    for (int e = threadIdx.x; e < kept; e += 256) {
+    const int held = 2 * hkv * per_head;                     // items of keys and values: a multiple of 4
+    const int turning = o.pairs ? o.rot / 8 : o.rot / 16, per_turned = turning + (d - o.rot) / 8;
+    for (int e = blockIdx.y * 256 + threadIdx.x; e < held + hq * per_turned; e += 256 * gridDim.y) {
+        if (e >= held) {
+            const int head = (e - held) / per_turned, i = e - held - head * per_turned;
+            const bool turns = i < turning, two = turns && !o.pairs;
+            const int col = turns || o.pairs ? 8 * i : o.rot + 8 * (i - turning);
+            Eight<T> x, y;
+            x.load(in + (int64_t)head * d + col);
+            if (two) y.load(in + (int64_t)head * d + col + o.rot / 2);
+            if (turns) turn_item(x, y, two, angles + (two ? 2 * col : col));
+            if (!at.placed) {
+                float v[8];
+#pragma unroll
+                for (int t = 0; t < 8; ++t) v[t] = at.beyond ? __builtin_nanf("") : 0.f;
+                x.set(v);
+                y = x;
+            }
+            T* out = (T*)o.Q + (int64_t)row * o.ldq + (int64_t)head * d + col;
+            x.store(out);
+            if (two) y.store(out + o.rot / 2);
+            continue;
+        }
+        if (!at.kept) continue;
         const int head2 = e / per_head, i = e - head2 * per_head, col = 8 * i;
         const bool is_value = head2 >= hkv;
         const int head = is_value ? head2 - hkv : head2;
@@ -277,26 +299,6 @@ void rope_append_fp4_kernel(RopeAppend o) {
         }
         if ((i & 3) == 0) piece[scale_at(d, kv.page_shift, at.in_page, i / 4, is_value)] = (uint8_t)byte;
     }
-    const int turning = o.pairs ? o.rot / 8 : o.rot / 16, per_turned = turning + (d - o.rot) / 8;
-    for (int e = threadIdx.x; e < hq * per_turned; e += 256) {
-        const int head = e / per_turned, i = e - head * per_turned;
-        const bool turns = i < turning, two = turns && !o.pairs;
-        const int col = turns || o.pairs ? 8 * i : o.rot + 8 * (i - turning);
-        Eight<T> x, y;
-        x.load(in + (int64_t)head * d + col);
-        if (two) y.load(in + (int64_t)head * d + col + o.rot / 2);
-        if (turns) turn_item(x, y, two, angles + (two ? 2 * col : col));
-        if (!at.placed) {
-            float v[8];
-#pragma unroll
-            for (int t = 0; t < 8; ++t) v[t] = at.beyond ? __builtin_nanf("") : 0.f;
-            x.set(v);
-            y = x;
-        }
-        T* out = (T*)o.Q + (int64_t)row * o.ldq + (int64_t)head * d + col;
-        x.store(out);
-        if (two) y.store(out + o.rot / 2);
-    }
 }
 
 // Rows of a cache of 4 bits as values: 8 to an item.
@@ -308,7 +310,7 @@ void cache_rows_fp4_kernel(CacheRows o) {
     Fp4Row at;
     if (!find_row(o.batch, kv, row, &at)) return;
     const int d = kv.head_dim, hkv = kv.n_kv_heads, per_head = d / 8;
-    for (int e = threadIdx.x; e < 2 * hkv * per_head; e += 256) {
+    for (int e = blockIdx.y * 256 + threadIdx.x; e < 2 * hkv * per_head; e += 256 * gridDim.y) {
         const int head2 = e / per_head, i = e - head2 * per_head;
         const bool is_value = head2 >= hkv;
         const int head = is_value ? head2 - hkv : head2;
@@ -354,15 +356,24 @@ hipError_t rope_append(const RopeAppend& o, int is_bf16, hipStream_t stream) {
     return hipGetLastError();
 }
 
+// workgroups to a row: as many as its items fill, where the rows leave CUs idle
+static int shares(int n_rows, int items) {
+    const int most = (items + 255) / 256, idle = 1024 / n_rows;
+    return idle < 1 ? 1 : idle < most ? idle : most;
+}
+
 hipError_t rope_append_fp4(const RopeAppend& o, int is_bf16, hipStream_t stream) {
-    if (is_bf16) hipLaunchKernelGGL(rope_append_fp4_kernel<uint16_t>, dim3(o.batch.n_rows), dim3(256), 0, stream, o);
-    else hipLaunchKernelGGL(rope_append_fp4_kernel<float>, dim3(o.batch.n_rows), dim3(256), 0, stream, o);
+    const int d = o.cache.head_dim, items = 2 * o.cache.n_kv_heads * d / 8 + o.n_q_heads * ((o.pairs ? o.rot / 8 : o.rot / 16) + (d - o.rot) / 8);
+    const dim3 grid(o.batch.n_rows, shares(o.batch.n_rows, items));
+    if (is_bf16) hipLaunchKernelGGL(rope_append_fp4_kernel<uint16_t>, grid, dim3(256), 0, stream, o);
+    else hipLaunchKernelGGL(rope_append_fp4_kernel<float>, grid, dim3(256), 0, stream, o);
     return hipGetLastError();
 }
 
 hipError_t cache_rows_fp4(const CacheRows& o, int is_bf16, hipStream_t stream) {
-    if (is_bf16) hipLaunchKernelGGL(cache_rows_fp4_kernel<uint16_t>, dim3(o.batch.n_rows), dim3(256), 0, stream, o);
-    else hipLaunchKernelGGL(cache_rows_fp4_kernel<float>, dim3(o.batch.n_rows), dim3(256), 0, stream, o);
+    const dim3 grid(o.batch.n_rows, shares(o.batch.n_rows, 2 * o.cache.n_kv_heads * o.cache.head_dim / 8));
+    if (is_bf16) hipLaunchKernelGGL(cache_rows_fp4_kernel<uint16_t>, grid, dim3(256), 0, stream, o);
+    else hipLaunchKernelGGL(cache_rows_fp4_kernel<float>, grid, dim3(256), 0, stream, o);
     return hipGetLastError();
 }
 

@@ -317,10 +317,18 @@ def test_attention_of_single_tokens(ctx, dtype, kv, hq, hkv, d, page, order):
     run_attention(ctx, dtype, [1] * len(kv), kv, hq, hkv, d, page, order, True, one_row=True)
 
 
+def way(dtype, new, kv, hq, hkv, d, causal=True):
+    """0: few columns to a key head, 1: many, 2: many in pairs; plus 4 where the cache is cut, 8 where a wave has a head to itself."""
+    return ctypes.CDLL(g.LIB_PATH)["_ZN4gelo17attention_fp4_wayEiiiiiiiii"](int(dtype == BF16), int(causal), hq, hkv, d, len(kv), sum(new), max(new), max(kv))
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
-def test_single_tokens_of_many_sequences(ctx, dtype):
-    kv = [0, 1, 15, 16, 17, 31, 32, 33, 100, 127, 128, 129] * 11
-    run_attention(ctx, dtype, [1] * len(kv), kv, 16, 16, 64, 16, "pages", True, one_row=True, seed=2, heads=(0, 9, 15))
+@pytest.mark.parametrize("d,hq,order", [(64, 16, "pages"), (96, 32, "heads"), (128, 16, "both"), (256, 48, "pages")])
+def test_single_tokens_of_many_sequences(ctx, dtype, d, hq, order):
+    """So many sequences and heads that a wave has a head of its own; lengths at the edges of tiles and steps."""
+    kv = [0, 1, 15, 16, 17, 31, 32, 33, 63, 64, 65, 129] * 11
+    assert way(dtype, [1] * len(kv), kv, hq, 16, d) == (0 if dtype == F32 and d >= 128 else 8)
+    run_attention(ctx, dtype, [1] * len(kv), kv, hq, 16, d, 16, order, True, one_row=True, seed=2, heads=(0, hq // 2 + 1, hq - 1))
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
@@ -414,22 +422,25 @@ EDGES = [(1, 1), (5, 1), (16, 16), (17, 17), (31, 40), (32, 32), (33, 63), (63, 
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("d,hq,hkv,page,order", [(64, 32, 16, 16, "pages"), (96, 16, 16, 32, "heads"), (128, 32, 16, 16, "both"), (256, 16, 16, 64, "pages")])
 def test_many_columns_at_the_edges_of_tiles(ctx, d, hq, hkv, page, order, causal):
-    """New rows and lengths at, before and behind the ends of tiles, steps and groups, none, and more rows than keys; rows of the cache that
+    """The kernel for prompts.  New rows and lengths at, before and behind the ends of tiles, steps and groups, none, and more rows than keys; rows of the cache that
     belong to nobody are NaN.  All rows of three heads."""
+    assert way(BF16, [x[0] for x in EDGES], [x[1] for x in EDGES], hq, hkv, d, causal) in (1, 2)
     run_attention(ctx, BF16, [x[0] for x in EDGES], [x[1] for x in EDGES], hq, hkv, d, page, order, causal, seed=3, heads=(0, hq // 2 + 1, hq - 1))
 
 
-ODD = [  # dtype, sequences, rows, heads, page
-    (BF16, 2, 1, 4, 16), (F32, 2, 1, 4, 16), (BF16, 1, 12, 1, 16), (F32, 1, 150, 2, 32), (BF16, 16, 150, 16, 16), (BF16, 8, 512, 16, 16)]
+ODD = [  # dtype, sequences, rows, heads, page, the ways it goes at the widths in turn
+    (BF16, 2, 1, 4, 16, (0, 0, 0, 0)), (F32, 2, 1, 4, 16, (0, 0, 0, 0)), (BF16, 1, 12, 1, 16, (0, 0, 0, 0)), (F32, 1, 150, 2, 32, (0, 0, 0, 0)),
+    (BF16, 16, 150, 16, 16, (1, 1, 1, 2)), (BF16, 8, 512, 16, 16, (1, 1, 1, 2)), (BF16, 16, 384, 16, 16, (2, 2, 2, 1)), (BF16, 132, 1, 16, 16, (8, 8, 8, 8))]
 
 
-@pytest.mark.parametrize("dtype,n_seqs,rows,heads,page", ODD)
+@pytest.mark.parametrize("dtype,n_seqs,rows,heads,page,ways", ODD)
 @pytest.mark.parametrize("d", [64, 96, 128, 256])
-def test_blocks_that_are_nan_reach_only_rows_that_see_them(ctx, d, dtype, n_seqs, rows, heads, page):
+def test_blocks_that_are_nan_reach_only_rows_that_see_them(ctx, d, dtype, n_seqs, rows, heads, page, ways):
     """One block of one value row in every sequence and head: only query rows from its own on, and only that block's components; everything else keeps its bits.  A
     key's block: the rows before it do not see it.  A page number outside the cache: its sequence alone."""
     kv = max(rows, 90)
     at, block = 75, 1
+    assert way(dtype, [rows] * n_seqs, [kv] * n_seqs, heads, heads, d) == ways[(64, 96, 128, 256).index(d)]
     each = (kv + page - 1) // page
     K, V, _, _ = filled(n_seqs * each, heads, page, d, 3)
     table = torch.arange(n_seqs * each, dtype=torch.int32, device="cuda").view(n_seqs, each)

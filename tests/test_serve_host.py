@@ -149,3 +149,35 @@ def test_reserved_workspace_of_adapters_serves_every_smaller_call():
             d, p = 8 * rng.randint(1, 2000), 8 * rng.randint(2, 3000)
             got = needs(rng.randint(0, 1), less, d, p, rng.choice([8, rank]), rng.randint(1, parts), rng.choice([count, rng.randint(1, count)]))
             assert 0 < got <= reserved, (n, rank, parts, count, less, d, p)
+
+
+def test_reserved_workspace_of_attention_serves_caches_of_4_bits():
+    """gelo_reserve_attention sizes one workspace for both kinds of cache."""
+    lib = ctypes.CDLL(g.LIB_PATH)
+    needs, bound = lib["_ZN4gelo19attention_fp4_partsEiiiiiiiii"], lib["_ZN4gelo25attention_workspace_boundEi"]
+    needs.restype = bound.restype = ctypes.c_size_t
+    rng = random.Random(2)
+    for _ in range(20000):
+        d, hkv = rng.choice([64, 96, 128, 256]), rng.choice([1, 2, 3, 4, 8, 16, 32, 40])
+        seqs, rows, kv = (int(2 ** rng.uniform(0, x)) for x in (9, 13, 20))
+        got = needs(rng.randint(0, 1), rng.randint(0, 1), hkv * rng.choice([1, 2, 4, 7, 16]), hkv, d, seqs, seqs * rows if rng.random() < 0.7 else rows, rows, kv)
+        assert got <= bound(d), (d, hkv, seqs, rows, kv)
+
+
+def test_which_way_attention_over_4_bits_goes():
+    """Few columns to a key head or many (1, 2: tiles in pairs), the cache cut (4), a head to a wave (8).  Measured, us, few and many: 1 x 100 rows of 32 heads of 128 6.2 and 10.3,
+    16 x 32 rows on 512 keys, 12 heads of 64, 8.8 and 14.4, 8 x 128 on 512, 32 heads, 37.7 and 23.4, 8 x 512 118 and 45.7, 1 x 2000 32/8 113 and 62.8, 1 x 500 on 8500 8/8 of 64 39 and 35."""
+    way = ctypes.CDLL(g.LIB_PATH)["_ZN4gelo17attention_fp4_wayEiiiiiiiii"]
+    for want, args in ((0, (1, 1, 32, 32, 128, 1, 100, 100, 100)), (0, (1, 1, 12, 12, 64, 16, 512, 32, 512)), (1, (1, 1, 32, 32, 128, 8, 1024, 128, 512)), (2, (1, 1, 32, 32, 128, 8, 4096, 512, 512)),
+                       (4, (1, 1, 32, 8, 128, 3, 3, 1, 32768)), (8, (1, 1, 32, 32, 128, 64, 64, 1, 4096)), (0, (0, 1, 32, 32, 128, 64, 64, 1, 4096)), (8, (0, 1, 32, 32, 64, 64, 64, 1, 4096)),
+                       (0, (0, 1, 32, 32, 128, 8, 4096, 512, 512)), (5, (1, 1, 8, 8, 64, 1, 500, 500, 8500))):
+        assert way(*args) == want, args
+
+
+def test_which_way_adapters_go():
+    """Rows by themselves, groups as they come (1), groups put in order (2).  Measured, us: see kRowsRead and few_adapters in adapt.hip."""
+    way = ctypes.CDLL(g.LIB_PATH)["_ZN4gelo9adapt_wayEiiiiiii"]
+    for want, args in ((0, (1, 64, 4096, 12288, 16, 3, 48)), (0, (1, 96, 4096, 12288, 16, 3, 1)), (1, (1, 128, 4096, 12288, 16, 3, 1)), (0, (1, 128, 4096, 12288, 16, 3, 64)),
+                       (2, (1, 192, 4096, 12288, 16, 3, 64)), (1, (1, 64, 4096, 4096, 128, 1, 1)), (0, (1, 1024, 1024, 1024, 8, 1, 4)), (2, (1, 1024, 4096, 12288, 16, 3, 8)),
+                       (1, (1, 4096, 4096, 12288, 16, 3, 8)), (2, (1, 4096, 4096, 12288, 16, 3, 9)), (0, (1, 4096, 4096, 12288, 16, 3, 12288))):
+        assert way(*args) == want, args
