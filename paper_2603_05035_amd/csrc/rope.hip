@@ -62,39 +62,6 @@ template <> struct Eight<float> {
     __device__ __forceinline__ void set(const float (&v)[8]) { a = f32x4_t{v[0], v[1], v[2], v[3]}; b = f32x4_t{v[4], v[5], v[6], v[7]}; }
 };
 
-// The items x and, rot / 2 components further on, y turn; without `two` the neighbours in x.  angles: cosine and sine of the first pair.
-template <class T>
-__device__ __forceinline__ void turn_item(Eight<T>& x, Eight<T>& y, bool two, const float* angles) {
-    float v[8], cs[16];
-    x.get(v);
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        if (!two && t >= 2) break;
-        const f32x4_t c = *reinterpret_cast<const f32x4_t*>(angles + 4 * t);
-#pragma unroll
-        for (int u = 0; u < 4; ++u) cs[4 * t + u] = c[u];
-    }
-    if (two) {
-        float w[8], p[8], q[8];
-        y.get(w);
-#pragma unroll
-        for (int t = 0; t < 8; ++t) {
-            p[t] = v[t] * cs[2 * t] - w[t] * cs[2 * t + 1];
-            q[t] = w[t] * cs[2 * t] + v[t] * cs[2 * t + 1];
-        }
-        x.set(p);
-        y.set(q);
-    } else {
-        float p[8];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            p[2 * t] = v[2 * t] * cs[2 * t] - v[2 * t + 1] * cs[2 * t + 1];
-            p[2 * t + 1] = v[2 * t + 1] * cs[2 * t] + v[2 * t] * cs[2 * t + 1];
-        }
-        x.set(p);
-    }
-}
-
 // A workgroup takes a row of QKV.  Its work is cut into items of 8 values, or of 8 + 8 where components rot / 2 apart turn together: a
 // head that turns has `per_turned` items, rot / 16 such pairs and then the components behind rot; a value head has d / 8.
 template <class T>
@@ -134,7 +101,37 @@ void rope_append_kernel(RopeAppend o) {
         x.load(in + (int64_t)from * d + col);
         const bool two = turns && !o.pairs;
         if (two) y.load(in + (int64_t)from * d + col + o.rot / 2);
-        if (turns) turn_item(x, y, two, angles + (two ? 2 * col : col));
+        if (turns) {
+            float v[8], cs[16];
+            x.get(v);
+            const int at_angle = two ? 2 * col : col;          // float of the table's row
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                if (!two && t >= 2) break;
+                const f32x4_t c = *reinterpret_cast<const f32x4_t*>(angles + at_angle + 4 * t);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) cs[4 * t + u] = c[u];
+            }
+            if (two) {
+                float w[8], p[8], q[8];
+                y.get(w);
+#pragma unroll
+                for (int t = 0; t < 8; ++t) {
+                    p[t] = v[t] * cs[2 * t] - w[t] * cs[2 * t + 1];
+                    q[t] = w[t] * cs[2 * t] + v[t] * cs[2 * t + 1];
+                }
+                x.set(p);
+                y.set(q);
+            } else {
+                float p[8];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    p[2 * t] = v[2 * t] * cs[2 * t] - v[2 * t + 1] * cs[2 * t + 1];
+                    p[2 * t + 1] = v[2 * t + 1] * cs[2 * t] + v[2 * t] * cs[2 * t + 1];
+                }
+                x.set(p);
+            }
+        }
         T* out;
         if (!is_value && head < hq) {
             out = (T*)o.Q + (int64_t)row * o.ldq + (int64_t)head * d + col;
@@ -212,7 +209,37 @@ void rope_append_fp4_kernel(RopeAppend o) {
             Eight<T> x, y;
             x.load(in + (int64_t)head * d + col);
             if (two) y.load(in + (int64_t)head * d + col + o.rot / 2);
-            if (turns) turn_item(x, y, two, angles + (two ? 2 * col : col));
+            if (turns) {
+                float v[8], cs[16];
+                x.get(v);
+                const int at_angle = two ? 2 * col : col;          // float of the table's row
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    if (!two && t >= 2) break;
+                    const f32x4_t c = *reinterpret_cast<const f32x4_t*>(angles + at_angle + 4 * t);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) cs[4 * t + u] = c[u];
+                }
+                if (two) {
+                    float w[8], p[8], q[8];
+                    y.get(w);
+#pragma unroll
+                    for (int t = 0; t < 8; ++t) {
+                        p[t] = v[t] * cs[2 * t] - w[t] * cs[2 * t + 1];
+                        q[t] = w[t] * cs[2 * t] + v[t] * cs[2 * t + 1];
+                    }
+                    x.set(p);
+                    y.set(q);
+                } else {
+                    float p[8];
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        p[2 * t] = v[2 * t] * cs[2 * t] - v[2 * t + 1] * cs[2 * t + 1];
+                        p[2 * t + 1] = v[2 * t + 1] * cs[2 * t] + v[2 * t] * cs[2 * t + 1];
+                    }
+                    x.set(p);
+                }
+            }
             if (!at.placed) {
                 float v[8];
 #pragma unroll
