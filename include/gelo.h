@@ -355,8 +355,8 @@ gelo_status gelo_reserve_attention(gelo_ctx* ctx, int head_dim);
  *
  * gelo_kv_cache_fp4: K and V are arrays of n_pages pages; head h of page g is a piece of gelo_fp4_page_bytes(page_rows, head_dim) bytes from byte
  * g page_stride + h head_stride of either (strides in bytes, multiples of 16, of pages below 2^31).  page_rows is a power of two from 16 on, head_dim a multiple of 32, their
- * product at most 2^28.  k and v are 16-byte aligned DEVICE pointers.  A piece is the codes of its rows, then their scale bytes (e + 127; 255: NaN), as
- * gelo_rope_append_fp4 writes them: two codes to a byte, the value of even number in the lower half; of keys row by row, of values four rows at a time: of each
+ * product at most 2^28.  k and v are 16-byte aligned DEVICE pointers.  A piece is the codes of its rows, then their scale bytes (e + 127; 255: NaN; a query that
+ * sees a block of another byte beyond 252 or below 17 gets what it may), as gelo_rope_append_fp4 writes them: two codes to a byte, the value of even number in the lower half; of keys row by row, of values four rows at a time: of each
  * of the four rows the first head_dim / 32 bytes of its codes, then of each the next, 16 times; and of each the first block's scale, then of each the next block's. */
 typedef struct gelo_kv_cache_fp4 {
     uint8_t* k;

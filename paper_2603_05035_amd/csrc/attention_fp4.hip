@@ -152,11 +152,12 @@ struct Few {
             }
         });
     }
-    // slots of a half whose block (of heads of 96: first or second one) is NaN
+    // slots of a half whose block (of heads of 96: first or second one) is NaN, or has a scale beyond the format's: what lies behind a sequence's end may be anything, and
+    // its 6 2^126 are infinities
     __device__ __forceinline__ uint32_t odd_slots(int half, int b) const {
         uint32_t odd = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) odd |= (uint32_t)(((v_scale[2 * half + (i >> 2)][b] >> (8 * (i & 3))) & 0xFFu) == 0xFFu) << i;
+        for (int i = 0; i < 8; ++i) odd |= (uint32_t)(((v_scale[2 * half + (i >> 2)][b] >> (8 * (i & 3))) & 0xFFu) > kFp4MostScale) << i;
         return odd;
     }
     // as accumulate, where some keys are hidden from some columns (seen: bit per slot): 0 times NaN would be NaN in those.  How many NaN a column sees of a

@@ -14,6 +14,8 @@ namespace gelo {
 
 __device__ __forceinline__ int fp4_scales_at(int d, int page_shift) { return (d / 2) << page_shift; }       // bytes of a piece before its scales
 
+constexpr uint32_t kFp4MostScale = 125 + 127;                // bytes beyond it are not finite: 255, and 253 and 254, which are never written
+
 // the float 2^(byte - 127); 255: what the conversions take for a NaN scale
 __device__ __forceinline__ float fp4_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
 

@@ -264,8 +264,8 @@ def attention_bound(ref, absolute, Q, K, scale, kv, d, dtype):
     return bound + 1e-30
 
 
-def hide(K, V, table, kv, page, d):
-    """Everything that no query may see - rows behind a sequence's end, pages of nobody - becomes bytes 255: NaN."""
+def hide(K, V, table, kv, page, d, byte=255):
+    """Everything that no query may see - rows behind a sequence's end, pages of nobody - becomes such bytes; 255: NaN."""
     n_pages = K.shape[0]
     seen = np.zeros((n_pages, page), dtype=bool)
     for s, n in enumerate(kv):
@@ -277,7 +277,7 @@ def hide(K, V, table, kv, page, d):
         for places in (at, at_scale):
             for r in range(page):
                 mask[np.ix_(seen[:, r], places[r])] = False
-        pool.masked_fill_(torch.from_numpy(mask).cuda()[:, None], 255)
+        pool.masked_fill_(torch.from_numpy(mask).cuda()[:, None], byte)
 
 
 def run_attention(ctx, dtype, new, kv, hq, hkv, d, page, order, causal, scale=None, max_kv=None, one_row=False, seed=7, heads=None):
@@ -473,6 +473,22 @@ def test_blocks_that_are_nan_reach_only_rows_that_see_them(ctx, d, dtype, n_seqs
     assert torch.equal(o[:-1], clean[:-1]) and torch.isnan(o[-1, -1]).all()
     bad[n_seqs - 1, 2] = -3
     assert torch.isnan(run(K, V, g.SeqBatch(batch.kv_len, bad, kv, row_start=row_start, max_rows=rows))[-1, -1]).all()
+
+
+@pytest.mark.parametrize("dtype,new,kv,heads", [(BF16, [1, 1, 1], [1, 77, 2050], 2), (F32, [3, 40], [3, 75], 2), (BF16, [1] * 132, [70] * 132, 16), (BF16, [150] * 16, [155] * 16, 16)])
+@pytest.mark.parametrize("d", [64, 96, 128, 256])
+def test_nothing_that_lies_where_nobody_sees_it_is_felt(ctx, d, dtype, new, kv, heads):
+    """Rows behind a sequence's end that were never written may hold any byte, scales that no append writes among them: with 253 and 254 there the values are infinite."""
+    batch, table, row_start, n_pages = make_batch(new, kv, 16, 6)
+    K, V, _, _ = filled(n_pages, heads, 16, d, 5)
+    Q = rand((int(row_start[-1]), heads * d), 8, dtype)
+    results = []
+    for byte in (0, 127, 252, 253, 254, 255):
+        hide(K, V, table, kv, 16, d, byte)
+        results.append(torch.empty_like(Q))
+        g.gelo_attention_fp4(ctx, Q, results[-1], heads, g.KvCacheFp4(K, V, 16, d), batch, d ** -0.5)
+        assert torch.isfinite(results[-1].float()).all(), byte
+        assert torch.equal(results[-1], results[0]), byte
 
 
 @pytest.mark.parametrize("dtype,new,hq", [(BF16, [1] * 5, 4), (F32, [1] * 5, 4), (BF16, [150] * 8, 16), (F32, [40] * 3, 2)])
