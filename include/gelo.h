@@ -406,7 +406,7 @@ typedef struct gelo_adapters {
 
 /* Z[i, j] = base[i, j] + scale[w] sum_r (sum_k H[i, k] A_w[r, k]) B_w[j, r], r over the rank rows of j's part, w = which[i] (DEVICE, n 32-bit
  * integers).  A row whose number is no adapter's (-1, say) gets base[i].  H: n x d (ldh), base, Z: n x p (ldb, ldz) of type `dtype`; Z may be base itself, and
- * shares no memory with H or with base otherwise.  Sums are float, one rounding at the end; GELO_BF16 holds the inner sum in 16 bits for the second product.  A
+ * shares no memory with H or with base otherwise.  Sums are float, one rounding at the end; GELO_BF16 may hold the inner sum in 16 bits for the second product.  A
  * NaN or infinity in H, base or an adapter reaches only the rows it belongs to.  Rows in any order.
  * The inner sums go through float workspace of the context (gelo_reserve_adapt sizes it ahead; else the first call that needs more allocates, and what it replaces stays
  * until the context ends): calls on one context must not overlap in time on different streams. */

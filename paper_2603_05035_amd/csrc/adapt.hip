@@ -155,14 +155,14 @@ __device__ __forceinline__ void read_t(const AdaptArgs& a, const float* t, float
 #pragma unroll
     for (int e = 0; e < PER; ++e) v[e] *= scale;
 }
-// as an operand: of bfloat16 the upper part, or (rest) what it leaves
+// as an operand: of bfloat16 the upper part, or (rest) what it leaves, of the same sign and not zero: an infinity in B would be NaN by a zero
 __device__ __forceinline__ bf16x8_t piece_of(const float (&v)[8], bool rest) {
     bf16x8_t f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const float up = __uint_as_float(__float_as_uint(v[e]) & 0xFFFF0000u);
-        const float low = fabsf(v[e]) < __builtin_inff() ? v[e] - up : 0.f;
-        f[e] = (__bf16)(rest ? low : fabsf(v[e]) <= __builtin_inff() ? up : v[e]);
+        const float low = v[e] - up;
+        f[e] = (__bf16)(rest && fabsf(v[e]) < __builtin_inff() ? low != 0.f ? low : 0x1p-40f * v[e] : rest || v[e] != v[e] ? v[e] : up);
     }
     return f;
 }

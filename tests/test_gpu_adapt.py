@@ -212,6 +212,28 @@ def test_what_is_not_finite_reaches_only_its_rows(ctx, bad, n, d, rank, count, w
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,d,rank,count,want", [(40, 136, 16, 4, 0), (900, 1400, 16, 4, 1), (700, 1400, 48, 4, 1), (700, 1400, 64, 9, 2)])
+def test_an_infinite_weight_has_the_sign_of_what_it_meets(ctx, n, d, rank, count, want, dtype):
+    """T whole numbers of few bits, which a bfloat16 holds with nothing left: T times an infinity is one."""
+    parts, p = (48, 32), 80
+    H, base, A, B, scale, ends = make(n, d, parts, rank, count, dtype, 3)
+    H.copy_(torch.randint(1, 3, H.shape, generator=torch.Generator().manual_seed(1)))
+    A.zero_()
+    A[:, :, 0] = 1.0
+    A[:, 3, 0] = -1.0                                        # of the first part's ranks
+    assert way(n, d, p, rank, 2, count, dtype) == want
+    B[1, 5, 3] = float("inf")
+    B[1, 6, 2] = float("inf")
+    B[1, 60, 3] = float("-inf")
+    ids = torch.tensor([i % count for i in range(n)], dtype=torch.int32).cuda()
+    Z = g.gelo_adapt(ctx, H, g.Adapters(A, B, part_ends=ends), ids, torch.empty_like(base), base=base)
+    mine = Z[ids == 1].float()
+    assert (mine[:, [5, 60]] == -float("inf")).all() and (mine[:, 6] == float("inf")).all()
+    mine[:, [5, 6, 60]] = 0
+    assert torch.isfinite(mine).all() and torch.isfinite(Z[ids != 1].float()).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("n,d,rank,count,want", [(33, 264, 16, 6, 0), (600, 1400, 56, 4, 1), (600, 1400, 80, 6, 2)])
 def test_a_row_s_bits_do_not_go_by_the_rows_around_it(ctx, n, d, rank, count, want, dtype):
     """The same rows in another order, and with other adapters beside them."""
