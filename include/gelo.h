@@ -340,8 +340,8 @@ gelo_status gelo_rope_append(gelo_ctx* ctx, gelo_dtype dtype, int n_q_heads, con
  * bits for the product with V; a call where max_rows times the query heads of a key head is more than 16 may round them to bfloat16, in their sum too.  What lies in
  * cache rows that no query of the batch sees does not reach the result, NaN and infinity included.
  * Where the rows and heads are too few to fill the chip the cache's length is cut over workgroups and their parts are joined through float
- * workspace of the context (gelo_reserve_attention sizes it ahead; else the first call that needs more allocates): calls on one context must not
- * overlap in time on different streams. */
+ * workspace of the context (gelo_reserve_attention sizes it ahead; else the first call that needs more allocates, and what it replaces stays until the context
+ * ends): calls on one context must not overlap in time on different streams. */
 gelo_status gelo_attention(gelo_ctx* ctx, gelo_dtype dtype, int n_q_heads, const void* Q, int64_t ldq, const gelo_kv_cache* cache,
                            const gelo_seq_batch* batch, float scale, int causal, void* O, int64_t ldo, void* stream);
 /* Allocates that workspace (as much as any batch of heads of this width needs): gelo_attention then allocates nothing. */

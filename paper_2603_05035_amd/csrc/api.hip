@@ -102,7 +102,7 @@ struct gelo_ctx {
     void* quant_ws;  size_t quant_ws_bytes;    // FP8 projection: codes and row scales of the current U
     void* attention_ws; size_t attention_ws_bytes; // parts of a cut cache
     void* adapt_ws; size_t adapt_ws_bytes;         // the first products of adapters
-    void* adapt_outgrown[48]; int n_outgrown;      // smaller ones that captured calls may still name: each at least twice the one before
+    void* outgrown[80]; int n_outgrown;            // smaller ones of these two that captured calls may still name: each at least twice the one before
     void* project_ws; size_t project_ws_bytes; // bf16 projection of at most 128 rows: float partial sums of the K slices
     float* host_scalars;         // pinned: kappa read-back, one slot per lane
     int* host_flag;
@@ -452,7 +452,7 @@ gelo_status gelo_destroy(gelo_ctx* ctx) {
     if (ctx->project_ws) (void)hipFree(ctx->project_ws);
     if (ctx->attention_ws) (void)hipFree(ctx->attention_ws);
     if (ctx->adapt_ws) (void)hipFree(ctx->adapt_ws);
-    for (int i = 0; i < ctx->n_outgrown; ++i) (void)hipFree(ctx->adapt_outgrown[i]);
+    for (int i = 0; i < ctx->n_outgrown; ++i) (void)hipFree(ctx->outgrown[i]);
     if (ctx->host_scalars) (void)hipHostFree(ctx->host_scalars);
     delete ctx;
     return GELO_OK;
@@ -1644,6 +1644,20 @@ static gelo_status check_attention(gelo_ctx* ctx, gelo_dtype dtype, int n_q_head
     return GELO_OK;
 }
 
+// As grow, but what is outgrown stays until the context ends: a captured call has its address.
+static gelo_status grow_kept(gelo_ctx* ctx, void** buf, size_t* have, size_t need) {
+    if (*have >= need) return GELO_OK;
+    if (need < 2 * *have) need = 2 * *have;
+    void* larger = nullptr;
+    size_t bytes = 0;
+    const gelo_status st = grow(ctx, &larger, &bytes, need);
+    if (st != GELO_OK) return st;
+    if (*buf) ctx->outgrown[ctx->n_outgrown++] = *buf;       // (two workspaces of 256 bytes at least: no device has what 40 doublings of either make)
+    *buf = larger;
+    *have = bytes;
+    return GELO_OK;
+}
+
 static gelo_status too_many_for_a_launch(gelo_ctx* ctx, const gelo_seq_batch* batch, int n_q_heads) {
     return fail(ctx, GELO_ESHAPE, "%d sequences of up to %d rows and %d heads are too many for one launch", batch->n_seqs, batch->max_rows, n_q_heads);
 }
@@ -1659,7 +1673,7 @@ gelo_status gelo_attention(gelo_ctx* ctx, gelo_dtype dtype, int n_q_heads, const
     if (!attention_fits(o, dtype == GELO_BF16)) return too_many_for_a_launch(ctx, batch, n_q_heads);
     GELO_HIP(ctx, hipSetDevice(ctx->device));
     const size_t need = attention_workspace_bytes(o, dtype == GELO_BF16);
-    if (need > 0) st = grow(ctx, &ctx->attention_ws, &ctx->attention_ws_bytes, need);
+    if (need > 0) st = grow_kept(ctx, &ctx->attention_ws, &ctx->attention_ws_bytes, need);
     if (st != GELO_OK) return st;
     o.workspace = (float*)ctx->attention_ws;
     GELO_HIP(ctx, attention(o, dtype == GELO_BF16, (hipStream_t)stream));
@@ -1677,7 +1691,7 @@ gelo_status gelo_attention_fp4(gelo_ctx* ctx, gelo_dtype dtype, int n_q_heads, c
     if (!attention_fp4_fits(o, dtype == GELO_BF16)) return too_many_for_a_launch(ctx, batch, n_q_heads);
     GELO_HIP(ctx, hipSetDevice(ctx->device));
     const size_t need = attention_fp4_workspace_bytes(o, dtype == GELO_BF16);
-    if (need > 0) st = grow(ctx, &ctx->attention_ws, &ctx->attention_ws_bytes, need);
+    if (need > 0) st = grow_kept(ctx, &ctx->attention_ws, &ctx->attention_ws_bytes, need);
     if (st != GELO_OK) return st;
     o.workspace = (float*)ctx->attention_ws;
     GELO_HIP(ctx, attention_fp4(o, dtype == GELO_BF16, (hipStream_t)stream));
@@ -1688,21 +1702,7 @@ gelo_status gelo_reserve_attention(gelo_ctx* ctx, int head_dim) {
     if (!ctx) return GELO_EINVAL;
     if (head_dim != 64 && head_dim != 96 && head_dim != 128 && head_dim != 256) return fail(ctx, GELO_ESHAPE, "head_dim=%d is none of 64, 96, 128, 256", head_dim);
     GELO_HIP(ctx, hipSetDevice(ctx->device));
-    return grow(ctx, &ctx->attention_ws, &ctx->attention_ws_bytes, attention_workspace_bound(head_dim));
-}
-
-// The first products' workspace.  What is outgrown stays until the context ends: a captured call has its address.
-static gelo_status grow_adapt(gelo_ctx* ctx, size_t need) {
-    if (ctx->adapt_ws_bytes >= need) return GELO_OK;
-    if (need < 2 * ctx->adapt_ws_bytes) need = 2 * ctx->adapt_ws_bytes;
-    void* larger = nullptr;
-    size_t have = 0;
-    const gelo_status st = grow(ctx, &larger, &have, need);
-    if (st != GELO_OK) return st;
-    if (ctx->adapt_ws) ctx->adapt_outgrown[ctx->n_outgrown++] = ctx->adapt_ws;         // (48 doublings of 512 bytes are more than any device has)
-    ctx->adapt_ws = larger;
-    ctx->adapt_ws_bytes = have;
-    return GELO_OK;
+    return grow_kept(ctx, &ctx->attention_ws, &ctx->attention_ws_bytes, attention_workspace_bound(head_dim));
 }
 
 static gelo_status check_adapters(gelo_ctx* ctx, const gelo_adapters* a, int d, int p) {
@@ -1748,7 +1748,7 @@ gelo_status gelo_adapt(gelo_ctx* ctx, gelo_dtype dtype, int n, int d, int p, con
     for (int k = 0; k < kMostParts; ++k) o.part_end[k] = k < o.n_parts ? adapters->part_end[k] : p;
     if (!adapt_fits(o, dtype == GELO_BF16)) return fail(ctx, GELO_ESHAPE, "%d rows of %d columns are too many for one launch", n, p);
     GELO_HIP(ctx, hipSetDevice(ctx->device));
-    st = grow_adapt(ctx, adapt_workspace_bytes(o, dtype == GELO_BF16));
+    st = grow_kept(ctx, &ctx->adapt_ws, &ctx->adapt_ws_bytes, adapt_workspace_bytes(o, dtype == GELO_BF16));
     if (st != GELO_OK) return st;
     o.workspace = (float*)ctx->adapt_ws;
     GELO_HIP(ctx, adapt(o, dtype == GELO_BF16, (hipStream_t)stream));
@@ -1761,7 +1761,7 @@ gelo_status gelo_reserve_adapt(gelo_ctx* ctx, int n, int rank, int n_parts, int 
     if (rank < 8 || rank % 8 != 0 || rank > GELO_ADAPT_MAX_RANK || n_parts < 1 || n_parts > GELO_ADAPT_MAX_PARTS)
         return fail(ctx, GELO_ESHAPE, "rank=%d n_parts=%d", rank, n_parts);
     GELO_HIP(ctx, hipSetDevice(ctx->device));
-    return grow_adapt(ctx, adapt_workspace_bound(n, rank, n_parts, n_adapters));
+    return grow_kept(ctx, &ctx->adapt_ws, &ctx->adapt_ws_bytes, adapt_workspace_bound(n, rank, n_parts, n_adapters));
 }
 
 }  // extern "C"

@@ -655,6 +655,50 @@ def test_other_streams_and_captured_graphs(ctx):
             assert torch.equal(x, y)
 
 
+@pytest.mark.parametrize("later", ["fp4", "plain"])
+def test_workspace_that_is_outgrown_serves_captured_calls(ctx, later):
+    """A captured call keeps its workspace's address: a call later that needs more, of either kind of cache, takes another one."""
+    c = g.gelo_create(0, 1)
+    try:
+        a, b = ([1], [2500], 2, 64), ([1] * 4, [4000] * 4, 4, 256)
+        lib = ctypes.CDLL(g.LIB_PATH)
+
+        def needs(new, kv, heads, d):
+            parts = getattr(lib, "_ZN4gelo19attention_fp4_partsEiiiiiiiii")
+            parts.restype = ctypes.c_size_t
+            return parts(1, 1, heads, heads, d, len(new), len(new), 1, max(kv))
+        assert 0 < 2 * needs(*a) < needs(*b)
+
+        def state(new, kv, heads, d):
+            batch, _, _, n_pages = make_batch(new, kv, 16, 3, one_row=True)
+            Q = rand((len(new), heads * d), 4, BF16)
+            K, V, _, _ = filled(n_pages, heads, 16, d, 5)
+            return Q, torch.empty_like(Q), heads, g.KvCacheFp4(K, V, 16, d), batch, d ** -0.5
+        small, large = state(*a), state(*b)
+        g.gelo_attention_fp4(c, *small)
+        want = small[1].clone()
+        graph = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph):
+            g.gelo_attention_fp4(c, *small)
+        if later == "fp4":
+            g.gelo_attention_fp4(c, *large)
+        else:
+            pool = rand((4 * 250 + 3, 4, 16, 256), 6, BF16)
+            g.gelo_attention(c, large[0], large[1], 4, g.KvCache(pool, pool), large[4], 0.1)
+        hold = [torch.full((1 << 20,), 3.0, device="cuda") for _ in range(8)]        # what the runtime may put into memory that was given back
+        for _ in range(3):
+            small[1].fill_(5)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(small[1], want)
+            if later == "fp4":
+                g.gelo_attention_fp4(c, *large)
+        del hold
+    finally:
+        g.gelo_destroy(c)
+
+
 def test_the_same_call_twice_gives_the_same_bits(ctx):
     O = run_attention(ctx, BF16, [1, 1], [2000, 1111], 8, 2, 128, 16, "pages", True, one_row=True)
     assert torch.equal(O, run_attention(ctx, BF16, [1, 1], [2000, 1111], 8, 2, 128, 16, "pages", True, one_row=True))
