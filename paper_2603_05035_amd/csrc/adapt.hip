@@ -3,11 +3,12 @@
 //
 // T = H A_w^T for all parts, in float, d cut over workgroups whose sums lie side by side; then base + scale T B_w^T.  Bound by the bytes of H, base, Z and the
 // adapters.
-//   few rows   two launches.  A tile is 16 rows as they come; a tile's adapters go side by side, rows of others count as zeros and their results are dropped.
+//   few rows   two launches.  The first takes tiles of 16 rows as they come; a tile's adapters go side by side, rows of others count as zeros and their results are
+//              dropped.  The second takes row by row.
 //   many rows  three: the first puts the rows of an adapter together, 64 to a group (rows that are so already stay in runs); then a tile is a group.
 // A row's sums do not go by the rows around it: each is a column of a matrix instruction.
 //
-// bfloat16 takes v_mfma_f32_16x16x32_bf16, and the float T of the second product as two bfloat16, 16 bits of it: with one, its rounding would show where what the
+// bfloat16 takes v_mfma_f32_16x16x32_bf16, and (many rows) the float T of the second product as two bfloat16, 16 bits of it: with one, its rounding would show where what the
 // adapter adds is as large as base.  float takes v_mfma_f32_16x16x4_f32.
 #include "gelo_internal.h"
 
@@ -40,6 +41,11 @@ template <class T> __device__ __forceinline__ typename Lane<T>::piece_t none() {
     return __builtin_bit_cast(typename Lane<T>::piece_t, u32x4_t{0, 0, 0, 0});
 }
 
+// lane l's 16 bytes land at lds_addr + 16 l (wave-uniform: it travels in M0)
+__device__ __forceinline__ void fetch16(const void* from, uint32_t lds_addr) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" :: "v"(from), "s"(lds_addr) : "memory", "m0");
+}
+
 struct AdaptArgs {
     Adapt o;
     int all;                             // rank n_parts: values of a row of T
@@ -50,7 +56,8 @@ struct AdaptArgs {
     // many rows put in order; null: as they come
     int2* groups;                        // of each group its adapter (-1: none) and how many rows it has; n_groups of them, some have none
     int* order;                          // 64 places to each group
-    int n_groups;
+    int n_groups;                        // (a multiple of 8)
+    bool by_die;                         // the second product of a group on the die that had its first
 };
 
 __device__ __forceinline__ int part_of_block(const AdaptArgs& a, int block) {
@@ -78,7 +85,8 @@ struct Tile {
     }
 };
 
-// Few rows, the first product.  A workgroup: one of the adapters of a tile, 64 rows of A, one part of d, whose steps its waves share out.
+// Few rows, the first product.  A workgroup: one of the adapters of a tile, 64 rows of A, one part of d, whose steps its waves share out.  64 rows with 48 adapters of
+// 48 x 4096: 19 MB in 5.8 us; a smaller part of d makes more of T, which every workgroup of the second product adds up again.
 template <class T>
 __global__ __launch_bounds__(64 * kWaves)
 void adapt_few_down_kernel(AdaptArgs a) {
@@ -202,7 +210,8 @@ template <class T> __device__ __forceinline__ Rank rank_of(int rank, int s, int 
 }
 
 // Few rows, the second product, as sums of products: a row has its adapter to itself as a rule, and a matrix instruction would multiply 15 rows of zeros.  A
-// workgroup: one row, kFewCols columns of one part, two side by side to a thread.  64 rows with 48 adapters, 12288 columns, rank 16: see launch().
+// workgroup: one row, kFewCols columns of one part, two side by side to a thread.  Bound by its trips to memory - whose row, T and B, base: 64 rows with 48 adapters, 12288 columns, rank 16, 16 MB in 5.3 us (tiles of matrix
+// instructions 10).
 constexpr int kFewCols = 512;
 template <class T>
 __global__ __launch_bounds__(256)
@@ -365,10 +374,13 @@ struct Some {
             if (count <= 0) return false;
             row = at * kGroup + first + min(lane, count - 1);
             id = lane < count ? a.o.which[row] : -1;
-            if (id >= a.o.n_adapters) id = -1;
         }
-        left = __ballot(id >= 0);
         return true;
+    }
+    // (apart, so that loads of rows do not wait for their numbers)
+    __device__ __forceinline__ void look(const AdaptArgs& a) {
+        if (id >= a.o.n_adapters) id = -1;
+        left = __ballot(id >= 0);
     }
     __device__ __forceinline__ int next(uint64_t* those) {
         const int w = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
@@ -379,18 +391,20 @@ struct Some {
 };
 
 // Many rows, the first product.  A workgroup: one group, 64 rows of A, one part of d, whose steps its waves share out.  Columns of rows of other adapters come
-// out as they may and are not kept, so the rows are sent for before their adapters are known.  Neighbouring groups go to one die: its L2 then has their A.
-// (16 rows and all of d to a workgroup: every 16 rows read A for themselves, 4096 rows 26 us instead of 13.  Half as many waves: twice the parts of d, which the second
-// product reads once for each of its workgroups, 60 instead of 57.5 for both.)
-constexpr int kDownWaves = 8;
+// out as they may and are not kept, so the rows are sent for before their adapters are known.  Neighbouring groups go to one die: its L2 then has their A.  A wave's piece of H
+// lies in its registers, that of A in its own part of LDS, put there by loads that need no registers: all of it is one trip to memory (tile after tile of A
+// through registers, a trip each, 2048 rows of 4096 values, rank 64: 12.8 us, 8.9).  (16 rows and all of d to a workgroup: every 16 rows read A for themselves, 4096 rows 26 us instead of 13.
+// Half as many waves: twice the parts of d, which the second product reads once for each of its workgroups, 60 instead of 57.5 for both.)
+constexpr int kDownWaves = 8, kDownWaveLds = 16 * 1024;
 template <class T>
 __global__ __launch_bounds__(64 * kDownWaves, 2)
 void adapt_many_down_kernel(AdaptArgs a) {
     typedef Lane<T> L;
     typedef typename L::piece_t piece_t;
     constexpr int STEP = 4 * L::PER, RT = 4, HT = kGroup / 16, AHEAD = 4;
+    static_assert(RT * AHEAD * 1024 == kDownWaveLds && HT * RT * 1024 == kDownWaveLds, "");
     const Adapt& o = a.o;
-    __shared__ f32x4_t sums[kDownWaves][RT][64];
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     Some<kGroup> rows;
     // (rows as they come: neighbours to one die, as the order has it)
     if (!rows.find(a, a.groups ? blockIdx.x : (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3), 0)) return;
@@ -398,6 +412,9 @@ void adapt_many_down_kernel(AdaptArgs a) {
     const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int rank_tiles = min((a.all - first_rank + 15) / 16, RT);
     const int begin = split * a.steps, end = min(begin + a.steps, (o.d + STEP - 1) / STEP);
+    const int each = min((a.steps + kDownWaves - 1) / kDownWaves, AHEAD);        // steps of a wave at a time
+    uint8_t* mine = lds + wave * kDownWaveLds;
+    const uint32_t mine_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)mine;
     const T* h[HT];
 #pragma unroll
     for (int i = 0; i < HT; ++i) h[i] = (const T*)o.H + __shfl(rows.row, 16 * i + c, 64) * o.ldh;
@@ -409,12 +426,13 @@ void adapt_many_down_kernel(AdaptArgs a) {
 #pragma unroll
             for (int i = 0; i < HT; ++i) {
                 x[u][i] = none<T>();
-                if (s0 + u < end && col < o.d) x[u][i] = *reinterpret_cast<const piece_t*>(h[i] + col);
+                if (s0 + u < min(s0 + each, end) && col < o.d) x[u][i] = *reinterpret_cast<const piece_t*>(h[i] + col);
             }
         }
     };
-    const int first = begin + wave * AHEAD;
+    const int first = begin + wave * each;
     read_h(first);
+    rows.look(a);
     bool there = true;
     while (rows.left) {
         uint64_t those;
@@ -425,47 +443,60 @@ void adapt_many_down_kernel(AdaptArgs a) {
         for (int i = 0; i < HT; ++i)
 #pragma unroll
             for (int t = 0; t < RT; ++t) sum[i][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        for (int s0 = first; s0 < end; s0 += kDownWaves * AHEAD) {
-            if (!there) read_h(s0);
-            there = end - first <= kDownWaves * AHEAD;       // nothing came behind them: another adapter finds them there
+        for (int s0 = first; s0 < end; s0 += kDownWaves * each) {
+            const int upto = min(s0 + each, end);
+            // what the wave multiplies lies in its own part of LDS, as its lanes take it (behind A's rows and columns: the last ones again)
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
             for (int t = 0; t < RT; ++t) {
                 if (t >= rank_tiles) break;
-                const int r = first_rank + 16 * t + c;
-                piece_t y[AHEAD];
-#pragma unroll
-                for (int u = 0; u < AHEAD; ++u) {
-                    const int col = (s0 + u) * STEP + g * L::PER;
-                    y[u] = none<T>();
-                    if (s0 + u < end && col < o.d && r < a.all) y[u] = *reinterpret_cast<const piece_t*>(A + r * o.lda + col);
-                }
+                const T* from = A + min(first_rank + 16 * t + c, a.all - 1) * o.lda;
 #pragma unroll
                 for (int u = 0; u < AHEAD; ++u)
+                    if (s0 + u < upto) fetch16(from + min((s0 + u) * STEP + g * L::PER, o.d - L::PER), mine_at + (t * AHEAD + u) * 1024);
+            }
+            if (!there) read_h(s0);
+            there = end - first <= kDownWaves * each;       // nothing came behind them: another adapter finds them there
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
-                    for (int i = 0; i < HT; ++i) sum[i][t] = L::multiply(y[u], x[u][i], sum[i][t]);
+            for (int t = 0; t < RT; ++t) {
+                if (t >= rank_tiles) break;
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) {
+                    piece_t y = *reinterpret_cast<const piece_t*>(mine + (t * AHEAD + u) * 1024 + 16 * lane);
+                    if (s0 + u >= upto || (s0 + u) * STEP + g * L::PER >= o.d) y = none<T>();
+#pragma unroll
+                    for (int i = 0; i < HT; ++i) sum[i][t] = L::multiply(y, x[u][i], sum[i][t]);
+                }
             }
         }
-        // one tile of rows after the other through LDS; wave t adds up tile t of ranks: rank 16 t + 4 g + r of row c
+        // through LDS: wave 2 i + t % 2 and the next add up tile i of rows and t of ranks: rank 16 t + 4 g + r of row c
 #pragma unroll
-        for (int i = 0; i < HT; ++i) {
-            if (!((those >> (16 * i)) & 0xFFFF)) continue;
-            __syncthreads();
+        for (int i = 0; i < HT; ++i)
 #pragma unroll
-            for (int t = 0; t < RT; ++t) sums[wave][t][lane] = sum[i][t];
-            __syncthreads();
-            const int r = first_rank + 16 * wave + 4 * g, row = __shfl(rows.row, 16 * i + c, 64);
-            if (wave >= rank_tiles || r >= a.all || !((those >> (16 * i + c)) & 1)) continue;
-            f32x4_t all = sums[0][wave][lane];
+            for (int t = 0; t < RT; ++t) {
+                if (t >= rank_tiles) break;
+                *reinterpret_cast<f32x4_t*>(mine + (i * RT + t) * 1024 + 16 * lane) = sum[i][t];
+            }
+        __syncthreads();
 #pragma unroll
-            for (int k = 1; k < kDownWaves; ++k) all += sums[k][wave][lane];
+        for (int e = wave; e < HT * RT; e += kDownWaves) {
+            const int i = e / RT, t = e % RT, r = first_rank + 16 * t + 4 * g, row = __shfl(rows.row, 16 * i + c, 64);
+            if (t >= rank_tiles || r >= a.all || !((those >> (16 * i + c)) & 1)) continue;
+            f32x4_t all = *reinterpret_cast<const f32x4_t*>(lds + e * 1024 + 16 * lane);
+#pragma unroll
+            for (int k = 1; k < kDownWaves; ++k) all += *reinterpret_cast<const f32x4_t*>(lds + k * kDownWaveLds + e * 1024 + 16 * lane);
             *reinterpret_cast<f32x4_t*>(a.t + ((int64_t)split * o.n + row) * a.all + r) = all;
         }
+        if (rows.left) __syncthreads();                      // nobody reads what the next adapter's rows overwrite
     }
 }
 
 // Many rows, the second product.  A workgroup: half a group, 256 columns of one part, 64 to a wave.  What the matrix instructions leave goes through LDS, so that base is read
 // and Z written a row's 256 columns at a time (4096 x 12288 values in and out: 36 us; as the instructions leave them, 16 rows at a time, 41 to 45).  The workgroups of a
-// row's columns come one after the other, for memory's sake too (42 where those of a column do).  HALF: steps of a rank's upper parts at most.
+// row's columns come one after the other, for memory's sake too (42 where those of a column do).  Where T is a large part of what is read (by_die) they do so on the die whose L2
+// has the row's T, each die at rows of its own: 2048 rows of 4096 columns, rank 64, eight parts of d 29.1 us for both products and 26.0; 4096 rows of 12288, rank 16, four 57.3
+// and 59.6.  HALF: steps of a rank's upper parts at most.
 constexpr int kUpRows = 32, kUpCols = 256;
 template <class T, int HALF>
 __global__ __launch_bounds__(64 * kWaves, HALF == 1 && sizeof(T) == 2 ? 4 : HALF <= 2 ? 3 : 2)
@@ -477,11 +508,16 @@ void adapt_many_up_kernel(AdaptArgs a) {
     const Adapt& o = a.o;
     __shared__ piece_t z[TWICE * HALF][HT][64];
     __shared__ __attribute__((aligned(16))) float sums[kUpRows][kUpCols + 4];
-    const int blocks = a.first_block[o.n_parts], of_rows = blockIdx.x / blocks, block = blockIdx.x - of_rows * blocks;
+    const int blocks = a.first_block[o.n_parts], halves = kGroup / kUpRows;
+    int block = blockIdx.x % blocks, of_rows = blockIdx.x / blocks;
+    if (a.by_die) {
+        const int die = blockIdx.x & 7, k = blockIdx.x >> 3, j = k / blocks / halves;
+        block = k % blocks;
+        of_rows = (a.groups ? 8 * j + die : die * (a.n_groups >> 3) + j) * halves + k / blocks % halves;
+    }
     Some<kUpRows> rows;
-    if (!rows.find(a, of_rows / (kGroup / kUpRows), kUpRows * (of_rows % (kGroup / kUpRows)))) return;
+    if (!rows.find(a, of_rows / halves, kUpRows * (of_rows % halves))) return;
     const bool in_place = o.base == o.Z;
-    const uint64_t with = rows.left;                         // rows that have an adapter
     const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int part = part_of_block(a, block);
     const int first = (part > 0 ? o.part_end[part - 1] : 0) + a.wide * (block - a.first_block[part]), end = min(first + a.wide, o.part_end[part]);
@@ -497,6 +533,8 @@ void adapt_many_up_kernel(AdaptArgs a) {
         }
     };
     read(first);
+    rows.look(a);
+    const uint64_t with = rows.left;                         // rows that have an adapter
     // one row's PER rank values to a thread, those of a row side by side (what a row without an adapter has there is not used)
     const int slots = 4 * half;                              // pieces, and nothing to fill a step up with
     for (int e = threadIdx.x; e < kUpRows * slots; e += THREADS) {
@@ -603,7 +641,7 @@ constexpr double kRowsRead = 80e6, kOrderedRead = 110e6;
 // they come: 1024 rows of eight adapters in any order 34.5 and 50, of four 36.9 as they come, 4096 rows of eight in any order 67 and 92, in runs 67 and 57.5; so many rows are
 // prompts, whose rows lie side by side, more often than not.
 int few_adapters(int n) { return n >= 2048 ? 8 : 4; }
-struct Plan { bool many, ordered; int splits, steps, wide; int64_t most_groups, t_bytes, bytes; };
+struct Plan { bool many, ordered, by_die; int splits, steps, wide; int64_t most_groups, t_bytes, bytes; };
 Plan plan_of(int is_bf16, int n, int d, int p, int rank, int n_parts, int n_adapters) {
     Plan r;
     const double read = (double)n * rank * ((double)n_parts * d + p) * (is_bf16 ? 2 : 4);
@@ -612,17 +650,20 @@ Plan plan_of(int is_bf16, int n, int d, int p, int rank, int n_parts, int n_adap
     const int all = steps_of(is_bf16, d), rank_groups = (rank * n_parts + 63) / 64;
     const int64_t alone = n_adapters < n ? n_adapters + 1 : n;          // groups that are not full
     r.most_groups = round_up(r.ordered ? n / kGroup + alone : r.many ? (n + kGroup - 1) / kGroup : 0, 8);
-    // workgroups that fill the chip with the first product, of 8 waves or (few rows, which have an adapter each as a rule) 4; four steps to a wave at least
+    // workgroups that fill the chip with the first product, of 8 waves or (few rows, which have an adapter each as a rule) 4; two steps to a wave at least, or four
     const int64_t items = (r.many ? (n + kGroup - 1) / kGroup : n) * (int64_t)rank_groups, target = r.many ? 256 : 512;
     int64_t cuts = items >= target ? 1 : target / items;
-    const int to_each = 4 * (r.many ? kDownWaves : kWaves), most = (all + to_each - 1) / to_each;
+    const int to_each = r.many ? 2 * kDownWaves : 4 * kWaves, most = (all + to_each - 1) / to_each;
     cuts = cuts < most ? cuts : most;
     cuts = cuts < (r.many ? 8 : 16) ? cuts : (r.many ? 8 : 16);
     r.steps = (int)((all + cuts - 1) / cuts);
     r.splits = (all + r.steps - 1) / r.steps;
-    // two blocks of columns to a workgroup of the second product where that leaves 1024 of them: it reads T once (4096 rows, us: 62 with one, 57.5, 61 with four)
+    // two blocks of columns to a workgroup of the second product where that leaves 512 of them: it reads T once (4096 rows, us: 62 with one, 57.5, 61 with four; 1024 rows of
+    // 12288 columns, 768 workgroups, 34.4 and 32.0)
     r.wide = kFewCols;
-    if (r.many) for (r.wide = 2 * kUpCols; r.wide > kUpCols && (n + kUpRows - 1) / kUpRows * (int64_t)((p + r.wide - 1) / r.wide) < 1024;) r.wide /= 2;
+    if (r.many) for (r.wide = 2 * kUpCols; r.wide > kUpCols && (n + kUpRows - 1) / kUpRows * (int64_t)((p + r.wide - 1) / r.wide) < 512;) r.wide /= 2;
+    // (T goes to 8 dies otherwise: where that is a fifth of base and Z)
+    r.by_die = 5 * 8 * r.splits * rank * n_parts * (int64_t)sizeof(float) > 2 * (int64_t)p * (is_bf16 ? 2 : 4);
     r.t_bytes = round_up((int64_t)r.splits * n * rank * n_parts * sizeof(float), 256);
     r.bytes = r.t_bytes + (r.ordered ? (8 + 4 * kGroup) * r.most_groups : 0);
     return r;
@@ -634,7 +675,7 @@ hipError_t launch(const Adapt& o, hipStream_t stream) {
     a.o = o;
     a.all = o.rank * o.n_parts;
     const Plan p = plan_of(sizeof(T) == 2, o.n, o.d, o.p, o.rank, o.n_parts, o.n_adapters);
-    a.splits = p.splits; a.steps = p.steps; a.wide = p.wide;
+    a.splits = p.splits; a.steps = p.steps; a.wide = p.wide; a.by_die = p.by_die;
     a.first_block[0] = 0;
     for (int k = 0; k < kMostParts; ++k)
         a.first_block[k + 1] = a.first_block[k] + (k < o.n_parts ? (o.part_end[k] - (k ? o.part_end[k - 1] : 0) + a.wide - 1) / a.wide : 0);
@@ -646,7 +687,7 @@ hipError_t launch(const Adapt& o, hipStream_t stream) {
     a.order = (int*)(ws + p.t_bytes + 8 * p.most_groups);
     if (p.many) {
         if (p.ordered) hipLaunchKernelGGL(adapt_order_kernel, dim3(1), dim3(kOrderThreads), 0, stream, a);
-        hipLaunchKernelGGL(adapt_many_down_kernel<T>, dim3((unsigned)p.most_groups, a.splits, rank_groups), dim3(64 * kDownWaves), 0, stream, a);
+        hipLaunchKernelGGL(adapt_many_down_kernel<T>, dim3((unsigned)p.most_groups, a.splits, rank_groups), dim3(64 * kDownWaves), kDownWaves * kDownWaveLds, stream, a);
         const dim3 up((unsigned)(kGroup / kUpRows * p.most_groups * blocks));
         const int half = (o.rank + 4 * Lane<T>::PER - 1) / (4 * Lane<T>::PER);
         if (half <= 1) hipLaunchKernelGGL((adapt_many_up_kernel<T, 1>), up, dim3(64 * kWaves), 0, stream, a);
@@ -688,6 +729,11 @@ int adapt_way(int is_bf16, int n, int d, int p, int rank, int n_parts, int n_ada
 // adapt_workspace_bytes of these sizes
 size_t adapt_needs(int is_bf16, int n, int d, int p, int rank, int n_parts, int n_adapters) {
     return (size_t)plan_of(is_bf16, n, d, p, rank, n_parts, n_adapters).bytes;
+}
+
+hipError_t adapt_init() {
+    const hipError_t e = hipFuncSetAttribute((const void*)&adapt_many_down_kernel<uint16_t>, hipFuncAttributeMaxDynamicSharedMemorySize, kDownWaves * kDownWaveLds);
+    return e != hipSuccess ? e : hipFuncSetAttribute((const void*)&adapt_many_down_kernel<float>, hipFuncAttributeMaxDynamicSharedMemorySize, kDownWaves * kDownWaveLds);
 }
 
 hipError_t adapt(const Adapt& o, int is_bf16, hipStream_t stream) { return is_bf16 ? launch<uint16_t>(o, stream) : launch<float>(o, stream); }

@@ -382,7 +382,7 @@ static hipError_t kernels_init(int device) {
     static std::atomic<bool> done[kStaticMaxDevices];       // (two threads at once both do it: the calls may be repeated)
     if (device < kStaticMaxDevices && done[device].load(std::memory_order_acquire)) return hipSuccess;
     hipError_t (*const inits[])() = {gemm_bf16_init, gemm_f32_init, inverse_init, structured_init, small_init, gemm_fp8_init,
-                                     factor_init, block_reflect_init, block_factor_init, sampler_init, attention_init, attention_fp4_init};
+                                     factor_init, block_reflect_init, block_factor_init, sampler_init, attention_init, attention_fp4_init, adapt_init};
     for (auto init : inits) {
         const hipError_t e = init();
         if (e != hipSuccess) return e;
