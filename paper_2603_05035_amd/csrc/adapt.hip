@@ -86,7 +86,7 @@ struct Tile {
 };
 
 // Few rows, the first product.  A workgroup: one of the adapters of a tile, 64 rows of A, one part of d, whose steps its waves share out.  64 rows with 48 adapters of
-// 48 x 4096: 19 MB in 5.8 us; a smaller part of d makes more of T, which every workgroup of the second product adds up again.
+// 48 x 4096, a row without now and then: 14 MB in 6.5 us; a smaller part of d makes more of T, which every workgroup of the second product adds up again.
 template <class T>
 __global__ __launch_bounds__(64 * kWaves)
 void adapt_few_down_kernel(AdaptArgs a) {
@@ -210,7 +210,7 @@ template <class T> __device__ __forceinline__ Rank rank_of(int rank, int s, int 
 }
 
 // Few rows, the second product, as sums of products: a row has its adapter to itself as a rule, and a matrix instruction would multiply 15 rows of zeros.  A
-// workgroup: one row, kFewCols columns of one part, two side by side to a thread.  Bound by its trips to memory - whose row, T and B, base: 64 rows with 48 adapters, 12288 columns, rank 16, 16 MB in 5.3 us (tiles of matrix
+// workgroup: one row, kFewCols columns of one part, two side by side to a thread.  Bound by its trips to memory - whose row, T and B, base: 64 rows with 48 adapters, 12288 columns, rank 16, 17 MB in 5.6 us (tiles of matrix
 // instructions 10).
 constexpr int kFewCols = 512;
 template <class T>

@@ -389,6 +389,8 @@ void attention_few_fp4_kernel(AttnArgs a) {
     }
 }
 
+constexpr int kFewLong = 4096, kFewMost = 4096;             // keys; workgroups, whose columns are as many as the workspace's bound has
+static_assert(kFewMost * 16 <= kPromptTarget * 32 * kPromptWaves, "");
 static_assert(64 * kFewWaves <= 256 && 64 * kPromptWaves <= 256, "workgroups as kMostWorkgroups has them");
 
 Plan plan_few(const Attention& o, int64_t columns, int is_bf16, double* us) {
@@ -397,7 +399,11 @@ Plan plan_few(const Attention& o, int64_t columns, int is_bf16, double* us) {
     p.col_tiles = (columns + 15) / 16;
     const int64_t tiles = (int64_t)o.batch.n_seqs * o.cache.n_kv_heads * p.col_tiles;
     const int64_t most = (o.batch.max_kv_len + kFewLeast - 1) / kFewLeast;
-    const int64_t cuts = kFewTarget / tiles;
+    // Long caches are cut further, into 4096 keys, once that makes four: sequences of a batch end at lengths of their own, and the longest would work alone at the end (us as few as
+    // fill the chip, and so: 6 sequences of 18658-37317 keys of 32 heads 188 and 160, 39 of 21295-42590 of 5 213 and 167, 106 of 26353-52707 of one head of 64, float, 134 and 108; cut in
+    // two or three 17 of 6000-12000 of 32 135 and 161; 2048 keys, 16 of 32000 of 4 54 and 60).
+    const int64_t fill = kFewTarget / tiles, fine = o.batch.max_kv_len / kFewLong < kFewMost / tiles ? o.batch.max_kv_len / kFewLong : kFewMost / tiles;
+    const int64_t cuts = fine >= 4 && fine > fill ? fine : fill;
     cut(&p, o.batch.max_kv_len, cuts < 1 ? 1 : cuts < most ? cuts : most);
     p.workgroups = tiles * p.n_chunks;
     p.by_head = (is_bf16 || o.cache.head_dim < 128) && p.n_chunks == 1 && p.col_tiles == 1 && o.cache.n_kv_heads % kFewWaves == 0 && tiles / kFewWaves >= kFewTarget;

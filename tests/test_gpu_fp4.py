@@ -323,6 +323,17 @@ def way(dtype, new, kv, hq, hkv, d, causal=True):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("kv,hq,hkv,d,chunks", [([16500, 300, 0, 4224, 4225, 8449, 1] + [17] * 123, 4, 2, 64, 4), ([20481, 5, 9000], 64, 64, 96, 5)])
+def test_long_caches_are_cut_beyond_what_fills_the_chip(ctx, kv, hq, hkv, d, chunks, dtype):
+    """Sequences that end in the first piece, at a piece's end, in none."""
+    parts = ctypes.CDLL(g.LIB_PATH)["_ZN4gelo19attention_fp4_partsEiiiiiiiii"]
+    parts.restype = ctypes.c_size_t
+    n = len(kv)
+    assert parts(int(dtype == BF16), 1, hq, hkv, d, n, n, 1, max(kv)) == chunks * n * hq * (d + 2) * 4
+    run_attention(ctx, dtype, [1] * n, kv, hq, hkv, d, 64, "pages", True, one_row=True, heads=(0, hq - 1))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("d,hq,order", [(64, 16, "pages"), (96, 32, "heads"), (128, 16, "both"), (256, 48, "pages")])
 def test_single_tokens_of_many_sequences(ctx, dtype, d, hq, order):
     """So many sequences and heads that a wave has a head of its own; lengths at the edges of tiles and steps."""
