@@ -210,64 +210,83 @@ template <class T> __device__ __forceinline__ Rank rank_of(int rank, int s, int 
 }
 
 // Few rows, the second product, as sums of products: a row has its adapter to itself as a rule, and a matrix instruction would multiply 15 rows of zeros.  A
-// workgroup: one row, kFewCols columns of one part, two side by side to a thread.  Bound by its trips to memory - whose row, T and B, base: 64 rows with 48 adapters, 12288 columns, rank 16, 17 MB in 5.6 us (tiles of matrix
-// instructions 10).
+// workgroup: one row, kFewCols columns of one part.  Bound by its trips to memory - whose row, T and B, base: 64 rows with 48 adapters, 12288 columns, rank 16, 17 MB in
+// 5.5 us (tiles of matrix instructions 10).  A column's rank values lie side by side: from 64 bytes on LANES = 4 lanes take 16 each, of 8 columns (by a lane alone, two columns: both products of
+// 40 rows of 11760 columns, rank 64, 19.8 us, 14.5; of 32 of 12288 21.6, 17.6); fewer belong to one lane (64 rows, rank 16, 11.2 us, 14.9 by four).
 constexpr int kFewCols = 512;
-template <class T>
+template <class T, int LANES>
 __global__ __launch_bounds__(256)
 void adapt_few_up_kernel(AdaptArgs a) {
     const Adapt& o = a.o;
-    __shared__ __attribute__((aligned(16))) float t[128];    // the row's T
+    __shared__ __attribute__((aligned(16))) float t[kMostRank], sums[kFewCols];          // the row's T, and what it adds
     const int blocks = a.first_block[o.n_parts], row = blockIdx.x / blocks, block = blockIdx.x - row * blocks;
     const int id = o.which[row], part = part_of_block(a, block);
-    const int first = (part > 0 ? o.part_end[part - 1] : 0) + kFewCols * (block - a.first_block[part]), col = first + 2 * threadIdx.x;
-    const bool in = col < o.part_end[part], has = id >= 0 && id < o.n_adapters;
+    const int first = (part > 0 ? o.part_end[part - 1] : 0) + kFewCols * (block - a.first_block[part]), end = o.part_end[part], col = first + 2 * threadIdx.x;
+    const bool in = col < end, has = id >= 0 && id < o.n_adapters;
     if (!has && o.base == o.Z) return;
     typedef T pair_t __attribute__((ext_vector_type(2)));
     pair_t x = {};
     if (in) x = *reinterpret_cast<const pair_t*>((const T*)o.base + row * o.ldb + col);
     if (has) {
-        constexpr int PER = 16 / sizeof(T), TOGETHER = 16 / PER;             // rank values of a load, loads sent for together
-        const T* B = (const T*)o.B + id * o.b_stride + col * o.ldbw;
-        u32x4_t y[2][TOGETHER];
-        auto read = [&](int r) {
+        constexpr int PER = 16 / sizeof(T), SLOTS = 256 / LANES, COLS = kFewCols / SLOTS;
+        const int q = threadIdx.x % LANES, slot = threadIdx.x / LANES, pieces = o.rank / PER;
+        constexpr int DEEP = LANES == 1 ? 2 : 1, APART = LANES == 1 ? 1 : SLOTS;               // pieces sent for together; from one column of a lane to its next
+        const int my_first = first + (LANES == 1 ? COLS * slot : slot);
+        const T* B = (const T*)o.B + id * o.b_stride + my_first * o.ldbw;
+        u32x4_t y[DEEP][COLS];
+        auto read = [&](int piece) {
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
+            for (int u = 0; u < DEEP; ++u)
 #pragma unroll
-                for (int u = 0; u < TOGETHER; ++u)
-                    if (in && r + u * PER < o.rank) y[k][u] = *reinterpret_cast<const u32x4_t*>(B + k * o.ldbw + r + u * PER);
+                for (int k = 0; k < COLS; ++k) {
+                    if (LANES > 1) y[u][k] = u32x4_t{0, 0, 0, 0};            // (one lane breaks off instead)
+                    if ((LANES == 1 ? in : my_first + k * APART < end) && piece + u < pieces) y[u][k] = *reinterpret_cast<const u32x4_t*>(B + k * APART * o.ldbw + (piece + u) * PER);
+                }
         };
-        read(0);
-        if ((int)threadIdx.x < o.rank) {
+        read(q);
+        if (threadIdx.x < kMostRank) {
             float sum = 0.f;
-            const float* from = a.t + (int64_t)row * a.all + part * o.rank + threadIdx.x;
+            if ((int)threadIdx.x < o.rank) {
+                const float* from = a.t + (int64_t)row * a.all + part * o.rank + threadIdx.x;
 #pragma unroll 8
-            for (int s = 0; s < a.splits; ++s) sum += from[(int64_t)s * o.n * a.all];
+                for (int s = 0; s < a.splits; ++s) sum += from[(int64_t)s * o.n * a.all];
+            }
             t[threadIdx.x] = sum;
         }
         const float scale = o.scale ? o.scale[id] : 1.f;
         __syncthreads();
-        float sum[2] = {0.f, 0.f};
-        for (int r = 0; r < o.rank; r += 16) {
+        float sum[COLS];
 #pragma unroll
-            for (int u = 0; u < TOGETHER; ++u) {
-                if (r + u * PER >= o.rank) break;
+        for (int k = 0; k < COLS; ++k) sum[k] = 0.f;
+        for (int piece = q; piece - q < pieces; piece += LANES * DEEP) {
 #pragma unroll
-                for (int e = 0; e < PER; ++e) {
-                    const float with = t[r + u * PER + e];
+            for (int u = 0; u < DEEP; ++u) {
+                if (LANES == 1 && piece + u >= pieces) break;
+                float with[PER];
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const float b = sizeof(T) == 4 ? __uint_as_float(y[k][u][e & 3]) : __uint_as_float(e & 1 ? y[k][u][e >> 1] & 0xFFFF0000u : y[k][u][e >> 1] << 16);
-                        sum[k] += with * b;
-                    }
-                }
+                for (int e = 0; e < PER; e += 4) *reinterpret_cast<f32x4_t*>(with + e) = *reinterpret_cast<const f32x4_t*>(t + min(piece + u, kMostRank / PER - 1) * PER + e);
+#pragma unroll
+                for (int k = 0; k < COLS; ++k)
+#pragma unroll
+                    for (int e = 0; e < PER; ++e)
+                        sum[k] += with[e] * (sizeof(T) == 4 ? __uint_as_float(y[u][k][e & 3]) : __uint_as_float(e & 1 ? y[u][k][e >> 1] & 0xFFFF0000u : y[u][k][e >> 1] << 16));
             }
-            read(r + 16);
+            read(piece + LANES * DEEP);
+        }
+        if constexpr (LANES > 1) {
+#pragma unroll
+            for (int k = 0; k < COLS; ++k) {
+#pragma unroll
+                for (int by = 1; by < LANES; by *= 2) sum[k] += __shfl_xor(sum[k], by, 64);
+                if (q == 0) sums[slot + k * SLOTS] = sum[k];
+            }
+            __syncthreads();
         }
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            if constexpr (sizeof(T) == 4) x[k] += scale * sum[k];
-            else x[k] = __builtin_bit_cast(uint16_t, (__bf16)(__uint_as_float((uint32_t)x[k] << 16) + scale * sum[k]));
+            const float more = scale * (LANES > 1 ? sums[2 * threadIdx.x + k] : sum[k]);
+            if constexpr (sizeof(T) == 4) x[k] += more;
+            else x[k] = __builtin_bit_cast(uint16_t, (__bf16)(__uint_as_float((uint32_t)x[k] << 16) + more));
         }
     }
     if (in) *reinterpret_cast<pair_t*>((T*)o.Z + row * o.ldz + col) = x;
@@ -698,7 +717,10 @@ hipError_t launch(const Adapt& o, hipStream_t stream) {
     }
     const int tiles = (o.n + 15) / 16;
     hipLaunchKernelGGL(adapt_few_down_kernel<T>, dim3(tiles * 16, a.splits, rank_groups), dim3(64 * kWaves), 0, stream, a);
-    hipLaunchKernelGGL(adapt_few_up_kernel<T>, dim3((unsigned)(blocks * o.n)), dim3(256), 0, stream, a);
+    const dim3 up((unsigned)(blocks * o.n));
+    const int pieces = o.rank / (16 / (int)sizeof(T));
+    if (pieces < 4) hipLaunchKernelGGL((adapt_few_up_kernel<T, 1>), up, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((adapt_few_up_kernel<T, 4>), up, dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 

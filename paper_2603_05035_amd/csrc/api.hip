@@ -1705,6 +1705,7 @@ gelo_status gelo_reserve_attention(gelo_ctx* ctx, int head_dim) {
     return grow_kept(ctx, &ctx->attention_ws, &ctx->attention_ws_bytes, attention_workspace_bound(head_dim));
 }
 
+static_assert(kMostParts == GELO_ADAPT_MAX_PARTS && kMostRank == GELO_ADAPT_MAX_RANK, "");
 static gelo_status check_adapters(gelo_ctx* ctx, const gelo_adapters* a, int d, int p) {
     if (!a || !a->a || !a->b) return fail(ctx, GELO_EINVAL, "adapters and their matrices must not be NULL");
     if (a->n_adapters < 1 || a->n_parts < 1 || a->rank < 1) return fail(ctx, GELO_EINVAL, "adapters: n_adapters=%d n_parts=%d rank=%d", a->n_adapters, a->n_parts, a->rank);

@@ -446,7 +446,7 @@ hipError_t attention_fp4(const Attention& o, int is_bf16, hipStream_t stream);
 hipError_t attention_fp4_init();
 
 // adapt.hip: see gelo_adapt.  Parts of the columns end at part_end[0 ... n_parts - 1], multiples of 16 but for the last; ranks are multiples of 8.
-constexpr int kMostParts = 4;
+constexpr int kMostParts = 4, kMostRank = 128;
 struct Adapt {
     const void* H; int64_t ldh;
     const void* base; int64_t ldb;
