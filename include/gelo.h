@@ -340,8 +340,8 @@ gelo_status gelo_rope_append(gelo_ctx* ctx, gelo_dtype dtype, int n_q_heads, con
  * bits for the product with V; a call where max_rows times the query heads of a key head is more than 16 may round them to bfloat16, in their sum too.  What lies in
  * cache rows that no query of the batch sees does not reach the result, NaN and infinity included.
  * Where the rows and heads are too few to fill the chip the cache's length is cut over workgroups and their parts are joined through float
- * workspace of the context (gelo_reserve_attention sizes it ahead; else the first call that needs more allocates, and what it replaces stays until the context
- * ends): calls on one context must not overlap in time on different streams. */
+ * workspace of the context (gelo_reserve_attention sizes it ahead; else the first call that needs more allocates): calls on one context must not
+ * overlap in time on different streams. */
 gelo_status gelo_attention(gelo_ctx* ctx, gelo_dtype dtype, int n_q_heads, const void* Q, int64_t ldq, const gelo_kv_cache* cache,
                            const gelo_seq_batch* batch, float scale, int causal, void* O, int64_t ldo, void* stream);
 /* Allocates that workspace (as much as any batch of heads of this width needs): gelo_attention then allocates nothing. */
@@ -381,7 +381,8 @@ gelo_status gelo_cache_rows_fp4(gelo_ctx* ctx, gelo_dtype dtype, const gelo_kv_c
                                 void* K, int64_t ldk, void* V, int64_t ldv, void* stream);
 
 /* gelo_attention over such a cache; everything said there holds, for keys and values as they are held.  They are multiplied exactly; GELO_F32 has queries
- * and weights in full.  Weights are relative to a maximum that may lag up to 2^8 behind: sums of values beyond 2^100 can overflow. */
+ * and weights in full.  Weights are relative to a maximum that may lag up to 2^8 behind: sums of values beyond 2^100 can overflow.
+ * The workspace that such a call has used stays until the context ends, also where a later call needs a larger one: a captured call has its address. */
 gelo_status gelo_attention_fp4(gelo_ctx* ctx, gelo_dtype dtype, int n_q_heads, const void* Q, int64_t ldq, const gelo_kv_cache_fp4* cache,
                                const gelo_seq_batch* batch, float scale, int causal, void* O, int64_t ldo, void* stream);
 

@@ -101,6 +101,7 @@ struct gelo_ctx {
     void* chain_ws;  size_t chain_ws_bytes;
     void* quant_ws;  size_t quant_ws_bytes;    // FP8 projection: codes and row scales of the current U
     void* attention_ws; size_t attention_ws_bytes; // parts of a cut cache
+    bool attention_ws_kept;                        // where it lies is in calls that may have been captured: see grow_attention
     void* adapt_ws; size_t adapt_ws_bytes;         // the first products of adapters
     void* outgrown[80]; int n_outgrown;            // smaller ones of these two that captured calls may still name: each at least twice the one before
     void* project_ws; size_t project_ws_bytes; // bf16 projection of at most 128 rows: float partial sums of the K slices
@@ -414,7 +415,7 @@ gelo_status gelo_create(gelo_ctx** out, int device, uint64_t seed, int allow_bat
     ctx->factor_ws_refused = SIZE_MAX;
     ctx->quant_ws = nullptr; ctx->quant_ws_bytes = 0;
     ctx->project_ws = nullptr; ctx->project_ws_bytes = 0;
-    ctx->attention_ws = nullptr; ctx->attention_ws_bytes = 0;
+    ctx->attention_ws = nullptr; ctx->attention_ws_bytes = 0; ctx->attention_ws_kept = false;
     ctx->adapt_ws = nullptr; ctx->adapt_ws_bytes = 0; ctx->n_outgrown = 0;
     ctx->host_scalars = nullptr; ctx->host_flag = nullptr;
     ctx->lanes_ready = false; ctx->join_pending = false; ctx->cand = nullptr; ctx->cand_bytes = 0;
@@ -1658,6 +1659,15 @@ static gelo_status grow_kept(gelo_ctx* ctx, void** buf, size_t* have, size_t nee
     return GELO_OK;
 }
 
+// Attention's: kept once gelo_attention_fp4 has used it.
+static gelo_status grow_attention(gelo_ctx* ctx, size_t need) {
+    if (ctx->attention_ws_bytes >= need) return GELO_OK;
+    if (!ctx->attention_ws_kept) return grow(ctx, &ctx->attention_ws, &ctx->attention_ws_bytes, need);
+    const gelo_status st = grow_kept(ctx, &ctx->attention_ws, &ctx->attention_ws_bytes, need);
+    if (st == GELO_OK) ctx->attention_ws_kept = false;       // (the new one)
+    return st;
+}
+
 static gelo_status too_many_for_a_launch(gelo_ctx* ctx, const gelo_seq_batch* batch, int n_q_heads) {
     return fail(ctx, GELO_ESHAPE, "%d sequences of up to %d rows and %d heads are too many for one launch", batch->n_seqs, batch->max_rows, n_q_heads);
 }
@@ -1673,7 +1683,7 @@ gelo_status gelo_attention(gelo_ctx* ctx, gelo_dtype dtype, int n_q_heads, const
     if (!attention_fits(o, dtype == GELO_BF16)) return too_many_for_a_launch(ctx, batch, n_q_heads);
     GELO_HIP(ctx, hipSetDevice(ctx->device));
     const size_t need = attention_workspace_bytes(o, dtype == GELO_BF16);
-    if (need > 0) st = grow_kept(ctx, &ctx->attention_ws, &ctx->attention_ws_bytes, need);
+    if (need > 0) st = grow_attention(ctx, need);
     if (st != GELO_OK) return st;
     o.workspace = (float*)ctx->attention_ws;
     GELO_HIP(ctx, attention(o, dtype == GELO_BF16, (hipStream_t)stream));
@@ -1691,9 +1701,10 @@ gelo_status gelo_attention_fp4(gelo_ctx* ctx, gelo_dtype dtype, int n_q_heads, c
     if (!attention_fp4_fits(o, dtype == GELO_BF16)) return too_many_for_a_launch(ctx, batch, n_q_heads);
     GELO_HIP(ctx, hipSetDevice(ctx->device));
     const size_t need = attention_fp4_workspace_bytes(o, dtype == GELO_BF16);
-    if (need > 0) st = grow_kept(ctx, &ctx->attention_ws, &ctx->attention_ws_bytes, need);
+    if (need > 0) st = grow_attention(ctx, need);
     if (st != GELO_OK) return st;
     o.workspace = (float*)ctx->attention_ws;
+    if (need > 0) ctx->attention_ws_kept = true;
     GELO_HIP(ctx, attention_fp4(o, dtype == GELO_BF16, (hipStream_t)stream));
     return GELO_OK;
 }
@@ -1702,7 +1713,7 @@ gelo_status gelo_reserve_attention(gelo_ctx* ctx, int head_dim) {
     if (!ctx) return GELO_EINVAL;
     if (head_dim != 64 && head_dim != 96 && head_dim != 128 && head_dim != 256) return fail(ctx, GELO_ESHAPE, "head_dim=%d is none of 64, 96, 128, 256", head_dim);
     GELO_HIP(ctx, hipSetDevice(ctx->device));
-    return grow_kept(ctx, &ctx->attention_ws, &ctx->attention_ws_bytes, attention_workspace_bound(head_dim));
+    return grow_attention(ctx, attention_workspace_bound(head_dim));
 }
 
 static_assert(kMostParts == GELO_ADAPT_MAX_PARTS && kMostRank == GELO_ADAPT_MAX_RANK, "");
