@@ -656,16 +656,17 @@ int steps_of(int is_bf16, int d) { return (d + (is_bf16 ? 31 : 15)) / (is_bf16 ?
 // rows.  4096 -> 12288 columns, rank 16, one adapter, us by rows and by groups: 64 rows 10.9 and 16.2, 96 (75 MB) 16.5 and 16.4, 128 18.2 and 16.4, 256 28.2 and 17.4; 4096 ->
 // 4096, rank 128, 64 rows (134 MB) 22.4 and 20.9; 1024 -> 1024, rank 8, 1024 rows (34 MB) 10.9 and 19.3.
 constexpr double kRowsRead = 80e6, kOrderedRead = 110e6;
-// Putting rows in order is a launch of 4 to 6 us, and what follows finds its rows a trip later.  Without it a group's adapters follow each other.  Of that kind, us in order and as
-// they come: 1024 rows of eight adapters in any order 34.5 and 50, of four 36.9 as they come, 4096 rows of eight in any order 67 and 92, in runs 67 and 57.5; so many rows are
-// prompts, whose rows lie side by side, more often than not.
-int few_adapters(int n) { return n >= 2048 ? 8 : 4; }
+// Putting rows in order is a launch of 4 to 6 us, and what follows finds its rows a trip later.  Without it a group's adapters follow each other, each a trip to its B and so many more
+// instructions.  4096 -> 12288 columns, rank 16, us in order and as they come: 1024 rows of eight adapters in any order 29 and 44, of four 31 as they come; 4096 rows of eight in any
+// order 67 and 92, in runs 67 and 57.  So many rows are prompts, whose rows lie side by side, more often than not - but at high ranks a wrong guess costs more: 4096 rows of 2048 values, 2048
+// columns, eight adapters of rank 64 in any order 33 and 63, in runs 33 and 25, of rank 128 43 and 101, 43 and 35.
+int few_adapters(int n, int rank) { return n >= 2048 && rank <= 32 ? 8 : 4; }
 struct Plan { bool many, ordered, by_die; int splits, steps, wide; int64_t most_groups, t_bytes, bytes; };
 Plan plan_of(int is_bf16, int n, int d, int p, int rank, int n_parts, int n_adapters) {
     Plan r;
     const double read = (double)n * rank * ((double)n_parts * d + p) * (is_bf16 ? 2 : 4);
-    r.many = n_adapters < kMostBins && read > (n_adapters > few_adapters(n) ? kOrderedRead : kRowsRead);
-    r.ordered = r.many && n_adapters > few_adapters(n);
+    r.many = n_adapters < kMostBins && read > (n_adapters > few_adapters(n, rank) ? kOrderedRead : kRowsRead);
+    r.ordered = r.many && n_adapters > few_adapters(n, rank);
     const int all = steps_of(is_bf16, d), rank_groups = (rank * n_parts + 63) / 64;
     const int64_t alone = n_adapters < n ? n_adapters + 1 : n;          // groups that are not full
     r.most_groups = round_up(r.ordered ? n / kGroup + alone : r.many ? (n + kGroup - 1) / kGroup : 0, 8);

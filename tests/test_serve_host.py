@@ -179,5 +179,5 @@ def test_which_way_adapters_go():
     way = ctypes.CDLL(g.LIB_PATH)["_ZN4gelo9adapt_wayEiiiiiii"]
     for want, args in ((0, (1, 64, 4096, 12288, 16, 3, 48)), (0, (1, 96, 4096, 12288, 16, 3, 1)), (1, (1, 128, 4096, 12288, 16, 3, 1)), (0, (1, 128, 4096, 12288, 16, 3, 64)),
                        (2, (1, 192, 4096, 12288, 16, 3, 64)), (1, (1, 64, 4096, 4096, 128, 1, 1)), (0, (1, 1024, 1024, 1024, 8, 1, 4)), (2, (1, 1024, 4096, 12288, 16, 3, 8)),
-                       (1, (1, 4096, 4096, 12288, 16, 3, 8)), (2, (1, 4096, 4096, 12288, 16, 3, 9)), (0, (1, 4096, 4096, 12288, 16, 3, 12288))):
+                       (1, (1, 4096, 4096, 12288, 16, 3, 8)), (2, (1, 4096, 2048, 2048, 64, 1, 8)), (1, (1, 4096, 2048, 2048, 64, 1, 4)), (2, (1, 4096, 4096, 12288, 16, 3, 9)), (0, (1, 4096, 4096, 12288, 16, 3, 12288))):
         assert way(*args) == want, args
