@@ -4,7 +4,7 @@
 // T = H A_w^T for all parts, in float, d cut over workgroups whose sums lie side by side; then base + scale T B_w^T.  Bound by the bytes of H, base, Z and the
 // adapters.
 //   few rows   two launches.  The first takes tiles of 16 rows as they come; a tile's adapters go side by side, rows of others count as zeros and their results are
-//              dropped.  The second takes row by row.
+//              dropped.  The second takes row by row; of small rows it does both.
 //   many rows  three: the first puts the rows of an adapter together, 64 to a group (rows that are so already stay in runs); then a tile is a group.
 // A row's sums do not go by the rows around it: each is a column of a matrix instruction.
 //
@@ -212,10 +212,12 @@ template <class T> __device__ __forceinline__ Rank rank_of(int rank, int s, int 
 // Few rows, the second product, as sums of products: a row has its adapter to itself as a rule, and a matrix instruction would multiply 15 rows of zeros.  A
 // workgroup: one row, kFewCols columns of one part.  Bound by its trips to memory - whose row, T and B, base: 64 rows with 48 adapters, 12288 columns, rank 16, 17 MB in
 // 5.5 us (tiles of matrix instructions 10).  A column's rank values lie side by side: from 64 bytes on LANES = 4 lanes take 16 each, of 8 columns (by a lane alone, two columns: both products of
-// 40 rows of 11760 columns, rank 64, 19.8 us, 14.5; of 32 of 12288 21.6, 17.6); fewer belong to one lane (64 rows, rank 16, 11.2 us, 14.9 by four).
+// 40 rows of 11760 columns, rank 64, 19.8 us, 13.7; of 32 of 12288 21.6, 16.9); fewer belong to one lane (64 rows, rank 16, 11.2 us, 14.9 by four).
 constexpr int kFewCols = 512;
-template <class T, int LANES>
-__global__ __launch_bounds__(256)
+// WHOLE: the first product too, in the same launch, by every workgroup for itself: a wave has a quarter of the ranks, its lanes the row's values.
+constexpr int kWholeRank = 32;
+template <class T, int LANES, bool WHOLE>
+__global__ __launch_bounds__(256, WHOLE ? 4 : 1)
 void adapt_few_up_kernel(AdaptArgs a) {
     const Adapt& o = a.o;
     __shared__ __attribute__((aligned(16))) float t[kMostRank], sums[kFewCols];          // the row's T, and what it adds
@@ -231,26 +233,56 @@ void adapt_few_up_kernel(AdaptArgs a) {
         constexpr int PER = 16 / sizeof(T), SLOTS = 256 / LANES, COLS = kFewCols / SLOTS;
         const int q = threadIdx.x % LANES, slot = threadIdx.x / LANES, pieces = o.rank / PER;
         constexpr int DEEP = LANES == 1 ? 2 : 1, APART = LANES == 1 ? 1 : SLOTS;               // pieces sent for together; from one column of a lane to its next
+        // (columns behind the last one: that one again; what comes of them is not used)
         const int my_first = first + (LANES == 1 ? COLS * slot : slot);
-        const T* B = (const T*)o.B + id * o.b_stride + my_first * o.ldbw;
+        const T* B = (const T*)o.B + id * o.b_stride;
         u32x4_t y[DEEP][COLS];
         auto read = [&](int piece) {
 #pragma unroll
-            for (int u = 0; u < DEEP; ++u)
+            for (int u = 0; u < DEEP; ++u) {
+                if (piece + u >= pieces) break;
 #pragma unroll
-                for (int k = 0; k < COLS; ++k) {
-                    if (LANES > 1) y[u][k] = u32x4_t{0, 0, 0, 0};            // (one lane breaks off instead)
-                    if ((LANES == 1 ? in : my_first + k * APART < end) && piece + u < pieces) y[u][k] = *reinterpret_cast<const u32x4_t*>(B + k * APART * o.ldbw + (piece + u) * PER);
-                }
+                for (int k = 0; k < COLS; ++k) y[u][k] = *reinterpret_cast<const u32x4_t*>(B + min(my_first + k * APART, end - 1) * o.ldbw + (piece + u) * PER);
+            }
         };
         read(q);
-        if (threadIdx.x < kMostRank) {
-            float sum = 0.f;
-            if ((int)threadIdx.x < o.rank) {
-                const float* from = a.t + (int64_t)row * a.all + part * o.rank + threadIdx.x;
-#pragma unroll 8
-                for (int s = 0; s < a.splits; ++s) sum += from[(int64_t)s * o.n * a.all];
+        if constexpr (WHOLE) {
+            constexpr int MINE = kWholeRank / 4;
+            const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mine = o.rank / 4;
+            const T* h = (const T*)o.H + row * o.ldh;
+            const T* A = (const T*)o.A + id * o.a_stride + (part * o.rank + wave * mine) * o.lda;
+            float sum[MINE];
+#pragma unroll
+            for (int r = 0; r < MINE; ++r) sum[r] = 0.f;
+            auto value = [](const u32x4_t& v, int e) {
+                return sizeof(T) == 4 ? __uint_as_float(v[e & 3]) : __uint_as_float(e & 1 ? v[e >> 1] & 0xFFFF0000u : v[e >> 1] << 16);
+            };
+#pragma unroll 2
+            for (int c = PER * lane; c < o.d; c += 64 * PER) {
+                const u32x4_t x = *reinterpret_cast<const u32x4_t*>(h + c);
+                u32x4_t w[MINE];
+#pragma unroll
+                for (int r = 0; r < MINE; ++r)
+                    if (r < mine) w[r] = *reinterpret_cast<const u32x4_t*>(A + r * o.lda + c);
+#pragma unroll
+                for (int r = 0; r < MINE; ++r) {
+                    if (r >= mine) break;
+#pragma unroll
+                    for (int e = 0; e < PER; ++e) sum[r] += value(x, e) * value(w[r], e);
+                }
             }
+#pragma unroll
+            for (int r = 0; r < MINE; ++r) {
+                if (r >= mine) break;
+#pragma unroll
+                for (int by = 1; by < 64; by *= 2) sum[r] += __shfl_xor(sum[r], by, 64);
+                if (lane == 0) t[wave * mine + r] = sum[r];
+            }
+        } else if ((int)threadIdx.x < o.rank) {
+            float sum = 0.f;
+            const float* from = a.t + (int64_t)row * a.all + part * o.rank + threadIdx.x;
+#pragma unroll 8
+            for (int s = 0; s < a.splits; ++s) sum += from[(int64_t)s * o.n * a.all];
             t[threadIdx.x] = sum;
         }
         const float scale = o.scale ? o.scale[id] : 1.f;
@@ -261,10 +293,10 @@ void adapt_few_up_kernel(AdaptArgs a) {
         for (int piece = q; piece - q < pieces; piece += LANES * DEEP) {
 #pragma unroll
             for (int u = 0; u < DEEP; ++u) {
-                if (LANES == 1 && piece + u >= pieces) break;
+                if (piece + u >= pieces) break;
                 float with[PER];
 #pragma unroll
-                for (int e = 0; e < PER; e += 4) *reinterpret_cast<f32x4_t*>(with + e) = *reinterpret_cast<const f32x4_t*>(t + min(piece + u, kMostRank / PER - 1) * PER + e);
+                for (int e = 0; e < PER; e += 4) *reinterpret_cast<f32x4_t*>(with + e) = *reinterpret_cast<const f32x4_t*>(t + (piece + u) * PER + e);
 #pragma unroll
                 for (int k = 0; k < COLS; ++k)
 #pragma unroll
@@ -661,7 +693,7 @@ constexpr double kRowsRead = 80e6, kOrderedRead = 110e6;
 // order 67 and 92, in runs 67 and 57.  So many rows are prompts, whose rows lie side by side, more often than not - but at high ranks a wrong guess costs more: 4096 rows of 2048 values, 2048
 // columns, eight adapters of rank 64 in any order 33 and 63, in runs 33 and 25, of rank 128 43 and 101, 43 and 35.
 int few_adapters(int n, int rank) { return n >= 2048 && rank <= 32 ? 8 : 4; }
-struct Plan { bool many, ordered, by_die; int splits, steps, wide; int64_t most_groups, t_bytes, bytes; };
+struct Plan { bool many, ordered, by_die, whole; int splits, steps, wide; int64_t most_groups, t_bytes, bytes; };
 Plan plan_of(int is_bf16, int n, int d, int p, int rank, int n_parts, int n_adapters) {
     Plan r;
     const double read = (double)n * rank * ((double)n_parts * d + p) * (is_bf16 ? 2 : 4);
@@ -682,6 +714,10 @@ Plan plan_of(int is_bf16, int n, int d, int p, int rank, int n_parts, int n_adap
     // 12288 columns, 768 workgroups, 34.4 and 32.0)
     r.wide = kFewCols;
     if (r.many) for (r.wide = 2 * kUpCols; r.wide > kUpCols && (n + kUpRows - 1) / kUpRows * (int64_t)((p + r.wide - 1) / r.wide) < 512;) r.wide /= 2;
+    // One launch for small rows: every workgroup of the second product reads A once more, a few trips one behind the other.  16 rows, us in two launches and in one: of 256 values, rank 16 6.3
+    // and 4.3; 1024, rank 32 8.1 and 7.1; 2048, rank 16 7.1 and 6.5, rank 32 8.7 and 9.4; 4096, rank 8 6.5 and 7.3; 256 rows of 2048, 67 MB, 9.9 and 8.7.
+    const double row_bytes = (double)d * (is_bf16 ? 2 : 4), reads = rank * row_bytes;
+    r.whole = !r.many && rank <= kWholeRank && row_bytes <= 4096 && reads <= 65536 && reads * n * ((p + kFewCols - 1) / kFewCols + n_parts - 1) <= 70e6;
     // (T goes to 8 dies otherwise: where that is a fifth of base and Z)
     r.by_die = 5 * 8 * r.splits * rank * n_parts * (int64_t)sizeof(float) > 2 * (int64_t)p * (is_bf16 ? 2 : 4);
     r.t_bytes = round_up((int64_t)r.splits * n * rank * n_parts * sizeof(float), 256);
@@ -717,11 +753,13 @@ hipError_t launch(const Adapt& o, hipStream_t stream) {
         return hipGetLastError();
     }
     const int tiles = (o.n + 15) / 16;
-    hipLaunchKernelGGL(adapt_few_down_kernel<T>, dim3(tiles * 16, a.splits, rank_groups), dim3(64 * kWaves), 0, stream, a);
+    if (!p.whole) hipLaunchKernelGGL(adapt_few_down_kernel<T>, dim3(tiles * 16, a.splits, rank_groups), dim3(64 * kWaves), 0, stream, a);
     const dim3 up((unsigned)(blocks * o.n));
     const int pieces = o.rank / (16 / (int)sizeof(T));
-    if (pieces < 4) hipLaunchKernelGGL((adapt_few_up_kernel<T, 1>), up, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((adapt_few_up_kernel<T, 4>), up, dim3(256), 0, stream, a);
+    if (p.whole && pieces < 4) hipLaunchKernelGGL((adapt_few_up_kernel<T, 1, true>), up, dim3(256), 0, stream, a);
+    else if (p.whole) hipLaunchKernelGGL((adapt_few_up_kernel<T, 4, true>), up, dim3(256), 0, stream, a);
+    else if (pieces < 4) hipLaunchKernelGGL((adapt_few_up_kernel<T, 1, false>), up, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((adapt_few_up_kernel<T, 4, false>), up, dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 
@@ -743,7 +781,11 @@ size_t adapt_workspace_bound(int n, int rank, int n_parts, int n_adapters) {
     if (rows < n) rows = n;
     return (size_t)(round_up(rows * rank * n_parts * (int64_t)sizeof(float), 256) + (8 + 4 * kGroup) * round_up(n / kGroup + alone, 8));
 }
-// Which way a call of these sizes goes: 0 rows by themselves, 1 groups of rows as they come, 2 groups of rows put in order.
+// Which way a call of these sizes goes: 0 rows by themselves, 1 groups of rows as they come, 2 groups of rows put in order.  adapt_launches: in so many.
+int adapt_launches(int is_bf16, int n, int d, int p, int rank, int n_parts, int n_adapters) {
+    const Plan r = plan_of(is_bf16, n, d, p, rank, n_parts, n_adapters);
+    return r.whole ? 1 : 2 + r.ordered;
+}
 int adapt_way(int is_bf16, int n, int d, int p, int rank, int n_parts, int n_adapters) {
     const Plan r = plan_of(is_bf16, n, d, p, rank, n_parts, n_adapters);
     return r.many + r.ordered;

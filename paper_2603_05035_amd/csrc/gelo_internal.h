@@ -463,6 +463,7 @@ bool adapt_fits(const Adapt& o, int is_bf16);    // as one launch each
 size_t adapt_workspace_bytes(const Adapt& o, int is_bf16);
 size_t adapt_workspace_bound(int n, int rank, int n_parts, int n_adapters);
 int adapt_way(int is_bf16, int n, int d, int p, int rank, int n_parts, int n_adapters);
+int adapt_launches(int is_bf16, int n, int d, int p, int rank, int n_parts, int n_adapters);
 size_t adapt_needs(int is_bf16, int n, int d, int p, int rank, int n_parts, int n_adapters);
 hipError_t adapt_init();
 hipError_t adapt(const Adapt& o, int is_bf16, hipStream_t stream);

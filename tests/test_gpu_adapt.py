@@ -161,6 +161,23 @@ def test_numbers_of_rows_at_the_edges_of_tiles(ctx, n, dtype):
     check(ctx, *make(n, 104, (64, 72), 8, 3, dtype, n, 8), [(i // 5) % 4 - 1 for i in range(n)], dtype)
 
 
+WHOLE = [  # n, d, widths of the parts, rank, adapters, launches in bfloat16 and float
+    (5, 1024, (1032,), 8, 3, (1, 1)), (5, 1032, (528, 16, 8), 24, 3, (1, 2)), (7, 2048, (48, 32), 16, 2, (1, 2)), (7, 2056, (48, 32), 16, 2, (2, 2)), (33, 40, (1536,), 32, 9, (1, 1)), (3, 1024, (64, 512), 32, 2, (1, 2)),
+    (9, 8, (16, 24), 32, 3, (1, 1)), (9, 8, (16, 24), 40, 3, (2, 2)), (500, 512, (512, 512, 512), 16, 64, (1, 2)), (700, 72, (528,), 8, 700, (1, 1))]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("gap", [0, 16])
+@pytest.mark.parametrize("n,d,parts,rank,count,launches", WHOLE)
+def test_small_rows_in_one_launch(ctx, n, d, parts, rank, count, launches, gap, dtype):
+    go = ctypes.CDLL(g.LIB_PATH)["_ZN4gelo14adapt_launchesEiiiiiii"]
+    assert go(int(dtype == BF16), n, d, sum(parts), rank, len(parts), count) == launches[dtype == F32]
+    H, base, A, B, scale, ends = make(n, d, parts, rank, count, dtype, 17, gap)
+    ids = np.random.default_rng(4).integers(-1, count + 1, n)
+    check(ctx, H, base, A, B, scale, ends, [int(x) for x in ids], dtype)
+    check(ctx, H, base, A, B, None, ends, [0] * n, dtype)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("n,d,rank,count", [(1, 136, 16, 4), (20, 136, 16, 4), (600, 1400, 104, 4), (600, 1400, 104, 9)])
 def test_without_factors_and_without_any_adapter(ctx, n, d, rank, count, dtype):
@@ -275,10 +292,12 @@ def test_workspace_that_is_outgrown_serves_captured_calls(ctx):
     """A captured call keeps its workspace's address: a larger call later takes another one."""
     c = g.gelo_create(0, 1)
     try:
-        H, base, A, B, scale, ends = make(20, 264, (48, 32), 16, 4, BF16, 5)
+        H, base, A, B, scale, ends = make(20, 2056, (48, 32), 16, 4, BF16, 5)
         adapters = g.Adapters(A, B, scale=scale, part_ends=ends)
         which = torch.tensor([i % 4 for i in range(20)], dtype=torch.int32).cuda()
         Z, Y = torch.empty_like(base), torch.empty_like(base)
+        go = ctypes.CDLL(g.LIB_PATH)["_ZN4gelo14adapt_launchesEiiiiiii"]
+        assert go(1, 20, 2056, 80, 16, 2, 4) == 2            # (a call in one launch has no use for it)
         g.gelo_reserve_adapt(c, 20, 16, 2, 4)
         graph = torch.cuda.CUDAGraph()
         torch.cuda.synchronize()
