@@ -645,17 +645,19 @@ def gelo_reserve_attention(ctx, head_dim: int) -> None:
 
 def gelo_adapt(ctx, H: torch.Tensor, adapters: Adapters, which: torch.Tensor, Z: torch.Tensor, base: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """Z = base + what the adapter of each row adds (base None: Z's own values).  which: int32, the adapter of every row; a number that is none's: base alone."""
-    if base is None:
-        base = Z
-    shape, out = H.shape, Z.shape
+    shape, out, dtype = H.shape, Z.shape, adapters.torch_dtype
     hp, ldh = _matrix(H, "H")
-    bp, ldb = _matrix(base, "base")
-    zp, ldz = _matrix(Z, "Z")
-    dtype = adapters.torch_dtype
-    if H.dtype != dtype or Z.dtype != dtype or base.dtype != dtype:
-        raise GeloError(3, "H, base, Z and the adapters differ in type")
-    if shape[1] != adapters.d or out != (shape[0], adapters.p) or base.shape != out:
-        raise GeloError(2, f"H must have rows of {adapters.d} values, base and Z as many of {adapters.p}")
+    zp, ldz = bp, ldb = _matrix(Z, "Z")
+    if base is not None:
+        bp, ldb = _matrix(base, "base")
+        if base.dtype != dtype:
+            raise GeloError(3, "base and the adapters differ in type")
+        if base.shape != out:
+            raise GeloError(2, f"base must be of Z's shape, {tuple(out)}")
+    if H.dtype != dtype or Z.dtype != dtype:
+        raise GeloError(3, "H, Z and the adapters differ in type")
+    if shape[1] != adapters.d or out != (shape[0], adapters.p):
+        raise GeloError(2, f"H must have rows of {adapters.d} values, Z as many of {adapters.p}")
     _vector(which, "which", torch.int32, shape[0])
     status = load_library().gelo_adapt(ctx, adapters.dtype, shape[0], adapters.d, adapters.p, hp, ldh, adapters.address, which.data_ptr(), bp, ldb, zp, ldz,
                                        _stream(stream))

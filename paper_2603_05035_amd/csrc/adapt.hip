@@ -444,7 +444,7 @@ struct Some {
 // Many rows, the first product.  A workgroup: one group, 64 rows of A, one part of d, whose steps its waves share out.  Columns of rows of other adapters come
 // out as they may and are not kept, so the rows are sent for before their adapters are known.  Neighbouring groups go to one die: its L2 then has their A.  A wave's piece of H
 // lies in its registers, that of A in its own part of LDS, put there by loads that need no registers: all of it is one trip to memory (tile after tile of A
-// through registers, a trip each, 2048 rows of 4096 values, rank 64: 12.8 us, 8.9).  (16 rows and all of d to a workgroup: every 16 rows read A for themselves, 4096 rows 26 us instead of 13.
+// through registers, a trip each, 2048 rows of 4096 values, rank 64: 12.8 us, 9.7).  (16 rows and all of d to a workgroup: every 16 rows read A for themselves, 4096 rows 26 us instead of 13.
 // Half as many waves: twice the parts of d, which the second product reads once for each of its workgroups, 60 instead of 57.5 for both.)
 constexpr int kDownWaves = 8, kDownWaveLds = 16 * 1024;
 template <class T>
