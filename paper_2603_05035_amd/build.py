@@ -44,14 +44,14 @@ def build_sanitized(verbose: bool = False) -> str:
     """Host-side sanitizer target: api.hip's HOST code (argument checks, context and mixing-object life cycle)
     compiled with AddressSanitizer + UndefinedBehaviorSanitizer, linked with the other, uninstrumented objects of
     `build()` into libgelo_hostsan.so, plus the drivers of tests/host_sanitize/, lifecycle.cpp -> lifecycle_hostsan, layer.cpp ->
-    layer_hostsan and serve.cpp -> serve_hostsan (all beside libgelo.so).
+    layer_hostsan, serve.cpp -> serve_hostsan and serve_limits.cpp -> serve_limits_hostsan (all beside libgelo.so).
     The GPU code is not instrumented.  Call build() first."""
     obj_dir = os.path.join(HERE, "_build")
     root = os.path.dirname(HERE)
     san = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined", "-Xarch_host", "-fno-omit-frame-pointer", "-g"]
     api_obj = os.path.join(obj_dir, "api_hostsan.o")
     lib = os.path.join(HERE, "libgelo_hostsan.so")           # beside libgelo.so, where the host-side tests look for it
-    exes = [os.path.join(HERE, f"{name}_hostsan") for name in ("lifecycle", "layer", "serve")]
+    exes = [os.path.join(HERE, f"{name}_hostsan") for name in ("lifecycle", "layer", "serve", "serve_limits")]
     cmds = [
         [HIPCC, *FLAGS, *san, "-c", os.path.join(CSRC, "api.hip"), "-o", api_obj],
         [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-fsanitize=address", "-fsanitize=undefined", "-fno-gpu-sanitize", api_obj,

@@ -700,10 +700,11 @@ Plan plan_of(int is_bf16, int n, int d, int p, int rank, int n_parts, int n_adap
     r.many = n_adapters < kMostBins && read > (n_adapters > few_adapters(n, rank) ? kOrderedRead : kRowsRead);
     r.ordered = r.many && n_adapters > few_adapters(n, rank);
     const int all = steps_of(is_bf16, d), rank_groups = (rank * n_parts + 63) / 64;
+    const int64_t rows = n, groups = (rows + kGroup - 1) / kGroup;      // (what is added to n may leave 32 bits; adapt_fits refuses such calls, from what is reckoned here)
     const int64_t alone = n_adapters < n ? n_adapters + 1 : n;          // groups that are not full
-    r.most_groups = round_up(r.ordered ? n / kGroup + alone : r.many ? (n + kGroup - 1) / kGroup : 0, 8);
+    r.most_groups = round_up(r.ordered ? rows / kGroup + alone : r.many ? groups : 0, 8);
     // workgroups that fill the chip with the first product, of 8 waves or (few rows, which have an adapter each as a rule) 4; two steps to a wave at least, or four
-    const int64_t items = (r.many ? (n + kGroup - 1) / kGroup : n) * (int64_t)rank_groups, target = r.many ? 256 : 512;
+    const int64_t items = (r.many ? groups : rows) * rank_groups, target = r.many ? 256 : 512;
     int64_t cuts = items >= target ? 1 : target / items;
     const int to_each = r.many ? 2 * kDownWaves : 4 * kWaves, most = (all + to_each - 1) / to_each;
     cuts = cuts < most ? cuts : most;
@@ -713,7 +714,7 @@ Plan plan_of(int is_bf16, int n, int d, int p, int rank, int n_parts, int n_adap
     // two blocks of columns to a workgroup of the second product where that leaves 512 of them: it reads T once (4096 rows, us: 62 with one, 57.5, 61 with four; 1024 rows of
     // 12288 columns, 768 workgroups, 34.4 and 32.0)
     r.wide = kFewCols;
-    if (r.many) for (r.wide = 2 * kUpCols; r.wide > kUpCols && (n + kUpRows - 1) / kUpRows * (int64_t)((p + r.wide - 1) / r.wide) < 512;) r.wide /= 2;
+    if (r.many) for (r.wide = 2 * kUpCols; r.wide > kUpCols && (rows + kUpRows - 1) / kUpRows * ((p + r.wide - 1) / r.wide) < 512;) r.wide /= 2;
     // One launch for small rows: every workgroup of the second product reads A once more, a few trips one behind the other.  16 rows, us in two launches and in one: of 256 values, rank 16 6.3
     // and 4.3; 1024, rank 32 8.1 and 7.1; 2048, rank 16 7.1 and 6.5, rank 32 8.7 and 9.4; 4096, rank 8 6.5 and 7.3; 256 rows of 2048, 67 MB, 9.9 and 8.7.
     const double row_bytes = (double)d * (is_bf16 ? 2 : 4), reads = rank * row_bytes;
@@ -769,7 +770,7 @@ bool adapt_fits(const Adapt& o, int is_bf16) {
     const Plan p = plan_of(is_bf16, o.n, o.d, o.p, o.rank, o.n_parts, o.n_adapters);
     const int64_t blocks = o.p / p.wide + o.n_parts, most = kMostThreads / (64 * kWaves), rank_groups = (o.rank * o.n_parts + 63) / 64;
     if (p.many) return kGroup / kUpRows * p.most_groups * blocks <= most && 2 * p.most_groups * p.splits * rank_groups <= most;
-    const int64_t tiles = (o.n + 15) / 16;
+    const int64_t tiles = ((int64_t)o.n + 15) / 16;
     return o.n * blocks <= most && 16 * tiles * p.splits * rank_groups <= most;
 }
 

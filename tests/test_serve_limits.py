@@ -1,0 +1,34 @@
+"""Adapters and the cache of 4 bits at the ends of what a call may say: what the library reckons on the host.  Nothing here launches a kernel or needs a GPU."""
+import subprocess
+import sys
+
+import pytest
+
+from paper_2603_05035_amd import binding as g
+
+ROWS = """
+import ctypes, sys
+lib = ctypes.CDLL(sys.argv[1])
+way, needs, fits = lib["_ZN4gelo9adapt_wayEiiiiiii"], lib["_ZN4gelo11adapt_needsEiiiiiii"], lib["_ZN4gelo10adapt_fitsERKNS_5AdaptEi"]
+needs.restype, fits.restype = ctypes.c_size_t, ctypes.c_bool
+P, I, L = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64
+class Adapt(ctypes.Structure):
+    _fields_ = [("H", P), ("ldh", L), ("base", P), ("ldb", L), ("Z", P), ("ldz", L), ("A", P), ("a_stride", L), ("lda", L), ("B", P), ("b_stride", L), ("ldbw", L),
+                ("scale", P), ("which", P), ("n", I), ("d", I), ("p", I), ("rank", I), ("n_parts", I), ("n_adapters", I), ("part_end", I * 4), ("workspace", P)]
+adapters, d, p = (int(x) for x in sys.argv[2:])
+for n in (2 ** 31 - 1, 2 ** 31 - 15, 2 ** 31 - 31, 2 ** 31 - 32, 2 ** 31 - 62, 2 ** 31 - 63, 2 ** 31 - 64, 2 ** 30, 2 ** 28 + 1):
+    for bf16 in (0, 1):
+        o = Adapt(n=n, d=d, p=p, rank=16, n_parts=1, n_adapters=adapters)
+        assert not fits(ctypes.byref(o), bf16), n            # refused
+        assert way(bf16, n, d, p, 16, 1, adapters) in (0, 1, 2)
+        assert needs(bf16, n, d, p, 16, 1, adapters) >= n * 16 * 4
+assert fits(ctypes.byref(Adapt(n=4096, d=d, p=p, rank=16, n_parts=1, n_adapters=adapters)), 1)
+"""
+
+
+@pytest.mark.parametrize("adapters", [1, 20, 12287, 12288, 2 ** 31 - 1])
+@pytest.mark.parametrize("d,p", [(4096, 4096), (8, 8)])
+def test_numbers_of_rows_at_the_end_of_32_bits(adapters, d, p):
+    """No launch has so many rows: they are refused, by sums that stay what they are.  (In a process of its own: a division by zero would end it.)"""
+    r = subprocess.run([sys.executable, "-c", ROWS, g.LIB_PATH, str(adapters), str(d), str(p)], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=120)
+    assert r.returncode == 0, (r.returncode, r.stdout[-2000:])
