@@ -422,6 +422,12 @@ class KvCacheFp4:
         self.address = ctypes.addressof(self.struct)
 
 
+def _of_4_bits(cache) -> None:
+    """A cache of values has the same fields in front, so the library would take its strides for bytes."""
+    if not isinstance(cache, KvCacheFp4):
+        raise TypeError(f"cache must be a KvCacheFp4, not a {type(cache).__name__}")
+
+
 class Adapters:
     """Low-rank adapters beside one projection (see gelo_adapters in include/gelo.h): A (adapters, parts x rank, width of H), B (adapters, columns of Z, rank),
     rows contiguous; scale: a float32 factor to each, or None; part_ends: the columns where the parts of a fused projection end (None: one part).  Describes the
@@ -561,6 +567,7 @@ def gelo_rope_append(ctx, QKV: torch.Tensor, n_q_heads: int, cache: KvCache, bat
 def gelo_rope_append_fp4(ctx, QKV: torch.Tensor, n_q_heads: int, cache: KvCacheFp4, batch: SeqBatch, Q: torch.Tensor | None = None,
                          table: torch.Tensor | None = None, rot_dim: int = 0, layout: int = GELO_ROPE_HALF, stream=None):
     """gelo_rope_append into a cache of 4 bits."""
+    _of_4_bits(cache)
     zp, ld = _matrix(QKV, "QKV")
     rows, width = QKV.shape
     if width != (n_q_heads + 2 * cache.n_kv_heads) * cache.head_dim:
@@ -585,6 +592,7 @@ def gelo_rope_append_fp4(ctx, QKV: torch.Tensor, n_q_heads: int, cache: KvCacheF
 
 def gelo_cache_rows_fp4(ctx, cache: KvCacheFp4, batch: SeqBatch, K: torch.Tensor | None = None, V: torch.Tensor | None = None, stream=None):
     """The values that the batch's rows are held as, a row of all key heads to each, into K and V (either may be None)."""
+    _of_4_bits(cache)
     some = V if K is None else K
     if some is None:
         raise ValueError("K and V are both None: nothing to write")
@@ -625,6 +633,7 @@ def gelo_attention(ctx, Q: torch.Tensor, O: torch.Tensor, n_q_heads: int, cache:
 def gelo_attention_fp4(ctx, Q: torch.Tensor, O: torch.Tensor, n_q_heads: int, cache: KvCacheFp4, batch: SeqBatch, scale: float, causal: bool = True,
                        stream=None) -> torch.Tensor:
     """gelo_attention over a cache of 4 bits."""
+    _of_4_bits(cache)
     qp, ldq = _matrix(Q, "Q")
     op, ldo = _matrix(O, "O")
     shape = Q.shape

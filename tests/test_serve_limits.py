@@ -3,6 +3,7 @@ import subprocess
 import sys
 
 import pytest
+import torch
 
 from paper_2603_05035_amd import binding as g
 
@@ -32,3 +33,36 @@ def test_numbers_of_rows_at_the_end_of_32_bits(adapters, d, p):
     """No launch has so many rows: they are refused, by sums that stay what they are.  (In a process of its own: a division by zero would end it.)"""
     r = subprocess.run([sys.executable, "-c", ROWS, g.LIB_PATH, str(adapters), str(d), str(p)], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=120)
     assert r.returncode == 0, (r.returncode, r.stdout[-2000:])
+
+
+class OnGpu(torch.Tensor):
+    """A host tensor that says it lives on the GPU: for code that looks at shapes and strides only."""
+
+    @property
+    def is_cuda(self):
+        return True
+
+
+def zeros(*shape, dtype=torch.bfloat16):
+    return torch.zeros(shape, dtype=dtype).as_subclass(OnGpu)
+
+
+@pytest.mark.parametrize("call", ["append", "rows", "attention"])
+def test_a_cache_of_values_is_not_one_of_4_bits(call, monkeypatch):
+    """Nothing reaches the library: with the address of the other kind's structure it would write codes over values."""
+    def load():
+        raise AssertionError("reached the library")
+    piece = g.gelo_fp4_page_bytes(16, 64)
+    pool, bytes_ = zeros(8, 2, 16, 64), zeros(8, 2, piece, dtype=torch.uint8)
+    values, codes = g.KvCache(pool, pool.clone()), g.KvCacheFp4(bytes_, bytes_.clone(), 16, 64)
+    batch = g.SeqBatch(zeros(3, dtype=torch.int32), zeros(3, 2, dtype=torch.int32), 32)
+    Q, QKV, K = zeros(3, 256), zeros(3, 512), zeros(3, 128)
+    run = {"append": lambda cache: g.gelo_rope_append_fp4(None, QKV, 4, cache, batch, Q=Q, stream=0),
+           "rows": lambda cache: g.gelo_cache_rows_fp4(None, cache, batch, K, stream=0),
+           "attention": lambda cache: g.gelo_attention_fp4(None, Q, zeros(3, 256), 4, cache, batch, 1.0, stream=0)}[call]
+    monkeypatch.setattr(g, "load_library", load)
+    for cache in (values, None, bytes_):
+        with pytest.raises(TypeError):
+            run(cache)
+    with pytest.raises(AssertionError):                      # the right kind does
+        run(codes)
