@@ -1,7 +1,7 @@
 // Low-rank adapters of many requests beside one projection: Z[i] = base[i] + scale_w (H[i] A_w^T) B_w^T, w = which[i] the adapter of row i.  Parts of the
 // columns (the queries, keys and values of a fused projection) have an A each: rows k rank ... (k + 1) rank - 1 of A_w belong to part k.
 //
-// T = H A_w^T for all parts, in float, d cut over workgroups whose sums lie side by side; then base + scale T B_w^T.  Bound by the bytes of H, base, Z and the
+// T = H A_w^T for all parts, in float, d cut over workgroups whose sums lie side by side; then base + scale (T B_w^T).  Bound by the bytes of H, base, Z and the
 // adapters.
 //   few rows   two launches.  The first takes tiles of 16 rows as they come; a tile's adapters go side by side, rows of others count as zeros and their results are
 //              dropped.  The second takes row by row; of small rows it does both.
@@ -145,9 +145,9 @@ void adapt_few_down_kernel(AdaptArgs a) {
     }
 }
 
-// A row's PER values of T from `t` on, summed over the parts of d and scaled
+// A row's PER values of T from `t` on, summed over the parts of d
 template <class T>
-__device__ __forceinline__ void read_t(const AdaptArgs& a, const float* t, float scale, float (&v)[Lane<T>::PER]) {
+__device__ __forceinline__ void read_t(const AdaptArgs& a, const float* t, float (&v)[Lane<T>::PER]) {
     constexpr int PER = Lane<T>::PER;
 #pragma unroll
     for (int e = 0; e < PER; ++e) v[e] = 0.f;
@@ -160,8 +160,6 @@ __device__ __forceinline__ void read_t(const AdaptArgs& a, const float* t, float
             for (int u = 0; u < 4; ++u) v[e + u] += x[u];
         }
     }
-#pragma unroll
-    for (int e = 0; e < PER; ++e) v[e] *= scale;
 }
 // as an operand: of bfloat16 the upper part, or (rest) what it leaves, of the same sign and not zero: an infinity in B would be NaN by a zero
 __device__ __forceinline__ bf16x8_t piece_of(const float (&v)[8], bool rest) {
@@ -176,21 +174,21 @@ __device__ __forceinline__ bf16x8_t piece_of(const float (&v)[8], bool rest) {
 }
 __device__ __forceinline__ f32x4_t piece_of(const float (&v)[4], bool) { return f32x4_t{v[0], v[1], v[2], v[3]}; }
 
-// 16 bytes of Z: base's and what lies at `more`, rounded once
-__device__ __forceinline__ void add_to(u32x4_t& x, const float* more, uint16_t) {
+// 16 bytes of Z: base's and `by` times what lies at `more`, rounded once
+__device__ __forceinline__ void add_to(u32x4_t& x, float by, const float* more, uint16_t) {
     typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
     const f32x4_t a = *reinterpret_cast<const f32x4_t*>(more), b = *reinterpret_cast<const f32x4_t*>(more + 4);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float m0 = i < 2 ? a[2 * i] : b[2 * i - 4], m1 = i < 2 ? a[2 * i + 1] : b[2 * i - 3];
-        const bf16x2_t pair = {(__bf16)(__uint_as_float(x[i] << 16) + m0), (__bf16)(__uint_as_float(x[i] & 0xFFFF0000u) + m1)};
+        const bf16x2_t pair = {(__bf16)(__uint_as_float(x[i] << 16) + by * m0), (__bf16)(__uint_as_float(x[i] & 0xFFFF0000u) + by * m1)};
         x[i] = __builtin_bit_cast(uint32_t, pair);
     }
 }
-__device__ __forceinline__ void add_to(u32x4_t& x, const float* more, float) {
+__device__ __forceinline__ void add_to(u32x4_t& x, float by, const float* more, float) {
     const f32x4_t a = *reinterpret_cast<const f32x4_t*>(more);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) + a[i]);
+    for (int i = 0; i < 4; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) + by * a[i]);
 }
 
 // Rank values go by pieces of PER; of bfloat16 every one comes twice, its upper parts and the rests.  Ranks of up to 16 put both into one instruction.
@@ -586,15 +584,17 @@ void adapt_many_up_kernel(AdaptArgs a) {
     read(first);
     rows.look(a);
     const uint64_t with = rows.left;                         // rows that have an adapter
+    // a row's factor, for its sums as a whole: T times one could leave float's range where the sums do not (T times it, eight values to a thread, was 1 to 3% less time)
+    const float factor = rows.id >= 0 && o.scale ? o.scale[rows.id] : 1.f;
     // one row's PER rank values to a thread, those of a row side by side (what a row without an adapter has there is not used)
     const int slots = 4 * half;                              // pieces, and nothing to fill a step up with
     for (int e = threadIdx.x; e < kUpRows * slots; e += THREADS) {
         const int i = e / slots, q = e - i * slots, to = i & 15;
-        const int row = __shfl(rows.row, i, 64), w = __shfl(rows.id, i, 64);
+        const int row = __shfl(rows.row, i, 64);
         float v[PER];
 #pragma unroll
         for (int k = 0; k < PER; ++k) v[k] = 0.f;
-        if (q < pieces) read_t<T>(a, a.t + (int64_t)row * a.all + part * o.rank + q * PER, w >= 0 && o.scale ? o.scale[w] : 1.f, v);
+        if (q < pieces) read_t<T>(a, a.t + (int64_t)row * a.all + part * o.rank + q * PER, v);
         if constexpr (sizeof(T) == 4) {
             z[q >> 2][i >> 4][16 * (q & 3) + to] = piece_of(v, false);
         } else if (pieces <= 2) {
@@ -675,8 +675,9 @@ void adapt_many_up_kernel(AdaptArgs a) {
             const int e = threadIdx.x + k * THREADS, i = e / TO_ROW, col = at + VEC * (e - i * TO_ROW);
             const int64_t row = __shfl(rows.row, i, 64);
             const bool has = (with >> i) & 1;
+            const float by = __shfl(factor, i, 64);
             if (col >= end || i >= rows.count || (!has && in_place)) continue;
-            if (has) add_to(was[k], &sums[i][col - at], T());
+            if (has) add_to(was[k], by, &sums[i][col - at], T());
             *reinterpret_cast<u32x4_t*>((T*)o.Z + row * o.ldz + col) = was[k];
         }
     }

@@ -250,6 +250,43 @@ def test_an_infinite_weight_has_the_sign_of_what_it_meets(ctx, n, d, rank, count
     assert torch.isfinite(mine).all() and torch.isfinite(Z[ids != 1].float()).all()
 
 
+FACTORS = [(9, 64, 8, 4, 0), (40, 136, 64, 4, 0), (700, 1400, 48, 4, 1), (700, 1400, 64, 9, 2)]          # n, d, rank, adapters, way
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,d,rank,count,want", FACTORS)
+@pytest.mark.parametrize("inner,outer,factor", [(1e12, 1e-30, 1e27), (1e-20, 1e28, 1e-25)])
+def test_factors_that_the_inner_sum_could_not_take(ctx, inner, outer, factor, n, d, rank, count, want, dtype):
+    """A factor multiplies the sum over the ranks: inner sums of 1e12 times 1e27 leave float's range upwards, of 1e-20 times 1e-25 downwards, the sums of their products with B and what
+    these are times the factor (1e9, 1e-17) stay far inside."""
+    H, base, A, B, scale, ends = make(n, d, (48, 32), rank, count, dtype, 11)
+    assert way(n, d, 80, rank, 2, count, dtype) == want
+    A.mul_(inner), B.mul_(outer), scale.mul_(factor)
+    if factor < 1:
+        base.zero_()
+    check(ctx, H, base, A, B, scale, ends, [i % (count + 1) - 1 for i in range(n)], dtype, range(0, n, max(1, n // 60)))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,d,rank,count,want", FACTORS)
+def test_an_infinite_factor_has_the_sign_of_the_sum(ctx, n, d, rank, count, want, dtype):
+    """Sums that are off from 0 by more than they can err; everything else keeps its bits."""
+    H, base, A, B, scale, ends = make(n, d, (48, 32), rank, count, dtype, 12)
+    assert way(n, d, 80, rank, 2, count, dtype) == want
+    which = [i % (count + 1) - 1 for i in range(n)]
+    ids = torch.tensor(which, dtype=torch.int32).cuda()
+    clean = g.gelo_adapt(ctx, H, g.Adapters(A, B, scale=scale, part_ends=ends), ids, torch.empty_like(base), base=base)
+    odd = scale.clone()
+    odd[1] = float("inf")
+    Z = g.gelo_adapt(ctx, H, g.Adapters(A, B, scale=odd, part_ends=ends), ids, torch.empty_like(base), base=base)
+    mine = ids == 1
+    assert torch.equal(Z[~mine], clean[~mine])
+    rows = [i for i in range(n) if which[i] == 1][:60]
+    added, size = so.adapt(host(H)[rows], 0 * host(base)[rows], host(A), host(B), [1.0] * count, [1] * len(rows), ends)
+    sure = np.abs(added) > adapt_bound(0 * added, size, d, rank, dtype)
+    assert sure.mean() > 0.9 and np.array_equal(host(Z)[rows][sure], np.sign(added[sure]) * np.inf)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("n,d,rank,count,want", [(33, 264, 16, 6, 0), (600, 1400, 56, 4, 1), (600, 1400, 80, 6, 2)])
 def test_a_row_s_bits_do_not_go_by_the_rows_around_it(ctx, n, d, rank, count, want, dtype):
