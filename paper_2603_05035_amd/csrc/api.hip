@@ -103,7 +103,7 @@ struct gelo_ctx {
     void* attention_ws; size_t attention_ws_bytes; // parts of a cut cache
     bool attention_ws_kept;                        // where it lies is in calls that may have been captured: see grow_attention
     void* adapt_ws; size_t adapt_ws_bytes;         // the first products of adapters
-    void* outgrown[80]; int n_outgrown;            // smaller ones of these two that captured calls may still name: each at least twice the one before
+    std::vector<void*> outgrown;                   // smaller ones of these two that captured calls may still name
     void* project_ws; size_t project_ws_bytes; // bf16 projection of at most 128 rows: float partial sums of the K slices
     float* host_scalars;         // pinned: kappa read-back, one slot per lane
     int* host_flag;
@@ -416,7 +416,7 @@ gelo_status gelo_create(gelo_ctx** out, int device, uint64_t seed, int allow_bat
     ctx->quant_ws = nullptr; ctx->quant_ws_bytes = 0;
     ctx->project_ws = nullptr; ctx->project_ws_bytes = 0;
     ctx->attention_ws = nullptr; ctx->attention_ws_bytes = 0; ctx->attention_ws_kept = false;
-    ctx->adapt_ws = nullptr; ctx->adapt_ws_bytes = 0; ctx->n_outgrown = 0;
+    ctx->adapt_ws = nullptr; ctx->adapt_ws_bytes = 0;
     ctx->host_scalars = nullptr; ctx->host_flag = nullptr;
     ctx->lanes_ready = false; ctx->join_pending = false; ctx->cand = nullptr; ctx->cand_bytes = 0;
     for (int i = 0; i < kLanes; ++i) ctx->lane_graph_ok[i] = false;
@@ -453,7 +453,7 @@ gelo_status gelo_destroy(gelo_ctx* ctx) {
     if (ctx->project_ws) (void)hipFree(ctx->project_ws);
     if (ctx->attention_ws) (void)hipFree(ctx->attention_ws);
     if (ctx->adapt_ws) (void)hipFree(ctx->adapt_ws);
-    for (int i = 0; i < ctx->n_outgrown; ++i) (void)hipFree(ctx->outgrown[i]);
+    for (void* p : ctx->outgrown) (void)hipFree(p);
     if (ctx->host_scalars) (void)hipHostFree(ctx->host_scalars);
     delete ctx;
     return GELO_OK;
@@ -1645,15 +1645,21 @@ static gelo_status check_attention(gelo_ctx* ctx, gelo_dtype dtype, int n_q_head
     return GELO_OK;
 }
 
-// As grow, but what is outgrown stays until the context ends: a captured call has its address.
+// As grow, but what is outgrown stays until the context ends: a captured call has its address.  Twice as much as there was, so that little is left lying, or what is needed where
+// the device does not have that.
 static gelo_status grow_kept(gelo_ctx* ctx, void** buf, size_t* have, size_t need) {
     if (*have >= need) return GELO_OK;
-    if (need < 2 * *have) need = 2 * *have;
+    try {
+        ctx->outgrown.reserve(ctx->outgrown.size() + 1);
+    } catch (const std::bad_alloc&) {
+        return fail(ctx, GELO_ENOMEM, "no host memory");
+    }
     void* larger = nullptr;
     size_t bytes = 0;
-    const gelo_status st = grow(ctx, &larger, &bytes, need);
+    gelo_status st = grow(ctx, &larger, &bytes, need < 2 * *have ? 2 * *have : need);
+    if (st == GELO_ENOMEM && need < 2 * *have) st = grow(ctx, &larger, &bytes, need);
     if (st != GELO_OK) return st;
-    if (*buf) ctx->outgrown[ctx->n_outgrown++] = *buf;       // (two workspaces of 256 bytes at least: no device has what 40 doublings of either make)
+    if (*buf) ctx->outgrown.push_back(*buf);
     *buf = larger;
     *have = bytes;
     return GELO_OK;
