@@ -554,6 +554,7 @@ void adapt_many_up_kernel(AdaptArgs a) {
     typedef typename L::piece_t piece_t;
     constexpr int PER = L::PER, HT = kUpRows / 16, TWICE = sizeof(T) == 2 ? 2 : 1, THREADS = 64 * kWaves;
     constexpr int VEC = 16 / sizeof(T), TO_ROW = kUpCols / VEC, VECS = kUpRows * TO_ROW / THREADS;         // 16 bytes of a row to a thread
+    static_assert(4 * PER * (HALF / 2) < kMostRank, "no rank has so many steps");
     const Adapt& o = a.o;
     __shared__ piece_t z[TWICE * HALF][HT][64];
     __shared__ __attribute__((aligned(16))) float sums[kUpRows][kUpCols + 4];
@@ -751,7 +752,7 @@ hipError_t launch(const Adapt& o, hipStream_t stream) {
         if (half <= 1) hipLaunchKernelGGL((adapt_many_up_kernel<T, 1>), up, dim3(64 * kWaves), 0, stream, a);
         else if (half <= 2) hipLaunchKernelGGL((adapt_many_up_kernel<T, 2>), up, dim3(64 * kWaves), 0, stream, a);
         else if (half <= 4) hipLaunchKernelGGL((adapt_many_up_kernel<T, 4>), up, dim3(64 * kWaves), 0, stream, a);
-        else hipLaunchKernelGGL((adapt_many_up_kernel<T, 8>), up, dim3(64 * kWaves), 0, stream, a);
+        else if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((adapt_many_up_kernel<T, 8>), up, dim3(64 * kWaves), 0, stream, a);
         return hipGetLastError();
     }
     const int tiles = (o.n + 15) / 16;
