@@ -349,9 +349,10 @@ gelo_status gelo_reserve_attention(gelo_ctx* ctx, int head_dim);
 
 /* ---------------------------------------------------------------------------------------------------------------
  * A paged cache of 4 bits: a block of 32 values of a head's row is held as codes - a sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 -
- * times 2^e, e the least whole number from -110 to 125 with max |value| <= 7 2^e, each to nearest, ties to the even code: no value is off by more than
- * 2^e, a seventh of the block's largest at least and two sevenths at most.  A block with a NaN or an infinity is NaN as a whole.  17/32 of a byte to
- * a value: 2.1 GB of keys and values of bfloat16 are 0.57 GB.
+ * times 2^e, e the least whole number from -110 to 125 with max |value| <= 7 2^e (125 if none is), each to nearest, ties to the even code.  No value is off by more than
+ * 2^e, a seventh of the block's largest at least and below two sevenths of it, but at the ends: what lies beyond 7 2^125 (3.0e38) becomes 6 2^125, and a block whose largest is
+ * 3.5 2^-110 (2.7e-33) or less has 2^-110 all the same, so that no value is off by more than 2^-111 and those of 2^-112 and less are zeros.
+ * A block with a NaN or an infinity is NaN as a whole.  17/32 of a byte to a value: 2.1 GB of keys and values of bfloat16 are 0.57 GB.
  *
  * gelo_kv_cache_fp4: K and V are arrays of n_pages pages; head h of page g is a piece of gelo_fp4_page_bytes(page_rows, head_dim) bytes from byte
  * g page_stride + h head_stride of either (strides in bytes, multiples of 16, of pages below 2^31).  page_rows is a power of two from 16 on, head_dim a multiple of 32, their

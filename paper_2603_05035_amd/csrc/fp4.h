@@ -36,7 +36,7 @@ __device__ __forceinline__ float odd_float(double v) {
 }
 
 // Scale byte of a block whose largest |value| is `top`: the least 2^e with top <= 7 2^e, so that no value is off by more than 2^e, half of the largest
-// step; e from -110 on (products of such values stay normal floats) to 125 (6 2^125 is one).
+// step; e from -110 on (products of such values stay normal floats; smaller blocks are off by 2^-111 at most) to 125 (6 2^125 is one; larger values become it).
 __device__ __forceinline__ uint32_t fp4_scale_byte(float top) {
     const uint32_t u = __float_as_uint(top);
     const int e = (int)(u >> 23) - 127 - ((u & 0x7FFFFFu) > 0x600000u ? 1 : 2);

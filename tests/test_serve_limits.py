@@ -2,9 +2,11 @@
 import subprocess
 import sys
 
+import numpy as np
 import pytest
 import torch
 
+from oracle import serve_oracle as so
 from paper_2603_05035_amd import binding as g
 
 ROWS = """
@@ -66,3 +68,26 @@ def test_a_cache_of_values_is_not_one_of_4_bits(call, monkeypatch):
             run(cache)
     with pytest.raises(AssertionError):                      # the right kind does
         run(codes)
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_how_far_a_value_of_4_bits_is_off(seed):
+    """As include/gelo.h says it, at the ends of the scales too (the kernels' codes are compared with the oracle's to the bit where there is a GPU)."""
+    rng = np.random.default_rng(seed)
+    most, least = 7 * 2.0 ** 125, 3.5 * 2.0 ** -110
+    tops = np.concatenate((most * np.array([1 - 2.0 ** -20, 1.0, 1 + 2.0 ** -20, 8 / 7, 1.6]), least * np.array([2.0, 1 + 2.0 ** -20, 1.0, 0.6, 0.1, 0.05, 1e-4]),
+                           10.0 ** rng.uniform(-32, 38, 40)))
+    x = rng.uniform(-1, 1, (len(tops), 32))
+    x[:, 7] = 1
+    x = x / np.abs(x).max(1, keepdims=True) * tops[:, None]
+    codes, scales = so.hold(x)
+    off, step = np.abs(so.held(codes, scales) - x), 2.0 ** (scales[:, 0] - 127.0)
+    inside = np.abs(x) <= most
+    assert (off <= step[:, None])[inside].all() and (np.abs(so.held(codes, scales))[~inside] == 6 * 2.0 ** 125).all() and not inside.all()
+    usual = (tops > least) & (tops <= most)
+    assert (step[usual] >= tops[usual] / 7 * (1 - 2.0 ** -50)).all() and (step[usual] < tops[usual] * 2 / 7).all()
+    small = tops <= least
+    assert small.sum() == 5 and (step[small] == 2.0 ** -110).all() and (off[small] <= 2.0 ** -111).all()
+    assert (so.held(codes, scales)[np.abs(x) <= 2.0 ** -112] == 0).all()
+    # (at the ends a value can be off by more than the step, and the step be more than two sevenths)
+    assert (off[3:5] > step[3:5, None]).any(1).all() and (step[8:12] > tops[8:12] * 2 / 7).all()
