@@ -409,7 +409,10 @@ typedef struct gelo_adapters {
 /* Z[i, j] = base[i, j] + scale[w] sum_r (sum_k H[i, k] A_w[r, k]) B_w[j, r], r over the rank rows of j's part, w = which[i] (DEVICE, n 32-bit
  * integers).  A row whose number is no adapter's (-1, say) gets base[i].  H: n x d (ldh), base, Z: n x p (ldb, ldz) of type `dtype`; Z may be base itself, and
  * shares no memory with H or with base otherwise.  Sums are float, one rounding at the end; GELO_BF16 may hold the inner sum in 16 bits for the second product.  A
- * NaN or infinity in H, base or an adapter reaches only the rows it belongs to.  Rows in any order.
+ * NaN or infinity in H, base or an adapter reaches only the rows it belongs to.  Rows in any order.  A row's bits do not go by the other rows; they may go by the sizes of the call, n and
+ * n_adapters among them.  Calls of many rows put those that share one of the n_adapters together, which takes longer the more there are, and from 12288 on do not: each row
+ * then reads its adapter for itself (4096 rows of 4096 -> 12288 columns that share eight of rank 16, us: 51 where n_adapters is 8, 60 at 64, 153 at 12287, 326 at 12288).  Where many are kept
+ * it pays to describe the range of them that a batch of prompts uses.
  * The inner sums go through float workspace of the context (gelo_reserve_adapt sizes it ahead; else the first call that needs more allocates, and what it replaces stays
  * until the context ends): calls on one context must not overlap in time on different streams. */
 gelo_status gelo_adapt(gelo_ctx* ctx, gelo_dtype dtype, int n, int d, int p, const void* H, int64_t ldh, const gelo_adapters* adapters, const int32_t* which,

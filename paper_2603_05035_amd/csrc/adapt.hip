@@ -6,7 +6,8 @@
 //   few rows   two launches.  The first takes tiles of 16 rows as they come; a tile's adapters go side by side, rows of others count as zeros and their results are
 //              dropped.  The second takes row by row; of small rows it does both.
 //   many rows  three: the first puts the rows of an adapter together, 64 to a group (rows that are so already stay in runs); then a tile is a group.
-// A row's sums do not go by the rows around it: each is a column of a matrix instruction.
+// A row's sums do not go by what the rows around it hold or which adapters they have: each is a column of a matrix instruction.  The order of its sums, and whether T is two bfloat16, go by
+// the sizes of the call (plan_of), how many rows and adapters it has among them.
 //
 // bfloat16 takes v_mfma_f32_16x16x32_bf16, and (many rows) the float T of the second product as two bfloat16, 16 bits of it: with one, its rounding would show where what the
 // adapter adds is as large as base.  float takes v_mfma_f32_16x16x4_f32.
@@ -689,6 +690,9 @@ int steps_of(int is_bf16, int d) { return (d + (is_bf16 ? 31 : 15)) / (is_bf16 ?
 // Rows by themselves read their adapters at 7.5 TB/s, from L2 for the most part; groups take three launches and their trips, 10 us more, and read an adapter once for 64
 // rows.  4096 -> 12288 columns, rank 16, one adapter, us by rows and by groups: 64 rows 10.9 and 16.2, 96 (75 MB) 16.5 and 16.4, 128 18.2 and 16.4, 256 28.2 and 17.4; 4096 ->
 // 4096, rank 128, 64 rows (134 MB) 22.4 and 20.9; 1024 -> 1024, rank 8, 1024 rows (34 MB) 10.9 and 19.3.
+// All this goes by how many adapters are described: which of them a batch uses, and in what order, is on the GPU.  The more there are, the more groups there could be, whose workgroups start
+// to find nothing, and the counts fit no more than kMostBins: 4096 rows in runs of eight adapters, 4096 -> 12288 columns, rank 16, one set of inputs again and again, 51 us where 8 are described, 60 with
+// 9 or 64, 153 with 12287, 326 with 12288, where every row reads its own.
 constexpr double kRowsRead = 80e6, kOrderedRead = 110e6;
 // Putting rows in order is a launch of 4 to 6 us, and what follows finds its rows a trip later.  Without it a group's adapters follow each other, each a trip to its B and so many more
 // instructions.  4096 -> 12288 columns, rank 16, us in order and as they come: 1024 rows of eight adapters in any order 29 and 44, of four 31 as they come; 4096 rows of eight in any
