@@ -406,6 +406,12 @@ Plan plan_few(const Attention& o, int64_t columns, int is_bf16, double* us) {
     const int64_t cuts = fine >= 4 && fine > fill ? fine : fill;
     cut(&p, o.batch.max_kv_len, cuts < 1 ? 1 : cuts < most ? cuts : most);
     p.workgroups = tiles * p.n_chunks;
+    // A head to a wave needs no join, but a wave walks its cache alone: where one round of such workgroups fills the chip.  us with a cache shared out and by head, bfloat16, caches of 85 to 100% of 64,
+    // 512, 2000 and 4000 keys:
+    //   32 heads of 128   48 sequences 12.3, 25.0, 74, 139 and 7.8, 26.4, 83, 160;  56 15.1, 28.2, 87, 156 and 7.7, 26.8, 90, 163;  63 16.2, 31.2, 96, 178 and 7.9, 28.0, 95, 179
+    //                     64 16.2, 31.9, 96, 178 and 8.2, 28.5, 93, 180;  72 19.1, 36.5, 110, 201 and 11.4, 40.9, 133, 251;  96 23.9, 46.9, 145, 261 and 11.7, 42.8, 146, 270
+    //   16 heads of 64    128 sequences 10.2, 21.2, 64, 116 and 6.5, 20.6, 73, 138
+    // So it is right for short caches on both sides of the border, and takes up to a quarter more where caches are long and the last round nearly empty, or heads narrow: the rule looks at neither.
     p.by_head = (is_bf16 || o.cache.head_dim < 128) && p.n_chunks == 1 && p.col_tiles == 1 && o.cache.n_kv_heads % kFewWaves == 0 && tiles / kFewWaves >= kFewTarget;
     if (p.by_head) p.workgroups = tiles / kFewWaves;
     p.past = p.col_tiles == 1 && 17.0 / 16 * tiles * o.batch.max_kv_len * o.cache.head_dim > 100e6;

@@ -20,6 +20,8 @@ __device__ __forceinline__ float add_pair(uint32_t pair, float sum) {
 // of O^T, if A = V^T takes its keys in that order - two transposing reads of four rows each.
 // A wave works on three groups of 32 keys at once, whose instructions depend on nothing of each other: the scores of the next group and the
 // weighted sum of the last one (matrix pipe) beside the weights of the present one (vector pipe).
+// Weights are rounded to bfloat16 for the product with V, and their sum is that of the rounded ones: what a rounding leaves would be half as many matrix instructions more, and they are what prompts
+// wait for.  Distance from 64 bits, relative in the Frobenius norm: 8 x 301-512 rows 0.0021, 6000 behind 2000 0.0023; of these the rounding of the result is 0.0016 to 0.0017.
 // 6000 rows behind 2000, 32/8 heads of 128: 472 us on one chip, 477 to 490 on others = 1.00 to 1.04 PFLOP/s, at 1.83 GHz under the power limit; a library's product
 // of 8192^3 reaches 1.24.  Of 507 us (an earlier step) the fetches were 73, maximum and masks 114, the reads of LDS 159, each taken out alone.
 // 8 prompts of 301 to 512 rows, 32 heads of 128: 38 to 43 us = 0.26 PFLOP/s of what causal rows see: 12 us for one row of keys, and tiles that end early.

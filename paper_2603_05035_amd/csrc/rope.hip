@@ -187,8 +187,8 @@ __device__ __forceinline__ int scale_at(int d, int page_shift, int in_page, int 
     return is_value ? first + (in_page >> 2) * 4 * per + 4 * block + (in_page & 3) : first + in_page * per + block;
 }
 
-// A workgroup takes a row of QKV, or a share of its items (grid y), or a few rows.  Bound by the trips before a row's first store - sequence, length, page, angles - and the
-// products in double: 3126 rows of 32/8 heads of 128 17.8 us, 67 MB at 3.8 TB/s; 64 rows of 32/32 4.1.  Keys and values go by items of 8 components, four lanes to a block: each of them loads the components that its own turn
+// A workgroup takes a row of QKV, or a share of its items (grid y), or a few rows.  Bound by the trips before a row's first store, one behind the other - sequence, length, page, angles:
+// 3126 rows of 32/8 heads of 128 17.8 us, 67 MB at 3.8 TB/s; 64 rows of 32/32 4.1.  Where nothing turns the 3126 take 15.0 us, in pairs 16.6, in halves 16.8 to 17.7 (a call after the other).  Keys and values go by items of 8 components, four lanes to a block: each of them loads the components that its own turn
 // with, too, so that any rot / 2 will do.  A turned key is worked out in double, where the two products are exact and their sum as good as, and its code is
 // that value's: in float one in some millions would fall on the other side of the middle between two codes.  Queries turn as in rope_append_kernel, to the bit.
 template <class T>
